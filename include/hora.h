@@ -385,6 +385,110 @@ hora_status_t hora_token_broadcast(const float *adv, const int64_t *token_offset
                                    float *token_adv, void *stream);
 
 /*
+ * ---------------------------------------------------------------------------------------------------------------
+ * The decode step of a batch of rollout groups.  hora_allocate says how many rollouts each prompt gets; the calls
+ * below generate them together: every rollout of a group attends to its prompt's cache, kept once for the group, and
+ * to its own.  group_offsets is hora_allocate's output, used where it lies.  Order of a step, per layer:
+ *   hora_kv_write (the new tokens' keys and values) -> hora_group_attention;  after the last layer: hora_verify_drafts.
+ */
+
+/* Element types of the calls below. */
+enum { HORA_DTYPE_F32 = 0, HORA_DTYPE_BF16 = 1, HORA_DTYPE_F16 = 2, HORA_DTYPE_E4M3 = 3 };
+
+/*
+ * The paged cache.  Keys and values lie in two pools of n_pages pages; a page holds page_size tokens (16, 32, 64 or
+ * 128) for every one of H heads, one head's tokens next to each other:
+ *   k_cache, v_cache   [n_pages, H, page_size, D]   BF16, F16 or E4M3, 16-byte aligned;  D = 64 or 128
+ *   k_exp, v_exp       [n_pages, H, page_size]      uint8, E4M3 only (2-byte aligned), else NULL
+ * An E4M3 row (one token, one head) has one power-of-two scale, stored as its biased exponent: the row's values are
+ * code * 2^(exp - 127).  A slot is page * page_size + (place in the page).
+ *
+ * hora_kv_write — store n_tokens new rows of keys and values in the cache, rounding or quantising them on the way.
+ *   k, v        row t, head h at k + t * in_row_stride + h * D (elements): F32, BF16 or F16; 16-byte aligned, and
+ *               in_row_stride >= H * D with in_row_stride * element size a multiple of 16 (a slice of a fused projection will do)
+ *   slots       [n_tokens] int64: where each token goes; negative: the token is not stored
+ *               (a 16-bit cache rounds other types to nearest even)
+ * E4M3: with a = max |x| over the row's finite values, exp - 127 = the least e >= -126 with a / 2^e <= 448 (0 for a row
+ * without a finite value other than zero); code = x / 2^e rounded to nearest even, +-infinity as +-448, NaN as NaN.  x / 2^e is exact, so
+ * one rounding is all the error there is and the codes do not depend on how they were computed.
+ * A slot beyond the cache raises INVALID_VALUE in status_dev (optional) and is skipped.  A slot given twice holds either.
+ *
+ * hora_kv_read — the other way: row t of k, v (out_dtype F32, BF16 or F16) is the content of slots[t]; zeros where
+ * slots[t] is negative or beyond the cache (the latter raises INVALID_VALUE).  Rows as for hora_kv_write.
+ */
+hora_status_t hora_kv_write(const void *k, const void *v, int32_t in_dtype, int64_t in_row_stride, const int64_t *slots,
+                            int64_t n_tokens, int32_t H, int32_t D, void *k_cache, void *v_cache, uint8_t *k_exp,
+                            uint8_t *v_exp, int32_t cache_dtype, int64_t n_pages, int32_t page_size,
+                            int32_t *status_dev, void *stream);
+
+hora_status_t hora_kv_read(const void *k_cache, const void *v_cache, const uint8_t *k_exp, const uint8_t *v_exp,
+                           int32_t cache_dtype, int64_t n_pages, int32_t page_size, const int64_t *slots, int64_t n_tokens,
+                           int32_t H, int32_t D, void *k, void *v, int32_t out_dtype, int64_t out_row_stride,
+                           int32_t *status_dev, void *stream);
+
+/*
+ * hora_group_attention — attention of R rollouts in N groups, T query slots each, over a cache whose prompt part is
+ * shared by the group.  Rollout r of group i (group_offsets[i] <= r < group_offsets[i+1]) has the keys and values
+ *   prompt:  tokens 0 .. prefix_len[i]-1 of page list prefix_pages[i]      seen by all of its queries
+ *   its own: tokens 0 .. suffix_len[r]-1 of page list suffix_pages[r]      the queries are the last q_len[r] of them
+ * Query t < q_len[r] sees its own tokens 0 .. suffix_len[r]-q_len[r]+t (none if that is negative).  For each head
+ *   s_j = sm_scale * q . k_j,   out = sum_j e^(s_j) v_j / sum_j e^(s_j),   lse = log sum_j e^(s_j)
+ * over the keys it sees; out = 0 and lse = -infinity where there are none, for slots t >= q_len[r], and for rollouts at
+ * or beyond group_offsets[N].  Every prompt's cache is read once for its whole group, whatever the group's size.
+ * Scores, maxima, sums and outputs are held in fp32; the weights are rounded to the 16-bit type of the product they enter.
+ *
+ *   q            (r, t) at q + (r*T + t) * q_row_stride (elements), heads next to each other: [Hq, D], BF16 or F16,
+ *                16-byte aligned, q_row_stride >= Hq * D and a multiple of 8.  Query head h reads cache head h / (Hq/Hkv).
+ *   q_len        [R] int32 in [0, T], or NULL for T everywhere
+ *   cache        as above, of q's type or E4M3.  Cached rows within the lengths have to be finite (a row that only some
+ *                queries of its rollout see included); what lies beyond the lengths, in a page's unused slots too, has no effect.
+ *   prefix_pages [N, prefix_ld] int32, prefix_len [N] int32 in [0, prefix_ld * page_size];  suffix_* alike, [R, suffix_ld], [R]
+ *   out          like q, out_row_stride;  lse [R, T, Hq] fp32 or NULL
+ *   workspace    hora_group_attention_workspace_bytes(...) bytes, 256-byte aligned, contents undefined on entry and exit
+ *   status_dev   optional: INVALID_VALUE for decreasing or too large offsets, lengths or q_len out of range, and page
+ *                numbers out of range.  Such values are clamped: outputs they touch are wrong, nothing else is read or written.
+ * Limits: T * Hq / Hkv <= 4096, R * T * Hq < 2^31, N >= 1 when R > 0.
+ */
+size_t hora_group_attention_workspace_bytes(int64_t N, int64_t R, int32_t T, int32_t Hq, int32_t Hkv, int32_t D);
+
+hora_status_t hora_group_attention(const void *q, int32_t q_dtype, int64_t q_row_stride, const int64_t *group_offsets,
+                                   int64_t N, int64_t R, int32_t T, const int32_t *q_len, int32_t Hq, int32_t Hkv,
+                                   int32_t D, float sm_scale, const void *k_cache, const void *v_cache,
+                                   const uint8_t *k_exp, const uint8_t *v_exp, int32_t cache_dtype, int64_t n_pages,
+                                   int32_t page_size, const int32_t *prefix_pages, int32_t prefix_ld,
+                                   const int32_t *prefix_len, const int32_t *suffix_pages, int32_t suffix_ld,
+                                   const int32_t *suffix_len, void *out, int64_t out_row_stride, float *lse,
+                                   int32_t *status_dev, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * hora_verify_drafts — which of K drafted tokens the target distribution accepts, and the token that follows them
+ * (speculative sampling: the tokens returned are distributed as the target's own samples).
+ *
+ * Rollout r drafted tokens x_0 .. x_(L-1), L = draft_len[r]; p_t is the target's distribution after the first t of them,
+ * q_t the one x_t was drawn from.  n_accepted[r] is the number of drafts before the first with  u_accept[r,t] * q_t(x_t) >= p_t(x_t)
+ * (the product taken exactly).  One more token is drawn: from the weights
+ *   w_v = max(P_v - Q_v, 0)   of the refused position t = n_accepted (from P if all w are zero),
+ *   w_v = P_v                 of position t = L when nothing was refused,
+ * where P_v, Q_v are p, q (clamped to [0, 1], NaN as 0) rounded down to multiples of 2^-38: the token is the first v with
+ *   w_0 + .. + w_v > floor(U * sum w),  U = u_sample[r] rounded down to a multiple of 2^-24.
+ * The sums are exact integers, so the tokens do not depend on the order of summation.  tokens[r] = the accepted
+ * drafts, the drawn token, then -1.  K = 0 draws one token from the target.
+ *
+ *   target        row (r, t) at target + (r*(K+1) + t) * target_row_stride (elements), V values: F32, BF16 or F16
+ *   draft         row (r, t) at draft + (r*K + t) * draft_row_stride, same type; NULL: drafts without probabilities
+ *                 (looked up, not sampled): q_t is 1 at x_t and 0 elsewhere
+ *   draft_tokens  [R, K] int32;  draft_len [R] int32 in [0, K] or NULL for K;  u_accept [R, K], u_sample [R] fp32 in [0, 1)
+ *   n_accepted    [R] int32 out;  tokens [R, K+1] int32 out
+ *   status_dev    optional: INVALID_VALUE for a drafted token outside [0, V) (refused), draft_len out of range (clamped), a
+ *                 negative or NaN value in a row that is read, or a row without any weight (the drawn token is then -1)
+ * Limits: 0 <= K <= 255, 1 <= V <= 2^22.  Rows on 16-byte boundaries are read with 16-byte loads throughout.
+ */
+hora_status_t hora_verify_drafts(const void *target, int32_t dtype, int64_t target_row_stride, const void *draft,
+                                 int64_t draft_row_stride, const int32_t *draft_tokens, const int32_t *draft_len,
+                                 int64_t R, int32_t K, int32_t V, const float *u_accept, const float *u_sample,
+                                 int32_t *n_accepted, int32_t *tokens, int32_t *status_dev, void *stream);
+
+/*
  * hora_allocate_profile_events — measurement aid, no counterpart in the paper.  With two non-NULL cudaEvent_t
  * handles (created by the caller with timing enabled), every following hora_allocate / hora_allocate_static
  * call records `start_event` just before and `stop_event` just after the launch of its full-read selection

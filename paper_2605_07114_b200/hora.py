@@ -25,6 +25,8 @@ FLAG_HARD_FIRST = 8
 FLAG_SHARED_INT_PRIOR = 4            # the same flag under the name of its first use
 ADV_GRPO, ADV_RLOO = 0, 1
 WEIGHT_PER_TOKEN, WEIGHT_CONST_LENGTH = 0, 1
+DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_E4M3 = range(4)
+_DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.float8_e4m3fn: DTYPE_E4M3}
 
 EXPORTS = ("hora_gains", "hora_allocate_workspace_bytes", "hora_allocate", "hora_group_advantage",
            "hora_token_broadcast", "hora_status_string", "hora_version", "hora_launch_count",
@@ -32,7 +34,8 @@ EXPORTS = ("hora_gains", "hora_allocate_workspace_bytes", "hora_allocate", "hora
            "hora_allocate_batched", "hora_allocate_batched_workspace_bytes", "hora_rollout_weights",
            "hora_learned_prior", "hora_beta_binomial_nll", "hora_pass_at_k", "hora_pass_at_k_workspace_bytes",
            "hora_group_advantage_tokens", "hora_allocation_share", "hora_allocate_hard_first",
-           "hora_allocate_hard_first_workspace_bytes", "hora_fp64_probe", "hora_checked_violation")
+           "hora_allocate_hard_first_workspace_bytes", "hora_fp64_probe", "hora_checked_violation", "hora_kv_write",
+           "hora_kv_read", "hora_group_attention", "hora_group_attention_workspace_bytes", "hora_verify_drafts")
 
 
 class HoraError(RuntimeError):
@@ -111,6 +114,17 @@ def load() -> C.CDLL:
     L.hora_rollout_weights.restype = C.c_int
     L.hora_token_broadcast.argtypes = [p, p, i64, i64, p, p]
     L.hora_token_broadcast.restype = C.c_int
+    L.hora_kv_write.argtypes = [p, p, i32, i64, p, i64, i32, i32, p, p, p, p, i32, i64, i32, p, p]
+    L.hora_kv_write.restype = C.c_int
+    L.hora_kv_read.argtypes = [p, p, p, p, i32, i64, i32, p, i64, i32, i32, p, p, i32, i64, p, p]
+    L.hora_kv_read.restype = C.c_int
+    L.hora_group_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
+    L.hora_group_attention_workspace_bytes.restype = C.c_size_t
+    L.hora_group_attention.argtypes = [p, i32, i64, p, i64, i64, i32, p, i32, i32, i32, C.c_float, p, p, p, p, i32, i64,
+                                       i32, p, i32, p, p, i32, p, p, i64, p, p, p, C.c_size_t, p]
+    L.hora_group_attention.restype = C.c_int
+    L.hora_verify_drafts.argtypes = [p, i32, i64, p, i64, p, p, i64, i32, i32, p, p, p, p, p, p]
+    L.hora_verify_drafts.restype = C.c_int
     L.hora_checked_violation.restype = C.c_int32
     L.hora_fp64_probe.argtypes = [i32, p, p]
     L.hora_fp64_probe.restype = C.c_uint64
@@ -339,6 +353,196 @@ def hora_token_broadcast(adv, token_offsets, R, T, token_adv):
     rc = load().hora_token_broadcast(_ptr(adv, torch.float32, "adv"), _ptr(token_offsets, torch.int64, "token_offsets"),
                                      R, T, _ptr(token_adv, torch.float32, "token_adv"), _stream())
     _check(rc, "hora_token_broadcast")
+
+
+# ------------------------------------------------------------------------------------------------
+# The decode step of rollout groups.  These calls run once per layer and token, so their marshalling is kept short:
+# shapes are read from the tensors, pointers are passed as plain integers.
+def _at(t: Optional[torch.Tensor], dtype, name: str, numel: Optional[int] = None) -> Optional[int]:
+    if t is None:
+        return None
+    if not t.is_cuda or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor of {dtype}, got {t.dtype} on {t.device}")
+    if numel is not None and t.numel() < numel:
+        raise ValueError(f"{name} must hold {numel} values, got {t.numel()}")
+    return t.data_ptr()
+
+
+def _row_stride(t: torch.Tensor, lead: int, inner, name: str) -> int:
+    """Distance (elements) between the rows of t: the first `lead` dimensions count rows at one distance from each
+    other, each row holds `inner` values next to each other."""
+    shape, stride = t.shape, t.stride()
+    if not t.is_cuda or tuple(shape[lead:]) != tuple(inner):
+        raise ValueError(f"{name} must be a CUDA tensor with {lead} leading dimensions and rows of {tuple(inner)}, got {tuple(shape)}")
+    want = 1
+    for d in range(len(shape) - 1, lead - 1, -1):
+        if shape[d] != 1 and stride[d] != want:
+            raise ValueError(f"{name}: the values of a row must lie next to each other")
+        want *= shape[d]
+    step, count = None, 1
+    for d in range(lead - 1, -1, -1):
+        if shape[d] > 1:
+            if step is None:
+                step = stride[d] // count if stride[d] % count == 0 else -1
+            if stride[d] != step * count:
+                raise ValueError(f"{name}: rows must lie at one distance from each other")
+        count *= shape[d]
+    return max(want, 1) if step is None else step
+
+
+def _raw_stream(t: torch.Tensor) -> int:
+    return torch._C._cuda_getCurrentRawStream(t.get_device())    # current_stream().cuda_stream, without building a Stream
+
+
+def _dtype_code(t: torch.Tensor, name: str) -> int:
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: unsupported dtype {t.dtype}")
+    return code
+
+
+def _kv_rows(k: torch.Tensor, v: torch.Tensor, n: int, H: int, D: int):
+    if k.dtype != v.dtype or k.shape[0] != n or v.shape[0] != n:
+        raise ValueError("k and v must have one type and one row for each slot")
+    stride = _row_stride(k, 1, (H, D), "k")
+    other = _row_stride(v, 1, (H, D), "v")
+    if n > 1 and stride != other:
+        raise ValueError("k and v must have the same row stride")
+    return stride
+
+
+def hora_kv_write(k, v, slots, k_cache, v_cache, k_exp=None, v_exp=None, status_dev=None):
+    """k, v [n, H, D] (rows may be strided) into the pools [n_pages, H, page_size, D] at slots [n] int64."""
+    n_pages, H, page, D = k_cache.shape
+    n = slots.shape[0]
+    stride = _kv_rows(k, v, n, H, D)
+    ct = k_cache.dtype
+    ne = n_pages * H * page
+    rc = load().hora_kv_write(k.data_ptr(), v.data_ptr(), _dtype_code(k, "k"), stride, _at(slots, torch.int64, "slots"), n, H, D,
+                              _at(k_cache, ct, "k_cache"), _at(v_cache, ct, "v_cache", ne * D), _at(k_exp, torch.uint8, "k_exp", ne),
+                              _at(v_exp, torch.uint8, "v_exp", ne), _dtype_code(k_cache, "k_cache"), n_pages, page,
+                              _at(status_dev, torch.int32, "status_dev"), _raw_stream(k))
+    _check(rc, "hora_kv_write")
+
+
+def hora_kv_read(k_cache, v_cache, k_exp, v_exp, slots, k, v, status_dev=None):
+    """The rows at slots [n] int64 of the pools into k, v [n, H, D] (rows may be strided)."""
+    n_pages, H, page, D = k_cache.shape
+    n = slots.shape[0]
+    stride = _kv_rows(k, v, n, H, D)
+    ct = k_cache.dtype
+    ne = n_pages * H * page
+    rc = load().hora_kv_read(_at(k_cache, ct, "k_cache"), _at(v_cache, ct, "v_cache", ne * D), _at(k_exp, torch.uint8, "k_exp", ne),
+                             _at(v_exp, torch.uint8, "v_exp", ne), _dtype_code(k_cache, "k_cache"), n_pages, page,
+                             _at(slots, torch.int64, "slots"), n, H, D, k.data_ptr(), v.data_ptr(), _dtype_code(k, "k"), stride,
+                             _at(status_dev, torch.int32, "status_dev"), _raw_stream(k))
+    _check(rc, "hora_kv_read")
+
+
+def hora_group_attention_workspace_bytes(N, R, T, Hq, Hkv, D) -> int:
+    return int(load().hora_group_attention_workspace_bytes(N, R, T, Hq, Hkv, D))
+
+
+def hora_group_attention(q, group_offsets, q_len, sm_scale, k_cache, v_cache, k_exp, v_exp, prefix_pages, prefix_len,
+                         suffix_pages, suffix_len, out, lse, workspace, status_dev=None):
+    """q, out [R, T, Hq, D] (rows (r, t) may be strided); the other shapes as in the header.  GroupAttention keeps the
+    buffers and the marshalled arguments between the calls of a decode loop."""
+    GroupAttention._bind(PagedCache.over(k_cache, v_cache, k_exp, v_exp), q.shape[2], q.shape[1], q.dtype, group_offsets, prefix_pages,
+                         prefix_len, suffix_pages, suffix_len, q_len, sm_scale, workspace, status_dev)(q, out, lse)
+
+
+def hora_verify_drafts(target, draft, draft_tokens, draft_len, R, K, V, u_accept, u_sample, n_accepted, tokens, status_dev=None):
+    """target [R, K+1, V], draft [R, K, V] or None: rows may be strided, of one type."""
+    if tuple(target.shape[:2]) != (R, K + 1):
+        raise ValueError(f"target must have the shape {(R, K + 1, V)}, got {tuple(target.shape)}")
+    ts, ds = _row_stride(target, 2, (V,), "target"), 0
+    if draft is not None:
+        if draft.dtype != target.dtype or tuple(draft.shape[:2]) != (R, K):
+            raise ValueError(f"draft must have the shape {(R, K, V)} and the target's type")
+        ds = _row_stride(draft, 2, (V,), "draft")
+    rc = load().hora_verify_drafts(target.data_ptr(), _dtype_code(target, "target"), ts, None if draft is None else draft.data_ptr(), ds,
+                                   _at(draft_tokens, torch.int32, "draft_tokens", R * K), _at(draft_len, torch.int32, "draft_len", R), R, K, V,
+                                   _at(u_accept, torch.float32, "u_accept", R * K), _at(u_sample, torch.float32, "u_sample", R),
+                                   _at(n_accepted, torch.int32, "n_accepted", R), _at(tokens, torch.int32, "tokens", R * (K + 1)),
+                                   _at(status_dev, torch.int32, "status_dev"), _raw_stream(target))
+    _check(rc, "hora_verify_drafts")
+
+
+class PagedCache:
+    """The two pools of a paged cache (and their scale bytes, e4m3 only) with the calls that fill and read them."""
+
+    def __init__(self, k, v, k_exp=None, v_exp=None):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("the pools must be of one shape [n_pages, H, page_size, D] and one type")
+        if (k.dtype == torch.float8_e4m3fn) != (k_exp is not None and v_exp is not None):
+            raise ValueError("an e4m3 cache has scale bytes, the others have none")
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.n_pages, self.H, self.page_size, self.D = k.shape
+
+    @classmethod
+    def over(cls, *pools):
+        return cls(*pools)
+
+    @classmethod
+    def empty(cls, n_pages: int, page_size: int, H: int, D: int, dtype=torch.bfloat16, device="cuda"):
+        shape = (n_pages, H, page_size, D)
+        pools = [torch.empty(shape, dtype=dtype, device=device) for _ in range(2)]
+        if dtype == torch.float8_e4m3fn:
+            pools += [torch.full(shape[:3], 127, dtype=torch.uint8, device=device) for _ in range(2)]
+        return cls(*pools)
+
+    def write(self, k, v, slots, status_dev=None):
+        hora_kv_write(k, v, slots, self.k, self.v, self.k_exp, self.v_exp, status_dev)
+
+    def read(self, slots, k, v, status_dev=None):
+        hora_kv_read(self.k, self.v, self.k_exp, self.v_exp, slots, k, v, status_dev)
+
+
+class GroupAttention:
+    """hora_group_attention over buffers that stay where they are from step to step (the tables' and lengths' contents
+    may change): owns the workspace and the outputs, keeps the marshalled arguments."""
+
+    def __init__(self, cache: PagedCache, Hq: int, T: int, dtype, *, group_offsets, prefix_pages, prefix_len, suffix_pages, suffix_len,
+                 q_len=None, sm_scale: Optional[float] = None, status_dev=None):
+        N, R = prefix_len.shape[0], suffix_len.shape[0]
+        dev = cache.k.device
+        wb = hora_group_attention_workspace_bytes(N, R, T, Hq, cache.H, cache.D)
+        self.workspace = torch.empty(max(wb, 256), dtype=torch.uint8, device=dev)
+        self.out = torch.empty((R, T, Hq, cache.D), dtype=dtype, device=dev)
+        self.lse = torch.empty((R, T, Hq), dtype=torch.float32, device=dev)
+        self._call = self._bind(cache, Hq, T, dtype, group_offsets, prefix_pages, prefix_len, suffix_pages, suffix_len, q_len,
+                                cache.D ** -0.5 if sm_scale is None else sm_scale, self.workspace, status_dev)
+
+    @staticmethod
+    def _bind(cache, Hq, T, dtype, group_offsets, prefix_pages, prefix_len, suffix_pages, suffix_len, q_len, sm_scale, workspace, status_dev):
+        N, R = prefix_len.shape[0], suffix_len.shape[0]
+        i32, D, ne = torch.int32, cache.D, cache.n_pages * cache.H * cache.page_size
+        if prefix_pages.dim() != 2 or suffix_pages.dim() != 2 or prefix_pages.shape[0] != N or suffix_pages.shape[0] != R:
+            raise ValueError("the page tables must have one row for each prompt and each rollout")
+        if dtype not in _DTYPES:
+            raise ValueError(f"unsupported dtype {dtype}")
+        keep = (cache, group_offsets, prefix_pages, prefix_len, suffix_pages, suffix_len, q_len, workspace, status_dev)
+        middle = (_at(group_offsets, torch.int64, "group_offsets", N + 1), N, R, T, _at(q_len, i32, "q_len", R), Hq, cache.H, D, float(sm_scale),
+                  _at(cache.k, cache.k.dtype, "k_cache"), _at(cache.v, cache.k.dtype, "v_cache"), _at(cache.k_exp, torch.uint8, "k_exp", ne),
+                  _at(cache.v_exp, torch.uint8, "v_exp", ne), _DTYPES[cache.k.dtype], cache.n_pages, cache.page_size,
+                  _at(prefix_pages, i32, "prefix_pages"), prefix_pages.shape[1], _at(prefix_len, i32, "prefix_len"),
+                  _at(suffix_pages, i32, "suffix_pages"), suffix_pages.shape[1], _at(suffix_len, i32, "suffix_len"))
+        tail = (_at(status_dev, i32, "status_dev"), _at(workspace, torch.uint8, "workspace"), workspace.numel())
+        code, f, inner = _DTYPES[dtype], load().hora_group_attention, (Hq, D)
+
+        def call(q, out, lse, _keep=keep):
+            if q.dtype != dtype or out.dtype != dtype or tuple(q.shape[:2]) != (R, T) or tuple(out.shape[:2]) != (R, T):
+                raise ValueError(f"q and out must be {dtype} tensors of the shape {(R, T, Hq, D)}")
+            _check(f(q.data_ptr(), code, _row_stride(q, 2, inner, "q"), *middle, out.data_ptr(), _row_stride(out, 2, inner, "out"),
+                     _at(lse, torch.float32, "lse", R * T * Hq), *tail, _raw_stream(q)), "hora_group_attention")
+        return call
+
+    def run(self, q, out=None, lse=None):
+        """q [R, T, Hq, D]; returns (out, lse): the object's own buffers unless others are given."""
+        out = self.out if out is None else out
+        lse = self.lse if lse is None else lse
+        self._call(q, out, lse)
+        return out, lse
 
 
 # ------------------------------------------------------------------------------------------------
