@@ -399,7 +399,7 @@ enum { HORA_DTYPE_F32 = 0, HORA_DTYPE_BF16 = 1, HORA_DTYPE_F16 = 2, HORA_DTYPE_E
  * The paged cache.  Keys and values lie in two pools of n_pages pages; a page holds page_size tokens (16, 32, 64 or
  * 128) for every one of H heads, one head's tokens next to each other:
  *   k_cache, v_cache   [n_pages, H, page_size, D]   BF16, F16 or E4M3, 16-byte aligned;  D = 64 or 128
- *   k_exp, v_exp       [n_pages, H, page_size]      uint8, E4M3 only (2-byte aligned), else NULL
+ *   k_exp, v_exp       [n_pages, H, page_size]      uint8, 16-byte aligned, E4M3 only, else NULL
  * An E4M3 row (one token, one head) has one power-of-two scale, stored as its biased exponent: the row's values are
  * code * 2^(exp - 127).  A slot is page * page_size + (place in the page).
  *

@@ -91,7 +91,7 @@ attention_join_kernel(const AttnArgs a) {
     Joined<E> j;
     const int32_t grp = a.group_of[r];
     if (grp >= 0 && t < query_count(a, r)) {
-        const int64_t per = steps_per_cta(a);
+        const int64_t per = steps_per_stream(a);
         bool bad = false;
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
@@ -147,13 +147,13 @@ static size_t lay_out(AttnArgs &a, int32_t D, char *base) {
         return p;
     };
     const size_t rows = (size_t)a.R * a.T * a.Hq;
-    a.n_ctas = sm_count() * 3;
+    a.n_streams = sm_count() * kStreamsPerSm;
     a.start = reinterpret_cast<int64_t *>(take(((size_t)a.N + a.R + 1) * 8));
     a.group_of = reinterpret_cast<int32_t *>(take((size_t)a.R * 4));
     a.main_o = reinterpret_cast<float *>(take(rows * 2 * D * 4));
     a.main_ml = reinterpret_cast<float *>(take(rows * 2 * 2 * 4));
-    a.cont_o = reinterpret_cast<float *>(take((size_t)a.n_ctas * kTileRows * D * 4));
-    a.cont_ml = reinterpret_cast<float *>(take((size_t)a.n_ctas * kTileRows * 2 * 4));
+    a.cont_o = reinterpret_cast<float *>(take((size_t)a.n_streams * kTileRows * D * 4));
+    a.cont_ml = reinterpret_cast<float *>(take((size_t)a.n_streams * kTileRows * 2 * 4));
     return used;
 }
 

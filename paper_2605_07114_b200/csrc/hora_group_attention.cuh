@@ -3,13 +3,13 @@
 // The work is a list of N + R key sequences: the N prompts' (all queries of the group attend to them) and the R
 // rollouts' own.  A sequence has `rows` query rows for each cache head: (rollout, slot t, head of the cache head's
 // group), in that order.  A row tile of a sequence and one cache head is an item; an item's keys come in steps.  All steps
-// of all items, in order, form one line that is cut into equal pieces, one for each CTA, so every CTA reads about the same
-// number of bytes whatever the lengths are.  A piece's part of an item is a partial result (m, l, o): m the largest
-// score in units of log2, l = sum 2^(s - m), o = sum 2^(s - m) v.  Partials are joined at the end: m = max m_i,
-// l = sum l_i 2^(m_i - m), o = sum o_i 2^(m_i - m), out = o / l.
+// of all items, in order, form one line that is cut into equal pieces, one for each stream (a warp that runs by itself), so
+// every stream reads about the same number of bytes whatever the lengths are.  A piece's part of an item is a partial
+// result (m, l, o): m the largest score in units of log2, l = sum 2^(s - m), o = sum 2^(s - m) v.  Partials are joined at
+// the end: m = max m_i, l = sum l_i 2^(m_i - m), o = sum o_i 2^(m_i - m), out = o / l.
 //
 // Where a partial goes: the part of an item that begins the item has a place of its own for each output row; a part
-// that goes on with an item begun by an earlier CTA is the first thing its CTA does, so that one has a place for each CTA.
+// that goes on with an item begun by an earlier stream is the first thing its stream does, so that one has a place for each stream.
 #pragma once
 
 #include "hora_rows16.cuh"
@@ -17,7 +17,9 @@
 namespace hora {
 
 constexpr int kTileRows = 16;                            // query rows of an item
-constexpr int kStepKeys = 64;                            // keys of a step
+constexpr int kStepKeys = 16;                            // keys of a step
+constexpr int kStreamsPerSm = 12;                       // 168 registers a lane, 16 KiB of keys and values in flight each
+constexpr int kMinSteps = 4;                             // a stream shorter than this costs more to join than it saves
 
 struct AttnArgs {
     const void *q;
@@ -30,13 +32,13 @@ struct AttnArgs {
     int32_t *status;
     int64_t q_row_stride, out_row_stride, n_pages;
     int32_t N, R, T, Hq, Hkv, g, page_shift, prefix_ld, suffix_ld;
-    int32_t n_ctas;
+    int32_t n_streams;
     float scale_log2;                                    // sm_scale * log2(e)
     // workspace
     int64_t *start;                                      // [N + R + 1] first step of each sequence on the line
     int32_t *group_of;                                   // [R] group of each rollout, -1: none
     float *main_o, *main_ml;                             // [2][R * T * Hq][D], [..][2]: prompt part, own part
-    float *cont_o, *cont_ml;                             // [n_ctas][kTileRows][D], [..][2]
+    float *cont_o, *cont_ml;                             // [n_streams][kTileRows][D], [..][2]
 };
 
 // A sequence: its query rows per cache head, its keys, and how it is cut.
@@ -79,10 +81,10 @@ __device__ __forceinline__ Sequence sequence(const AttnArgs &a, int32_t i, bool 
     return s;
 }
 
-// Steps of the line that go to one CTA.
-__device__ __forceinline__ int64_t steps_per_cta(const AttnArgs &a) {
+// Steps of the line that go to one stream.
+__device__ __forceinline__ int64_t steps_per_stream(const AttnArgs &a) {
     const int64_t total = __ldg(a.start + a.N + a.R);
-    return (total + a.n_ctas - 1) / a.n_ctas;
+    return max((int64_t)kMinSteps, (total + a.n_streams - 1) / a.n_streams);
 }
 
 // A row of an item: which query it is and how many of the sequence's keys it sees.

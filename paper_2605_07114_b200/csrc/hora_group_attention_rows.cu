@@ -1,28 +1,33 @@
 // hora_group_attention, the kernel for items of up to 16 query rows: decode of single tokens over long caches.
 //
 // The call is bound by the cache's bytes (16 rows or fewer to a key: at most 16 products a byte), so the tensor unit matters only in
-// that it has to be out of the way, and what counts is loads in flight.  Keys and values go from global memory
-// straight into the registers that mma.m16n8k16 takes them in, with no shared memory, no barrier and no copy in between:
+// that it has to be out of the way, and what counts is bytes in flight.  Every warp is a stream of its own, with its own
+// running maximum, sum and output and its own ring of stages in shared memory: a stage is sixteen keys and values, fetched by
+// cp.async (16 KiB of stages a warp, twelve warps an SM: up to 192 KiB in flight, several times what 6.5 TB/s needs at
+// the latency of HBM under load).  No barrier joins the warps, and none waits for another.
+//
+// From the ring the operands go into the registers of mma.m16n8k16 by 16-byte loads, with no transposition:
 //   - scores S = Q K^T sum over the head's dimensions, in any order that Q and K agree on: lane (n, c) = (lane / 4, lane % 4) of
-//     a warp takes 16 neighbouring bytes of key n, and the four lanes of a key neighbouring blocks of 16;
-//   - O += P V sums over keys, two neighbouring ones to a register: lane (n, c) loads 16 bytes of keys 2c, 2c+1, 2c+8, 2c+9
-//     from dimension n * 8 (16 for one-byte values) on and pairs them up by byte permutations.  The column n of the product then is
-//     dimension n * 8 + j of the head for the j-th register: a lane ends up with runs of neighbouring dimensions.
-// Each warp runs over its own keys with its own running maximum, sum and output; the next keys are requested
-// before the softmax of the present ones, the next values after their product.  The four warps of a CTA take a step's 64 keys,
-// 16 each, and join their partials in shared memory when the CTA's part of an item ends.
+//     a warp takes 16 neighbouring bytes of a key, and the four lanes of a key neighbouring blocks of 16;
+//   - O += P V sums over keys, two to a register: lane (n, c) loads 16 bytes of the two keys from dimension n * 8 (16 for
+//     one-byte values) on and pairs them up by byte permutations.  Column n of the product is then dimension n * 8 + j of the
+//     head for the j-th register: a lane ends up with runs of neighbouring dimensions, which it stores as they are.
+// The 16-byte chunks of a row lie at places exchanged by the row's number, and column n stands for key key_of(n), such that the eight
+// lanes of each phase of a load hit different banks, for keys and for values.
 //
 // An e4m3 cache is multiplied in fp16, which holds its codes exactly: a row's power-of-two scale is applied to its score, and to
 // its weight relative to the largest value scale met so far, so that weights stay within [0, 1]; queries are scaled by a power of
 // two to lie well within fp16's range.
+#include <type_traits>
+
 #include "hora_group_attention.cuh"
 
 namespace hora {
 
 constexpr int kStepThreads = 128;
 constexpr int kStepWarps = kStepThreads / kWarp;
-constexpr int kWarpKeys = kStepKeys / kStepWarps;        // 16: one mma's worth
-static_assert(kWarpKeys == 16, "a warp takes sixteen keys of a step");
+constexpr int kRingBytes = 16384;                        // stages of one warp
+static_assert(kStepKeys == 16, "a step is one mma's worth of keys");
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -46,51 +51,90 @@ __device__ __forceinline__ float quad_sum(float v) {
 
 __device__ __forceinline__ float exponent_byte(uint32_t b) { return __uint_as_float(b ? b << 23 : 0x400000u); }
 
-// sixteen keys of a warp on their way through the registers
+__device__ __forceinline__ void copy16(uint32_t to, const void *from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int LEFT>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
+
+__device__ __forceinline__ uint4 lds16(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint2 lds8(uint32_t at) {
+    uint2 v;
+    asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
+    return v;
+}
+__device__ __forceinline__ uint32_t lds1(uint32_t at) {
+    uint32_t v;
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at));
+    return v;
+}
+
+// A stage of a warp's ring: keys, values, and (one-byte types) their scale bytes.
 template <bool F8, int D>
-struct Keys {
-    static constexpr int kBlocks = F8 ? D / 64 : D / 32;          // 16-byte loads for each key in K
-    static constexpr int kHalves = F8 ? 1 : D / 64;               // 16-byte (D = 64 in one-byte values: 8-byte) loads for each key in V
-    uint4 k[2][kBlocks], v[4][kHalves];
-    uint32_t ke[2], ve[2];                                        // scale bytes of keys 2c, 2c+1 and 2c+8, 2c+9
+struct Stage {
+    static constexpr int kRowBytes = F8 ? D : 2 * D;
+    static constexpr int kHalf = kStepKeys * kRowBytes;                       // keys; values follow
+    static constexpr int kStages = kRingBytes / (2 * kHalf);
+    static constexpr int kExpBytes = F8 ? 2 * kStepKeys : 0;
+    static constexpr int kBytes = 2 * kHalf;
+    static constexpr int kWarpBytes = kStages * (kBytes + kExpBytes);         // scale bytes of all stages behind the rows
+    static constexpr int kChunks = kRowBytes / 16;
+
+    // place of 16-byte chunk `chunk` of row `row` (both below 16)
+    static __device__ __forceinline__ uint32_t place(int row, int chunk) {
+        if constexpr (kRowBytes == 64) return (row >> 1) * 128 + ((((row & 1) * 4 + chunk) ^ ((row & 6))) << 4);
+        else return row * kRowBytes + ((chunk ^ (row & 7)) << 4);
+    }
+    // key that column n (below 8) of a score tile stands for
+    static __device__ __forceinline__ int key_of(int n) { return kRowBytes == 64 ? n : n ^ ((n & 1) << 2); }
 };
 
 template <typename Q, bool F8, int D>
-__global__ void __launch_bounds__(kStepThreads, 3)
+__global__ void __launch_bounds__(kStepThreads, kStreamsPerSm / kStepWarps)
 attention_rows_kernel(const AttnArgs a) {
     pdl_enter();
     using M = std::conditional_t<F8, __half, Q>;                  // the type of the products
-    using Elem = std::conditional_t<F8, uint8_t, uint16_t>;       // a cached element
-    constexpr int kBlocks = Keys<F8, D>::kBlocks, kHalves = Keys<F8, D>::kHalves;
-    constexpr int kBlockDims = F8 ? 64 : 32;                      // dimensions of one K load over the four lanes of a key
+    using St = Stage<F8, D>;
+    constexpr int kBlocks = F8 ? D / 64 : D / 32;                 // 16-byte loads of a lane for each key in K
+    constexpr int kHalves = F8 ? 1 : D / 64;                      // and for each key in V (one-byte values, D = 64: 8 bytes)
     constexpr int kOut = D / 8;                                   // column tiles of the output
-    __shared__ float s_o[kStepWarps][kTileRows][D + 4];
-    __shared__ float s_m[kStepWarps][kTileRows], s_l[kStepWarps][kTileRows];
+    constexpr int kStages = St::kStages;
+    extern __shared__ __align__(128) uint8_t s_ring[];
     const int lane = lane_id(), warp = threadIdx.x >> 5;
     const int n = lane >> 2, c = lane & 3;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + warp * St::kWarpBytes;
+    const uint32_t exps = ring + kStages * St::kBytes;
+    const int32_t stream = blockIdx.x * kStepWarps + warp;
     const int32_t n_seq = a.N + a.R;
     const int64_t total = __ldg(a.start + n_seq);
-    const int64_t per = (total + a.n_ctas - 1) / a.n_ctas;
+    const int64_t per = steps_per_stream(a);
     const int64_t rows_all = (int64_t)a.R * a.T * a.Hq;
-    int64_t u = (int64_t)blockIdx.x * per;
+    int64_t u = (int64_t)stream * per;
     const int64_t u_end = min(total, u + per);
     if (u >= u_end) return;
 
     // the sequence that holds step u: the last i with start[i] <= u, 32 probes at a time
     int32_t i = 0;
-    for (int32_t lo = 0, hi = n_seq;;) {                          // start[lo] <= u < start[hi]
-        const int32_t gap = (hi - lo + kWarp - 1) / kWarp;
-        const int32_t probe = min(hi, lo + lane * gap);
-        const unsigned at_or_before = __ballot_sync(kFull, __ldg(a.start + probe) <= u && probe < hi);
+    for (int32_t hi = n_seq; hi - i > 1;) {                       // start[i] <= u < start[hi]
+        const int32_t gap = (hi - i + kWarp - 1) / kWarp;
+        const int32_t probe = min(hi, i + lane * gap);
+        const unsigned at_or_before = __ballot_sync(kFull, probe < hi && __ldg(a.start + probe) <= u);
         const int32_t top = 31 - __clz(at_or_before);             // lane 0 always is
-        hi = min(hi, lo + (top + 1) * gap);
-        lo = lo + top * gap;
-        i = lo;
-        if (hi - lo <= 1) break;
+        hi = min(hi, i + (top + 1) * gap);
+        i += top * gap;
     }
     bool bad = false;
     Sequence s = sequence(a, i, bad);
     int64_t s_start = __ldg(a.start + i);
+
+    // where this lane reads: keys key_of(n), key_of(n) + 8 for the scores, and the two keys of columns 2c and 2c + 1 (and
+    // those eight further on) for the product with the weights
+    const int key_n = St::key_of(n), key_a = St::key_of(2 * c), key_b = St::key_of(2 * c + 1);
 
     while (u < u_end) {
         while (u >= s_start + (int64_t)s.steps * s.tiles * a.Hkv) {           // on to the next sequence that has steps
@@ -105,8 +149,40 @@ attention_rows_kernel(const AttnArgs a) {
         const bool prompt = i < a.N;
         const int32_t *__restrict__ pages = prompt ? a.prefix_pages + (int64_t)i * a.prefix_ld
                                                    : a.suffix_pages + (int64_t)(i - a.N) * a.suffix_ld;
+
+        // page numbers are looked up one step before the copies that need them
+        auto page_of = [&](int32_t step) { return step < step1 ? __ldg(pages + ((step * kStepKeys) >> a.page_shift)) : 0; };
+        auto fetch = [&](int32_t step, int32_t page) {
+            if (step < step1) {
+                if (page < 0 || page >= a.n_pages) { bad = true; page = 0; }
+                const int64_t row = (((int64_t)page * a.Hkv + h) << a.page_shift) + ((step * kStepKeys) & ((1 << a.page_shift) - 1));
+                const int slot = (step - step0) % kStages;
+                const uint32_t to = ring + slot * St::kBytes;
+                const uint8_t *__restrict__ k = static_cast<const uint8_t *>(a.k_cache) + row * St::kRowBytes + lane * 16;
+                const uint8_t *__restrict__ v = static_cast<const uint8_t *>(a.v_cache) + row * St::kRowBytes + lane * 16;
+#pragma unroll
+                for (int x = 0; x < St::kHalf / 512; ++x) {
+                    const int chunk = x * kWarp + lane;
+                    copy16(to + St::place(chunk / St::kChunks, chunk % St::kChunks), k + x * 512);
+                }
+#pragma unroll
+                for (int x = 0; x < St::kHalf / 512; ++x) {
+                    const int chunk = x * kWarp + lane;
+                    copy16(to + St::kHalf + St::place(chunk / St::kChunks, chunk % St::kChunks), v + x * 512);
+                }
+                if (F8 && lane < 2) copy16(exps + slot * St::kExpBytes + lane * kStepKeys, (lane == 0 ? a.k_exp : a.v_exp) + row);
+            }
+            copies_done();                                        // a group for each step, empty ones too: the waits count groups
+        };
+        int32_t page[kStages];
+#pragma unroll
+        for (int x = 0; x < kStages; ++x) page[x] = page_of(step0 + x);
+#pragma unroll
+        for (int x = 0; x < kStages; ++x) fetch(step0 + x, page[x]);
+        int32_t page_next = page_of(step0 + kStages);
+
         // rows n and n + 8 of the tile are this lane's
-        const QueryRow row0 = query_row(a, s, prompt, h, tile * kTileRows + n);
+const QueryRow row0 = query_row(a, s, prompt, h, tile * kTileRows + n);
         const QueryRow row1 = query_row(a, s, prompt, h, tile * kTileRows + n + 8);
         uint32_t qf[2 * kBlocks * (F8 ? 2 : 1)][4];               // one mma step (16 dimensions) each
         float q_unit0 = 1.f, q_unit1 = 1.f;                       // what the stored queries have to be multiplied by
@@ -163,60 +239,19 @@ attention_rows_kernel(const AttnArgs a) {
         float o[kOut][4] = {};
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         float v_unit = 0.f;                                       // F8: o is in units of this (0: nothing added yet)
-
-        Keys<F8, D> x;
-        auto page_row = [&](int32_t key) {                        // pool row of the warp's first key; lengths end inside the table
-            int32_t p = key < s.len ? __ldg(pages + (key >> a.page_shift)) : 0;
-            if (p < 0 || p >= a.n_pages) { bad = true; p = 0; }
-            return (((int64_t)p * a.Hkv + h) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
-        };
-        auto load_k = [&](int64_t row) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int b = 0; b < kBlocks; ++b)
-                    x.k[j][b] = __ldcs(reinterpret_cast<const uint4 *>(static_cast<const Elem *>(a.k_cache) + (row + j * 8 + n) * D + b * kBlockDims + c * (16 / (int)sizeof(Elem))));
-            if constexpr (F8) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) x.ke[j] = __ldg(reinterpret_cast<const uint16_t *>(a.k_exp + row + j * 8 + 2 * c));
-            }
-        };
-        auto load_v = [&](int64_t row) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int b = 0; b < kHalves; ++b) {
-                    const Elem *__restrict__ p = static_cast<const Elem *>(a.v_cache) + (row + (j >> 1) * 8 + 2 * c + (j & 1)) * D;
-                    if constexpr (F8 && D == 64) {
-                        const uint2 y = __ldcs(reinterpret_cast<const uint2 *>(p + n * 8));
-                        x.v[j][b] = make_uint4(y.x, y.y, 0u, 0u);
-                    } else if constexpr (F8) {
-                        x.v[j][b] = __ldcs(reinterpret_cast<const uint4 *>(p + n * 16));
-                    } else {
-                        x.v[j][b] = __ldcs(reinterpret_cast<const uint4 *>(p + b * 64 + n * 8));
-                    }
-                }
-            if constexpr (F8) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) x.ve[j] = __ldg(reinterpret_cast<const uint16_t *>(a.v_exp + row + j * 8 + 2 * c));
-            }
-        };
-
-        int32_t key = step0 * kStepKeys + warp * kWarpKeys;
-        const int32_t key_end = min(step1 * kStepKeys, s.len);
-        if (key < key_end) {
-            const int64_t row = page_row(key);
-            load_k(row);
-            load_v(row);
-        }
-        for (; key < key_end; key += kStepKeys) {
-            const int64_t next = key + kStepKeys < key_end ? page_row(key + kStepKeys) : -1;
+        for (int32_t step = step0; step < step1; ++step) {
+            const int32_t key = step * kStepKeys;
+            const int slot = (step - step0) % kStages;
+            const uint32_t at_k = ring + slot * St::kBytes, at_v = at_k + St::kHalf;
+            copies_wait<kStages - 1>();
+            __syncwarp();
             float sc[2][4] = {};
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
-                    const uint32_t w[4] = {x.k[j][b].x, x.k[j][b].y, x.k[j][b].z, x.k[j][b].w};
+                    const uint4 x = lds16(at_k + St::place(j * 8 + key_n, b * 4 + c));
+                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
                     if constexpr (F8) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
@@ -226,19 +261,17 @@ attention_rows_kernel(const AttnArgs a) {
                         mma16816(sc[j], qf[2 * b + 1], w[2], w[3], M());
                     }
                 }
-            uint32_t ke[2] = {0u, 0u};
-            if constexpr (F8) { ke[0] = x.ke[0]; ke[1] = x.ke[1]; }
-            if (next >= 0) load_k(next);
             // scores in units of log2, hidden keys at -infinity
-            const bool whole = key + kWarpKeys <= min(row0.limit, row1.limit);
+            const bool whole = key + kStepKeys <= min(row0.limit, row1.limit);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
+                    const int k = j * 8 + ((e & 1) ? key_b : key_a);
                     float f = e < 2 ? to_log2_0 : to_log2_1;
-                    if constexpr (F8) f *= exponent_byte((ke[j] >> (8 * (e & 1))) & 0xFFu);
+                    if constexpr (F8) f *= exponent_byte(lds1(exps + slot * St::kExpBytes + k));
                     sc[j][e] *= f;
-                    if (!whole && key + j * 8 + 2 * c + (e & 1) >= (e < 2 ? row0.limit : row1.limit)) sc[j][e] = -INFINITY;
+                    if (!whole && key + k >= (e < 2 ? row0.limit : row1.limit)) sc[j][e] = -INFINITY;
                 }
             const float top0 = fmaxf(m0, quad_max(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1]))));
             const float top1 = fmaxf(m1, quad_max(fmaxf(fmaxf(sc[0][2], sc[0][3]), fmaxf(sc[1][2], sc[1][3]))));
@@ -257,8 +290,8 @@ attention_rows_kernel(const AttnArgs a) {
                 float e4[4], top = v_unit;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const bool in = key + (j >> 1) * 8 + 2 * c + (j & 1) < s.len;
-                    e4[j] = in ? exponent_byte((x.ve[j >> 1] >> (8 * (j & 1))) & 0xFFu) : 0.f;
+                    const int k = (j >> 1) * 8 + ((j & 1) ? key_b : key_a);
+                    e4[j] = key + k < s.len ? exponent_byte(lds1(exps + slot * St::kExpBytes + kStepKeys + k)) : 0.f;
                     top = fmaxf(top, e4[j]);
                 }
                 top = quad_max(top);                              // the same in all quads: they hold the same keys
@@ -273,26 +306,33 @@ attention_rows_kernel(const AttnArgs a) {
             }
 #pragma unroll
             for (int t = 0; t < kOut; ++t) { o[t][0] *= f0; o[t][1] *= f0; o[t][2] *= f1; o[t][3] *= f1; }
-            if (key + kWarpKeys > s.len) {                        // what lies beyond the length may be anything: 0 * NaN is not 0
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (key + (j >> 1) * 8 + 2 * c + (j & 1) >= s.len)
-#pragma unroll
-                        for (int b = 0; b < kHalves; ++b) x.v[j][b] = make_uint4(0, 0, 0, 0);
-            }
             const uint32_t p[4] = {pack2(sc[0][0], sc[0][1], M()), pack2(sc[0][2], sc[0][3], M()),
                                    pack2(sc[1][0], sc[1][1], M()), pack2(sc[1][2], sc[1][3], M())};
 #pragma unroll
             for (int b = 0; b < kHalves; ++b) {
-                const uint32_t v0[4] = {x.v[0][b].x, x.v[0][b].y, x.v[0][b].z, x.v[0][b].w};
-                const uint32_t v1[4] = {x.v[1][b].x, x.v[1][b].y, x.v[1][b].z, x.v[1][b].w};
-                const uint32_t v2[4] = {x.v[2][b].x, x.v[2][b].y, x.v[2][b].z, x.v[2][b].w};
-                const uint32_t v3[4] = {x.v[3][b].x, x.v[3][b].y, x.v[3][b].z, x.v[3][b].w};
+                uint32_t v[4][4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int k = (j >> 1) * 8 + ((j & 1) ? key_b : key_a);
+                    uint4 x;
+                    if constexpr (F8 && D == 64) {
+                        const uint2 y = lds8(at_v + St::place(k, n >> 1) + (n & 1) * 8);
+                        x = make_uint4(y.x, y.y, 0u, 0u);
+                    } else {
+                        x = lds16(at_v + St::place(k, b * 8 + n));
+                    }
+                    // what lies beyond the length may be anything, and 0 * NaN is not 0
+                    const bool in = key + k < s.len;
+                    v[j][0] = in ? x.x : 0u;
+                    v[j][1] = in ? x.y : 0u;
+                    v[j][2] = in ? x.z : 0u;
+                    v[j][3] = in ? x.w : 0u;
+                }
                 if constexpr (F8) {
 #pragma unroll
                     for (int w = 0; w < kOut / 4; ++w) {          // four dimensions of a key to a word
-                        const uint32_t lo0 = __byte_perm(v0[w], v1[w], 0x5140), hi0 = __byte_perm(v0[w], v1[w], 0x7362);
-                        const uint32_t lo1 = __byte_perm(v2[w], v3[w], 0x5140), hi1 = __byte_perm(v2[w], v3[w], 0x7362);
+                        const uint32_t lo0 = __byte_perm(v[0][w], v[1][w], 0x5140), hi0 = __byte_perm(v[0][w], v[1][w], 0x7362);
+                        const uint32_t lo1 = __byte_perm(v[2][w], v[3][w], 0x5140), hi1 = __byte_perm(v[2][w], v[3][w], 0x7362);
                         mma16816(o[4 * w], p, e4m3x2_to_half2(lo0 & 0xFFFFu), e4m3x2_to_half2(lo1 & 0xFFFFu), M());
                         mma16816(o[4 * w + 1], p, e4m3x2_to_half2(lo0 >> 16), e4m3x2_to_half2(lo1 >> 16), M());
                         mma16816(o[4 * w + 2], p, e4m3x2_to_half2(hi0 & 0xFFFFu), e4m3x2_to_half2(hi1 & 0xFFFFu), M());
@@ -301,81 +341,60 @@ attention_rows_kernel(const AttnArgs a) {
                 } else {
 #pragma unroll
                     for (int w = 0; w < 4; ++w) {                 // two dimensions of a key to a word
-                        mma16816(o[8 * b + 2 * w], p, __byte_perm(v0[w], v1[w], 0x5410), __byte_perm(v2[w], v3[w], 0x5410), M());
-                        mma16816(o[8 * b + 2 * w + 1], p, __byte_perm(v0[w], v1[w], 0x7632), __byte_perm(v2[w], v3[w], 0x7632), M());
+                        mma16816(o[8 * b + 2 * w], p, __byte_perm(v[0][w], v[1][w], 0x5410), __byte_perm(v[2][w], v[3][w], 0x5410), M());
+                        mma16816(o[8 * b + 2 * w + 1], p, __byte_perm(v[0][w], v[1][w], 0x7632), __byte_perm(v[2][w], v[3][w], 0x7632), M());
                     }
                 }
             }
-            if (next >= 0) load_v(next);
+            __syncwarp();                                         // every lane has read the stage that is filled next
+            fetch(step + kStages, page_next);
+            page_next = page_of(step + kStages + 1);
         }
         l0 = quad_sum(l0);
         l1 = quad_sum(l1);
 
-        // join the four warps.  o[t] holds columns 2c and 2c+1 of tile t: dimension column * run + t within its part of the head
+        // o[t] holds columns 2c and 2c + 1 of tile t; column x is dimension x * kRun + t of its part of the head
         constexpr int kRun = F8 ? D / 8 : 8;
 #pragma unroll
-        for (int t = 0; t < kOut; ++t) {
-            const int part = F8 ? 0 : (t >> 3) * 64, j = F8 ? t : t & 7;
-            const float f = F8 ? v_unit : 1.f;
-            s_o[warp][n][part + 2 * c * kRun + j] = o[t][0] * f;
-            s_o[warp][n][part + (2 * c + 1) * kRun + j] = o[t][1] * f;
-            s_o[warp][n + 8][part + 2 * c * kRun + j] = o[t][2] * f;
-            s_o[warp][n + 8][part + (2 * c + 1) * kRun + j] = o[t][3] * f;
-        }
-        if (c == 0) {
-            s_m[warp][n] = m0;
-            s_m[warp][n + 8] = m1;
-            s_l[warp][n] = l0;
-            s_l[warp][n + 8] = l1;
-        }
-        __syncthreads();
-        const int32_t tile_rows = min(kTileRows, s.rows - tile * kTileRows);
-        for (int32_t at = warp; at < tile_rows; at += kStepWarps) {
-            float m = -INFINITY, l = 0.f, f[kStepWarps];
-#pragma unroll
-            for (int w = 0; w < kStepWarps; ++w) m = fmaxf(m, s_m[w][at]);
-            const float z = m == -INFINITY ? 0.f : m;
-#pragma unroll
-            for (int w = 0; w < kStepWarps; ++w) {
-                f[w] = exp2f(s_m[w][at] - z);
-                l += s_l[w][at] * f[w];
-            }
-            const int64_t out = query_row(a, s, prompt, h, tile * kTileRows + at).out;
-            const int64_t place = step0 > 0 ? (int64_t)blockIdx.x * kTileRows + at : (prompt ? out : rows_all + out);
+        for (int half = 0; half < 2; ++half) {
+            const int64_t out = half ? row1.out : row0.out;
+            if (out < 0) continue;
+            const int64_t place = step0 > 0 ? (int64_t)stream * kTileRows + n + half * 8 : (prompt ? out : rows_all + out);
             float *__restrict__ po = (step0 > 0 ? a.cont_o : a.main_o) + place * D;
-            float *__restrict__ pml = (step0 > 0 ? a.cont_ml : a.main_ml) + place * 2;
+            const float f = F8 ? v_unit : 1.f;
 #pragma unroll
-            for (int d = lane * 2; d < D; d += 2 * kWarp) {
-                float2 y = make_float2(0.f, 0.f);
+            for (int part = 0; part < kOut / kRun; ++part)
 #pragma unroll
-                for (int w = 0; w < kStepWarps; ++w) {
-                    const float2 v = *reinterpret_cast<const float2 *>(&s_o[w][at][d]);
-                    y.x += v.x * f[w];
-                    y.y += v.y * f[w];
-                }
-                *reinterpret_cast<float2 *>(po + d) = y;
-            }
-            if (lane == 0) *reinterpret_cast<float2 *>(pml) = make_float2(m, l);
+                for (int x = 0; x < 2; ++x)
+#pragma unroll
+                    for (int t = 0; t < kRun; t += 4)
+                        *reinterpret_cast<float4 *>(po + part * 64 + (2 * c + x) * kRun + t) =
+                            make_float4(o[part * kRun + t][2 * half + x] * f, o[part * kRun + t + 1][2 * half + x] * f,
+                                        o[part * kRun + t + 2][2 * half + x] * f, o[part * kRun + t + 3][2 * half + x] * f);
+            if (c == 0) *reinterpret_cast<float2 *>((step0 > 0 ? a.cont_ml : a.main_ml) + place * 2) = make_float2(half ? m1 : m0, half ? l1 : l0);
         }
-        __syncthreads();
         u += step1 - step0;
     }
     if (bad) raise_status(a.status, HORA_ERR_INVALID_VALUE);
 }
 
+template <typename Q, bool F8, int D>
+static hora_status_t launch_rows(const AttnArgs &a, cudaStream_t stream) {
+    constexpr int kSmem = kStepWarps * Stage<F8, D>::kWarpBytes;
+    cudaError_t e = cudaFuncSetAttribute(attention_rows_kernel<Q, F8, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e == cudaSuccess) e = launch_pdl(attention_rows_kernel<Q, F8, D>, a.n_streams / kStepWarps, kStepThreads, kSmem, stream, a);
+    count_launches(1);
+    return cuda_ok(e);
+}
+
 hora_status_t launch_attention_steps(const AttnArgs &a, int32_t q_dtype, int32_t cache_dtype, int32_t D, cudaStream_t stream) {
-    auto go = [&](auto kernel) {
-        const cudaError_t e = launch_pdl(kernel, a.n_ctas, kStepThreads, 0, stream, a);
-        count_launches(1);
-        return cuda_ok(e);
-    };
     const bool bf = q_dtype == HORA_DTYPE_BF16;
     if (cache_dtype == HORA_DTYPE_E4M3) {
-        if (D == 64) return bf ? go(attention_rows_kernel<__nv_bfloat16, true, 64>) : go(attention_rows_kernel<__half, true, 64>);
-        return bf ? go(attention_rows_kernel<__nv_bfloat16, true, 128>) : go(attention_rows_kernel<__half, true, 128>);
+        if (D == 64) return bf ? launch_rows<__nv_bfloat16, true, 64>(a, stream) : launch_rows<__half, true, 64>(a, stream);
+        return bf ? launch_rows<__nv_bfloat16, true, 128>(a, stream) : launch_rows<__half, true, 128>(a, stream);
     }
-    if (D == 64) return bf ? go(attention_rows_kernel<__nv_bfloat16, false, 64>) : go(attention_rows_kernel<__half, false, 64>);
-    return bf ? go(attention_rows_kernel<__nv_bfloat16, false, 128>) : go(attention_rows_kernel<__half, false, 128>);
+    if (D == 64) return bf ? launch_rows<__nv_bfloat16, false, 64>(a, stream) : launch_rows<__half, false, 64>(a, stream);
+    return bf ? launch_rows<__nv_bfloat16, false, 128>(a, stream) : launch_rows<__half, false, 128>(a, stream);
 }
 
 }  // namespace hora

@@ -136,7 +136,7 @@ inline bool cache_ok(const void *k, const void *v, const void *k_exp, const void
     if (k == nullptr || v == nullptr || ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) & 15u)) return false;
     if (dtype == HORA_DTYPE_E4M3) {
         if (k_exp == nullptr || v_exp == nullptr) return false;
-        if ((reinterpret_cast<uintptr_t>(k_exp) | reinterpret_cast<uintptr_t>(v_exp)) & 1u) return false;
+        if ((reinterpret_cast<uintptr_t>(k_exp) | reinterpret_cast<uintptr_t>(v_exp)) & 15u) return false;
     }
     return true;
 }
