@@ -4,39 +4,49 @@
 namespace hora {
 
 constexpr int kPlanThreads = 1024;
+constexpr int kWideFrom = 33;
 
-// start[i] = steps before sequence i on the line, group_of[r].  One CTA: every thread takes a run of sequences.
+// start[line][i] = steps before sequence i on its line, group_of[r].  One CTA: every thread takes a run of sequences.
 __global__ void __launch_bounds__(kPlanThreads)
 attention_plan_kernel(const AttnArgs a) {
     pdl_enter();
-    __shared__ int64_t s_warp[kPlanThreads / kWarp];
+    __shared__ int64_t s_warp[2][kPlanThreads / kWarp];
     const int64_t n = (int64_t)a.N + a.R;
     const int64_t each = (n + kPlanThreads - 1) / kPlanThreads;
     const int64_t lo = min(n, each * threadIdx.x), hi = min(n, lo + each);
     bool bad = false;
-    int64_t sum = 0;
+    int64_t sum[2] = {0, 0}, run[2];
     for (int64_t i = lo; i < hi; ++i) {
         const Sequence s = sequence(a, (int32_t)i, bad);
-        sum += (int64_t)s.steps * s.tiles * a.Hkv;
+        (s.wide ? sum[1] : sum[0]) += total_steps(a, s);
     }
-    int64_t incl = sum;
     const int lane = lane_id(), warp = threadIdx.x >> 5;
 #pragma unroll
-    for (int d = 1; d < kWarp; d <<= 1) {
-        const int64_t o = __shfl_up_sync(kFull, incl, d);
-        if (lane >= d) incl += o;
+    for (int w = 0; w < 2; ++w) {
+        int64_t incl = sum[w];
+#pragma unroll
+        for (int d = 1; d < kWarp; d <<= 1) {
+            const int64_t o = __shfl_up_sync(kFull, incl, d);
+            if (lane >= d) incl += o;
+        }
+        if (lane == kWarp - 1) s_warp[w][warp] = incl;
+        run[w] = incl - sum[w];
     }
-    if (lane == kWarp - 1) s_warp[warp] = incl;
     __syncthreads();
-    int64_t run = incl - sum;
-    for (int w = 0; w < warp; ++w) run += s_warp[w];
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+        for (int x = 0; x < warp; ++x) run[w] += s_warp[w][x];
     for (int64_t i = lo; i < hi; ++i) {
-        a.start[i] = run;
+        a.start[0][i] = run[0];
+        a.start[1][i] = run[1];
         bool again = false;
         const Sequence s = sequence(a, (int32_t)i, again);
-        run += (int64_t)s.steps * s.tiles * a.Hkv;
+        (s.wide ? run[1] : run[0]) += total_steps(a, s);
     }
-    if (threadIdx.x == kPlanThreads - 1) a.start[n] = run;
+    if (threadIdx.x == kPlanThreads - 1) {
+        a.start[0][n] = run[0];
+        a.start[1][n] = run[1];
+    }
     const int64_t covered = __ldg(a.group_offsets + a.N);
     for (int32_t r = threadIdx.x; r < a.R; r += kPlanThreads) {
         int32_t g = -1;
@@ -91,23 +101,28 @@ attention_join_kernel(const AttnArgs a) {
     Joined<E> j;
     const int32_t grp = a.group_of[r];
     if (grp >= 0 && t < query_count(a, r)) {
-        const int64_t per = steps_per_stream(a);
         bool bad = false;
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
-            const int32_t i = part == 0 ? grp : a.N + r;
+            const int32_t i = part == kPromptPart ? grp : a.N + r;
             const Sequence s = sequence(a, i, bad);
-            if (s.steps == 0 || s.rollouts == 0 || r < s.first || r >= s.first + s.rollouts) continue;
+            if (s.steps == 0 || r < s.first || r >= s.first + s.rollouts) continue;
             const int32_t x = ((r - s.first) * a.T + t) * a.g + head % a.g;
-            const int32_t tile = x / kTileRows, at = x % kTileRows;
-            const int64_t u0 = __ldg(a.start + i) + ((int64_t)h * s.tiles + tile) * s.steps;
-            const float2 ml = *reinterpret_cast<const float2 *>(a.main_ml + (part * rows + row) * 2);
-            j.add(ml.x, ml.y, a.main_o + (part * rows + row) * D, lane);
-            const int32_t b1 = (int32_t)((u0 + s.steps - 1) / per);
-            for (int32_t b = (int32_t)(u0 / per) + 1; b <= b1; ++b) {
-                const int64_t c = (int64_t)b * kTileRows + at;
-                const float2 ml2 = *reinterpret_cast<const float2 *>(a.cont_ml + c * 2);
-                j.add(ml2.x, ml2.y, a.cont_o + c * D, lane);
+            const int32_t tile = x / s.tile_rows, at = x % s.tile_rows;
+            const int64_t u0 = __ldg(a.start[s.wide] + i) + ((int64_t)h * s.tiles + tile) * s.steps;
+            const int64_t per = s.wide ? steps_per_stream<true>(a) : steps_per_stream<false>(a);
+            // a wide item of one half has its keys dealt to two halves, each with a partial of its own
+            const int halves = s.wide && min(s.tile_rows, s.rows - tile * s.tile_rows) <= kWideHalf ? 2 : 1;
+            const int32_t b0 = (int32_t)(u0 / per), b1 = (int32_t)((u0 + s.steps - 1) / per);
+            for (int half = 0; half < halves; ++half) {
+                const int64_t place = (part + half * kSecondHalf) * rows + row;
+                const float2 ml = *reinterpret_cast<const float2 *>(a.main_ml + place * 2);
+                j.add(ml.x, ml.y, a.main_o + place * D, lane);
+                for (int32_t b = b0 + 1; b <= b1; ++b) {
+                    const int64_t c = (int64_t)b * (s.wide ? kWideRows : kNarrowRows) + half * kWideHalf + at;
+                    const float2 ml2 = *reinterpret_cast<const float2 *>(a.cont_ml[s.wide] + c * 2);
+                    j.add(ml2.x, ml2.y, a.cont_o[s.wide] + c * D, lane);
+                }
             }
         }
     }
@@ -118,13 +133,13 @@ attention_join_kernel(const AttnArgs a) {
     if (a.lse != nullptr && lane == 0) a.lse[row] = j.m == -INFINITY ? -INFINITY : 0.6931471805599453f * j.m + logf(j.l);
 }
 
-hora_status_t launch_attention_plan(const AttnArgs &a, cudaStream_t stream) {
+static hora_status_t launch_plan(const AttnArgs &a, cudaStream_t stream) {
     const cudaError_t e = launch_pdl(attention_plan_kernel, 1, kPlanThreads, 0, stream, a);
     count_launches(1);
     return cuda_ok(e);
 }
 
-hora_status_t launch_attention_join(const AttnArgs &a, int32_t q_dtype, int32_t D, cudaStream_t stream) {
+static hora_status_t launch_join(const AttnArgs &a, int32_t q_dtype, int32_t D, cudaStream_t stream) {
     const int64_t rows = (int64_t)a.R * a.T * a.Hq;
     const int grid = (int)((rows + 7) / 8);
     cudaError_t e;
@@ -147,13 +162,17 @@ static size_t lay_out(AttnArgs &a, int32_t D, char *base) {
         return p;
     };
     const size_t rows = (size_t)a.R * a.T * a.Hq;
-    a.n_streams = sm_count() * kStreamsPerSm;
-    a.start = reinterpret_cast<int64_t *>(take(((size_t)a.N + a.R + 1) * 8));
+    a.n_narrow = sm_count() * kNarrowPerSm;
+    a.n_wide = sm_count();
+    for (int w = 0; w < 2; ++w) {
+        const size_t cont = w ? (size_t)a.n_wide * kWideRows : (size_t)a.n_narrow * kNarrowRows;
+        a.start[w] = reinterpret_cast<int64_t *>(take(((size_t)a.N + a.R + 1) * 8));
+        a.cont_o[w] = reinterpret_cast<float *>(take(cont * D * 4));
+        a.cont_ml[w] = reinterpret_cast<float *>(take(cont * 2 * 4));
+    }
     a.group_of = reinterpret_cast<int32_t *>(take((size_t)a.R * 4));
-    a.main_o = reinterpret_cast<float *>(take(rows * 2 * D * 4));
-    a.main_ml = reinterpret_cast<float *>(take(rows * 2 * 2 * 4));
-    a.cont_o = reinterpret_cast<float *>(take((size_t)a.n_streams * kTileRows * D * 4));
-    a.cont_ml = reinterpret_cast<float *>(take((size_t)a.n_streams * kTileRows * 2 * 4));
+    a.main_o = reinterpret_cast<float *>(take(rows * 4 * D * 4));
+    a.main_ml = reinterpret_cast<float *>(take(rows * 4 * 2 * 4));
     return used;
 }
 
@@ -229,8 +248,11 @@ extern "C" hora_status_t hora_group_attention(const void *q, int32_t q_dtype, in
     a.suffix_ld = suffix_ld;
     a.scale_log2 = sm_scale * 1.4426950408889634f;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    hora_status_t rc = launch_attention_plan(a, s);
-    if (rc == HORA_OK) rc = launch_attention_steps(a, q_dtype, cache_dtype, D, s);
-    if (rc == HORA_OK) rc = launch_attention_join(a, q_dtype, D, s);
+    if (cache_dtype == HORA_DTYPE_E4M3) a.n_wide = 0;
+    a.wide_from = kWideFrom;
+    hora_status_t rc = launch_plan(a, s);
+    if (rc == HORA_OK) rc = launch_attention_narrow(a, q_dtype, cache_dtype, D, s);
+    if (rc == HORA_OK && a.n_wide > 0) rc = launch_attention_wide(a, q_dtype, D, s);
+    if (rc == HORA_OK) rc = launch_join(a, q_dtype, D, s);
     return rc;
 }

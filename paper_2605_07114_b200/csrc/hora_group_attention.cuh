@@ -2,10 +2,12 @@
 //
 // The work is a list of N + R key sequences: the N prompts' (all queries of the group attend to them) and the R
 // rollouts' own.  A sequence has `rows` query rows for each cache head: (rollout, slot t, head of the cache head's
-// group), in that order.  A row tile of a sequence and one cache head is an item; an item's keys come in steps.  All steps
-// of all items, in order, form one line that is cut into equal pieces, one for each stream (a warp that runs by itself), so
-// every stream reads about the same number of bytes whatever the lengths are.  A piece's part of an item is a partial
-// result (m, l, o): m the largest score in units of log2, l = sum 2^(s - m), o = sum 2^(s - m) v.  Partials are joined at
+// group), in that order.  A block of rows of a sequence and one cache head is an item; an item's keys come in steps.
+// Sequences with few rows to a key are bound by the cache's bytes and go to the kernel for narrow items (mma.sync, a warp
+// to a stream); those with many have the products to do and go to the kernel for wide items (tcgen05, a CTA to a stream).
+// For each kernel all steps of its items, in order, form one line that is cut into equal pieces, one for each of its streams, so
+// every stream has about the same to do whatever the lengths are.  A piece's part of an item is a partial
+// result (m, l, o): m a reference score in units of log2, l = sum 2^(s - m), o = sum 2^(s - m) v.  Partials are joined at
 // the end: m = max m_i, l = sum l_i 2^(m_i - m), o = sum o_i 2^(m_i - m), out = o / l.
 //
 // Where a partial goes: the part of an item that begins the item has a place of its own for each output row; a part
@@ -16,10 +18,17 @@
 
 namespace hora {
 
-constexpr int kTileRows = 16;                            // query rows of an item
-constexpr int kStepKeys = 16;                            // keys of a step
-constexpr int kStreamsPerSm = 12;                       // 168 registers a lane, 16 KiB of keys and values in flight each
-constexpr int kMinSteps = 4;                             // a stream shorter than this costs more to join than it saves
+constexpr int kNarrowRows = 16;                          // query rows of a narrow item
+constexpr int kNarrowKeys = 16;                          // keys of its steps
+constexpr int kNarrowPerSm = 12;                         // streams an SM: 168 registers a lane, 16 KiB of keys and values in flight each
+constexpr int kNarrowMinSteps = 4;                       // a stream shorter than this costs more to join than it saves
+
+constexpr int kWideRows = 256;                           // query rows of a wide item, in two halves
+constexpr int kWideHalf = kWideRows / 2;
+constexpr int kWideKeys = 128;
+
+// Parts that a row's result is joined from, other than the continued ones.
+enum { kPromptPart = 0, kOwnPart = 1, kSecondHalf = 2 }; // kSecondHalf: added for the second half of the keys (wide items of one half)
 
 struct AttnArgs {
     const void *q;
@@ -32,19 +41,21 @@ struct AttnArgs {
     int32_t *status;
     int64_t q_row_stride, out_row_stride, n_pages;
     int32_t N, R, T, Hq, Hkv, g, page_shift, prefix_ld, suffix_ld;
-    int32_t n_streams;
+    int32_t n_narrow, n_wide;                            // streams; n_wide 0: every sequence is narrow
+    int32_t wide_from;                                   // rows from which a sequence is wide
     float scale_log2;                                    // sm_scale * log2(e)
     // workspace
-    int64_t *start;                                      // [N + R + 1] first step of each sequence on the line
+    int64_t *start[2];                                   // [N + R + 1] first step of each sequence on the narrow, the wide line
     int32_t *group_of;                                   // [R] group of each rollout, -1: none
-    float *main_o, *main_ml;                             // [2][R * T * Hq][D], [..][2]: prompt part, own part
-    float *cont_o, *cont_ml;                             // [n_streams][kTileRows][D], [..][2]
+    float *main_o, *main_ml;                             // [2 or 4][R * T * Hq][D], [..][2], by part
+    float *cont_o[2], *cont_ml[2];                       // [streams][rows of an item][D], [..][2]
 };
 
 // A sequence: its query rows per cache head, its keys, and how it is cut.
 struct Sequence {
     int32_t first, rollouts;                             // rollouts that attend to it
-    int32_t rows, len, steps, tiles;
+    int32_t rows, len, steps, tiles, tile_rows;
+    bool wide;
 };
 
 __device__ __forceinline__ int32_t clamp_i64(int64_t v, int32_t lo, int32_t hi) { return v < lo ? lo : (v > hi ? hi : (int32_t)v); }
@@ -76,16 +87,80 @@ __device__ __forceinline__ Sequence sequence(const AttnArgs &a, int32_t i, bool 
         s.len = checked_len(__ldg(a.suffix_len + s.first), a.suffix_ld, a.page_shift, bad);
     }
     s.rows = s.rollouts * a.T * a.g;
-    s.steps = (s.len + kStepKeys - 1) / kStepKeys;
-    s.tiles = (s.rows + kTileRows - 1) / kTileRows;
+    s.wide = a.n_wide > 0 && s.rows >= a.wide_from;
+    if (s.wide) {                                        // blocks of about the same size, so that their steps take the same time
+        s.tiles = (s.rows + kWideRows - 1) / kWideRows;
+        s.tile_rows = (s.rows + s.tiles - 1) / s.tiles;
+        s.steps = (s.len + kWideKeys - 1) / kWideKeys;
+    } else {
+        s.tiles = (s.rows + kNarrowRows - 1) / kNarrowRows;
+        s.tile_rows = kNarrowRows;
+        s.steps = (s.len + kNarrowKeys - 1) / kNarrowKeys;
+    }
     return s;
 }
 
-// Steps of the line that go to one stream.
+__device__ __forceinline__ int64_t total_steps(const AttnArgs &a, const Sequence &s) { return (int64_t)s.steps * s.tiles * a.Hkv; }
+
+// Steps of a line that go to one stream.
+template <bool WIDE>
 __device__ __forceinline__ int64_t steps_per_stream(const AttnArgs &a) {
-    const int64_t total = __ldg(a.start + a.N + a.R);
-    return max((int64_t)kMinSteps, (total + a.n_streams - 1) / a.n_streams);
+    const int64_t total = __ldg(a.start[WIDE] + a.N + a.R), n = WIDE ? a.n_wide : a.n_narrow;
+    return max((int64_t)(WIDE ? 1 : kNarrowMinSteps), (total + n - 1) / n);
 }
+
+// A stream's part of one item.
+struct Piece {
+    int32_t h, row0, rows, step0, step1;
+    bool prompt;
+    const int32_t *pages;
+};
+
+// Walks a stream's pieces in order; `s` is the sequence of the last one.  All lanes of a warp together.
+template <bool WIDE>
+struct Pieces {
+    int64_t u, u_end, s_start;
+    int32_t i;
+    Sequence s;
+
+    __device__ __forceinline__ Pieces(const AttnArgs &a, int32_t stream, bool &bad) {
+        const int64_t *__restrict__ start = a.start[WIDE];
+        const int32_t n_seq = a.N + a.R;
+        const int64_t per = steps_per_stream<WIDE>(a);
+        u = (int64_t)stream * per;
+        u_end = min(__ldg(start + n_seq), u + per);
+        i = 0;
+        if (u >= u_end) return;
+        for (int32_t hi = n_seq; hi - i > 1;) {          // start[i] <= u < start[hi], 32 probes at a time
+            const int32_t gap = (hi - i + kWarp - 1) / kWarp;
+            const int32_t probe = min(hi, i + lane_id() * gap);
+            const unsigned at_or_before = __ballot_sync(kFull, probe < hi && __ldg(start + probe) <= u);
+            const int32_t top = 31 - __clz(at_or_before); // lane 0 always is
+            hi = min(hi, i + (top + 1) * gap);
+            i += top * gap;
+        }
+        s = sequence(a, i, bad);
+        s_start = __ldg(start + i);
+    }
+
+    __device__ __forceinline__ bool next(const AttnArgs &a, Piece &p, bool &bad) {
+        if (u >= u_end) return false;
+        while (s.wide != WIDE || u >= s_start + total_steps(a, s)) {        // on to the next sequence with steps on this line
+            if (s.wide == WIDE) s_start += total_steps(a, s);
+            s = sequence(a, ++i, bad);
+        }
+        const int64_t item = (u - s_start) / s.steps;
+        p.step0 = (int32_t)((u - s_start) - item * s.steps);
+        p.step1 = (int32_t)min((int64_t)s.steps, p.step0 + (u_end - u));
+        p.h = (int32_t)(item / s.tiles);
+        p.row0 = (int32_t)(item % s.tiles) * s.tile_rows;
+        p.rows = min(s.tile_rows, s.rows - p.row0);
+        p.prompt = i < a.N;
+        p.pages = p.prompt ? a.prefix_pages + (int64_t)i * a.prefix_ld : a.suffix_pages + (int64_t)(i - a.N) * a.suffix_ld;
+        u += p.step1 - p.step0;
+        return true;
+    }
+};
 
 // A row of an item: which query it is and how many of the sequence's keys it sees.
 struct QueryRow {
@@ -93,20 +168,20 @@ struct QueryRow {
     int32_t limit;
 };
 
-__device__ __forceinline__ QueryRow query_row(const AttnArgs &a, const Sequence &s, bool prompt, int32_t h, int32_t x) {
+// Row x of a sequence and cache head h, for a sequence of `rows` rows and `len` keys whose first rollout is `first`.
+__device__ __forceinline__ QueryRow query_row(const AttnArgs &a, int32_t first, int32_t rows, int32_t len, bool prompt, int32_t h, int32_t x) {
     QueryRow q = {-1, 0};
-    if (x >= s.rows) return q;
+    if (x >= rows) return q;
     const int32_t per = a.T * a.g;
-    const int32_t r = s.first + x / per, rem = x % per, t = rem / a.g;
+    const int32_t r = first + x / per, rem = x % per, t = rem / a.g;
     const int32_t n = query_count(a, r);
     q.out = ((int64_t)r * a.T + t) * a.Hq + h * a.g + rem % a.g;
     if (t >= n) return q;
-    q.limit = prompt ? s.len : max(0, min(s.len, s.len - n + t + 1));
+    q.limit = prompt ? len : max(0, min(len, len - n + t + 1));
     return q;
 }
 
-hora_status_t launch_attention_plan(const AttnArgs &a, cudaStream_t stream);
-hora_status_t launch_attention_steps(const AttnArgs &a, int32_t q_dtype, int32_t cache_dtype, int32_t D, cudaStream_t stream);
-hora_status_t launch_attention_join(const AttnArgs &a, int32_t q_dtype, int32_t D, cudaStream_t stream);
+hora_status_t launch_attention_narrow(const AttnArgs &a, int32_t q_dtype, int32_t cache_dtype, int32_t D, cudaStream_t stream);
+hora_status_t launch_attention_wide(const AttnArgs &a, int32_t q_dtype, int32_t D, cudaStream_t stream);
 
 }  // namespace hora

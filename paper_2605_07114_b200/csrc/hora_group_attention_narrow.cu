@@ -1,4 +1,4 @@
-// hora_group_attention, the kernel for items of up to 16 query rows: decode of single tokens over long caches.
+// hora_group_attention, the kernel for narrow items, up to 16 query rows: decode of single tokens over long caches.
 //
 // The call is bound by the cache's bytes (16 rows or fewer to a key: at most 16 products a byte), so the tensor unit matters only in
 // that it has to be out of the way, and what counts is bytes in flight.  Every warp is a stream of its own, with its own
@@ -24,10 +24,10 @@
 
 namespace hora {
 
-constexpr int kStepThreads = 128;
-constexpr int kStepWarps = kStepThreads / kWarp;
+constexpr int kNarrowThreads = 128;
+constexpr int kNarrowWarps = kNarrowThreads / kWarp;
 constexpr int kRingBytes = 16384;                        // stages of one warp
-static_assert(kStepKeys == 16, "a step is one mma's worth of keys");
+static_assert(kNarrowKeys == 16, "a step is one mma's worth of keys");
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -78,9 +78,9 @@ __device__ __forceinline__ uint32_t lds1(uint32_t at) {
 template <bool F8, int D>
 struct Stage {
     static constexpr int kRowBytes = F8 ? D : 2 * D;
-    static constexpr int kHalf = kStepKeys * kRowBytes;                       // keys; values follow
+    static constexpr int kHalf = kNarrowKeys * kRowBytes;                       // keys; values follow
     static constexpr int kStages = kRingBytes / (2 * kHalf);
-    static constexpr int kExpBytes = F8 ? 2 * kStepKeys : 0;
+    static constexpr int kExpBytes = F8 ? 2 * kNarrowKeys : 0;
     static constexpr int kBytes = 2 * kHalf;
     static constexpr int kWarpBytes = kStages * (kBytes + kExpBytes);         // scale bytes of all stages behind the rows
     static constexpr int kChunks = kRowBytes / 16;
@@ -95,8 +95,8 @@ struct Stage {
 };
 
 template <typename Q, bool F8, int D>
-__global__ void __launch_bounds__(kStepThreads, kStreamsPerSm / kStepWarps)
-attention_rows_kernel(const AttnArgs a) {
+__global__ void __launch_bounds__(kNarrowThreads, kNarrowPerSm / kNarrowWarps)
+attention_narrow_kernel(const AttnArgs a) {
     pdl_enter();
     using M = std::conditional_t<F8, __half, Q>;                  // the type of the products
     using St = Stage<F8, D>;
@@ -109,53 +109,26 @@ attention_rows_kernel(const AttnArgs a) {
     const int n = lane >> 2, c = lane & 3;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + warp * St::kWarpBytes;
     const uint32_t exps = ring + kStages * St::kBytes;
-    const int32_t stream = blockIdx.x * kStepWarps + warp;
-    const int32_t n_seq = a.N + a.R;
-    const int64_t total = __ldg(a.start + n_seq);
-    const int64_t per = steps_per_stream(a);
+    const int32_t stream = blockIdx.x * kNarrowWarps + warp;
     const int64_t rows_all = (int64_t)a.R * a.T * a.Hq;
-    int64_t u = (int64_t)stream * per;
-    const int64_t u_end = min(total, u + per);
-    if (u >= u_end) return;
-
-    // the sequence that holds step u: the last i with start[i] <= u, 32 probes at a time
-    int32_t i = 0;
-    for (int32_t hi = n_seq; hi - i > 1;) {                       // start[i] <= u < start[hi]
-        const int32_t gap = (hi - i + kWarp - 1) / kWarp;
-        const int32_t probe = min(hi, i + lane * gap);
-        const unsigned at_or_before = __ballot_sync(kFull, probe < hi && __ldg(a.start + probe) <= u);
-        const int32_t top = 31 - __clz(at_or_before);             // lane 0 always is
-        hi = min(hi, i + (top + 1) * gap);
-        i += top * gap;
-    }
     bool bad = false;
-    Sequence s = sequence(a, i, bad);
-    int64_t s_start = __ldg(a.start + i);
+    Pieces<false> pieces(a, stream, bad);
+    Piece w;
 
     // where this lane reads: keys key_of(n), key_of(n) + 8 for the scores, and the two keys of columns 2c and 2c + 1 (and
     // those eight further on) for the product with the weights
     const int key_n = St::key_of(n), key_a = St::key_of(2 * c), key_b = St::key_of(2 * c + 1);
 
-    while (u < u_end) {
-        while (u >= s_start + (int64_t)s.steps * s.tiles * a.Hkv) {           // on to the next sequence that has steps
-            s_start += (int64_t)s.steps * s.tiles * a.Hkv;
-            ++i;
-            s = sequence(a, i, bad);
-        }
-        const int64_t item = (u - s_start) / s.steps;
-        const int32_t step0 = (int32_t)((u - s_start) - item * s.steps);
-        const int32_t step1 = (int32_t)min((int64_t)s.steps, step0 + (u_end - u));
-        const int32_t h = (int32_t)(item / s.tiles), tile = (int32_t)(item % s.tiles);
-        const bool prompt = i < a.N;
-        const int32_t *__restrict__ pages = prompt ? a.prefix_pages + (int64_t)i * a.prefix_ld
-                                                   : a.suffix_pages + (int64_t)(i - a.N) * a.suffix_ld;
+    while (pieces.next(a, w, bad)) {
+        const Sequence &s = pieces.s;
+        const int32_t step0 = w.step0, step1 = w.step1, h = w.h;
 
         // page numbers are looked up one step before the copies that need them
-        auto page_of = [&](int32_t step) { return step < step1 ? __ldg(pages + ((step * kStepKeys) >> a.page_shift)) : 0; };
+        auto page_of = [&](int32_t step) { return step < step1 ? __ldg(w.pages + ((step * kNarrowKeys) >> a.page_shift)) : 0; };
         auto fetch = [&](int32_t step, int32_t page) {
             if (step < step1) {
                 if (page < 0 || page >= a.n_pages) { bad = true; page = 0; }
-                const int64_t row = (((int64_t)page * a.Hkv + h) << a.page_shift) + ((step * kStepKeys) & ((1 << a.page_shift) - 1));
+                const int64_t row = (((int64_t)page * a.Hkv + h) << a.page_shift) + ((step * kNarrowKeys) & ((1 << a.page_shift) - 1));
                 const int slot = (step - step0) % kStages;
                 const uint32_t to = ring + slot * St::kBytes;
                 const uint8_t *__restrict__ k = static_cast<const uint8_t *>(a.k_cache) + row * St::kRowBytes + lane * 16;
@@ -170,7 +143,7 @@ attention_rows_kernel(const AttnArgs a) {
                     const int chunk = x * kWarp + lane;
                     copy16(to + St::kHalf + St::place(chunk / St::kChunks, chunk % St::kChunks), v + x * 512);
                 }
-                if (F8 && lane < 2) copy16(exps + slot * St::kExpBytes + lane * kStepKeys, (lane == 0 ? a.k_exp : a.v_exp) + row);
+                if (F8 && lane < 2) copy16(exps + slot * St::kExpBytes + lane * kNarrowKeys, (lane == 0 ? a.k_exp : a.v_exp) + row);
             }
             copies_done();                                        // a group for each step, empty ones too: the waits count groups
         };
@@ -182,8 +155,8 @@ attention_rows_kernel(const AttnArgs a) {
         int32_t page_next = page_of(step0 + kStages);
 
         // rows n and n + 8 of the tile are this lane's
-const QueryRow row0 = query_row(a, s, prompt, h, tile * kTileRows + n);
-        const QueryRow row1 = query_row(a, s, prompt, h, tile * kTileRows + n + 8);
+        const QueryRow row0 = query_row(a, s.first, s.rows, s.len, w.prompt, h, w.row0 + n);
+        const QueryRow row1 = query_row(a, s.first, s.rows, s.len, w.prompt, h, w.row0 + n + 8);
         uint32_t qf[2 * kBlocks * (F8 ? 2 : 1)][4];               // one mma step (16 dimensions) each
         float q_unit0 = 1.f, q_unit1 = 1.f;                       // what the stored queries have to be multiplied by
         {
@@ -240,7 +213,7 @@ const QueryRow row0 = query_row(a, s, prompt, h, tile * kTileRows + n);
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         float v_unit = 0.f;                                       // F8: o is in units of this (0: nothing added yet)
         for (int32_t step = step0; step < step1; ++step) {
-            const int32_t key = step * kStepKeys;
+            const int32_t key = step * kNarrowKeys;
             const int slot = (step - step0) % kStages;
             const uint32_t at_k = ring + slot * St::kBytes, at_v = at_k + St::kHalf;
             copies_wait<kStages - 1>();
@@ -251,18 +224,18 @@ const QueryRow row0 = query_row(a, s, prompt, h, tile * kTileRows + n);
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
                     const uint4 x = lds16(at_k + St::place(j * 8 + key_n, b * 4 + c));
-                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                    const uint32_t x4[4] = {x.x, x.y, x.z, x.w};
                     if constexpr (F8) {
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            mma16816(sc[j], qf[4 * b + e], e4m3x2_to_half2(w[e] & 0xFFFFu), e4m3x2_to_half2(w[e] >> 16), M());
+                            mma16816(sc[j], qf[4 * b + e], e4m3x2_to_half2(x4[e] & 0xFFFFu), e4m3x2_to_half2(x4[e] >> 16), M());
                     } else {
-                        mma16816(sc[j], qf[2 * b], w[0], w[1], M());
-                        mma16816(sc[j], qf[2 * b + 1], w[2], w[3], M());
+                        mma16816(sc[j], qf[2 * b], x4[0], x4[1], M());
+                        mma16816(sc[j], qf[2 * b + 1], x4[2], x4[3], M());
                     }
                 }
             // scores in units of log2, hidden keys at -infinity
-            const bool whole = key + kStepKeys <= min(row0.limit, row1.limit);
+            const bool whole = key + kNarrowKeys <= min(row0.limit, row1.limit);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -291,7 +264,7 @@ const QueryRow row0 = query_row(a, s, prompt, h, tile * kTileRows + n);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int k = (j >> 1) * 8 + ((j & 1) ? key_b : key_a);
-                    e4[j] = key + k < s.len ? exponent_byte(lds1(exps + slot * St::kExpBytes + kStepKeys + k)) : 0.f;
+                    e4[j] = key + k < s.len ? exponent_byte(lds1(exps + slot * St::kExpBytes + kNarrowKeys + k)) : 0.f;
                     top = fmaxf(top, e4[j]);
                 }
                 top = quad_max(top);                              // the same in all quads: they hold the same keys
@@ -359,8 +332,8 @@ const QueryRow row0 = query_row(a, s, prompt, h, tile * kTileRows + n);
         for (int half = 0; half < 2; ++half) {
             const int64_t out = half ? row1.out : row0.out;
             if (out < 0) continue;
-            const int64_t place = step0 > 0 ? (int64_t)stream * kTileRows + n + half * 8 : (prompt ? out : rows_all + out);
-            float *__restrict__ po = (step0 > 0 ? a.cont_o : a.main_o) + place * D;
+            const int64_t place = step0 > 0 ? (int64_t)stream * kNarrowRows + n + half * 8 : (w.prompt ? kPromptPart : kOwnPart) * rows_all + out;
+            float *__restrict__ po = (step0 > 0 ? a.cont_o[0] : a.main_o) + place * D;
             const float f = F8 ? v_unit : 1.f;
 #pragma unroll
             for (int part = 0; part < kOut / kRun; ++part)
@@ -371,30 +344,29 @@ const QueryRow row0 = query_row(a, s, prompt, h, tile * kTileRows + n);
                         *reinterpret_cast<float4 *>(po + part * 64 + (2 * c + x) * kRun + t) =
                             make_float4(o[part * kRun + t][2 * half + x] * f, o[part * kRun + t + 1][2 * half + x] * f,
                                         o[part * kRun + t + 2][2 * half + x] * f, o[part * kRun + t + 3][2 * half + x] * f);
-            if (c == 0) *reinterpret_cast<float2 *>((step0 > 0 ? a.cont_ml : a.main_ml) + place * 2) = make_float2(half ? m1 : m0, half ? l1 : l0);
+            if (c == 0) *reinterpret_cast<float2 *>((step0 > 0 ? a.cont_ml[0] : a.main_ml) + place * 2) = make_float2(half ? m1 : m0, half ? l1 : l0);
         }
-        u += step1 - step0;
     }
     if (bad) raise_status(a.status, HORA_ERR_INVALID_VALUE);
 }
 
 template <typename Q, bool F8, int D>
-static hora_status_t launch_rows(const AttnArgs &a, cudaStream_t stream) {
-    constexpr int kSmem = kStepWarps * Stage<F8, D>::kWarpBytes;
-    cudaError_t e = cudaFuncSetAttribute(attention_rows_kernel<Q, F8, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    if (e == cudaSuccess) e = launch_pdl(attention_rows_kernel<Q, F8, D>, a.n_streams / kStepWarps, kStepThreads, kSmem, stream, a);
+static hora_status_t launch_narrow(const AttnArgs &a, cudaStream_t stream) {
+    constexpr int kSmem = kNarrowWarps * Stage<F8, D>::kWarpBytes;
+    cudaError_t e = cudaFuncSetAttribute(attention_narrow_kernel<Q, F8, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e == cudaSuccess) e = launch_pdl(attention_narrow_kernel<Q, F8, D>, a.n_narrow / kNarrowWarps, kNarrowThreads, kSmem, stream, a);
     count_launches(1);
     return cuda_ok(e);
 }
 
-hora_status_t launch_attention_steps(const AttnArgs &a, int32_t q_dtype, int32_t cache_dtype, int32_t D, cudaStream_t stream) {
+hora_status_t launch_attention_narrow(const AttnArgs &a, int32_t q_dtype, int32_t cache_dtype, int32_t D, cudaStream_t stream) {
     const bool bf = q_dtype == HORA_DTYPE_BF16;
     if (cache_dtype == HORA_DTYPE_E4M3) {
-        if (D == 64) return bf ? launch_rows<__nv_bfloat16, true, 64>(a, stream) : launch_rows<__half, true, 64>(a, stream);
-        return bf ? launch_rows<__nv_bfloat16, true, 128>(a, stream) : launch_rows<__half, true, 128>(a, stream);
+        if (D == 64) return bf ? launch_narrow<__nv_bfloat16, true, 64>(a, stream) : launch_narrow<__half, true, 64>(a, stream);
+        return bf ? launch_narrow<__nv_bfloat16, true, 128>(a, stream) : launch_narrow<__half, true, 128>(a, stream);
     }
-    if (D == 64) return bf ? launch_rows<__nv_bfloat16, false, 64>(a, stream) : launch_rows<__half, false, 64>(a, stream);
-    return bf ? launch_rows<__nv_bfloat16, false, 128>(a, stream) : launch_rows<__half, false, 128>(a, stream);
+    if (D == 64) return bf ? launch_narrow<__nv_bfloat16, false, 64>(a, stream) : launch_narrow<__half, false, 64>(a, stream);
+    return bf ? launch_narrow<__nv_bfloat16, false, 128>(a, stream) : launch_narrow<__half, false, 128>(a, stream);
 }
 
 }  // namespace hora
