@@ -4,6 +4,8 @@
 namespace hora {
 
 constexpr int kPlanThreads = 1024;
+constexpr int kPlanKept = 4;                             // sequences of a thread whose steps it keeps in registers
+constexpr int kPlanOffsets = 4096;                       // group offsets kept in shared memory for the searches
 constexpr int kWideFrom = 33;
 
 // start[line][i] = steps before sequence i on its line, group_of[r].  One CTA: every thread takes a run of sequences.
@@ -11,14 +13,30 @@ __global__ void __launch_bounds__(kPlanThreads)
 attention_plan_kernel(const AttnArgs a) {
     pdl_enter();
     __shared__ int64_t s_warp[2][kPlanThreads / kWarp];
+    __shared__ int64_t s_off[kPlanOffsets];
     const int64_t n = (int64_t)a.N + a.R;
     const int64_t each = (n + kPlanThreads - 1) / kPlanThreads;
     const int64_t lo = min(n, each * threadIdx.x), hi = min(n, lo + each);
     bool bad = false;
-    int64_t sum[2] = {0, 0}, run[2];
-    for (int64_t i = lo; i < hi; ++i) {
+    int64_t sum[2] = {0, 0}, run[2], kept[kPlanKept];
+    bool kept_wide[kPlanKept];
+    const bool in_shared = a.N + 1 <= kPlanOffsets;
+    if (in_shared)
+        for (int32_t i = threadIdx.x; i <= a.N; i += kPlanThreads) s_off[i] = __ldg(a.group_offsets + i);
+#pragma unroll
+    for (int x = 0; x < kPlanKept; ++x) {
+        kept[x] = 0;
+        kept_wide[x] = false;
+        if (lo + x < hi) {
+            const Sequence s = sequence(a, (int32_t)(lo + x), bad);
+            kept[x] = total_steps(a, s);
+            kept_wide[x] = s.wide;
+            sum[s.wide] += kept[x];
+        }
+    }
+    for (int64_t i = lo + kPlanKept; i < hi; ++i) {
         const Sequence s = sequence(a, (int32_t)i, bad);
-        (s.wide ? sum[1] : sum[0]) += total_steps(a, s);
+        sum[s.wide] += total_steps(a, s);
     }
     const int lane = lane_id(), warp = threadIdx.x >> 5;
 #pragma unroll
@@ -33,15 +51,27 @@ attention_plan_kernel(const AttnArgs a) {
         run[w] = incl - sum[w];
     }
     __syncthreads();
+    // this warp's sums before it: lane x has warp x's
 #pragma unroll
-    for (int w = 0; w < 2; ++w)
-        for (int x = 0; x < warp; ++x) run[w] += s_warp[w][x];
-    for (int64_t i = lo; i < hi; ++i) {
+    for (int w = 0; w < 2; ++w) {
+        int64_t before = lane < warp ? s_warp[w][lane] : 0;
+#pragma unroll
+        for (int d = kWarp / 2; d > 0; d >>= 1) before += __shfl_xor_sync(kFull, before, d);
+        run[w] += before;
+    }
+#pragma unroll
+    for (int x = 0; x < kPlanKept; ++x)
+        if (lo + x < hi) {
+            a.start[0][lo + x] = run[0];
+            a.start[1][lo + x] = run[1];
+            run[kept_wide[x]] += kept[x];
+        }
+    for (int64_t i = lo + kPlanKept; i < hi; ++i) {
         a.start[0][i] = run[0];
         a.start[1][i] = run[1];
         bool again = false;
         const Sequence s = sequence(a, (int32_t)i, again);
-        (s.wide ? run[1] : run[0]) += total_steps(a, s);
+        run[s.wide] += total_steps(a, s);
     }
     if (threadIdx.x == kPlanThreads - 1) {
         a.start[0][n] = run[0];
@@ -54,7 +84,7 @@ attention_plan_kernel(const AttnArgs a) {
             int32_t l = 0, h = a.N - 1;                  // the last group that begins at or before r
             while (l < h) {
                 const int32_t mid = (l + h + 1) >> 1;
-                if (__ldg(a.group_offsets + mid) <= r) l = mid;
+                if ((in_shared ? s_off[mid] : __ldg(a.group_offsets + mid)) <= r) l = mid;
                 else h = mid - 1;
             }
             g = l;
@@ -64,27 +94,50 @@ attention_plan_kernel(const AttnArgs a) {
     if (bad) raise_status(a.status, HORA_ERR_INVALID_VALUE);
 }
 
-// Joins the partials of one output row; a warp to a row, D / 32 neighbouring elements a lane.
-template <int E>
-struct Joined {
-    float m = -INFINITY, l = 0.f, o[E] = {};
+// Division of step numbers: 64-bit only where they need it.
+__device__ __forceinline__ int32_t stream_of(int64_t u, int64_t per) {
+    return ((u | per) >> 32) == 0 ? (int32_t)((uint32_t)u / (uint32_t)per) : (int32_t)(u / per);
+}
 
-    __device__ __forceinline__ void add(float m2, float l2, const float *__restrict__ p, int lane) {
-        if (m2 == -INFINITY) return;                     // no key of that part is seen
-        const float top = fmaxf(m, m2), f = exp2f(m - top), f2 = exp2f(m2 - top);
-        l = l * f + l2 * f2;
-        float x[E];
-#pragma unroll
-        for (int e = 0; e < E; e += 2) {
-            const float2 y = __ldcs(reinterpret_cast<const float2 *>(p + lane * E + e));
-            x[e] = y.x;
-            x[e + 1] = y.y;
+// Where the partials of one row and one of its two sequences are.
+struct Parts {
+    int64_t main;                                        // place among the main ones
+    uint32_t cont, count, halves;                        // first continued row, partials of a half, halves
+    bool wide;
+
+    // partial x of count * halves
+    __device__ __forceinline__ void at(const AttnArgs &a, int64_t rows, uint32_t x, int32_t D, const float *&ml, const float *&o) const {
+        const uint32_t half = x >= count ? 1 : 0, b = x - half * count;
+        if (b == 0) {
+            const int64_t place = main + (int64_t)half * kSecondHalf * rows;
+            ml = a.main_ml + place * 2;
+            o = a.main_o + place * D;
+        } else {
+            const int64_t place = (int64_t)cont + (int64_t)(b - 1) * (wide ? kWideRows : kNarrowRows) + half * kWideHalf;
+            ml = a.cont_ml[wide] + place * 2;
+            o = a.cont_o[wide] + place * D;
         }
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] = o[e] * f + x[e] * f2;
-        m = top;
     }
 };
+
+__device__ __forceinline__ Parts parts_of(const AttnArgs &a, const Sequence &q, int64_t start, int64_t per, int32_t part, uint32_t r, uint32_t t, uint32_t head,
+                                          int64_t row, int64_t rows) {
+    Parts p = {part * rows + row, 0u, 0u, 1u, q.wide};
+    if (q.steps == 0 || (int32_t)r < q.first || (int32_t)r >= q.first + q.rollouts) return p;
+    const uint32_t x = ((r - q.first) * a.T + t) * a.g + head % a.g, tile = x / (uint32_t)q.tile_rows, at = x - tile * q.tile_rows;
+    const int64_t u0 = start + ((int64_t)(head / a.g) * q.tiles + tile) * q.steps;
+    const int32_t b0 = stream_of(u0, per);
+    const int64_t last = u0 - b0 * per + q.steps - 1;
+    p.count = 1 + (last < per ? 0 : stream_of(last, per));
+    // a wide item of one half has its keys dealt to two halves, each with a partial of its own
+    p.halves = q.wide && min(q.tile_rows, q.rows - (int32_t)tile * q.tile_rows) <= kWideHalf ? 2 : 1;
+    p.cont = (uint32_t)(b0 + 1) * (q.wide ? kWideRows : kNarrowRows) + at;
+    return p;
+}
+
+// Joins the partials of an output row, a warp to a row, D / 32 neighbouring elements a lane.  Partials are taken kJoinAtOnce at a
+// time, all their loads in flight together: what bounds the kernel is the chain rollout -> group -> sequence -> partial.
+constexpr int kJoinAtOnce = 4;
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256)
@@ -92,45 +145,69 @@ attention_join_kernel(const AttnArgs a) {
     pdl_enter();
     constexpr int E = D / kWarp;
     const int lane = lane_id();
-    const int64_t rows = (int64_t)a.R * a.T * a.Hq;
-    const int64_t row = (int64_t)blockIdx.x * (blockDim.x / kWarp) + (threadIdx.x >> 5);
-    if (row >= rows) return;
-    const int32_t head = (int32_t)(row % a.Hq);
-    const int64_t rt = row / a.Hq;
-    const int32_t r = (int32_t)(rt / a.T), t = (int32_t)(rt % a.T), h = head / a.g;
-    Joined<E> j;
-    const int32_t grp = a.group_of[r];
-    if (grp >= 0 && t < query_count(a, r)) {
+    const uint32_t n_rows = (uint32_t)a.R * a.T * a.Hq, row = blockIdx.x * (blockDim.x / kWarp) + (threadIdx.x >> 5);
+    if (row >= n_rows) return;
+    const uint32_t rt = row / a.Hq, head = row - rt * a.Hq, r = rt / a.T, t = rt - r * a.T;
+    const int64_t rows = n_rows;
+    const int32_t grp = __ldg(a.group_of + r);
+    float m = -INFINITY, l = 0.f, o[E] = {};
+    if (grp >= 0 && (int32_t)t < query_count(a, r)) {
         bool bad = false;
+        const Sequence own = sequence(a, a.N + r, bad), prompt = sequence(a, grp, bad);
+        const int64_t per_narrow = steps_per_stream<false>(a), per_wide = a.n_wide > 0 ? steps_per_stream<true>(a) : 1;
+        const Parts p0 = parts_of(a, prompt, __ldg((prompt.wide ? a.start[1] : a.start[0]) + grp), prompt.wide ? per_wide : per_narrow, kPromptPart, r, t, head, row, rows);
+        const Parts p1 = parts_of(a, own, __ldg((own.wide ? a.start[1] : a.start[0]) + a.N + r), own.wide ? per_wide : per_narrow, kOwnPart, r, t, head, row, rows);
+        const uint32_t n0 = p0.count * p0.halves, n = n0 + p1.count * p1.halves;
+        for (uint32_t x0 = 0; x0 < n; x0 += kJoinAtOnce) {
+            float2 ml[kJoinAtOnce];
+            float y[kJoinAtOnce][E];
 #pragma unroll
-        for (int part = 0; part < 2; ++part) {
-            const int32_t i = part == kPromptPart ? grp : a.N + r;
-            const Sequence s = sequence(a, i, bad);
-            if (s.steps == 0 || r < s.first || r >= s.first + s.rollouts) continue;
-            const int32_t x = ((r - s.first) * a.T + t) * a.g + head % a.g;
-            const int32_t tile = x / s.tile_rows, at = x % s.tile_rows;
-            const int64_t u0 = __ldg(a.start[s.wide] + i) + ((int64_t)h * s.tiles + tile) * s.steps;
-            const int64_t per = s.wide ? steps_per_stream<true>(a) : steps_per_stream<false>(a);
-            // a wide item of one half has its keys dealt to two halves, each with a partial of its own
-            const int halves = s.wide && min(s.tile_rows, s.rows - tile * s.tile_rows) <= kWideHalf ? 2 : 1;
-            const int32_t b0 = (int32_t)(u0 / per), b1 = (int32_t)((u0 + s.steps - 1) / per);
-            for (int half = 0; half < halves; ++half) {
-                const int64_t place = (part + half * kSecondHalf) * rows + row;
-                const float2 ml = *reinterpret_cast<const float2 *>(a.main_ml + place * 2);
-                j.add(ml.x, ml.y, a.main_o + place * D, lane);
-                for (int32_t b = b0 + 1; b <= b1; ++b) {
-                    const int64_t c = (int64_t)b * (s.wide ? kWideRows : kNarrowRows) + half * kWideHalf + at;
-                    const float2 ml2 = *reinterpret_cast<const float2 *>(a.cont_ml[s.wide] + c * 2);
-                    j.add(ml2.x, ml2.y, a.cont_o[s.wide] + c * D, lane);
+            for (int x = 0; x < kJoinAtOnce; ++x) {
+                ml[x] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+                for (int e = 0; e < E; ++e) y[x][e] = 0.f;
+                if (x0 + x < n) {
+                    const float *pml, *po;
+                    if (x0 + x < n0) p0.at(a, rows, x0 + x, D, pml, po);
+                    else p1.at(a, rows, x0 + x - n0, D, pml, po);
+                    ml[x] = __ldcg(reinterpret_cast<const float2 *>(pml));
+                    if constexpr (E == 4) {
+                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(po) + lane);
+                        y[x][0] = v.x; y[x][1] = v.y; y[x][2] = v.z; y[x][3] = v.w;
+                    } else {
+                        const float2 v = __ldcg(reinterpret_cast<const float2 *>(po) + lane);
+                        y[x][0] = v.x; y[x][1] = v.y;
+                    }
                 }
+            }
+            float top = m;
+#pragma unroll
+            for (int x = 0; x < kJoinAtOnce; ++x) top = fmaxf(top, ml[x].x);
+            if (top == -INFINITY) continue;              // no key seen so far
+            const float f = exp2_fast(m - top);
+            l *= f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] *= f;
+            m = top;
+#pragma unroll
+            for (int x = 0; x < kJoinAtOnce; ++x) {
+                const bool none = ml[x].x == -INFINITY;  // its output may not have been written
+                const float g = exp2_fast(ml[x].x - top);
+                if (!none) l += ml[x].y * g;
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (!none) o[e] += y[x][e] * g;
             }
         }
     }
-    const float inv = j.l > 0.f ? 1.f / j.l : (j.m == -INFINITY ? 0.f : 1.f / j.l);
-    T *__restrict__ out = static_cast<T *>(a.out) + rt * a.out_row_stride + (int64_t)head * D + lane * E;
+    const float inv = m == -INFINITY ? 0.f : 1.f / l;
+    uint32_t w[E / 2];
 #pragma unroll
-    for (int e = 0; e < E; e += 2) *reinterpret_cast<uint32_t *>(out + e) = pack2(j.o[e] * inv, j.o[e + 1] * inv, T());
-    if (a.lse != nullptr && lane == 0) a.lse[row] = j.m == -INFINITY ? -INFINITY : 0.6931471805599453f * j.m + logf(j.l);
+    for (int e = 0; e < E; e += 2) w[e / 2] = pack2(o[e] * inv, o[e + 1] * inv, T());
+    T *__restrict__ out = static_cast<T *>(a.out) + rt * a.out_row_stride + (int64_t)head * D + lane * E;
+    if constexpr (E == 4) *reinterpret_cast<uint2 *>(out) = make_uint2(w[0], w[1]);
+    else *reinterpret_cast<uint32_t *>(out) = w[0];
+    if (a.lse != nullptr && lane == 0) a.lse[row] = m == -INFINITY ? -INFINITY : 0.6931471805599453f * m + logf(l);
 }
 
 static hora_status_t launch_plan(const AttnArgs &a, cudaStream_t stream) {
@@ -249,6 +326,7 @@ extern "C" hora_status_t hora_group_attention(const void *q, int32_t q_dtype, in
     a.scale_log2 = sm_scale * 1.4426950408889634f;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (cache_dtype == HORA_DTYPE_E4M3) a.n_wide = 0;
+    a.narrow_keys = narrow_keys(cache_dtype == HORA_DTYPE_E4M3, D);
     a.wide_from = kWideFrom;
     hora_status_t rc = launch_plan(a, s);
     if (rc == HORA_OK) rc = launch_attention_narrow(a, q_dtype, cache_dtype, D, s);

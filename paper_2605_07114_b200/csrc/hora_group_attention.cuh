@@ -19,7 +19,8 @@
 namespace hora {
 
 constexpr int kNarrowRows = 16;                          // query rows of a narrow item
-constexpr int kNarrowKeys = 16;                          // keys of its steps
+// keys of its steps: 16 where that is 8 KiB, else 32 (twice the independent work between two looks at the maximum)
+constexpr int narrow_keys(bool f8, int D) { return !f8 && D == 128 ? 16 : 32; }
 constexpr int kNarrowPerSm = 12;                         // streams an SM: 168 registers a lane, 16 KiB of keys and values in flight each
 constexpr int kNarrowMinSteps = 4;                       // a stream shorter than this costs more to join than it saves
 
@@ -42,6 +43,7 @@ struct AttnArgs {
     int64_t q_row_stride, out_row_stride, n_pages;
     int32_t N, R, T, Hq, Hkv, g, page_shift, prefix_ld, suffix_ld;
     int32_t n_narrow, n_wide;                            // streams; n_wide 0: every sequence is narrow
+    int32_t narrow_keys;                                 // keys of a narrow step
     int32_t wide_from;                                   // rows from which a sequence is wide
     float scale_log2;                                    // sm_scale * log2(e)
     // workspace
@@ -57,6 +59,12 @@ struct Sequence {
     int32_t rows, len, steps, tiles, tile_rows;
     bool wide;
 };
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
 __device__ __forceinline__ int32_t clamp_i64(int64_t v, int32_t lo, int32_t hi) { return v < lo ? lo : (v > hi ? hi : (int32_t)v); }
 
@@ -95,7 +103,7 @@ __device__ __forceinline__ Sequence sequence(const AttnArgs &a, int32_t i, bool 
     } else {
         s.tiles = (s.rows + kNarrowRows - 1) / kNarrowRows;
         s.tile_rows = kNarrowRows;
-        s.steps = (s.len + kNarrowKeys - 1) / kNarrowKeys;
+        s.steps = (s.len + a.narrow_keys - 1) / a.narrow_keys;
     }
     return s;
 }

@@ -2,7 +2,7 @@
 //
 // The call is bound by the cache's bytes (16 rows or fewer to a key: at most 16 products a byte), so the tensor unit matters only in
 // that it has to be out of the way, and what counts is bytes in flight.  Every warp is a stream of its own, with its own
-// running maximum, sum and output and its own ring of stages in shared memory: a stage is sixteen keys and values, fetched by
+// running maximum, sum and output and its own ring of stages in shared memory: a stage is the keys and values of a step, fetched by
 // cp.async (16 KiB of stages a warp, twelve warps an SM: up to 192 KiB in flight, several times what 6.5 TB/s needs at
 // the latency of HBM under load).  No barrier joins the warps, and none waits for another.
 //
@@ -27,7 +27,6 @@ namespace hora {
 constexpr int kNarrowThreads = 128;
 constexpr int kNarrowWarps = kNarrowThreads / kWarp;
 constexpr int kRingBytes = 16384;                        // stages of one warp
-static_assert(kNarrowKeys == 16, "a step is one mma's worth of keys");
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -78,16 +77,17 @@ __device__ __forceinline__ uint32_t lds1(uint32_t at) {
 template <bool F8, int D>
 struct Stage {
     static constexpr int kRowBytes = F8 ? D : 2 * D;
-    static constexpr int kHalf = kNarrowKeys * kRowBytes;                       // keys; values follow
+    static constexpr int kKeys = narrow_keys(F8, D);
+    static constexpr int kHalf = kKeys * kRowBytes;                           // keys; values follow
     static constexpr int kStages = kRingBytes / (2 * kHalf);
-    static constexpr int kExpBytes = F8 ? 2 * kNarrowKeys : 0;
+    static constexpr int kExpBytes = F8 ? 2 * kKeys : 0;
     static constexpr int kBytes = 2 * kHalf;
     static constexpr int kWarpBytes = kStages * (kBytes + kExpBytes);         // scale bytes of all stages behind the rows
     static constexpr int kChunks = kRowBytes / 16;
 
-    // place of 16-byte chunk `chunk` of row `row` (both below 16)
+    // place of 16-byte chunk `chunk` of row `row`
     static __device__ __forceinline__ uint32_t place(int row, int chunk) {
-        if constexpr (kRowBytes == 64) return (row >> 1) * 128 + ((((row & 1) * 4 + chunk) ^ ((row & 6))) << 4);
+        if constexpr (kRowBytes == 64) return (row >> 1) * 128 + ((((row & 1) * 4 + chunk) ^ (row & 6)) << 4);
         else return row * kRowBytes + ((chunk ^ (row & 7)) << 4);
     }
     // key that column n (below 8) of a score tile stands for
@@ -103,7 +103,7 @@ attention_narrow_kernel(const AttnArgs a) {
     constexpr int kBlocks = F8 ? D / 64 : D / 32;                 // 16-byte loads of a lane for each key in K
     constexpr int kHalves = F8 ? 1 : D / 64;                      // and for each key in V (one-byte values, D = 64: 8 bytes)
     constexpr int kOut = D / 8;                                   // column tiles of the output
-    constexpr int kStages = St::kStages;
+    constexpr int kStages = St::kStages, kKeys = St::kKeys, kEights = kKeys / 8, kSixteens = kKeys / 16;
     extern __shared__ __align__(128) uint8_t s_ring[];
     const int lane = lane_id(), warp = threadIdx.x >> 5;
     const int n = lane >> 2, c = lane & 3;
@@ -124,35 +124,50 @@ attention_narrow_kernel(const AttnArgs a) {
         const int32_t step0 = w.step0, step1 = w.step1, h = w.h;
 
         // page numbers are looked up one step before the copies that need them
-        auto page_of = [&](int32_t step) { return step < step1 ? __ldg(w.pages + ((step * kNarrowKeys) >> a.page_shift)) : 0; };
-        auto fetch = [&](int32_t step, int32_t page) {
+        struct Ids { int32_t id[kSixteens]; };
+        auto pages_of = [&](int32_t step) {
+            Ids p;
+#pragma unroll
+            for (int y = 0; y < kSixteens; ++y) {
+                const int32_t key = step * kKeys + y * 16;
+                p.id[y] = step < step1 && key < s.len ? __ldg(w.pages + (key >> a.page_shift)) : 0;
+            }
+            return p;
+        };
+        auto fetch = [&](int32_t step, const Ids &p) {
             if (step < step1) {
-                if (page < 0 || page >= a.n_pages) { bad = true; page = 0; }
-                const int64_t row = (((int64_t)page * a.Hkv + h) << a.page_shift) + ((step * kNarrowKeys) & ((1 << a.page_shift) - 1));
                 const int slot = (step - step0) % kStages;
                 const uint32_t to = ring + slot * St::kBytes;
-                const uint8_t *__restrict__ k = static_cast<const uint8_t *>(a.k_cache) + row * St::kRowBytes + lane * 16;
-                const uint8_t *__restrict__ v = static_cast<const uint8_t *>(a.v_cache) + row * St::kRowBytes + lane * 16;
 #pragma unroll
-                for (int x = 0; x < St::kHalf / 512; ++x) {
-                    const int chunk = x * kWarp + lane;
-                    copy16(to + St::place(chunk / St::kChunks, chunk % St::kChunks), k + x * 512);
-                }
+                for (int y = 0; y < kSixteens; ++y) {             // sixteen keys lie in one page, one after the other
+                    const int32_t key = step * kKeys + y * 16;
+                    if (key >= s.len) break;
+                    int32_t page = p.id[y];
+                    if (page < 0 || page >= a.n_pages) { bad = true; page = 0; }
+                    const int64_t row = (((int64_t)page * a.Hkv + h) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
+                    const uint8_t *__restrict__ k = static_cast<const uint8_t *>(a.k_cache) + row * St::kRowBytes + lane * 16;
+                    const uint8_t *__restrict__ v = static_cast<const uint8_t *>(a.v_cache) + row * St::kRowBytes + lane * 16;
 #pragma unroll
-                for (int x = 0; x < St::kHalf / 512; ++x) {
-                    const int chunk = x * kWarp + lane;
-                    copy16(to + St::kHalf + St::place(chunk / St::kChunks, chunk % St::kChunks), v + x * 512);
+                    for (int x = 0; x < St::kRowBytes / 32; ++x) {
+                        const int chunk = x * kWarp + lane;
+                        copy16(to + St::place(y * 16 + chunk / St::kChunks, chunk % St::kChunks), k + x * 512);
+                    }
+#pragma unroll
+                    for (int x = 0; x < St::kRowBytes / 32; ++x) {
+                        const int chunk = x * kWarp + lane;
+                        copy16(to + St::kHalf + St::place(y * 16 + chunk / St::kChunks, chunk % St::kChunks), v + x * 512);
+                    }
+                    if (F8 && lane < 2) copy16(exps + slot * St::kExpBytes + lane * kKeys + y * 16, (lane == 0 ? a.k_exp : a.v_exp) + row);
                 }
-                if (F8 && lane < 2) copy16(exps + slot * St::kExpBytes + lane * kNarrowKeys, (lane == 0 ? a.k_exp : a.v_exp) + row);
             }
             copies_done();                                        // a group for each step, empty ones too: the waits count groups
         };
-        int32_t page[kStages];
+        Ids page[kStages];
 #pragma unroll
-        for (int x = 0; x < kStages; ++x) page[x] = page_of(step0 + x);
+        for (int x = 0; x < kStages; ++x) page[x] = pages_of(step0 + x);
 #pragma unroll
         for (int x = 0; x < kStages; ++x) fetch(step0 + x, page[x]);
-        int32_t page_next = page_of(step0 + kStages);
+        Ids page_next = pages_of(step0 + kStages);
 
         // rows n and n + 8 of the tile are this lane's
         const QueryRow row0 = query_row(a, s.first, s.rows, s.len, w.prompt, h, w.row0 + n);
@@ -213,14 +228,14 @@ attention_narrow_kernel(const AttnArgs a) {
         float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
         float v_unit = 0.f;                                       // F8: o is in units of this (0: nothing added yet)
         for (int32_t step = step0; step < step1; ++step) {
-            const int32_t key = step * kNarrowKeys;
+            const int32_t key = step * kKeys;
             const int slot = (step - step0) % kStages;
-            const uint32_t at_k = ring + slot * St::kBytes, at_v = at_k + St::kHalf;
+            const uint32_t at_k = ring + slot * St::kBytes, at_v = at_k + St::kHalf, at_ke = exps + slot * St::kExpBytes, at_ve = at_ke + kKeys;
             copies_wait<kStages - 1>();
             __syncwarp();
-            float sc[2][4] = {};
+            float sc[kEights][4] = {};                            // eight keys each
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < kEights; ++j)
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
                     const uint4 x = lds16(at_k + St::place(j * 8 + key_n, b * 4 + c));
@@ -235,93 +250,117 @@ attention_narrow_kernel(const AttnArgs a) {
                     }
                 }
             // scores in units of log2, hidden keys at -infinity
-            const bool whole = key + kNarrowKeys <= min(row0.limit, row1.limit);
+            const bool whole = key + kKeys <= min(row0.limit, row1.limit);
+            float top0 = -INFINITY, top1 = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
+            for (int j = 0; j < kEights; ++j) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int k = j * 8 + ((e & 1) ? key_b : key_a);
-                    float f = e < 2 ? to_log2_0 : to_log2_1;
-                    if constexpr (F8) f *= exponent_byte(lds1(exps + slot * St::kExpBytes + k));
-                    sc[j][e] *= f;
-                    if (!whole && key + k >= (e < 2 ? row0.limit : row1.limit)) sc[j][e] = -INFINITY;
-                }
-            const float top0 = fmaxf(m0, quad_max(fmaxf(fmaxf(sc[0][0], sc[0][1]), fmaxf(sc[1][0], sc[1][1]))));
-            const float top1 = fmaxf(m1, quad_max(fmaxf(fmaxf(sc[0][2], sc[0][3]), fmaxf(sc[1][2], sc[1][3]))));
-            // where no key has been seen the maximum is -infinity and every weight has to come out as 0
-            const float z0 = top0 == -INFINITY ? 0.f : top0, z1 = top1 == -INFINITY ? 0.f : top1;
-            float f0 = exp2f(m0 - z0), f1 = exp2f(m1 - z1);
-            m0 = top0;
-            m1 = top1;
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) sc[j][e] = exp2f(sc[j][e] - (e < 2 ? z0 : z1));
-            l0 = l0 * f0 + ((sc[0][0] + sc[0][1]) + (sc[1][0] + sc[1][1]));
-            l1 = l1 * f1 + ((sc[0][2] + sc[0][3]) + (sc[1][2] + sc[1][3]));
-            if constexpr (F8) {
-                float e4[4], top = v_unit;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int k = (j >> 1) * 8 + ((j & 1) ? key_b : key_a);
-                    e4[j] = key + k < s.len ? exponent_byte(lds1(exps + slot * St::kExpBytes + kNarrowKeys + k)) : 0.f;
-                    top = fmaxf(top, e4[j]);
-                }
-                top = quad_max(top);                              // the same in all quads: they hold the same keys
-                const float inv = 1.f / top;                      // powers of two; at least one key is within the length
-                f0 *= v_unit * inv;
-                f1 *= v_unit * inv;
-                v_unit = top;
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[j][e] *= e4[2 * j + (e & 1)] * inv;
-            }
-#pragma unroll
-            for (int t = 0; t < kOut; ++t) { o[t][0] *= f0; o[t][1] *= f0; o[t][2] *= f1; o[t][3] *= f1; }
-            const uint32_t p[4] = {pack2(sc[0][0], sc[0][1], M()), pack2(sc[0][2], sc[0][3], M()),
-                                   pack2(sc[1][0], sc[1][1], M()), pack2(sc[1][2], sc[1][3], M())};
-#pragma unroll
-            for (int b = 0; b < kHalves; ++b) {
-                uint32_t v[4][4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int k = (j >> 1) * 8 + ((j & 1) ? key_b : key_a);
-                    uint4 x;
-                    if constexpr (F8 && D == 64) {
-                        const uint2 y = lds8(at_v + St::place(k, n >> 1) + (n & 1) * 8);
-                        x = make_uint4(y.x, y.y, 0u, 0u);
-                    } else {
-                        x = lds16(at_v + St::place(k, b * 8 + n));
+                for (int x = 0; x < 2; ++x) {
+                    const int k = j * 8 + (x ? key_b : key_a);
+                    const float f = F8 ? exponent_byte(lds1(at_ke + k)) : 1.f;
+                    sc[j][x] *= F8 ? to_log2_0 * f : to_log2_0;
+                    sc[j][2 + x] *= F8 ? to_log2_1 * f : to_log2_1;
+                    if (!whole) {
+                        if (key + k >= row0.limit) sc[j][x] = -INFINITY;
+                        if (key + k >= row1.limit) sc[j][2 + x] = -INFINITY;
                     }
-                    // what lies beyond the length may be anything, and 0 * NaN is not 0
-                    const bool in = key + k < s.len;
-                    v[j][0] = in ? x.x : 0u;
-                    v[j][1] = in ? x.y : 0u;
-                    v[j][2] = in ? x.z : 0u;
-                    v[j][3] = in ? x.w : 0u;
                 }
+                top0 = fmaxf(top0, fmaxf(sc[j][0], sc[j][1]));
+                top1 = fmaxf(top1, fmaxf(sc[j][2], sc[j][3]));
+            }
+            float e4[kEights][2], v_top = v_unit;
+            if constexpr (F8) {
+#pragma unroll
+                for (int j = 0; j < kEights; ++j)
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const int k = j * 8 + (x ? key_b : key_a);
+                        e4[j][x] = key + k < s.len ? exponent_byte(lds1(at_ve + k)) : 0.f;
+                        v_top = fmaxf(v_top, e4[j][x]);
+                    }
+            }
+            // The reference of a row is raised when a score exceeds it by 2^8: weights up to 256 are as exact as weights up
+            // to 1, and the output is hardly ever rescaled.
+            if (__any_sync(kFull, top0 > m0 + 8.f || top1 > m1 + 8.f || (F8 && v_top > v_unit))) {
+                const float up0 = fmaxf(m0, quad_max(top0)), up1 = fmaxf(m1, quad_max(top1));
+                float f0 = up0 == -INFINITY ? 0.f : exp2_fast(m0 - up0), f1 = up1 == -INFINITY ? 0.f : exp2_fast(m1 - up1);
+                m0 = up0;
+                m1 = up1;
+                l0 *= f0;
+                l1 *= f1;
+                if constexpr (F8) {
+                    v_top = quad_max(v_top);                      // the same in all quads: they hold the same keys
+                    f0 *= v_unit / v_top;                         // powers of two; at least one key is within the length
+                    f1 *= v_unit / v_top;
+                    v_unit = v_top;
+                }
+#pragma unroll
+                for (int t = 0; t < kOut; ++t) { o[t][0] *= f0; o[t][1] *= f0; o[t][2] *= f1; o[t][3] *= f1; }
+            }
+            // where no key has been seen the reference is -infinity and every weight has to come out as 0
+            const float z0 = m0 == -INFINITY ? 0.f : m0, z1 = m1 == -INFINITY ? 0.f : m1;
+            const float v_inv = F8 ? 1.f / v_unit : 1.f;
+#pragma unroll
+            for (int j = 0; j < kEights; ++j) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[j][e] = exp2_fast(sc[j][e] - (e < 2 ? z0 : z1));
+                l0 += sc[j][0] + sc[j][1];
+                l1 += sc[j][2] + sc[j][3];
                 if constexpr (F8) {
 #pragma unroll
-                    for (int w = 0; w < kOut / 4; ++w) {          // four dimensions of a key to a word
-                        const uint32_t lo0 = __byte_perm(v[0][w], v[1][w], 0x5140), hi0 = __byte_perm(v[0][w], v[1][w], 0x7362);
-                        const uint32_t lo1 = __byte_perm(v[2][w], v[3][w], 0x5140), hi1 = __byte_perm(v[2][w], v[3][w], 0x7362);
-                        mma16816(o[4 * w], p, e4m3x2_to_half2(lo0 & 0xFFFFu), e4m3x2_to_half2(lo1 & 0xFFFFu), M());
-                        mma16816(o[4 * w + 1], p, e4m3x2_to_half2(lo0 >> 16), e4m3x2_to_half2(lo1 >> 16), M());
-                        mma16816(o[4 * w + 2], p, e4m3x2_to_half2(hi0 & 0xFFFFu), e4m3x2_to_half2(hi1 & 0xFFFFu), M());
-                        mma16816(o[4 * w + 3], p, e4m3x2_to_half2(hi0 >> 16), e4m3x2_to_half2(hi1 >> 16), M());
-                    }
-                } else {
+                    for (int e = 0; e < 4; ++e) sc[j][e] *= e4[j][e & 1] * v_inv;
+                }
+            }
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {                 // two dimensions of a key to a word
-                        mma16816(o[8 * b + 2 * w], p, __byte_perm(v[0][w], v[1][w], 0x5410), __byte_perm(v[2][w], v[3][w], 0x5410), M());
-                        mma16816(o[8 * b + 2 * w + 1], p, __byte_perm(v[0][w], v[1][w], 0x7632), __byte_perm(v[2][w], v[3][w], 0x7632), M());
+            for (int y = 0; y < kSixteens; ++y) {
+                if (y > 0 && key + y * 16 >= s.len) break;        // those keys were not fetched
+                const uint32_t p[4] = {pack2(sc[2 * y][0], sc[2 * y][1], M()), pack2(sc[2 * y][2], sc[2 * y][3], M()),
+                                       pack2(sc[2 * y + 1][0], sc[2 * y + 1][1], M()), pack2(sc[2 * y + 1][2], sc[2 * y + 1][3], M())};
+#pragma unroll
+                for (int b = 0; b < kHalves; ++b) {
+                    uint32_t v[4][4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int k = y * 16 + (j >> 1) * 8 + ((j & 1) ? key_b : key_a);
+                        uint4 x;
+                        if constexpr (F8 && D == 64) {
+                            const uint2 x2 = lds8(at_v + St::place(k, n >> 1) + (n & 1) * 8);
+                            x = make_uint4(x2.x, x2.y, 0u, 0u);
+                        } else {
+                            x = lds16(at_v + St::place(k, b * 8 + n));
+                        }
+                        v[j][0] = x.x;
+                        v[j][1] = x.y;
+                        v[j][2] = x.z;
+                        v[j][3] = x.w;
+                    }
+                    if (key + y * 16 + 16 > s.len) {              // what lies beyond the length may be anything, and 0 * NaN is not 0
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            if (key + y * 16 + (j >> 1) * 8 + ((j & 1) ? key_b : key_a) >= s.len) v[j][0] = v[j][1] = v[j][2] = v[j][3] = 0u;
+                    }
+                    if constexpr (F8) {
+#pragma unroll
+                        for (int q = 0; q < kOut / 4; ++q) {      // four dimensions of a key to a word
+                            const uint32_t lo0 = __byte_perm(v[0][q], v[1][q], 0x5140), hi0 = __byte_perm(v[0][q], v[1][q], 0x7362);
+                            const uint32_t lo1 = __byte_perm(v[2][q], v[3][q], 0x5140), hi1 = __byte_perm(v[2][q], v[3][q], 0x7362);
+                            mma16816(o[4 * q], p, e4m3x2_to_half2(lo0 & 0xFFFFu), e4m3x2_to_half2(lo1 & 0xFFFFu), M());
+                            mma16816(o[4 * q + 1], p, e4m3x2_to_half2(lo0 >> 16), e4m3x2_to_half2(lo1 >> 16), M());
+                            mma16816(o[4 * q + 2], p, e4m3x2_to_half2(hi0 & 0xFFFFu), e4m3x2_to_half2(hi1 & 0xFFFFu), M());
+                            mma16816(o[4 * q + 3], p, e4m3x2_to_half2(hi0 >> 16), e4m3x2_to_half2(hi1 >> 16), M());
+                        }
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {             // two dimensions of a key to a word
+                            mma16816(o[8 * b + 2 * q], p, __byte_perm(v[0][q], v[1][q], 0x5410), __byte_perm(v[2][q], v[3][q], 0x5410), M());
+                            mma16816(o[8 * b + 2 * q + 1], p, __byte_perm(v[0][q], v[1][q], 0x7632), __byte_perm(v[2][q], v[3][q], 0x7632), M());
+                        }
                     }
                 }
             }
             __syncwarp();                                         // every lane has read the stage that is filled next
             fetch(step + kStages, page_next);
-            page_next = page_of(step + kStages + 1);
+            page_next = pages_of(step + kStages + 1);
         }
         l0 = quad_sum(l0);
         l1 = quad_sum(l1);

@@ -2,10 +2,10 @@
 //
 // S = Q K^T and O += P V on the tensor cores' own memory: tcgen05.mma takes 128 rows at a time, S (128 x 128) and O
 // (128 x D) are accumulated in tensor memory, the weights P replace the scores there and are the left operand of the second
-// product.  A CTA is a stream and holds an SM: two halves of 128 rows, each with four warps that do its softmax, one thread to a row,
-// share the keys and values that one warp brings in by TMA; one thread issues all products.  While one half does
-// its softmax the tensor cores work for the other.  An item with no more than 128 rows gives both halves the same rows and deals
-// them the key tiles in turn: two partials, joined like all others.
+// product.  A CTA is a stream and holds an SM: two halves of 128 rows share the keys and values that one warp brings in by TMA.
+// Each half has one warp that issues its products and eight that do its softmax, two threads to a row: the chain scores ->
+// maximum -> weights -> product of one half is what takes long, and the two halves run theirs against each other.  An item with no more
+// than 128 rows gives both halves the same rows and deals them the key tiles in turn: two partials, joined like all others.
 //   Keys (K-major) and queries lie in shared memory in rows of 128 bytes with the 128-byte swizzle, values as they come are the
 // right operand with the head's dimension contiguous: nothing is transposed.
 //   The reference score of a row is raised only when a tile's maximum exceeds it by 2^8 (weights up to 256 are as exact as
@@ -21,12 +21,13 @@
 
 namespace hora {
 
-constexpr int kWideThreads = 384;                        // two halves of four warps; one for TMA, one for the products, one for the list of pieces, a spare one
-constexpr int kTmaWarp = 8, kMmaWarp = 9, kListWarp = 10;
-constexpr int kPieceBatch = 32;                          // pieces listed at a time
-// Registers: launched with 168 a thread (three warps share a scheduler's 16384); the softmax warps, which hold 128 scores each thread, take
-// what the others leave: 2 * 224 + 56 = 3 * 168.
-constexpr int kSoftmaxRegs = 224, kOtherRegs = 56;
+constexpr int kSoftmaxWarps = 16, kHalfThreads = kSoftmaxWarps / 2 * kWarp;
+constexpr int kTmaWarp = kSoftmaxWarps, kMmaWarp = kTmaWarp + 1, kListWarp = kMmaWarp + 2;        // one for TMA, one a half for the products, one to list the pieces
+constexpr int kWideThreads = (kListWarp + 1) * kWarp;
+constexpr int kPieceBatch = 16;                          // pieces listed at a time
+// Registers: launched with 96 a thread (five warps share a scheduler's 16384); the softmax warps, which hold 64 scores a thread, take
+// some of the others': 4 * 104 + 64 = 5 * 96.
+constexpr int kSoftmaxRegs = 104, kOtherRegs = 64;
 constexpr uint32_t kWaitTries = 4000000;                 // of at least a microsecond each unless the barrier is passed
 
 template <int D>
@@ -36,8 +37,7 @@ struct WideSmem {
     static constexpr int kStages = D == 128 ? 5 : 10;
     static constexpr int kQ = 0;                                      // [2][D / 64][128][128 bytes]
     static constexpr int kRing = 2 * kQBytes;                         // [stages][D / 64][128][128 bytes]
-    static constexpr int kBars = kRing + kStages * kStageBytes;
-    static constexpr int kBytes = kBars + 256 + 1024;                 // and room to begin on a multiple of 1024
+    static constexpr int kSmall = kRing + kStages * kStageBytes;       // WideShared
 };
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -95,6 +95,12 @@ __device__ __forceinline__ void mma_tmem(uint32_t d, uint32_t a, uint32_t b, uin
         "r"(a), "r"(b), "r"(idesc), "r"(add), "r"(kOperandHigh)
         : "memory");
 }
+// One lane of a converged warp.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.b32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one != 0;
+}
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
@@ -112,23 +118,27 @@ __device__ __forceinline__ void tmem_load(uint32_t at, float (&r)[32]) {
           "=f"(r[30]), "=f"(r[31])
         : "r"(at));
 }
-__device__ __forceinline__ void tmem_store(uint32_t at, const uint32_t (&r)[32]) {
+__device__ __forceinline__ void tmem_load16(uint32_t at, float (&r)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
-        "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-        "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]),
-        "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(at)
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=f"(r[0]), "=f"(r[1]), "=f"(r[2]), "=f"(r[3]), "=f"(r[4]), "=f"(r[5]), "=f"(r[6]), "=f"(r[7]), "=f"(r[8]), "=f"(r[9]),
+          "=f"(r[10]), "=f"(r[11]), "=f"(r[12]), "=f"(r[13]), "=f"(r[14]), "=f"(r[15])
+        : "r"(at));
+}
+__device__ __forceinline__ void tmem_store8(uint32_t at, const uint32_t (&r)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%8], {%0,%1,%2,%3,%4,%5,%6,%7};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
+                 "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(at)
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_store16(uint32_t at, const float (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"f"(r[0]), "f"(r[1]),
+        "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]),
+        "f"(r[14]), "f"(r[15]), "r"(at)
         : "memory");
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-__device__ __forceinline__ float exp2_fast(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 
 // A piece as the warps of its CTA need it.
 struct WidePiece {
@@ -148,20 +158,96 @@ struct WideBars {
     uint32_t full, empty, scores, weights, queries, output;          // arrays of 8-byte barriers: [stages] x 2, [2] x 4
 };
 
-// O of a warp's rows, times f.
-template <int D>
+__device__ __forceinline__ void store16(uint32_t at, const uint4 &v) {
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+__device__ __forceinline__ uint4 load16(uint32_t at) {
+    uint4 v;
+    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+
+// Two fp32 operations an instruction.
+__device__ __forceinline__ uint64_t two(float2 x) { return (uint64_t)__float_as_uint(x.y) << 32 | __float_as_uint(x.x); }
+__device__ __forceinline__ float2 two(uint64_t x) { return make_float2(__uint_as_float((uint32_t)x), __uint_as_float((uint32_t)(x >> 32))); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(two(a)), "l"(two(b)), "l"(two(c)));
+    return two(d);
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(two(a)), "l"(two(b)));
+    return two(d);
+}
+
+// 2^x by multiplications, for x <= 8: the special function unit takes 8 cycles a warp, as long as the tensor cores need for its
+// share of the products, so a quarter of the exponentials is computed beside it.  2^x = 2^n 2^f, n = round(x), |f| <= 1/2;
+// 2^f by the polynomial of degree 5 with the least largest relative error (7.5e-8, 2.0e-7 with fp32 rounding; fitted by iterated
+// weighted least squares), n added to its exponent.  Below 2^-126 the result is 2^-126 in place of less.
+__device__ __forceinline__ float2 exp2_by_products(float2 x) {
+    x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
+    const float2 big = make_float2(12582912.f, 12582912.f), t = add2(x, big);      // 1.5 * 2^23: the low bits of t are n
+    const float2 f = fma2(add2(t, make_float2(-12582912.f, -12582912.f)), make_float2(-1.f, -1.f), x);
+    float2 p = make_float2(1.3276471519402e-3f, 1.3276471519402e-3f);
+    p = fma2(p, f, make_float2(9.6755413306768e-3f, 9.6755413306768e-3f));
+    p = fma2(p, f, make_float2(5.5507132749614e-2f, 5.5507132749614e-2f));
+    p = fma2(p, f, make_float2(2.4022119723934e-1f, 2.4022119723934e-1f));
+    p = fma2(p, f, make_float2(6.9314696706386e-1f, 6.9314696706386e-1f));
+    p = fma2(p, f, make_float2(1.0000000716547f, 1.0000000716547f));
+    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
+                       __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+}
+
+// Columns of O of a warp's rows, times f; few at a time, since the scores are in registers meanwhile.
+template <int COLUMNS>
 __device__ __forceinline__ void scale_output(uint32_t t_o, float f) {
-#pragma unroll
-    for (int b = 0; b < D / 32; ++b) {
-        float o[32];
-        uint32_t y[32];
-        tmem_load(t_o + b * 32, o);
+#pragma unroll 1
+    for (int b = 0; b < COLUMNS / 16; ++b) {
+        float o[16];
+        tmem_load16(t_o + b * 16, o);
         tmem_load_wait();
 #pragma unroll
-        for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(o[e] * f);
-        tmem_store(t_o + b * 32, y);
+        for (int e = 0; e < 16; ++e) o[e] *= f;
+        tmem_store16(t_o + b * 16, o);
     }
 }
+
+// Whether any of a half's threads says yes; a barrier for them.
+__device__ __forceinline__ bool any_of_half(int half, bool yes) {
+    uint32_t any;
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %1, 0;\nbarrier.cta.red.or.pred q, %2, %3, p;\nselp.b32 %0, 1, 0, q;\n}"
+                 : "=r"(any)
+                 : "r"((uint32_t)yes), "r"(1 + half), "n"(kHalfThreads)
+                 : "memory");
+    return any != 0;
+}
+
+// Clears the values beyond the last of a tile's `keys` keys, among the sixteen that the product reads last: they may be anything,
+// and 0 * NaN is not 0.  The tile is the piece's last, its values are in stage number `last`.  All threads of a half; one half does it
+// where both read the stage.
+template <int D>
+__device__ __forceinline__ bool clear_values(const WideBars &bars, uint32_t base, volatile int32_t *failed, int32_t keys, int32_t last, int thread, bool other) {
+    if (keys >= kWideKeys || (keys & 15) == 0 || other) return true;
+    using Smem = WideSmem<D>;
+    const uint32_t stage = last % Smem::kStages;
+    if (!bar_wait(bars.full + 8 * stage, (last / Smem::kStages) & 1, failed)) return false;
+    const int32_t clear = ((keys + 15) & ~15) - keys;
+    for (int32_t c = thread; c < clear * (D / 8); c += kHalfThreads) {
+        const int32_t r = keys + c / (D / 8), chunk = c % (D / 8);
+        store16(base + Smem::kRing + stage * Smem::kStageBytes + (chunk >> 3) * (kWideKeys * 128) + r * 128 + (chunk & 7) * 16, make_uint4(0, 0, 0, 0));
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    return true;
+}
+
+struct WideShared {
+    uint64_t bars[32];
+    WidePiece piece[kPieceBatch];
+    float row[2][kWideHalf];                             // between the two threads of a row
+    int32_t pieces, failed;
+    uint32_t tmem;
+};
 
 template <typename Q, int D>
 __global__ void __launch_bounds__(kWideThreads, 1)
@@ -169,47 +255,48 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
     pdl_enter();
     using Smem = WideSmem<D>;
     constexpr int kStages = Smem::kStages, kParts = D / 64;
-    extern __shared__ uint8_t s_raw[];
-    __shared__ int32_t s_failed;
-    __shared__ uint32_t s_tmem;
-    __shared__ WidePiece s_piece[kPieceBatch];
-    __shared__ int32_t s_pieces;
-    const uint32_t base = (smem_at(s_raw) + 1023u) & ~1023u;
-    const WideBars bars = {base + Smem::kBars, base + Smem::kBars + 8 * kStages, base + Smem::kBars + 16 * kStages,
-                           base + Smem::kBars + 16 * kStages + 16, base + Smem::kBars + 16 * kStages + 32, base + Smem::kBars + 16 * kStages + 48};
+    extern __shared__ __align__(1024) uint8_t s_tiles[];              // the swizzle goes by addresses: tiles begin at multiples of 1024
+    WideShared &sh = *reinterpret_cast<WideShared *>(s_tiles + Smem::kSmall);
+    const uint32_t base = smem_at(s_tiles), at_bars = smem_at(sh.bars);
+    const WideBars bars = {at_bars, at_bars + 8 * kStages, at_bars + 16 * kStages, at_bars + 16 * kStages + 16, at_bars + 16 * kStages + 32, at_bars + 16 * kStages + 48};
+    static_assert(2 * kStages + 8 <= 32, "barriers");
     const int warp = threadIdx.x >> 5, lane = lane_id();
     bool bad = false;
+    if (base & 1023u) {
+        raise_status(a.status, HORA_ERR_INTERNAL);
+        return;
+    }
     if ((int64_t)blockIdx.x * steps_per_stream<true>(a) >= __ldg(a.start[1] + a.N + a.R)) return;       // nothing on this stream
 
     if (threadIdx.x == 0) {
-        s_failed = 0;
+        sh.failed = 0;
         for (int s = 0; s < kStages; ++s) {
             bar_init(bars.full + 8 * s, 1);
-            bar_init(bars.empty + 8 * s, 1);
+            bar_init(bars.empty + 8 * s, 2);             // both halves' products
         }
         for (int h = 0; h < 2; ++h) {
             bar_init(bars.scores + 8 * h, 1);
-            bar_init(bars.weights + 8 * h, kWideHalf);
-            bar_init(bars.queries + 8 * h, kWideHalf);
+            bar_init(bars.weights + 8 * h, kHalfThreads);
+            bar_init(bars.queries + 8 * h, kHalfThreads);
             bar_init(bars.output + 8 * h, 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
     if (warp == 0) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_at(&s_tmem)) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_at(&sh.tmem)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
         fence_before();
     }
     __syncthreads();
     fence_after();
-    const uint32_t tmem = s_tmem;                        // columns: S of the halves, 128 each, then O, D each
-    volatile int32_t *failed = &s_failed;
+    const uint32_t tmem = sh.tmem;                        // columns: S of the halves, 128 each, then O, D each
+    volatile int32_t *failed = &sh.failed;
 
     // All warps go through the stream's pieces in batches: one warp lists a batch, the others work through it.  Returns how many there are.
     auto next_batch = [&]() {
         __syncthreads();
-        return s_failed ? 0 : s_pieces;
+        return sh.failed ? 0 : sh.pieces;
     };
     if (warp >= kTmaWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
@@ -221,7 +308,7 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
                 Piece w;
                 while (warp == kListWarp && n < kPieceBatch && pieces.next(a, w, bad)) {
                     if (lane == 0) {
-                        WidePiece &p = s_piece[n];
+                        WidePiece &p = sh.piece[n];
                         p.pages = w.pages;
                         p.first = pieces.s.first;
                         p.seq_rows = pieces.s.rows;
@@ -237,7 +324,7 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
                     }
                     ++n;
                 }
-                if (warp == kListWarp && lane == 0) s_pieces = n;
+                if (warp == kListWarp && lane == 0) sh.pieces = n;
                 n = next_batch();
                 __syncthreads();                             // the batch has been worked through
             }
@@ -265,7 +352,7 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
             };
             while (const int32_t listed = next_batch()) {
                 for (int32_t at = 0; at < listed && ok; ++at) {
-                    const WidePiece &p = s_piece[at];
+                    const WidePiece &p = sh.piece[at];
                     const int32_t n = p.count(0), halves = p.both ? 1 : 2;
                     for (int32_t it = 0; it <= n && ok; ++it)
                         for (int half = 0; half < halves && ok; ++half) {
@@ -283,65 +370,76 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
                 __syncthreads();
             }
             __syncthreads();
-        } else if (warp == kMmaWarp) {
-            // ---- products
+        } else {
+            // ---- products of one half
+            const int half = warp - kMmaWarp;
             constexpr uint32_t kType = std::is_same<Q, __nv_bfloat16>::value ? 1u : 0u;
             constexpr uint32_t kIdescS = (1u << 4) | (kType << 7) | (kType << 10) | ((kWideKeys / 8) << 17) | ((kWideHalf / 16) << 24);
             constexpr uint32_t kIdescO = (1u << 4) | (kType << 7) | (kType << 10) | (1u << 16) | ((D / 8) << 17) | ((kWideHalf / 16) << 24);
-            int32_t pos = 0, k_pos = 0, v_pos = 0;
-            uint32_t n_weights[2] = {0, 0}, n_queries[2] = {0, 0};
+            // the stages in the order of their first use, as counters that wrap
+            uint32_t stage = 0, round = 0, weights_phase = 0, queries_phase = 0;
+            const uint32_t k0 = operand(base + Smem::kRing, 16), v0 = operand(base + Smem::kRing, kWideKeys * 128);
+            const uint32_t q = operand(base + Smem::kQ + half * Smem::kQBytes, 16), t_s = tmem + half * 128, t_o = tmem + 256 + half * D;
             bool ok = true;
+            auto next_stage = [&](bool mine) {           // the next one, once its copy has arrived if it is for this half
+                const uint32_t now = stage;
+                if (mine) ok = ok && bar_wait(bars.full + 8 * now, round, failed);
+                if (++stage == kStages) { stage = 0; round ^= 1; }
+                return now;
+            };
+            auto release = [&](uint32_t used, bool both) {
+                mma_commit(bars.empty + 8 * used);
+                if (!both) mma_commit(bars.empty + 8 * used);
+            };
             while (const int32_t listed = next_batch()) {
                 for (int32_t at = 0; at < listed && ok; ++at) {
-                    const WidePiece &p = s_piece[at];
-                    const int32_t n0 = p.count(0);
-                    for (int32_t it = 0; it <= n0 && ok; ++it) {
+                    const bool both = sh.piece[at].both;
+                    const int32_t len = sh.piece[at].len, key0 = sh.piece[at].key0, tiles = sh.piece[at].n;
+                    const int32_t n0 = both ? tiles : (tiles + 1) >> 1, n1 = both ? tiles : tiles >> 1, n = half ? n1 : n0;
+                    for (int32_t it = 0; it <= n0 && ok; ++it)
+                        for (int turn = 0; turn < (both ? 1 : 2) && ok; ++turn) {
+                            const bool mine = both || turn == half;
+                            const int32_t nt = turn ? n1 : n0;
+                            if (it >= 1 && it - 1 < nt) {
+                                const uint32_t used = next_stage(mine);
+                                if (mine) {
+                                    const int32_t left = len - key0 - (both ? it - 1 : 2 * (it - 1) + half) * kWideKeys;
+                                    ok = ok && bar_wait(bars.weights + 8 * half, weights_phase, failed);
+                                    weights_phase ^= 1;
+                                    fence_after();
+                                    if (ok && elect_one()) {
+                                        const uint32_t v = v0 + used * (Smem::kStageBytes >> 4);
 #pragma unroll
-                        for (int half = 0; half < 2; ++half) {
-                            if (!ok) break;
-                            const int32_t n = p.count(half);
-                            const bool first_use = !p.both || half == 0, last_use = !p.both || half == 1;
-                            if (it >= 1 && it - 1 < n) {
-                                if (first_use) v_pos = pos++;
-                                const int stage = v_pos % kStages;
-                                ok = bar_wait(bars.weights + 8 * half, n_weights[half]++ & 1, failed) &&
-                                     bar_wait(bars.full + 8 * stage, (v_pos / kStages) & 1, failed);
-                                if (!ok) break;
-                                fence_after();
-                                const int32_t groups = (min(kWideKeys, p.len - p.key(half, it - 1)) + 15) >> 4;
-                                if (lane == 0) {
-                                    const uint32_t v = operand(base + Smem::kRing + stage * Smem::kStageBytes, kWideKeys * 128);
-#pragma unroll
-                                    for (int g = 0; g < kWideKeys / 16; ++g)
-                                        if (g < groups)
-                                            mma_tmem(tmem + 256 + half * D, tmem + half * 128 + g * 8, v + g * (2048 >> 4), kIdescO, it > 1 || g > 0);
-                                    if (last_use) mma_commit(bars.empty + 8 * stage);
-                                    if (it == n) mma_commit(bars.output + 8 * half);
-                                }
-                                __syncwarp();
-                            }
-                            if (it < n) {
-                                if (first_use) k_pos = pos++;
-                                const int stage = k_pos % kStages;
-                                if (it == 0) ok = bar_wait(bars.queries + 8 * half, n_queries[half]++ & 1, failed);
-                                ok = ok && bar_wait(bars.full + 8 * stage, (k_pos / kStages) & 1, failed);
-                                if (!ok) break;
-                                fence_after();
-                                if (lane == 0) {
-                                    const uint32_t q = operand(base + Smem::kQ + half * Smem::kQBytes, 16);
-                                    const uint32_t k = operand(base + Smem::kRing + stage * Smem::kStageBytes, 16);
-#pragma unroll
-                                    for (int x = 0; x < D / 16; ++x) {
-                                        const uint32_t off = ((x >> 2) * (kWideKeys * 128) + (x & 3) * 32) >> 4;
-                                        mma_smem(tmem + half * 128, q + off, k + off, kIdescS, x > 0);
+                                        for (int g = 0; g < kWideKeys / 16; ++g)
+                                            if (g * 16 < left) mma_tmem(t_o, t_s + g * 8, v + g * (2048 >> 4), kIdescO, it > 1 || g > 0);
+                                        release(used, both);
+                                        if (it == n) mma_commit(bars.output + 8 * half);
                                     }
-                                    mma_commit(bars.scores + 8 * half);
-                                    if (last_use) mma_commit(bars.empty + 8 * stage);
+                                    __syncwarp();
                                 }
-                                __syncwarp();
+                            }
+                            if (it < nt) {
+                                const uint32_t used = next_stage(mine);
+                                if (mine) {
+                                    if (it == 0) {
+                                        ok = ok && bar_wait(bars.queries + 8 * half, queries_phase, failed);
+                                        queries_phase ^= 1;
+                                    }
+                                    fence_after();
+                                    if (ok && elect_one()) {
+                                        const uint32_t k = k0 + used * (Smem::kStageBytes >> 4);
+#pragma unroll
+                                        for (int x = 0; x < D / 16; ++x) {
+                                            const uint32_t off = ((x >> 2) * (kWideKeys * 128) + (x & 3) * 32) >> 4;
+                                            mma_smem(t_s, q + off, k + off, kIdescS, x > 0);
+                                        }
+                                        mma_commit(bars.scores + 8 * half);
+                                        release(used, both);
+                                    }
+                                    __syncwarp();
+                                }
                             }
                         }
-                    }
                 }
                 __syncthreads();
             }
@@ -349,33 +447,38 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        // ---- softmax: thread `row` of a half has row `row` of its scores
-        const int half = warp >> 2, row = threadIdx.x & (kWideHalf - 1);
+        // ---- softmax: two threads have row `row` of a half, for 64 keys of a tile and half of the output's columns each
+        const int half = warp >> 3, side = (warp >> 2) & 1, thread = threadIdx.x & (kHalfThreads - 1), row = threadIdx.x & (kWideHalf - 1);
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);           // this warp's 32 lanes of tensor memory
-        const uint32_t t_s = lanes + half * 128, t_o = lanes + 256 + half * D;
+        const uint32_t t_s = lanes + half * 128, t_o = lanes + 256 + half * D + side * (D / 2);
         uint32_t n_scores = 0, n_output = 0;
         int32_t pos = 0;                                 // stages of all pieces before this one
         bool ok = true;
+        // A warp that has failed goes on without waiting or working, so that the barriers of its half stay in step.
         while (const int32_t listed = next_batch()) {
             for (int32_t at = 0; at < listed; ++at) {
-                const WidePiece &p = s_piece[at];
+                const WidePiece &p = sh.piece[at];
                 const int32_t n = p.count(half);
                 const int32_t x = (p.both ? half * kWideHalf : 0) + row;      // row of the item
                 QueryRow qr = {-1, 0};
                 if (x < p.rows) qr = query_row(a, p.first, p.seq_rows, p.len, p.prompt, p.h, p.row0 + x);
+                const int32_t limit = qr.limit;
                 const bool warp_has_rows = __any_sync(kFull, qr.out >= 0);
                 float m = -INFINITY, l = 0.f;
                 if (n > 0) {
-                    // queries into shared memory; the products that read the last ones are done (their output was waited for)
+                    // queries into shared memory, neighbouring lanes along a row; the products that read the last ones are done (their
+                    // output was waited for)
                     if (warp_has_rows) {
-                        const Q *__restrict__ q = static_cast<const Q *>(a.q) + (qr.out >= 0 ? qr.out / a.Hq * a.q_row_stride + qr.out % a.Hq * D : 0);
-                        const uint32_t to = base + Smem::kQ + half * Smem::kQBytes + row * 128;
+                        const int64_t from = qr.out >= 0 ? qr.out / a.Hq * a.q_row_stride + qr.out % a.Hq * D : -1;
+                        constexpr int kLanes = D / 8, kRows = kWarp / kLanes;             // lanes to a row, rows at a time
+                        const int c = lane % kLanes;
 #pragma unroll
-                        for (int c = 0; c < D / 8; ++c) {
-                            const uint4 v = qr.out >= 0 ? __ldg(reinterpret_cast<const uint4 *>(q) + c) : make_uint4(0, 0, 0, 0);
-                            asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(to + (c >> 3) * (kWideHalf * 128) + (((c & 7) ^ (row & 7)) << 4)),
-                                         "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
-                                         : "memory");
+                        for (int y = 0; y < kLanes / 2; ++y) {
+                            const int r = (side * (kLanes / 2) + y) * kRows + lane / kLanes;
+                            const int64_t at_r = __shfl_sync(kFull, from, r);
+                            const uint4 v = at_r >= 0 ? __ldg(reinterpret_cast<const uint4 *>(static_cast<const Q *>(a.q) + at_r) + c) : make_uint4(0, 0, 0, 0);
+                            const int qrow = (warp & 3) * kWarp + r;
+                            store16(base + Smem::kQ + half * Smem::kQBytes + (c >> 3) * (kWideHalf * 128) + qrow * 128 + (((c & 7) ^ (qrow & 7)) << 4), v);
                         }
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -384,95 +487,110 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
                         const int32_t key0 = p.key(half, k);
                         ok = ok && bar_wait(bars.scores + 8 * half, n_scores++ & 1, failed);
                         ok = __all_sync(kFull, ok);
-                        if (!ok) break;
                         fence_after();
-                        if (warp_has_rows) {
-                            float s[4][32];
+                        const bool work = ok && warp_has_rows;
+                        float s[2][32], top = -INFINITY;
+                        if (work) {
 #pragma unroll
-                            for (int b = 0; b < 4; ++b) tmem_load(t_s + b * 32, s[b]);
+                            for (int b = 0; b < 2; ++b) tmem_load(t_s + side * 64 + b * 32, s[b]);
                             tmem_load_wait();
-                            if (key0 + kWideKeys > qr.limit) {
+                            const int32_t first = key0 + side * 64;
+                            if (first + 64 > limit) {
 #pragma unroll
-                                for (int b = 0; b < 4; ++b)
+                                for (int b = 0; b < 2; ++b)
 #pragma unroll
                                     for (int e = 0; e < 32; ++e)
-                                        if (key0 + b * 32 + e >= qr.limit) s[b][e] = -INFINITY;
+                                        if (first + b * 32 + e >= limit) s[b][e] = -INFINITY;
                             }
-                            float top = -INFINITY;
+                            float t4[4];
 #pragma unroll
-                            for (int b = 0; b < 4; ++b)
+                            for (int b = 0; b < 4; ++b) {
+                                t4[b] = s[b >> 1][(b & 1) * 16];
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) top = fmaxf(top, s[b][e]);
-                            top *= a.scale_log2;
-                            if (k == 0) {
-                                m = top;
-                            } else if (__any_sync(kFull, top > m + 8.f)) {
-                                const float up = fmaxf(m, top), f = up == -INFINITY ? 1.f : exp2_fast(m - up);
-                                l *= f;
-                                m = up;
-                                scale_output<D>(t_o, f);
+                                for (int e = 1; e < 15; e += 2) t4[b] = fmaxf(t4[b], fmaxf(s[b >> 1][(b & 1) * 16 + e], s[b >> 1][(b & 1) * 16 + e + 1]));
+                                t4[b] = fmaxf(t4[b], s[b >> 1][(b & 1) * 16 + 15]);
                             }
+                            top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * a.scale_log2;
+                        }
+                        ok = clear_values<D>(bars, base, failed, p.len - key0, pos + 2 * p.n - 1, thread, p.both && half == 1) && ok;
+                        // The barrier also holds back the weights of one thread until the other has read the scores they replace.
+                        if (any_of_half(half, work && (k == 0 || top > m + 8.f))) {
+                            if (side == 0) sh.row[half][row] = top;
+                            any_of_half(half, false);
+                            if (side == 1) sh.row[half][row] = fmaxf(top, sh.row[half][row]);
+                            any_of_half(half, false);
+                            const float up = fmaxf(m, sh.row[half][row]), f = up == -INFINITY ? 1.f : exp2_fast(m - up);
+                            l *= f;
+                            m = up;
+                            if (work && k > 0) scale_output<D / 2>(t_o, f);
+                        }
+                        if (work) {
                             // where no key has been seen the reference is -infinity and every weight has to come out as 0
                             const float z = m == -INFINITY ? 0.f : m;
+                            float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-                            for (int b = 0; b < 2; ++b) {
-                                uint32_t w[32];
+                            for (int b = 0; b < 4; ++b) {
+                                uint32_t w[8];
 #pragma unroll
-                                for (int e = 0; e < 32; ++e) {
-                                    const float p0 = exp2_fast(fmaf(s[2 * b + (e >> 4)][(2 * e) & 31], a.scale_log2, -z));
-                                    const float p1 = exp2_fast(fmaf(s[2 * b + (e >> 4)][(2 * e + 1) & 31], a.scale_log2, -z));
-                                    l += p0 + p1;
-                                    w[e] = pack2(p0, p1, Q());
+                                for (int e = 0; e < 8; ++e) {
+                                    float2 y = make_float2(s[b >> 1][(b & 1) * 16 + 2 * e], s[b >> 1][(b & 1) * 16 + 2 * e + 1]);
+                                    y = fma2(y, make_float2(a.scale_log2, a.scale_log2), make_float2(-z, -z));
+                                    if (e % 4 == 3) y = exp2_by_products(y);
+                                    else y = make_float2(exp2_fast(y.x), exp2_fast(y.y));
+                                    sum = add2(sum, y);
+                                    w[e] = pack2(y.x, y.y, Q());
                                 }
-                                tmem_store(t_s + b * 32, w);
+                                tmem_store8(t_s + side * 32 + b * 8, w);
                             }
+                            l += sum.x + sum.y;
                             tmem_store_wait();
-                        }
-                        // the last tile's values beyond the length, among the sixteen keys that the product reads last
-                        const int32_t keys = p.len - key0;
-                        if (keys < kWideKeys && (keys & 15) != 0 && !(p.both && half == 1)) {
-                            const int32_t last = pos + 2 * p.n - 1;           // the piece's last stage holds them
-                            const uint32_t stage = base + Smem::kRing + last % kStages * Smem::kStageBytes;
-                            ok = bar_wait(bars.full + 8 * (last % kStages), (last / kStages) & 1, failed);
-                            const int32_t clear = ((keys + 15) & ~15) - keys;
-                            if (ok)
-                                for (int32_t c = row; c < clear * (D / 8); c += kWideHalf) {
-                                    const int32_t r = keys + c / (D / 8), chunk = c % (D / 8);
-                                    asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(stage + (chunk >> 3) * (kWideKeys * 128) + r * 128 + (chunk & 7) * 16),
-                                                 "r"(0)
-                                                 : "memory");
-                                }
-                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         }
                         fence_before();
                         bar_arrive(bars.weights + 8 * half);
                     }
                     ok = ok && bar_wait(bars.output + 8 * half, n_output++ & 1, failed);
                     ok = __all_sync(kFull, ok);
-                    if (!ok) break;
                     fence_after();
                 }
                 pos += 2 * p.n;
-                if (!warp_has_rows) continue;
-                // the partial
-                const int64_t rows_all = (int64_t)a.R * a.T * a.Hq;
+                // the partial: sums of the two threads of a row, then the output
+                const int64_t rows_all = (int64_t)a.R * a.T * a.Hq, out = x < p.rows ? query_row(a, p.first, p.seq_rows, p.len, p.prompt, p.h, p.row0 + x).out : -1;
                 const int64_t place = p.continued ? (int64_t)blockIdx.x * kWideRows + half * kWideHalf + row
-                                                  : (int64_t)((p.prompt ? kPromptPart : kOwnPart) + (!p.both && half ? kSecondHalf : 0)) * rows_all + qr.out;
-                float *__restrict__ po = (p.continued ? a.cont_o[1] : a.main_o) + place * D;
-                if (n > 0) {
+                                                  : (int64_t)((p.prompt ? kPromptPart : kOwnPart) + (!p.both && half ? kSecondHalf : 0)) * rows_all + out;
+                if (side == 1) sh.row[half][row] = l;
+                any_of_half(half, false);
+                if (side == 0 && out >= 0)
+                    *reinterpret_cast<float2 *>((p.continued ? a.cont_ml[1] : a.main_ml) + place * 2) = make_float2(m, l + sh.row[half][row]);
+                if (ok && n > 0 && warp_has_rows) {
+                    // through the query tile, which nobody reads any more, so that neighbouring lanes store along a row
+                    constexpr int kColumns = D / 4, kLanes = kColumns / 4, kRows = kWarp / kLanes;            // columns at a time
+                    const uint32_t tile = base + Smem::kQ + half * Smem::kQBytes + (warp & 7) * (kWarp * kColumns * 4);
+                    float *__restrict__ po = (p.continued ? a.cont_o[1] : a.main_o) + side * (D / 2);
+                    const int64_t from = out >= 0 ? place * D : -1;
 #pragma unroll
-                    for (int b = 0; b < D / 32; ++b) {
-                        float o[32];
-                        tmem_load(t_o + b * 32, o);
+                    for (int y = 0; y < 2; ++y) {
+                        float o[kColumns];
+                        if constexpr (D == 128) tmem_load(t_o + y * kColumns, o);
+                        else tmem_load16(t_o + y * kColumns, o);
                         tmem_load_wait();
-                        if (qr.out >= 0) {
+                        __syncwarp();
 #pragma unroll
-                            for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4 *>(po + b * 32 + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        for (int c = 0; c < kLanes; ++c)
+                            store16(tile + lane * (kColumns * 4) + ((c ^ (lane & (kLanes - 1))) << 4),
+                                    make_uint4(__float_as_uint(o[4 * c]), __float_as_uint(o[4 * c + 1]), __float_as_uint(o[4 * c + 2]), __float_as_uint(o[4 * c + 3])));
+                        __syncwarp();
+                        const int c = lane % kLanes;
+#pragma unroll
+                        for (int v = 0; v < kLanes; ++v) {
+                            const int r = v * kRows + lane / kLanes;
+                            const int64_t to = __shfl_sync(kFull, from, r);
+                            const uint4 got = load16(tile + r * (kColumns * 4) + ((c ^ (r & (kLanes - 1))) << 4));
+                            if (to >= 0) *reinterpret_cast<uint4 *>(po + to + y * kColumns + c * 4) = got;
                         }
                     }
                 }
-                if (qr.out >= 0) *reinterpret_cast<float2 *>((p.continued ? a.cont_ml[1] : a.main_ml) + place * 2) = make_float2(m, l);
                 fence_before();                          // the next item's products may overwrite O: its weights come after this
+                any_of_half(half, false);                // and its queries overwrite the tile that all have to be done with
             }
             __syncthreads();
         }
@@ -481,7 +599,7 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
     if (bad) raise_status(a.status, HORA_ERR_INVALID_VALUE);
     fence_before();
     __syncthreads();
-    if (threadIdx.x == 0 && s_failed) raise_status(a.status, HORA_ERR_INTERNAL);
+    if (threadIdx.x == 0 && sh.failed) raise_status(a.status, HORA_ERR_INTERNAL);
     if (warp == 0) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
@@ -512,7 +630,7 @@ static hora_status_t launch_wide(const AttnArgs &a, int32_t dtype, cudaStream_t 
     CUtensorMap k, v;
     const int64_t rows = (a.n_pages * a.Hkv) << a.page_shift;
     if (!pool_map(&k, a.k_cache, dtype, rows, D, 1 << a.page_shift) || !pool_map(&v, a.v_cache, dtype, rows, D, 1 << a.page_shift)) return HORA_ERR_CUDA;
-    constexpr int kSmem = WideSmem<D>::kBytes;
+    constexpr int kSmem = WideSmem<D>::kSmall + sizeof(WideShared);
     cudaError_t e = cudaFuncSetAttribute(attention_wide_kernel<Q, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e == cudaSuccess) e = launch_pdl(attention_wide_kernel<Q, D>, a.n_wide, kWideThreads, kSmem, stream, a, k, v);
     count_launches(1);
