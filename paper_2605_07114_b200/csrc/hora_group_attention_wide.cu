@@ -1,11 +1,12 @@
 // hora_group_attention, the kernel for wide items: many query rows to a key, as the prompt's keys of a large group have.
 //
-// S = Q K^T and O += P V on the tensor cores' own memory: tcgen05.mma takes 128 rows at a time, S (128 x 128) and O
+// S = Q K^T and O += P V on the tensor cores' own memory: tcgen05.mma takes 128 rows at a time, S (128 x 64, twice) and O
 // (128 x D) are accumulated in tensor memory, the weights P replace the scores there and are the left operand of the second
 // product.  A CTA is a stream and holds an SM: two halves of 128 rows share the keys and values that one warp brings in by TMA.
-// Each half has one warp that issues its products and eight that do its softmax, two threads to a row: the chain scores ->
-// maximum -> weights -> product of one half is what takes long, and the two halves run theirs against each other.  An item with no more
-// than 128 rows gives both halves the same rows and deals them the key tiles in turn: two partials, joined like all others.
+// Each half has one warp that issues its products and four that do its softmax, one thread to a row.  The chain scores -> maximum ->
+// weights -> product takes much longer than its products, so four of them are under way at any time: a step's 128 keys
+// make two tiles, and while a half's softmax works on one the tensor cores compute the scores of the next.  An item with no more
+// than 128 rows gives both halves the same rows and deals them the steps in turn: two partials, joined like all others.
 //   Keys (K-major) and queries lie in shared memory in rows of 128 bytes with the 128-byte swizzle, values as they come are the
 // right operand with the head's dimension contiguous: nothing is transposed.
 //   The reference score of a row is raised only when a tile's maximum exceeds it by 2^8 (weights up to 256 are as exact as
@@ -21,13 +22,11 @@
 
 namespace hora {
 
-constexpr int kSoftmaxWarps = 16, kHalfThreads = kSoftmaxWarps / 2 * kWarp;
+constexpr int kSoftmaxWarps = 8, kHalfThreads = kSoftmaxWarps / 2 * kWarp;
 constexpr int kTmaWarp = kSoftmaxWarps, kMmaWarp = kTmaWarp + 1, kListWarp = kMmaWarp + 2;        // one for TMA, one a half for the products, one to list the pieces
 constexpr int kWideThreads = (kListWarp + 1) * kWarp;
+constexpr int kTileKeys = 64;
 constexpr int kPieceBatch = 16;                          // pieces listed at a time
-// Registers: launched with 96 a thread (five warps share a scheduler's 16384); the softmax warps, which hold 64 scores a thread, take
-// some of the others': 4 * 104 + 64 = 5 * 96.
-constexpr int kSoftmaxRegs = 104, kOtherRegs = 64;
 constexpr uint32_t kWaitTries = 4000000;                 // of at least a microsecond each unless the barrier is passed
 
 template <int D>
@@ -148,14 +147,18 @@ struct WidePiece {
     bool prompt, continued;
     bool both;                                           // both halves take every tile (their rows differ)
 
-    // key tiles of a half, and which its k-th is
+    // steps of a half, the first key of its k-th, and the tiles of all of them
     __device__ __forceinline__ int32_t count(int half) const { return both ? n : (n + 1 - half) >> 1; }
     __device__ __forceinline__ int32_t key(int half, int32_t k) const { return key0 + (both ? k : 2 * k + half) * kWideKeys; }
+    __device__ __forceinline__ int32_t tiles(int half) const {
+        const int32_t k = count(half);
+        return k == 0 ? 0 : 2 * k - (len - key(half, k - 1) <= kTileKeys ? 1 : 0);
+    }
 };
 
 // What the warps of a CTA share beside the tiles.
 struct WideBars {
-    uint32_t full, empty, scores, weights, queries, output;          // arrays of 8-byte barriers: [stages] x 2, [2] x 4
+    uint32_t full, empty, scores, weights, queries, product, output;           // 8-byte barriers: [stages] x 2, [half][tile & 1] x 2, [half] x 3
 };
 
 __device__ __forceinline__ void store16(uint32_t at, const uint4 &v) {
@@ -199,11 +202,11 @@ __device__ __forceinline__ float2 exp2_by_products(float2 x) {
                        __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
 }
 
-// Columns of O of a warp's rows, times f; few at a time, since the scores are in registers meanwhile.
-template <int COLUMNS>
+// O of a warp's rows, times f; few columns at a time, since the scores are in registers meanwhile.
+template <int D>
 __device__ __forceinline__ void scale_output(uint32_t t_o, float f) {
 #pragma unroll 1
-    for (int b = 0; b < COLUMNS / 16; ++b) {
+    for (int b = 0; b < D / 16; ++b) {
         float o[16];
         tmem_load16(t_o + b * 16, o);
         tmem_load_wait();
@@ -213,28 +216,19 @@ __device__ __forceinline__ void scale_output(uint32_t t_o, float f) {
     }
 }
 
-// Whether any of a half's threads says yes; a barrier for them.
-__device__ __forceinline__ bool any_of_half(int half, bool yes) {
-    uint32_t any;
-    asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %1, 0;\nbarrier.cta.red.or.pred q, %2, %3, p;\nselp.b32 %0, 1, 0, q;\n}"
-                 : "=r"(any)
-                 : "r"((uint32_t)yes), "r"(1 + half), "n"(kHalfThreads)
-                 : "memory");
-    return any != 0;
-}
-
 // Clears the values beyond the last of a tile's `keys` keys, among the sixteen that the product reads last: they may be anything,
-// and 0 * NaN is not 0.  The tile is the piece's last, its values are in stage number `last`.  All threads of a half; one half does it
-// where both read the stage.
+// and 0 * NaN is not 0.  The tile is the last (number `tile` of its step) of the piece, whose last stage, number `last`, holds its
+// values; a half whose tiles end before that has nothing to clear.  All threads of a half; where both halves read the stage
+// both do it, since either may be the first to need it.
 template <int D>
-__device__ __forceinline__ bool clear_values(const WideBars &bars, uint32_t base, volatile int32_t *failed, int32_t keys, int32_t last, int thread, bool other) {
-    if (keys >= kWideKeys || (keys & 15) == 0 || other) return true;
+__device__ __forceinline__ bool clear_values(const WideBars &bars, uint32_t base, volatile int32_t *failed, int32_t keys, int tile, int32_t last, int thread) {
+    if (keys >= kTileKeys || (keys & 15) == 0) return true;
     using Smem = WideSmem<D>;
     const uint32_t stage = last % Smem::kStages;
     if (!bar_wait(bars.full + 8 * stage, (last / Smem::kStages) & 1, failed)) return false;
     const int32_t clear = ((keys + 15) & ~15) - keys;
     for (int32_t c = thread; c < clear * (D / 8); c += kHalfThreads) {
-        const int32_t r = keys + c / (D / 8), chunk = c % (D / 8);
+        const int32_t r = tile * kTileKeys + keys + c / (D / 8), chunk = c % (D / 8);
         store16(base + Smem::kRing + stage * Smem::kStageBytes + (chunk >> 3) * (kWideKeys * 128) + r * 128 + (chunk & 7) * 16, make_uint4(0, 0, 0, 0));
     }
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -242,9 +236,8 @@ __device__ __forceinline__ bool clear_values(const WideBars &bars, uint32_t base
 }
 
 struct WideShared {
-    uint64_t bars[32];
+    uint64_t bars[40];
     WidePiece piece[kPieceBatch];
-    float row[2][kWideHalf];                             // between the two threads of a row
     int32_t pieces, failed;
     uint32_t tmem;
 };
@@ -258,8 +251,8 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
     extern __shared__ __align__(1024) uint8_t s_tiles[];              // the swizzle goes by addresses: tiles begin at multiples of 1024
     WideShared &sh = *reinterpret_cast<WideShared *>(s_tiles + Smem::kSmall);
     const uint32_t base = smem_at(s_tiles), at_bars = smem_at(sh.bars);
-    const WideBars bars = {at_bars, at_bars + 8 * kStages, at_bars + 16 * kStages, at_bars + 16 * kStages + 16, at_bars + 16 * kStages + 32, at_bars + 16 * kStages + 48};
-    static_assert(2 * kStages + 8 <= 32, "barriers");
+    const WideBars bars = {at_bars, at_bars + 8 * kStages, at_bars + 16 * kStages, at_bars + 16 * kStages + 32, at_bars + 16 * kStages + 64, at_bars + 16 * kStages + 80, at_bars + 16 * kStages + 96};
+    static_assert(2 * kStages + 14 <= 40, "barriers");
     const int warp = threadIdx.x >> 5, lane = lane_id();
     bool bad = false;
     if (base & 1023u) {
@@ -275,9 +268,12 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
             bar_init(bars.empty + 8 * s, 2);             // both halves' products
         }
         for (int h = 0; h < 2; ++h) {
-            bar_init(bars.scores + 8 * h, 1);
-            bar_init(bars.weights + 8 * h, kHalfThreads);
+            for (int x = 0; x < 2; ++x) {
+                bar_init(bars.scores + 16 * h + 8 * x, 1);
+                bar_init(bars.weights + 16 * h + 8 * x, kHalfThreads);
+            }
             bar_init(bars.queries + 8 * h, kHalfThreads);
+            bar_init(bars.product + 8 * h, 1);
             bar_init(bars.output + 8 * h, 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -299,7 +295,6 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
         return sh.failed ? 0 : sh.pieces;
     };
     if (warp >= kTmaWarp) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (warp >= kListWarp) {
             Pieces<true> pieces(a, blockIdx.x, bad);
             int32_t n = 1;
@@ -374,7 +369,7 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
             // ---- products of one half
             const int half = warp - kMmaWarp;
             constexpr uint32_t kType = std::is_same<Q, __nv_bfloat16>::value ? 1u : 0u;
-            constexpr uint32_t kIdescS = (1u << 4) | (kType << 7) | (kType << 10) | ((kWideKeys / 8) << 17) | ((kWideHalf / 16) << 24);
+            constexpr uint32_t kIdescS = (1u << 4) | (kType << 7) | (kType << 10) | ((kTileKeys / 8) << 17) | ((kWideHalf / 16) << 24);
             constexpr uint32_t kIdescO = (1u << 4) | (kType << 7) | (kType << 10) | (1u << 16) | ((D / 8) << 17) | ((kWideHalf / 16) << 24);
             // the stages in the order of their first use, as counters that wrap
             uint32_t stage = 0, round = 0, weights_phase = 0, queries_phase = 0;
@@ -391,54 +386,68 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
                 mma_commit(bars.empty + 8 * used);
                 if (!both) mma_commit(bars.empty + 8 * used);
             };
+            uint32_t k_used = 0, v_used = 0;
             while (const int32_t listed = next_batch()) {
                 for (int32_t at = 0; at < listed && ok; ++at) {
                     const bool both = sh.piece[at].both;
-                    const int32_t len = sh.piece[at].len, key0 = sh.piece[at].key0, tiles = sh.piece[at].n;
-                    const int32_t n0 = both ? tiles : (tiles + 1) >> 1, n1 = both ? tiles : tiles >> 1, n = half ? n1 : n0;
+                    const int32_t len = sh.piece[at].len, key0 = sh.piece[at].key0 + (both ? 0 : half * kWideKeys), stride = both ? kWideKeys : 2 * kWideKeys;
+                    const int32_t n0 = sh.piece[at].count(0), n1 = sh.piece[at].count(1), tiles = sh.piece[at].tiles(half);
+                    // scores of tile t, whose step's keys are in stage k_used
+                    auto scores = [&](int32_t t) {
+                        fence_after();
+                        if (ok && elect_one()) {
+                            const uint32_t k = k0 + k_used * (Smem::kStageBytes >> 4) + (t & 1) * ((kTileKeys * 128) >> 4), d = t_s + (t & 1) * kTileKeys;
+#pragma unroll
+                            for (int x = 0; x < D / 16; ++x) {
+                                const uint32_t off = ((x >> 2) * (kWideKeys * 128) + (x & 3) * 32) >> 4;
+                                mma_smem(d, q + off, k + off, kIdescS, x > 0);
+                            }
+                            mma_commit(bars.scores + 16 * half + 8 * (t & 1));
+                            if ((t & 1) || t == tiles - 1) release(k_used, both);
+                        }
+                        __syncwarp();
+                    };
+                    auto product = [&](int32_t t) {
+                        ok = ok && bar_wait(bars.weights + 16 * half + 8 * (t & 1), (weights_phase >> (t & 1)) & 1, failed);
+                        weights_phase ^= 1u << (t & 1);
+                        fence_after();
+                        if (ok && elect_one()) {
+                            const uint32_t v = v0 + v_used * (Smem::kStageBytes >> 4) + (t & 1) * ((kTileKeys * 128) >> 4), w = t_s + (t & 1) * kTileKeys;
+                            const int32_t left = len - key0 - (t >> 1) * stride - (t & 1) * kTileKeys;
+#pragma unroll
+                            for (int g = 0; g < kTileKeys / 16; ++g)
+                                if (g * 16 < left) mma_tmem(t_o, w + g * 8, v + g * (2048 >> 4), kIdescO, t > 0 || g > 0);
+                            mma_commit(bars.product + 8 * half);
+                            if ((t & 1) || t == tiles - 1) release(v_used, both);
+                            if (t == tiles - 1) mma_commit(bars.output + 8 * half);
+                        }
+                        __syncwarp();
+                    };
+                    // stages come in the order in which the halves need them: for each of their steps, first the values of the step before
                     for (int32_t it = 0; it <= n0 && ok; ++it)
                         for (int turn = 0; turn < (both ? 1 : 2) && ok; ++turn) {
                             const bool mine = both || turn == half;
                             const int32_t nt = turn ? n1 : n0;
-                            if (it >= 1 && it - 1 < nt) {
+                            const bool values = it >= 1 && it - 1 < nt, keys = it < nt;
+                            if (values) {
                                 const uint32_t used = next_stage(mine);
-                                if (mine) {
-                                    const int32_t left = len - key0 - (both ? it - 1 : 2 * (it - 1) + half) * kWideKeys;
-                                    ok = ok && bar_wait(bars.weights + 8 * half, weights_phase, failed);
-                                    weights_phase ^= 1;
-                                    fence_after();
-                                    if (ok && elect_one()) {
-                                        const uint32_t v = v0 + used * (Smem::kStageBytes >> 4);
-#pragma unroll
-                                        for (int g = 0; g < kWideKeys / 16; ++g)
-                                            if (g * 16 < left) mma_tmem(t_o, t_s + g * 8, v + g * (2048 >> 4), kIdescO, it > 1 || g > 0);
-                                        release(used, both);
-                                        if (it == n) mma_commit(bars.output + 8 * half);
-                                    }
-                                    __syncwarp();
-                                }
+                                if (mine) v_used = used;
                             }
-                            if (it < nt) {
+                            if (mine && values) product(2 * it - 2);
+                            if (keys) {
                                 const uint32_t used = next_stage(mine);
-                                if (mine) {
-                                    if (it == 0) {
-                                        ok = ok && bar_wait(bars.queries + 8 * half, queries_phase, failed);
-                                        queries_phase ^= 1;
-                                    }
-                                    fence_after();
-                                    if (ok && elect_one()) {
-                                        const uint32_t k = k0 + used * (Smem::kStageBytes >> 4);
-#pragma unroll
-                                        for (int x = 0; x < D / 16; ++x) {
-                                            const uint32_t off = ((x >> 2) * (kWideKeys * 128) + (x & 3) * 32) >> 4;
-                                            mma_smem(t_s, q + off, k + off, kIdescS, x > 0);
-                                        }
-                                        mma_commit(bars.scores + 8 * half);
-                                        release(used, both);
-                                    }
-                                    __syncwarp();
-                                }
+                                if (mine) k_used = used;
                             }
+                            if (!mine) continue;
+                            if (keys) {
+                                if (it == 0) {
+                                    ok = ok && bar_wait(bars.queries + 8 * half, queries_phase, failed);
+                                    queries_phase ^= 1;
+                                }
+                                scores(2 * it);
+                            }
+                            if (values && 2 * it - 1 < tiles) product(2 * it - 1);
+                            if (keys && 2 * it + 1 < tiles) scores(2 * it + 1);
                         }
                 }
                 __syncthreads();
@@ -446,35 +455,32 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
             __syncthreads();
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftmaxRegs));
-        // ---- softmax: two threads have row `row` of a half, for 64 keys of a tile and half of the output's columns each
-        const int half = warp >> 3, side = (warp >> 2) & 1, thread = threadIdx.x & (kHalfThreads - 1), row = threadIdx.x & (kWideHalf - 1);
+        // ---- softmax: thread `row` of a half has row `row` of its scores
+        const int half = warp >> 2, row = threadIdx.x & (kWideHalf - 1);
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);           // this warp's 32 lanes of tensor memory
-        const uint32_t t_s = lanes + half * 128, t_o = lanes + 256 + half * D + side * (D / 2);
-        uint32_t n_scores = 0, n_output = 0;
+        const uint32_t t_s = lanes + half * 128, t_o = lanes + 256 + half * D;
+        uint32_t scores_phase = 0, n_product = 0, n_output = 0;
         int32_t pos = 0;                                 // stages of all pieces before this one
         bool ok = true;
-        // A warp that has failed goes on without waiting or working, so that the barriers of its half stay in step.
         while (const int32_t listed = next_batch()) {
-            for (int32_t at = 0; at < listed; ++at) {
+            for (int32_t at = 0; at < listed && ok; ++at) {
                 const WidePiece &p = sh.piece[at];
-                const int32_t n = p.count(half);
+                const int32_t tiles = p.tiles(half);
                 const int32_t x = (p.both ? half * kWideHalf : 0) + row;      // row of the item
                 QueryRow qr = {-1, 0};
                 if (x < p.rows) qr = query_row(a, p.first, p.seq_rows, p.len, p.prompt, p.h, p.row0 + x);
-                const int32_t limit = qr.limit;
                 const bool warp_has_rows = __any_sync(kFull, qr.out >= 0);
                 float m = -INFINITY, l = 0.f;
-                if (n > 0) {
+                if (tiles > 0) {
                     // queries into shared memory, neighbouring lanes along a row; the products that read the last ones are done (their
                     // output was waited for)
                     if (warp_has_rows) {
                         const int64_t from = qr.out >= 0 ? qr.out / a.Hq * a.q_row_stride + qr.out % a.Hq * D : -1;
                         constexpr int kLanes = D / 8, kRows = kWarp / kLanes;             // lanes to a row, rows at a time
                         const int c = lane % kLanes;
-#pragma unroll
-                        for (int y = 0; y < kLanes / 2; ++y) {
-                            const int r = (side * (kLanes / 2) + y) * kRows + lane / kLanes;
+#pragma unroll 8
+                        for (int y = 0; y < kLanes; ++y) {
+                            const int r = y * kRows + lane / kLanes;
                             const int64_t at_r = __shfl_sync(kFull, from, r);
                             const uint4 v = at_r >= 0 ? __ldg(reinterpret_cast<const uint4 *>(static_cast<const Q *>(a.q) + at_r) + c) : make_uint4(0, 0, 0, 0);
                             const int qrow = (warp & 3) * kWarp + r;
@@ -483,24 +489,24 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     bar_arrive(bars.queries + 8 * half);
-                    for (int32_t k = 0; k < n; ++k) {
-                        const int32_t key0 = p.key(half, k);
-                        ok = ok && bar_wait(bars.scores + 8 * half, n_scores++ & 1, failed);
+                    for (int32_t t = 0; t < tiles; ++t) {
+                        const int32_t key0 = p.key(half, t >> 1) + (t & 1) * kTileKeys;
+                        ok = ok && bar_wait(bars.scores + 16 * half + 8 * (t & 1), (scores_phase >> (t & 1)) & 1, failed);
+                        scores_phase ^= 1u << (t & 1);
                         ok = __all_sync(kFull, ok);
+                        if (!ok) break;
                         fence_after();
-                        const bool work = ok && warp_has_rows;
-                        float s[2][32], top = -INFINITY;
-                        if (work) {
+                        if (warp_has_rows) {
+                            float s[2][32];
 #pragma unroll
-                            for (int b = 0; b < 2; ++b) tmem_load(t_s + side * 64 + b * 32, s[b]);
+                            for (int b = 0; b < 2; ++b) tmem_load(t_s + (t & 1) * kTileKeys + b * 32, s[b]);
                             tmem_load_wait();
-                            const int32_t first = key0 + side * 64;
-                            if (first + 64 > limit) {
+                            if (key0 + kTileKeys > qr.limit) {
 #pragma unroll
                                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                                     for (int e = 0; e < 32; ++e)
-                                        if (first + b * 32 + e >= limit) s[b][e] = -INFINITY;
+                                        if (key0 + b * 32 + e >= qr.limit) s[b][e] = -INFINITY;
                             }
                             float t4[4];
 #pragma unroll
@@ -510,21 +516,19 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
                                 for (int e = 1; e < 15; e += 2) t4[b] = fmaxf(t4[b], fmaxf(s[b >> 1][(b & 1) * 16 + e], s[b >> 1][(b & 1) * 16 + e + 1]));
                                 t4[b] = fmaxf(t4[b], s[b >> 1][(b & 1) * 16 + 15]);
                             }
-                            top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * a.scale_log2;
-                        }
-                        ok = clear_values<D>(bars, base, failed, p.len - key0, pos + 2 * p.n - 1, thread, p.both && half == 1) && ok;
-                        // The barrier also holds back the weights of one thread until the other has read the scores they replace.
-                        if (any_of_half(half, work && (k == 0 || top > m + 8.f))) {
-                            if (side == 0) sh.row[half][row] = top;
-                            any_of_half(half, false);
-                            if (side == 1) sh.row[half][row] = fmaxf(top, sh.row[half][row]);
-                            any_of_half(half, false);
-                            const float up = fmaxf(m, sh.row[half][row]), f = up == -INFINITY ? 1.f : exp2_fast(m - up);
-                            l *= f;
-                            m = up;
-                            if (work && k > 0) scale_output<D / 2>(t_o, f);
-                        }
-                        if (work) {
+                            const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * a.scale_log2;
+                            if (t == 0) {
+                                m = top;
+                            } else if (__any_sync(kFull, top > m + 8.f)) {
+                                // the last product has to be in before its output is scaled
+                                ok = bar_wait(bars.product + 8 * half, (n_product + t - 1) & 1, failed);
+                                ok = __all_sync(kFull, ok);
+                                fence_after();
+                                const float up = fmaxf(m, top), f = up == -INFINITY ? 1.f : exp2_fast(m - up);
+                                l *= f;
+                                m = up;
+                                scale_output<D>(t_o, f);
+                            }
                             // where no key has been seen the reference is -infinity and every weight has to come out as 0
                             const float z = m == -INFINITY ? 0.f : m;
                             float2 sum = make_float2(0.f, 0.f);
@@ -540,57 +544,57 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
                                     sum = add2(sum, y);
                                     w[e] = pack2(y.x, y.y, Q());
                                 }
-                                tmem_store8(t_s + side * 32 + b * 8, w);
+                                tmem_store8(t_s + (t & 1) * kTileKeys + b * 8, w);
                             }
                             l += sum.x + sum.y;
                             tmem_store_wait();
                         }
+                        if (t == tiles - 1) ok = clear_values<D>(bars, base, failed, p.len - key0, t & 1, pos + 2 * p.n - 1, row) && ok;
                         fence_before();
-                        bar_arrive(bars.weights + 8 * half);
+                        bar_arrive(bars.weights + 16 * half + 8 * (t & 1));
                     }
+                    n_product += tiles;
                     ok = ok && bar_wait(bars.output + 8 * half, n_output++ & 1, failed);
                     ok = __all_sync(kFull, ok);
+                    if (!ok) break;
                     fence_after();
                 }
                 pos += 2 * p.n;
-                // the partial: sums of the two threads of a row, then the output
-                const int64_t rows_all = (int64_t)a.R * a.T * a.Hq, out = x < p.rows ? query_row(a, p.first, p.seq_rows, p.len, p.prompt, p.h, p.row0 + x).out : -1;
+                if (!warp_has_rows) continue;
+                // the partial
+                const int64_t rows_all = (int64_t)a.R * a.T * a.Hq;
                 const int64_t place = p.continued ? (int64_t)blockIdx.x * kWideRows + half * kWideHalf + row
-                                                  : (int64_t)((p.prompt ? kPromptPart : kOwnPart) + (!p.both && half ? kSecondHalf : 0)) * rows_all + out;
-                if (side == 1) sh.row[half][row] = l;
-                any_of_half(half, false);
-                if (side == 0 && out >= 0)
-                    *reinterpret_cast<float2 *>((p.continued ? a.cont_ml[1] : a.main_ml) + place * 2) = make_float2(m, l + sh.row[half][row]);
-                if (ok && n > 0 && warp_has_rows) {
-                    // through the query tile, which nobody reads any more, so that neighbouring lanes store along a row
-                    constexpr int kColumns = D / 4, kLanes = kColumns / 4, kRows = kWarp / kLanes;            // columns at a time
-                    const uint32_t tile = base + Smem::kQ + half * Smem::kQBytes + (warp & 7) * (kWarp * kColumns * 4);
-                    float *__restrict__ po = (p.continued ? a.cont_o[1] : a.main_o) + side * (D / 2);
-                    const int64_t from = out >= 0 ? place * D : -1;
-#pragma unroll
-                    for (int y = 0; y < 2; ++y) {
+                                                  : (int64_t)((p.prompt ? kPromptPart : kOwnPart) + (!p.both && half ? kSecondHalf : 0)) * rows_all + qr.out;
+                if (qr.out >= 0) *reinterpret_cast<float2 *>((p.continued ? a.cont_ml[1] : a.main_ml) + place * 2) = make_float2(m, l);
+                if (tiles > 0) {
+                    // through the warp's rows of the query tile, which nobody reads any more, so that neighbouring lanes store along a row
+                    constexpr int kColumns = 32, kLanes = kColumns / 4, kRows = kWarp / kLanes;               // columns at a time
+                    const uint32_t tile = base + Smem::kQ + half * Smem::kQBytes + (warp & 3) * (kWarp * 128);
+                    float *__restrict__ po = p.continued ? a.cont_o[1] : a.main_o;
+                    const int64_t from = qr.out >= 0 ? place * D : -1;
+                    const int c = lane % kLanes;
+#pragma unroll 1
+                    for (int y = 0; y < D / kColumns; ++y) {
                         float o[kColumns];
-                        if constexpr (D == 128) tmem_load(t_o + y * kColumns, o);
-                        else tmem_load16(t_o + y * kColumns, o);
+                        tmem_load(t_o + y * kColumns, o);
                         tmem_load_wait();
                         __syncwarp();
 #pragma unroll
-                        for (int c = 0; c < kLanes; ++c)
-                            store16(tile + lane * (kColumns * 4) + ((c ^ (lane & (kLanes - 1))) << 4),
-                                    make_uint4(__float_as_uint(o[4 * c]), __float_as_uint(o[4 * c + 1]), __float_as_uint(o[4 * c + 2]), __float_as_uint(o[4 * c + 3])));
+                        for (int v = 0; v < kLanes; ++v)
+                            store16(tile + lane * 128 + ((v ^ (lane & 7)) << 4),
+                                    make_uint4(__float_as_uint(o[4 * v]), __float_as_uint(o[4 * v + 1]), __float_as_uint(o[4 * v + 2]), __float_as_uint(o[4 * v + 3])));
                         __syncwarp();
-                        const int c = lane % kLanes;
 #pragma unroll
                         for (int v = 0; v < kLanes; ++v) {
                             const int r = v * kRows + lane / kLanes;
                             const int64_t to = __shfl_sync(kFull, from, r);
-                            const uint4 got = load16(tile + r * (kColumns * 4) + ((c ^ (r & (kLanes - 1))) << 4));
+                            const uint4 got = load16(tile + r * 128 + ((c ^ (r & 7)) << 4));
                             if (to >= 0) *reinterpret_cast<uint4 *>(po + to + y * kColumns + c * 4) = got;
                         }
                     }
+                    __syncwarp();
                 }
                 fence_before();                          // the next item's products may overwrite O: its weights come after this
-                any_of_half(half, false);                // and its queries overwrite the tile that all have to be done with
             }
             __syncthreads();
         }
