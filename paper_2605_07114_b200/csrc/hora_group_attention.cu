@@ -76,6 +76,8 @@ attention_plan_kernel(const AttnArgs a) {
     if (threadIdx.x == kPlanThreads - 1) {
         a.start[0][n] = run[0];
         a.start[1][n] = run[1];
+        a.start[0][n + 1] = max((int64_t)kNarrowMinSteps, (run[0] + a.n_narrow - 1) / a.n_narrow);
+        a.start[1][n + 1] = a.n_wide > 0 ? max((int64_t)1, (run[1] + a.n_wide - 1) / a.n_wide) : 1;
     }
     const int64_t covered = __ldg(a.group_offsets + a.N);
     for (int32_t r = threadIdx.x; r < a.R; r += kPlanThreads) {
@@ -99,45 +101,90 @@ __device__ __forceinline__ int32_t stream_of(int64_t u, int64_t per) {
     return ((u | per) >> 32) == 0 ? (int32_t)((uint32_t)u / (uint32_t)per) : (int32_t)(u / per);
 }
 
-// Where the partials of one row and one of its two sequences are.
+// Where the partials of a row are that come from one of its two sequences; rows are taken in order.
 struct Parts {
     int64_t main;                                        // place among the main ones
+    int64_t u_item, per;                                 // first step of the present item; steps of a stream
     uint32_t cont, count, halves;                        // first continued row, partials of a half, halves
+    int32_t tile_rows, steps, left, at, step_rows;       // rows of an item, its steps, rows of the sequence from the item on, place in the item
     bool wide;
 
-    // partial x of count * halves
-    __device__ __forceinline__ void at(const AttnArgs &a, int64_t rows, uint32_t x, int32_t D, const float *&ml, const float *&o) const {
-        const uint32_t half = x >= count ? 1 : 0, b = x - half * count;
-        if (b == 0) {
-            const int64_t place = main + (int64_t)half * kSecondHalf * rows;
-            ml = a.main_ml + place * 2;
-            o = a.main_o + place * D;
-        } else {
-            const int64_t place = (int64_t)cont + (int64_t)(b - 1) * (wide ? kWideRows : kNarrowRows) + half * kWideHalf;
-            ml = a.cont_ml[wide] + place * 2;
-            o = a.cont_o[wide] + place * D;
+    __device__ __forceinline__ void enter_item() {
+        const int32_t b0 = stream_of(u_item, per);
+        const int64_t last = u_item - b0 * per + steps - 1;
+        count = 1 + (last < per ? 0 : stream_of(last, per));
+        // a wide item of one half has its keys dealt to two halves, each with a partial of its own
+        halves = wide && min(tile_rows, left) <= kWideHalf ? 2 : 1;
+        cont = (uint32_t)(b0 + 1) * step_rows + at;
+    }
+    __device__ __forceinline__ void init(const AttnArgs &a, const Sequence &q, int64_t start, int64_t per_, int32_t part, uint32_t r, uint32_t t, uint32_t h,
+                                         int64_t row, int64_t rows) {
+        main = part * rows + row;
+        count = 0;
+        halves = 1;
+        wide = q.wide;
+        steps = 0;
+        if (q.steps == 0 || (int32_t)r < q.first || (int32_t)r >= q.first + q.rollouts) return;
+        const uint32_t x = ((r - q.first) * a.T + t) * a.g, tile = x / (uint32_t)q.tile_rows;
+        at = x - tile * q.tile_rows;
+        steps = q.steps;
+        tile_rows = q.tile_rows;
+        left = q.rows - (int32_t)tile * q.tile_rows;
+        per = per_;
+        step_rows = q.wide ? kWideRows : kNarrowRows;
+        u_item = start + ((int64_t)h * q.tiles + tile) * q.steps;
+        enter_item();
+    }
+    __device__ __forceinline__ void next_row() {
+        ++main;
+        if (steps == 0) return;
+        ++at;
+        ++cont;
+        if (at == tile_rows) {
+            at = 0;
+            left -= tile_rows;
+            u_item += steps;
+            enter_item();
         }
+    }
+    // partial x of count * halves
+    __device__ __forceinline__ void where(const AttnArgs &a, int64_t rows, uint32_t x, int32_t D, const float *&ml, const float *&o) const {
+        const uint32_t half = x >= count ? 1 : 0, b = x - half * count;
+        const int64_t place = b == 0 ? main + (int64_t)half * kSecondHalf * rows : (int64_t)cont + (b - 1) * step_rows + half * kWideHalf;
+        ml = (b == 0 ? a.main_ml : wide ? a.cont_ml[1] : a.cont_ml[0]) + place * 2;
+        o = (b == 0 ? a.main_o : wide ? a.cont_o[1] : a.cont_o[0]) + place * D;
     }
 };
 
-__device__ __forceinline__ Parts parts_of(const AttnArgs &a, const Sequence &q, int64_t start, int64_t per, int32_t part, uint32_t r, uint32_t t, uint32_t head,
-                                          int64_t row, int64_t rows) {
-    Parts p = {part * rows + row, 0u, 0u, 1u, q.wide};
-    if (q.steps == 0 || (int32_t)r < q.first || (int32_t)r >= q.first + q.rollouts) return p;
-    const uint32_t x = ((r - q.first) * a.T + t) * a.g + head % a.g, tile = x / (uint32_t)q.tile_rows, at = x - tile * q.tile_rows;
-    const int64_t u0 = start + ((int64_t)(head / a.g) * q.tiles + tile) * q.steps;
-    const int32_t b0 = stream_of(u0, per);
-    const int64_t last = u0 - b0 * per + q.steps - 1;
-    p.count = 1 + (last < per ? 0 : stream_of(last, per));
-    // a wide item of one half has its keys dealt to two halves, each with a partial of its own
-    p.halves = q.wide && min(q.tile_rows, q.rows - (int32_t)tile * q.tile_rows) <= kWideHalf ? 2 : 1;
-    p.cont = (uint32_t)(b0 + 1) * (q.wide ? kWideRows : kNarrowRows) + at;
-    return p;
-}
+// Joins the partials of the output rows: a warp to a query's heads of one cache head, D / 32 neighbouring elements a lane.  What
+// bounds the kernel is the chain rollout -> group -> sequence -> partial and the arithmetic on places, so both are done
+// once for all these rows; two rows and four partials of each are in flight at a time.
+constexpr int kJoinRows = 2, kJoinAtOnce = 4;
 
-// Joins the partials of an output row, a warp to a row, D / 32 neighbouring elements a lane.  Partials are taken kJoinAtOnce at a
-// time, all their loads in flight together: what bounds the kernel is the chain rollout -> group -> sequence -> partial.
-constexpr int kJoinAtOnce = 4;
+template <int E>
+struct Row {
+    float m = -INFINITY, l = 0.f, o[E] = {};
+
+    __device__ __forceinline__ void add(const float2 (&ml)[kJoinAtOnce], const float (&y)[kJoinAtOnce][E]) {
+        float top = m;
+#pragma unroll
+        for (int x = 0; x < kJoinAtOnce; ++x) top = fmaxf(top, ml[x].x);
+        if (top == -INFINITY) return;                    // no key seen so far
+        const float f = exp2_fast(m - top);
+        l *= f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] *= f;
+        m = top;
+#pragma unroll
+        for (int x = 0; x < kJoinAtOnce; ++x) {
+            if (ml[x].x == -INFINITY) continue;          // its output may not have been written
+            const float g = exp2_fast(ml[x].x - top);
+            l += ml[x].y * g;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] += y[x][e] * g;
+        }
+    }
+};
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256)
@@ -145,69 +192,76 @@ attention_join_kernel(const AttnArgs a) {
     pdl_enter();
     constexpr int E = D / kWarp;
     const int lane = lane_id();
-    const uint32_t n_rows = (uint32_t)a.R * a.T * a.Hq, row = blockIdx.x * (blockDim.x / kWarp) + (threadIdx.x >> 5);
-    if (row >= n_rows) return;
-    const uint32_t rt = row / a.Hq, head = row - rt * a.Hq, r = rt / a.T, t = rt - r * a.T;
-    const int64_t rows = n_rows;
+    const uint32_t n_tasks = (uint32_t)a.R * a.T * a.Hkv, task = blockIdx.x * (blockDim.x / kWarp) + (threadIdx.x >> 5);
+    if (task >= n_tasks) return;
+    const uint32_t rt = task / a.Hkv, h = task - rt * a.Hkv, r = rt / a.T, t = rt - r * a.T;
+    const int64_t rows = (int64_t)a.R * a.T * a.Hq, row = (int64_t)rt * a.Hq + h * a.g;
     const int32_t grp = __ldg(a.group_of + r);
-    float m = -INFINITY, l = 0.f, o[E] = {};
-    if (grp >= 0 && (int32_t)t < query_count(a, r)) {
+    const bool some = grp >= 0 && (int32_t)t < query_count(a, r);
+    Parts p0, p1;
+    if (some) {
         bool bad = false;
         const Sequence own = sequence(a, a.N + r, bad), prompt = sequence(a, grp, bad);
-        const int64_t per_narrow = steps_per_stream<false>(a), per_wide = a.n_wide > 0 ? steps_per_stream<true>(a) : 1;
-        const Parts p0 = parts_of(a, prompt, __ldg((prompt.wide ? a.start[1] : a.start[0]) + grp), prompt.wide ? per_wide : per_narrow, kPromptPart, r, t, head, row, rows);
-        const Parts p1 = parts_of(a, own, __ldg((own.wide ? a.start[1] : a.start[0]) + a.N + r), own.wide ? per_wide : per_narrow, kOwnPart, r, t, head, row, rows);
-        const uint32_t n0 = p0.count * p0.halves, n = n0 + p1.count * p1.halves;
-        for (uint32_t x0 = 0; x0 < n; x0 += kJoinAtOnce) {
-            float2 ml[kJoinAtOnce];
-            float y[kJoinAtOnce][E];
+        const int64_t per_narrow = steps_per_stream<false>(a), per_wide = steps_per_stream<true>(a);
+        p0.init(a, prompt, __ldg((prompt.wide ? a.start[1] : a.start[0]) + grp), prompt.wide ? per_wide : per_narrow, kPromptPart, r, t, h, row, rows);
+        p1.init(a, own, __ldg((own.wide ? a.start[1] : a.start[0]) + a.N + r), own.wide ? per_wide : per_narrow, kOwnPart, r, t, h, row, rows);
+    }
+    for (int32_t j0 = 0; j0 < a.g; j0 += kJoinRows) {
+        Row<E> sum[kJoinRows];
+        if (some) {
+            Parts q0[kJoinRows], q1[kJoinRows];
+            uint32_t n[kJoinRows], most = 0;
 #pragma unroll
-            for (int x = 0; x < kJoinAtOnce; ++x) {
-                ml[x] = make_float2(-INFINITY, 0.f);
-#pragma unroll
-                for (int e = 0; e < E; ++e) y[x][e] = 0.f;
-                if (x0 + x < n) {
-                    const float *pml, *po;
-                    if (x0 + x < n0) p0.at(a, rows, x0 + x, D, pml, po);
-                    else p1.at(a, rows, x0 + x - n0, D, pml, po);
-                    ml[x] = __ldcg(reinterpret_cast<const float2 *>(pml));
-                    if constexpr (E == 4) {
-                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(po) + lane);
-                        y[x][0] = v.x; y[x][1] = v.y; y[x][2] = v.z; y[x][3] = v.w;
-                    } else {
-                        const float2 v = __ldcg(reinterpret_cast<const float2 *>(po) + lane);
-                        y[x][0] = v.x; y[x][1] = v.y;
-                    }
-                }
+            for (int j = 0; j < kJoinRows; ++j) {
+                q0[j] = p0;
+                q1[j] = p1;
+                n[j] = j0 + j < a.g ? p0.count * p0.halves + p1.count * p1.halves : 0;
+                most = max(most, n[j]);
+                p0.next_row();
+                p1.next_row();
             }
-            float top = m;
+            for (uint32_t x0 = 0; x0 < most; x0 += kJoinAtOnce) {
+                float2 ml[kJoinRows][kJoinAtOnce];
+                float y[kJoinRows][kJoinAtOnce][E];
 #pragma unroll
-            for (int x = 0; x < kJoinAtOnce; ++x) top = fmaxf(top, ml[x].x);
-            if (top == -INFINITY) continue;              // no key seen so far
-            const float f = exp2_fast(m - top);
-            l *= f;
+                for (int j = 0; j < kJoinRows; ++j)
 #pragma unroll
-            for (int e = 0; e < E; ++e) o[e] *= f;
-            m = top;
+                    for (int x = 0; x < kJoinAtOnce; ++x) {
+                        ml[j][x] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-            for (int x = 0; x < kJoinAtOnce; ++x) {
-                const bool none = ml[x].x == -INFINITY;  // its output may not have been written
-                const float g = exp2_fast(ml[x].x - top);
-                if (!none) l += ml[x].y * g;
+                        for (int e = 0; e < E; ++e) y[j][x][e] = 0.f;
+                        if (x0 + x < n[j]) {
+                            const uint32_t n0 = q0[j].count * q0[j].halves;
+                            const float *pml, *po;
+                            if (x0 + x < n0) q0[j].where(a, rows, x0 + x, D, pml, po);
+                            else q1[j].where(a, rows, x0 + x - n0, D, pml, po);
+                            ml[j][x] = __ldcg(reinterpret_cast<const float2 *>(pml));
+                            if constexpr (E == 4) {
+                                const float4 v = __ldcg(reinterpret_cast<const float4 *>(po) + lane);
+                                y[j][x][0] = v.x; y[j][x][1] = v.y; y[j][x][2] = v.z; y[j][x][3] = v.w;
+                            } else {
+                                const float2 v = __ldcg(reinterpret_cast<const float2 *>(po) + lane);
+                                y[j][x][0] = v.x; y[j][x][1] = v.y;
+                            }
+                        }
+                    }
 #pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (!none) o[e] += y[x][e] * g;
+                for (int j = 0; j < kJoinRows; ++j) sum[j].add(ml[j], y[j]);
             }
         }
-    }
-    const float inv = m == -INFINITY ? 0.f : 1.f / l;
-    uint32_t w[E / 2];
 #pragma unroll
-    for (int e = 0; e < E; e += 2) w[e / 2] = pack2(o[e] * inv, o[e + 1] * inv, T());
-    T *__restrict__ out = static_cast<T *>(a.out) + rt * a.out_row_stride + (int64_t)head * D + lane * E;
-    if constexpr (E == 4) *reinterpret_cast<uint2 *>(out) = make_uint2(w[0], w[1]);
-    else *reinterpret_cast<uint32_t *>(out) = w[0];
-    if (a.lse != nullptr && lane == 0) a.lse[row] = m == -INFINITY ? -INFINITY : 0.6931471805599453f * m + logf(l);
+        for (int j = 0; j < kJoinRows; ++j) {
+            if (j0 + j >= a.g) break;
+            const float inv = sum[j].m == -INFINITY ? 0.f : 1.f / sum[j].l;
+            uint32_t w[E / 2];
+#pragma unroll
+            for (int e = 0; e < E; e += 2) w[e / 2] = pack2(sum[j].o[e] * inv, sum[j].o[e + 1] * inv, T());
+            T *__restrict__ out = static_cast<T *>(a.out) + rt * a.out_row_stride + (int64_t)(h * a.g + j0 + j) * D + lane * E;
+            if constexpr (E == 4) *reinterpret_cast<uint2 *>(out) = make_uint2(w[0], w[1]);
+            else *reinterpret_cast<uint32_t *>(out) = w[0];
+            if (a.lse != nullptr && lane == 0) a.lse[row + j0 + j] = sum[j].m == -INFINITY ? -INFINITY : 0.6931471805599453f * sum[j].m + logf(sum[j].l);
+        }
+    }
 }
 
 static hora_status_t launch_plan(const AttnArgs &a, cudaStream_t stream) {
@@ -217,8 +271,8 @@ static hora_status_t launch_plan(const AttnArgs &a, cudaStream_t stream) {
 }
 
 static hora_status_t launch_join(const AttnArgs &a, int32_t q_dtype, int32_t D, cudaStream_t stream) {
-    const int64_t rows = (int64_t)a.R * a.T * a.Hq;
-    const int grid = (int)((rows + 7) / 8);
+    const int64_t tasks = (int64_t)a.R * a.T * a.Hkv;
+    const int grid = (int)((tasks + 7) / 8);
     cudaError_t e;
     if (q_dtype == HORA_DTYPE_BF16)
         e = D == 64 ? launch_pdl(attention_join_kernel<__nv_bfloat16, 64>, grid, 256, 0, stream, a)
@@ -239,11 +293,12 @@ static size_t lay_out(AttnArgs &a, int32_t D, char *base) {
         return p;
     };
     const size_t rows = (size_t)a.R * a.T * a.Hq;
-    a.n_narrow = sm_count() * kNarrowPerSm;
-    a.n_wide = sm_count();
+    a.n_sm = sm_count();
+    a.n_narrow = a.n_sm * kNarrowPerSm;
+    a.n_wide = a.n_sm;
     for (int w = 0; w < 2; ++w) {
         const size_t cont = w ? (size_t)a.n_wide * kWideRows : (size_t)a.n_narrow * kNarrowRows;
-        a.start[w] = reinterpret_cast<int64_t *>(take(((size_t)a.N + a.R + 1) * 8));
+        a.start[w] = reinterpret_cast<int64_t *>(take(((size_t)a.N + a.R + 2) * 8));
         a.cont_o[w] = reinterpret_cast<float *>(take(cont * D * 4));
         a.cont_ml[w] = reinterpret_cast<float *>(take(cont * 2 * 4));
     }
@@ -329,8 +384,7 @@ extern "C" hora_status_t hora_group_attention(const void *q, int32_t q_dtype, in
     a.narrow_keys = narrow_keys(cache_dtype == HORA_DTYPE_E4M3, D);
     a.wide_from = kWideFrom;
     hora_status_t rc = launch_plan(a, s);
-    if (rc == HORA_OK) rc = launch_attention_narrow(a, q_dtype, cache_dtype, D, s);
-    if (rc == HORA_OK && a.n_wide > 0) rc = launch_attention_wide(a, q_dtype, D, s);
+    if (rc == HORA_OK) rc = launch_attention_main(a, q_dtype, cache_dtype, D, s);
     if (rc == HORA_OK) rc = launch_join(a, q_dtype, D, s);
     return rc;
 }

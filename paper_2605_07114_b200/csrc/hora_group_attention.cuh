@@ -3,9 +3,9 @@
 // The work is a list of N + R key sequences: the N prompts' (all queries of the group attend to them) and the R
 // rollouts' own.  A sequence has `rows` query rows for each cache head: (rollout, slot t, head of the cache head's
 // group), in that order.  A block of rows of a sequence and one cache head is an item; an item's keys come in steps.
-// Sequences with few rows to a key are bound by the cache's bytes and go to the kernel for narrow items (mma.sync, a warp
-// to a stream); those with many have the products to do and go to the kernel for wide items (tcgen05, a CTA to a stream).
-// For each kernel all steps of its items, in order, form one line that is cut into equal pieces, one for each of its streams, so
+// Sequences with few rows to a key are bound by the cache's bytes: their items are narrow (mma.sync, a warp to a stream);
+// those with many have the products to do: theirs are wide (tcgen05, a CTA to a stream).  All steps of the narrow
+// items, in order, form one line that is cut into equal pieces, one for each stream, and so do those of the wide items, so
 // every stream has about the same to do whatever the lengths are.  A piece's part of an item is a partial
 // result (m, l, o): m a reference score in units of log2, l = sum 2^(s - m), o = sum 2^(s - m) v.  Partials are joined at
 // the end: m = max m_i, l = sum l_i 2^(m_i - m), o = sum o_i 2^(m_i - m), out = o / l.
@@ -22,6 +22,7 @@ constexpr int kNarrowRows = 16;                          // query rows of a narr
 // keys of its steps: 16 where that is 8 KiB, else 32 (twice the independent work between two looks at the maximum)
 constexpr int narrow_keys(bool f8, int D) { return !f8 && D == 128 ? 16 : 32; }
 constexpr int kNarrowPerSm = 12;                         // streams an SM: 168 registers a lane, 16 KiB of keys and values in flight each
+constexpr int kAttnThreads = kNarrowPerSm * kWarp;
 constexpr int kNarrowMinSteps = 4;                       // a stream shorter than this costs more to join than it saves
 
 constexpr int kWideRows = 256;                           // query rows of a wide item, in two halves
@@ -42,12 +43,12 @@ struct AttnArgs {
     int32_t *status;
     int64_t q_row_stride, out_row_stride, n_pages;
     int32_t N, R, T, Hq, Hkv, g, page_shift, prefix_ld, suffix_ld;
-    int32_t n_narrow, n_wide;                            // streams; n_wide 0: every sequence is narrow
+    int32_t n_sm, n_narrow, n_wide;                      // CTAs, streams of each line; n_wide 0: every sequence is narrow
     int32_t narrow_keys;                                 // keys of a narrow step
     int32_t wide_from;                                   // rows from which a sequence is wide
     float scale_log2;                                    // sm_scale * log2(e)
     // workspace
-    int64_t *start[2];                                   // [N + R + 1] first step of each sequence on the narrow, the wide line
+    int64_t *start[2];                                   // [N + R + 2] first step of each sequence on the narrow, the wide line; all; a stream's
     int32_t *group_of;                                   // [R] group of each rollout, -1: none
     float *main_o, *main_ml;                             // [2 or 4][R * T * Hq][D], [..][2], by part
     float *cont_o[2], *cont_ml[2];                       // [streams][rows of an item][D], [..][2]
@@ -110,12 +111,9 @@ __device__ __forceinline__ Sequence sequence(const AttnArgs &a, int32_t i, bool 
 
 __device__ __forceinline__ int64_t total_steps(const AttnArgs &a, const Sequence &s) { return (int64_t)s.steps * s.tiles * a.Hkv; }
 
-// Steps of a line that go to one stream.
+// Steps of a line that go to one stream; the plan leaves it behind the line's starts.
 template <bool WIDE>
-__device__ __forceinline__ int64_t steps_per_stream(const AttnArgs &a) {
-    const int64_t total = __ldg(a.start[WIDE] + a.N + a.R), n = WIDE ? a.n_wide : a.n_narrow;
-    return max((int64_t)(WIDE ? 1 : kNarrowMinSteps), (total + n - 1) / n);
-}
+__device__ __forceinline__ int64_t steps_per_stream(const AttnArgs &a) { return __ldg(a.start[WIDE] + a.N + a.R + 1); }
 
 // A stream's part of one item.
 struct Piece {
@@ -189,7 +187,6 @@ __device__ __forceinline__ QueryRow query_row(const AttnArgs &a, int32_t first, 
     return q;
 }
 
-hora_status_t launch_attention_narrow(const AttnArgs &a, int32_t q_dtype, int32_t cache_dtype, int32_t D, cudaStream_t stream);
-hora_status_t launch_attention_wide(const AttnArgs &a, int32_t q_dtype, int32_t D, cudaStream_t stream);
+hora_status_t launch_attention_main(const AttnArgs &a, int32_t q_dtype, int32_t cache_dtype, int32_t D, cudaStream_t stream);
 
 }  // namespace hora

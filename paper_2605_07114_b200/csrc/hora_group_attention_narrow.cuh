@@ -1,4 +1,4 @@
-// hora_group_attention, the kernel for narrow items, up to 16 query rows: decode of single tokens over long caches.
+// hora_group_attention: narrow items, up to 16 query rows: decode of single tokens over long caches.
 //
 // The call is bound by the cache's bytes (16 rows or fewer to a key: at most 16 products a byte), so the tensor unit matters only in
 // that it has to be out of the way, and what counts is bytes in flight.  Every warp is a stream of its own, with its own
@@ -18,14 +18,14 @@
 // An e4m3 cache is multiplied in fp16, which holds its codes exactly: a row's power-of-two scale is applied to its score, and to
 // its weight relative to the largest value scale met so far, so that weights stay within [0, 1]; queries are scaled by a power of
 // two to lie well within fp16's range.
+#pragma once
+
 #include <type_traits>
 
 #include "hora_group_attention.cuh"
 
 namespace hora {
 
-constexpr int kNarrowThreads = 128;
-constexpr int kNarrowWarps = kNarrowThreads / kWarp;
 constexpr int kRingBytes = 16384;                        // stages of one warp
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
@@ -94,22 +94,18 @@ struct Stage {
     static __device__ __forceinline__ int key_of(int n) { return kRowBytes == 64 ? n : n ^ ((n & 1) << 2); }
 };
 
+// One stream, by one warp, with its ring at `ring` in shared memory.
 template <typename Q, bool F8, int D>
-__global__ void __launch_bounds__(kNarrowThreads, kNarrowPerSm / kNarrowWarps)
-attention_narrow_kernel(const AttnArgs a) {
-    pdl_enter();
+__device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream, uint32_t ring) {
     using M = std::conditional_t<F8, __half, Q>;                  // the type of the products
     using St = Stage<F8, D>;
     constexpr int kBlocks = F8 ? D / 64 : D / 32;                 // 16-byte loads of a lane for each key in K
     constexpr int kHalves = F8 ? 1 : D / 64;                      // and for each key in V (one-byte values, D = 64: 8 bytes)
     constexpr int kOut = D / 8;                                   // column tiles of the output
     constexpr int kStages = St::kStages, kKeys = St::kKeys, kEights = kKeys / 8, kSixteens = kKeys / 16;
-    extern __shared__ __align__(128) uint8_t s_ring[];
-    const int lane = lane_id(), warp = threadIdx.x >> 5;
+    const int lane = lane_id();
     const int n = lane >> 2, c = lane & 3;
-    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(s_ring) + warp * St::kWarpBytes;
     const uint32_t exps = ring + kStages * St::kBytes;
-    const int32_t stream = blockIdx.x * kNarrowWarps + warp;
     const int64_t rows_all = (int64_t)a.R * a.T * a.Hq;
     bool bad = false;
     Pieces<false> pieces(a, stream, bad);
@@ -387,25 +383,6 @@ attention_narrow_kernel(const AttnArgs a) {
         }
     }
     if (bad) raise_status(a.status, HORA_ERR_INVALID_VALUE);
-}
-
-template <typename Q, bool F8, int D>
-static hora_status_t launch_narrow(const AttnArgs &a, cudaStream_t stream) {
-    constexpr int kSmem = kNarrowWarps * Stage<F8, D>::kWarpBytes;
-    cudaError_t e = cudaFuncSetAttribute(attention_narrow_kernel<Q, F8, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    if (e == cudaSuccess) e = launch_pdl(attention_narrow_kernel<Q, F8, D>, a.n_narrow / kNarrowWarps, kNarrowThreads, kSmem, stream, a);
-    count_launches(1);
-    return cuda_ok(e);
-}
-
-hora_status_t launch_attention_narrow(const AttnArgs &a, int32_t q_dtype, int32_t cache_dtype, int32_t D, cudaStream_t stream) {
-    const bool bf = q_dtype == HORA_DTYPE_BF16;
-    if (cache_dtype == HORA_DTYPE_E4M3) {
-        if (D == 64) return bf ? launch_narrow<__nv_bfloat16, true, 64>(a, stream) : launch_narrow<__half, true, 64>(a, stream);
-        return bf ? launch_narrow<__nv_bfloat16, true, 128>(a, stream) : launch_narrow<__half, true, 128>(a, stream);
-    }
-    if (D == 64) return bf ? launch_narrow<__nv_bfloat16, false, 64>(a, stream) : launch_narrow<__half, false, 64>(a, stream);
-    return bf ? launch_narrow<__nv_bfloat16, false, 128>(a, stream) : launch_narrow<__half, false, 128>(a, stream);
 }
 
 }  // namespace hora

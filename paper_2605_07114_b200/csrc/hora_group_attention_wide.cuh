@@ -1,4 +1,4 @@
-// hora_group_attention, the kernel for wide items: many query rows to a key, as the prompt's keys of a large group have.
+// hora_group_attention: wide items: many query rows to a key, as the prompt's keys of a large group have.
 //
 // S = Q K^T and O += P V on the tensor cores' own memory: tcgen05.mma takes 128 rows at a time, S (128 x 64, twice) and O
 // (128 x D) are accumulated in tensor memory, the weights P replace the scores there and are the left operand of the second
@@ -14,6 +14,8 @@
 //   Keys beyond the length are not fetched; the product stops at the last sixteen that hold one, and what is beyond the length
 // among those is cleared in shared memory first (0 * NaN is not 0).
 //   Every wait has a limit; a wait that reaches it makes the CTA give up and report HORA_ERR_INTERNAL.
+#pragma once
+
 #include <cuda.h>
 
 #include <type_traits>
@@ -24,7 +26,7 @@ namespace hora {
 
 constexpr int kSoftmaxWarps = 8, kHalfThreads = kSoftmaxWarps / 2 * kWarp;
 constexpr int kTmaWarp = kSoftmaxWarps, kMmaWarp = kTmaWarp + 1, kListWarp = kMmaWarp + 2;        // one for TMA, one a half for the products, one to list the pieces
-constexpr int kWideThreads = (kListWarp + 1) * kWarp;
+static_assert((kListWarp + 1) * kWarp == kAttnThreads, "every warp has a role");
 constexpr int kTileKeys = 64;
 constexpr int kPieceBatch = 16;                          // pieces listed at a time
 constexpr uint32_t kWaitTries = 4000000;                 // of at least a microsecond each unless the barrier is passed
@@ -242,23 +244,17 @@ struct WideShared {
     uint32_t tmem;
 };
 
+// One stream, by a whole CTA, with its tiles and WideShared at s_tiles.  All threads return together.
 template <typename Q, int D>
-__global__ void __launch_bounds__(kWideThreads, 1)
-attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
-    pdl_enter();
+__device__ __forceinline__ void wide_stream(const AttnArgs &a, const CUtensorMap &k_map, const CUtensorMap &v_map, uint8_t *s_tiles) {
     using Smem = WideSmem<D>;
     constexpr int kStages = Smem::kStages, kParts = D / 64;
-    extern __shared__ __align__(1024) uint8_t s_tiles[];              // the swizzle goes by addresses: tiles begin at multiples of 1024
     WideShared &sh = *reinterpret_cast<WideShared *>(s_tiles + Smem::kSmall);
     const uint32_t base = smem_at(s_tiles), at_bars = smem_at(sh.bars);
     const WideBars bars = {at_bars, at_bars + 8 * kStages, at_bars + 16 * kStages, at_bars + 16 * kStages + 32, at_bars + 16 * kStages + 64, at_bars + 16 * kStages + 80, at_bars + 16 * kStages + 96};
     static_assert(2 * kStages + 14 <= 40, "barriers");
     const int warp = threadIdx.x >> 5, lane = lane_id();
     bool bad = false;
-    if (base & 1023u) {
-        raise_status(a.status, HORA_ERR_INTERNAL);
-        return;
-    }
     if ((int64_t)blockIdx.x * steps_per_stream<true>(a) >= __ldg(a.start[1] + a.N + a.R)) return;       // nothing on this stream
 
     if (threadIdx.x == 0) {
@@ -608,42 +604,6 @@ attention_wide_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_ma
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
     }
-}
-
-// One pool as a matrix of [pages * heads * page_size] rows of D elements, fetched 64 elements of one page's rows at a time.
-static bool pool_map(CUtensorMap *map, const void *pool, int32_t dtype, int64_t rows, int32_t D, int32_t page) {
-    using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
-                                const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-    static const Encode encode = [] {
-        void *f = nullptr;
-        cudaDriverEntryPointQueryResult found;
-        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
-            f = nullptr;
-        return reinterpret_cast<Encode>(f);
-    }();
-    if (encode == nullptr) return false;
-    const cuuint64_t dims[2] = {(cuuint64_t)D, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)D * 2};
-    const cuuint32_t box[2] = {64, (cuuint32_t)page}, steps[2] = {1, 1};
-    return encode(map, dtype == HORA_DTYPE_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(pool), dims,
-                  strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-template <typename Q, int D>
-static hora_status_t launch_wide(const AttnArgs &a, int32_t dtype, cudaStream_t stream) {
-    CUtensorMap k, v;
-    const int64_t rows = (a.n_pages * a.Hkv) << a.page_shift;
-    if (!pool_map(&k, a.k_cache, dtype, rows, D, 1 << a.page_shift) || !pool_map(&v, a.v_cache, dtype, rows, D, 1 << a.page_shift)) return HORA_ERR_CUDA;
-    constexpr int kSmem = WideSmem<D>::kSmall + sizeof(WideShared);
-    cudaError_t e = cudaFuncSetAttribute(attention_wide_kernel<Q, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    if (e == cudaSuccess) e = launch_pdl(attention_wide_kernel<Q, D>, a.n_wide, kWideThreads, kSmem, stream, a, k, v);
-    count_launches(1);
-    return cuda_ok(e);
-}
-
-hora_status_t launch_attention_wide(const AttnArgs &a, int32_t q_dtype, int32_t D, cudaStream_t stream) {
-    if (q_dtype == HORA_DTYPE_BF16) return D == 64 ? launch_wide<__nv_bfloat16, 64>(a, q_dtype, stream) : launch_wide<__nv_bfloat16, 128>(a, q_dtype, stream);
-    return D == 64 ? launch_wide<__half, 64>(a, q_dtype, stream) : launch_wide<__half, 128>(a, q_dtype, stream);
 }
 
 }  // namespace hora
