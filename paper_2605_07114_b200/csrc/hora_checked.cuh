@@ -7,6 +7,9 @@
 // index is computed from device DATA (histogram bins taken from key bits, list slots handed out by atomics, row
 // positions found by searches, slab positions derived from offsets); loop counters that run to a bound stated
 // next to them are left alone.
+//
+// HORA_IN(index, count) is the same check for accesses that are not array elements (asynchronous copies, shared memory by
+// address): false, and recorded, where the index is outside, and the caller leaves the access out; true in the normal build.
 #pragma once
 
 #include "hora_common.cuh"
@@ -28,11 +31,20 @@ __device__ __forceinline__ T &checked_at(T *arr, long long i, long long n, unsig
     return arr[i];
 }
 
+// Whether index i lies in [0, n); records where it does not, so that the caller leaves the access out.
+__device__ __forceinline__ bool checked_in(long long i, long long n, unsigned site) {
+    if (i >= 0 && i < n) return true;
+    atomicCAS(&g_check_word, 0u, site);
+    return false;
+}
+
 // host: every checked translation unit registers how to read (and clear) its word
 void register_check_word(unsigned (*fetch_and_clear)());
 
 #define HORA_AT(arr, i, n) \
     (::hora::checked_at((arr), (long long)(i), (long long)(n), (unsigned)((HORA_FILE_ID << 20) | __LINE__)))
+
+#define HORA_IN(i, n) (::hora::checked_in((long long)(i), (long long)(n), (unsigned)((HORA_FILE_ID << 20) | __LINE__)))
 
 #define HORA_CHECKED_REGISTER()                                                                  \
     namespace {                                                                                  \
@@ -49,6 +61,7 @@ void register_check_word(unsigned (*fetch_and_clear)());
     }
 #else
 #define HORA_AT(arr, i, n) ((arr)[i])
+#define HORA_IN(i, n) true
 #define HORA_CHECKED_REGISTER()
 #endif
 

@@ -1,5 +1,8 @@
 // hora_group_attention: plan, joining of the partial results, and the C entry.
+#define HORA_FILE_ID 5
 #include "hora_group_attention.cuh"
+
+HORA_CHECKED_REGISTER()
 
 namespace hora {
 
@@ -22,7 +25,7 @@ attention_plan_kernel(const AttnArgs a) {
     bool kept_wide[kPlanKept];
     const bool in_shared = a.N + 1 <= kPlanOffsets;
     if (in_shared)
-        for (int32_t i = threadIdx.x; i <= a.N; i += kPlanThreads) s_off[i] = __ldg(a.group_offsets + i);
+        for (int32_t i = threadIdx.x; i <= a.N; i += kPlanThreads) s_off[i] = __ldcg(a.group_offsets + i);
 #pragma unroll
     for (int x = 0; x < kPlanKept; ++x) {
         kept[x] = 0;
@@ -79,14 +82,14 @@ attention_plan_kernel(const AttnArgs a) {
         a.start[0][n + 1] = max((int64_t)kNarrowMinSteps, (run[0] + a.n_narrow - 1) / a.n_narrow);
         a.start[1][n + 1] = a.n_wide > 0 ? max((int64_t)1, (run[1] + a.n_wide - 1) / a.n_wide) : 1;
     }
-    const int64_t covered = __ldg(a.group_offsets + a.N);
+    const int64_t covered = __ldcg(a.group_offsets + a.N);
     for (int32_t r = threadIdx.x; r < a.R; r += kPlanThreads) {
         int32_t g = -1;
         if (r < covered) {
             int32_t l = 0, h = a.N - 1;                  // the last group that begins at or before r
             while (l < h) {
                 const int32_t mid = (l + h + 1) >> 1;
-                if ((in_shared ? s_off[mid] : __ldg(a.group_offsets + mid)) <= r) l = mid;
+                if ((in_shared ? s_off[mid] : __ldcg(a.group_offsets + mid)) <= r) l = mid;
                 else h = mid - 1;
             }
             g = l;
@@ -148,11 +151,13 @@ struct Parts {
         }
     }
     // partial x of count * halves
-    __device__ __forceinline__ void where(const AttnArgs &a, int64_t rows, uint32_t x, int32_t D, const float *&ml, const float *&o) const {
+    __device__ __forceinline__ bool where(const AttnArgs &a, int64_t rows, uint32_t x, int32_t D, const float *&ml, const float *&o) const {
         const uint32_t half = x >= count ? 1 : 0, b = x - half * count;
         const int64_t place = b == 0 ? main + (int64_t)half * kSecondHalf * rows : (int64_t)cont + (b - 1) * step_rows + half * kWideHalf;
+        if (!HORA_IN(place, b == 0 ? 4 * rows : wide ? (int64_t)a.n_wide * kWideRows : (int64_t)a.n_narrow * kNarrowRows)) return false;
         ml = (b == 0 ? a.main_ml : wide ? a.cont_ml[1] : a.cont_ml[0]) + place * 2;
         o = (b == 0 ? a.main_o : wide ? a.cont_o[1] : a.cont_o[0]) + place * D;
+        return true;
     }
 };
 
@@ -196,15 +201,15 @@ attention_join_kernel(const AttnArgs a) {
     if (task >= n_tasks) return;
     const uint32_t rt = task / a.Hkv, h = task - rt * a.Hkv, r = rt / a.T, t = rt - r * a.T;
     const int64_t rows = (int64_t)a.R * a.T * a.Hq, row = (int64_t)rt * a.Hq + h * a.g;
-    const int32_t grp = __ldg(a.group_of + r);
+    const int32_t grp = __ldcg(a.group_of + r);
     const bool some = grp >= 0 && (int32_t)t < query_count(a, r);
     Parts p0, p1;
     if (some) {
         bool bad = false;
         const Sequence own = sequence(a, a.N + r, bad), prompt = sequence(a, grp, bad);
         const int64_t per_narrow = steps_per_stream<false>(a), per_wide = steps_per_stream<true>(a);
-        p0.init(a, prompt, __ldg((prompt.wide ? a.start[1] : a.start[0]) + grp), prompt.wide ? per_wide : per_narrow, kPromptPart, r, t, h, row, rows);
-        p1.init(a, own, __ldg((own.wide ? a.start[1] : a.start[0]) + a.N + r), own.wide ? per_wide : per_narrow, kOwnPart, r, t, h, row, rows);
+        p0.init(a, prompt, __ldcg((prompt.wide ? a.start[1] : a.start[0]) + grp), prompt.wide ? per_wide : per_narrow, kPromptPart, r, t, h, row, rows);
+        p1.init(a, own, __ldcg((own.wide ? a.start[1] : a.start[0]) + a.N + r), own.wide ? per_wide : per_narrow, kOwnPart, r, t, h, row, rows);
     }
     for (int32_t j0 = 0; j0 < a.g; j0 += kJoinRows) {
         Row<E> sum[kJoinRows];
@@ -233,8 +238,7 @@ attention_join_kernel(const AttnArgs a) {
                         if (x0 + x < n[j]) {
                             const uint32_t n0 = q0[j].count * q0[j].halves;
                             const float *pml, *po;
-                            if (x0 + x < n0) q0[j].where(a, rows, x0 + x, D, pml, po);
-                            else q1[j].where(a, rows, x0 + x - n0, D, pml, po);
+                            if (!(x0 + x < n0 ? q0[j].where(a, rows, x0 + x, D, pml, po) : q1[j].where(a, rows, x0 + x - n0, D, pml, po))) continue;
                             ml[j][x] = __ldcg(reinterpret_cast<const float2 *>(pml));
                             if constexpr (E == 4) {
                                 const float4 v = __ldcg(reinterpret_cast<const float4 *>(po) + lane);

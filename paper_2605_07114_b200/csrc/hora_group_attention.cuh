@@ -14,6 +14,7 @@
 // that goes on with an item begun by an earlier stream is the first thing its stream does, so that one has a place for each stream.
 #pragma once
 
+#include "hora_checked.cuh"
 #include "hora_rows16.cuh"
 
 namespace hora {
@@ -76,24 +77,25 @@ __device__ __forceinline__ int32_t checked_len(int32_t len, int32_t ld, int32_t 
 }
 
 __device__ __forceinline__ int32_t query_count(const AttnArgs &a, int32_t r) {
-    const int32_t n = a.q_len ? __ldg(a.q_len + r) : a.T;
+    const int32_t n = a.q_len ? __ldcg(a.q_len + r) : a.T;
     return n < 0 ? 0 : (n > a.T ? a.T : n);
 }
 
 __device__ __forceinline__ Sequence sequence(const AttnArgs &a, int32_t i, bool &bad) {
-    Sequence s;
+    Sequence s = {};
+    if (!HORA_IN(i, a.N + a.R)) return s;
     if (i < a.N) {
-        const int64_t lo = __ldg(a.group_offsets + i), hi = __ldg(a.group_offsets + i + 1);
+        const int64_t lo = __ldcg(a.group_offsets + i), hi = __ldcg(a.group_offsets + i + 1);
         if (lo < 0 || hi < lo || hi > a.R || (i == 0 && lo != 0)) bad = true;
         s.first = clamp_i64(lo, 0, a.R);
         s.rollouts = clamp_i64(hi, s.first, a.R) - s.first;
-        s.len = checked_len(__ldg(a.prefix_len + i), a.prefix_ld, a.page_shift, bad);
+        s.len = checked_len(__ldcg(a.prefix_len + i), a.prefix_ld, a.page_shift, bad);
     } else {
         s.first = i - a.N;
-        const int32_t n = a.q_len ? __ldg(a.q_len + s.first) : a.T;
+        const int32_t n = a.q_len ? __ldcg(a.q_len + s.first) : a.T;
         if (n < 0 || n > a.T) bad = true;
-        s.rollouts = s.first < __ldg(a.group_offsets + a.N) ? 1 : 0;
-        s.len = checked_len(__ldg(a.suffix_len + s.first), a.suffix_ld, a.page_shift, bad);
+        s.rollouts = s.first < __ldcg(a.group_offsets + a.N) ? 1 : 0;
+        s.len = checked_len(__ldcg(a.suffix_len + s.first), a.suffix_ld, a.page_shift, bad);
     }
     s.rows = s.rollouts * a.T * a.g;
     s.wide = a.n_wide > 0 && s.rows >= a.wide_from;
@@ -113,7 +115,7 @@ __device__ __forceinline__ int64_t total_steps(const AttnArgs &a, const Sequence
 
 // Steps of a line that go to one stream; the plan leaves it behind the line's starts.
 template <bool WIDE>
-__device__ __forceinline__ int64_t steps_per_stream(const AttnArgs &a) { return __ldg(a.start[WIDE] + a.N + a.R + 1); }
+__device__ __forceinline__ int64_t steps_per_stream(const AttnArgs &a) { return __ldcg(a.start[WIDE] + a.N + a.R + 1); }
 
 // A stream's part of one item.
 struct Piece {
@@ -134,24 +136,25 @@ struct Pieces {
         const int32_t n_seq = a.N + a.R;
         const int64_t per = steps_per_stream<WIDE>(a);
         u = (int64_t)stream * per;
-        u_end = min(__ldg(start + n_seq), u + per);
+        u_end = min(__ldcg(start + n_seq), u + per);
         i = 0;
         if (u >= u_end) return;
         for (int32_t hi = n_seq; hi - i > 1;) {          // start[i] <= u < start[hi], 32 probes at a time
             const int32_t gap = (hi - i + kWarp - 1) / kWarp;
             const int32_t probe = min(hi, i + lane_id() * gap);
-            const unsigned at_or_before = __ballot_sync(kFull, probe < hi && __ldg(start + probe) <= u);
+            const unsigned at_or_before = __ballot_sync(kFull, probe < hi && __ldcg(start + probe) <= u);
             const int32_t top = 31 - __clz(at_or_before); // lane 0 always is
             hi = min(hi, i + (top + 1) * gap);
             i += top * gap;
         }
         s = sequence(a, i, bad);
-        s_start = __ldg(start + i);
+        s_start = __ldcg(start + i);
     }
 
     __device__ __forceinline__ bool next(const AttnArgs &a, Piece &p, bool &bad) {
         if (u >= u_end) return false;
         while (s.wide != WIDE || u >= s_start + total_steps(a, s)) {        // on to the next sequence with steps on this line
+            if (!HORA_IN(i + 1, a.N + a.R)) return false;
             if (s.wide == WIDE) s_start += total_steps(a, s);
             s = sequence(a, ++i, bad);
         }

@@ -1,8 +1,11 @@
 // hora_group_attention: the kernel.  One CTA of twelve warps to an SM: together they are a stream of the wide line (products on
 // tcgen05), then each of them is a stream of the narrow line.  One launch for both, so that no SM waits for the slowest
 // of the others in between.
+#define HORA_FILE_ID 6
 #include "hora_group_attention_narrow.cuh"
 #include "hora_group_attention_wide.cuh"
+
+HORA_CHECKED_REGISTER()
 
 namespace hora {
 
@@ -11,9 +14,6 @@ constexpr int attention_smem() {
     constexpr int kRings = kNarrowPerSm * Stage<F8, D>::kWarpBytes, kWide = WideSmem<D>::kSmall + (int)sizeof(WideShared);
     return F8 || kRings > kWide ? kRings : kWide;
 }
-
-// Tiles of 128-byte rows are swizzled by address: they begin at multiples of 1024.
-extern __shared__ __align__(1024) uint8_t s_attention[];
 
 template <typename Q, int D>
 __global__ void __launch_bounds__(kAttnThreads, 1)

@@ -26,6 +26,9 @@
 
 namespace hora {
 
+// Tiles of 128-byte rows are swizzled by address: they begin at multiples of 1024.
+extern __shared__ __align__(1024) uint8_t s_attention[];
+
 constexpr int kRingBytes = 16384;                        // stages of one warp
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
@@ -50,7 +53,15 @@ __device__ __forceinline__ float quad_sum(float v) {
 
 __device__ __forceinline__ float exponent_byte(uint32_t b) { return __uint_as_float(b ? b << 23 : 0x400000u); }
 
+// Shared memory by address: 0 where an access of `bytes` bytes at `at` lies in the kernel's.
+__device__ __forceinline__ uint32_t in_shared(uint32_t at, uint32_t bytes) {
+    uint32_t size;
+    asm("mov.u32 %0, %%dynamic_smem_size;" : "=r"(size));
+    return at - (uint32_t)__cvta_generic_to_shared(s_attention) <= size - bytes ? 0u : 1u;
+}
+
 __device__ __forceinline__ void copy16(uint32_t to, const void *from) {
+    if (!HORA_IN(in_shared(to, 16), 1)) return;
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
@@ -58,16 +69,19 @@ template <int LEFT>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
 __device__ __forceinline__ uint4 lds16(uint32_t at) {
+    if (!HORA_IN(in_shared(at, 16), 1)) return make_uint4(0, 0, 0, 0);
     uint4 v;
     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at));
     return v;
 }
 __device__ __forceinline__ uint2 lds8(uint32_t at) {
+    if (!HORA_IN(in_shared(at, 8), 1)) return make_uint2(0, 0);
     uint2 v;
     asm volatile("ld.shared.v2.b32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at));
     return v;
 }
 __device__ __forceinline__ uint32_t lds1(uint32_t at) {
+    if (!HORA_IN(in_shared(at, 1), 1)) return 0u;
     uint32_t v;
     asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(at));
     return v;
@@ -126,7 +140,7 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
 #pragma unroll
             for (int y = 0; y < kSixteens; ++y) {
                 const int32_t key = step * kKeys + y * 16;
-                p.id[y] = step < step1 && key < s.len ? __ldg(w.pages + (key >> a.page_shift)) : 0;
+                p.id[y] = step < step1 && key < s.len && HORA_IN(key >> a.page_shift, w.prompt ? a.prefix_ld : a.suffix_ld) ? __ldcg(w.pages + (key >> a.page_shift)) : 0;
             }
             return p;
         };
@@ -141,6 +155,7 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
                     int32_t page = p.id[y];
                     if (page < 0 || page >= a.n_pages) { bad = true; page = 0; }
                     const int64_t row = (((int64_t)page * a.Hkv + h) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
+                    if (!HORA_IN(row + 15, (a.n_pages * a.Hkv) << a.page_shift)) break;
                     const uint8_t *__restrict__ k = static_cast<const uint8_t *>(a.k_cache) + row * St::kRowBytes + lane * 16;
                     const uint8_t *__restrict__ v = static_cast<const uint8_t *>(a.v_cache) + row * St::kRowBytes + lane * 16;
 #pragma unroll
@@ -178,8 +193,8 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
                 const int dim = F8 ? (b >> 1) * 64 + c * 16 + (b & 1) * 8 : b * 32 + c * 8;
                 x0[b] = x1[b] = make_uint4(0, 0, 0, 0);
                 const Q *__restrict__ q = static_cast<const Q *>(a.q);
-                if (row0.out >= 0) x0[b] = __ldg(reinterpret_cast<const uint4 *>(q + row0.out / a.Hq * a.q_row_stride + row0.out % a.Hq * D + dim));
-                if (row1.out >= 0) x1[b] = __ldg(reinterpret_cast<const uint4 *>(q + row1.out / a.Hq * a.q_row_stride + row1.out % a.Hq * D + dim));
+                if (row0.out >= 0 && HORA_IN(row0.out, rows_all)) x0[b] = __ldcg(reinterpret_cast<const uint4 *>(q + row0.out / a.Hq * a.q_row_stride + row0.out % a.Hq * D + dim));
+                if (row1.out >= 0 && HORA_IN(row1.out, rows_all)) x1[b] = __ldcg(reinterpret_cast<const uint4 *>(q + row1.out / a.Hq * a.q_row_stride + row1.out % a.Hq * D + dim));
             }
             if constexpr (F8) {
                 // to fp16 with the row's largest value in [64, 128): smaller ones keep 11 bits down to 2^-21 of it
@@ -368,6 +383,7 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
             const int64_t out = half ? row1.out : row0.out;
             if (out < 0) continue;
             const int64_t place = step0 > 0 ? (int64_t)stream * kNarrowRows + n + half * 8 : (w.prompt ? kPromptPart : kOwnPart) * rows_all + out;
+            if (!HORA_IN(place, step0 > 0 ? (int64_t)a.n_narrow * kNarrowRows : 2 * rows_all)) continue;
             float *__restrict__ po = (step0 > 0 ? a.cont_o[0] : a.main_o) + place * D;
             const float f = F8 ? v_unit : 1.f;
 #pragma unroll

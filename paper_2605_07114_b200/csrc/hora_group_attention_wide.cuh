@@ -20,7 +20,7 @@
 
 #include <type_traits>
 
-#include "hora_group_attention.cuh"
+#include "hora_group_attention_narrow.cuh"
 
 namespace hora {
 
@@ -67,6 +67,7 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
         if (*failed) return false;
     }
     *failed = 1;
+    (void)HORA_IN(-1, 1);
     return false;
 }
 
@@ -164,10 +165,12 @@ struct WideBars {
 };
 
 __device__ __forceinline__ void store16(uint32_t at, const uint4 &v) {
+    if (!HORA_IN(in_shared(at, 16), 1)) return;
     asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 __device__ __forceinline__ uint4 load16(uint32_t at) {
-    uint4 v;
+    uint4 v = make_uint4(0, 0, 0, 0);
+    if (!HORA_IN(in_shared(at, 16), 1)) return v;
     asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
     return v;
 }
@@ -255,7 +258,7 @@ __device__ __forceinline__ void wide_stream(const AttnArgs &a, const CUtensorMap
     static_assert(2 * kStages + 14 <= 40, "barriers");
     const int warp = threadIdx.x >> 5, lane = lane_id();
     bool bad = false;
-    if ((int64_t)blockIdx.x * steps_per_stream<true>(a) >= __ldg(a.start[1] + a.N + a.R)) return;       // nothing on this stream
+    if ((int64_t)blockIdx.x * steps_per_stream<true>(a) >= __ldcg(a.start[1] + a.N + a.R)) return;       // nothing on this stream
 
     if (threadIdx.x == 0) {
         sh.failed = 0;
@@ -329,7 +332,7 @@ __device__ __forceinline__ void wide_stream(const AttnArgs &a, const CUtensorMap
                 const int32_t boxes = (min(kWideKeys, p.len - key0) + page - 1) >> a.page_shift;
                 const int stage = pos % kStages;
                 int32_t id = 0;
-                if (lane_box < boxes) id = __ldg(p.pages + (key0 >> a.page_shift) + lane_box);
+                if (lane_box < boxes && HORA_IN((key0 >> a.page_shift) + lane_box, p.prompt ? a.prefix_ld : a.suffix_ld)) id = __ldcg(p.pages + (key0 >> a.page_shift) + lane_box);
                 if (id < 0 || id >= a.n_pages) { bad = true; id = 0; }
                 if (pos >= kStages) ok = bar_wait(bars.empty + 8 * stage, (pos / kStages + 1) & 1, failed);
                 ok = __all_sync(kFull, ok);
@@ -478,7 +481,7 @@ __device__ __forceinline__ void wide_stream(const AttnArgs &a, const CUtensorMap
                         for (int y = 0; y < kLanes; ++y) {
                             const int r = y * kRows + lane / kLanes;
                             const int64_t at_r = __shfl_sync(kFull, from, r);
-                            const uint4 v = at_r >= 0 ? __ldg(reinterpret_cast<const uint4 *>(static_cast<const Q *>(a.q) + at_r) + c) : make_uint4(0, 0, 0, 0);
+                            const uint4 v = at_r >= 0 && HORA_IN(at_r + c * 8 + 7, (int64_t)a.R * a.T * a.q_row_stride) ? __ldcg(reinterpret_cast<const uint4 *>(static_cast<const Q *>(a.q) + at_r) + c) : make_uint4(0, 0, 0, 0);
                             const int qrow = (warp & 3) * kWarp + r;
                             store16(base + Smem::kQ + half * Smem::kQBytes + (c >> 3) * (kWideHalf * 128) + qrow * 128 + (((c & 7) ^ (qrow & 7)) << 4), v);
                         }
@@ -561,7 +564,7 @@ __device__ __forceinline__ void wide_stream(const AttnArgs &a, const CUtensorMap
                 const int64_t rows_all = (int64_t)a.R * a.T * a.Hq;
                 const int64_t place = p.continued ? (int64_t)blockIdx.x * kWideRows + half * kWideHalf + row
                                                   : (int64_t)((p.prompt ? kPromptPart : kOwnPart) + (!p.both && half ? kSecondHalf : 0)) * rows_all + qr.out;
-                if (qr.out >= 0) *reinterpret_cast<float2 *>((p.continued ? a.cont_ml[1] : a.main_ml) + place * 2) = make_float2(m, l);
+                if (qr.out >= 0 && HORA_IN(place, p.continued ? (int64_t)a.n_wide * kWideRows : 4 * rows_all)) *reinterpret_cast<float2 *>((p.continued ? a.cont_ml[1] : a.main_ml) + place * 2) = make_float2(m, l);
                 if (tiles > 0) {
                     // through the warp's rows of the query tile, which nobody reads any more, so that neighbouring lanes store along a row
                     constexpr int kColumns = 32, kLanes = kColumns / 4, kRows = kWarp / kLanes;               // columns at a time
@@ -585,7 +588,7 @@ __device__ __forceinline__ void wide_stream(const AttnArgs &a, const CUtensorMap
                             const int r = v * kRows + lane / kLanes;
                             const int64_t to = __shfl_sync(kFull, from, r);
                             const uint4 got = load16(tile + r * 128 + ((c ^ (r & 7)) << 4));
-                            if (to >= 0) *reinterpret_cast<uint4 *>(po + to + y * kColumns + c * 4) = got;
+                            if (to >= 0 && HORA_IN(to / D, p.continued ? (int64_t)a.n_wide * kWideRows : 4 * rows_all)) *reinterpret_cast<uint4 *>(po + to + y * kColumns + c * 4) = got;
                         }
                     }
                     __syncwarp();

@@ -67,7 +67,7 @@ kv_write_kernel(const In *__restrict__ k, const In *__restrict__ v, const int64_
             head[u] = w.h;
             zero8(raw[u]);
             if (w.t < n_tok) {
-                slot[u] = __ldg(slots + t0 + w.t);
+                slot[u] = __ldcg(slots + t0 + w.t);
                 load8(raw[u], in + (t0 + w.t) * s.row_stride + w.h * D + sub * 8);
             }
             w.next();
@@ -131,13 +131,13 @@ kv_read_kernel(const Cache *__restrict__ k_cache, const Cache *__restrict__ v_ca
             zero8(raw[u]);
             if (w.t < n_tok) {
                 to[u] = (t0 + w.t) * s.row_stride + w.h * D + sub * 8;
-                const int64_t slot = __ldg(slots + t0 + w.t);
+                const int64_t slot = __ldcg(slots + t0 + w.t);
                 if (slot >= s.n_slots) {
                     if (sub == 0) raise_status(status, HORA_ERR_INVALID_VALUE);
                 } else if (slot >= 0) {
                     const int64_t row = pool_row(slot, w.h, s);
                     load8(raw[u], cache + row * D + sub * 8);
-                    if constexpr (sizeof(Cache) == 1) e[u] = __ldg(exps + row);
+                    if constexpr (sizeof(Cache) == 1) e[u] = __ldcg(exps + row);
                 }
             }
             w.next();

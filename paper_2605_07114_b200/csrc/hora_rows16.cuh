@@ -1,4 +1,8 @@
 // Eight consecutive elements of a row in one lane: loads, stores and conversions of the types the decode-step calls take.
+//
+// The kernels of the decode step load through L2 or by ordinary loads, never by __ldg: they start before the kernel in front has
+// finished (programmatic dependent launch), what they read may have been written by it, and a non-coherent load may
+// return a line that the multiprocessor's L1 holds from before.
 #pragma once
 
 #include <cuda_bf16.h>

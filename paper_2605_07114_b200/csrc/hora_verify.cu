@@ -120,20 +120,20 @@ verify_kernel(const VerifyArgs a) {
     bool bad = false;
 
     if (warp == 0) {
-        int32_t len = a.draft_len ? __ldg(a.draft_len + r) : a.K;
+        int32_t len = a.draft_len ? __ldcg(a.draft_len + r) : a.K;
         if (len < 0 || len > a.K) { bad = true; len = len < 0 ? 0 : a.K; }
         int32_t n = len;
         for (int32_t base = 0; base < len; base += kWarp) {
             const int32_t t = base + lane;
             bool refuse = false;
             if (t < len) {
-                const int32_t x = __ldg(a.draft_tokens + r * a.K + t);
+                const int32_t x = __ldcg(a.draft_tokens + r * a.K + t);
                 refuse = x < 0 || x >= a.V;
                 bad |= refuse;
                 if (!refuse) {
                     const double p = as_float(static_cast<const T *>(a.target)[(r * (a.K + 1) + t) * a.target_stride + x]);
                     const double q = a.draft ? as_float(static_cast<const T *>(a.draft)[(r * a.K + t) * a.draft_stride + x]) : 1.f;
-                    refuse = !((double)__ldg(a.u_accept + r * a.K + t) * q < p);      // exact: two 24-bit factors
+                    refuse = !((double)__ldcg(a.u_accept + r * a.K + t) * q < p);      // exact: two 24-bit factors
                 }
             }
             const unsigned ballot = __ballot_sync(kFull, refuse);
@@ -147,7 +147,7 @@ verify_kernel(const VerifyArgs a) {
     rows.V = a.V;
     rows.plus = static_cast<const T *>(a.target) + (r * (a.K + 1) + n) * a.target_stride;
     rows.minus = (n < len && a.draft != nullptr) ? static_cast<const T *>(a.draft) + (r * a.K + n) * a.draft_stride : nullptr;
-    rows.one_hot = (n < len && a.draft == nullptr) ? __ldg(a.draft_tokens + r * a.K + n) : -1;
+    rows.one_hot = (n < len && a.draft == nullptr) ? __ldcg(a.draft_tokens + r * a.K + n) : -1;
 
     // the vocabulary in blocks of 16 bytes as they lie in memory: `lead` elements of the first one are not the row's
     constexpr int kPer16 = 16 / sizeof(T);
@@ -195,7 +195,7 @@ verify_kernel(const VerifyArgs a) {
     if (rank == 0) {
         if (threadIdx.x == 0) a.n_accepted[r] = n;
         for (int32_t t = threadIdx.x; t <= a.K; t += kVfThreads)
-            if (t != n) out[t] = t < n ? __ldg(a.draft_tokens + r * a.K + t) : -1;
+            if (t != n) out[t] = t < n ? __ldcg(a.draft_tokens + r * a.K + t) : -1;
     }
     if (total == 0) {
         if (rank == 0 && threadIdx.x == 0) {
@@ -205,7 +205,7 @@ verify_kernel(const VerifyArgs a) {
         return;
     }
     // floor(U * total) with U = k 2^-24: the product has at most 60 + 24 bits
-    const float u = __ldg(a.u_sample + r);
+    const float u = __ldcg(a.u_sample + r);
     const uint64_t k = (uint64_t)fminf(fmaxf(u * 16777216.f, 0.f), 16777215.f);
     const uint64_t limit = (__umul64hi(total, k) << 40) | ((total * k) >> 24);
     if (limit < first || limit >= first + mine) return;  // uniform over the CTA: another one holds the token
