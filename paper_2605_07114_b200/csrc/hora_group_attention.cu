@@ -121,20 +121,20 @@ struct Parts {
         cont = (uint32_t)(b0 + 1) * step_rows + at;
     }
     __device__ __forceinline__ void init(const AttnArgs &a, const Sequence &q, int64_t start, int64_t per_, int32_t part, uint32_t r, uint32_t t, uint32_t h,
-                                         int64_t row, int64_t rows) {
-        main = part * rows + row;
+                                         uint32_t g0, int64_t row, int64_t rows) {
+        main = part * rows + row + g0;
         count = 0;
         halves = 1;
         wide = q.wide;
         steps = 0;
         if (q.steps == 0 || (int32_t)r < q.first || (int32_t)r >= q.first + q.rollouts) return;
-        const uint32_t x = ((r - q.first) * a.T + t) * a.g, tile = x / (uint32_t)q.tile_rows;
+        const uint32_t x = ((r - q.first) * a.T + t) * a.g + g0, tile = x / (uint32_t)q.tile_rows;
         at = x - tile * q.tile_rows;
         steps = q.steps;
         tile_rows = q.tile_rows;
         left = q.rows - (int32_t)tile * q.tile_rows;
         per = per_;
-        step_rows = q.wide ? kWideRows : kNarrowRows;
+        step_rows = q.wide ? kWideRows : a.narrow_rows;
         u_item = start + ((int64_t)h * q.tiles + tile) * q.steps;
         enter_item();
     }
@@ -154,7 +154,7 @@ struct Parts {
     __device__ __forceinline__ bool where(const AttnArgs &a, int64_t rows, uint32_t x, int32_t D, const float *&ml, const float *&o) const {
         const uint32_t half = x >= count ? 1 : 0, b = x - half * count;
         const int64_t place = b == 0 ? main + (int64_t)half * kSecondHalf * rows : (int64_t)cont + (b - 1) * step_rows + half * kWideHalf;
-        if (!HORA_IN(place, b == 0 ? 4 * rows : wide ? (int64_t)a.n_wide * kWideRows : (int64_t)a.n_narrow * kNarrowRows)) return false;
+        if (!HORA_IN(place, b == 0 ? 4 * rows : wide ? (int64_t)a.n_wide * kWideRows : (int64_t)a.n_narrow * a.narrow_rows)) return false;
         ml = (b == 0 ? a.main_ml : wide ? a.cont_ml[1] : a.cont_ml[0]) + place * 2;
         o = (b == 0 ? a.main_o : wide ? a.cont_o[1] : a.cont_o[0]) + place * D;
         return true;
@@ -163,8 +163,9 @@ struct Parts {
 
 // Joins the partials of the output rows: a warp to a query's heads of one cache head, D / 32 neighbouring elements a lane.  What
 // bounds the kernel is the chain rollout -> group -> sequence -> partial and the arithmetic on places, so both are done
-// once for all these rows; two rows and four partials of each are in flight at a time.
-constexpr int kJoinRows = 2, kJoinAtOnce = 4;
+// once for all these rows (join_rows of them where there are few queries: then more warps at work count for more); two rows and four
+// partials of each are in flight at a time.
+constexpr int kJoinRows = 2, kJoinAtOnce = 4, kJoinWarps = 16;
 
 template <int E>
 struct Row {
@@ -197,9 +198,11 @@ attention_join_kernel(const AttnArgs a) {
     pdl_enter();
     constexpr int E = D / kWarp;
     const int lane = lane_id();
-    const uint32_t n_tasks = (uint32_t)a.R * a.T * a.Hkv, task = blockIdx.x * (blockDim.x / kWarp) + (threadIdx.x >> 5);
+    const uint32_t chunks = (a.g + a.join_rows - 1) / a.join_rows, n_tasks = (uint32_t)a.R * a.T * a.Hkv * chunks;
+    const uint32_t task = blockIdx.x * (blockDim.x / kWarp) + (threadIdx.x >> 5);
     if (task >= n_tasks) return;
-    const uint32_t rt = task / a.Hkv, h = task - rt * a.Hkv, r = rt / a.T, t = rt - r * a.T;
+    const uint32_t rth = task / chunks, g0 = (task - rth * chunks) * a.join_rows, g1 = min((uint32_t)a.g, g0 + a.join_rows);
+    const uint32_t rt = rth / a.Hkv, h = rth - rt * a.Hkv, r = rt / a.T, t = rt - r * a.T;
     const int64_t rows = (int64_t)a.R * a.T * a.Hq, row = (int64_t)rt * a.Hq + h * a.g;
     const int32_t grp = __ldcg(a.group_of + r);
     const bool some = grp >= 0 && (int32_t)t < query_count(a, r);
@@ -208,10 +211,10 @@ attention_join_kernel(const AttnArgs a) {
         bool bad = false;
         const Sequence own = sequence(a, a.N + r, bad), prompt = sequence(a, grp, bad);
         const int64_t per_narrow = steps_per_stream<false>(a), per_wide = steps_per_stream<true>(a);
-        p0.init(a, prompt, __ldcg((prompt.wide ? a.start[1] : a.start[0]) + grp), prompt.wide ? per_wide : per_narrow, kPromptPart, r, t, h, row, rows);
-        p1.init(a, own, __ldcg((own.wide ? a.start[1] : a.start[0]) + a.N + r), own.wide ? per_wide : per_narrow, kOwnPart, r, t, h, row, rows);
+        p0.init(a, prompt, __ldcg((prompt.wide ? a.start[1] : a.start[0]) + grp), prompt.wide ? per_wide : per_narrow, kPromptPart, r, t, h, g0, row, rows);
+        p1.init(a, own, __ldcg((own.wide ? a.start[1] : a.start[0]) + a.N + r), own.wide ? per_wide : per_narrow, kOwnPart, r, t, h, g0, row, rows);
     }
-    for (int32_t j0 = 0; j0 < a.g; j0 += kJoinRows) {
+    for (uint32_t j0 = g0; j0 < g1; j0 += kJoinRows) {
         Row<E> sum[kJoinRows];
         if (some) {
             Parts q0[kJoinRows], q1[kJoinRows];
@@ -220,7 +223,7 @@ attention_join_kernel(const AttnArgs a) {
             for (int j = 0; j < kJoinRows; ++j) {
                 q0[j] = p0;
                 q1[j] = p1;
-                n[j] = j0 + j < a.g ? p0.count * p0.halves + p1.count * p1.halves : 0;
+                n[j] = j0 + j < g1 ? p0.count * p0.halves + p1.count * p1.halves : 0;
                 most = max(most, n[j]);
                 p0.next_row();
                 p1.next_row();
@@ -255,7 +258,7 @@ attention_join_kernel(const AttnArgs a) {
         }
 #pragma unroll
         for (int j = 0; j < kJoinRows; ++j) {
-            if (j0 + j >= a.g) break;
+            if (j0 + j >= g1) break;
             const float inv = sum[j].m == -INFINITY ? 0.f : 1.f / sum[j].l;
             uint32_t w[E / 2];
 #pragma unroll
@@ -275,7 +278,7 @@ static hora_status_t launch_plan(const AttnArgs &a, cudaStream_t stream) {
 }
 
 static hora_status_t launch_join(const AttnArgs &a, int32_t q_dtype, int32_t D, cudaStream_t stream) {
-    const int64_t tasks = (int64_t)a.R * a.T * a.Hkv;
+    const int64_t tasks = (int64_t)a.R * a.T * a.Hkv * ((a.g + a.join_rows - 1) / a.join_rows);
     const int grid = (int)((tasks + 7) / 8);
     cudaError_t e;
     if (q_dtype == HORA_DTYPE_BF16)
@@ -299,9 +302,10 @@ static size_t lay_out(AttnArgs &a, int32_t D, char *base) {
     const size_t rows = (size_t)a.R * a.T * a.Hq;
     a.n_sm = sm_count();
     a.n_narrow = a.n_sm * kNarrowPerSm;
+    a.narrow_rows = 8 * narrow_eights(a.T * a.g, D);
     a.n_wide = a.n_sm;
     for (int w = 0; w < 2; ++w) {
-        const size_t cont = w ? (size_t)a.n_wide * kWideRows : (size_t)a.n_narrow * kNarrowRows;
+        const size_t cont = w ? (size_t)a.n_wide * kWideRows : (size_t)a.n_narrow * a.narrow_rows;
         a.start[w] = reinterpret_cast<int64_t *>(take(((size_t)a.N + a.R + 2) * 8));
         a.cont_o[w] = reinterpret_cast<float *>(take(cont * D * 4));
         a.cont_ml[w] = reinterpret_cast<float *>(take(cont * 2 * 4));
@@ -329,6 +333,7 @@ extern "C" size_t hora_group_attention_workspace_bytes(int64_t N, int64_t R, int
     a.R = (int32_t)R;
     a.T = T;
     a.Hq = Hq;
+    a.g = Hq / Hkv;
     return lay_out(a, D, nullptr);
 }
 
@@ -387,6 +392,8 @@ extern "C" hora_status_t hora_group_attention(const void *q, int32_t q_dtype, in
     if (cache_dtype == HORA_DTYPE_E4M3) a.n_wide = 0;
     a.narrow_keys = narrow_keys(cache_dtype == HORA_DTYPE_E4M3, D);
     a.wide_from = kWideFrom;
+    // all heads of a cache head to a warp where that makes enough warps
+    a.join_rows = R * T * Hkv >= (int64_t)a.n_sm * kJoinWarps ? a.g : kJoinRows;
     hora_status_t rc = launch_plan(a, s);
     if (rc == HORA_OK) rc = launch_attention_main(a, q_dtype, cache_dtype, D, s);
     if (rc == HORA_OK) rc = launch_join(a, q_dtype, D, s);

@@ -19,7 +19,8 @@
 
 namespace hora {
 
-constexpr int kNarrowRows = 16;                          // query rows of a narrow item
+// query rows of a narrow item: as many eights as a rollout's queries of one cache head need, while the registers last
+constexpr int narrow_eights(int rows, int D) { return rows <= 8 ? 1 : rows <= 16 || D == 128 ? 2 : 4; }
 // keys of its steps: 16 where that is 8 KiB, else 32 (twice the independent work between two looks at the maximum)
 constexpr int narrow_keys(bool f8, int D) { return !f8 && D == 128 ? 16 : 32; }
 constexpr int kNarrowPerSm = 12;                         // streams an SM: 168 registers a lane, 16 KiB of keys and values in flight each
@@ -45,7 +46,8 @@ struct AttnArgs {
     int64_t q_row_stride, out_row_stride, n_pages;
     int32_t N, R, T, Hq, Hkv, g, page_shift, prefix_ld, suffix_ld;
     int32_t n_sm, n_narrow, n_wide;                      // CTAs, streams of each line; n_wide 0: every sequence is narrow
-    int32_t narrow_keys;                                 // keys of a narrow step
+    int32_t narrow_keys, narrow_rows;                    // keys of a narrow step, rows of a narrow item
+    int32_t join_rows;                                   // heads that a warp joins
     int32_t wide_from;                                   // rows from which a sequence is wide
     float scale_log2;                                    // sm_scale * log2(e)
     // workspace
@@ -104,8 +106,8 @@ __device__ __forceinline__ Sequence sequence(const AttnArgs &a, int32_t i, bool 
         s.tile_rows = (s.rows + s.tiles - 1) / s.tiles;
         s.steps = (s.len + kWideKeys - 1) / kWideKeys;
     } else {
-        s.tiles = (s.rows + kNarrowRows - 1) / kNarrowRows;
-        s.tile_rows = kNarrowRows;
+        s.tiles = (s.rows + a.narrow_rows - 1) / a.narrow_rows;
+        s.tile_rows = a.narrow_rows;
         s.steps = (s.len + a.narrow_keys - 1) / a.narrow_keys;
     }
     return s;

@@ -15,7 +15,7 @@ constexpr int attention_smem() {
     return F8 || kRings > kWide ? kRings : kWide;
 }
 
-template <typename Q, int D>
+template <typename Q, int D, int NT>
 __global__ void __launch_bounds__(kAttnThreads, 1)
 attention_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     pdl_enter();
@@ -25,16 +25,16 @@ attention_kernel(const AttnArgs a, const __grid_constant__ CUtensorMap k_map, co
     }
     wide_stream<Q, D>(a, k_map, v_map, s_attention);
     const int warp = threadIdx.x >> 5;
-    narrow_stream<Q, false, D>(a, blockIdx.x * kNarrowPerSm + warp, smem_at(s_attention) + warp * Stage<false, D>::kWarpBytes);
+    narrow_stream<Q, false, D, NT>(a, blockIdx.x * kNarrowPerSm + warp, smem_at(s_attention) + warp * Stage<false, D>::kWarpBytes);
 }
 
 // An e4m3 cache: every item is narrow.
-template <typename Q, int D>
+template <typename Q, int D, int NT>
 __global__ void __launch_bounds__(kAttnThreads, 1)
 attention_e4m3_kernel(const AttnArgs a) {
     pdl_enter();
     const int warp = threadIdx.x >> 5;
-    narrow_stream<Q, true, D>(a, blockIdx.x * kNarrowPerSm + warp, smem_at(s_attention) + warp * Stage<true, D>::kWarpBytes);
+    narrow_stream<Q, true, D, NT>(a, blockIdx.x * kNarrowPerSm + warp, smem_at(s_attention) + warp * Stage<true, D>::kWarpBytes);
 }
 
 // One pool as a matrix of [pages * heads * page_size] rows of D elements, fetched 64 elements of one page's rows at a time.
@@ -56,29 +56,35 @@ static bool pool_map(CUtensorMap *map, const void *pool, int32_t dtype, int64_t 
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename Q, int D>
+template <typename Q, int D, int NT>
 static hora_status_t launch(const AttnArgs &a, int32_t q_dtype, bool f8, cudaStream_t stream) {
     cudaError_t e;
     if (f8) {
         constexpr int kSmem = attention_smem<true, D>();
-        e = cudaFuncSetAttribute(attention_e4m3_kernel<Q, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-        if (e == cudaSuccess) e = launch_pdl(attention_e4m3_kernel<Q, D>, a.n_sm, kAttnThreads, kSmem, stream, a);
+        e = cudaFuncSetAttribute(attention_e4m3_kernel<Q, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e == cudaSuccess) e = launch_pdl(attention_e4m3_kernel<Q, D, NT>, a.n_sm, kAttnThreads, kSmem, stream, a);
     } else {
         CUtensorMap k, v;
         const int64_t rows = (a.n_pages * a.Hkv) << a.page_shift;
         if (!pool_map(&k, a.k_cache, q_dtype, rows, D, 1 << a.page_shift) || !pool_map(&v, a.v_cache, q_dtype, rows, D, 1 << a.page_shift)) return HORA_ERR_CUDA;
         constexpr int kSmem = attention_smem<false, D>();
-        e = cudaFuncSetAttribute(attention_kernel<Q, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-        if (e == cudaSuccess) e = launch_pdl(attention_kernel<Q, D>, a.n_sm, kAttnThreads, kSmem, stream, a, k, v);
+        e = cudaFuncSetAttribute(attention_kernel<Q, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        if (e == cudaSuccess) e = launch_pdl(attention_kernel<Q, D, NT>, a.n_sm, kAttnThreads, kSmem, stream, a, k, v);
     }
     count_launches(1);
     return cuda_ok(e);
 }
 
+template <typename Q>
+static hora_status_t launch_for(const AttnArgs &a, int32_t q_dtype, bool f8, int32_t D, cudaStream_t stream) {
+    const int nt = a.narrow_rows / 8;
+    if (D == 128) return nt == 1 ? launch<Q, 128, 1>(a, q_dtype, f8, stream) : launch<Q, 128, 2>(a, q_dtype, f8, stream);
+    return nt == 1 ? launch<Q, 64, 1>(a, q_dtype, f8, stream) : nt == 2 ? launch<Q, 64, 2>(a, q_dtype, f8, stream) : launch<Q, 64, 4>(a, q_dtype, f8, stream);
+}
+
 hora_status_t launch_attention_main(const AttnArgs &a, int32_t q_dtype, int32_t cache_dtype, int32_t D, cudaStream_t stream) {
     const bool f8 = cache_dtype == HORA_DTYPE_E4M3;
-    if (q_dtype == HORA_DTYPE_BF16) return D == 64 ? launch<__nv_bfloat16, 64>(a, q_dtype, f8, stream) : launch<__nv_bfloat16, 128>(a, q_dtype, f8, stream);
-    return D == 64 ? launch<__half, 64>(a, q_dtype, f8, stream) : launch<__half, 128>(a, q_dtype, f8, stream);
+    return q_dtype == HORA_DTYPE_BF16 ? launch_for<__nv_bfloat16>(a, q_dtype, f8, D, stream) : launch_for<__half>(a, q_dtype, f8, D, stream);
 }
 
 }  // namespace hora

@@ -1,4 +1,4 @@
-// hora_group_attention: narrow items, up to 16 query rows: decode of single tokens over long caches.
+// hora_group_attention: narrow items, up to 8, 16 or 32 query rows: decode of single tokens over long caches.
 //
 // The call is bound by the cache's bytes (16 rows or fewer to a key: at most 16 products a byte), so the tensor unit matters only in
 // that it has to be out of the way, and what counts is bytes in flight.  Every warp is a stream of its own, with its own
@@ -6,13 +6,16 @@
 // cp.async (16 KiB of stages a warp, twelve warps an SM: up to 192 KiB in flight, several times what 6.5 TB/s needs at
 // the latency of HBM under load).  No barrier joins the warps, and none waits for another.
 //
-// From the ring the operands go into the registers of mma.m16n8k16 by 16-byte loads, with no transposition:
-//   - scores S = Q K^T sum over the head's dimensions, in any order that Q and K agree on: lane (n, c) = (lane / 4, lane % 4) of
-//     a warp takes 16 neighbouring bytes of a key, and the four lanes of a key neighbouring blocks of 16;
-//   - O += P V sums over keys, two to a register: lane (n, c) loads 16 bytes of the two keys from dimension n * 8 (16 for
-//     one-byte values) on and pairs them up by byte permutations.  Column n of the product is then dimension n * 8 + j of the
-//     head for the j-th register: a lane ends up with runs of neighbouring dimensions, which it stores as they are.
-// The 16-byte chunks of a row lie at places exchanged by the row's number, and column n stands for key key_of(n), such that the eight
+// From the ring the operands go into the registers of mma.m16n8k16 by 16-byte loads, with no transposition.  Keys and values
+// are its left operand (16 keys, or 16 dimensions), queries and weights the right one (8 query rows): a key has few query rows to it,
+// and so none of them is padding up to eight.
+//   - scores S^T = K Q^T sum over the head's dimensions, in any order that Q and K agree on: lane (n, c) = (lane / 4, lane % 4)
+//     takes 16 neighbouring bytes of a key, and the four lanes of a key neighbouring blocks of 16;
+//   - O^T += V^T P^T sums over keys, two to a register: lane (n, c) loads 16 bytes of the two keys from dimension n * 8 (16 for
+//     one-byte values) on and pairs them up by byte permutations.  Row n of the j-th product is then dimension n * 8 + j of the
+//     head: a lane ends up with runs of neighbouring dimensions, which it stores as they are.  The weights come out of the first
+//     product as (key, row) and go into the second as (row, key): one movmatrix for eight keys.
+// The 16-byte chunks of a row lie at places exchanged by the row's number, and index n stands for key key_of(n), such that the eight
 // lanes of each phase of a load hit different banks, for keys and for values.
 //
 // An e4m3 cache is multiplied in fp16, which holds its codes exactly: a row's power-of-two scale is applied to its score, and to
@@ -42,13 +45,22 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-__device__ __forceinline__ float quad_max(float v) {
-    v = fmaxf(v, __shfl_xor_sync(kFull, v, 1));
-    return fmaxf(v, __shfl_xor_sync(kFull, v, 2));
+// over the eight lanes that hold the same two query rows
+__device__ __forceinline__ float rows_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(kFull, v, 4));
+    v = fmaxf(v, __shfl_xor_sync(kFull, v, 8));
+    return fmaxf(v, __shfl_xor_sync(kFull, v, 16));
 }
-__device__ __forceinline__ float quad_sum(float v) {
-    v += __shfl_xor_sync(kFull, v, 1);
-    return v + __shfl_xor_sync(kFull, v, 2);
+__device__ __forceinline__ float rows_sum(float v) {
+    v += __shfl_xor_sync(kFull, v, 4);
+    v += __shfl_xor_sync(kFull, v, 8);
+    return v + __shfl_xor_sync(kFull, v, 16);
+}
+// an 8 x 8 matrix of 16-bit values over the warp, transposed
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {
+    uint32_t t;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(t) : "r"(v));
+    return t;
 }
 
 __device__ __forceinline__ float exponent_byte(uint32_t b) { return __uint_as_float(b ? b << 23 : 0x400000u); }
@@ -104,19 +116,21 @@ struct Stage {
         if constexpr (kRowBytes == 64) return (row >> 1) * 128 + ((((row & 1) * 4 + chunk) ^ (row & 6)) << 4);
         else return row * kRowBytes + ((chunk ^ (row & 7)) << 4);
     }
-    // key that column n (below 8) of a score tile stands for
+    // key that index n (below 8) of a product stands for
     static __device__ __forceinline__ int key_of(int n) { return kRowBytes == 64 ? n : n ^ ((n & 1) << 2); }
 };
 
-// One stream, by one warp, with its ring at `ring` in shared memory.
-template <typename Q, bool F8, int D>
+// One stream, by one warp, with its ring at `ring` in shared memory; items of NT * 8 rows.
+template <typename Q, bool F8, int D, int NT>
 __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream, uint32_t ring) {
     using M = std::conditional_t<F8, __half, Q>;                  // the type of the products
     using St = Stage<F8, D>;
     constexpr int kBlocks = F8 ? D / 64 : D / 32;                 // 16-byte loads of a lane for each key in K
     constexpr int kHalves = F8 ? 1 : D / 64;                      // and for each key in V (one-byte values, D = 64: 8 bytes)
-    constexpr int kOut = D / 8;                                   // column tiles of the output
-    constexpr int kStages = St::kStages, kKeys = St::kKeys, kEights = kKeys / 8, kSixteens = kKeys / 16;
+    constexpr int kSteps = D / 16;                                // products over D for scores, tiles of 16 dimensions of the output
+    constexpr int kRun = F8 ? D / 8 : 8;                          // neighbouring dimensions that a lane holds of the output
+    constexpr int kRows = NT * 8;
+    constexpr int kStages = St::kStages, kKeys = St::kKeys, kSixteens = kKeys / 16;
     const int lane = lane_id();
     const int n = lane >> 2, c = lane & 3;
     const uint32_t exps = ring + kStages * St::kBytes;
@@ -125,7 +139,7 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
     Pieces<false> pieces(a, stream, bad);
     Piece w;
 
-    // where this lane reads: keys key_of(n), key_of(n) + 8 for the scores, and the two keys of columns 2c and 2c + 1 (and
+    // where this lane reads: keys key_of(n), key_of(n) + 8 for the scores, and the two keys of indices 2c and 2c + 1 (and
     // those eight further on) for the product with the weights
     const int key_n = St::key_of(n), key_a = St::key_of(2 * c), key_b = St::key_of(2 * c + 1);
 
@@ -180,63 +194,65 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
         for (int x = 0; x < kStages; ++x) fetch(step0 + x, page[x]);
         Ids page_next = pages_of(step0 + kStages);
 
-        // rows n and n + 8 of the tile are this lane's
-        const QueryRow row0 = query_row(a, s.first, s.rows, s.len, w.prompt, h, w.row0 + n);
-        const QueryRow row1 = query_row(a, s.first, s.rows, s.len, w.prompt, h, w.row0 + n + 8);
-        uint32_t qf[2 * kBlocks * (F8 ? 2 : 1)][4];               // one mma step (16 dimensions) each
-        float q_unit0 = 1.f, q_unit1 = 1.f;                       // what the stored queries have to be multiplied by
-        {
+        // queries: lane (n, c) has row n of each eight, in the dimensions that it takes of the keys
+        uint32_t qf[NT][kSteps][2];
+        float to_log2[NT][2];                                     // of rows 2c and 2c + 1, which are this lane's in the products
+        int32_t limit[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const QueryRow row = query_row(a, s.first, s.rows, s.len, w.prompt, h, w.row0 + t * 8 + n);
             constexpr int kLoads = kBlocks * (F8 ? 2 : 1);
-            uint4 x0[kLoads], x1[kLoads];
+            const bool have = row.out >= 0 && HORA_IN(row.out, rows_all);
+            const Q *from = static_cast<const Q *>(a.q) + (have ? row.out / a.Hq * a.q_row_stride + row.out % a.Hq * D : 0);
+            uint4 x[kLoads];
 #pragma unroll
             for (int b = 0; b < kLoads; ++b) {
                 const int dim = F8 ? (b >> 1) * 64 + c * 16 + (b & 1) * 8 : b * 32 + c * 8;
-                x0[b] = x1[b] = make_uint4(0, 0, 0, 0);
-                const Q *__restrict__ q = static_cast<const Q *>(a.q);
-                if (row0.out >= 0 && HORA_IN(row0.out, rows_all)) x0[b] = __ldcg(reinterpret_cast<const uint4 *>(q + row0.out / a.Hq * a.q_row_stride + row0.out % a.Hq * D + dim));
-                if (row1.out >= 0 && HORA_IN(row1.out, rows_all)) x1[b] = __ldcg(reinterpret_cast<const uint4 *>(q + row1.out / a.Hq * a.q_row_stride + row1.out % a.Hq * D + dim));
+                x[b] = have ? __ldcg(reinterpret_cast<const uint4 *>(from + dim)) : make_uint4(0, 0, 0, 0);
             }
+            float unit = 1.f;                                     // what the stored queries have to be multiplied by
             if constexpr (F8) {
                 // to fp16 with the row's largest value in [64, 128): smaller ones keep 11 bits down to 2^-21 of it
-                float m0 = 0.f, m1 = 0.f, y0[kLoads][8], y1[kLoads][8];
+                float top = 0.f, y[kLoads][8];
 #pragma unroll
                 for (int b = 0; b < kLoads; ++b) {
-                    widen8(Raw8<Q>{x0[b]}, y0[b]);
-                    widen8(Raw8<Q>{x1[b]}, y1[b]);
+                    widen8(Raw8<Q>{x[b]}, y[b]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) { m0 = fmaxf(m0, fabsf(y0[b][e])); m1 = fmaxf(m1, fabsf(y1[b][e])); }
+                    for (int e = 0; e < 8; ++e) top = fmaxf(top, fabsf(y[b][e]));
                 }
-                auto unit = [](float m) {
-                    const int e = (int)(__float_as_uint(m) >> 23) - 127 - 6;
-                    return m > 0.f && e < 120 ? __uint_as_float((uint32_t)(max(e, -120) + 127) << 23) : 1.f;
-                };
-                q_unit0 = unit(quad_max(m0));
-                q_unit1 = unit(quad_max(m1));
-                const float f0 = 1.f / q_unit0, f1 = 1.f / q_unit1;              // powers of two: exact
+                top = fmaxf(top, __shfl_xor_sync(kFull, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(kFull, top, 2));
+                const int e2 = (int)(__float_as_uint(top) >> 23) - 127 - 6;
+                if (top > 0.f && e2 < 120) unit = __uint_as_float((uint32_t)(max(e2, -120) + 127) << 23);
+                const float f = 1.f / unit;                       // powers of two: exact
 #pragma unroll
                 for (int b = 0; b < kLoads; ++b) {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) { y0[b][e] *= f0; y1[b][e] *= f1; }
-                    x0[b] = pack8<__half>(y0[b]);
-                    x1[b] = pack8<__half>(y1[b]);
+                    for (int e = 0; e < 8; ++e) y[b][e] *= f;
+                    x[b] = pack8<__half>(y[b]);
                 }
             }
 #pragma unroll
             for (int b = 0; b < kLoads; ++b) {
-                const uint32_t w0[4] = {x0[b].x, x0[b].y, x0[b].z, x0[b].w}, w1[4] = {x1[b].x, x1[b].y, x1[b].z, x1[b].w};
+                qf[t][2 * b][0] = x[b].x;
+                qf[t][2 * b][1] = x[b].y;
+                qf[t][2 * b + 1][0] = x[b].z;
+                qf[t][2 * b + 1][1] = x[b].w;
+            }
+            // row r's values lie in lanes 4r .. 4r + 3
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    qf[2 * b + j][0] = w0[2 * j];
-                    qf[2 * b + j][1] = w1[2 * j];
-                    qf[2 * b + j][2] = w0[2 * j + 1];
-                    qf[2 * b + j][3] = w1[2 * j + 1];
-                }
+            for (int e = 0; e < 2; ++e) {
+                to_log2[t][e] = a.scale_log2 * __shfl_sync(kFull, unit, (2 * c + e) * 4);
+                limit[t][e] = __shfl_sync(kFull, row.limit, (2 * c + e) * 4);
             }
         }
-        const float to_log2_0 = a.scale_log2 * q_unit0, to_log2_1 = a.scale_log2 * q_unit1;
+        // keys that every query of the piece sees
+        const int32_t open = w.prompt ? s.len : s.len - a.T + 1;
 
-        float o[kOut][4] = {};
-        float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
+        float o[kSteps][NT][4] = {};
+        float m[NT][2], l[NT][2];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) m[t][0] = m[t][1] = -INFINITY, l[t][0] = l[t][1] = 0.f;
         float v_unit = 0.f;                                       // F8: o is in units of this (0: nothing added yet)
         for (int32_t step = step0; step < step1; ++step) {
             const int32_t key = step * kKeys;
@@ -244,89 +260,118 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
             const uint32_t at_k = ring + slot * St::kBytes, at_v = at_k + St::kHalf, at_ke = exps + slot * St::kExpBytes, at_ve = at_ke + kKeys;
             copies_wait<kStages - 1>();
             __syncwarp();
-            float sc[kEights][4] = {};                            // eight keys each
+            float sc[kSixteens][NT][4];                           // keys key_n, key_n + 8 by rows 2c, 2c + 1
 #pragma unroll
-            for (int j = 0; j < kEights; ++j)
+            for (int y = 0; y < kSixteens; ++y) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sc[y][t][e] = 0.f;
 #pragma unroll
                 for (int b = 0; b < kBlocks; ++b) {
-                    const uint4 x = lds16(at_k + St::place(j * 8 + key_n, b * 4 + c));
-                    const uint32_t x4[4] = {x.x, x.y, x.z, x.w};
+                    const uint4 x0 = lds16(at_k + St::place(y * 16 + key_n, b * 4 + c)), x1 = lds16(at_k + St::place(y * 16 + 8 + key_n, b * 4 + c));
+                    const uint32_t k0[4] = {x0.x, x0.y, x0.z, x0.w}, k1[4] = {x1.x, x1.y, x1.z, x1.w};
                     if constexpr (F8) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            mma16816(sc[j], qf[4 * b + e], e4m3x2_to_half2(x4[e] & 0xFFFFu), e4m3x2_to_half2(x4[e] >> 16), M());
+                        for (int e = 0; e < 4; ++e) {
+                            const uint32_t kf[4] = {e4m3x2_to_half2(k0[e] & 0xFFFFu), e4m3x2_to_half2(k1[e] & 0xFFFFu), e4m3x2_to_half2(k0[e] >> 16), e4m3x2_to_half2(k1[e] >> 16)};
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) mma16816(sc[y][t], kf, qf[t][4 * b + e][0], qf[t][4 * b + e][1], M());
+                        }
                     } else {
-                        mma16816(sc[j], qf[2 * b], x4[0], x4[1], M());
-                        mma16816(sc[j], qf[2 * b + 1], x4[2], x4[3], M());
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const uint32_t kf[4] = {k0[2 * e], k1[2 * e], k0[2 * e + 1], k1[2 * e + 1]};
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) mma16816(sc[y][t], kf, qf[t][2 * b + e][0], qf[t][2 * b + e][1], M());
+                        }
                     }
                 }
+            }
             // scores in units of log2, hidden keys at -infinity
-            const bool whole = key + kKeys <= min(row0.limit, row1.limit);
-            float top0 = -INFINITY, top1 = -INFINITY;
+            float ve[kSixteens][2], v_top = v_unit;
 #pragma unroll
-            for (int j = 0; j < kEights; ++j) {
+            for (int y = 0; y < kSixteens; ++y)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
-                    const int k = j * 8 + (x ? key_b : key_a);
+                    const int k = y * 16 + x * 8 + key_n;
                     const float f = F8 ? exponent_byte(lds1(at_ke + k)) : 1.f;
-                    sc[j][x] *= F8 ? to_log2_0 * f : to_log2_0;
-                    sc[j][2 + x] *= F8 ? to_log2_1 * f : to_log2_1;
-                    if (!whole) {
-                        if (key + k >= row0.limit) sc[j][x] = -INFINITY;
-                        if (key + k >= row1.limit) sc[j][2 + x] = -INFINITY;
+                    if constexpr (F8) {
+                        ve[y][x] = key + k < s.len ? exponent_byte(lds1(at_ve + k)) : 0.f;
+                        v_top = fmaxf(v_top, ve[y][x]);
                     }
+#pragma unroll
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) sc[y][t][2 * x + e] *= F8 ? to_log2[t][e] * f : to_log2[t][e];
                 }
-                top0 = fmaxf(top0, fmaxf(sc[j][0], sc[j][1]));
-                top1 = fmaxf(top1, fmaxf(sc[j][2], sc[j][3]));
-            }
-            float e4[kEights][2], v_top = v_unit;
-            if constexpr (F8) {
+            if (key + kKeys > open) {
 #pragma unroll
-                for (int j = 0; j < kEights; ++j)
+                for (int y = 0; y < kSixteens; ++y)
 #pragma unroll
-                    for (int x = 0; x < 2; ++x) {
-                        const int k = j * 8 + (x ? key_b : key_a);
-                        e4[j][x] = key + k < s.len ? exponent_byte(lds1(at_ve + k)) : 0.f;
-                        v_top = fmaxf(v_top, e4[j][x]);
-                    }
+                    for (int t = 0; t < NT; ++t)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            if (key + y * 16 + (e >> 1) * 8 + key_n >= limit[t][e & 1]) sc[y][t][e] = -INFINITY;
             }
             // The reference of a row is raised when a score exceeds it by 2^8: weights up to 256 are as exact as weights up
             // to 1, and the output is hardly ever rescaled.
-            if (__any_sync(kFull, top0 > m0 + 8.f || top1 > m1 + 8.f || (F8 && v_top > v_unit))) {
-                const float up0 = fmaxf(m0, quad_max(top0)), up1 = fmaxf(m1, quad_max(top1));
-                float f0 = up0 == -INFINITY ? 0.f : exp2_fast(m0 - up0), f1 = up1 == -INFINITY ? 0.f : exp2_fast(m1 - up1);
-                m0 = up0;
-                m1 = up1;
-                l0 *= f0;
-                l1 *= f1;
+            bool raise = F8 && v_top > v_unit;
+            float top[NT][2];
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    top[t][e] = fmaxf(sc[0][t][e], sc[0][t][2 + e]);
+#pragma unroll
+                    for (int y = 1; y < kSixteens; ++y) top[t][e] = fmaxf(top[t][e], fmaxf(sc[y][t][e], sc[y][t][2 + e]));
+                    raise |= top[t][e] > m[t][e] + 8.f;
+                }
+            if (__any_sync(kFull, raise)) {
+                float f_v = 1.f;
                 if constexpr (F8) {
-                    v_top = quad_max(v_top);                      // the same in all quads: they hold the same keys
-                    f0 *= v_unit / v_top;                         // powers of two; at least one key is within the length
-                    f1 *= v_unit / v_top;
+                    v_top = rows_max(v_top);                      // over all keys; powers of two, and at least one key is within the length
+                    f_v = v_unit / v_top;
                     v_unit = v_top;
                 }
 #pragma unroll
-                for (int t = 0; t < kOut; ++t) { o[t][0] *= f0; o[t][1] *= f0; o[t][2] *= f1; o[t][3] *= f1; }
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float up = fmaxf(m[t][e], rows_max(top[t][e])), f = up == -INFINITY ? 0.f : exp2_fast(m[t][e] - up);
+                        m[t][e] = up;
+                        l[t][e] *= f;
+#pragma unroll
+                        for (int d = 0; d < kSteps; ++d) {
+                            o[d][t][e] *= f * f_v;
+                            o[d][t][2 + e] *= f * f_v;
+                        }
+                    }
             }
-            // where no key has been seen the reference is -infinity and every weight has to come out as 0
-            const float z0 = m0 == -INFINITY ? 0.f : m0, z1 = m1 == -INFINITY ? 0.f : m1;
             const float v_inv = F8 ? 1.f / v_unit : 1.f;
+            uint32_t p[kSixteens][NT][2];
 #pragma unroll
-            for (int j = 0; j < kEights; ++j) {
+            for (int t = 0; t < NT; ++t) {
+                // where no key has been seen the reference is -infinity and every weight has to come out as 0
+                const float z0 = m[t][0] == -INFINITY ? 0.f : m[t][0], z1 = m[t][1] == -INFINITY ? 0.f : m[t][1];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) sc[j][e] = exp2_fast(sc[j][e] - (e < 2 ? z0 : z1));
-                l0 += sc[j][0] + sc[j][1];
-                l1 += sc[j][2] + sc[j][3];
-                if constexpr (F8) {
+                for (int y = 0; y < kSixteens; ++y)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) sc[j][e] *= e4[j][e & 1] * v_inv;
-                }
+                    for (int x = 0; x < 2; ++x) {
+                        float w0 = exp2_fast(sc[y][t][2 * x] - z0), w1 = exp2_fast(sc[y][t][2 * x + 1] - z1);
+                        l[t][0] += w0;
+                        l[t][1] += w1;
+                        if constexpr (F8) {
+                            const float f = ve[y][x] * v_inv;
+                            w0 *= f;
+                            w1 *= f;
+                        }
+                        p[y][t][x] = transposed(pack2(w0, w1, M()));
+                    }
             }
 #pragma unroll
             for (int y = 0; y < kSixteens; ++y) {
                 if (y > 0 && key + y * 16 >= s.len) break;        // those keys were not fetched
-                const uint32_t p[4] = {pack2(sc[2 * y][0], sc[2 * y][1], M()), pack2(sc[2 * y][2], sc[2 * y][3], M()),
-                                       pack2(sc[2 * y + 1][0], sc[2 * y + 1][1], M()), pack2(sc[2 * y + 1][2], sc[2 * y + 1][3], M())};
 #pragma unroll
                 for (int b = 0; b < kHalves; ++b) {
                     uint32_t v[4][4];
@@ -352,19 +397,24 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
                     }
                     if constexpr (F8) {
 #pragma unroll
-                        for (int q = 0; q < kOut / 4; ++q) {      // four dimensions of a key to a word
+                        for (int q = 0; q < kSteps / 2; ++q) {    // four dimensions of a key to a word
                             const uint32_t lo0 = __byte_perm(v[0][q], v[1][q], 0x5140), hi0 = __byte_perm(v[0][q], v[1][q], 0x7362);
                             const uint32_t lo1 = __byte_perm(v[2][q], v[3][q], 0x5140), hi1 = __byte_perm(v[2][q], v[3][q], 0x7362);
-                            mma16816(o[4 * q], p, e4m3x2_to_half2(lo0 & 0xFFFFu), e4m3x2_to_half2(lo1 & 0xFFFFu), M());
-                            mma16816(o[4 * q + 1], p, e4m3x2_to_half2(lo0 >> 16), e4m3x2_to_half2(lo1 >> 16), M());
-                            mma16816(o[4 * q + 2], p, e4m3x2_to_half2(hi0 & 0xFFFFu), e4m3x2_to_half2(hi1 & 0xFFFFu), M());
-                            mma16816(o[4 * q + 3], p, e4m3x2_to_half2(hi0 >> 16), e4m3x2_to_half2(hi1 >> 16), M());
+                            const uint32_t vf0[4] = {e4m3x2_to_half2(lo0 & 0xFFFFu), e4m3x2_to_half2(lo0 >> 16), e4m3x2_to_half2(lo1 & 0xFFFFu), e4m3x2_to_half2(lo1 >> 16)};
+                            const uint32_t vf1[4] = {e4m3x2_to_half2(hi0 & 0xFFFFu), e4m3x2_to_half2(hi0 >> 16), e4m3x2_to_half2(hi1 & 0xFFFFu), e4m3x2_to_half2(hi1 >> 16)};
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) {
+                                mma16816(o[2 * q][t], vf0, p[y][t][0], p[y][t][1], M());
+                                mma16816(o[2 * q + 1][t], vf1, p[y][t][0], p[y][t][1], M());
+                            }
                         }
                     } else {
 #pragma unroll
                         for (int q = 0; q < 4; ++q) {             // two dimensions of a key to a word
-                            mma16816(o[8 * b + 2 * q], p, __byte_perm(v[0][q], v[1][q], 0x5410), __byte_perm(v[2][q], v[3][q], 0x5410), M());
-                            mma16816(o[8 * b + 2 * q + 1], p, __byte_perm(v[0][q], v[1][q], 0x7632), __byte_perm(v[2][q], v[3][q], 0x7632), M());
+                            const uint32_t vf[4] = {__byte_perm(v[0][q], v[1][q], 0x5410), __byte_perm(v[0][q], v[1][q], 0x7632),
+                                                    __byte_perm(v[2][q], v[3][q], 0x5410), __byte_perm(v[2][q], v[3][q], 0x7632)};
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) mma16816(o[4 * b + q][t], vf, p[y][t][0], p[y][t][1], M());
                         }
                     }
                 }
@@ -373,30 +423,29 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
             fetch(step + kStages, page_next);
             page_next = pages_of(step + kStages + 1);
         }
-        l0 = quad_sum(l0);
-        l1 = quad_sum(l1);
 
-        // o[t] holds columns 2c and 2c + 1 of tile t; column x is dimension x * kRun + t of its part of the head
-        constexpr int kRun = F8 ? D / 8 : 8;
+        // o[d][t] holds rows 2c, 2c + 1 of the t-th eight, each in dimensions n * kRun + 2d and the next one (by parts of 8 * kRun)
+        const float f = F8 ? v_unit : 1.f;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int64_t out = half ? row1.out : row0.out;
-            if (out < 0) continue;
-            const int64_t place = step0 > 0 ? (int64_t)stream * kNarrowRows + n + half * 8 : (w.prompt ? kPromptPart : kOwnPart) * rows_all + out;
-            if (!HORA_IN(place, step0 > 0 ? (int64_t)a.n_narrow * kNarrowRows : 2 * rows_all)) continue;
-            float *__restrict__ po = (step0 > 0 ? a.cont_o[0] : a.main_o) + place * D;
-            const float f = F8 ? v_unit : 1.f;
+        for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int part = 0; part < kOut / kRun; ++part)
+            for (int e = 0; e < 2; ++e) {
+                const float sum = rows_sum(l[t][e]);
+                const int32_t x = t * 8 + 2 * c + e;
+                const int64_t out = query_row(a, s.first, s.rows, s.len, w.prompt, h, w.row0 + x).out;
+                if (out < 0) continue;
+                const int64_t place = step0 > 0 ? (int64_t)stream * kRows + x : (w.prompt ? kPromptPart : kOwnPart) * rows_all + out;
+                if (!HORA_IN(place, step0 > 0 ? (int64_t)a.n_narrow * kRows : 2 * rows_all)) continue;
+                float *po = (step0 > 0 ? a.cont_o[0] : a.main_o) + place * D;
 #pragma unroll
-                for (int x = 0; x < 2; ++x)
+                for (int part = 0; part < D / (8 * kRun); ++part)
 #pragma unroll
-                    for (int t = 0; t < kRun; t += 4)
-                        *reinterpret_cast<float4 *>(po + part * 64 + (2 * c + x) * kRun + t) =
-                            make_float4(o[part * kRun + t][2 * half + x] * f, o[part * kRun + t + 1][2 * half + x] * f,
-                                        o[part * kRun + t + 2][2 * half + x] * f, o[part * kRun + t + 3][2 * half + x] * f);
-            if (c == 0) *reinterpret_cast<float2 *>((step0 > 0 ? a.cont_ml[0] : a.main_ml) + place * 2) = make_float2(half ? m1 : m0, half ? l1 : l0);
-        }
+                    for (int d = 0; d < kRun / 2; d += 2)
+                        *reinterpret_cast<float4 *>(po + part * 8 * kRun + n * kRun + 2 * d) =
+                            make_float4(o[part * (kRun / 2) + d][t][e] * f, o[part * (kRun / 2) + d][t][2 + e] * f, o[part * (kRun / 2) + d + 1][t][e] * f,
+                                        o[part * (kRun / 2) + d + 1][t][2 + e] * f);
+                if (n == 0) *reinterpret_cast<float2 *>((step0 > 0 ? a.cont_ml[0] : a.main_ml) + place * 2) = make_float2(m[t][e], sum);
+            }
     }
     if (bad) raise_status(a.status, HORA_ERR_INVALID_VALUE);
 }
