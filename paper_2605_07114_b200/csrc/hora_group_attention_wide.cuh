@@ -221,16 +221,40 @@ __device__ __forceinline__ void scale_output(uint32_t t_o, float f) {
     }
 }
 
+struct WideShared {
+    uint64_t bars[40];
+    WidePiece piece[kPieceBatch];
+    int32_t pieces, failed;
+    int32_t issued;                                      // copies begun so far
+    uint32_t tmem;
+};
+
+// Waits for the copy into a stage, number `pos` of all.  A warp may come here many stages after the last one that it waited for
+// (the others were the other half's), and a barrier only tells two neighbouring phases apart: the count of the copies begun says that
+// the stage's copy before this one is over.
+template <int STAGES>
+__device__ __forceinline__ bool wait_for_copy(const WideShared &sh, const WideBars &bars, int32_t pos, volatile int32_t *failed) {
+    const volatile int32_t *issued = &sh.issued;
+    for (uint32_t i = 0; *issued <= pos; ++i)
+        if (*failed || i >= kWaitTries * 8) {
+            *failed = 1;
+            (void)HORA_IN(-1, 1);
+            return false;
+        }
+    return bar_wait(bars.full + 8 * (pos % STAGES), (pos / STAGES) & 1, failed);
+}
+
 // Clears the values beyond the last of a tile's `keys` keys, among the sixteen that the product reads last: they may be anything,
 // and 0 * NaN is not 0.  The tile is the last (number `tile` of its step) of the piece, whose last stage, number `last`, holds its
 // values; a half whose tiles end before that has nothing to clear.  All threads of a half; where both halves read the stage
 // both do it, since either may be the first to need it.
 template <int D>
-__device__ __forceinline__ bool clear_values(const WideBars &bars, uint32_t base, volatile int32_t *failed, int32_t keys, int tile, int32_t last, int thread) {
+__device__ __forceinline__ bool clear_values(const WideShared &sh, const WideBars &bars, uint32_t base, volatile int32_t *failed, int32_t keys, int tile, int32_t last,
+                                             int thread) {
     if (keys >= kTileKeys || (keys & 15) == 0) return true;
     using Smem = WideSmem<D>;
     const uint32_t stage = last % Smem::kStages;
-    if (!bar_wait(bars.full + 8 * stage, (last / Smem::kStages) & 1, failed)) return false;
+    if (!wait_for_copy<Smem::kStages>(sh, bars, last, failed)) return false;
     const int32_t clear = ((keys + 15) & ~15) - keys;
     for (int32_t c = thread; c < clear * (D / 8); c += kHalfThreads) {
         const int32_t r = tile * kTileKeys + keys + c / (D / 8), chunk = c % (D / 8);
@@ -239,13 +263,6 @@ __device__ __forceinline__ bool clear_values(const WideBars &bars, uint32_t base
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     return true;
 }
-
-struct WideShared {
-    uint64_t bars[40];
-    WidePiece piece[kPieceBatch];
-    int32_t pieces, failed;
-    uint32_t tmem;
-};
 
 // One stream, by a whole CTA, with its tiles and WideShared at s_tiles.  All threads return together.
 template <typename Q, int D>
@@ -262,6 +279,7 @@ __device__ __forceinline__ void wide_stream(const AttnArgs &a, const CUtensorMap
 
     if (threadIdx.x == 0) {
         sh.failed = 0;
+        sh.issued = 0;
         for (int s = 0; s < kStages; ++s) {
             bar_init(bars.full + 8 * s, 1);
             bar_init(bars.empty + 8 * s, 2);             // both halves' products
@@ -337,7 +355,11 @@ __device__ __forceinline__ void wide_stream(const AttnArgs &a, const CUtensorMap
                 if (pos >= kStages) ok = bar_wait(bars.empty + 8 * stage, (pos / kStages + 1) & 1, failed);
                 ok = __all_sync(kFull, ok);
                 if (!ok) return;
-                if (lane == 0) bar_expect(bars.full + 8 * stage, boxes * page * D * 2);
+                if (lane == 0) {
+                    bar_expect(bars.full + 8 * stage, boxes * page * D * 2);
+                    __threadfence_block();
+                    *const_cast<volatile int32_t *>(&sh.issued) = pos + 1;
+                }
                 __syncwarp();
                 if (lane_box < boxes)
                     tma_box(base + Smem::kRing + stage * Smem::kStageBytes + lane_part * (kWideKeys * 128) + lane_box * page * 128, map, lane_part * 64,
@@ -370,16 +392,15 @@ __device__ __forceinline__ void wide_stream(const AttnArgs &a, const CUtensorMap
             constexpr uint32_t kType = std::is_same<Q, __nv_bfloat16>::value ? 1u : 0u;
             constexpr uint32_t kIdescS = (1u << 4) | (kType << 7) | (kType << 10) | ((kTileKeys / 8) << 17) | ((kWideHalf / 16) << 24);
             constexpr uint32_t kIdescO = (1u << 4) | (kType << 7) | (kType << 10) | (1u << 16) | ((D / 8) << 17) | ((kWideHalf / 16) << 24);
-            // the stages in the order of their first use, as counters that wrap
-            uint32_t stage = 0, round = 0, weights_phase = 0, queries_phase = 0;
+            // the stages in the order of their first use
+            uint32_t weights_phase = 0, queries_phase = 0;
+            int32_t pos = 0;
             const uint32_t k0 = operand(base + Smem::kRing, 16), v0 = operand(base + Smem::kRing, kWideKeys * 128);
             const uint32_t q = operand(base + Smem::kQ + half * Smem::kQBytes, 16), t_s = tmem + half * 128, t_o = tmem + 256 + half * D;
             bool ok = true;
             auto next_stage = [&](bool mine) {           // the next one, once its copy has arrived if it is for this half
-                const uint32_t now = stage;
-                if (mine) ok = ok && bar_wait(bars.full + 8 * now, round, failed);
-                if (++stage == kStages) { stage = 0; round ^= 1; }
-                return now;
+                if (mine) ok = ok && wait_for_copy<kStages>(sh, bars, pos, failed);
+                return (uint32_t)(pos++ % kStages);
             };
             auto release = [&](uint32_t used, bool both) {
                 mma_commit(bars.empty + 8 * used);
@@ -548,7 +569,7 @@ __device__ __forceinline__ void wide_stream(const AttnArgs &a, const CUtensorMap
                             l += sum.x + sum.y;
                             tmem_store_wait();
                         }
-                        if (t == tiles - 1) ok = clear_values<D>(bars, base, failed, p.len - key0, t & 1, pos + 2 * p.n - 1, row) && ok;
+                        if (t == tiles - 1) ok = clear_values<D>(sh, bars, base, failed, p.len - key0, t & 1, pos + 2 * p.n - 1, row) && ok;
                         fence_before();
                         bar_arrive(bars.weights + 16 * half + 8 * (t & 1));
                     }

@@ -158,6 +158,42 @@ def test_ragged_queries_empty_rows_and_strides(dtype, cache, D, Hq, Hkv, T):
     assert (out[3, 2:] == 0).all()
 
 
+@pytest.mark.parametrize("D,dtype", [(64, torch.bfloat16), (128, torch.float16)])
+def test_many_short_items_of_many_rows(D, dtype):
+    """Drafts and many heads to a cache head make each rollout's own keys an item of many rows; hundreds of them, one or a few
+    tiles long, follow each other on every multiprocessor."""
+    rng = np.random.default_rng(D)
+    R = 130
+    suffix = rng.integers(3, 450, R)
+    suffix[::9] = rng.integers(3, 60, len(suffix[::9]))
+    t, h = make([70, 60], [130, 700], suffix, 3, 64, 4, D, dtype, dtype, 16, 21, q_len=rng.integers(1, 4, R))
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, lse = call(t, D ** -0.5, status=status)
+    assert int(status) == 0
+    check(t, h, D ** -0.5, out, lse)
+
+
+def test_steps_follow_each_other_without_waiting():
+    """Lengths, queries and caches change between calls on one stream that nothing waits between; the second of two states
+    shares the first one's workspace."""
+    hora = _hora()
+    a, ha = make([6, 3], [300, 40], [50, 3, 20, 77, 8, 16, 5, 9, 100], 1, 8, 2, 128, torch.bfloat16, torch.bfloat16, 16, 31, garbage=False)
+    b, hb = make([40], [900], [33] * 40, 1, 8, 2, 128, torch.bfloat16, torch.bfloat16, 16, 32, garbage=False)
+    size = max(hora.hora_group_attention_workspace_bytes(x["pl"].shape[0], x["q"].shape[0], 1, 8, 2, 128) for x in (a, b))
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    scale, got = 128 ** -0.5, []
+    for i in range(12):
+        x, h = (a, ha) if i % 2 == 0 else (b, hb)
+        x["sl"].sub_(1).clamp_(min=1)                          # the next call sees one key less of each rollout
+        h["sl"] = np.maximum(h["sl"] - 1, 1)
+        out, lse = torch.empty_like(x["q"]), torch.empty(x["q"].shape[:3], device=DEV)
+        hora.hora_group_attention(x["q"], x["off"], None, scale, x["k"], x["v"], None, None, x["pp"], x["pl"], x["sp"], x["sl"], out, lse, ws)
+        got.append((x, dict(h), out, lse))
+    torch.cuda.synchronize()
+    for x, h, out, lse in got:
+        check(x, h, scale, out, lse)
+
+
 def test_long_lists_are_split_and_joined():
     """Few rows over many keys: every CTA gets a part of an item, so most of the result comes from joining."""
     for cache in (torch.bfloat16, F8):
