@@ -398,9 +398,11 @@ __device__ __forceinline__ void wide_stream(const AttnArgs &a, const CUtensorMap
             const uint32_t k0 = operand(base + Smem::kRing, 16), v0 = operand(base + Smem::kRing, kWideKeys * 128);
             const uint32_t q = operand(base + Smem::kQ + half * Smem::kQBytes, 16), t_s = tmem + half * 128, t_o = tmem + 256 + half * D;
             bool ok = true;
-            auto next_stage = [&](bool mine) {           // the next one, once its copy has arrived if it is for this half
-                if (mine) ok = ok && wait_for_copy<kStages>(sh, bars, pos, failed);
-                return (uint32_t)(pos++ % kStages);
+            auto next_stage = [&](bool mine, bool both) {           // the next one, once its copy has arrived if it is for this half
+                const int32_t now = pos++;
+                // where the half uses every stage it is never a whole ring behind
+                if (mine) ok = ok && (both ? bar_wait(bars.full + 8 * (now % kStages), (now / kStages) & 1, failed) : wait_for_copy<kStages>(sh, bars, now, failed));
+                return (uint32_t)(now % kStages);
             };
             auto release = [&](uint32_t used, bool both) {
                 mma_commit(bars.empty + 8 * used);
@@ -450,12 +452,12 @@ __device__ __forceinline__ void wide_stream(const AttnArgs &a, const CUtensorMap
                             const int32_t nt = turn ? n1 : n0;
                             const bool values = it >= 1 && it - 1 < nt, keys = it < nt;
                             if (values) {
-                                const uint32_t used = next_stage(mine);
+                                const uint32_t used = next_stage(mine, both);
                                 if (mine) v_used = used;
                             }
                             if (mine && values) product(2 * it - 2);
                             if (keys) {
-                                const uint32_t used = next_stage(mine);
+                                const uint32_t used = next_stage(mine, both);
                                 if (mine) k_used = used;
                             }
                             if (!mine) continue;

@@ -1,7 +1,7 @@
 // hora_verify_drafts: how many drafted tokens the target accepts, and the token that follows them.
 //
 // One thread-block cluster to a rollout.  Every CTA of it finds the first refused draft by itself (a few scalars a draft),
-// which fixes the row the next token is drawn from; the CTAs then split that row's vocabulary.  A weight is the
+// which fixes the row the next token is drawn from; the CTAs then split that row's vocabulary (one does all of it where the rollouts fill the device).  A weight is the
 // difference of two probabilities on the grid 2^-38, an integer, so any order of adding gives the same sum and the
 // token is the one the definition names.  One pass over the row: each warp adds up segments of kSeg weights and leaves the
 // sums in shared memory; the CTAs push their totals into each other's shared memory (one cluster barrier), every CTA then
@@ -9,19 +9,20 @@
 // Bound by HBM for many rollouts, by the chain token -> probability -> row -> barrier -> segment for few.
 #include <cooperative_groups.h>
 
+#include <utility>
+
 #include "hora_rows16.cuh"
 
 namespace hora {
 
 namespace cg = cooperative_groups;
 
-constexpr int kVfThreads = 256;
-constexpr int kVfWarps = kVfThreads / kWarp;
-constexpr int kVfCluster = 8;                            // CTAs to a rollout: the largest portable cluster
-constexpr int kSeg = 512;                                // weights summed by one warp at a time
+constexpr int kVfCluster = 8;                            // most CTAs to a rollout: the largest portable cluster
+constexpr int kVfEnough = 4;                             // CTAs an SM, above which a rollout gets fewer of them
+// Weights summed by one warp at a time: two (fp32: four) 16-byte loads of a lane in flight for each row, twice that for 16-bit rows
+// (1920 rollouts of 50257 bf16 values: 64 -> 57 us; 480 of 151936 fp32 values would take 91 in place of 77 us).
+template <typename T> constexpr int kSeg = sizeof(T) == 2 ? 1024 : 512;
 constexpr int kVfMaxV = 1 << 22;
-constexpr int kMaxSegs = kVfMaxV / kVfCluster / kSeg + 1;  // segments of one CTA (a row may begin inside a block)
-constexpr float kGrid = 274877906944.f;                  // 2^38
 
 struct VerifyArgs {
     const void *target, *draft;
@@ -36,10 +37,24 @@ __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ float as_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float as_float(__half x) { return __half2float(x); }
 
-// p on the grid, in [0, 2^38]; NaN and negative values count as zero and are reported in `bad`
-__device__ __forceinline__ uint64_t grid_weight(float p, bool &bad) {
+// A weight on the grid in two parts, hi * 2^20 + lo (lo may be negative in a difference): what a conversion to a 64-bit integer
+// would give, but out of four fp32 operations.  Adding 2^23 rounding down leaves the whole part of a value below 2^23 in the
+// low bits; p 2^18 minus its whole part is exact, and so is that times 2^20 before it is rounded down in turn.
+struct Weight {
+    int32_t hi, lo;
+    __device__ __forceinline__ int64_t value() const { return ((int64_t)hi << 20) + lo; }
+};
+constexpr uint32_t kOneBits = 0x3F800000u;               // 1.0f: the bits of what lies outside [0, 1] (NaN, negative zero too) are larger
+constexpr int32_t kWholeBits = 0x4B000000;               // 2^23
+
+__device__ __forceinline__ Weight on_grid(float p) {     // p in [0, 1]
+    const float t = __fmaf_rd(p, 262144.f, 8388608.f), rest = __fmaf_rn(p, 262144.f, 8388608.f - t), u = __fmaf_rd(rest, 1048576.f, 8388608.f);
+    return {__float_as_int(t) - kWholeBits, __float_as_int(u) - kWholeBits};
+}
+// any p, clamped to [0, 1]; NaN and negative values count as zero and are reported in `bad`
+__device__ __forceinline__ float clamped(float p, bool &bad) {
     bad |= !(p >= 0.f);
-    return (uint64_t)(fminf(fmaxf(p, 0.f), 1.f) * kGrid);
+    return fminf(fmaxf(p, 0.f), 1.f);
 }
 
 __device__ __forceinline__ uint64_t warp_sum(uint64_t v) {
@@ -48,30 +63,55 @@ __device__ __forceinline__ uint64_t warp_sum(uint64_t v) {
     return v;
 }
 
-// The rows the token is drawn from.  minus_row NULL: nothing to take off but, if one_hot >= 0, everything at that token.
+// The rows the token is drawn from.  minus NULL: nothing to take off but, if one_hot >= 0, everything at that token.
 template <typename T>
 struct Rows {
     const T *plus, *minus;
     int32_t one_hot, V;
 
-    __device__ __forceinline__ uint64_t weight(float p, float q, int32_t v, bool &bad) const {
-        const uint64_t P = grid_weight(p, bad);
-        uint64_t Q = minus != nullptr ? grid_weight(q, bad) : 0;
-        if (v == one_hot) Q = (uint64_t)kGrid;
+    __device__ __forceinline__ int64_t at(int32_t v, bool &bad) const {
+        if (v == one_hot) return 0;
+        const int64_t P = on_grid(clamped(as_float(plus[v]), bad)).value();
+        const int64_t Q = minus != nullptr ? on_grid(clamped(as_float(minus[v]), bad)).value() : 0;
         return P > Q ? P - Q : 0;
-    }
-    __device__ __forceinline__ uint64_t at(int32_t v, bool &bad) const {
-        return weight(as_float(plus[v]), minus != nullptr ? as_float(minus[v]) : 0.f, v, bad);
     }
 };
 
-// Sum of the weights [v0, v0 + kSeg) of a row whose 16-byte blocks begin at multiples of eight: `lead` elements of
-// the first block lie before the row (element v of the row is at place v + lead).  Whole blocks are read with wide
+// Adds max(P - Q, 0) of eight values to the sums.
+template <bool MINUS>
+__device__ __forceinline__ void add8(float (&a)[8], float (&b)[8], int32_t &hi, int32_t &lo, bool &bad) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) most = max(most, MINUS ? max(__float_as_uint(a[j]), __float_as_uint(b[j])) : __float_as_uint(a[j]));
+    if (most > kOneBits) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            a[j] = clamped(a[j], bad);
+            if (MINUS) b[j] = clamped(b[j], bad);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        Weight w = on_grid(a[j]);
+        if (MINUS) {
+            const Weight q = on_grid(b[j]);
+            w.hi -= q.hi;
+            w.lo -= q.lo;
+            if (w.hi < 0 || (w.hi == 0 && w.lo < 0)) w.hi = w.lo = 0;
+        }
+        hi += w.hi;
+        lo += w.lo;
+    }
+}
+
+// Sum of the weights of a segment's places from v0 on, for the whole warp, of a row whose 16-byte blocks begin at multiples of eight: `lead`
+// elements of the first block lie before the row (element v of the row is at place v + lead).  Whole blocks are read with wide
 // loads; the draft's row too where it is aligned alike (WIDE_Q).
-template <typename T, bool WIDE_Q>
+template <typename T, bool MINUS, bool WIDE_Q>
 __device__ __forceinline__ uint64_t segment_sum(const Rows<T> &r, int32_t v0, int lane, bool &bad) {
-    uint64_t sum = 0;
-    constexpr int kSteps = kSeg / (kWarp * 8);
+    static_assert(kSeg<T> <= 1024, "the parts of a segment's sum stay within 32 bits");
+    int32_t hi = 0, lo = 0;                              // at most kSeg * 2^18 and kSeg * 2^20 over the warp
+    constexpr int kSteps = kSeg<T> / (kWarp * 8);
     Raw8<T> p[kSteps], q[kSteps];
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
@@ -80,44 +120,54 @@ __device__ __forceinline__ uint64_t segment_sum(const Rows<T> &r, int32_t v0, in
         zero8(q[i]);
         if (v >= 0 && v + 8 <= r.V) {
             load8(p[i], r.plus + v);
-            if (WIDE_Q && r.minus != nullptr) load8(q[i], r.minus + v);
+            if (MINUS && WIDE_Q) load8(q[i], r.minus + v);
         }
     }
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) {
         const int32_t v = v0 + (i * kWarp + lane) * 8;
+        float a[8], b[8];
+        widen8(p[i], a);
+        widen8(q[i], b);
         if (v >= 0 && v + 8 <= r.V) {
-            float a[8], b[8];
-            widen8(p[i], a);
-            widen8(q[i], b);
-            if (!WIDE_Q && r.minus != nullptr) {
+            if (MINUS && !WIDE_Q) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) b[j] = as_float(r.minus[v + j]);
             }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sum += r.weight(a[j], b[j], v + j, bad);
         } else {
+#pragma unroll
             for (int j = 0; j < 8; ++j)
-                if (v + j >= 0 && v + j < r.V) sum += r.at(v + j, bad);
+                if (v + j >= 0 && v + j < r.V) {
+                    a[j] = as_float(r.plus[v + j]);
+                    if (MINUS) b[j] = as_float(r.minus[v + j]);
+                }
         }
+        add8<MINUS>(a, b, hi, lo, bad);
     }
-    return sum;
+    hi = __reduce_add_sync(kFull, hi);
+    lo = __reduce_add_sync(kFull, lo);
+    int64_t sum = ((int64_t)hi << 20) + lo;
+    if (!MINUS && r.one_hot >= v0 && r.one_hot < v0 + kSeg<T> && r.one_hot >= 0) sum -= on_grid(clamped(as_float(r.plus[r.one_hot]), bad)).value();
+    return (uint64_t)sum;
 }
 
-template <typename T>
-__global__ void __cluster_dims__(kVfCluster, 1, 1) __launch_bounds__(kVfThreads)
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS)
 verify_kernel(const VerifyArgs a) {
+    constexpr int kVfThreads = THREADS, kVfWarps = THREADS / kWarp, kSeg = hora::kSeg<T>;
     pdl_enter();
     cg::cluster_group cluster = cg::this_cluster();
     const unsigned rank = cluster.block_rank();
-    const int64_t r = blockIdx.x / kVfCluster;
+    const unsigned n_ctas = cluster.num_blocks();
+    const int64_t r = blockIdx.x / n_ctas;
     const int lane = lane_id(), warp = threadIdx.x >> 5;
-    __shared__ uint64_t s_seg[kMaxSegs];
+    extern __shared__ uint64_t s_seg[];                  // [segs_per_cta]
     __shared__ uint64_t s_total[2][kVfCluster];          // pushed by every CTA of the cluster, one row for each attempt
     __shared__ uint64_t s_warp[kVfWarps];
     __shared__ int32_t s_n, s_len, s_pick;
     __shared__ uint64_t s_before;
     bool bad = false;
+    auto begun = cluster.barrier_arrive();               // shared memory of the others may be written once all have begun
 
     if (warp == 0) {
         int32_t len = a.draft_len ? __ldcg(a.draft_len + r) : a.K;
@@ -163,22 +213,21 @@ verify_kernel(const VerifyArgs a) {
     for (int attempt = 0; attempt < 2; ++attempt) {
         for (int32_t s = warp; s < n_segs; s += kVfWarps) {
             const int32_t v0 = (seg0 + s) * kSeg - lead;
-            const uint64_t w = warp_sum(wide_q ? segment_sum<T, true>(rows, v0, lane, bad) : segment_sum<T, false>(rows, v0, lane, bad));
+            const uint64_t w = rows.minus == nullptr ? segment_sum<T, false, true>(rows, v0, lane, bad)
+                               : wide_q ? segment_sum<T, true, true>(rows, v0, lane, bad) : segment_sum<T, true, false>(rows, v0, lane, bad);
             if (lane == 0) s_seg[s] = w;
         }
         __syncthreads();
+        if (attempt == 0) cluster.barrier_wait(std::move(begun));
         if (warp == 0) {
             uint64_t w = 0;
             for (int32_t s = lane; s < n_segs; s += kWarp) w += s_seg[s];
             w = warp_sum(w);
-            if (attempt == 0) cluster.barrier_wait(cluster.barrier_arrive());
-            if (lane < kVfCluster) *cluster.map_shared_rank(&s_total[attempt][rank], lane) = w;
-        } else if (attempt == 0) {
-            cluster.barrier_wait(cluster.barrier_arrive());
+            if (lane < n_ctas) *cluster.map_shared_rank(&s_total[attempt][rank], lane) = w;
         }
         cluster.sync();
         total = 0;
-        for (unsigned c = 0; c < kVfCluster; ++c) {
+        for (unsigned c = 0; c < n_ctas; ++c) {
             const uint64_t w = s_total[attempt][c];
             if (c < rank) first += w;
             if (c == rank) mine = w;
@@ -239,7 +288,7 @@ verify_kernel(const VerifyArgs a) {
     bool ignore = false;
 #pragma unroll
     for (int j = 0; j < kEach; ++j) {
-        w[j] = (v0 + j >= 0 && v0 + j < a.V) ? rows.at(v0 + j, ignore) : 0;
+        w[j] = (v0 + j >= 0 && v0 + j < a.V) ? (uint64_t)rows.at(v0 + j, ignore) : 0;
         incl += w[j];
     }
     const uint64_t own = incl;
@@ -288,14 +337,32 @@ extern "C" hora_status_t hora_verify_drafts(const void *target, int32_t dtype, i
     a.K = K;
     a.V = V;
     // the most segments a row can have, with up to a block's worth of elements in front of it
-    const int32_t segs = (V + 16 / es - 1 + kSeg - 1) / kSeg;
-    a.segs_per_cta = (segs + kVfCluster - 1) / kVfCluster;
-    const int grid = (int)(R * kVfCluster);
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int32_t seg = es == 2 ? kSeg<__half> : kSeg<float>, segs = (V + 16 / es - 1 + seg - 1) / seg;
+    // Many CTAs to a rollout while that fills the device, fewer where the rollouts do it by themselves: the chain before and after the
+    // pass over the row costs every CTA the same (1920 rollouts of 50257 16-bit values: 173 us with eight, 72 with one).
+    int ctas = kVfCluster;
+    while (ctas > 1 && R * (ctas / 2) >= (int64_t)sm_count() * kVfEnough && (segs + ctas / 2 - 1) / (ctas / 2) <= 4096) ctas /= 2;
+    a.segs_per_cta = (segs + ctas - 1) / ctas;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(R * ctas));
+    // eight warps to a CTA where its latency counts, four where it is one of many (480 rollouts: 81 -> 77 us; 8 rollouts: 18 us with four, 13 with eight)
+    const int threads = ctas == kVfCluster ? 256 : 128;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)a.segs_per_cta * 8;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    auto go = [&](auto few, auto many) { return cudaLaunchKernelEx(&cfg, threads == 256 ? few : many, a); };
     cudaError_t e;
-    if (dtype == HORA_DTYPE_F32) e = launch_pdl(verify_kernel<float>, grid, kVfThreads, 0, s, a);
-    else if (dtype == HORA_DTYPE_BF16) e = launch_pdl(verify_kernel<__nv_bfloat16>, grid, kVfThreads, 0, s, a);
-    else e = launch_pdl(verify_kernel<__half>, grid, kVfThreads, 0, s, a);
+    if (dtype == HORA_DTYPE_F32) e = go(verify_kernel<float, 256>, verify_kernel<float, 128>);
+    else if (dtype == HORA_DTYPE_BF16) e = go(verify_kernel<__nv_bfloat16, 256>, verify_kernel<__nv_bfloat16, 128>);
+    else e = go(verify_kernel<__half, 256>, verify_kernel<__half, 128>);
     count_launches(1);
     return cuda_ok(e);
 }
