@@ -9,41 +9,61 @@ namespace hora {
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanKept = 4;                             // sequences of a thread whose steps it keeps in registers
 constexpr int kPlanOffsets = 4096;                       // group offsets kept in shared memory for the searches
+// Sequences with fewer rows are narrow: a CTA for 128 rows at a time would be mostly idle.
 constexpr int kWideFrom = 33;
+// The wide items' pass costs about 15 us however little there is to do in it: they are taken as narrow ones instead while
+// that makes no more than this many steps a stream (of 8 rows and 16 or 32 keys, about a microsecond each).
+#ifdef HORA_CHECKED
+constexpr int kWideWorth = -1;                           // the checked build takes the wide way wherever it can: small problems check it too
+#else
+constexpr int kWideWorth = 16;
+#endif
 
 // start[line][i] = steps before sequence i on its line, group_of[r].  One CTA: every thread takes a run of sequences.
 __global__ void __launch_bounds__(kPlanThreads)
 attention_plan_kernel(const AttnArgs a) {
     pdl_enter();
-    __shared__ int64_t s_warp[2][kPlanThreads / kWarp];
+    __shared__ int64_t s_warp[3][kPlanThreads / kWarp];
+    static_assert(kPlanThreads / kWarp == kWarp, "a lane to each warp's sums");
     __shared__ int64_t s_off[kPlanOffsets];
     const int64_t n = (int64_t)a.N + a.R;
     const int64_t each = (n + kPlanThreads - 1) / kPlanThreads;
     const int64_t lo = min(n, each * threadIdx.x), hi = min(n, lo + each);
-    bool bad = false;
-    int64_t sum[2] = {0, 0}, run[2], kept[kPlanKept];
-    bool kept_wide[kPlanKept];
+    bool bad = false, ignore = false;
+    // steps of the sequences that are narrow anyhow; of those that can be wide, as wide and as narrow ones
+    enum { kNarrow, kWide, kEither, kSums };
+    int64_t sum[kSums] = {0, 0, 0}, run[kSums], all[kSums];
+    int32_t kept[kPlanKept][2];                          // of this thread's first sequences: steps as wide ones (0: always narrow), as narrow ones
     const bool in_shared = a.N + 1 <= kPlanOffsets;
     if (in_shared)
         for (int32_t i = threadIdx.x; i <= a.N; i += kPlanThreads) s_off[i] = __ldcg(a.group_offsets + i);
+    auto count = [&](int64_t i, int64_t &as_wide, int64_t &as_narrow) {
+        const Sequence n = sequence(a, (int32_t)i, false, bad);
+        as_narrow = total_steps(a, n);
+        as_wide = 0;
+        if (a.n_wide > 0 && n.rows >= a.wide_from) as_wide = total_steps(a, sequence(a, (int32_t)i, true, ignore));
+        sum[as_wide ? kEither : kNarrow] += as_narrow;
+        sum[kWide] += as_wide;
+    };
+    const bool fits = __syncthreads_and(each <= kPlanKept);
 #pragma unroll
     for (int x = 0; x < kPlanKept; ++x) {
-        kept[x] = 0;
-        kept_wide[x] = false;
-        if (lo + x < hi) {
-            const Sequence s = sequence(a, (int32_t)(lo + x), bad);
-            kept[x] = total_steps(a, s);
-            kept_wide[x] = s.wide;
-            sum[s.wide] += kept[x];
+        kept[x][0] = kept[x][1] = 0;
+        if (fits && lo + x < hi) {
+            int64_t w, n;
+            count(lo + x, w, n);
+            kept[x][0] = (int32_t)min(w, (int64_t)INT32_MAX);
+            kept[x][1] = (int32_t)min(n, (int64_t)INT32_MAX);
         }
     }
-    for (int64_t i = lo + kPlanKept; i < hi; ++i) {
-        const Sequence s = sequence(a, (int32_t)i, bad);
-        sum[s.wide] += total_steps(a, s);
-    }
+    if (!fits)
+        for (int64_t i = lo; i < hi; ++i) {
+            int64_t w, n;
+            count(i, w, n);
+        }
     const int lane = lane_id(), warp = threadIdx.x >> 5;
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
+    for (int w = 0; w < kSums; ++w) {
         int64_t incl = sum[w];
 #pragma unroll
         for (int d = 1; d < kWarp; d <<= 1) {
@@ -54,33 +74,42 @@ attention_plan_kernel(const AttnArgs a) {
         run[w] = incl - sum[w];
     }
     __syncthreads();
-    // this warp's sums before it: lane x has warp x's
+    // sums of the warps before this one, and of all: lane x has warp x's
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        int64_t before = lane < warp ? s_warp[w][lane] : 0;
+    for (int w = 0; w < kSums; ++w) {
+        all[w] = s_warp[w][lane];
+        int64_t before = lane < warp ? all[w] : 0;
 #pragma unroll
-        for (int d = kWarp / 2; d > 0; d >>= 1) before += __shfl_xor_sync(kFull, before, d);
+        for (int d = kWarp / 2; d > 0; d >>= 1) {
+            before += __shfl_xor_sync(kFull, before, d);
+            all[w] += __shfl_xor_sync(kFull, all[w], d);
+        }
         run[w] += before;
     }
+    const bool wide = a.n_wide > 0 && all[kEither] > (int64_t)kWideWorth * a.n_narrow;
+    int64_t at_narrow = run[kNarrow] + (wide ? 0 : run[kEither]), at_wide = wide ? run[kWide] : 0;
+    auto place = [&](int64_t i, int64_t as_wide, int64_t as_narrow) {
+        a.start[0][i] = at_narrow;
+        a.start[1][i] = at_wide;
+        if (wide && as_wide) at_wide += as_wide;
+        else at_narrow += as_narrow;
+    };
 #pragma unroll
     for (int x = 0; x < kPlanKept; ++x)
-        if (lo + x < hi) {
-            a.start[0][lo + x] = run[0];
-            a.start[1][lo + x] = run[1];
-            run[kept_wide[x]] += kept[x];
+        if (fits && lo + x < hi) place(lo + x, kept[x][0], kept[x][1]);
+    if (!fits)
+        for (int64_t i = lo; i < hi; ++i) {
+            const Sequence n = sequence(a, (int32_t)i, false, ignore);
+            const bool can = a.n_wide > 0 && n.rows >= a.wide_from;
+            place(i, can ? total_steps(a, sequence(a, (int32_t)i, true, ignore)) : 0, total_steps(a, n));
         }
-    for (int64_t i = lo + kPlanKept; i < hi; ++i) {
-        a.start[0][i] = run[0];
-        a.start[1][i] = run[1];
-        bool again = false;
-        const Sequence s = sequence(a, (int32_t)i, again);
-        run[s.wide] += total_steps(a, s);
-    }
-    if (threadIdx.x == kPlanThreads - 1) {
-        a.start[0][n] = run[0];
-        a.start[1][n] = run[1];
-        a.start[0][n + 1] = max((int64_t)kNarrowMinSteps, (run[0] + a.n_narrow - 1) / a.n_narrow);
-        a.start[1][n + 1] = a.n_wide > 0 ? max((int64_t)1, (run[1] + a.n_wide - 1) / a.n_wide) : 1;
+    if (threadIdx.x == 0) {
+        const int64_t narrow = all[kNarrow] + (wide ? 0 : all[kEither]), wides = wide ? all[kWide] : 0;
+        a.start[0][n] = narrow;
+        a.start[1][n] = wides;
+        a.start[0][n + 1] = max((int64_t)kNarrowMinSteps, (narrow + a.n_narrow - 1) / a.n_narrow);
+        a.start[1][n + 1] = wide ? max((int64_t)1, (wides + a.n_wide - 1) / a.n_wide) : 1;
+        a.start[1][n + 2] = wide ? 1 : 0;
     }
     const int64_t covered = __ldcg(a.group_offsets + a.N);
     for (int32_t r = threadIdx.x; r < a.R; r += kPlanThreads) {
@@ -165,7 +194,7 @@ struct Parts {
 // bounds the kernel is the chain rollout -> group -> sequence -> partial and the arithmetic on places, so both are done
 // once for all these rows (join_rows of them where there are few queries: then more warps at work count for more); two rows and four
 // partials of each are in flight at a time.
-constexpr int kJoinRows = 2, kJoinAtOnce = 4, kJoinWarps = 16;
+constexpr int kJoinRows = 2, kJoinAtOnce = 4, kJoinWarps = 8;
 
 template <int E>
 struct Row {
@@ -209,7 +238,8 @@ attention_join_kernel(const AttnArgs a) {
     Parts p0, p1;
     if (some) {
         bool bad = false;
-        const Sequence own = sequence(a, a.N + r, bad), prompt = sequence(a, grp, bad);
+        const bool wide = has_wide(a);
+        const Sequence own = sequence(a, a.N + r, wide, bad), prompt = sequence(a, grp, wide, bad);
         const int64_t per_narrow = steps_per_stream<false>(a), per_wide = steps_per_stream<true>(a);
         p0.init(a, prompt, __ldcg((prompt.wide ? a.start[1] : a.start[0]) + grp), prompt.wide ? per_wide : per_narrow, kPromptPart, r, t, h, g0, row, rows);
         p1.init(a, own, __ldcg((own.wide ? a.start[1] : a.start[0]) + a.N + r), own.wide ? per_wide : per_narrow, kOwnPart, r, t, h, g0, row, rows);
@@ -306,7 +336,7 @@ static size_t lay_out(AttnArgs &a, int32_t D, char *base) {
     a.n_wide = a.n_sm;
     for (int w = 0; w < 2; ++w) {
         const size_t cont = w ? (size_t)a.n_wide * kWideRows : (size_t)a.n_narrow * a.narrow_rows;
-        a.start[w] = reinterpret_cast<int64_t *>(take(((size_t)a.N + a.R + 2) * 8));
+        a.start[w] = reinterpret_cast<int64_t *>(take(((size_t)a.N + a.R + 3) * 8));
         a.cont_o[w] = reinterpret_cast<float *>(take(cont * D * 4));
         a.cont_ml[w] = reinterpret_cast<float *>(take(cont * 2 * 4));
     }

@@ -20,7 +20,7 @@
 namespace hora {
 
 // query rows of a narrow item: as many eights as a rollout's queries of one cache head need, while the registers last
-constexpr int narrow_eights(int rows, int D) { return rows <= 8 ? 1 : rows <= 16 || D == 128 ? 2 : 4; }
+constexpr int narrow_eights(int rows, int D) { return rows <= 8 ? 1 : rows <= 16 || D == 128 ? 2 : 3; }
 // keys of its steps: 16 where that is 8 KiB, else 32 (twice the independent work between two looks at the maximum)
 constexpr int narrow_keys(bool f8, int D) { return !f8 && D == 128 ? 16 : 32; }
 constexpr int kNarrowPerSm = 12;                         // streams an SM: 168 registers a lane, 16 KiB of keys and values in flight each
@@ -51,7 +51,7 @@ struct AttnArgs {
     int32_t wide_from;                                   // rows from which a sequence is wide
     float scale_log2;                                    // sm_scale * log2(e)
     // workspace
-    int64_t *start[2];                                   // [N + R + 2] first step of each sequence on the narrow, the wide line; all; a stream's
+    int64_t *start[2];                                   // [N + R + 3] first step of each sequence on the narrow, the wide line; all; a stream's; [1]: has_wide
     int32_t *group_of;                                   // [R] group of each rollout, -1: none
     float *main_o, *main_ml;                             // [2 or 4][R * T * Hq][D], [..][2], by part
     float *cont_o[2], *cont_ml[2];                       // [streams][rows of an item][D], [..][2]
@@ -83,7 +83,8 @@ __device__ __forceinline__ int32_t query_count(const AttnArgs &a, int32_t r) {
     return n < 0 ? 0 : (n > a.T ? a.T : n);
 }
 
-__device__ __forceinline__ Sequence sequence(const AttnArgs &a, int32_t i, bool &bad) {
+// `wide`: whether sequences with enough rows for it are wide in this call.
+__device__ __forceinline__ Sequence sequence(const AttnArgs &a, int32_t i, bool wide, bool &bad) {
     Sequence s = {};
     if (!HORA_IN(i, a.N + a.R)) return s;
     if (i < a.N) {
@@ -100,7 +101,7 @@ __device__ __forceinline__ Sequence sequence(const AttnArgs &a, int32_t i, bool 
         s.len = checked_len(__ldcg(a.suffix_len + s.first), a.suffix_ld, a.page_shift, bad);
     }
     s.rows = s.rollouts * a.T * a.g;
-    s.wide = a.n_wide > 0 && s.rows >= a.wide_from;
+    s.wide = wide && s.rows >= a.wide_from;
     if (s.wide) {                                        // blocks of about the same size, so that their steps take the same time
         s.tiles = (s.rows + kWideRows - 1) / kWideRows;
         s.tile_rows = (s.rows + s.tiles - 1) / s.tiles;
@@ -118,6 +119,8 @@ __device__ __forceinline__ int64_t total_steps(const AttnArgs &a, const Sequence
 // Steps of a line that go to one stream; the plan leaves it behind the line's starts.
 template <bool WIDE>
 __device__ __forceinline__ int64_t steps_per_stream(const AttnArgs &a) { return __ldcg(a.start[WIDE] + a.N + a.R + 1); }
+// Whether the call has wide items: the plan leaves that there too.
+__device__ __forceinline__ bool has_wide(const AttnArgs &a) { return __ldcg(a.start[1] + a.N + a.R + 2) != 0; }
 
 // A stream's part of one item.
 struct Piece {
@@ -131,6 +134,7 @@ template <bool WIDE>
 struct Pieces {
     int64_t u, u_end, s_start;
     int32_t i;
+    bool wide;
     Sequence s;
 
     __device__ __forceinline__ Pieces(const AttnArgs &a, int32_t stream, bool &bad) {
@@ -149,7 +153,8 @@ struct Pieces {
             hi = min(hi, i + (top + 1) * gap);
             i += top * gap;
         }
-        s = sequence(a, i, bad);
+        wide = has_wide(a);
+        s = sequence(a, i, wide, bad);
         s_start = __ldcg(start + i);
     }
 
@@ -158,7 +163,7 @@ struct Pieces {
         while (s.wide != WIDE || u >= s_start + total_steps(a, s)) {        // on to the next sequence with steps on this line
             if (!HORA_IN(i + 1, a.N + a.R)) return false;
             if (s.wide == WIDE) s_start += total_steps(a, s);
-            s = sequence(a, ++i, bad);
+            s = sequence(a, ++i, wide, bad);
         }
         const int64_t item = (u - s_start) / s.steps;
         p.step0 = (int32_t)((u - s_start) - item * s.steps);

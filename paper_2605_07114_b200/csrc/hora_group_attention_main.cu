@@ -79,7 +79,7 @@ template <typename Q>
 static hora_status_t launch_for(const AttnArgs &a, int32_t q_dtype, bool f8, int32_t D, cudaStream_t stream) {
     const int nt = a.narrow_rows / 8;
     if (D == 128) return nt == 1 ? launch<Q, 128, 1>(a, q_dtype, f8, stream) : launch<Q, 128, 2>(a, q_dtype, f8, stream);
-    return nt == 1 ? launch<Q, 64, 1>(a, q_dtype, f8, stream) : nt == 2 ? launch<Q, 64, 2>(a, q_dtype, f8, stream) : launch<Q, 64, 4>(a, q_dtype, f8, stream);
+    return nt == 1 ? launch<Q, 64, 1>(a, q_dtype, f8, stream) : nt == 2 ? launch<Q, 64, 2>(a, q_dtype, f8, stream) : launch<Q, 64, 3>(a, q_dtype, f8, stream);
 }
 
 hora_status_t launch_attention_main(const AttnArgs &a, int32_t q_dtype, int32_t cache_dtype, int32_t D, cudaStream_t stream) {

@@ -1,4 +1,4 @@
-// hora_group_attention: narrow items, up to 8, 16 or 32 query rows: decode of single tokens over long caches.
+// hora_group_attention: narrow items, up to 8, 16 or 24 query rows: decode of single tokens over long caches.
 //
 // The call is bound by the cache's bytes (16 rows or fewer to a key: at most 16 products a byte), so the tensor unit matters only in
 // that it has to be out of the way, and what counts is bytes in flight.  Every warp is a stream of its own, with its own

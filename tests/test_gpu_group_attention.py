@@ -27,6 +27,21 @@ def _hora():
     return hora
 
 
+@pytest.fixture(params=["normal", "checked"])
+def build(request):
+    """The tests run through the normal build and through the checked one, whose index checks have to stay silent and which
+    gives every item with enough rows to the wide kernel (the normal build leaves problems as small as these to the narrow one)."""
+    from paper_2605_07114_b200 import build as b
+    hora = _hora()
+    if request.param == "checked":
+        hora.use_library(b.build(checked=True))
+        assert hora.hora_checked_violation() == 0
+    yield request.param
+    left = hora.hora_checked_violation() if request.param == "checked" else 0
+    hora.use_library(None)
+    assert left == 0, f"index check failed: file {left >> 20}, line {left & 0xFFFFF}"
+
+
 def make(sizes, prefix, suffix, T, Hq, Hkv, D, dtype, cache, page, seed, q_len=None, extra_rollouts=0, stride_extra=0, garbage=True, q_scale=2.0):
     """Everything a call takes, on the device, and the same on the host in 64 bits.  Unused slots hold NaN."""
     rng = np.random.default_rng(seed)
@@ -130,7 +145,7 @@ CASES = [
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("dtype,cache", [(torch.bfloat16, torch.bfloat16), (torch.float16, torch.float16), (torch.bfloat16, F8), (torch.float16, F8)])
 @pytest.mark.parametrize("case", range(len(CASES)))
-def test_attention_over_shared_and_own_keys(case, dtype, cache, D):
+def test_attention_over_shared_and_own_keys(build, case, dtype, cache, D):
     sizes, prefix, suffix, T, Hq, Hkv, page = CASES[case]
     t, h = make(sizes, prefix, suffix, T, Hq, Hkv, D, dtype, cache, page, 100 * case + D)
     status = torch.zeros(1, dtype=torch.int32, device=DEV)
@@ -140,7 +155,7 @@ def test_attention_over_shared_and_own_keys(case, dtype, cache, D):
 
 
 @pytest.mark.parametrize("dtype,cache,D,Hq,Hkv,T", [(torch.bfloat16, torch.bfloat16, 128, 8, 2, 4), (torch.float16, F8, 64, 6, 1, 7), (torch.bfloat16, torch.bfloat16, 64, 32, 1, 5)])
-def test_ragged_queries_empty_rows_and_strides(dtype, cache, D, Hq, Hkv, T):
+def test_ragged_queries_empty_rows_and_strides(build, dtype, cache, D, Hq, Hkv, T):
     """Fewer queries than slots, none at all, more queries than own tokens (their first see no own token), rollouts beyond the
     last group, no prompt, rows cut out of wider ones on both sides."""
     sizes = [3, 2, 4]
@@ -159,7 +174,7 @@ def test_ragged_queries_empty_rows_and_strides(dtype, cache, D, Hq, Hkv, T):
 
 
 @pytest.mark.parametrize("D,dtype", [(64, torch.bfloat16), (128, torch.float16)])
-def test_many_short_items_of_many_rows(D, dtype):
+def test_many_short_items_of_many_rows(build, D, dtype):
     """Drafts and many heads to a cache head make each rollout's own keys an item of many rows; hundreds of them, one or a few
     tiles long, follow each other on every multiprocessor."""
     rng = np.random.default_rng(D)
@@ -173,7 +188,7 @@ def test_many_short_items_of_many_rows(D, dtype):
     check(t, h, D ** -0.5, out, lse)
 
 
-def test_steps_follow_each_other_without_waiting():
+def test_steps_follow_each_other_without_waiting(build):
     """Lengths, queries and caches change between calls on one stream that nothing waits between; the second of two states
     shares the first one's workspace."""
     hora = _hora()
@@ -194,7 +209,43 @@ def test_steps_follow_each_other_without_waiting():
         check(x, h, scale, out, lse)
 
 
-def test_long_lists_are_split_and_joined():
+@pytest.mark.parametrize("D,Hq,Hkv,T,dtype,cache,page", [(128, 32, 4, 2, torch.bfloat16, torch.bfloat16, 64), (64, 16, 2, 3, torch.float16, torch.float16, 16),
+                                                           (128, 40, 8, 1, torch.float16, torch.float16, 128), (128, 16, 2, 2, torch.bfloat16, F8, 32)])
+def test_large_groups_over_long_prompts(D, Hq, Hkv, T, dtype, cache, page):
+    """Sizes at which the normal build takes the wide kernel, against plain 64-bit arithmetic on the device."""
+    rng = np.random.default_rng(5)
+    sizes = [90, 33, 1, 150]
+    R = sum(sizes)
+    plen = [2600, 1023, 640, 1409]
+    t, h = make(sizes, plen, rng.integers(T, 90, R), T, Hq, Hkv, D, dtype, cache, page, 51)
+    scale = D ** -0.5
+    out, lse = call(t, scale)
+    u_out = UNIT[dtype]
+    u_w = 2.0 ** -11 if cache == F8 else u_out
+    k, v, q = (torch.from_numpy(h[x]).to(DEV) for x in ("k", "v", "q"))
+    for i in range(len(sizes)):
+        for r in range(int(h["off"][i]), int(h["off"][i + 1])):
+            def rows(pool, pages, n):
+                return pool[torch.from_numpy(pages[:-(-n // page)].astype(np.int64)).to(DEV)].transpose(1, 2).reshape(-1, Hkv, D)[:n].transpose(0, 1)
+            n = int(h["sl"][r])
+            kk = torch.cat([rows(k, h["pp"][i], plen[i]), rows(k, h["sp"][r], n)], 1)
+            vv = torch.cat([rows(v, h["pp"][i], plen[i]), rows(v, h["sp"][r], n)], 1)
+            qq = q[r].reshape(T, Hkv, Hq // Hkv, D).transpose(0, 1).reshape(Hkv, -1, D)              # [Hkv, T * g, D]
+            z = scale * (qq @ kk.transpose(1, 2))
+            seen = plen[i] + n - T + 1 + torch.arange(T, device=DEV)
+            hidden = torch.arange(kk.shape[1], device=DEV) >= seen[:, None]
+            z = z.reshape(Hkv, T, Hq // Hkv, -1).masked_fill(hidden[None, :, None, :], -math.inf).reshape(Hkv, T * (Hq // Hkv), -1)
+            e = torch.logsumexp(z, -1, keepdim=True)
+            w = torch.exp(z - e)
+            back = lambda x: x.reshape(Hkv, T, Hq // Hkv, -1).transpose(0, 1).reshape(T, Hq, -1)  # noqa: E731
+            want, bound, ds = back(w @ vv), back(w @ vv.abs()), D * 2.0 ** -23 * scale * (qq.abs() @ kk.abs().transpose(1, 2)).amax()
+            small = 0.0 if u_w == 2.0 ** -8 else 2.0 ** -25 * kk.shape[1] * vv.abs().amax()
+            tol = bound * (u_w + 2 * ds + 2.0 ** -18) + u_out * want.abs() + small * (1 + u_out) + 2.0 ** -24
+            assert ((out[r].double() - want).abs() <= tol).all(), (i, r)
+            assert ((lse[r].double() - back(e)[..., 0]).abs() <= ds + 2.0 ** -18 * (1 + back(e)[..., 0].abs())).all(), (i, r)
+
+
+def test_long_lists_are_split_and_joined(build):
     """Few rows over many keys: every CTA gets a part of an item, so most of the result comes from joining."""
     for cache in (torch.bfloat16, F8):
         t, h = make([2], [5003], [2100, 1], 1, 4, 1, 128, torch.bfloat16, cache, 128, 11)
@@ -202,7 +253,7 @@ def test_long_lists_are_split_and_joined():
         check(t, h, 128 ** -0.5, out, lse)
 
 
-def test_scores_of_all_magnitudes():
+def test_scores_of_all_magnitudes(build):
     """Very peaked and very flat attention, and scores that grow and fall along the keys."""
     for q_scale in (1e-3, 30.0):
         t, h = make([3], [200], [100, 3, 50], 1, 8, 2, 128, torch.bfloat16, torch.bfloat16, 16, 12, q_scale=q_scale)
@@ -210,7 +261,7 @@ def test_scores_of_all_magnitudes():
         check(t, h, 128 ** -0.5, out, lse)
 
 
-def test_twice_the_same_bits_and_workspace_contents_do_not_matter():
+def test_twice_the_same_bits_and_workspace_contents_do_not_matter(build):
     t, _ = make([9, 30], [700, 65], [40] * 39, 2, 16, 4, 128, torch.bfloat16, torch.bfloat16, 32, 13)
     a, la = call(t, 0.09)
     b, lb = call(t, 0.09)
@@ -230,7 +281,7 @@ def test_on_another_stream_and_through_the_object():
     check(t, h, 64 ** -0.5, out, lse)
 
 
-def test_values_that_are_out_of_range_are_reported_and_stay_in_bounds():
+def test_values_that_are_out_of_range_are_reported_and_stay_in_bounds(build):
     """Lengths, counts, page numbers and offsets that cannot be: reported, clamped; the other rollouts' results stand."""
     hora = _hora()
     for what in ("page", "length", "negative", "offsets", "q_len"):
