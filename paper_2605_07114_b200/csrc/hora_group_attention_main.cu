@@ -1,6 +1,8 @@
 // hora_group_attention: the kernel.  One CTA of twelve warps to an SM: together they are a stream of the wide line (products on
 // tcgen05), then each of them is a stream of the narrow line.  One launch for both, so that no SM waits for the slowest
 // of the others in between.
+#include <atomic>
+
 #define HORA_FILE_ID 6
 #include "hora_group_attention_narrow.cuh"
 #include "hora_group_attention_wide.cuh"
@@ -56,19 +58,33 @@ static bool pool_map(CUtensorMap *map, const void *pool, int32_t dtype, int64_t 
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// Shared memory beyond the default has to be asked for once per kernel and device.
+static cudaError_t allow_shared(const void *kernel, int bytes, std::atomic<uint64_t> &devices) {
+    int dev = -1;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = dev >= 0 && dev < 64 ? 1ull << dev : 0;
+    if (devices.load(std::memory_order_acquire) & bit) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) devices.fetch_or(bit, std::memory_order_release);
+    return e;
+}
+
 template <typename Q, int D, int NT>
 static hora_status_t launch(const AttnArgs &a, int32_t q_dtype, bool f8, cudaStream_t stream) {
     cudaError_t e;
     if (f8) {
         constexpr int kSmem = attention_smem<true, D>();
-        e = cudaFuncSetAttribute(attention_e4m3_kernel<Q, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        static std::atomic<uint64_t> devices{0};
+        e = allow_shared(reinterpret_cast<const void *>(attention_e4m3_kernel<Q, D, NT>), kSmem, devices);
         if (e == cudaSuccess) e = launch_pdl(attention_e4m3_kernel<Q, D, NT>, a.n_sm, kAttnThreads, kSmem, stream, a);
     } else {
         CUtensorMap k, v;
         const int64_t rows = (a.n_pages * a.Hkv) << a.page_shift;
         if (!pool_map(&k, a.k_cache, q_dtype, rows, D, 1 << a.page_shift) || !pool_map(&v, a.v_cache, q_dtype, rows, D, 1 << a.page_shift)) return HORA_ERR_CUDA;
         constexpr int kSmem = attention_smem<false, D>();
-        e = cudaFuncSetAttribute(attention_kernel<Q, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+        static std::atomic<uint64_t> devices{0};
+        e = allow_shared(reinterpret_cast<const void *>(attention_kernel<Q, D, NT>), kSmem, devices);
         if (e == cudaSuccess) e = launch_pdl(attention_kernel<Q, D, NT>, a.n_sm, kAttnThreads, kSmem, stream, a, k, v);
     }
     count_launches(1);

@@ -401,42 +401,49 @@ def _dtype_code(t: torch.Tensor, name: str) -> int:
     return code
 
 
-def _kv_rows(k: torch.Tensor, v: torch.Tensor, n: int, H: int, D: int):
+def _kv_rows(k: torch.Tensor, v: torch.Tensor, n: int, H: int, D: int) -> int:
+    ks = k.stride()
+    if k.dtype == v.dtype and k.shape == v.shape == (n, H, D) and ks == v.stride() and ks[1:] == (D, 1) and k.is_cuda and v.is_cuda:
+        return ks[0]                                               # the usual case, in few steps
     if k.dtype != v.dtype or k.shape[0] != n or v.shape[0] != n:
         raise ValueError("k and v must have one type and one row for each slot")
     stride = _row_stride(k, 1, (H, D), "k")
-    other = _row_stride(v, 1, (H, D), "v")
-    if n > 1 and stride != other:
+    if n > 1 and stride != _row_stride(v, 1, (H, D), "v"):
         raise ValueError("k and v must have the same row stride")
     return stride
 
 
+def _pools(k_cache, v_cache, k_exp, v_exp):
+    """The cache's part of the arguments: pointers, type, shape."""
+    n_pages, H, page, D = k_cache.shape
+    ne, dtype = n_pages * H * page, k_cache.dtype
+    return (_at(k_cache, dtype, "k_cache"), _at(v_cache, dtype, "v_cache", ne * D), _at(k_exp, torch.uint8, "k_exp", ne),
+            _at(v_exp, torch.uint8, "v_exp", ne), _dtype_code(k_cache, "k_cache"), n_pages, page)
+
+
+def _kv_write(pools, H, D, k, v, slots, status_dev):
+    n = slots.shape[0]
+    kp, vp, ke, ve, code, n_pages, page = pools
+    rc = load().hora_kv_write(k.data_ptr(), v.data_ptr(), _dtype_code(k, "k"), _kv_rows(k, v, n, H, D), _at(slots, torch.int64, "slots"), n, H, D,
+                              kp, vp, ke, ve, code, n_pages, page, _at(status_dev, torch.int32, "status_dev"), _raw_stream(k))
+    _check(rc, "hora_kv_write")
+
+
+def _kv_read(pools, H, D, slots, k, v, status_dev):
+    n = slots.shape[0]
+    rc = load().hora_kv_read(*pools, _at(slots, torch.int64, "slots"), n, H, D, k.data_ptr(), v.data_ptr(), _dtype_code(k, "k"),
+                             _kv_rows(k, v, n, H, D), _at(status_dev, torch.int32, "status_dev"), _raw_stream(k))
+    _check(rc, "hora_kv_read")
+
+
 def hora_kv_write(k, v, slots, k_cache, v_cache, k_exp=None, v_exp=None, status_dev=None):
     """k, v [n, H, D] (rows may be strided) into the pools [n_pages, H, page_size, D] at slots [n] int64."""
-    n_pages, H, page, D = k_cache.shape
-    n = slots.shape[0]
-    stride = _kv_rows(k, v, n, H, D)
-    ct = k_cache.dtype
-    ne = n_pages * H * page
-    rc = load().hora_kv_write(k.data_ptr(), v.data_ptr(), _dtype_code(k, "k"), stride, _at(slots, torch.int64, "slots"), n, H, D,
-                              _at(k_cache, ct, "k_cache"), _at(v_cache, ct, "v_cache", ne * D), _at(k_exp, torch.uint8, "k_exp", ne),
-                              _at(v_exp, torch.uint8, "v_exp", ne), _dtype_code(k_cache, "k_cache"), n_pages, page,
-                              _at(status_dev, torch.int32, "status_dev"), _raw_stream(k))
-    _check(rc, "hora_kv_write")
+    _kv_write(_pools(k_cache, v_cache, k_exp, v_exp), k_cache.shape[1], k_cache.shape[3], k, v, slots, status_dev)
 
 
 def hora_kv_read(k_cache, v_cache, k_exp, v_exp, slots, k, v, status_dev=None):
     """The rows at slots [n] int64 of the pools into k, v [n, H, D] (rows may be strided)."""
-    n_pages, H, page, D = k_cache.shape
-    n = slots.shape[0]
-    stride = _kv_rows(k, v, n, H, D)
-    ct = k_cache.dtype
-    ne = n_pages * H * page
-    rc = load().hora_kv_read(_at(k_cache, ct, "k_cache"), _at(v_cache, ct, "v_cache", ne * D), _at(k_exp, torch.uint8, "k_exp", ne),
-                             _at(v_exp, torch.uint8, "v_exp", ne), _dtype_code(k_cache, "k_cache"), n_pages, page,
-                             _at(slots, torch.int64, "slots"), n, H, D, k.data_ptr(), v.data_ptr(), _dtype_code(k, "k"), stride,
-                             _at(status_dev, torch.int32, "status_dev"), _raw_stream(k))
-    _check(rc, "hora_kv_read")
+    _kv_read(_pools(k_cache, v_cache, k_exp, v_exp), k_cache.shape[1], k_cache.shape[3], slots, k, v, status_dev)
 
 
 def hora_group_attention_workspace_bytes(N, R, T, Hq, Hkv, D) -> int:
@@ -453,13 +460,13 @@ def hora_group_attention(q, group_offsets, q_len, sm_scale, k_cache, v_cache, k_
 
 def hora_verify_drafts(target, draft, draft_tokens, draft_len, R, K, V, u_accept, u_sample, n_accepted, tokens, status_dev=None):
     """target [R, K+1, V], draft [R, K, V] or None: rows may be strided, of one type."""
-    if tuple(target.shape[:2]) != (R, K + 1):
+    if target.shape != (R, K + 1, V):
         raise ValueError(f"target must have the shape {(R, K + 1, V)}, got {tuple(target.shape)}")
-    ts, ds = _row_stride(target, 2, (V,), "target"), 0
+    ts, ds = V if target.is_cuda and target.is_contiguous() else _row_stride(target, 2, (V,), "target"), 0
     if draft is not None:
-        if draft.dtype != target.dtype or tuple(draft.shape[:2]) != (R, K):
+        if draft.dtype != target.dtype or draft.shape != (R, K, V):
             raise ValueError(f"draft must have the shape {(R, K, V)} and the target's type")
-        ds = _row_stride(draft, 2, (V,), "draft")
+        ds = V if draft.is_cuda and draft.is_contiguous() else _row_stride(draft, 2, (V,), "draft")
     rc = load().hora_verify_drafts(target.data_ptr(), _dtype_code(target, "target"), ts, None if draft is None else draft.data_ptr(), ds,
                                    _at(draft_tokens, torch.int32, "draft_tokens", R * K), _at(draft_len, torch.int32, "draft_len", R), R, K, V,
                                    _at(u_accept, torch.float32, "u_accept", R * K), _at(u_sample, torch.float32, "u_sample", R),
@@ -478,6 +485,7 @@ class PagedCache:
             raise ValueError("an e4m3 cache has scale bytes, the others have none")
         self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
         self.n_pages, self.H, self.page_size, self.D = k.shape
+        self._pools = _pools(k, v, k_exp, v_exp)
 
     @classmethod
     def over(cls, *pools):
@@ -492,10 +500,10 @@ class PagedCache:
         return cls(*pools)
 
     def write(self, k, v, slots, status_dev=None):
-        hora_kv_write(k, v, slots, self.k, self.v, self.k_exp, self.v_exp, status_dev)
+        _kv_write(self._pools, self.H, self.D, k, v, slots, status_dev)
 
     def read(self, slots, k, v, status_dev=None):
-        hora_kv_read(self.k, self.v, self.k_exp, self.v_exp, slots, k, v, status_dev)
+        _kv_read(self._pools, self.H, self.D, slots, k, v, status_dev)
 
 
 class GroupAttention:
@@ -516,25 +524,30 @@ class GroupAttention:
     @staticmethod
     def _bind(cache, Hq, T, dtype, group_offsets, prefix_pages, prefix_len, suffix_pages, suffix_len, q_len, sm_scale, workspace, status_dev):
         N, R = prefix_len.shape[0], suffix_len.shape[0]
-        i32, D, ne = torch.int32, cache.D, cache.n_pages * cache.H * cache.page_size
+        i32, D = torch.int32, cache.D
         if prefix_pages.dim() != 2 or suffix_pages.dim() != 2 or prefix_pages.shape[0] != N or suffix_pages.shape[0] != R:
             raise ValueError("the page tables must have one row for each prompt and each rollout")
         if dtype not in _DTYPES:
             raise ValueError(f"unsupported dtype {dtype}")
         keep = (cache, group_offsets, prefix_pages, prefix_len, suffix_pages, suffix_len, q_len, workspace, status_dev)
+        kp, vp, ke, ve, cache_code, n_pages, page = cache._pools
         middle = (_at(group_offsets, torch.int64, "group_offsets", N + 1), N, R, T, _at(q_len, i32, "q_len", R), Hq, cache.H, D, float(sm_scale),
-                  _at(cache.k, cache.k.dtype, "k_cache"), _at(cache.v, cache.k.dtype, "v_cache"), _at(cache.k_exp, torch.uint8, "k_exp", ne),
-                  _at(cache.v_exp, torch.uint8, "v_exp", ne), _DTYPES[cache.k.dtype], cache.n_pages, cache.page_size,
+                  kp, vp, ke, ve, cache_code, n_pages, page,
                   _at(prefix_pages, i32, "prefix_pages"), prefix_pages.shape[1], _at(prefix_len, i32, "prefix_len"),
                   _at(suffix_pages, i32, "suffix_pages"), suffix_pages.shape[1], _at(suffix_len, i32, "suffix_len"))
         tail = (_at(status_dev, i32, "status_dev"), _at(workspace, torch.uint8, "workspace"), workspace.numel())
         code, f, inner = _DTYPES[dtype], load().hora_group_attention, (Hq, D)
 
+        shape, packed = (R, T, Hq, D), (T * Hq * D, Hq * D, D, 1)
+
+        def rows(t, name):
+            if t.dtype != dtype or t.shape != shape:
+                raise ValueError(f"{name} must be a {dtype} tensor of the shape {shape}")
+            return Hq * D if t.is_cuda and t.stride() == packed else _row_stride(t, 2, inner, name)
+
         def call(q, out, lse, _keep=keep):
-            if q.dtype != dtype or out.dtype != dtype or tuple(q.shape[:2]) != (R, T) or tuple(out.shape[:2]) != (R, T):
-                raise ValueError(f"q and out must be {dtype} tensors of the shape {(R, T, Hq, D)}")
-            _check(f(q.data_ptr(), code, _row_stride(q, 2, inner, "q"), *middle, out.data_ptr(), _row_stride(out, 2, inner, "out"),
-                     _at(lse, torch.float32, "lse", R * T * Hq), *tail, _raw_stream(q)), "hora_group_attention")
+            _check(f(q.data_ptr(), code, rows(q, "q"), *middle, out.data_ptr(), rows(out, "out"), _at(lse, torch.float32, "lse", R * T * Hq), *tail,
+                     _raw_stream(q)), "hora_group_attention")
         return call
 
     def run(self, q, out=None, lse=None):
