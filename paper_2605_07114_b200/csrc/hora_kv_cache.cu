@@ -3,7 +3,8 @@
 // A row (one token, one head, D elements) belongs to D/8 neighbouring lanes, eight elements each: one 16-byte access a
 // lane on the 16-bit side, the row's largest magnitude by log2(D/8) shuffles, one 8-byte access on the e4m3 side.  The scale of
 // a quantised row is a power of two, so x / 2^e is exact and the code is the one rounding of the definition.  Nothing is
-// reused: the calls are bound by HBM.  Every lane group has kRowsInFlight rows' loads in flight before it converts the first.
+// reused: the calls are bound by HBM.  Slots are read by ordinary loads, which L1 serves to the other heads of a token (through L2
+// the same takes 346 us).  Every lane group has kRowsInFlight rows' loads in flight before it converts the first.
 #include <type_traits>
 
 #include "hora_rows16.cuh"
@@ -11,7 +12,7 @@
 namespace hora {
 
 constexpr int kKvThreads = 256;
-constexpr int kRowsInFlight = 4;
+constexpr int kRowsInFlight = 4;                         // 131072 tokens, 8 heads of 128, bf16 -> e4m3 -> bf16: 314 us (5.1 TB/s); 2: 369, 8: 441
 
 struct KvShape {
     int64_t n_tokens, row_stride, n_slots;
@@ -43,7 +44,7 @@ struct RowWalk {
 
 template <typename In, typename Cache, int D>
 __global__ void __launch_bounds__(kKvThreads)
-kv_write_kernel(const In *__restrict__ k, const In *__restrict__ v, const int64_t *__restrict__ slots, KvShape s,
+kv_write_kernel(const In *__restrict__ k, const In *__restrict__ v, const int64_t *slots, KvShape s,
                 Cache *__restrict__ k_cache, Cache *__restrict__ v_cache, uint8_t *__restrict__ k_exp,
                 uint8_t *__restrict__ v_exp, int32_t *status) {
     pdl_enter();
@@ -67,7 +68,7 @@ kv_write_kernel(const In *__restrict__ k, const In *__restrict__ v, const int64_
             head[u] = w.h;
             zero8(raw[u]);
             if (w.t < n_tok) {
-                slot[u] = __ldcg(slots + t0 + w.t);
+                slot[u] = slots[t0 + w.t];
                 load8(raw[u], in + (t0 + w.t) * s.row_stride + w.h * D + sub * 8);
             }
             w.next();
@@ -108,7 +109,7 @@ kv_write_kernel(const In *__restrict__ k, const In *__restrict__ v, const int64_
 template <typename Out, typename Cache, int D>
 __global__ void __launch_bounds__(kKvThreads)
 kv_read_kernel(const Cache *__restrict__ k_cache, const Cache *__restrict__ v_cache, const uint8_t *__restrict__ k_exp,
-               const uint8_t *__restrict__ v_exp, const int64_t *__restrict__ slots, KvShape s, Out *__restrict__ k,
+               const uint8_t *__restrict__ v_exp, const int64_t *slots, KvShape s, Out *__restrict__ k,
                Out *__restrict__ v, int32_t *status) {
     pdl_enter();
     constexpr int kLanes = D / 8, kGroups = kKvThreads / kLanes;
@@ -131,7 +132,7 @@ kv_read_kernel(const Cache *__restrict__ k_cache, const Cache *__restrict__ v_ca
             zero8(raw[u]);
             if (w.t < n_tok) {
                 to[u] = (t0 + w.t) * s.row_stride + w.h * D + sub * 8;
-                const int64_t slot = __ldcg(slots + t0 + w.t);
+                const int64_t slot = slots[t0 + w.t];
                 if (slot >= s.n_slots) {
                     if (sub == 0) raise_status(status, HORA_ERR_INVALID_VALUE);
                 } else if (slot >= 0) {
