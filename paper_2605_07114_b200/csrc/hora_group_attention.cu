@@ -133,96 +133,13 @@ __device__ __forceinline__ int32_t stream_of(int64_t u, int64_t per) {
     return ((u | per) >> 32) == 0 ? (int32_t)((uint32_t)u / (uint32_t)per) : (int32_t)(u / per);
 }
 
-// Where the partials of a row are that come from one of its two sequences; rows are taken in order.
-struct Parts {
-    int64_t main;                                        // place among the main ones
-    int64_t u_item, per;                                 // first step of the present item; steps of a stream
-    uint32_t cont, count, halves;                        // first continued row, partials of a half, halves
-    int32_t tile_rows, steps, left, at, step_rows;       // rows of an item, its steps, rows of the sequence from the item on, place in the item
-    bool wide;
-
-    __device__ __forceinline__ void enter_item() {
-        const int32_t b0 = stream_of(u_item, per);
-        const int64_t last = u_item - b0 * per + steps - 1;
-        count = 1 + (last < per ? 0 : stream_of(last, per));
-        // a wide item of one half has its keys dealt to two halves, each with a partial of its own
-        halves = wide && min(tile_rows, left) <= kWideHalf ? 2 : 1;
-        cont = (uint32_t)(b0 + 1) * step_rows + at;
-    }
-    __device__ __forceinline__ void init(const AttnArgs &a, const Sequence &q, int64_t start, int64_t per_, int32_t part, uint32_t r, uint32_t t, uint32_t h,
-                                         uint32_t g0, int64_t row, int64_t rows) {
-        main = part * rows + row + g0;
-        count = 0;
-        halves = 1;
-        wide = q.wide;
-        steps = 0;
-        if (q.steps == 0 || (int32_t)r < q.first || (int32_t)r >= q.first + q.rollouts) return;
-        const uint32_t x = ((r - q.first) * a.T + t) * a.g + g0, tile = x / (uint32_t)q.tile_rows;
-        at = x - tile * q.tile_rows;
-        steps = q.steps;
-        tile_rows = q.tile_rows;
-        left = q.rows - (int32_t)tile * q.tile_rows;
-        per = per_;
-        step_rows = q.wide ? kWideRows : a.narrow_rows;
-        u_item = start + ((int64_t)h * q.tiles + tile) * q.steps;
-        enter_item();
-    }
-    __device__ __forceinline__ void next_row() {
-        ++main;
-        if (steps == 0) return;
-        ++at;
-        ++cont;
-        if (at == tile_rows) {
-            at = 0;
-            left -= tile_rows;
-            u_item += steps;
-            enter_item();
-        }
-    }
-    // partial x of count * halves
-    __device__ __forceinline__ bool where(const AttnArgs &a, int64_t rows, uint32_t x, int32_t D, const float *&ml, const float *&o) const {
-        const uint32_t half = x >= count ? 1 : 0, b = x - half * count;
-        const int64_t place = b == 0 ? main + (int64_t)half * kSecondHalf * rows : (int64_t)cont + (b - 1) * step_rows + half * kWideHalf;
-        if (!HORA_IN(place, b == 0 ? 4 * rows : wide ? (int64_t)a.n_wide * kWideRows : (int64_t)a.n_narrow * a.narrow_rows)) return false;
-        ml = (b == 0 ? a.main_ml : wide ? a.cont_ml[1] : a.cont_ml[0]) + place * 2;
-        o = (b == 0 ? a.main_o : wide ? a.cont_o[1] : a.cont_o[0]) + place * D;
-        return true;
-    }
-};
-
-// Joins the partials of the output rows: a warp to a query's heads of one cache head, D / 32 neighbouring elements a lane.  What
-// bounds the kernel is the chain rollout -> group -> sequence -> partial and the arithmetic on places, so both are done
-// once for all these rows (join_rows of them where there are few queries: then more warps at work count for more); two rows and four
-// partials of each are in flight at a time.
-constexpr int kJoinRows = 2, kJoinAtOnce = 4, kJoinWarps = 8;
-
-template <int E>
-struct Row {
-    float m = -INFINITY, l = 0.f, o[E] = {};
-
-    __device__ __forceinline__ void add(const float2 (&ml)[kJoinAtOnce], const float (&y)[kJoinAtOnce][E]) {
-        float top = m;
-#pragma unroll
-        for (int x = 0; x < kJoinAtOnce; ++x) top = fmaxf(top, ml[x].x);
-        if (top == -INFINITY) return;                    // no key seen so far
-        const float f = exp2_fast(m - top);
-        l *= f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) o[e] *= f;
-        m = top;
-#pragma unroll
-        for (int x = 0; x < kJoinAtOnce; ++x) {
-            if (ml[x].x == -INFINITY) continue;          // its output may not have been written
-            const float g = exp2_fast(ml[x].x - top);
-            l += ml[x].y * g;
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[e] += y[x][e] * g;
-        }
-    }
-};
+// Joins the partials of the output rows: a warp to a query's heads of one cache head, up to kJoinRows of them, D / 32
+// neighbouring elements a lane.  These rows' partials lie next to each other wherever they are (as long as they are of one item), so
+// what is loaded for one part of an item is a block, all of it in flight together, and its place is worked out once.
+constexpr int kJoinRows = 8, kJoinFewRows = 2, kJoinWarps = 8;
 
 template <typename T, int D>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, 2)
 attention_join_kernel(const AttnArgs a) {
     pdl_enter();
     constexpr int E = D / kWarp;
@@ -230,74 +147,92 @@ attention_join_kernel(const AttnArgs a) {
     const uint32_t chunks = (a.g + a.join_rows - 1) / a.join_rows, n_tasks = (uint32_t)a.R * a.T * a.Hkv * chunks;
     const uint32_t task = blockIdx.x * (blockDim.x / kWarp) + (threadIdx.x >> 5);
     if (task >= n_tasks) return;
-    const uint32_t rth = task / chunks, g0 = (task - rth * chunks) * a.join_rows, g1 = min((uint32_t)a.g, g0 + a.join_rows);
+    const uint32_t rth = task / chunks, g0 = (task - rth * chunks) * a.join_rows;
     const uint32_t rt = rth / a.Hkv, h = rth - rt * a.Hkv, r = rt / a.T, t = rt - r * a.T;
-    const int64_t rows = (int64_t)a.R * a.T * a.Hq, row = (int64_t)rt * a.Hq + h * a.g;
+    const int32_t n = min(a.g - (int32_t)g0, a.join_rows);
+    const int64_t rows = (int64_t)a.R * a.T * a.Hq, row = (int64_t)rt * a.Hq + h * a.g + g0;
     const int32_t grp = __ldcg(a.group_of + r);
-    const bool some = grp >= 0 && (int32_t)t < query_count(a, r);
-    Parts p0, p1;
-    if (some) {
+    float m[kJoinRows], l[kJoinRows], o[kJoinRows][E];
+#pragma unroll
+    for (int k = 0; k < kJoinRows; ++k) {
+        m[k] = -INFINITY;
+        l[k] = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[k][e] = 0.f;
+    }
+    if (grp >= 0 && (int32_t)t < query_count(a, r)) {
         bool bad = false;
         const bool wide = has_wide(a);
-        const Sequence own = sequence(a, a.N + r, wide, bad), prompt = sequence(a, grp, wide, bad);
         const int64_t per_narrow = steps_per_stream<false>(a), per_wide = steps_per_stream<true>(a);
-        p0.init(a, prompt, __ldcg((prompt.wide ? a.start[1] : a.start[0]) + grp), prompt.wide ? per_wide : per_narrow, kPromptPart, r, t, h, g0, row, rows);
-        p1.init(a, own, __ldcg((own.wide ? a.start[1] : a.start[0]) + a.N + r), own.wide ? per_wide : per_narrow, kOwnPart, r, t, h, g0, row, rows);
-    }
-    for (uint32_t j0 = g0; j0 < g1; j0 += kJoinRows) {
-        Row<E> sum[kJoinRows];
-        if (some) {
-            Parts q0[kJoinRows], q1[kJoinRows];
-            uint32_t n[kJoinRows], most = 0;
+        const Sequence seq[2] = {sequence(a, grp, wide, bad), sequence(a, a.N + r, wide, bad)};
+        const int64_t start[2][2] = {{__ldcg(a.start[0] + grp), __ldcg(a.start[1] + grp)}, {__ldcg(a.start[0] + a.N + r), __ldcg(a.start[1] + a.N + r)}};
 #pragma unroll
-            for (int j = 0; j < kJoinRows; ++j) {
-                q0[j] = p0;
-                q1[j] = p1;
-                n[j] = j0 + j < g1 ? p0.count * p0.halves + p1.count * p1.halves : 0;
-                most = max(most, n[j]);
-                p0.next_row();
-                p1.next_row();
-            }
-            for (uint32_t x0 = 0; x0 < most; x0 += kJoinAtOnce) {
-                float2 ml[kJoinRows][kJoinAtOnce];
-                float y[kJoinRows][kJoinAtOnce][E];
+        for (int part = 0; part < 2; ++part) {
+            const Sequence &q = seq[part];
+            if (q.steps == 0 || (int32_t)r < q.first || (int32_t)r >= q.first + q.rollouts) continue;
+            const int64_t per = q.wide ? per_wide : per_narrow, first = q.wide ? start[part][1] : start[part][0];
+            const int32_t stream_rows = q.wide ? kWideRows : a.narrow_rows;
+            const float *cont_ml = q.wide ? a.cont_ml[1] : a.cont_ml[0], *cont_o = q.wide ? a.cont_o[1] : a.cont_o[0];
+            uint32_t x = ((r - q.first) * a.T + t) * a.g + g0;
+            for (int32_t j = 0; j < n;) {                // rows j .. j + count - 1 are of one item
+                const uint32_t tile = x / (uint32_t)q.tile_rows, at = x - tile * q.tile_rows;
+                const int32_t count = min(n - j, q.tile_rows - (int32_t)at);
+                const int64_t u = first + ((int64_t)h * q.tiles + tile) * q.steps;
+                const int32_t b0 = stream_of(u, per);
+                const int64_t last = u - b0 * per + q.steps - 1;
+                const int32_t more = last < per ? 0 : stream_of(last, per);
+                // a wide item of one half has its keys dealt to two halves, each with a partial of its own
+                const int halves = q.wide && min(q.tile_rows, q.rows - (int32_t)tile * q.tile_rows) <= kWideHalf ? 2 : 1;
+                for (int half = 0; half < halves; ++half)
+                    for (int32_t b = 0; b <= more; ++b) {
+                        const int64_t place = b == 0 ? (part + half * kSecondHalf) * rows + row + j : (int64_t)(b0 + b) * stream_rows + half * kWideHalf + at;
+                        if (!HORA_IN(place + count - 1, b == 0 ? 4 * rows : q.wide ? (int64_t)a.n_wide * kWideRows : (int64_t)a.n_narrow * a.narrow_rows)) continue;
+                        const float2 *pml = reinterpret_cast<const float2 *>(b == 0 ? a.main_ml : cont_ml) + place - j;
+                        const float *po = (b == 0 ? a.main_o : cont_o) + (place - j) * D + lane * E;
+                        float2 ml[kJoinRows];
+                        float y[kJoinRows][E];
 #pragma unroll
-                for (int j = 0; j < kJoinRows; ++j)
+                        for (int k = 0; k < kJoinRows; ++k) {
+                            ml[k] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-                    for (int x = 0; x < kJoinAtOnce; ++x) {
-                        ml[j][x] = make_float2(-INFINITY, 0.f);
-#pragma unroll
-                        for (int e = 0; e < E; ++e) y[j][x][e] = 0.f;
-                        if (x0 + x < n[j]) {
-                            const uint32_t n0 = q0[j].count * q0[j].halves;
-                            const float *pml, *po;
-                            if (!(x0 + x < n0 ? q0[j].where(a, rows, x0 + x, D, pml, po) : q1[j].where(a, rows, x0 + x - n0, D, pml, po))) continue;
-                            ml[j][x] = __ldcg(reinterpret_cast<const float2 *>(pml));
-                            if constexpr (E == 4) {
-                                const float4 v = __ldcg(reinterpret_cast<const float4 *>(po) + lane);
-                                y[j][x][0] = v.x; y[j][x][1] = v.y; y[j][x][2] = v.z; y[j][x][3] = v.w;
-                            } else {
-                                const float2 v = __ldcg(reinterpret_cast<const float2 *>(po) + lane);
-                                y[j][x][0] = v.x; y[j][x][1] = v.y;
+                            for (int e = 0; e < E; ++e) y[k][e] = 0.f;
+                            if (k >= j && k < j + count) {
+                                ml[k] = __ldcg(pml + k);
+                                if constexpr (E == 4) {
+                                    const float4 v = __ldcg(reinterpret_cast<const float4 *>(po + k * D));
+                                    y[k][0] = v.x; y[k][1] = v.y; y[k][2] = v.z; y[k][3] = v.w;
+                                } else {
+                                    const float2 v = __ldcg(reinterpret_cast<const float2 *>(po + k * D));
+                                    y[k][0] = v.x; y[k][1] = v.y;
+                                }
                             }
                         }
-                    }
 #pragma unroll
-                for (int j = 0; j < kJoinRows; ++j) sum[j].add(ml[j], y[j]);
+                        for (int k = 0; k < kJoinRows; ++k) {
+                            if (ml[k].x == -INFINITY) continue;             // no key seen there (and its output may not have been written)
+                            const float top = fmaxf(m[k], ml[k].x), f = exp2_fast(m[k] - top), g = exp2_fast(ml[k].x - top);
+                            m[k] = top;
+                            l[k] = l[k] * f + ml[k].y * g;
+#pragma unroll
+                            for (int e = 0; e < E; ++e) o[k][e] = o[k][e] * f + y[k][e] * g;
+                        }
+                    }
+                j += count;
+                x += count;
             }
         }
+    }
+    T *__restrict__ out = static_cast<T *>(a.out) + rt * a.out_row_stride + (int64_t)(h * a.g + g0) * D + lane * E;
 #pragma unroll
-        for (int j = 0; j < kJoinRows; ++j) {
-            if (j0 + j >= g1) break;
-            const float inv = sum[j].m == -INFINITY ? 0.f : 1.f / sum[j].l;
-            uint32_t w[E / 2];
+    for (int k = 0; k < kJoinRows; ++k) {
+        if (k >= n) break;
+        const float inv = m[k] == -INFINITY ? 0.f : 1.f / l[k];
+        uint32_t w[E / 2];
 #pragma unroll
-            for (int e = 0; e < E; e += 2) w[e / 2] = pack2(sum[j].o[e] * inv, sum[j].o[e + 1] * inv, T());
-            T *__restrict__ out = static_cast<T *>(a.out) + rt * a.out_row_stride + (int64_t)(h * a.g + j0 + j) * D + lane * E;
-            if constexpr (E == 4) *reinterpret_cast<uint2 *>(out) = make_uint2(w[0], w[1]);
-            else *reinterpret_cast<uint32_t *>(out) = w[0];
-            if (a.lse != nullptr && lane == 0) a.lse[row + j0 + j] = sum[j].m == -INFINITY ? -INFINITY : 0.6931471805599453f * sum[j].m + logf(sum[j].l);
-        }
+        for (int e = 0; e < E; e += 2) w[e / 2] = pack2(o[k][e] * inv, o[k][e + 1] * inv, T());
+        if constexpr (E == 4) *reinterpret_cast<uint2 *>(out + k * D) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t *>(out + k * D) = w[0];
+        if (a.lse != nullptr && lane == 0) a.lse[row + k] = m[k] == -INFINITY ? -INFINITY : 0.6931471805599453f * m[k] + logf(l[k]);
     }
 }
 
@@ -422,8 +357,8 @@ extern "C" hora_status_t hora_group_attention(const void *q, int32_t q_dtype, in
     if (cache_dtype == HORA_DTYPE_E4M3) a.n_wide = 0;
     a.narrow_keys = narrow_keys(cache_dtype == HORA_DTYPE_E4M3, D);
     a.wide_from = kWideFrom;
-    // all heads of a cache head to a warp where that makes enough warps
-    a.join_rows = R * T * Hkv >= (int64_t)a.n_sm * kJoinWarps ? a.g : kJoinRows;
+    // eight rows to a warp where that makes enough warps, else fewer: then the time of one warp counts
+    a.join_rows = R * T * Hkv >= (int64_t)a.n_sm * kJoinWarps ? kJoinRows : kJoinFewRows;
     hora_status_t rc = launch_plan(a, s);
     if (rc == HORA_OK) rc = launch_attention_main(a, q_dtype, cache_dtype, D, s);
     if (rc == HORA_OK) rc = launch_join(a, q_dtype, D, s);
