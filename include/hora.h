@@ -15,6 +15,8 @@
  * This library covers exactly that path, four calls, in execution order:
  *   hora_gains -> hora_allocate -> [rollouts and rewards happen elsewhere] ->
  *   hora_group_advantage -> hora_token_broadcast
+ * and, for where the rollouts happen, the operators of a decode step over such groups (hora_kv_write, hora_group_attention,
+ * hora_verify_drafts).
  *
  * Conventions for every call
  *   - Unless a parameter says "host", every pointer is a DEVICE pointer on the current CUDA device.
@@ -29,8 +31,8 @@
  *   - Results are deterministic: the same inputs give bitwise identical outputs on every run.
  *   - Calls on different streams may run concurrently as long as they do not share output
  *     buffers or workspaces.
- *   - The kernels of hora_gains, hora_allocate, hora_group_advantage, hora_token_broadcast and
- *     hora_group_advantage_tokens are launched with the programmatic-dependent-launch attribute and wait
+ *   - The kernels of hora_gains, hora_allocate, hora_group_advantage, hora_token_broadcast,
+ *     hora_group_advantage_tokens and the decode-step calls are launched with the programmatic-dependent-launch attribute and wait
  *     (griddepcontrol.wait) for the work before them in the stream before they touch memory, so stream order
  *     holds as usual; a kernel of the caller's that follows them with the same attribute must do its own wait.
  */

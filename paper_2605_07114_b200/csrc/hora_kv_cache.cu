@@ -3,16 +3,16 @@
 // A row (one token, one head, D elements) belongs to D/8 neighbouring lanes, eight elements each: one 16-byte access a
 // lane on the 16-bit side, the row's largest magnitude by log2(D/8) shuffles, one 8-byte access on the e4m3 side.  The scale of
 // a quantised row is a power of two, so x / 2^e is exact and the code is the one rounding of the definition.  Nothing is
-// reused: the calls are bound by HBM.  Slots are read by ordinary loads, which L1 serves to the other heads of a token (through L2
-// the same takes 346 us).  Every lane group has kRowsInFlight rows' loads in flight before it converts the first.
+// reused: the calls are bound by HBM.  Slots are read by ordinary loads, which L1 serves to the other heads of a token (through L2 the same took a
+// tenth longer).  Every lane group has kRowsInFlight rows' loads in flight before it converts the first.
 #include <type_traits>
 
 #include "hora_rows16.cuh"
 
 namespace hora {
 
-constexpr int kKvThreads = 256;
-constexpr int kRowsInFlight = 4;                         // 131072 tokens, 8 heads of 128, bf16 -> e4m3 -> bf16: 314 us (5.1 TB/s); 2: 369, 8: 441
+constexpr int kKvThreads = 128;                          // 131072 tokens (below): 291 us with 128, 317 with 256
+constexpr int kRowsInFlight = 4;                         // 131072 tokens, 8 heads of 128, bf16 -> e4m3 -> bf16: 291 us (5.5 TB/s); with 2 and 8, at 256 threads, 369 and 441 against 317
 
 struct KvShape {
     int64_t n_tokens, row_stride, n_slots;
@@ -82,11 +82,11 @@ kv_write_kernel(const In *__restrict__ k, const In *__restrict__ v, const int64_
             float x[8];
             widen8(raw[u], x);
             if constexpr (sizeof(Cache) == 1) {
-                float a = 0.f;
+                float a = largest8(raw[u]);
+                if (!(a <= 3.402823466e38f)) {                             // not finite: the largest of those that are
+                    a = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float y = fabsf(x[i]);
-                    a = y <= 3.402823466e38f ? fmaxf(a, y) : a;            // finite values only (a NaN fails the comparison)
+                    for (int i = 0; i < 8; ++i) a = fabsf(x[i]) <= 3.402823466e38f ? fmaxf(a, fabsf(x[i])) : a;
                 }
 #pragma unroll
                 for (int d = kLanes / 2; d > 0; d >>= 1) a = fmaxf(a, __shfl_xor_sync(kFull, a, d));

@@ -70,6 +70,21 @@ __device__ __forceinline__ void widen8(const Raw8<__half> &r, float (&x)[8]) {
         x[2 * i + 1] = f.y;
     }
 }
+// Largest magnitude of the eight, by their bits, which order like the magnitudes (infinity and NaN above all others).
+__device__ __forceinline__ float largest8(const Raw8<float> &r) {
+    const float x[8] = {r.a.x, r.a.y, r.a.z, r.a.w, r.b.x, r.b.y, r.b.z, r.b.w};
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    return __uint_as_float(m);
+}
+__device__ __forceinline__ uint32_t largest_half_bits(const uint4 &w) {
+    const uint32_t m = __vmaxu2(__vmaxu2(w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu), __vmaxu2(w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu));
+    return max(m & 0xFFFFu, m >> 16);
+}
+__device__ __forceinline__ float largest8(const Raw8<__nv_bfloat16> &r) { return __uint_as_float(largest_half_bits(r.a) << 16); }
+__device__ __forceinline__ float largest8(const Raw8<__half> &r) { return half2_bits(largest_half_bits(r.a)).x; }
+
 // two codes (the low 16 bits) as a pair of halves; exact, NaN stays NaN
 __device__ __forceinline__ uint32_t e4m3x2_to_half2(uint32_t two) {
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
