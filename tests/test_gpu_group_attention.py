@@ -281,6 +281,66 @@ def test_on_another_stream_and_through_the_object():
     check(t, h, 64 ** -0.5, out, lse)
 
 
+def test_thousands_of_small_groups(build):
+    """More sequences than a thread of the plan keeps in registers, empty groups among them; a sample of the rollouts is checked."""
+    rng = np.random.default_rng(8)
+    sizes = rng.integers(0, 7, 1700)
+    R = int(sizes.sum())
+    assert R + 1700 > 4 * 1024
+    t, h = make(sizes, rng.integers(0, 40, 1700), rng.integers(0, 50, R), 1, 3, 1, 64, torch.bfloat16, torch.bfloat16, 16, 61)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    out, lse = call(t, 0.125, status=status)
+    assert int(status) == 0
+    group = np.repeat(np.arange(1700), sizes)
+    for r in rng.permutation(R)[:80].tolist() + [0, R - 1]:
+        i = group[r]
+        k, v = (np.concatenate([pool[h["pp"][i][np.arange(h["pl"][i]) // 16], 0, np.arange(h["pl"][i]) % 16],
+                                pool[h["sp"][r][np.arange(h["sl"][r]) // 16], 0, np.arange(h["sl"][r]) % 16]]) for pool in (h["k"], h["v"]))
+        for x in range(3):
+            want, wlse, bound, reach = orc.attention_query(h["q"][r, 0, x], k, v, 0.125)
+            tol = bound * (2.0 ** -8 + 64 * 2.0 ** -22 * reach + 2.0 ** -18) + 2.0 ** -8 * np.abs(want) + 2.0 ** -24
+            assert (np.abs(out[r, 0, x].double().cpu().numpy() - want) <= tol).all(), (r, x)
+            got = float(lse[r, 0, x])
+            assert got == wlse if math.isinf(wlse) else abs(got - wlse) <= 64 * 2.0 ** -23 * reach + 2.0 ** -18 * (1 + abs(wlse))
+
+
+@pytest.mark.parametrize("cache", [torch.bfloat16, F8])
+def test_pages_beyond_32_bit_offsets(cache):
+    """Pools of more than 2^32 bytes and 2^31 elements: keys and values in the last pages, written, read back and attended to."""
+    hora = _hora()
+    D, Hkv, page, G, P = 128, 2, 64, 40, 500
+    n_pages = (1 << 31) // (Hkv * page * D) + 40 if cache != F8 else (1 << 32) // (Hkv * page * D) + 40
+    c = hora.PagedCache.empty(n_pages, page, Hkv, D, cache)
+    g = torch.Generator(device=DEV).manual_seed(4)
+    pages = n_pages - 1 - torch.arange(8, device=DEV)
+    own = n_pages - 9 - torch.arange(G, device=DEV) % 20            # rollouts share pages here: they are only read
+    at = torch.arange(P, device=DEV)
+    k, v = (torch.randn(P, Hkv, D, device=DEV, generator=g).to(torch.bfloat16) for _ in range(2))
+    slots = pages[at // page] * page + at % page
+    c.write(k, v, slots)
+    ko, vo = (torch.empty(P, Hkv, D, device=DEV) for _ in range(2))
+    c.read(slots, ko, vo)
+    if cache != F8:
+        assert torch.equal(ko, k.float()) and torch.equal(vo, v.float())
+    else:
+        assert ((ko - k.float()).abs() <= k.float().abs() / 16 + 2.0 ** -12 * k.float().abs().amax(-1, keepdim=True)).all()
+    ks, vs = (torch.randn(20 * page, Hkv, D, device=DEV, generator=g).to(torch.bfloat16) for _ in range(2))
+    c.write(ks, vs, ((n_pages - 9 - torch.arange(20, device=DEV))[:, None] * page + torch.arange(page, device=DEV)).flatten())
+    kso, vso = (torch.empty(20 * page, Hkv, D, device=DEV) for _ in range(2))
+    c.read(((n_pages - 9 - torch.arange(20, device=DEV))[:, None] * page + torch.arange(page, device=DEV)).flatten(), kso, vso)
+    i32 = lambda x: torch.as_tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    q = torch.randn(G, 1, 4, D, device=DEV, generator=g).to(torch.bfloat16)
+    op = hora.GroupAttention(c, 4, 1, torch.bfloat16, group_offsets=torch.tensor([0, G], device=DEV), prefix_pages=i32(pages)[None].contiguous(), prefix_len=i32([P]),
+                             suffix_pages=i32(own)[:, None].contiguous(), suffix_len=i32([page] * G))
+    out, _ = op.run(q)
+    r = torch.arange(G, device=DEV) % 20
+    kk = torch.cat([ko.double().expand(G, P, Hkv, D), kso.double().reshape(20, page, Hkv, D)[r]], 1).repeat_interleave(2, 2)
+    vv = torch.cat([vo.double().expand(G, P, Hkv, D), vso.double().reshape(20, page, Hkv, D)[r]], 1).repeat_interleave(2, 2)
+    w = torch.softmax(torch.einsum("rhd,rnhd->rhn", q[:, 0].double(), kk) * D ** -0.5, -1)
+    want, bound = torch.einsum("rhn,rnhd->rhd", w, vv), torch.einsum("rhn,rnhd->rhd", w, vv.abs())
+    assert ((out[:, 0].double() - want).abs() <= 2.0 ** -8 * (bound + want.abs()) + 2.0 ** -12 * bound + 1e-6).all()
+
+
 def test_values_that_are_out_of_range_are_reported_and_stay_in_bounds(build):
     """Lengths, counts, page numbers and offsets that cannot be: reported, clamped; the other rollouts' results stand."""
     hora = _hora()
