@@ -133,28 +133,30 @@ __device__ __forceinline__ int32_t stream_of(int64_t u, int64_t per) {
     return ((u | per) >> 32) == 0 ? (int32_t)((uint32_t)u / (uint32_t)per) : (int32_t)(u / per);
 }
 
-// Joins the partials of the output rows: a warp to a query's heads of one cache head, up to kJoinRows of them, D / 32
-// neighbouring elements a lane.  These rows' partials lie next to each other wherever they are (as long as they are of one item), so
-// what is loaded for one part of an item is a block, all of it in flight together, and its place is worked out once.
-constexpr int kJoinRows = 8, kJoinFewRows = 2, kJoinWarps = 8;
+// Joins the partials of the output rows: a warp to ROWS heads of a query and cache head, D / 32 neighbouring elements a lane.
+// These rows' partials lie next to each other wherever they are (as long as they are of one item), so what is loaded for PARTS parts of
+// an item is in flight together, and its place is worked out once.  With many rows eight of them and a part at a time; with few rows
+// there may be dozens of parts to each, and one row with eight parts at a time is faster (one prompt of 103485 keys, 64
+// rollouts, 37 parts a row: see below).
+constexpr int kJoinRows = 8, kJoinParts = 8, kJoinWarps = 8;
 
-template <typename T, int D>
+template <typename T, int D, int ROWS, int PARTS>
 __global__ void __launch_bounds__(256, 2)
 attention_join_kernel(const AttnArgs a) {
     pdl_enter();
     constexpr int E = D / kWarp;
     const int lane = lane_id();
-    const uint32_t chunks = (a.g + a.join_rows - 1) / a.join_rows, n_tasks = (uint32_t)a.R * a.T * a.Hkv * chunks;
+    const uint32_t chunks = (a.g + ROWS - 1) / ROWS, n_tasks = (uint32_t)a.R * a.T * a.Hkv * chunks;
     const uint32_t task = blockIdx.x * (blockDim.x / kWarp) + (threadIdx.x >> 5);
     if (task >= n_tasks) return;
-    const uint32_t rth = task / chunks, g0 = (task - rth * chunks) * a.join_rows;
+    const uint32_t rth = task / chunks, g0 = (task - rth * chunks) * ROWS;
     const uint32_t rt = rth / a.Hkv, h = rth - rt * a.Hkv, r = rt / a.T, t = rt - r * a.T;
-    const int32_t n = min(a.g - (int32_t)g0, a.join_rows);
+    const int32_t n = min(a.g - (int32_t)g0, ROWS);
     const int64_t rows = (int64_t)a.R * a.T * a.Hq, row = (int64_t)rt * a.Hq + h * a.g + g0;
     const int32_t grp = __ldcg(a.group_of + r);
-    float m[kJoinRows], l[kJoinRows], o[kJoinRows][E];
+    float m[ROWS], l[ROWS], o[ROWS][E];
 #pragma unroll
-    for (int k = 0; k < kJoinRows; ++k) {
+    for (int k = 0; k < ROWS; ++k) {
         m[k] = -INFINITY;
         l[k] = 0.f;
 #pragma unroll
@@ -183,40 +185,47 @@ attention_join_kernel(const AttnArgs a) {
                 const int32_t more = last < per ? 0 : stream_of(last, per);
                 // a wide item of one half has its keys dealt to two halves, each with a partial of its own
                 const int halves = q.wide && min(q.tile_rows, q.rows - (int32_t)tile * q.tile_rows) <= kWideHalf ? 2 : 1;
-                for (int half = 0; half < halves; ++half)
-                    for (int32_t b = 0; b <= more; ++b) {
+                const int32_t parts = halves * (more + 1);
+                for (int32_t p = 0; p < parts; p += PARTS) {
+                    float2 ml[PARTS][ROWS];
+                    float y[PARTS][ROWS][E];
+#pragma unroll
+                    for (int z = 0; z < PARTS; ++z) {
+                        const int half = p + z > more ? 1 : 0;
+                        const int32_t b = p + z - half * (more + 1);
                         const int64_t place = b == 0 ? (part + half * kSecondHalf) * rows + row + j : (int64_t)(b0 + b) * stream_rows + half * kWideHalf + at;
-                        if (!HORA_IN(place + count - 1, b == 0 ? 4 * rows : q.wide ? (int64_t)a.n_wide * kWideRows : (int64_t)a.n_narrow * a.narrow_rows)) continue;
+                        const bool have = p + z < parts && HORA_IN(place + count - 1, b == 0 ? 4 * rows : q.wide ? (int64_t)a.n_wide * kWideRows : (int64_t)a.n_narrow * a.narrow_rows);
                         const float2 *pml = reinterpret_cast<const float2 *>(b == 0 ? a.main_ml : cont_ml) + place - j;
                         const float *po = (b == 0 ? a.main_o : cont_o) + (place - j) * D + lane * E;
-                        float2 ml[kJoinRows];
-                        float y[kJoinRows][E];
 #pragma unroll
-                        for (int k = 0; k < kJoinRows; ++k) {
-                            ml[k] = make_float2(-INFINITY, 0.f);
+                        for (int k = 0; k < ROWS; ++k) {
+                            ml[z][k] = make_float2(-INFINITY, 0.f);
 #pragma unroll
-                            for (int e = 0; e < E; ++e) y[k][e] = 0.f;
-                            if (k >= j && k < j + count) {
-                                ml[k] = __ldcg(pml + k);
+                            for (int e = 0; e < E; ++e) y[z][k][e] = 0.f;
+                            if (have && k >= j && k < j + count) {
+                                ml[z][k] = __ldcg(pml + k);
                                 if constexpr (E == 4) {
                                     const float4 v = __ldcg(reinterpret_cast<const float4 *>(po + k * D));
-                                    y[k][0] = v.x; y[k][1] = v.y; y[k][2] = v.z; y[k][3] = v.w;
+                                    y[z][k][0] = v.x; y[z][k][1] = v.y; y[z][k][2] = v.z; y[z][k][3] = v.w;
                                 } else {
                                     const float2 v = __ldcg(reinterpret_cast<const float2 *>(po + k * D));
-                                    y[k][0] = v.x; y[k][1] = v.y;
+                                    y[z][k][0] = v.x; y[z][k][1] = v.y;
                                 }
                             }
                         }
-#pragma unroll
-                        for (int k = 0; k < kJoinRows; ++k) {
-                            if (ml[k].x == -INFINITY) continue;             // no key seen there (and its output may not have been written)
-                            const float top = fmaxf(m[k], ml[k].x), f = exp2_fast(m[k] - top), g = exp2_fast(ml[k].x - top);
-                            m[k] = top;
-                            l[k] = l[k] * f + ml[k].y * g;
-#pragma unroll
-                            for (int e = 0; e < E; ++e) o[k][e] = o[k][e] * f + y[k][e] * g;
-                        }
                     }
+#pragma unroll
+                    for (int z = 0; z < PARTS; ++z)
+#pragma unroll
+                        for (int k = 0; k < ROWS; ++k) {
+                            if (ml[z][k].x == -INFINITY) continue;          // no key seen there (and its output may not have been written)
+                            const float top = fmaxf(m[k], ml[z][k].x), f = exp2_fast(m[k] - top), g = exp2_fast(ml[z][k].x - top);
+                            m[k] = top;
+                            l[k] = l[k] * f + ml[z][k].y * g;
+#pragma unroll
+                            for (int e = 0; e < E; ++e) o[k][e] = o[k][e] * f + y[z][k][e] * g;
+                        }
+                }
                 j += count;
                 x += count;
             }
@@ -224,7 +233,7 @@ attention_join_kernel(const AttnArgs a) {
     }
     T *__restrict__ out = static_cast<T *>(a.out) + rt * a.out_row_stride + (int64_t)(h * a.g + g0) * D + lane * E;
 #pragma unroll
-    for (int k = 0; k < kJoinRows; ++k) {
+    for (int k = 0; k < ROWS; ++k) {
         if (k >= n) break;
         const float inv = m[k] == -INFINITY ? 0.f : 1.f / l[k];
         uint32_t w[E / 2];
@@ -242,16 +251,18 @@ static hora_status_t launch_plan(const AttnArgs &a, cudaStream_t stream) {
     return cuda_ok(e);
 }
 
+template <typename T, int D>
+static cudaError_t launch_join_of(const AttnArgs &a, cudaStream_t stream) {
+    const int64_t queries = (int64_t)a.R * a.T * a.Hkv;
+    const bool many = queries >= (int64_t)a.n_sm * kJoinWarps;
+    const int64_t tasks = queries * (many ? (a.g + kJoinRows - 1) / kJoinRows : a.g);
+    return launch_pdl(many ? attention_join_kernel<T, D, kJoinRows, 1> : attention_join_kernel<T, D, 1, kJoinParts>, (int)((tasks + 7) / 8), 256, 0, stream, a);
+}
+
 static hora_status_t launch_join(const AttnArgs &a, int32_t q_dtype, int32_t D, cudaStream_t stream) {
-    const int64_t tasks = (int64_t)a.R * a.T * a.Hkv * ((a.g + a.join_rows - 1) / a.join_rows);
-    const int grid = (int)((tasks + 7) / 8);
     cudaError_t e;
-    if (q_dtype == HORA_DTYPE_BF16)
-        e = D == 64 ? launch_pdl(attention_join_kernel<__nv_bfloat16, 64>, grid, 256, 0, stream, a)
-                    : launch_pdl(attention_join_kernel<__nv_bfloat16, 128>, grid, 256, 0, stream, a);
-    else
-        e = D == 64 ? launch_pdl(attention_join_kernel<__half, 64>, grid, 256, 0, stream, a)
-                    : launch_pdl(attention_join_kernel<__half, 128>, grid, 256, 0, stream, a);
+    if (q_dtype == HORA_DTYPE_BF16) e = D == 64 ? launch_join_of<__nv_bfloat16, 64>(a, stream) : launch_join_of<__nv_bfloat16, 128>(a, stream);
+    else e = D == 64 ? launch_join_of<__half, 64>(a, stream) : launch_join_of<__half, 128>(a, stream);
     count_launches(1);
     return cuda_ok(e);
 }
@@ -357,8 +368,6 @@ extern "C" hora_status_t hora_group_attention(const void *q, int32_t q_dtype, in
     if (cache_dtype == HORA_DTYPE_E4M3) a.n_wide = 0;
     a.narrow_keys = narrow_keys(cache_dtype == HORA_DTYPE_E4M3, D);
     a.wide_from = kWideFrom;
-    // eight rows to a warp where that makes enough warps, else fewer: then the time of one warp counts
-    a.join_rows = R * T * Hkv >= (int64_t)a.n_sm * kJoinWarps ? kJoinRows : kJoinFewRows;
     hora_status_t rc = launch_plan(a, s);
     if (rc == HORA_OK) rc = launch_attention_main(a, q_dtype, cache_dtype, D, s);
     if (rc == HORA_OK) rc = launch_join(a, q_dtype, D, s);

@@ -47,7 +47,6 @@ struct AttnArgs {
     int32_t N, R, T, Hq, Hkv, g, page_shift, prefix_ld, suffix_ld;
     int32_t n_sm, n_narrow, n_wide;                      // CTAs, streams of each line; n_wide 0: every sequence is narrow
     int32_t narrow_keys, narrow_rows;                    // keys of a narrow step, rows of a narrow item
-    int32_t join_rows;                                   // heads that a warp joins
     int32_t wide_from;                                   // rows from which a sequence is wide
     float scale_log2;                                    // sm_scale * log2(e)
     // workspace
