@@ -9,8 +9,6 @@ namespace hora {
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanKept = 4;                             // sequences of a thread whose steps it keeps in registers
 constexpr int kPlanOffsets = 4096;                       // group offsets kept in shared memory for the searches
-// Sequences with fewer rows are narrow: a CTA for 128 rows at a time would be mostly idle.
-constexpr int kWideFrom = 33;
 // The wide items' pass costs about 15 us however little there is to do in it: they are taken as narrow ones instead while
 // that makes no more than this many steps a stream (of 8 rows and 16 or 32 keys, about a microsecond each).
 #ifdef HORA_CHECKED
@@ -41,7 +39,7 @@ attention_plan_kernel(const AttnArgs a) {
         const Sequence n = sequence(a, (int32_t)i, false, bad);
         as_narrow = total_steps(a, n);
         as_wide = 0;
-        if (a.n_wide > 0 && n.rows >= a.wide_from) as_wide = total_steps(a, sequence(a, (int32_t)i, true, ignore));
+        if (can_be_wide(a, n)) as_wide = total_steps(a, sequence(a, (int32_t)i, true, ignore));
         sum[as_wide ? kEither : kNarrow] += as_narrow;
         sum[kWide] += as_wide;
     };
@@ -100,7 +98,7 @@ attention_plan_kernel(const AttnArgs a) {
     if (!fits)
         for (int64_t i = lo; i < hi; ++i) {
             const Sequence n = sequence(a, (int32_t)i, false, ignore);
-            const bool can = a.n_wide > 0 && n.rows >= a.wide_from;
+            const bool can = can_be_wide(a, n);
             place(i, can ? total_steps(a, sequence(a, (int32_t)i, true, ignore)) : 0, total_steps(a, n));
         }
     if (threadIdx.x == 0) {
@@ -136,8 +134,8 @@ __device__ __forceinline__ int32_t stream_of(int64_t u, int64_t per) {
 // Joins the partials of the output rows: a warp to ROWS heads of a query and cache head, D / 32 neighbouring elements a lane.
 // These rows' partials lie next to each other wherever they are (as long as they are of one item), so what is loaded for PARTS parts of
 // an item is in flight together, and its place is worked out once.  With many rows eight of them and a part at a time; with few rows
-// there may be dozens of parts to each, and one row with eight parts at a time is faster (one prompt of 103485 keys, 64
-// rollouts, 37 parts a row: see below).
+// there may be dozens of parts to each, and one row with eight parts at a time is faster (one prompt of 103485 keys, 24
+// rollouts, 37 parts a row: 147 us for the whole call with two rows and a part at a time, 125 so).
 constexpr int kJoinRows = 8, kJoinParts = 8, kJoinWarps = 8;
 
 template <typename T, int D, int ROWS, int PARTS>
@@ -367,7 +365,6 @@ extern "C" hora_status_t hora_group_attention(const void *q, int32_t q_dtype, in
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (cache_dtype == HORA_DTYPE_E4M3) a.n_wide = 0;
     a.narrow_keys = narrow_keys(cache_dtype == HORA_DTYPE_E4M3, D);
-    a.wide_from = kWideFrom;
     hora_status_t rc = launch_plan(a, s);
     if (rc == HORA_OK) rc = launch_attention_main(a, q_dtype, cache_dtype, D, s);
     if (rc == HORA_OK) rc = launch_join(a, q_dtype, D, s);

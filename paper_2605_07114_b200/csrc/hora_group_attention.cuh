@@ -30,6 +30,7 @@ constexpr int kNarrowMinSteps = 4;                       // a stream shorter tha
 constexpr int kWideRows = 256;                           // query rows of a wide item, in two halves
 constexpr int kWideHalf = kWideRows / 2;
 constexpr int kWideKeys = 128;
+constexpr int kWideFrom = 33, kWideLong = 1024;          // rows from which, keys from which a sequence's items can be wide
 
 // Parts that a row's result is joined from, other than the continued ones.
 enum { kPromptPart = 0, kOwnPart = 1, kSecondHalf = 2 }; // kSecondHalf: added for the second half of the keys (wide items of one half)
@@ -47,7 +48,6 @@ struct AttnArgs {
     int32_t N, R, T, Hq, Hkv, g, page_shift, prefix_ld, suffix_ld;
     int32_t n_sm, n_narrow, n_wide;                      // CTAs, streams of each line; n_wide 0: every sequence is narrow
     int32_t narrow_keys, narrow_rows;                    // keys of a narrow step, rows of a narrow item
-    int32_t wide_from;                                   // rows from which a sequence is wide
     float scale_log2;                                    // sm_scale * log2(e)
     // workspace
     int64_t *start[2];                                   // [N + R + 3] first step of each sequence on the narrow, the wide line; all; a stream's; [1]: has_wide
@@ -82,7 +82,15 @@ __device__ __forceinline__ int32_t query_count(const AttnArgs &a, int32_t r) {
     return n < 0 ? 0 : (n > a.T ? a.T : n);
 }
 
-// `wide`: whether sequences with enough rows for it are wide in this call.
+// Whether a sequence's items can be wide.  Many rows: a narrow item would read the keys again for every eight or sixteen of them.  Fewer rows
+// over a long list: the same, and the CTA's 128 rows may be mostly idle, since the bytes are what takes the time (103485 keys,
+// 32 rows of 4 heads each: 318 us as narrow items, 122 as wide ones).  Short lists of few rows are narrow: a piece of a wide item costs
+// some microseconds to begin and to end (256 rollouts of 20 rows over up to 1021 keys: 122 us, 172 as wide items).
+__device__ __forceinline__ bool can_be_wide(const AttnArgs &a, const Sequence &s) {
+    return a.n_wide > 0 && (s.rows >= kWideFrom || (s.rows > a.narrow_rows && s.len >= kWideLong));
+}
+
+// `wide`: whether sequences that can be are wide in this call.
 __device__ __forceinline__ Sequence sequence(const AttnArgs &a, int32_t i, bool wide, bool &bad) {
     Sequence s = {};
     if (!HORA_IN(i, a.N + a.R)) return s;
@@ -100,7 +108,7 @@ __device__ __forceinline__ Sequence sequence(const AttnArgs &a, int32_t i, bool 
         s.len = checked_len(__ldcg(a.suffix_len + s.first), a.suffix_ld, a.page_shift, bad);
     }
     s.rows = s.rollouts * a.T * a.g;
-    s.wide = wide && s.rows >= a.wide_from;
+    s.wide = wide && can_be_wide(a, s);
     if (s.wide) {                                        // blocks of about the same size, so that their steps take the same time
         s.tiles = (s.rows + kWideRows - 1) / kWideRows;
         s.tile_rows = (s.rows + s.tiles - 1) / s.tiles;
