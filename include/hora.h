@@ -528,12 +528,12 @@ uint64_t hora_fp64_probe(int32_t iters, double *sink_dev, void *stream);
 /*
  * hora_checked_violation — verification aid, no counterpart in the paper.  The library can be built a second time
  * with -DHORA_CHECKED (python -m paper_2605_07114_b200.build --checked writes libhora_checked.so): every access of
- * the allocation, batched-allocation, advantage and attention kernels whose index is computed from device data then checks
+ * the allocation, batched-allocation, advantage, attention and verification kernels whose index is computed from device data then checks
  * that index against the size of its array; a violation is recorded (never trapped: the access goes to a scratch
  * slot and the kernel runs on).  This call synchronises the device and returns 0 if no check has failed since the
  * last call, else (file id << 20) | source line of the first failure (file ids: 1 hora_allocate.cu,
  * 2 hora_allocate_batched.cu, 3 hora_advantage.cu, 4 hora_rank.cu,
- * 5 hora_group_attention.cu, 6 hora_group_attention_main.cu with what it includes); the record is cleared.  The normal build has no
+ * 5 hora_group_attention.cu, 6 hora_group_attention_main.cu with what it includes, 7 hora_verify.cu); the record is cleared.  The normal build has no
  * checks and returns -1; -2 reports a failed synchronisation.
  */
 int32_t hora_checked_violation(void);

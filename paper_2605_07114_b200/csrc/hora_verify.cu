@@ -11,7 +11,11 @@
 
 #include <utility>
 
+#define HORA_FILE_ID 7
+#include "hora_checked.cuh"
 #include "hora_rows16.cuh"
+
+HORA_CHECKED_REGISTER()
 
 namespace hora {
 
@@ -147,7 +151,7 @@ __device__ __forceinline__ uint64_t segment_sum(const Rows<T> &r, int32_t v0, in
     hi = __reduce_add_sync(kFull, hi);
     lo = __reduce_add_sync(kFull, lo);
     int64_t sum = ((int64_t)hi << 20) + lo;
-    if (!MINUS && r.one_hot >= v0 && r.one_hot < v0 + kSeg<T> && r.one_hot >= 0) sum -= on_grid(clamped(as_float(r.plus[r.one_hot]), bad)).value();
+    if (!MINUS && r.one_hot >= v0 && r.one_hot < v0 + kSeg<T> && r.one_hot >= 0 && HORA_IN(r.one_hot, r.V)) sum -= on_grid(clamped(as_float(r.plus[r.one_hot]), bad)).value();
     return (uint64_t)sum;
 }
 
@@ -197,7 +201,9 @@ verify_kernel(const VerifyArgs a) {
     rows.V = a.V;
     rows.plus = static_cast<const T *>(a.target) + (r * (a.K + 1) + n) * a.target_stride;
     rows.minus = (n < len && a.draft != nullptr) ? static_cast<const T *>(a.draft) + (r * a.K + n) * a.draft_stride : nullptr;
-    rows.one_hot = (n < len && a.draft == nullptr) ? __ldcg(a.draft_tokens + r * a.K + n) : -1;
+    // a token outside the vocabulary was refused for that: the row has no place for it, and nothing is taken off
+    const int32_t refused = (n < len && a.draft == nullptr) ? __ldcg(a.draft_tokens + r * a.K + n) : -1;
+    rows.one_hot = refused < a.V ? refused : -1;
 
     // the vocabulary in blocks of 16 bytes as they lie in memory: `lead` elements of the first one are not the row's
     constexpr int kPer16 = 16 / sizeof(T);
