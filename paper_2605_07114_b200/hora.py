@@ -408,7 +408,7 @@ def _kv_rows(k: torch.Tensor, v: torch.Tensor, n: int, H: int, D: int) -> int:
     if k.dtype != v.dtype or k.shape[0] != n or v.shape[0] != n:
         raise ValueError("k and v must have one type and one row for each slot")
     stride = _row_stride(k, 1, (H, D), "k")
-    if n > 1 and stride != _row_stride(v, 1, (H, D), "v"):
+    if stride != _row_stride(v, 1, (H, D), "v"):
         raise ValueError("k and v must have the same row stride")
     return stride
 
