@@ -404,7 +404,7 @@ def _dtype_code(t: torch.Tensor, name: str) -> int:
 def _kv_rows(k: torch.Tensor, v: torch.Tensor, n: int, H: int, D: int) -> int:
     ks = k.stride()
     if k.dtype == v.dtype and k.shape == v.shape == (n, H, D) and ks == v.stride() and ks[1:] == (D, 1) and k.is_cuda and v.is_cuda:
-        return ks[0]                                               # the usual case, in few steps
+        return ks[0] if n != 1 else H * D                          # the usual case, in few steps; a single row has no stride
     if k.dtype != v.dtype or k.shape[0] != n or v.shape[0] != n:
         raise ValueError("k and v must have one type and one row for each slot")
     stride = _row_stride(k, 1, (H, D), "k")

@@ -36,3 +36,10 @@ def test_values_are_checked_like_keys_whatever_the_number_of_tokens(n, v):
         hora._kv_rows(Rows(n, H, D), v(n), n, H, D)
     with pytest.raises(ValueError):
         hora._kv_rows(v(n), Rows(n, H, D), n, H, D)
+
+
+@pytest.mark.parametrize("stride", [(D, D, 1), (0, D, 1), (1, D, 1), (10 ** 9 + 1, D, 1)])
+def test_a_single_token_has_no_row_stride(stride):
+    """The stride of a dimension of size one says nothing (a transposed view leaves any number there): the call gets one that it takes."""
+    got = hora._kv_rows(Rows(1, H, D, stride=stride), Rows(1, H, D, stride=stride), 1, H, D)
+    assert got == H * D
