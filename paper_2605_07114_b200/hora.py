@@ -413,6 +413,12 @@ def _kv_rows(k: torch.Tensor, v: torch.Tensor, n: int, H: int, D: int) -> int:
     return stride
 
 
+def _slot_count(slots: torch.Tensor) -> int:
+    if slots.dim() != 1:
+        raise ValueError(f"slots must have one dimension, got the shape {tuple(slots.shape)}")
+    return slots.shape[0]
+
+
 def _pools(k_cache, v_cache, k_exp, v_exp):
     """The cache's part of the arguments: pointers, type, shape."""
     n_pages, H, page, D = k_cache.shape
@@ -422,7 +428,7 @@ def _pools(k_cache, v_cache, k_exp, v_exp):
 
 
 def _kv_write(pools, H, D, k, v, slots, status_dev):
-    n = slots.shape[0]
+    n = _slot_count(slots)
     kp, vp, ke, ve, code, n_pages, page = pools
     rc = load().hora_kv_write(k.data_ptr(), v.data_ptr(), _dtype_code(k, "k"), _kv_rows(k, v, n, H, D), _at(slots, torch.int64, "slots"), n, H, D,
                               kp, vp, ke, ve, code, n_pages, page, _at(status_dev, torch.int32, "status_dev"), _raw_stream(k))
@@ -430,7 +436,7 @@ def _kv_write(pools, H, D, k, v, slots, status_dev):
 
 
 def _kv_read(pools, H, D, slots, k, v, status_dev):
-    n = slots.shape[0]
+    n = _slot_count(slots)
     rc = load().hora_kv_read(*pools, _at(slots, torch.int64, "slots"), n, H, D, k.data_ptr(), v.data_ptr(), _dtype_code(k, "k"),
                              _kv_rows(k, v, n, H, D), _at(status_dev, torch.int32, "status_dev"), _raw_stream(k))
     _check(rc, "hora_kv_read")

@@ -43,3 +43,15 @@ def test_a_single_token_has_no_row_stride(stride):
     """The stride of a dimension of size one says nothing (a transposed view leaves any number there): the call gets one that it takes."""
     got = hora._kv_rows(Rows(1, H, D, stride=stride), Rows(1, H, D, stride=stride), 1, H, D)
     assert got == H * D
+
+
+@pytest.mark.parametrize("shape", [(), (2, 3), (2, 1)])
+def test_slots_are_one_list(shape):
+    """A table of slots is refused: its first dimension alone would be taken for the number of tokens."""
+    n = shape[0] if shape else 1
+    slots, rows = torch.zeros(shape, dtype=torch.int64), torch.zeros(n, H, D, dtype=torch.bfloat16)
+    pools = (None, None, None, None, hora.DTYPE_BF16, 4, 16)
+    with pytest.raises(ValueError, match="slots"):
+        hora._kv_write(pools, H, D, rows, rows, slots, None)
+    with pytest.raises(ValueError, match="slots"):
+        hora._kv_read(pools, H, D, slots, rows, rows, None)
