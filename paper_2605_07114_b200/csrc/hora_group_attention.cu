@@ -31,7 +31,9 @@ attention_plan_kernel(const AttnArgs a) {
     // steps of the sequences that are narrow anyhow; of those that can be wide, as wide and as narrow ones
     enum { kNarrow, kWide, kEither, kSums };
     int64_t sum[kSums] = {0, 0, 0}, run[kSums], all[kSums];
-    int32_t kept[kPlanKept][2];                          // of this thread's first sequences: steps as wide ones (0: always narrow), as narrow ones
+    // of this thread's first sequences: steps as wide ones (0: always narrow), as narrow ones.  One sequence can have more than 2^31 of them
+    // (a million one-byte keys under 2100 rollouts with 32 cache heads).
+    int64_t kept[kPlanKept][2];
     const bool in_shared = a.N + 1 <= kPlanOffsets;
     if (in_shared)
         for (int32_t i = threadIdx.x; i <= a.N; i += kPlanThreads) s_off[i] = __ldcg(a.group_offsets + i);
@@ -47,12 +49,7 @@ attention_plan_kernel(const AttnArgs a) {
 #pragma unroll
     for (int x = 0; x < kPlanKept; ++x) {
         kept[x][0] = kept[x][1] = 0;
-        if (fits && lo + x < hi) {
-            int64_t w, n;
-            count(lo + x, w, n);
-            kept[x][0] = (int32_t)min(w, (int64_t)INT32_MAX);
-            kept[x][1] = (int32_t)min(n, (int64_t)INT32_MAX);
-        }
+        if (fits && lo + x < hi) count(lo + x, kept[x][0], kept[x][1]);
     }
     if (!fits)
         for (int64_t i = lo; i < hi; ++i) {

@@ -168,7 +168,11 @@ struct Pieces {
     __device__ __forceinline__ bool next(const AttnArgs &a, Piece &p, bool &bad) {
         if (u >= u_end) return false;
         while (s.wide != WIDE || u >= s_start + total_steps(a, s)) {        // on to the next sequence with steps on this line
-            if (!HORA_IN(i + 1, a.N + a.R)) return false;
+            if (i + 1 >= a.N + a.R) {                    // lengths that have changed since the plan: nothing beyond the last sequence is read
+                (void)HORA_IN(i + 1, a.N + a.R);
+                bad = true;
+                return false;
+            }
             if (s.wide == WIDE) s_start += total_steps(a, s);
             s = sequence(a, ++i, wide, bad);
         }
