@@ -18,9 +18,12 @@
 // The 16-byte chunks of a row lie at places exchanged by the row's number, and index n stands for key key_of(n), such that the eight
 // lanes of each phase of a load hit different banks, for keys and for values.
 //
-// An e4m3 cache is multiplied in fp16, which holds its codes exactly: a row's power-of-two scale is applied to its score, and to
-// its weight relative to the largest value scale met so far, so that weights stay within [0, 256]; queries are scaled by a power
-// of two to lie well within fp16's range.
+// An e4m3 cache is multiplied in fp16, which holds its codes exactly: a key row's power-of-two scale is applied to its score, and a value
+// row's goes into the exponent of its weight, 2^(s + e_v - m_o).  m_o is a reference of its own beside m, raised like it when an
+// exponent exceeds it by 2^8: the largest weight times scale among the keys a row sees is then near 1 however far apart the scales are, and
+// what fp16 cannot hold is 2^-24 and less of that.  A value row of zeros has the scale 1, which says nothing about it: where m_o is
+// to be raised, such rows are found in the stage and left out.  l stays relative to m, and o is brought to m when the partial is stored.
+// Queries are scaled by a power of two to lie well within fp16's range.
 //   Measured: 480 rollouts of 1024 keys on average, 4 cache heads of 128, bf16: 5.6 TB/s; 1920 of 768 keys, 2 cache heads of 128, e4m3: 170 us
 // for 0.86 GB, half of the issue slots (with queries as the left operand, padded to 16 rows, 223 us).
 #pragma once
@@ -252,10 +255,9 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
         const int32_t open = w.prompt ? s.len : s.len - a.T + 1;
 
         float o[kSteps][NT][4] = {};
-        float m[NT][2], l[NT][2];
+        float m[NT][2], l[NT][2], m_o[NT][2];                     // m_o: F8, what o is relative to
 #pragma unroll
-        for (int t = 0; t < NT; ++t) m[t][0] = m[t][1] = -INFINITY, l[t][0] = l[t][1] = 0.f;
-        float v_unit = 0.f;                                       // F8: o is in units of this (0: nothing added yet)
+        for (int t = 0; t < NT; ++t) m[t][0] = m[t][1] = m_o[t][0] = m_o[t][1] = -INFINITY, l[t][0] = l[t][1] = 0.f;
         for (int32_t step = step0; step < step1; ++step) {
             const int32_t key = step * kKeys;
             const int slot = (step - step0) % kStages;
@@ -291,17 +293,15 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
                 }
             }
             // scores in units of log2, hidden keys at -infinity
-            float ve[kSixteens][2], v_top = v_unit;
+            float ve[kSixteens][2] = {};                          // F8: the exponents of the value scales
 #pragma unroll
             for (int y = 0; y < kSixteens; ++y)
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
                     const int k = y * 16 + x * 8 + key_n;
                     const float f = F8 ? exponent_byte(lds1(at_ke + k)) : 1.f;
-                    if constexpr (F8) {
-                        ve[y][x] = key + k < s.len ? exponent_byte(lds1(at_ve + k)) : 0.f;
-                        v_top = fmaxf(v_top, ve[y][x]);
-                    }
+                    // the byte behind the bits of 2^23 is 2^23 + byte; beyond the length it may be any, and the score is -infinity
+                    if constexpr (F8) ve[y][x] = __uint_as_float(0x4B000000u | lds1(at_ve + k)) - (8388608.f + 127.f);
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -318,8 +318,14 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
             }
             // The reference of a row is raised when a score exceeds it by 2^8: weights up to 256 are as exact as weights up
             // to 1, and the output is hardly ever rescaled.
-            bool raise = F8 && v_top > v_unit;
+            bool raise = false;
             float top[NT][2];
+            auto top_with_scale = [&](int t, int e) {             // F8: the largest s + e_v of this lane's keys
+                float x = fmaxf(sc[0][t][e] + ve[0][0], sc[0][t][2 + e] + ve[0][1]);
+#pragma unroll
+                for (int y = 1; y < kSixteens; ++y) x = fmaxf(x, fmaxf(sc[y][t][e] + ve[y][0], sc[y][t][2 + e] + ve[y][1]));
+                return x;
+            };
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -328,13 +334,24 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
 #pragma unroll
                     for (int y = 1; y < kSixteens; ++y) top[t][e] = fmaxf(top[t][e], fmaxf(sc[y][t][e], sc[y][t][2 + e]));
                     raise |= top[t][e] > m[t][e] + 8.f;
+                    if constexpr (F8) raise |= top_with_scale(t, e) > m_o[t][e] + 8.f;
                 }
             if (__any_sync(kFull, raise)) {
-                float f_v = 1.f;
                 if constexpr (F8) {
-                    v_top = rows_max(v_top);                      // over all keys; powers of two, and at least one key is within the length
-                    f_v = v_unit / v_top;
-                    v_unit = v_top;
+                    // rows of zeros: a lane to each of the step's values (what was not fetched is any, and its score -infinity)
+                    static_assert(kKeys == kWarp, "a lane to each key");
+                    uint32_t bits = 0u;
+#pragma unroll
+                    for (int x = 0; x < St::kChunks; ++x) {
+                        const uint4 v = lds16(at_v + St::place(lane, x));
+                        bits |= v.x | v.y | v.z | v.w;
+                    }
+                    const unsigned zeros = __ballot_sync(kFull, (bits & 0x7F7F7F7Fu) == 0u);
+#pragma unroll
+                    for (int y = 0; y < kSixteens; ++y)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+                            if (zeros >> (y * 16 + x * 8 + key_n) & 1u) ve[y][x] = -INFINITY;
                 }
 #pragma unroll
                 for (int t = 0; t < NT; ++t)
@@ -343,19 +360,25 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
                         const float up = fmaxf(m[t][e], rows_max(top[t][e])), f = up == -INFINITY ? 0.f : exp2_fast(m[t][e] - up);
                         m[t][e] = up;
                         l[t][e] *= f;
+                        float f_o = f;
+                        if constexpr (F8) {
+                            const float up_o = fmaxf(m_o[t][e], rows_max(top_with_scale(t, e)));
+                            f_o = up_o == -INFINITY ? 0.f : exp2_fast(m_o[t][e] - up_o);
+                            m_o[t][e] = up_o;
+                        }
 #pragma unroll
                         for (int d = 0; d < kSteps; ++d) {
-                            o[d][t][e] *= f * f_v;
-                            o[d][t][2 + e] *= f * f_v;
+                            o[d][t][e] *= f_o;
+                            o[d][t][2 + e] *= f_o;
                         }
                     }
             }
-            const float v_inv = F8 ? 1.f / v_unit : 1.f;
             uint32_t p[kSixteens][NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 // where no key has been seen the reference is -infinity and every weight has to come out as 0
                 const float z0 = m[t][0] == -INFINITY ? 0.f : m[t][0], z1 = m[t][1] == -INFINITY ? 0.f : m[t][1];
+                const float y0 = m_o[t][0] == -INFINITY ? 0.f : m_o[t][0], y1 = m_o[t][1] == -INFINITY ? 0.f : m_o[t][1];
 #pragma unroll
                 for (int y = 0; y < kSixteens; ++y)
 #pragma unroll
@@ -364,9 +387,8 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
                         l[t][0] += w0;
                         l[t][1] += w1;
                         if constexpr (F8) {
-                            const float f = ve[y][x] * v_inv;
-                            w0 *= f;
-                            w1 *= f;
+                            w0 = exp2_fast(sc[y][t][2 * x] + ve[y][x] - y0);
+                            w1 = exp2_fast(sc[y][t][2 * x + 1] + ve[y][x] - y1);
                         }
                         p[y][t][x] = transposed(pack2(w0, w1, M()));
                     }
@@ -427,12 +449,20 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
         }
 
         // o[d][t] holds rows 2c, 2c + 1 of the t-th eight, each in dimensions n * kRun + 2d and the next one (by parts of 8 * kRun)
-        const float f = F8 ? v_unit : 1.f;
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const float sum = rows_sum(l[t][e]);
+                // F8: o from m_o to m, in two steps, since 2^(m_o - m) by itself can pass fp32's range
+                if constexpr (F8) {
+                    const float f = m_o[t][e] == -INFINITY ? 0.f : exp2_fast(0.5f * (m_o[t][e] - m[t][e]));
+#pragma unroll
+                    for (int d = 0; d < kSteps; ++d) {
+                        o[d][t][e] = o[d][t][e] * f * f;
+                        o[d][t][2 + e] = o[d][t][2 + e] * f * f;
+                    }
+                }
                 const int32_t x = t * 8 + 2 * c + e;
                 const int64_t out = query_row(a, s.first, s.rows, s.len, w.prompt, h, w.row0 + x).out;
                 if (out < 0) continue;
@@ -444,8 +474,8 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
 #pragma unroll
                     for (int d = 0; d < kRun / 2; d += 2)
                         *reinterpret_cast<float4 *>(po + part * 8 * kRun + n * kRun + 2 * d) =
-                            make_float4(o[part * (kRun / 2) + d][t][e] * f, o[part * (kRun / 2) + d][t][2 + e] * f, o[part * (kRun / 2) + d + 1][t][e] * f,
-                                        o[part * (kRun / 2) + d + 1][t][2 + e] * f);
+                            make_float4(o[part * (kRun / 2) + d][t][e], o[part * (kRun / 2) + d][t][2 + e], o[part * (kRun / 2) + d + 1][t][e],
+                                        o[part * (kRun / 2) + d + 1][t][2 + e]);
                 if (n == 0) *reinterpret_cast<float2 *>((step0 > 0 ? a.cont_ml[0] : a.main_ml) + place * 2) = make_float2(m[t][e], sum);
             }
     }
