@@ -438,6 +438,7 @@ hora_status_t hora_kv_read(const void *k_cache, const void *v_cache, const uint8
  * over the keys it sees; out = 0 and lse = -infinity where there are none, for slots t >= q_len[r], and for rollouts at
  * or beyond group_offsets[N].  Every prompt's cache is read once for its whole group, whatever the group's size.
  * Scores, maxima, sums and outputs are held in fp32; the weights are rounded to the 16-bit type of the product they enter.
+ * A key that a query does not see has the weight zero; a score beyond fp32's range makes its row NaN.
  * For an E4M3 cache that is fp16, and a weight enters times its value row's scale, relative to the largest such product among the keys the
  * query sees (rows of zeros aside): value rows of any scales next to each other are all right.
  *

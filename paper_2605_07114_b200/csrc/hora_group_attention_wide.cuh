@@ -15,7 +15,7 @@
 // among those is cleared in shared memory first (0 * NaN is not 0).
 //   What bounds it: the chain, where both halves have rows of their own (2.3 us a step of 256 rows and 128 keys of D = 128, 825 TFLOP/s
 // over 103485 keys and 512 rows; with an eighth of the bytes a step takes as long); HBM for items of one half (1.6 us a step of
-// 64 KiB, 0.93 of the copy rate).  A quarter of the exponentials by products: 393 us in place of 402 for 1024 queries of 64 heads.
+// 64 KiB, 0.93 of the copy rate).  A quarter of the exponentials by products: 384 us in place of 392 for 1024 queries of 64 heads.
 //   Every wait has a limit; a wait that reaches it makes the CTA give up and report HORA_ERR_INTERNAL.
 #pragma once
 
@@ -191,13 +191,24 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(two(a)), "l"(two(b)));
     return two(d);
 }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+    uint64_t d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(two(a)), "l"(two(b)));
+    return two(d);
+}
+__device__ __forceinline__ float max_or_nan(float a, float b) {
+    float y;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+    return y;
+}
 
 // 2^x by multiplications, for x <= 8: the special function unit takes 8 cycles a warp, as long as the tensor cores need for its
 // share of the products, so a quarter of the exponentials is computed beside it.  2^x = 2^n 2^f, n = round(x), |f| <= 1/2;
 // 2^f by the polynomial of degree 5 with the least largest relative error (7.5e-8, 2.0e-7 with fp32 rounding; fitted by iterated
-// weighted least squares), n added to its exponent.  Below 2^-126 the result is 2^-126 in place of less.
+// weighted least squares), times 2^n, whose exponent comes from the low bits of the rounding.  Below 2^-126.5, for the -infinity of a hidden
+// key too, 2^n is 0 and so is the result, as the special function unit has it; NaN stays NaN.
 __device__ __forceinline__ float2 exp2_by_products(float2 x) {
-    x = make_float2(fmaxf(x.x, -126.f), fmaxf(x.y, -126.f));
+    x = make_float2(max_or_nan(x.x, -127.f), max_or_nan(x.y, -127.f));
     const float2 big = make_float2(12582912.f, 12582912.f), t = add2(x, big);      // 1.5 * 2^23: the low bits of t are n
     const float2 f = fma2(add2(t, make_float2(-12582912.f, -12582912.f)), make_float2(-1.f, -1.f), x);
     float2 p = make_float2(1.3276471519402e-3f, 1.3276471519402e-3f);
@@ -206,8 +217,7 @@ __device__ __forceinline__ float2 exp2_by_products(float2 x) {
     p = fma2(p, f, make_float2(2.4022119723934e-1f, 2.4022119723934e-1f));
     p = fma2(p, f, make_float2(6.9314696706386e-1f, 6.9314696706386e-1f));
     p = fma2(p, f, make_float2(1.0000000716547f, 1.0000000716547f));
-    return make_float2(__uint_as_float(__float_as_uint(p.x) + (__float_as_uint(t.x) << 23)),
-                       __uint_as_float(__float_as_uint(p.y) + (__float_as_uint(t.y) << 23)));
+    return mul2(p, make_float2(__uint_as_float((__float_as_uint(t.x) << 23) + 0x3F800000u), __uint_as_float((__float_as_uint(t.y) << 23) + 0x3F800000u)));
 }
 
 // O of a warp's rows, times f; few columns at a time, since the scores are in registers meanwhile.
