@@ -47,11 +47,11 @@ constexpr size_t kAdvSmem = sizeof(AdvWarpSmem) * kAdvWarps;
 __device__ __forceinline__ int64_t shfl_i64(int64_t v, int src) { return __shfl_sync(kFull, v, src); }
 
 // One group streamed from global memory by the whole warp (groups longer than a batch).
-__device__ void advantage_streamed(const float *__restrict__ rewards, int64_t s, int64_t e, int32_t mode, double eps,
+__device__ void advantage_streamed(const float *rewards, int64_t s, int64_t e, int32_t mode, double eps,
                                    int32_t ddof, float *__restrict__ adv, int lane) {
     double mean, scale;
     group_mean_scale(rewards, s, e, mode, eps, ddof, lane, mean, scale);
-    for (int64_t j = s + lane; j < e; j += kWarp) adv[j] = (float)(((double)__ldg(rewards + j) - mean) * scale);
+    for (int64_t j = s + lane; j < e; j += kWarp) adv[j] = (float)(((double)__ldca(rewards + j) - mean) * scale);
 }
 
 // exclusive running count over words of popc(word[c]); words beyond n_words count as empty
@@ -140,7 +140,7 @@ __device__ __forceinline__ void general_batch(float *buf, int done, int last, in
 // the 4-element boundary at or below its first element.
 template <bool VEC4>
 __global__ void __launch_bounds__(kAdvWarps *kWarp, 3)
-group_advantage_kernel(const float *__restrict__ rewards, const int64_t *__restrict__ off, int64_t N, int32_t mode,
+group_advantage_kernel(const float *rewards, const int64_t *off, int64_t N, int32_t mode,
                        double eps, int32_t ddof, float *__restrict__ adv, int32_t *status_dev) {
     pdl_enter();
     extern __shared__ __align__(16) unsigned char s_raw[];
@@ -150,14 +150,14 @@ group_advantage_kernel(const float *__restrict__ rewards, const int64_t *__restr
     const int64_t warp0 = (int64_t)blockIdx.x * kAdvWarps + (threadIdx.x >> 5);
     const int64_t stride = (int64_t)gridDim.x * kAdvWarps;
     const int64_t n_blocks = (N + kWarp - 1) / kWarp;
-    const int64_t n_all = __ldg(off + N);                     // nothing is read at or beyond this element
+    const int64_t n_all = __ldca(off + N);                     // nothing is read at or beyond this element
     // a lane's two offsets of the warp's NEXT 32 groups are fetched while the current ones are worked on
     auto fetch_offsets = [&](int64_t blk, int64_t &s, int64_t &e) {
         s = e = 0;
         const int64_t g = blk * kWarp + lane;
         if (blk < n_blocks && g < N) {
-            s = __ldg(off + g);
-            e = __ldg(off + g + 1);
+            s = __ldca(off + g);
+            e = __ldca(off + g + 1);
         }
     };
     int64_t nxt_s, nxt_e;
@@ -205,7 +205,7 @@ group_advantage_kernel(const float *__restrict__ rewards, const int64_t *__restr
                 cp_async_wait_all();
             } else {
                 for (int j = lane; j < 128 * n_rows; j += kWarp)
-                    HORA_AT(sm.buf, j, kSlab) = (j < span && start + j < n_all) ? __ldg(&HORA_AT(rewards, start + j, n_all)) : 0.0f;
+                    HORA_AT(sm.buf, j, kSlab) = (j < span && start + j < n_all) ? __ldca(&HORA_AT(rewards, start + j, n_all)) : 0.0f;
             }
             __syncwarp();
             // ---- which rewards are 1.0 (packed prefix words); is anything neither 0.0 nor 1.0? ----

@@ -18,8 +18,8 @@ namespace hora {
 
 template <bool VEC4, bool WEIGHT>
 __global__ void __launch_bounds__(kBcThreads)
-advantage_tokens_kernel(const float *__restrict__ rewards, const int64_t *__restrict__ goff, int64_t N,
-                        const int64_t *__restrict__ off, int64_t R, int64_t T, int64_t chunk, int32_t mode, double eps,
+advantage_tokens_kernel(const float *rewards, const int64_t *goff, int64_t N,
+                        const int64_t *off, int64_t R, int64_t T, int64_t chunk, int32_t mode, double eps,
                         int32_t ddof, int32_t weight_mode, double length_const, float *__restrict__ out,
                         float *__restrict__ out_w, int32_t *status_dev) {
     pdl_enter();
@@ -28,7 +28,7 @@ advantage_tokens_kernel(const float *__restrict__ rewards, const int64_t *__rest
     __shared__ float s_w[WEIGHT ? kStage : 1];
     __shared__ unsigned long long s_bounds[2];
     __shared__ int s_need;
-    const int64_t t_all = __ldg(off + R);
+    const int64_t t_all = __ldca(off + R);
     if (t_all < T) T = t_all;
     const int64_t c0 = (int64_t)blockIdx.x * chunk;
     if (c0 >= T) return;
@@ -42,7 +42,7 @@ advantage_tokens_kernel(const float *__restrict__ rewards, const int64_t *__rest
         __syncthreads();
         if (threadIdx.x == 0) s_need = 0;
         for (int j = threadIdx.x; j <= n_stage; j += kBcThreads) {
-            const int64_t d = __ldg(off + r_base + j) - c0;
+            const int64_t d = __ldca(off + r_base + j) - c0;
             s_rel[j] = d < 0 ? -1 : (d > len ? len : (int32_t)d);
         }
         __syncthreads();
@@ -61,7 +61,7 @@ advantage_tokens_kernel(const float *__restrict__ rewards, const int64_t *__rest
         }
         __syncthreads();
         for (int64_t g = g_first + warp; g < N; g += kBcWarps) {
-            const int64_t s = __ldg(goff + g), e = __ldg(goff + g + 1);
+            const int64_t s = __ldca(goff + g), e = __ldca(goff + g + 1);
             if (s >= r_end) break;
             if (e < s || s < 0) { raise_status(status_dev, HORA_ERR_INVALID_VALUE); continue; }
             if (e == s || e <= r_base) continue;
@@ -69,10 +69,10 @@ advantage_tokens_kernel(const float *__restrict__ rewards, const int64_t *__rest
             group_mean_scale(rewards, s, e, mode, eps, ddof, lane, mean, scale);
             const int64_t j0 = s > r_base ? s : r_base, j1 = e < r_end ? e : r_end;
             for (int64_t j = j0 + lane; j < j1; j += kWarp) {
-                s_adv[j - r_base] = (float)(((double)__ldg(rewards + j) - mean) * scale);
+                s_adv[j - r_base] = (float)(((double)__ldca(rewards + j) - mean) * scale);
                 if (WEIGHT) {
                     double denom = (double)(e - s) * length_const;
-                    if (weight_mode == HORA_WEIGHT_PER_TOKEN) denom = (double)(e - s) * (double)(__ldg(off + j + 1) - __ldg(off + j));
+                    if (weight_mode == HORA_WEIGHT_PER_TOKEN) denom = (double)(e - s) * (double)(__ldca(off + j + 1) - __ldca(off + j));
                     s_w[j - r_base] = denom > 0.0 ? (float)(1.0 / denom) : 0.0f;
                 }
             }

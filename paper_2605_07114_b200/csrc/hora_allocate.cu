@@ -227,8 +227,8 @@ __device__ void place_window(AllocHeader *hdr, const unsigned long long *hist, i
 // scales the rank B to the sample and places the two-bin window around the bin it falls in: towards the
 // upper neighbour when the rank falls in the upper half of that bin's count, else towards the lower one.
 __global__ void __launch_bounds__(kSelThreads)
-select_estimate(const int32_t *__restrict__ cap, int32_t cap_scalar, int64_t N, int32_t ld, int64_t every,
-                const double *__restrict__ gains, int64_t B, AllocHeader *hdr, unsigned long long *hist) {
+select_estimate(const int32_t *cap, int32_t cap_scalar, int64_t N, int32_t ld, int64_t every,
+                const double *gains, int64_t B, AllocHeader *hdr, unsigned long long *hist) {
     pdl_enter();
     __shared__ unsigned int s_hist[kBins];
     __shared__ long long s_warp[kSelThreads / kWarp];
@@ -241,7 +241,7 @@ select_estimate(const int32_t *__restrict__ cap, int32_t cap_scalar, int64_t N, 
     long long capsum = 0;
     for (int64_t sidx = warp0; sidx < n_sample; sidx += stride) {
         const int64_t row = sidx * every;
-        int32_t capi = cap ? __ldg(cap + row) : cap_scalar;
+        int32_t capi = cap ? __ldca(cap + row) : cap_scalar;
         capi = capi < 0 ? 0 : (capi > ld ? ld : capi);
         if (lane == 0) capsum += capi;
         const unsigned long long *keys = reinterpret_cast<const unsigned long long *>(gains) + row * (int64_t)ld;
@@ -250,7 +250,7 @@ select_estimate(const int32_t *__restrict__ cap, int32_t cap_scalar, int64_t N, 
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const int32_t j = k0 + u * kWarp + lane;
-                key[u] = j < capi ? __ldg(keys + j) : 0ull;
+                key[u] = j < capi ? __ldca(keys + j) : 0ull;
             }
 #pragma unroll
             for (int u = 0; u < 8; ++u)
@@ -397,20 +397,20 @@ struct Level0Item {
 };
 
 template <int E, bool VEC2, bool ONE>
-__device__ __forceinline__ void level0_fetch(Level0Item<E> &it, const int32_t *__restrict__ cap, int32_t cap_scalar,
+__device__ __forceinline__ void level0_fetch(Level0Item<E> &it, const int32_t *cap, int32_t cap_scalar,
                                              int64_t n_items, int32_t items_per_row, int32_t ld,
-                                             const double *__restrict__ gains, int64_t item, int lane, bool *bad) {
+                                             const double *gains, int64_t item, int lane, bool *bad) {
     it.capi = -1;
     if (item >= n_items) return;
     const int64_t row = ONE ? item : item / items_per_row;     // ONE: an item is a whole row (no 64-bit division)
     const int32_t k0 = ONE ? 0 : (int32_t)(item - row * items_per_row) * (kWarp * E);
-    int32_t capi = cap ? __ldg(cap + row) : cap_scalar;
+    int32_t capi = cap ? __ldca(cap + row) : cap_scalar;
     if (capi < 0 || capi > ld) { *bad = true; capi = 0; }
     it.capi = capi;
     const unsigned long long *keys = reinterpret_cast<const unsigned long long *>(gains) + row * (int64_t)ld + k0 + 2 * lane;
     if (VEC2 && k0 + kWarp * E <= capi) {                      // the whole item lies below the cap: plain loads
 #pragma unroll
-        for (int p = 0; p < E / 2; ++p) it.v[p] = __ldg(reinterpret_cast<const ulonglong2 *>(keys) + 32 * p);
+        for (int p = 0; p < E / 2; ++p) it.v[p] = __ldca(reinterpret_cast<const ulonglong2 *>(keys) + 32 * p);
     } else {                                                   // ragged: keys past the cap read as 0
 #pragma unroll
         for (int p = 0; p < E / 2; ++p) {
@@ -418,17 +418,17 @@ __device__ __forceinline__ void level0_fetch(Level0Item<E> &it, const int32_t *_
             it.v[p] = make_ulonglong2(0ull, 0ull);
             if (VEC2) {
                 if (k < capi) {
-                    it.v[p] = __ldg(reinterpret_cast<const ulonglong2 *>(keys) + 32 * p);
+                    it.v[p] = __ldca(reinterpret_cast<const ulonglong2 *>(keys) + 32 * p);
                     if (k + 1 >= capi) it.v[p].y = 0ull;
                 }
             } else {
-                if (k < capi) it.v[p].x = __ldg(keys + 64 * p);
-                if (k + 1 < capi) it.v[p].y = __ldg(keys + 64 * p + 1);
+                if (k < capi) it.v[p].x = __ldca(keys + 64 * p);
+                if (k + 1 < capi) it.v[p].y = __ldca(keys + 64 * p + 1);
             }
         }
     }
     it.before = kKeyInf - 1;
-    if (lane == 0 && k0 > 0 && k0 < capi) it.before = __ldg(keys - 1);
+    if (lane == 0 && k0 > 0 && k0 < capi) it.before = __ldca(keys - 1);
 }
 
 // Exact order check of an item, on the values: !(next <= prev) also catches a NaN on either side.  Keys past the
@@ -539,8 +539,8 @@ constexpr int level0_per_sm() { return E == 8 ? 3 : 5; }
 
 template <int E, bool VEC2, bool ONE>
 __global__ void __launch_bounds__(kSelThreads, level0_per_sm<E>())
-select_level0(const int32_t *__restrict__ cap, int32_t cap_scalar, int64_t N, int32_t ld,
-              const double *__restrict__ gains, int64_t B, AllocHeader *hdr, unsigned long long *hist_fine,
+select_level0(const int32_t *cap, int32_t cap_scalar, int64_t N, int32_t ld,
+              const double *gains, int64_t B, AllocHeader *hdr, unsigned long long *hist_fine,
               unsigned int *__restrict__ pguess) {
     pdl_enter();
     __shared__ unsigned int s_fine[kFineBins];             // the window's 23-bit bins
@@ -605,7 +605,7 @@ __device__ __forceinline__ int32_t level0_short_cap(const Level0ShortPass &ps, i
     const int32_t row = item * (kWarp / LG) + lane / LG;
     const bool there = row < ps.N;                             // (an item past the end has no row that is)
     int32_t capi = ps.cap_scalar;
-    if (ps.cap != nullptr) capi = __ldg(ps.cap + (there ? row : 0));
+    if (ps.cap != nullptr) capi = __ldca(ps.cap + (there ? row : 0));
     const bool ok = (unsigned)capi <= (unsigned)ps.ld;
     *bad |= (unsigned)(there && !ok);
     capi = there && ok ? capi : 0;
@@ -623,12 +623,12 @@ __device__ __forceinline__ void level0_short_fetch(Level0Short<LG> &it, const Le
 #pragma unroll
     for (int j = 0; j < 8; j += 2) {
         if (VEC2) {
-            const ulonglong2 t = __ldg(reinterpret_cast<const ulonglong2 *>(j < nvalid ? keys + j : g_zero_chunk));
+            const ulonglong2 t = __ldca(reinterpret_cast<const ulonglong2 *>(j < nvalid ? keys + j : g_zero_chunk));
             it.key[j] = t.x;
             it.key[j + 1] = j + 1 < nvalid ? t.y : 0ull;
         } else {
-            it.key[j] = __ldg(j < nvalid ? keys + j : g_zero_chunk);
-            it.key[j + 1] = __ldg(j + 1 < nvalid ? keys + j + 1 : g_zero_chunk);
+            it.key[j] = __ldca(j < nvalid ? keys + j : g_zero_chunk);
+            it.key[j + 1] = __ldca(j + 1 < nvalid ? keys + j + 1 : g_zero_chunk);
         }
     }
 }
@@ -666,8 +666,8 @@ __device__ __forceinline__ void level0_short_process(const Level0Short<LG> &it, 
 
 template <int LG, bool VEC2>
 __global__ void __launch_bounds__(kSelThreads, 3)
-select_level0_short(const int32_t *__restrict__ cap, int32_t cap_scalar, int64_t N, int32_t ld,
-                    const double *__restrict__ gains, int64_t B, AllocHeader *hdr, unsigned long long *hist_fine,
+select_level0_short(const int32_t *cap, int32_t cap_scalar, int64_t N, int32_t ld,
+                    const double *gains, int64_t B, AllocHeader *hdr, unsigned long long *hist_fine,
                     unsigned int *__restrict__ pguess) {
     pdl_enter();
     __shared__ unsigned int s_fine[kFineBins];
@@ -711,8 +711,8 @@ select_level0_short(const int32_t *__restrict__ cap, int32_t cap_scalar, int64_t
 // bits; the last CTA selects that digit and the selection goes on from there.  (The counts above the guess
 // that level 0 stored mean little then; level 1 falls back to searching the rows.)
 __global__ void __launch_bounds__(kSelThreads)
-select_level0_full(const int32_t *__restrict__ cap, int32_t cap_scalar, int64_t N, int32_t ld,
-                   const double *__restrict__ gains, AllocHeader *hdr, unsigned long long *hist) {
+select_level0_full(const int32_t *cap, int32_t cap_scalar, int64_t N, int32_t ld,
+                   const double *gains, AllocHeader *hdr, unsigned long long *hist) {
     pdl_enter();
     __shared__ unsigned int s_hist[kBins];
     __shared__ long long s_warp[kSelThreads / kWarp];
@@ -722,7 +722,7 @@ select_level0_full(const int32_t *__restrict__ cap, int32_t cap_scalar, int64_t 
     const int lane = lane_id();
     const int64_t stride = (int64_t)gridDim.x * (kSelThreads / kWarp);
     for (int64_t row = (int64_t)blockIdx.x * (kSelThreads / kWarp) + (threadIdx.x >> 5); row < N; row += stride) {
-        int32_t capi = cap ? __ldg(cap + row) : cap_scalar;
+        int32_t capi = cap ? __ldca(cap + row) : cap_scalar;
         capi = capi < 0 ? 0 : (capi > ld ? ld : capi);
         const unsigned long long *keys = reinterpret_cast<const unsigned long long *>(gains) + row * (int64_t)ld;
         for (int32_t k0 = 0; k0 < capi; k0 += 8 * kWarp) {      // eight coalesced loads in flight per lane
@@ -730,7 +730,7 @@ select_level0_full(const int32_t *__restrict__ cap, int32_t cap_scalar, int64_t 
 #pragma unroll
             for (int u = 0; u < 8; ++u) {
                 const int32_t j = k0 + u * kWarp + lane;
-                key[u] = j < capi ? __ldg(keys + j) : 0ull;
+                key[u] = j < capi ? __ldca(keys + j) : 0ull;
             }
 #pragma unroll
             for (int u = 0; u < 8; ++u)
@@ -812,8 +812,8 @@ struct Level0Tap {
 // Estimate for the fused pass: the sampled rows are computed, not read.
 template <int E>
 __global__ void __launch_bounds__(kSelThreads)
-select_estimate_fused(const double *__restrict__ alpha, const double *__restrict__ beta, double alpha0, double beta0,
-                      const int32_t *__restrict__ c, int32_t G0, const int32_t *__restrict__ cap, int32_t cap_scalar,
+select_estimate_fused(const double *alpha, const double *beta, double alpha0, double beta0,
+                      const int32_t *c, int32_t G0, const int32_t *cap, int32_t cap_scalar,
                       int64_t N, int32_t ld, int64_t every, int64_t B, AllocHeader *hdr, unsigned long long *hist) {
     pdl_enter();
     __shared__ unsigned int s_hist[kBins];
@@ -848,8 +848,8 @@ select_estimate_fused(const double *__restrict__ alpha, const double *__restrict
 // validated (the row loop raises the status for invalid priors, counts or caps).
 template <int E, bool VEC2, int LG>
 __global__ void __launch_bounds__(kSelThreads, 3)
-gains_level0_fused(const double *__restrict__ alpha, const double *__restrict__ beta, double alpha0, double beta0,
-                   const int32_t *__restrict__ c, int32_t G0, const int32_t *__restrict__ cap, int32_t cap_scalar,
+gains_level0_fused(const double *alpha, const double *beta, double alpha0, double beta0,
+                   const int32_t *c, int32_t G0, const int32_t *cap, int32_t cap_scalar,
                    int64_t N, int32_t ld, double *__restrict__ gains, int64_t B, AllocHeader *hdr,
                    unsigned long long *hist_fine, unsigned int *__restrict__ pguess) {
     pdl_enter();
@@ -889,11 +889,11 @@ __device__ __forceinline__ unsigned key_prefix(unsigned long long key, int r) { 
 
 // first index in [0, n) whose prefix is <= P (STRICT false) or < P (STRICT true); n if none
 template <bool STRICT>
-__device__ __forceinline__ int32_t first_not_above(const unsigned long long *__restrict__ keys, int32_t n, unsigned P, int r) {
+__device__ __forceinline__ int32_t first_not_above(const unsigned long long *keys, int32_t n, unsigned P, int r) {
     int32_t lo = 0, hi = n;
     while (lo < hi) {
         const int32_t mid = (lo + hi) >> 1;
-        const unsigned kp = key_prefix(__ldg(&HORA_AT(keys, mid, n)), r);
+        const unsigned kp = key_prefix(__ldca(&HORA_AT(keys, mid, n)), r);
         if (STRICT ? kp >= P : kp > P) lo = mid + 1; else hi = mid;
     }
     return lo;
@@ -901,10 +901,10 @@ __device__ __forceinline__ int32_t first_not_above(const unsigned long long *__r
 
 template <bool VEC2>
 __global__ void __launch_bounds__(kSelThreads, kLevel1PerSm)
-select_level1(const double *__restrict__ alpha, const double *__restrict__ beta, double alpha0, double beta0,
-              const int32_t *__restrict__ c, int32_t G0, const int32_t *__restrict__ cap, int32_t cap_scalar, int64_t N,
-              int32_t ld, const double *__restrict__ gains, AllocHeader *hdr, unsigned long long *hist1,
-              const unsigned int *__restrict__ pguess, int2 *__restrict__ rowstate,
+select_level1(const double *alpha, const double *beta, double alpha0, double beta0,
+              const int32_t *c, int32_t G0, const int32_t *cap, int32_t cap_scalar, int64_t N,
+              int32_t ld, const double *gains, AllocHeader *hdr, unsigned long long *hist1,
+              const unsigned int *pguess, int2 *__restrict__ rowstate,
               int32_t *__restrict__ active, unsigned long long *__restrict__ cand_key,
               int32_t *__restrict__ cand_row, long long *bsum_hi, double *__restrict__ objrow) {
     pdl_enter();
@@ -937,10 +937,10 @@ select_level1(const double *__restrict__ alpha, const double *__restrict__ beta,
         RowInputs in;
         in.al = alpha0; in.be = beta0; in.ci = 0; in.capi = cap_scalar; in.guess = 0;
         if (row < N) {
-            in.guess = __ldg(pguess + row);
-            if (alpha) { in.al = __ldg(alpha + row); in.be = __ldg(beta + row); }
-            in.ci = __ldg(c + row);
-            if (cap) in.capi = __ldg(cap + row);
+            in.guess = __ldca(pguess + row);
+            if (alpha) { in.al = __ldca(alpha + row); in.be = __ldca(beta + row); }
+            in.ci = __ldca(c + row);
+            if (cap) in.capi = __ldca(cap + row);
         }
         return in;
     };
@@ -972,13 +972,13 @@ select_level1(const double *__restrict__ alpha, const double *__restrict__ beta,
 #pragma unroll
                     for (int u = 0; u < 8; u += 2) {
                         ulonglong2 t = make_ulonglong2(0ull, 0ull);
-                        if (ws + u < we) t = __ldg(reinterpret_cast<const ulonglong2 *>(&HORA_AT(keys, ws + u, ld - 1)));
+                        if (ws + u < we) t = __ldca(reinterpret_cast<const ulonglong2 *>(&HORA_AT(keys, ws + u, ld - 1)));
                         kp[u] = key_prefix(t.x, r);
                         kp[u + 1] = key_prefix(t.y, r);
                     }
                 } else {
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) kp[u] = ws + u < we ? key_prefix(__ldg(&HORA_AT(keys, ws + u, ld)), r) : 0u;
+                    for (int u = 0; u < 8; ++u) kp[u] = ws + u < we ? key_prefix(__ldca(&HORA_AT(keys, ws + u, ld)), r) : 0u;
                 }
                 kp_first = kp[0];
 #pragma unroll
@@ -997,7 +997,7 @@ select_level1(const double *__restrict__ alpha, const double *__restrict__ beta,
                 if (!left_ok) {                                  // the 8 keys before (independent loads)
                     unsigned kp[8];
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) kp[u] = ws - 1 - u >= 0 ? key_prefix(__ldg(&HORA_AT(keys, ws - 1 - u, ld)), r) : 0u;
+                    for (int u = 0; u < 8; ++u) kp[u] = ws - 1 - u >= 0 ? key_prefix(__ldca(&HORA_AT(keys, ws - 1 - u, ld)), r) : 0u;
 #pragma unroll
                     for (int u = 0; u < 8; ++u) {
                         if (ws - 1 - u >= 0) {
@@ -1012,7 +1012,7 @@ select_level1(const double *__restrict__ alpha, const double *__restrict__ beta,
                 if (!right_ok) {                                 // the 8 keys after
                     unsigned kp[8];
 #pragma unroll
-                    for (int u = 0; u < 8; ++u) kp[u] = we + u < capi ? key_prefix(__ldg(&HORA_AT(keys, we + u, ld)), r) : 0u;
+                    for (int u = 0; u < 8; ++u) kp[u] = we + u < capi ? key_prefix(__ldca(&HORA_AT(keys, we + u, ld)), r) : 0u;
 #pragma unroll
                     for (int u = 0; u < 8; ++u) {
                         if (we + u < capi) {
@@ -1036,7 +1036,7 @@ select_level1(const double *__restrict__ alpha, const double *__restrict__ beta,
                 // no key in the threshold's bin: Delta_i = p_hi is final, and g_i(Delta_i) was just read (L1)
                 double u = -1.0;                                 // otherwise: evaluated by the output pass
                 if (n_eq == 0)
-                    u = p_hi > 0 ? utility_from_gain(__longlong_as_double((long long)__ldg(&HORA_AT(keys, p_hi - 1, ld))), post.a, post.b, p_hi)
+                    u = p_hi > 0 ? utility_from_gain(__longlong_as_double((long long)__ldca(&HORA_AT(keys, p_hi - 1, ld))), post.a, post.b, p_hi)
                                  : 0.0;
                 objrow[row] = u;
             }
@@ -1047,7 +1047,7 @@ select_level1(const double *__restrict__ alpha, const double *__restrict__ beta,
                 // none differs, the threshold is known.  (Letting the lanes that meet in a bin send one update
                 // between them made the pass slower.)
                 for (int32_t j = 0; j < n_eq; ++j) {
-                    const unsigned long long key = __ldg(&HORA_AT(keys, p_hi + j, ld));
+                    const unsigned long long key = __ldca(&HORA_AT(keys, p_hi + j, ld));
                     unsigned long long ref = *(volatile unsigned long long *)&s_ref;
                     if (ref == 0ull) {                           // the CTA's first key becomes its reference ...
                         ref = atomicCAS(&s_ref, 0ull, key);
@@ -1082,7 +1082,7 @@ select_level1(const double *__restrict__ alpha, const double *__restrict__ beta,
                 slot0 = __shfl_sync(kFull, slot0, 0);
                 const long long slot = (long long)slot0 + (inc - n_eq);
                 for (int32_t j = 0; j < n_eq; ++j) {
-                    const unsigned long long key = __ldg(&HORA_AT(keys, p_hi + j, ld));
+                    const unsigned long long key = __ldca(&HORA_AT(keys, p_hi + j, ld));
                     if (slot + j < kListCap) {
                         HORA_AT(cand_key, slot + j, kListCap) = key;
                         HORA_AT(cand_row, slot + j, kListCap) = (int32_t)row;
@@ -1114,11 +1114,11 @@ select_level1(const double *__restrict__ alpha, const double *__restrict__ beta,
 // the output pass, the exclusive prefixes of (#keys > lambda, #keys == lambda) over blocks of 1024 prompts.
 
 // Close a row's segment with the finished threshold: keys above it, keys equal to it.
-__device__ __forceinline__ int2 close_segment(const unsigned long long *__restrict__ keys, int2 st, unsigned long long lam,
+__device__ __forceinline__ int2 close_segment(const unsigned long long *keys, int2 st, unsigned long long lam,
                                               int32_t ld) {
     int32_t n_gt = 0, n_eq = 0;
     for (int32_t pp = st.x; pp < st.y; ++pp) {
-        const unsigned long long key = __ldg(&HORA_AT(keys, pp, ld));
+        const unsigned long long key = __ldca(&HORA_AT(keys, pp, ld));
         if (key > lam) ++n_gt;
         else if (key == lam) ++n_eq;
         else break;
@@ -1131,7 +1131,7 @@ __device__ __forceinline__ int2 close_segment(const unsigned long long *__restri
 // digits are found 13 bits per sweep.  Should more than kListSmall keys share that digit (ties), the sweeps
 // run over the list in global memory instead.  Then the block sums are corrected and scanned.
 __device__ void tail_list(int64_t B, AllocHeader *hdr, const unsigned long long *hist1,
-                          const unsigned long long *__restrict__ cand_key, const int32_t *__restrict__ cand_row,
+                          const unsigned long long *cand_key, const int32_t *cand_row,
                           long long *bsum_hi, long long *bsum_t, int64_t NB, unsigned int *s_hist,
                           unsigned long long *s_keys, long long *s_warp) {
     __shared__ long long s_pick[3];                              // digit, count above it, count of it
@@ -1297,9 +1297,9 @@ __device__ void tail_list(int64_t B, AllocHeader *hdr, const unsigned long long 
 // one level up; the keys that remain are histogrammed on the next digit, which CTA 0 selects between two
 // grid-wide barriers), then every segment is closed with the finished threshold, the block sums formed and
 // scanned.  The active list is in no particular order; nothing here depends on it.
-__device__ void tail_digits(int64_t N, int32_t ld, const double *__restrict__ gains, int64_t B, AllocHeader *hdr,
+__device__ void tail_digits(int64_t N, int32_t ld, const double *gains, int64_t B, AllocHeader *hdr,
                             unsigned long long *hist_all, int2 *__restrict__ rowstate,
-                            const int32_t *__restrict__ active, long long *bsum_hi, long long *bsum_t, int64_t NB,
+                            const int32_t *active, long long *bsum_hi, long long *bsum_t, int64_t NB,
                             unsigned int *s_hist, long long *s_warp) {
     cooperative_groups::grid_group grid = cooperative_groups::this_grid();
     const unsigned int n_active = hdr->n_active;
@@ -1334,7 +1334,7 @@ __device__ void tail_digits(int64_t N, int32_t ld, const double *__restrict__ ga
             const int32_t p_hi = st.x, p_end = st.y;
             int32_t p = p_hi, new_hi = p_hi;
             while (p < p_end) {
-                const unsigned long long key = __ldg(&HORA_AT(keys, p, ld));
+                const unsigned long long key = __ldca(&HORA_AT(keys, p, ld));
                 const unsigned long long dp = (key >> shift_prev) & mask_prev;
                 if (dp > d_prev) {
                     new_hi = p + 1;
@@ -1393,10 +1393,10 @@ __device__ void tail_digits(int64_t N, int32_t ld, const double *__restrict__ ga
 }
 
 __global__ void __launch_bounds__(kSelThreads, kTailPerSm)
-select_tail(int64_t N, int32_t ld, const double *__restrict__ gains, int64_t B, AllocHeader *hdr,
-            unsigned long long *hist_all, int2 *__restrict__ rowstate, const int32_t *__restrict__ active,
-            long long *bsum_hi, long long *bsum_t, int64_t NB, const unsigned long long *__restrict__ cand_key,
-            const int32_t *__restrict__ cand_row) {
+select_tail(int64_t N, int32_t ld, const double *gains, int64_t B, AllocHeader *hdr,
+            unsigned long long *hist_all, int2 *__restrict__ rowstate, const int32_t *active,
+            long long *bsum_hi, long long *bsum_t, int64_t NB, const unsigned long long *cand_key,
+            const int32_t *cand_row) {
     pdl_enter();
     __shared__ unsigned int s_hist[kBins];
     __shared__ unsigned long long s_keys[kListSmall];
@@ -1419,9 +1419,9 @@ __device__ __forceinline__ unsigned long long pack_type(unsigned long long a, un
 // Exact mode, step 1: per row, find the (at most one) candidate inside the band around the fp64
 // threshold, register its type, and store the provisional state (everything above the band is taken).
 __global__ void __launch_bounds__(kSelThreads)
-exact_collect(const double *__restrict__ alpha, const double *__restrict__ beta, double alpha0, double beta0,
-              const int32_t *__restrict__ c, int32_t G0, const int32_t *__restrict__ cap, int32_t cap_scalar,
-              int64_t N, int32_t ld, const double *__restrict__ gains, AllocHeader *hdr, int2 *__restrict__ rowstate,
+exact_collect(const double *alpha, const double *beta, double alpha0, double beta0,
+              const int32_t *c, int32_t G0, const int32_t *cap, int32_t cap_scalar,
+              int64_t N, int32_t ld, const double *gains, AllocHeader *hdr, int2 *__restrict__ rowstate,
               int32_t *__restrict__ rowslot, unsigned long long *tkeys, unsigned long long *tcounts,
               double *__restrict__ objrow) {
     pdl_enter();
@@ -1449,9 +1449,9 @@ exact_collect(const double *__restrict__ alpha, const double *__restrict__ beta,
         unsigned long long tkey = 0;
         int32_t q = 0;
         if (row < N) {
-            const double al = alpha ? __ldg(alpha + row) : alpha0, be = beta ? __ldg(beta + row) : beta0;
-            const int32_t ci = __ldg(c + row);
-            const int32_t capi = cap ? __ldg(cap + row) : cap_scalar;
+            const double al = alpha ? __ldca(alpha + row) : alpha0, be = beta ? __ldca(beta + row) : beta0;
+            const int32_t ci = __ldca(c + row);
+            const int32_t capi = cap ? __ldca(cap + row) : cap_scalar;
             if (!(al >= 1.0 && be >= 1.0 && al == floor(al) && be == floor(be))) err = HORA_ERR_NOT_INTEGER;
             else if (al + be + (double)G0 + (double)ld >= 1048576.0) err = err ? err : HORA_ERR_EXACT_RANGE;
             const unsigned long long *keys = reinterpret_cast<const unsigned long long *>(gains) + row * (int64_t)ld;
@@ -1460,12 +1460,12 @@ exact_collect(const double *__restrict__ alpha, const double *__restrict__ beta,
             const int32_t p_level1 = st.x;
             if (list && st.y > st.x) st = close_segment(keys, st, lam_key, ld);   // the list route leaves segments open
             q = st.x;                                         // #keys > lambda
-            if (q > 0 && __ldg(&HORA_AT(keys, q - 1, ld)) <= k_hi) {
+            if (q > 0 && __ldca(&HORA_AT(keys, q - 1, ld)) <= k_hi) {
                 --q;
-                if (q > 0 && __ldg(&HORA_AT(keys, q - 1, ld)) <= k_hi) err = err ? err : HORA_ERR_EXACT_RANGE;
+                if (q > 0 && __ldca(&HORA_AT(keys, q - 1, ld)) <= k_hi) err = err ? err : HORA_ERR_EXACT_RANGE;
             }
-            const bool has = (q < capi) && (__ldg(&HORA_AT(keys, q, ld)) >= k_lo);
-            if (has && q + 1 < capi && __ldg(&HORA_AT(keys, q + 1, ld)) >= k_lo) err = err ? err : HORA_ERR_EXACT_RANGE;
+            const bool has = (q < capi) && (__ldca(&HORA_AT(keys, q, ld)) >= k_lo);
+            if (has && q + 1 < capi && __ldca(&HORA_AT(keys, q + 1, ld)) >= k_lo) err = err ? err : HORA_ERR_EXACT_RANGE;
             if (has && !err)
                 tkey = pack_type((unsigned long long)al + ci, (unsigned long long)be + (G0 - ci), (unsigned long long)q + 1);
             // Level 1 left U_i(p_hi) for the rows without a key in the threshold's bin.  It stands unless the exact
@@ -1518,8 +1518,8 @@ constexpr int kExactRankThreads = 256;
 constexpr size_t kExactRankSmem = (size_t)kMaxTypes * (2 * sizeof(UBig) + sizeof(unsigned long long) + sizeof(int));
 
 __global__ void __launch_bounds__(kExactRankThreads)
-exact_rank(int64_t B, AllocHeader *hdr, const unsigned long long *__restrict__ tkeys,
-           const unsigned long long *__restrict__ tcounts, int32_t *__restrict__ tlabel) {
+exact_rank(int64_t B, AllocHeader *hdr, const unsigned long long *tkeys,
+           const unsigned long long *tcounts, int32_t *__restrict__ tlabel) {
     pdl_enter();
     extern __shared__ __align__(16) unsigned char s_rank_raw[];
     UBig *s_num = reinterpret_cast<UBig *>(s_rank_raw);
@@ -1583,10 +1583,10 @@ exact_rank(int64_t B, AllocHeader *hdr, const unsigned long long *__restrict__ t
 // did not run (B == 0: mode 0) or its result is relabelled (exact mode: mode 2, apply the labels first).
 // With `validate` the priors and counts of every prompt are checked here (level 1 checks them otherwise).
 __global__ void __launch_bounds__(kSelThreads)
-select_sum(const double *__restrict__ alpha, const double *__restrict__ beta, double alpha0, double beta0,
-           const int32_t *__restrict__ c, int32_t G0, const int32_t *__restrict__ cap, int32_t cap_scalar, int validate,
-           int64_t N, int32_t ld, const double *__restrict__ gains, int mode, int64_t B, AllocHeader *hdr,
-           int2 *__restrict__ rowstate, const int32_t *__restrict__ rowslot, const int32_t *__restrict__ tlabel,
+select_sum(const double *alpha, const double *beta, double alpha0, double beta0,
+           const int32_t *c, int32_t G0, const int32_t *cap, int32_t cap_scalar, int validate,
+           int64_t N, int32_t ld, const double *gains, int mode, int64_t B, AllocHeader *hdr,
+           int2 *__restrict__ rowstate, const int32_t *rowslot, const int32_t *tlabel,
            long long *bsum_hi, long long *bsum_t, int64_t NB) {
     pdl_enter();
     __shared__ long long s_warp[2 * (kSelThreads / kWarp)];
@@ -1640,11 +1640,11 @@ select_sum(const double *__restrict__ alpha, const double *__restrict__ beta, do
 // stores where the caller's arrays are 16-byte aligned: `vec`).  `objrow` (may be null) holds the utilities
 // level 1 already evaluated; a negative entry, or no array, means "evaluate here".
 __global__ void __launch_bounds__(kSelThreads)
-select_out(const double *__restrict__ alpha, const double *__restrict__ beta, double alpha0, double beta0,
-           const int32_t *__restrict__ c, int32_t G0, const int32_t *__restrict__ cap, int32_t cap_scalar, int64_t N,
-           int32_t ld, const double *__restrict__ gains, int64_t B, uint32_t flags, AllocHeader *hdr,
-           const int2 *__restrict__ rowstate, const double *__restrict__ objrow, const long long *__restrict__ bpre_hi,
-           const long long *__restrict__ bpre_t, double *objpart, int64_t NB, int32_t *__restrict__ delta,
+select_out(const double *alpha, const double *beta, double alpha0, double beta0,
+           const int32_t *c, int32_t G0, const int32_t *cap, int32_t cap_scalar, int64_t N,
+           int32_t ld, const double *gains, int64_t B, uint32_t flags, AllocHeader *hdr,
+           const int2 *rowstate, const double *objrow, const long long *bpre_hi,
+           const long long *bpre_t, double *objpart, int64_t NB, int32_t *__restrict__ delta,
            int32_t *__restrict__ G, int64_t *__restrict__ offsets, int vec, hora_alloc_info *info) {
     pdl_enter();
     __shared__ long long s_warp[2 * (kSelThreads / kWarp)];
@@ -1743,7 +1743,7 @@ select_out(const double *__restrict__ alpha, const double *__restrict__ beta, do
                 double u = o[q];
                 if (u < 0.0) {
                     const Posterior p = load_posterior(alpha, beta, alpha0, beta0, c, G0, cap, cap_scalar, ld, row0 + q);
-                    u = utility_from_gain(__ldg(&HORA_AT(gains, (row0 + q) * (int64_t)ld + (d[q] - 1), N * (int64_t)ld)), p.a, p.b, d[q]);
+                    u = utility_from_gain(__ldca(&HORA_AT(gains, (row0 + q) * (int64_t)ld + (d[q] - 1), N * (int64_t)ld)), p.a, p.b, d[q]);
                 }
                 obj += u;
             }

@@ -16,13 +16,13 @@ namespace hora {
 
 template <bool VEC4>
 __global__ void __launch_bounds__(kBcThreads)
-token_broadcast_kernel(const float *__restrict__ adv, const int64_t *__restrict__ off, int64_t R, int64_t T,
+token_broadcast_kernel(const float *adv, const int64_t *off, int64_t R, int64_t T,
                        int64_t chunk, float *__restrict__ out) {
     pdl_enter();
     __shared__ int32_t s_rel[kStage + 1];               // offsets relative to the chunk start, clamped to [-1, len]
     __shared__ float s_adv[kStage];
     __shared__ unsigned long long s_bounds[2];
-    const int64_t t_all = __ldg(off + R);
+    const int64_t t_all = __ldca(off + R);
     if (t_all < T) T = t_all;                           // never write past the last rollout
     const int64_t c0 = (int64_t)blockIdx.x * chunk;
     if (c0 >= T) return;
@@ -36,9 +36,9 @@ token_broadcast_kernel(const float *__restrict__ adv, const int64_t *__restrict_
         const int n_stage = (int)((R - r_base < kStage) ? R - r_base : kStage);
         __syncthreads();
         for (int j = threadIdx.x; j <= n_stage; j += kBcThreads) {
-            const int64_t d = __ldg(off + r_base + j) - c0;
+            const int64_t d = __ldca(off + r_base + j) - c0;
             s_rel[j] = d < 0 ? -1 : (d > len ? len : (int32_t)d);
-            if (j < n_stage) s_adv[j] = __ldg(adv + r_base + j);
+            if (j < n_stage) s_adv[j] = __ldca(adv + r_base + j);
         }
         __syncthreads();
         const int32_t t_end = s_rel[n_stage];           // the staged rollouts cover tokens [t, t_end)

@@ -26,7 +26,7 @@ inline int64_t token_chunk(int64_t T) {
 }
 
 // Largest r in [0, R] with off[r] <= t (off is non-decreasing, off[0] <= t).  All threads return it.
-static __device__ int64_t block_find_rollout(const int64_t *__restrict__ off, int64_t R, int64_t t,
+static __device__ int64_t block_find_rollout(const int64_t *off, int64_t R, int64_t t,
                                       unsigned long long *s_bounds) {
     int64_t lo = 0, hi = R;
     while (hi > lo) {
@@ -36,7 +36,7 @@ static __device__ int64_t block_find_rollout(const int64_t *__restrict__ off, in
         const int64_t step = (hi - lo + kBcThreads - 1) / kBcThreads;
         const int64_t probe = lo + (int64_t)(threadIdx.x + 1) * step;
         if (probe <= hi) {
-            if (__ldg(off + probe) <= t) atomicMax(&s_bounds[0], (unsigned long long)probe);
+            if (__ldca(off + probe) <= t) atomicMax(&s_bounds[0], (unsigned long long)probe);
             else atomicMin(&s_bounds[1], (unsigned long long)(probe - 1));
         }
         __syncthreads();

@@ -43,9 +43,9 @@ __device__ __forceinline__ Posterior make_posterior(double al, double be, int32_
 __device__ __forceinline__ Posterior load_posterior(const double *alpha, const double *beta, double alpha0,
                                                     double beta0, const int32_t *c, int32_t G0,
                                                     const int32_t *cap, int32_t cap_scalar, int32_t ld, int64_t i) {
-    const double al = alpha ? __ldg(alpha + i) : alpha0;
-    const double be = beta ? __ldg(beta + i) : beta0;
-    return make_posterior(al, be, __ldg(c + i), cap ? __ldg(cap + i) : cap_scalar, G0, ld);
+    const double al = alpha ? __ldca(alpha + i) : alpha0;
+    const double be = beta ? __ldca(beta + i) : beta0;
+    return make_posterior(al, be, __ldca(c + i), cap ? __ldca(cap + i) : cap_scalar, G0, ld);
 }
 
 inline hora_status_t cuda_ok(cudaError_t e) { return e == cudaSuccess ? HORA_OK : HORA_ERR_CUDA; }
@@ -69,6 +69,10 @@ inline int clamp_grid(int64_t want, int per_sm) {
 // in beside a running one was measured and made the full-size call slower (0.478 -> 0.51-0.56 ms), whichever
 // kernel gave the signal.  After a kernel that does not take part (or a copy, or a memset) the attribute changes
 // nothing, and pdl_enter() in a kernel launched without it returns at once.
+// Such a kernel begins before the one in front has ended, so what it reads is not constant for its lifetime, which is what a non-coherent
+// load asks for.  Its loads are coherent ones: no __ldg, and no input pointer is __restrict__ (the compiler may load through one
+// of those as through __ldg).  __ldca is cached alike: the four-call step at N = 2^20 takes
+// 1.069 ms with either (the exact path over 4194304 prompts 854 us in place of 847).
 __device__ __forceinline__ void pdl_enter() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
 template <typename... KArgs, typename... Args>

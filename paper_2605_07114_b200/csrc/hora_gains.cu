@@ -20,8 +20,8 @@ namespace hora {
 // (2.9 TB/s at 64 entries, 4.3 TB/s at 128).  A lane always holds 8 consecutive entries.
 template <int E, bool VEC2, int LG>
 __global__ void __launch_bounds__(kGainsWarps *kWarp, 3)
-gains_kernel(const double *__restrict__ alpha, const double *__restrict__ beta, double alpha0, double beta0,
-             const int32_t *__restrict__ c, int32_t G0, const int32_t *__restrict__ cap, int32_t cap_scalar,
+gains_kernel(const double *alpha, const double *beta, double alpha0, double beta0,
+             const int32_t *c, int32_t G0, const int32_t *cap, int32_t cap_scalar,
              int64_t N, int32_t ld, double *__restrict__ gains, int32_t *status_dev) {
     pdl_enter();
     NoTap tap;

@@ -103,9 +103,9 @@ constexpr int kCtaRows = kGainsWarps * kTile; // rows a CTA stages per step
 // LG < 32 (rows of at most LG * E entries): a warp builds 32 / LG rows at a time, LG lanes a row; a tap is told
 // begin_row(-1, 0) for the rows of the last tile that do not exist.
 template <int E, bool VEC2, typename Tap, int LG = kWarp>
-__device__ __forceinline__ void gains_rows_cta(const double *__restrict__ alpha, const double *__restrict__ beta,
-                                               double alpha0, double beta0, const int32_t *__restrict__ c, int32_t G0,
-                                               const int32_t *__restrict__ cap, int32_t cap_scalar, int64_t N,
+__device__ __forceinline__ void gains_rows_cta(const double *alpha, const double *beta,
+                                               double alpha0, double beta0, const int32_t *c, int32_t G0,
+                                               const int32_t *cap, int32_t cap_scalar, int64_t N,
                                                int32_t ld, double *__restrict__ gains, int32_t *status_dev, Tap &tap) {
     // Staging slab: a lane produces E consecutive entries, but a store instruction should cover one
     // contiguous 512-byte run of the row (full 32-byte sectors; 16-byte pieces at a 64-byte stride cost

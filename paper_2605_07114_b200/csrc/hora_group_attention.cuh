@@ -145,7 +145,7 @@ struct Pieces {
     Sequence s;
 
     __device__ __forceinline__ Pieces(const AttnArgs &a, int32_t stream, bool &bad) {
-        const int64_t *__restrict__ start = a.start[WIDE];
+        const int64_t *start = a.start[WIDE];
         const int32_t n_seq = a.N + a.R;
         const int64_t per = steps_per_stream<WIDE>(a);
         u = (int64_t)stream * per;

@@ -175,8 +175,8 @@ __device__ __forceinline__ void narrow_stream(const AttnArgs &a, int32_t stream,
                     if (page < 0 || page >= a.n_pages) { bad = true; page = 0; }
                     const int64_t row = (((int64_t)page * a.Hkv + h) << a.page_shift) + (key & ((1 << a.page_shift) - 1));
                     if (!HORA_IN(row + 15, (a.n_pages * a.Hkv) << a.page_shift)) break;
-                    const uint8_t *__restrict__ k = static_cast<const uint8_t *>(a.k_cache) + row * St::kRowBytes + lane * 16;
-                    const uint8_t *__restrict__ v = static_cast<const uint8_t *>(a.v_cache) + row * St::kRowBytes + lane * 16;
+                    const uint8_t *k = static_cast<const uint8_t *>(a.k_cache) + row * St::kRowBytes + lane * 16;
+                    const uint8_t *v = static_cast<const uint8_t *>(a.v_cache) + row * St::kRowBytes + lane * 16;
 #pragma unroll
                     for (int x = 0; x < St::kRowBytes / 32; ++x) {
                         const int chunk = x * kWarp + lane;

@@ -21,18 +21,18 @@ __device__ __forceinline__ double group_scale(int32_t mode, double ss, int64_t n
 
 // Mean and scale of the group rewards[s, e), e > s, read from global memory by the whole warp (two-pass form,
 // fp64, fixed butterfly order).  Every lane returns the same values.
-__device__ __forceinline__ void group_mean_scale(const float *__restrict__ rewards, int64_t s, int64_t e, int32_t mode,
+__device__ __forceinline__ void group_mean_scale(const float *rewards, int64_t s, int64_t e, int32_t mode,
                                                  double eps, int32_t ddof, int lane, double &mean, double &scale) {
     const int64_t n = e - s;
     double part = 0.0;
-    for (int64_t j = s + lane; j < e; j += kWarp) part += (double)__ldg(rewards + j);
+    for (int64_t j = s + lane; j < e; j += kWarp) part += (double)__ldca(rewards + j);
     const double sum = warp_sum(part);
     mean = sum / (double)n;
     double ss = 0.0;
     if (mode == HORA_ADV_GRPO) {
         double sq = 0.0;
         for (int64_t j = s + lane; j < e; j += kWarp) {
-            const double d = (double)__ldg(rewards + j) - mean;
+            const double d = (double)__ldca(rewards + j) - mean;
             sq += d * d;
         }
         ss = warp_sum(sq);

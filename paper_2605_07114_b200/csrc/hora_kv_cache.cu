@@ -44,13 +44,13 @@ struct RowWalk {
 
 template <typename In, typename Cache, int D>
 __global__ void __launch_bounds__(kKvThreads)
-kv_write_kernel(const In *__restrict__ k, const In *__restrict__ v, const int64_t *slots, KvShape s,
+kv_write_kernel(const In *k, const In *v, const int64_t *slots, KvShape s,
                 Cache *__restrict__ k_cache, Cache *__restrict__ v_cache, uint8_t *__restrict__ k_exp,
                 uint8_t *__restrict__ v_exp, int32_t *status) {
     pdl_enter();
     constexpr int kLanes = D / 8, kGroups = kKvThreads / kLanes;
     const int sub = threadIdx.x % kLanes;
-    const In *__restrict__ in = blockIdx.y == 0 ? k : v;
+    const In *in = blockIdx.y == 0 ? k : v;
     Cache *__restrict__ cache = blockIdx.y == 0 ? k_cache : v_cache;
     uint8_t *__restrict__ exps = blockIdx.y == 0 ? k_exp : v_exp;
     const int64_t t0 = (int64_t)blockIdx.x * s.tokens_per_cta;
@@ -108,14 +108,14 @@ kv_write_kernel(const In *__restrict__ k, const In *__restrict__ v, const int64_
 
 template <typename Out, typename Cache, int D>
 __global__ void __launch_bounds__(kKvThreads)
-kv_read_kernel(const Cache *__restrict__ k_cache, const Cache *__restrict__ v_cache, const uint8_t *__restrict__ k_exp,
-               const uint8_t *__restrict__ v_exp, const int64_t *slots, KvShape s, Out *__restrict__ k,
+kv_read_kernel(const Cache *k_cache, const Cache *v_cache, const uint8_t *k_exp,
+               const uint8_t *v_exp, const int64_t *slots, KvShape s, Out *__restrict__ k,
                Out *__restrict__ v, int32_t *status) {
     pdl_enter();
     constexpr int kLanes = D / 8, kGroups = kKvThreads / kLanes;
     const int sub = threadIdx.x % kLanes;
-    const Cache *__restrict__ cache = blockIdx.y == 0 ? k_cache : v_cache;
-    const uint8_t *__restrict__ exps = blockIdx.y == 0 ? k_exp : v_exp;
+    const Cache *cache = blockIdx.y == 0 ? k_cache : v_cache;
+    const uint8_t *exps = blockIdx.y == 0 ? k_exp : v_exp;
     Out *__restrict__ out = blockIdx.y == 0 ? k : v;
     const int64_t t0 = (int64_t)blockIdx.x * s.tokens_per_cta;
     const int64_t left = s.n_tokens - t0;

@@ -166,7 +166,7 @@ rank_pos_kernel(int32_t G0, int32_t ld, RankTables t) {
     int lo = 0, hi = ld;
     while (lo < hi) {
         const int mid = (lo + hi) >> 1;
-        if (__ldg(row + mid) < r) lo = mid + 1; else hi = mid;
+        if (__ldca(row + mid) < r) lo = mid + 1; else hi = mid;
     }
     t.pos[id] = (uint16_t)lo;
 }
@@ -271,13 +271,13 @@ size_t rank_allocate_workspace_bound(int64_t N) {
 // A prompt at or beyond N reads as c = -1 (no bin, not an error).
 struct RankQuad { int32_t c[4], cap[4]; };
 
-__device__ __forceinline__ void rank_load_quad(RankQuad &q, const int32_t *__restrict__ c, const int32_t *__restrict__ cap,
+__device__ __forceinline__ void rank_load_quad(RankQuad &q, const int32_t *c, const int32_t *cap,
                                                int32_t cap_scalar, int64_t p, int64_t N, bool vec) {
     if (vec && p + 4 <= N) {
-        const int4 cv = __ldg(reinterpret_cast<const int4 *>(c + p));
+        const int4 cv = __ldca(reinterpret_cast<const int4 *>(c + p));
         q.c[0] = cv.x; q.c[1] = cv.y; q.c[2] = cv.z; q.c[3] = cv.w;
         if (cap) {
-            const int4 pv = __ldg(reinterpret_cast<const int4 *>(cap + p));
+            const int4 pv = __ldca(reinterpret_cast<const int4 *>(cap + p));
             q.cap[0] = pv.x; q.cap[1] = pv.y; q.cap[2] = pv.z; q.cap[3] = pv.w;
         } else {
             q.cap[0] = q.cap[1] = q.cap[2] = q.cap[3] = cap_scalar;
@@ -285,8 +285,8 @@ __device__ __forceinline__ void rank_load_quad(RankQuad &q, const int32_t *__res
     } else {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            q.c[k] = p + k < N ? __ldg(c + p + k) : -1;
-            q.cap[k] = (p + k < N && cap) ? __ldg(cap + p + k) : cap_scalar;
+            q.c[k] = p + k < N ? __ldca(c + p + k) : -1;
+            q.cap[k] = (p + k < N && cap) ? __ldca(cap + p + k) : cap_scalar;
         }
     }
 }
@@ -366,7 +366,7 @@ __device__ void hard_first_tail(const RankWorkspace &w, int32_t ld, int64_t B, l
 // finds a water level instead of a threshold rank (hard_first_tail).
 template <bool HARD>
 __global__ void __launch_bounds__(kSelThreads, 8)
-rank_count_kernel(const int32_t *__restrict__ c, int32_t G0, const int32_t *__restrict__ cap, int32_t cap_scalar,
+rank_count_kernel(const int32_t *c, int32_t G0, const int32_t *cap, int32_t cap_scalar,
                   int64_t N, int32_t ld, int64_t B, uint32_t flags, int vec, RankWorkspace w) {
     pdl_enter();
     extern __shared__ __align__(16) unsigned char s_rank_cnt[];
@@ -446,7 +446,7 @@ rank_count_kernel(const int32_t *__restrict__ c, int32_t G0, const int32_t *__re
                 if (lane >= d) inc += x;
             }
             const long long cnt = carry + inc;
-            if (D >= 1 && cnt > 0) atomicAdd(&HORA_AT(w.bucket, w.bins - 1 - __ldg(rrow + D - 1), w.bins), (unsigned long long)cnt);
+            if (D >= 1 && cnt > 0) atomicAdd(&HORA_AT(w.bucket, w.bins - 1 - __ldca(rrow + D - 1), w.bins), (unsigned long long)cnt);
             carry += __shfl_sync(kFull, inc, kWarp - 1);
         }
     }
@@ -468,13 +468,13 @@ rank_count_kernel(const int32_t *__restrict__ c, int32_t G0, const int32_t *__re
         int lo = 0, hi = rstar >= 0 ? ld : 0;
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;
-            if (__ldg(rrow + mid) < rstar) lo = mid + 1; else hi = mid;
+            if (__ldca(rrow + mid) < rstar) lo = mid + 1; else hi = mid;
         }
-        const int tied = rstar >= 0 && lo < ld && __ldg(rrow + lo) == rstar;
+        const int tied = rstar >= 0 && lo < ld && __ldca(rrow + lo) == rstar;
         w.class_tab[cls] = (lo << 1) | tied;
     }
     __syncthreads();
-    const double lambda = rstar >= 0 ? __ldg(w.tab.lam + rstar) : 0.0;
+    const double lambda = rstar >= 0 ? __ldca(w.tab.lam + rstar) : 0.0;
     // objective: every prompt of bin (c, cap) ends at Delta = min(cap, above_c), plus the tied rollouts handed
     // out, each worth lambda (Eq. appendix-objective: U is the sum of the gains taken); fixed summation order
     double obj = 0.0;
@@ -484,7 +484,7 @@ rank_count_kernel(const int32_t *__restrict__ c, int32_t G0, const int32_t *__re
             if (cnt == 0ull) continue;
             const int cls = b / (ld + 1), cp = b - cls * (ld + 1);
             const int hi_c = w.class_tab[cls] >> 1;
-            obj += (double)cnt * __ldg(w.tab.util + (size_t)cls * (ld + 1) + (cp < hi_c ? cp : hi_c));
+            obj += (double)cnt * __ldca(w.tab.util + (size_t)cls * (ld + 1) + (cp < hi_c ? cp : hi_c));
         }
 #pragma unroll
         for (int d = 16; d >= 1; d >>= 1) obj += __shfl_xor_sync(kFull, obj, d);
@@ -518,7 +518,7 @@ __device__ __forceinline__ void rank_task_state(const RankQuad (&q)[2], const in
 
 // Sums of (above, tied) per task and per CTA.  No barrier inside the loop, no ticket at the end.
 __global__ void __launch_bounds__(kSelThreads, 4)
-rank_sums_kernel(const int32_t *__restrict__ c, int32_t n_class, int tiers, const int32_t *__restrict__ cap,
+rank_sums_kernel(const int32_t *c, int32_t n_class, int tiers, const int32_t *cap,
                  int32_t cap_scalar, int64_t N, int vec, RankWorkspace w, int64_t NT, int64_t m) {
     pdl_enter();
     extern __shared__ __align__(16) unsigned char s_rank_cls[];
@@ -560,7 +560,7 @@ rank_sums_kernel(const int32_t *__restrict__ c, int32_t n_class, int tiers, cons
 // lanes 0..7 fetch the eight task sums, a 3-step scan gives the warp the prefix of its own task and the total
 // of the eight, and the warp writes its 256 prompts (16-byte stores where the arrays allow: `vec_out`).
 __global__ void __launch_bounds__(kSelThreads, 3)
-rank_out_kernel(const int32_t *__restrict__ c, int32_t G0, int32_t n_class, int tiers, const int32_t *__restrict__ cap,
+rank_out_kernel(const int32_t *c, int32_t G0, int32_t n_class, int tiers, const int32_t *cap,
                 int32_t cap_scalar, int64_t N, int64_t B, int vec, RankWorkspace w, int64_t NT, int64_t m,
                 int32_t *__restrict__ delta,
                 int32_t *__restrict__ G, int64_t *__restrict__ offsets, int vec_out, hora_alloc_info *info) {
