@@ -28,7 +28,8 @@
  *     a too-small workspace, a failed launch).  Errors that depend on device DATA (a non-finite
  *     prior, B larger than the total cap, ...) are written to a status word in device memory; the
  *     caller reads it after synchronising.  Nothing traps, spins or aborts.
- *   - Results are deterministic: the same inputs give bitwise identical outputs on every run.
+ *   - Results are deterministic: the same inputs give bitwise identical outputs on every run
+ *     (one exception: a slot given twice to hora_kv_write).
  *   - Calls on different streams may run concurrently as long as they do not share output
  *     buffers or workspaces.
  *   - The kernels of hora_gains, hora_allocate, hora_group_advantage, hora_token_broadcast,
@@ -413,7 +414,9 @@ enum { HORA_DTYPE_F32 = 0, HORA_DTYPE_BF16 = 1, HORA_DTYPE_F16 = 2, HORA_DTYPE_E
  * E4M3: with a = max |x| over the row's finite values, exp - 127 = the least e >= -126 with a / 2^e <= 448 (0 for a row
  * without a finite value other than zero); code = x / 2^e rounded to nearest even, +-infinity as +-448, NaN as NaN.  x / 2^e is exact, so
  * one rounding is all the error there is and the codes do not depend on how they were computed.
- * A slot beyond the cache raises INVALID_VALUE in status_dev (optional) and is skipped.  A slot given twice holds either.
+ * A slot beyond the cache raises INVALID_VALUE in status_dev (optional) and is skipped.  Slots have to be distinct: one that is given twice
+ * holds any mixture of its tokens afterwards (codes of one, scale of another), and not the same one on every run.  The other slots
+ * are not affected; tokens that nobody will read get a negative slot.
  *
  * hora_kv_read — the other way: row t of k, v (out_dtype F32, BF16 or F16) is the content of slots[t]; zeros where
  * slots[t] is negative or beyond the cache (the latter raises INVALID_VALUE).  Rows as for hora_kv_write.
