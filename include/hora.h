@@ -439,7 +439,9 @@ hora_status_t hora_kv_read(const void *k_cache, const void *v_cache, const uint8
  * Query t < q_len[r] sees its own tokens 0 .. suffix_len[r]-q_len[r]+t (none if that is negative).  For each head
  *   s_j = sm_scale * q . k_j,   out = sum_j e^(s_j) v_j / sum_j e^(s_j),   lse = log sum_j e^(s_j)
  * over the keys it sees; out = 0 and lse = -infinity where there are none, for slots t >= q_len[r], and for rollouts at
- * or beyond group_offsets[N].  Every prompt's cache is read once for its whole group, whatever the group's size.
+ * or beyond group_offsets[N].  A prompt's cache is kept once for its group and read once for every block of the group's query rows
+ * (queries times heads of a cache head): blocks of up to 256 rows where a 16-bit cache has many rows to a key, else, and for an E4M3
+ * cache always, of 8, 16 or 24.
  * Scores, maxima, sums and outputs are held in fp32; the weights are rounded to the 16-bit type of the product they enter.
  * A key that a query does not see has the weight zero; a score beyond fp32's range makes its row NaN.
  * For an E4M3 cache that is fp16, and a weight enters times its value row's scale, relative to the largest such product among the keys the
@@ -489,7 +491,8 @@ hora_status_t hora_group_attention(const void *q, int32_t q_dtype, int64_t q_row
  *   n_accepted    [R] int32 out;  tokens [R, K+1] int32 out
  *   status_dev    optional: INVALID_VALUE for a drafted token outside [0, V) (refused), draft_len out of range (clamped), a
  *                 negative or NaN value in a row that is read, or a row without any weight (the drawn token is then -1)
- * Limits: 0 <= K <= 255, 1 <= V <= 2^22.  Rows on 16-byte boundaries are read with 16-byte loads throughout.
+ * Limits: 0 <= K <= 255, 1 <= V <= 2^22.  Rows are read with 16-byte loads wherever they begin,
+ * but for a draft row that lies at another place within 16 bytes than the target's (packed rows of an odd V): that one is read value by value.
  */
 hora_status_t hora_verify_drafts(const void *target, int32_t dtype, int64_t target_row_stride, const void *draft,
                                  int64_t draft_row_stride, const int32_t *draft_tokens, const int32_t *draft_len,
