@@ -54,3 +54,17 @@ def test_a_token_outside_the_vocabulary_is_refused(hora, V, token, dtype, rows):
     np.testing.assert_array_equal(out.cpu().numpy(), eo)
     assert int(status) == hora.ERR_INVALID_VALUE
     assert ((out.cpu().numpy()[np.arange(R), en] >= 0) & (out.cpu().numpy()[np.arange(R), en] < V)).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("R,V,pad", [(1, 2, 0), (9, 37, 0), (33, 1000, 24), (20, 4099, 3), (700, 513, 1), (2, 50257, 0)])
+def test_without_drafts_a_token_is_drawn_from_the_target(hora, R, V, pad, dtype):
+    from test_gpu_verify_drafts import call
+    s = draw(R, 0, V, dtype, False, R + V, pad)
+    s["u_sample"][::3] = 1.0 - 2.0 ** -24
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    n, out = call(s, status)
+    en, eo = expect(s)
+    np.testing.assert_array_equal(n, en)
+    np.testing.assert_array_equal(out, eo)
+    assert int(status) == 0 and (n == 0).all()
