@@ -524,6 +524,7 @@ class GroupAttention:
         self.workspace = torch.empty(max(wb, 256), dtype=torch.uint8, device=dev)
         self.out = torch.empty((R, T, Hq, cache.D), dtype=dtype, device=dev)
         self.lse = torch.empty((R, T, Hq), dtype=torch.float32, device=dev)
+        self._streams = set()
         self._call = self._bind(cache, Hq, T, dtype, group_offsets, prefix_pages, prefix_len, suffix_pages, suffix_len, q_len,
                                 cache.D ** -0.5 if sm_scale is None else sm_scale, self.workspace, status_dev)
 
@@ -561,6 +562,11 @@ class GroupAttention:
         out = self.out if out is None else out
         lse = self.lse if lse is None else lse
         self._call(q, out, lse)
+        raw = _raw_stream(q)
+        if raw not in self._streams:         # the object's memory is not handed on before this stream is through with it
+            self._streams.add(raw)
+            for t in (self.workspace, self.out, self.lse):
+                t.record_stream(torch.cuda.current_stream(t.device))
         return out, lse
 
 

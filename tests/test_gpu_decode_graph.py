@@ -69,3 +69,28 @@ def test_a_step_replayed_from_a_graph(dtype):
             assert torch.equal(a, b)
         own.copy_(own2 - T + outs[0][0] + 1)
     assert int(status) == 0 and int(own.min()) >= 6
+
+
+def test_buffers_outlive_their_object_on_another_stream():
+    """An object that is dropped while another stream still has its call in front of it: its memory is not given to anyone else before
+    that.  The side stream is kept busy for a fraction of a second meanwhile."""
+    from paper_2605_07114_b200 import hora
+    i32 = lambda x: torch.as_tensor(x, dtype=torch.int32, device=DEV)  # noqa: E731
+    cache = hora.PagedCache.empty(8, 16, 2, 64)
+    cache.k.normal_()
+    cache.v.normal_()
+    args = dict(group_offsets=torch.tensor([0, 3], device=DEV), prefix_pages=i32([[0, 1]]), prefix_len=i32([30]), suffix_pages=i32([[2], [3], [4]]), suffix_len=i32([5, 16, 1]))
+    q = torch.randn(3, 1, 8, 64, device=DEV).to(torch.bfloat16)
+    op = hora.GroupAttention(cache, 8, 1, torch.bfloat16, **args)
+    want = op.run(q)[0].clone()
+    out, size, at = torch.empty_like(q), op.workspace.numel(), op.workspace.data_ptr()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(200_000_000)
+        op.run(q, out=out)
+    del op
+    taken = [torch.full((size,), 0xFF, dtype=torch.uint8, device=DEV) for _ in range(2)]
+    assert not side.query() and all(t.data_ptr() != at for t in taken)
+    side.synchronize()
+    assert torch.equal(out.view(torch.int16), want.view(torch.int16))
