@@ -86,6 +86,9 @@ __device__ __forceinline__ int32_t query_count(const AttnArgs &a, int32_t r) {
 // over a long list: the same, and the CTA's 128 rows may be mostly idle, since the bytes are what takes the time (103485 keys,
 // 32 rows of 4 heads each: 318 us as narrow items, 122 as wide ones).  Short lists of few rows are narrow: a piece of a wide item costs
 // some microseconds to begin and to end (256 rollouts of 20 rows over up to 1021 keys: 122 us, 172 as wide items).
+//   From kWideFrom rows on the length does not enter, which costs short lists: 600 rollouts, 4 cache heads, us as wide / as narrow items
+//     D = 64:  40 rows, 128 keys 95 / 89, 1024 keys 361 / 242;  128 rows, 128 keys 221 / 221, 1024 keys 426 / 652
+//     D = 128: 40 rows, 128 keys 189 / 137, 1024 keys 424 / 503;  128 rows, 64 keys 266 / 245, 1024 keys 518 / 1303
 __device__ __forceinline__ bool can_be_wide(const AttnArgs &a, const Sequence &s) {
     return a.n_wide > 0 && (s.rows >= kWideFrom || (s.rows > a.narrow_rows && s.len >= kWideLong));
 }

@@ -24,8 +24,8 @@
 // what fp16 cannot hold is 2^-24 and less of that.  A value row of zeros has the scale 1, which says nothing about it: where m_o is
 // to be raised, such rows are found in the stage and left out.  l stays relative to m, and o is brought to m when the partial is stored.
 // Queries are scaled by a power of two to lie well within fp16's range.
-//   Measured: 480 rollouts of 1024 keys on average, 4 cache heads of 128, bf16: 5.6 TB/s; 1920 of 768 keys, 2 cache heads of 128, e4m3: 170 us
-// for 0.86 GB, half of the issue slots (with queries as the left operand, padded to 16 rows, 223 us).
+//   Measured: 480 rollouts of 1024 keys on average, 4 cache heads of 128, bf16: 5.6 TB/s; 1920 of 768 keys, 2 cache heads of 128, e4m3: 175 us
+// for 0.86 GB, half of the issue slots.
 #pragma once
 
 #include <type_traits>

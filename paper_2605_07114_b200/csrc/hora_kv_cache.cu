@@ -11,8 +11,8 @@
 
 namespace hora {
 
-constexpr int kKvThreads = 128;                          // 131072 tokens (below): 291 us with 128, 317 with 256
-constexpr int kRowsInFlight = 4;                         // 131072 tokens, 8 heads of 128, bf16 -> e4m3 -> bf16: 291 us (5.5 TB/s); with 2 and 8, at 256 threads, 369 and 441 against 317
+constexpr int kKvThreads = 128;                          // 131072 tokens (below): 291 us with 128, 316 with 256
+constexpr int kRowsInFlight = 4;                         // 131072 tokens, 8 heads of 128, bf16 -> e4m3 -> bf16: 291 us (5.5 TB/s; 310 on another GPU); 306 with 2, 296 with 8
 
 struct KvShape {
     int64_t n_tokens, row_stride, n_slots;

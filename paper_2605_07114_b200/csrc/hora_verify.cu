@@ -6,7 +6,7 @@
 // token is the one the definition names.  One pass over the row: each warp adds up segments of kSeg weights and leaves the
 // sums in shared memory; the CTAs push their totals into each other's shared memory (one cluster barrier), every CTA then
 // knows the drawn weight's position, and the CTA that holds it reads one segment again (from L2) to name the token.
-// Bound by HBM for many rollouts (480 of 151936 fp32 values: 77 us for 455 MB), by the chain token -> probability -> row -> barrier -> segment for few.
+// Bound by HBM for many rollouts (480 of 151936 fp32 values: 82 us for 455 MB; figures below are pairs from one GPU), by the chain token -> probability -> row -> barrier -> segment for few.
 #include <cooperative_groups.h>
 
 #include <utility>
