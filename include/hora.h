@@ -16,7 +16,8 @@
  *   hora_gains -> hora_allocate -> [rollouts and rewards happen elsewhere] ->
  *   hora_group_advantage -> hora_token_broadcast
  * and, for where the rollouts happen, the operators of a decode step over such groups (hora_kv_write, hora_group_attention,
- * hora_verify_drafts).
+ * hora_verify_drafts) and those of their prompts and of a training step over them (hora_qk_rotate, hora_packed_attention and their
+ * backward passes).
  *
  * Conventions for every call
  *   - Unless a parameter says "host", every pointer is a DEVICE pointer on the current CUDA device.
@@ -33,7 +34,8 @@
  *   - Calls on different streams may run concurrently as long as they do not share output
  *     buffers or workspaces.
  *   - The kernels of hora_gains, hora_allocate, hora_group_advantage, hora_token_broadcast,
- *     hora_group_advantage_tokens and the decode-step calls are launched with the programmatic-dependent-launch attribute and wait
+ *     hora_group_advantage_tokens, the decode-step calls and those for prompts and training steps are launched with the
+ *     programmatic-dependent-launch attribute and wait
  *     (griddepcontrol.wait) for the work before them in the stream before they touch memory, so stream order
  *     holds as usual; a kernel of the caller's that follows them with the same attribute must do its own wait.
  */
@@ -500,6 +502,104 @@ hora_status_t hora_verify_drafts(const void *target, int32_t dtype, int64_t targ
                                  int32_t *n_accepted, int32_t *tokens, int32_t *status_dev, void *stream);
 
 /*
+ * ---------------------------------------------------------------------------------------------------------------
+ * Prompts and training steps.  Before a prompt's keys and values go into the cache, and when the rollouts are scored again for the
+ * policy's update, the tokens lie packed one sequence after the other (the layout of hora_token_broadcast).  Order per layer:
+ *   projection -> hora_qk_rotate -> [hora_kv_write] -> hora_packed_attention;  backwards: hora_packed_attention_backward ->
+ *   hora_qk_rotate_backward.  A decode step calls hora_qk_rotate with one token (or T) a rollout in front of hora_kv_write.
+ */
+
+/* Which values of a head make a pair of hora_qk_rotate: i and i + rot/2, or 2i and 2i + 1 (i < rot/2). */
+enum { HORA_ROTATE_HALVES = 0, HORA_ROTATE_PAIRS = 1 };
+
+/*
+ * hora_qk_rotate — norms of queries and keys for each head, and the rotation by the token's position, in one pass.  For a row x
+ * (one token, one head, D values; D = 64 or 128):
+ *   z = x * w / sqrt(mean(x^2) + eps)        with the head weights w (z = x where they are NULL)
+ *   y = z with its first `rot` values turned pair by pair: (a, b) -> (a cos f - b sin f, a sin f + b cos f), f = position * inv_freq[i]
+ * f is worked out in 64 bits, everything else in 32, rounded once.
+ *
+ *   q, k          token t at q + t * q_row_stride (elements), heads next to each other: [Hq, D], [Hk, D]; F32, BF16 or F16, 16-byte aligned,
+ *                 row strides at least the heads' width and a multiple of 16 bytes (slices of a fused projection will do).  Hq or Hk may be 0, its
+ *                 pointers are then ignored.
+ *   q_out, k_out  of the same type, alike; q and k themselves (with their strides) for a pass in place, else they must not overlap them
+ *   positions     [n_tokens] int32, any value;  inv_freq [rot/2] fp64, finite;  both ignored where rot = 0
+ *   rot           0 <= rot <= D, a multiple of 16;  layout HORA_ROTATE_HALVES or HORA_ROTATE_PAIRS
+ *   q_weight, k_weight   [D] fp32, or NULL: those rows are not normed;  eps >= 0
+ * Values that are not finite stay within their row (and, without a norm, within their pair).  n_tokens == 0 is a no-op.
+ *
+ * hora_qk_rotate_backward — the gradients.  With g = dy turned back, r = 1 / sqrt(mean(x^2) + eps):
+ *   dx = r * (w g - x r * mean(x r w g)),   dw = sum over tokens and heads of x r g   (dx = g without a norm)
+ *   dq_out, dk_out   gradients of q_out, k_out;  dq, dk  out (may be the same memory as dq_out, dk_out, with their strides);  all rows as above
+ *   q, k             what hora_qk_rotate was given (not read, and may be NULL, where there is no norm)
+ *   dq_weight, dk_weight   [D] fp32 out, or NULL (and NULL where there is no norm): overwritten, summed in an order that does not change
+ *   workspace        hora_qk_rotate_backward_workspace_bytes(D) bytes, 256-byte aligned, contents undefined on entry and exit;
+ *                    NULL will do without the weights' gradients
+ * With n_tokens == 0 the weights' gradients are zeros.
+ */
+hora_status_t hora_qk_rotate(const void *q, const void *k, int32_t dtype, int64_t q_row_stride, int64_t k_row_stride, int64_t n_tokens,
+                             int32_t Hq, int32_t Hk, int32_t D, const int32_t *positions, const double *inv_freq, int32_t rot,
+                             int32_t layout, const float *q_weight, const float *k_weight, float eps, void *q_out, void *k_out,
+                             int64_t q_out_row_stride, int64_t k_out_row_stride, void *stream);
+
+size_t hora_qk_rotate_backward_workspace_bytes(int32_t D);
+
+hora_status_t hora_qk_rotate_backward(const void *dq_out, const void *dk_out, int32_t dtype, int64_t dq_out_row_stride,
+                                      int64_t dk_out_row_stride, const void *q, const void *k, int64_t q_row_stride,
+                                      int64_t k_row_stride, int64_t n_tokens, int32_t Hq, int32_t Hk, int32_t D,
+                                      const int32_t *positions, const double *inv_freq, int32_t rot, int32_t layout,
+                                      const float *q_weight, const float *k_weight, float eps, void *dq, void *dk,
+                                      int64_t dq_row_stride, int64_t dk_row_stride, float *dq_weight, float *dk_weight,
+                                      void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * hora_packed_attention — attention of packed sequences to themselves and, for the rollouts of groups, to their group's prompt.
+ * Sequence s holds the tokens seq_offsets[s] .. seq_offsets[s+1]-1.  Without group_offsets a query sees its own sequence.  With
+ * group_offsets (hora_allocate's output, used where it lies: rollouts of group i are group_offsets[i] .. group_offsets[i+1]-1) the
+ * sequences are, group after group, the group's prompt and then its rollouts, S = N + group_offsets[N] of them; the prompt is sequence
+ * group_offsets[i] + i, and a rollout's query sees all of it in front of its own sequence: the prompt lies once among the tokens, and its
+ * keys' and values' gradients are summed over the group.  causal = 1: of its own sequence a query sees itself and what is before it; 0: all of it.
+ * For each head
+ *   s_j = sm_scale * q . k_j,   out = sum_j e^(s_j) v_j / sum_j e^(s_j),   lse = log sum_j e^(s_j)
+ * Scores, maxima, sums and outputs are held in fp32; the weights are rounded to the 16-bit type of the product they enter.
+ *
+ *   q            token t at q + t * q_row_stride (elements), heads next to each other: [Hq, D], BF16 or F16; query head h reads head h / (Hq/Hkv)
+ *                of k, v, token t at k + t * kv_row_stride: [Hkv, D], of the same type.  D = 64 or 128.  All 16-byte aligned, row strides at least
+ *                the heads' width and multiples of 8 (slices of a fused projection will do).  T tokens in all.
+ *                Rows of a sequence have to be finite; a score beyond fp32's range makes its row NaN.
+ *   seq_offsets  [S+1] int64, non-decreasing, in [0, T] (sequences may be empty).  Tokens before the first or behind the last sequence take no
+ *                part, may hold anything, and keep what the outputs held there.
+ *   group_offsets [N+1] int64 from 0, non-decreasing, or NULL with N = 0
+ *   out          like q, out_row_stride;  lse [T, Hq] fp32 or NULL
+ *   workspace    hora_packed_attention_workspace_bytes(T, S, Hq, Hkv, D, 0) bytes, 256-byte aligned, contents undefined on entry and exit
+ *   status_dev   optional: INVALID_VALUE for offsets that decrease or leave [0, T] and group_offsets that do not fit.  Such values are
+ *                clamped: outputs they touch are wrong, nothing else is read or written.
+ * out must not overlap q, k or v.  T == 0 or S == 0 is a no-op.  Limits: T < 2^31 - 256, S < 2^30, Hq <= 65536.
+ *
+ * hora_packed_attention_backward — the gradients, for what hora_packed_attention was given and left:
+ *   P_j = e^(s_j - lse),  dv_j = sum P_j dout,  dS_j = P_j (dout . v_j - dout . out),  dq = sm_scale sum_j dS_j k_j,  dk_j = sm_scale sum dS_j q
+ * the sums of dk, dv over all queries that see key j, of all heads that read its head.  Sums are held in fp32 and rounded once; P and dS are
+ * rounded to the 16-bit type of the products they enter.  In F16 both are held relative to powers of two, dS to one that follows from the largest
+ * rows of dout and v: a dS less than 2^-39 of 2 max|dout row| max|v row| is lost.
+ *   out, lse, dout   rows like q, out_row_stride, dout_row_stride;  lse not NULL here
+ *   dq, dk, dv       out: rows like q, k, v, dq_row_stride, dkv_row_stride; must not overlap any input
+ *   workspace        hora_packed_attention_workspace_bytes(T, S, Hq, Hkv, D, 1) bytes
+ */
+size_t hora_packed_attention_workspace_bytes(int64_t T, int64_t S, int32_t Hq, int32_t Hkv, int32_t D, int32_t backward);
+
+hora_status_t hora_packed_attention(const void *q, const void *k, const void *v, int32_t dtype, int64_t q_row_stride, int64_t kv_row_stride,
+                                    int64_t T, const int64_t *seq_offsets, int64_t S, const int64_t *group_offsets, int64_t N, int32_t Hq,
+                                    int32_t Hkv, int32_t D, float sm_scale, int32_t causal, void *out, int64_t out_row_stride, float *lse,
+                                    int32_t *status_dev, void *workspace, size_t workspace_bytes, void *stream);
+
+hora_status_t hora_packed_attention_backward(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *dout,
+                                             int32_t dtype, int64_t q_row_stride, int64_t kv_row_stride, int64_t out_row_stride,
+                                             int64_t dout_row_stride, int64_t T, const int64_t *seq_offsets, int64_t S,
+                                             const int64_t *group_offsets, int64_t N, int32_t Hq, int32_t Hkv, int32_t D, float sm_scale,
+                                             int32_t causal, void *dq, void *dk, void *dv, int64_t dq_row_stride, int64_t dkv_row_stride,
+                                             int32_t *status_dev, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * hora_allocate_profile_events — measurement aid, no counterpart in the paper.  With two non-NULL cudaEvent_t
  * handles (created by the caller with timing enabled), every following hora_allocate / hora_allocate_static
  * call records `start_event` just before and `stop_event` just after the launch of its full-read selection
@@ -542,7 +642,8 @@ uint64_t hora_fp64_probe(int32_t iters, double *sink_dev, void *stream);
  * slot and the kernel runs on).  This call synchronises the device and returns 0 if no check has failed since the
  * last call, else (file id << 20) | source line of the first failure (file ids: 1 hora_allocate.cu,
  * 2 hora_allocate_batched.cu, 3 hora_advantage.cu, 4 hora_rank.cu,
- * 5 hora_group_attention.cu, 6 hora_group_attention_main.cu with what it includes, 7 hora_verify.cu); the record is cleared.  The normal build has no
+ * 5 hora_group_attention.cu, 6 hora_group_attention_main.cu with what it includes, 7 hora_verify.cu,
+ * 10 hora_packed_attention.cu, 11 hora_packed_attention_forward.cu, 12 hora_packed_attention_backward.cu); the record is cleared.  The normal build has no
  * checks and returns -1; -2 reports a failed synchronisation.
  */
 int32_t hora_checked_violation(void);

@@ -1,0 +1,69 @@
+// hora_packed_attention and its backward pass: what their kernels share.
+//
+// The packed tokens hold S sequences one after the other.  A query sees keys of its own sequence and, where that is a rollout, its group's
+// prompt, the sequence in front of the group's rollouts.  Both are runs of tokens, and in the causal case "sees" is: the key
+// lies in one of the two runs and not behind the query.  Seen from a key: the queries are one run, from the key to the end of its
+// sequence, or of its group if it is of a prompt.
+//   A tile of queries is tp tokens times hp heads of one cache head's g (hp divides g, hp * tp <= 128): all of them read the same keys.
+// Few tokens to a tile mean that the causal border cuts off little of it, and short sequences fill it.  A plan lists the tiles by
+// falling number of steps; CTAs, one to an SM, deal them out in turn (forwards and backwards, like cards), so none has much more to do.
+#pragma once
+
+#include "hora_checked.cuh"
+#include "hora_rows16.cuh"
+#include "hora_tensor.cuh"
+
+namespace hora {
+
+constexpr int kPackedRows = 128;                         // rows of a tile, keys of a step
+constexpr int kPackedThreads = 384;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Tokens whose queries are an item, their sequence's begin and end, and the prompt's.
+struct QueryItem {
+    int32_t token0, tokens, own0, end, shared0, shared1, pad[2];
+};
+// Keys that are an item, and the run of tokens whose queries may see them.
+struct KeyItem {
+    int32_t key0, keys, q0, q1;
+};
+
+struct PackedArgs {
+    const int64_t *seq_offsets, *group_offsets;
+    const void *out_in, *dout, *v;                       // of the backward pass's first kernel
+    void *out, *dq, *dk, *dv;
+    float *lse;
+    int32_t *status;
+    int64_t out_stride, dout_stride, kv_stride, dq_stride, dkv_stride;
+    int32_t S, N, T, Hq, Hkv, D, g, hp, tp, blocks;       // blocks: of hp heads, of all query heads
+    int32_t causal, half;                                // half: fp16 (weights and gradients of scores are held relative to a scale, see below)
+    float scale, scale_log2;
+    int32_t tile_tokens;                                 // tokens of a query item
+    int32_t query_cap, key_cap;
+    // workspace
+    int32_t *counts;                                     // query items, key items, bits of the largest |dout row|^2 and |v row|^2
+    QueryItem *query_items;
+    KeyItem *key_items;
+    float2 *stats;                                       // [T][Hq] (lse in units of log2, dout . out)
+};
+
+// The r-th item of a CTA: all rounds but the last are full.
+__device__ __forceinline__ int64_t dealt(int32_t r) {
+    return (int64_t)r * gridDim.x + ((r & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+}
+
+// In fp16 the smallest weights and gradients of scores would be lost: weights are held times 2^10, gradients of scores times a power
+// of two under which none of them can pass 2^15 (|dS| <= 2 |dout row| |v row|, P <= 1).  bf16 has fp32's exponents: no scale.
+constexpr int kHalfShift = 10;
+__device__ __forceinline__ int gradient_shift(const PackedArgs &a) {
+    if (!a.half) return 0;
+    const float d = __int_as_float(__ldcg(a.counts + 2)), v = __int_as_float(__ldcg(a.counts + 3));
+    const float bound = 2.f * sqrtf(d) * sqrtf(v);
+    if (!(bound > 0.f) || bound > 1e30f) return 0;
+    return max(-60, min(60, 14 - ilogbf(bound)));
+}
+
+hora_status_t launch_packed_forward(const PackedArgs &a, const void *q, const void *k, const void *v, int64_t q_stride, int32_t dtype, cudaStream_t stream);
+hora_status_t launch_packed_backward(const PackedArgs &a, const void *q, const void *k, const void *v, int64_t q_stride, int32_t dtype, cudaStream_t stream);
+
+}  // namespace hora

@@ -1,0 +1,760 @@
+// hora_packed_attention_backward: gradients of keys and values, and of queries.
+//
+//   P = 2^(scale q.k - lse) (in units of log2),  dP = dout . v,  dS = P (dP - dout . out)
+//   dV = P^T dO, dK = scale dS^T Q  (sums over queries and the heads of a cache head)      dQ = scale dS K  (a sum over keys)
+//
+// Two kernels, each with its sums in tensor memory from the first step to the last, so no sum depends on an order and nothing is
+// added up in memory; the price is that S and dP are computed twice (seven products where five would do).
+//   Keys: an item is 128 keys of one cache head and all queries that may see them, 128 rows (tokens times heads) a step.  S^T = K Q^T and dP^T = V dO^T
+// have the keys as rows: P^T and dS^T replace them in tensor memory in 16 bits and are the left operands of dV += P^T dO and dK += dS^T Q, for
+// which the same tiles of dO and Q are read the other way round.  Nothing but the four operands ever is in shared memory.
+//   Queries: an item is one tile of queries; S = Q K^T, dP = dO V^T, dQ += dS K.
+//   Eight warps do what is between the products, two threads to a row, 64 columns each; while they work on the weights of a step the tensor
+// cores compute its dP, and while they work on its dS the tensor cores have the next step's scores to do.
+//   Rows of a tile that are not of the run of queries (or keys) are cleared in shared memory where a product sums over them.
+//   Every wait has a limit; a wait that reaches it makes the CTA give up and report HORA_ERR_INTERNAL.
+#define HORA_FILE_ID 12
+#include <type_traits>
+
+#include "hora_packed_attention.cuh"
+
+HORA_CHECKED_REGISTER()
+
+namespace hora {
+
+namespace {
+
+constexpr int kTile = kPackedRows, kHalfTile = kTile / 2;
+constexpr int kMiddleThreads = 256, kLoadWarp = 8, kProductWarp = 9, kStatsThreads = 64;
+
+template <typename Q>
+constexpr uint32_t kType = std::is_same<Q, __nv_bfloat16>::value ? 1u : 0u;
+template <typename Q>
+constexpr uint32_t kIdescScores = (1u << 4) | (kType<Q> << 7) | (kType<Q> << 10) | ((kTile / 8) << 17) | ((kTile / 16) << 24);
+template <typename Q, int D>
+constexpr uint32_t kIdescSum = (1u << 4) | (kType<Q> << 7) | (kType<Q> << 10) | (1u << 16) | ((D / 8) << 17) | ((kTile / 16) << 24);
+
+// The product of two tiles of 128 rows over D: rows of `a` by rows of `b`.  One elected lane.
+template <typename Q, int D>
+__device__ __forceinline__ void product_of_rows(uint32_t d, uint32_t a, uint32_t b) {
+#pragma unroll
+    for (int x = 0; x < D / 16; ++x) {
+        const uint32_t off = ((x >> 2) * (kTile * 128) + (x & 3) * 32) >> 4;
+        mma_smem(d, a + off, b + off, kIdescScores<Q>, x > 0);
+    }
+}
+// d += w b, w 128 x `count` in tensor memory (16 bits, its two halves of 64 columns 64 columns of 32 bits apart), b `count` rows of D.
+template <typename Q, int D>
+__device__ __forceinline__ void product_with_weights(uint32_t d, uint32_t w, uint32_t b, int32_t count, bool first) {
+#pragma unroll
+    for (int g = 0; g < kTile / 16; ++g)
+        if (g * 16 < count) mma_tmem(d, w + (g < 4 ? g * 8 : kHalfTile + (g - 4) * 8), b + g * (2048 >> 4), kIdescSum<Q, D>, !first || g > 0);
+}
+
+// Rows count .. of a tile up to the last sixteen that a product reads are set to zero.  All lanes of a warp.
+template <int D>
+__device__ __forceinline__ void clear_rows(uint32_t tile, int32_t count) {
+    const int32_t clear = ((count + 15) & ~15) - count;
+    for (int32_t c = lane_id(); c < clear * (D / 8); c += kWarp) {
+        const uint32_t to = tile + (c % (D / 8) >> 3) * (kTile * 128) + (count + c / (D / 8)) * 128 + (c & 7) * 16;
+        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(to), "r"(0) : "memory");
+    }
+}
+
+__device__ __forceinline__ void publish_clears() {
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+}
+
+template <int COLUMNS, typename Q>
+__device__ __forceinline__ void store_row(Q *to, uint32_t from, float f, bool have) {
+#pragma unroll 1
+    for (int b = 0; b < COLUMNS / 32; ++b) {
+        float o[32];
+        tmem_load(from + b * 32, o);
+        tmem_load_wait();
+        if (have) {
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                float x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = o[v * 8 + e] * f;
+                *reinterpret_cast<uint4 *>(to + b * 32 + v * 8) = pack8<Q>(x);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// keys and values
+
+template <int D>
+struct KeysSmem {
+    static constexpr int kTileBytes = kTile * D * 2;
+    static constexpr int kStages = D == 128 ? 2 : 4;
+    static constexpr int kK = 0, kV = kTileBytes, kRing = 2 * kTileBytes;            // a stage: queries, gradients of outputs
+    static constexpr int kSmall = kRing + kStages * 2 * kTileBytes;
+};
+
+struct KeysShared {
+    float lse[4][kTile], delta[4][kTile];                // by stage: -lse, -dout.out, as the exponents and sums need them
+    uint64_t full[4], empty[4], keys, keys_free, scores, weights, products, gradients, sums, sums_free;
+    int32_t failed;
+    uint32_t tmem;
+};
+
+struct KeyWork {
+    int32_t key0, keys, q0, q1, head, steps;
+    bool valid;
+};
+
+__device__ __forceinline__ KeyWork fetch_keys(const PackedArgs &a, int32_t r, int32_t n_items) {
+    const int64_t x = dealt(r);
+    KeyWork w = {};
+    w.valid = x < (int64_t)n_items * a.Hkv;
+    if (!w.valid) return w;
+    const int64_t i = x / a.Hkv;
+    w.head = (int32_t)(x - i * a.Hkv);
+    const int4 v = __ldcg(reinterpret_cast<const int4 *>(a.key_items + i));
+    w.key0 = v.x;
+    w.keys = v.y;
+    w.q0 = v.z;
+    w.q1 = v.w;
+    w.steps = (v.w - v.z + a.tp - 1) / a.tp * (a.g / a.hp);
+    return w;
+}
+
+// Step s: which tokens, which block of heads, how many rows.
+struct KeyStep {
+    int32_t token0, block, count;
+    bool whole;
+};
+__device__ __forceinline__ KeyStep key_step(const PackedArgs &a, const KeyWork &w, int32_t s) {
+    const int32_t per = a.g / a.hp, tile = s / per;
+    KeyStep k;
+    k.token0 = w.q0 + tile * a.tp;
+    k.block = w.head * per + (s - tile * per);
+    const int32_t tokens = min(a.tp, w.q1 - k.token0);
+    k.count = tokens * a.hp;
+    k.whole = tokens == a.tp;
+    return k;
+}
+
+extern __shared__ __align__(1024) uint8_t s_backward[];
+
+template <typename Q, int D>
+__global__ void __launch_bounds__(kPackedThreads, 1)
+packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap do_map,
+                   const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    using Smem = KeysSmem<D>;
+    constexpr int kStages = Smem::kStages, kParts = D / 64;
+    KeysShared &sh = *reinterpret_cast<KeysShared *>(s_backward + Smem::kSmall);
+    const uint32_t base = smem_at(s_backward);
+    const int warp = threadIdx.x >> 5, lane = lane_id();
+    volatile int32_t *failed = &sh.failed;
+    if (base & 1023u) {
+        pdl_enter();
+        raise_status(a.status, HORA_ERR_INTERNAL);
+        return;
+    }
+    const uint32_t full = smem_at(sh.full), empty = smem_at(sh.empty), keys = smem_at(&sh.keys), keys_free = smem_at(&sh.keys_free), scores = smem_at(&sh.scores),
+                   weights = smem_at(&sh.weights), products = smem_at(&sh.products), gradients = smem_at(&sh.gradients), sums = smem_at(&sh.sums),
+                   sums_free = smem_at(&sh.sums_free);
+    if (threadIdx.x == 0) {
+        sh.failed = 0;
+        for (int s = 0; s < kStages; ++s) {
+            bar_init(full + 8 * s, 1 + kStatsThreads);
+            bar_init(empty + 8 * s, 1);
+        }
+        bar_init(keys, 1);
+        bar_init(keys_free, 1);
+        bar_init(scores, 1);
+        bar_init(weights, kMiddleThreads);
+        bar_init(products, 1);
+        bar_init(gradients, kMiddleThreads);
+        bar_init(sums, 1);
+        bar_init(sums_free, kMiddleThreads);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    // rows that no tile of queries fills
+    const int32_t rows = a.hp * a.tp, idle = kTile - rows;
+    for (int32_t c = threadIdx.x; c < 2 * kStages * kParts * idle * 8; c += kPackedThreads) {
+        const int32_t x = c >> 3, part = x / idle;
+        const uint32_t to = base + Smem::kRing + part * (kTile * 128) + (rows + x - part * idle) * 128 + (c & 7) * 16;
+        asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(to), "r"(0) : "memory");
+    }
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_at(&sh.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        fence_before();
+    }
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = sh.tmem;                       // columns: S^T, dP^T, dV, dK
+    pdl_enter();
+    const int32_t n_items = __ldcg(a.counts + 1);
+    const int shift = gradient_shift(a), up = a.half ? kHalfShift : 0;
+    bool ok = true;
+
+    if (warp == kLoadWarp) {
+        if (lane == 0) {
+            int32_t pos = 0;
+            uint32_t turn = 0;
+            KeyWork next = fetch_keys(a, 0, n_items);
+            for (int32_t r = 0; next.valid && ok; ++r, ++turn) {
+                const KeyWork it = next;
+                next = fetch_keys(a, r + 1, n_items);
+                if (r > 0) ok = bar_wait(keys_free, (turn + 1) & 1, failed);
+                if (!ok) break;
+                bar_expect(keys, 2 * Smem::kTileBytes);
+                for (int p = 0; p < kParts; ++p) {
+                    tma_box3(base + Smem::kK + p * (kTile * 128), &k_map, p * 64, it.head, it.key0, keys);
+                    tma_box3(base + Smem::kV + p * (kTile * 128), &v_map, p * 64, it.head, it.key0, keys);
+                }
+                for (int32_t s = 0; s < it.steps; ++s, ++pos) {
+                    const KeyStep k = key_step(a, it, s);
+                    const int stage = pos % kStages;
+                    if (pos >= kStages) ok = bar_wait(empty + 8 * stage, (pos / kStages + 1) & 1, failed);
+                    if (!ok) break;
+                    bar_expect(full + 8 * stage, 2 * kParts * rows * 128);
+                    const uint32_t at = base + Smem::kRing + stage * 2 * Smem::kTileBytes;
+                    for (int p = 0; p < kParts; ++p) {
+                        tma_box3(at + p * (kTile * 128), &q_map, p * 64, k.block * a.hp, k.token0, full + 8 * stage);
+                        tma_box3(at + Smem::kTileBytes + p * (kTile * 128), &do_map, p * 64, k.block * a.hp, k.token0, full + 8 * stage);
+                    }
+                }
+            }
+            if (!ok) {
+                // copies on their way to the CTA: the barriers of their stages may lack the other arrivals, so it is time that is waited for
+                int32_t never = 0;
+                if (turn > 0) bar_wait(keys, (turn - 1) & 1, &never);
+                for (int32_t x = max(0, pos - kStages); x < pos; ++x) bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, &never);
+            }
+        }
+    } else if (warp == kProductWarp) {
+        const uint32_t k_rows = operand(base + Smem::kK, 16), v_rows = operand(base + Smem::kV, 16);
+        uint32_t weights_phase = 0, gradients_phase = 0;
+        int32_t pos = 0;
+        KeyWork next = fetch_keys(a, 0, n_items);
+        for (int32_t r = 0; next.valid && ok; ++r) {
+            const KeyWork it = next;
+            next = fetch_keys(a, r + 1, n_items);
+            auto arrived = [&](int32_t s) {              // the tiles of step s
+                const int32_t x = pos + s;
+                if (!bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, failed)) return false;
+                const KeyStep k = key_step(a, it, s);
+                if (!k.whole && (k.count & 15)) {
+                    const uint32_t at = base + Smem::kRing + (x % kStages) * 2 * Smem::kTileBytes;
+                    clear_rows<D>(at, k.count);
+                    clear_rows<D>(at + Smem::kTileBytes, k.count);
+                    publish_clears();
+                }
+                fence_after();
+                return true;
+            };
+            auto tile = [&](int32_t s, int which, uint32_t lead) {
+                return operand(base + Smem::kRing + ((pos + s) % kStages * 2 + which) * Smem::kTileBytes, lead);
+            };
+            ok = bar_wait(keys, r & 1, failed) && arrived(0);
+            if (!ok) break;
+            if (elect_one()) {
+                product_of_rows<Q, D>(tmem, k_rows, tile(0, 0, 16));
+                mma_commit(scores);
+                product_of_rows<Q, D>(tmem + kTile, v_rows, tile(0, 1, 16));
+                mma_commit(products);
+            }
+            __syncwarp();
+            for (int32_t s = 0; s < it.steps; ++s) {
+                const int32_t count = key_step(a, it, s).count;
+                const bool more = s + 1 < it.steps;
+                ok = bar_wait(weights, weights_phase, failed);
+                weights_phase ^= 1;
+                if (ok && s == 0 && r > 0) ok = bar_wait(sums_free, (r + 1) & 1, failed);
+                if (!ok) break;
+                fence_after();
+                if (elect_one()) product_with_weights<Q, D>(tmem + 256, tmem, tile(s, 1, kTile * 128), count, s == 0);
+                __syncwarp();
+                if (more) {
+                    ok = arrived(s + 1);
+                    if (!ok) break;
+                    if (elect_one()) {
+                        product_of_rows<Q, D>(tmem, k_rows, tile(s + 1, 0, 16));
+                        mma_commit(scores);
+                    }
+                    __syncwarp();
+                }
+                ok = bar_wait(gradients, gradients_phase, failed);
+                gradients_phase ^= 1;
+                if (!ok) break;
+                fence_after();
+                if (elect_one()) {
+                    product_with_weights<Q, D>(tmem + 256 + D, tmem + kTile, tile(s, 0, kTile * 128), count, s == 0);
+                    mma_commit(empty + 8 * ((pos + s) % kStages));
+                    if (more) {
+                        product_of_rows<Q, D>(tmem + kTile, v_rows, tile(s + 1, 1, 16));
+                        mma_commit(products);
+                    } else {
+                        mma_commit(keys_free);
+                        mma_commit(sums);
+                    }
+                }
+                __syncwarp();
+            }
+            pos += it.steps;
+        }
+    } else if (warp > kProductWarp) {
+        // ---- of each row of a step: -lse and -dout.out
+        const int x0 = threadIdx.x - (kProductWarp + 1) * kWarp;
+        const float c = exp2f((float)(shift - up));
+        int32_t pos = 0;
+        KeyWork next = fetch_keys(a, 0, n_items);
+        for (int32_t r = 0; next.valid && ok; ++r) {
+            const KeyWork it = next;
+            next = fetch_keys(a, r + 1, n_items);
+            for (int32_t s = 0; s < it.steps; ++s, ++pos) {
+                const KeyStep k = key_step(a, it, s);
+                const int stage = pos % kStages;
+                float2 st[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int32_t row = x0 + i * kStatsThreads, token = k.token0 + row / a.hp;
+                    st[i] = make_float2(INFINITY, 0.f);
+                    if (row < k.count && HORA_IN(token, a.T)) st[i] = __ldcg(a.stats + (int64_t)token * a.Hq + k.block * a.hp + row % a.hp);
+                }
+                if (pos >= kStages) ok = bar_wait(empty + 8 * stage, (pos / kStages + 1) & 1, failed);
+                if (!ok) break;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    sh.lse[stage][x0 + i * kStatsThreads] = (float)up - st[i].x;
+                    sh.delta[stage][x0 + i * kStatsThreads] = -st[i].y * c;
+                }
+                bar_arrive(full + 8 * stage);
+            }
+        }
+    } else {
+        // ---- between the products: thread `row` of either half has 64 columns (queries) of a key
+        const int half = warp >> 2, row = threadIdx.x & (kTile - 1);
+        const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
+        const uint32_t t_s = lanes + half * kHalfTile, t_dp = lanes + kTile + half * kHalfTile;
+        const float c = exp2f((float)(shift - up));
+        const float2 scale2 = make_float2(a.scale_log2, a.scale_log2), c2 = make_float2(c, c);
+        uint32_t phase = 0;
+        int32_t pos = 0;
+        KeyWork next = fetch_keys(a, 0, n_items);
+        for (int32_t r = 0; next.valid && ok; ++r) {
+            const KeyWork it = next;
+            next = fetch_keys(a, r + 1, n_items);
+            for (int32_t s = 0; s < it.steps; ++s, ++pos, phase ^= 1) {
+                const KeyStep k = key_step(a, it, s);
+                const int stage = pos % kStages;
+                ok = bar_wait(full + 8 * stage, (pos / kStages) & 1, failed) && bar_wait(scores, phase, failed);
+                ok = __all_sync(kFull, ok);
+                if (!ok) break;
+                fence_after();
+                float p[2][32];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) tmem_load(t_s + b * 32, p[b]);
+                tmem_load_wait();
+                const float4 *lse = reinterpret_cast<const float4 *>(sh.lse[stage] + half * kHalfTile);
+                // causal: the query's token may not be in front of the key
+                const bool border = a.causal && k.token0 < it.key0 + it.keys - 1;
+                const int32_t from = border ? (it.key0 + row - k.token0) * a.hp - half * kHalfTile : 0;
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float4 z = lse[b * 4 + e];
+                        float *x = p[b >> 1] + (b & 1) * 16 + 4 * e;
+                        float2 y0 = fma2(make_float2(x[0], x[1]), scale2, make_float2(z.x, z.y)), y1 = fma2(make_float2(x[2], x[3]), scale2, make_float2(z.z, z.w));
+                        x[0] = exp2_approx(y0.x);
+                        x[1] = exp2_approx(y0.y);
+                        x[2] = exp2_approx(y1.x);
+                        x[3] = exp2_approx(y1.y);
+                        if (border) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (b * 16 + 4 * e + i < from) x[i] = 0.f;
+                        }
+                        w[2 * e] = pack2(x[0], x[1], Q());
+                        w[2 * e + 1] = pack2(x[2], x[3], Q());
+                    }
+                    tmem_store8(t_s + b * 8, w);
+                }
+                tmem_store_wait();
+                fence_before();
+                bar_arrive(weights);
+                ok = bar_wait(products, phase, failed);
+                ok = __all_sync(kFull, ok);
+                if (!ok) break;
+                fence_after();
+                const float4 *delta = reinterpret_cast<const float4 *>(sh.delta[stage] + half * kHalfTile);
+                float dp[2][32];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) tmem_load(t_dp + b * 32, dp[b]);
+                tmem_load_wait();
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float4 z = delta[b * 4 + e];
+                        const float *x = p[b >> 1] + (b & 1) * 16 + 4 * e, *d = dp[b >> 1] + (b & 1) * 16 + 4 * e;
+                        const float2 y0 = mul2(make_float2(x[0], x[1]), fma2(make_float2(d[0], d[1]), c2, make_float2(z.x, z.y)));
+                        const float2 y1 = mul2(make_float2(x[2], x[3]), fma2(make_float2(d[2], d[3]), c2, make_float2(z.z, z.w)));
+                        w[2 * e] = pack2(y0.x, y0.y, Q());
+                        w[2 * e + 1] = pack2(y1.x, y1.y, Q());
+                    }
+                    tmem_store8(t_dp + b * 8, w);
+                }
+                tmem_store_wait();
+                fence_before();
+                bar_arrive(gradients);
+            }
+            if (!ok) break;
+            ok = bar_wait(sums, r & 1, failed);
+            ok = __all_sync(kFull, ok);
+            if (!ok) break;
+            fence_after();
+            const int64_t to = (int64_t)(it.key0 + row) * a.dkv_stride + (int64_t)it.head * D;
+            store_row<D>(static_cast<Q *>(half ? a.dk : a.dv) + to, lanes + 256 + half * D, half ? a.scale * exp2f((float)-shift) : exp2f((float)-up), row < it.keys);
+            fence_before();
+            bar_arrive(sums_free);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && sh.failed) raise_status(a.status, HORA_ERR_INTERNAL);
+    if (warp == 0) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------------
+// queries
+
+template <int D>
+struct QueriesSmem {
+    static constexpr int kTileBytes = kTile * D * 2;
+    static constexpr int kStages = D == 128 ? 5 : 10;    // keys or values
+    static constexpr int kQ = 0, kDo = kTileBytes, kRing = 2 * kTileBytes, kSmall = kRing + kStages * kTileBytes;
+};
+
+struct QueriesShared {
+    uint64_t full[10], empty[10], queries, queries_free, scores, scores_free, products, gradients, sums, sums_free;
+    int32_t failed;
+    uint32_t tmem;
+};
+
+struct QueryWork {
+    int32_t token0, tokens, own0, end, shared0, shared1, block, n_shared, n;
+    bool valid;
+
+    __device__ __forceinline__ void keys(int32_t j, int32_t &key0, int32_t &count) const {
+        key0 = j < n_shared ? shared0 + j * kTile : own0 + (j - n_shared) * kTile;
+        count = min(kTile, (j < n_shared ? shared1 : end) - key0);
+    }
+};
+
+__device__ __forceinline__ QueryWork fetch_queries(const PackedArgs &a, int32_t r, int32_t n_items) {
+    const int64_t x = dealt(r);
+    QueryWork w = {};
+    w.valid = x < (int64_t)n_items * a.blocks;
+    if (!w.valid) return w;
+    const int64_t i = x / a.blocks;
+    w.block = (int32_t)(x - i * a.blocks);
+    const int4 *p = reinterpret_cast<const int4 *>(a.query_items + i);
+    const int4 u = __ldcg(p), v = __ldcg(p + 1);
+    w.token0 = u.x;
+    w.tokens = u.y;
+    w.own0 = u.z;
+    w.end = u.w;
+    w.shared0 = v.x;
+    w.shared1 = v.y;
+    w.n_shared = (v.y - v.x + kTile - 1) / kTile;
+    w.n = w.n_shared + ((a.causal ? u.x + u.y : u.w) - u.z + kTile - 1) / kTile;
+    return w;
+}
+
+template <typename Q, int D>
+__global__ void __launch_bounds__(kPackedThreads, 1)
+packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap do_map,
+                      const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
+    using Smem = QueriesSmem<D>;
+    constexpr int kStages = Smem::kStages, kParts = D / 64;
+    QueriesShared &sh = *reinterpret_cast<QueriesShared *>(s_backward + Smem::kSmall);
+    const uint32_t base = smem_at(s_backward);
+    const int warp = threadIdx.x >> 5, lane = lane_id();
+    volatile int32_t *failed = &sh.failed;
+    if (base & 1023u) {
+        pdl_enter();
+        raise_status(a.status, HORA_ERR_INTERNAL);
+        return;
+    }
+    const uint32_t full = smem_at(sh.full), empty = smem_at(sh.empty), queries = smem_at(&sh.queries), queries_free = smem_at(&sh.queries_free),
+                   scores = smem_at(&sh.scores), scores_free = smem_at(&sh.scores_free), products = smem_at(&sh.products), gradients = smem_at(&sh.gradients),
+                   sums = smem_at(&sh.sums), sums_free = smem_at(&sh.sums_free);
+    if (threadIdx.x == 0) {
+        sh.failed = 0;
+        for (int s = 0; s < kStages; ++s) {
+            bar_init(full + 8 * s, 1);
+            bar_init(empty + 8 * s, 1);
+        }
+        bar_init(queries, 1);
+        bar_init(queries_free, 1);
+        bar_init(scores, 1);
+        bar_init(scores_free, kMiddleThreads);
+        bar_init(products, 1);
+        bar_init(gradients, kMiddleThreads);
+        bar_init(sums, 1);
+        bar_init(sums_free, kMiddleThreads);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_at(&sh.tmem)) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        fence_before();
+    }
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = sh.tmem;                       // columns: S, dP, dQ
+    pdl_enter();
+    const int32_t n_items = __ldcg(a.counts);
+    const int shift = gradient_shift(a), up = a.half ? kHalfShift : 0;
+    bool ok = true;
+
+    if (warp == kLoadWarp) {
+        if (lane == 0) {
+            int32_t pos = 0;
+            uint32_t turn = 0;
+            QueryWork next = fetch_queries(a, 0, n_items);
+            for (int32_t r = 0; next.valid && ok; ++r, ++turn) {
+                const QueryWork it = next;
+                next = fetch_queries(a, r + 1, n_items);
+                const int32_t head = it.block * a.hp / a.g;
+                if (r > 0) ok = bar_wait(queries_free, (turn + 1) & 1, failed);
+                if (!ok) break;
+                bar_expect(queries, 2 * kParts * a.hp * a.tp * 128);
+                for (int p = 0; p < kParts; ++p) {
+                    tma_box3(base + Smem::kQ + p * (kTile * 128), &q_map, p * 64, it.block * a.hp, it.token0, queries);
+                    tma_box3(base + Smem::kDo + p * (kTile * 128), &do_map, p * 64, it.block * a.hp, it.token0, queries);
+                }
+                for (int32_t j = 0; j < it.n && ok; ++j) {
+                    int32_t key0, count;
+                    it.keys(j, key0, count);
+                    for (int which = 0; which < 2; ++which, ++pos) {
+                        const int stage = pos % kStages;
+                        if (pos >= kStages) ok = bar_wait(empty + 8 * stage, (pos / kStages + 1) & 1, failed);
+                        if (!ok) break;
+                        bar_expect(full + 8 * stage, Smem::kTileBytes);
+                        for (int p = 0; p < kParts; ++p)
+                            tma_box3(base + Smem::kRing + stage * Smem::kTileBytes + p * (kTile * 128), which ? &v_map : &k_map, p * 64, head, key0, full + 8 * stage);
+                    }
+                }
+            }
+            if (!ok) {
+                int32_t never = 0;
+                if (turn > 0) bar_wait(queries, (turn - 1) & 1, &never);
+                for (int32_t x = max(0, pos - kStages); x < pos; ++x) bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, &never);
+            }
+        }
+    } else if (warp == kProductWarp) {
+        const uint32_t q_rows = operand(base + Smem::kQ, 16), do_rows = operand(base + Smem::kDo, 16);
+        uint32_t free_phase = 0, gradients_phase = 0;
+        int32_t pos = 0;
+        QueryWork next = fetch_queries(a, 0, n_items);
+        for (int32_t r = 0; next.valid && ok; ++r) {
+            const QueryWork it = next;
+            next = fetch_queries(a, r + 1, n_items);
+            auto at = [&](int32_t j, int which) { return base + Smem::kRing + (uint32_t)((pos + 2 * j + which) % kStages) * Smem::kTileBytes; };
+            auto arrived = [&](int32_t j, int which) {
+                const int32_t x = pos + 2 * j + which;
+                if (!bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, failed)) return false;
+                int32_t key0, count;
+                it.keys(j, key0, count);
+                if (which == 0 && (count & 15)) {
+                    clear_rows<D>(at(j, 0), count);
+                    publish_clears();
+                }
+                fence_after();
+                return true;
+            };
+            auto scores_of = [&](int32_t j) {
+                if (elect_one()) {
+                    product_of_rows<Q, D>(tmem, q_rows, operand(at(j, 0), 16));
+                    mma_commit(scores);
+                }
+                __syncwarp();
+            };
+            auto products_of = [&](int32_t j) {
+                if (elect_one()) {
+                    product_of_rows<Q, D>(tmem + kTile, do_rows, operand(at(j, 1), 16));
+                    mma_commit(products);
+                    mma_commit(empty + 8 * ((pos + 2 * j + 1) % kStages));
+                    if (j + 1 == it.n) mma_commit(queries_free);
+                }
+                __syncwarp();
+            };
+            ok = bar_wait(queries, r & 1, failed) && arrived(0, 0);
+            // the scores of the item before have been read: its last gradients came after that
+            if (!ok) break;
+            if (r > 0) {
+                ok = bar_wait(scores_free, free_phase, failed);
+                free_phase ^= 1;
+                if (!ok) break;
+                fence_after();
+            }
+            scores_of(0);
+            ok = arrived(0, 1);
+            if (!ok) break;
+            products_of(0);
+            for (int32_t j = 0; j < it.n; ++j) {
+                const bool more = j + 1 < it.n;
+                if (more) {
+                    ok = bar_wait(scores_free, free_phase, failed);
+                    free_phase ^= 1;
+                    if (!ok || !arrived(j + 1, 0)) { ok = false; break; }
+                    scores_of(j + 1);
+                }
+                ok = bar_wait(gradients, gradients_phase, failed);
+                gradients_phase ^= 1;
+                if (ok && j == 0 && r > 0) ok = bar_wait(sums_free, (r + 1) & 1, failed);
+                if (!ok) break;
+                fence_after();
+                if (elect_one()) {
+                    int32_t key0, count;
+                    it.keys(j, key0, count);
+                    product_with_weights<Q, D>(tmem + 256, tmem + kTile, operand(at(j, 0), kTile * 128), count, j == 0);
+                    mma_commit(empty + 8 * ((pos + 2 * j) % kStages));
+                    if (!more) mma_commit(sums);
+                }
+                __syncwarp();
+                if (more) {
+                    ok = arrived(j + 1, 1);
+                    if (!ok) break;
+                    products_of(j + 1);
+                }
+            }
+            pos += 2 * it.n;
+        }
+    } else if (warp < 8) {
+        const int half = warp >> 2, row = threadIdx.x & (kTile - 1);
+        const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
+        const uint32_t t_s = lanes + half * kHalfTile, t_dp = lanes + kTile + half * kHalfTile;
+        const int32_t row_token = row / a.hp, row_head = row - row_token * a.hp;
+        const float c = exp2f((float)(shift - up));
+        const float2 scale2 = make_float2(a.scale_log2, a.scale_log2), c2 = make_float2(c, c);
+        auto stats_of = [&](const QueryWork &w) {
+            float2 st = make_float2(INFINITY, 0.f);
+            if (w.valid && row_token < w.tokens && HORA_IN(w.token0 + row_token, a.T)) st = __ldcg(a.stats + (int64_t)(w.token0 + row_token) * a.Hq + w.block * a.hp + row_head);
+            return st;
+        };
+        uint32_t phase = 0;
+        QueryWork next = fetch_queries(a, 0, n_items);
+        float2 st = stats_of(next);
+        for (int32_t r = 0; next.valid && ok; ++r) {
+            const QueryWork it = next;
+            const float2 lse2 = make_float2((float)up - st.x, (float)up - st.x), delta2 = make_float2(-st.y * c, -st.y * c);
+            next = fetch_queries(a, r + 1, n_items);
+            st = stats_of(next);
+            const bool have = row_token < it.tokens;
+            const int32_t token = it.token0 + row_token;
+            const int32_t seen_to = a.causal && have ? min(it.end, token + 1) : it.end;
+            for (int32_t j = 0; j < it.n; ++j, phase ^= 1) {
+                const int32_t limit = (j < it.n_shared ? it.shared1 - it.shared0 - j * kTile : seen_to - it.own0 - (j - it.n_shared) * kTile) - half * kHalfTile;
+                ok = bar_wait(scores, phase, failed);
+                ok = __all_sync(kFull, ok);
+                if (!ok) break;
+                fence_after();
+                float p[2][32];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) tmem_load(t_s + b * 32, p[b]);
+                tmem_load_wait();
+                fence_before();
+                bar_arrive(scores_free);
+                const bool border = __any_sync(kFull, limit < kHalfTile);
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        const float2 y = fma2(make_float2(p[b][e], p[b][e + 1]), scale2, lse2);
+                        p[b][e] = exp2_approx(y.x);
+                        p[b][e + 1] = exp2_approx(y.y);
+                    }
+                ok = bar_wait(products, phase, failed);
+                ok = __all_sync(kFull, ok);
+                if (!ok) break;
+                fence_after();
+                float dp[2][32];
+#pragma unroll
+                for (int b = 0; b < 2; ++b) tmem_load(t_dp + b * 32, dp[b]);
+                tmem_load_wait();
+#pragma unroll
+                for (int b = 0; b < 4; ++b) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float *x = p[b >> 1] + (b & 1) * 16 + 2 * e, *d = dp[b >> 1] + (b & 1) * 16 + 2 * e;
+                        float2 y = mul2(make_float2(x[0], x[1]), fma2(make_float2(d[0], d[1]), c2, delta2));
+                        if (border) {                    // keys of others may hold anything
+                            if (b * 16 + 2 * e >= limit) y.x = 0.f;
+                            if (b * 16 + 2 * e + 1 >= limit) y.y = 0.f;
+                        }
+                        w[e] = pack2(y.x, y.y, Q());
+                    }
+                    tmem_store8(t_dp + b * 8, w);
+                }
+                tmem_store_wait();
+                fence_before();
+                bar_arrive(gradients);
+            }
+            if (!ok) break;
+            ok = bar_wait(sums, r & 1, failed);
+            ok = __all_sync(kFull, ok);
+            if (!ok) break;
+            fence_after();
+            store_row<D / 2>(static_cast<Q *>(a.dq) + (int64_t)token * a.dq_stride + (int64_t)(it.block * a.hp + row_head) * D + half * (D / 2),
+                             lanes + 256 + half * (D / 2), a.scale * exp2f((float)-shift), have);
+            fence_before();
+            bar_arrive(sums_free);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (threadIdx.x == 0 && sh.failed) raise_status(a.status, HORA_ERR_INTERNAL);
+    if (warp == 0) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+    }
+}
+
+template <typename Q, int D>
+hora_status_t launch_backward(const PackedArgs &a, const void *q, const void *k, const void *v, int64_t q_stride, int32_t dtype, cudaStream_t stream) {
+    CUtensorMap q_map, do_map, k_map, v_map;
+    if (!head_map(&q_map, q, dtype, D, a.Hq, a.T, q_stride, a.hp, a.tp) || !head_map(&do_map, a.dout, dtype, D, a.Hq, a.T, a.dout_stride, a.hp, a.tp) ||
+        !head_map(&k_map, k, dtype, D, a.Hkv, a.T, a.kv_stride, 1, kTile) || !head_map(&v_map, v, dtype, D, a.Hkv, a.T, a.kv_stride, 1, kTile))
+        return HORA_ERR_CUDA;
+    constexpr int kKeysSmem = KeysSmem<D>::kSmall + (int)sizeof(KeysShared), kQueriesSmem = QueriesSmem<D>::kSmall + (int)sizeof(QueriesShared);
+    static std::atomic<uint64_t> keys_devices{0}, queries_devices{0};
+    cudaError_t e = allow_shared(reinterpret_cast<const void *>(packed_keys_kernel<Q, D>), kKeysSmem, keys_devices);
+    if (e == cudaSuccess) e = allow_shared(reinterpret_cast<const void *>(packed_queries_kernel<Q, D>), kQueriesSmem, queries_devices);
+    if (e == cudaSuccess)
+        e = launch_pdl(packed_keys_kernel<Q, D>, clamp_grid((int64_t)a.key_cap * a.Hkv, 1), kPackedThreads, kKeysSmem, stream, a, q_map, do_map, k_map, v_map);
+    if (e == cudaSuccess)
+        e = launch_pdl(packed_queries_kernel<Q, D>, clamp_grid((int64_t)a.query_cap * a.blocks, 1), kPackedThreads, kQueriesSmem, stream, a, q_map, do_map, k_map, v_map);
+    count_launches(2);
+    return cuda_ok(e);
+}
+
+}  // namespace
+
+hora_status_t launch_packed_backward(const PackedArgs &a, const void *q, const void *k, const void *v, int64_t q_stride, int32_t dtype, cudaStream_t stream) {
+    if (dtype == HORA_DTYPE_BF16)
+        return a.D == 128 ? launch_backward<__nv_bfloat16, 128>(a, q, k, v, q_stride, dtype, stream) : launch_backward<__nv_bfloat16, 64>(a, q, k, v, q_stride, dtype, stream);
+    return a.D == 128 ? launch_backward<__half, 128>(a, q, k, v, q_stride, dtype, stream) : launch_backward<__half, 64>(a, q, k, v, q_stride, dtype, stream);
+}
+
+}  // namespace hora

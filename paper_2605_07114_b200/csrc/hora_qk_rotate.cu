@@ -1,0 +1,341 @@
+// hora_qk_rotate, hora_qk_rotate_backward: norms of queries and keys for each head with the position rotation in the same pass.
+//
+//   r = 1 / sqrt(mean x^2 + eps), z = x r w, y = R z      R turns the pairs (a, b) of z: (a cos - b sin, a sin + b cos)
+//   g = R^T dy, dx = r (w g - x r mean(x r w g)), dw = sum over rows of x r g
+//
+// A row (one token, one head) lies in D / 8 neighbouring lanes, eight values each, so the mean is three or four shuffles and the
+// other value of a pair (i, i + rot/2) one more.  Such a group of lanes takes one token and several of its heads, one after the other: the
+// angles are worked out once for all of them, in 64 bits up to the fraction of a turn (a position of 10^5 times a frequency of 1
+// has lost 2^-8 of a radian in 32 bits), the weights are held in registers, and four heads' loads are in flight.
+//   What bounds it: HBM.  Nothing is read twice and nothing but the results is written.
+#define HORA_FILE_ID 8
+#include "hora_rows16.cuh"
+
+namespace hora {
+
+constexpr int kRotateThreads = 256;
+constexpr int kRotateHeads = 4;                          // heads whose loads are in flight together
+constexpr int kRotateUnits = 9472;                       // groups of lanes that fill the device: 148 * 8 warps of two, four times over
+constexpr int kRotatePerSm = 4;                          // CTAs of the backward pass an SM; each has a place for its part of the weights' gradients
+
+struct RotateArgs {
+    const void *x[2], *dy[2];                            // queries, keys
+    void *y[2];                                          // what is written: y, or dx
+    const float *w[2];
+    int64_t x_stride[2], dy_stride[2], y_stride[2];
+    const int32_t *positions;
+    const double *inv_freq;
+    int64_t units;
+    int32_t Hq, H, chunks, heads;                        // heads of a chunk
+    int32_t rot;
+    float eps;
+    float *parts;                                        // [CTAs][2][D]
+};
+
+template <int LANES>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+    for (int d = LANES / 2; d > 0; d >>= 1) v += __shfl_xor_sync(kFull, v, d);
+    return v;
+}
+
+// Cosines and sines of a lane's eight values; the sine's sign is that of its place in the pair, times `way` (-1: backwards).
+// `other`: how far away the lane with the other values of the pairs is (0 with neighbouring pairs, whose four angles come twice).
+template <int D, bool PAIRS>
+struct Turn {
+    float c[8], s[8];
+    int other;
+    bool turned;
+
+    __device__ __forceinline__ Turn(const RotateArgs &a, int64_t token, bool have, int lane, float way) {
+        const int e0 = lane * 8, half = a.rot / 2;
+        turned = have && e0 < a.rot;
+        const bool first = PAIRS || e0 < half;
+        other = PAIRS || e0 >= a.rot ? 0 : first ? half / 8 : -(half / 8);
+        const double at = turned ? (double)__ldcg(a.positions + token) : 0.0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (PAIRS && (i & 1)) continue;
+            const int f = PAIRS ? (e0 + i) / 2 : first ? e0 + i : e0 - half + i;
+            const double turns = turned ? at * (__ldca(a.inv_freq + f) * 0.15915494309189535) : 0.0;
+            float sn, cs;
+            sincospif(2.f * (float)(turns - rint(turns)), &sn, &cs);
+            sn *= way;
+            if constexpr (PAIRS) {
+                c[i] = c[i + 1] = cs;
+                s[i] = -sn;
+                s[i + 1] = sn;
+            } else {
+                c[i] = cs;
+                s[i] = first ? -sn : sn;
+            }
+        }
+    }
+
+    // all lanes of the warp
+    __device__ __forceinline__ void apply(float (&z)[8], int lane_in_warp) const {
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = PAIRS ? z[i ^ 1] : __shfl_sync(kFull, z[i], lane_in_warp + other);
+        if (turned) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = z[i] * c[i] + p[i] * s[i];
+        }
+    }
+};
+
+// One group's part: a token and `heads` of its heads.
+template <typename T, int D, bool PAIRS, bool BACKWARD>
+__device__ __forceinline__ void rotate_unit(const RotateArgs &a, int64_t unit, bool have, const float (&w)[2][8], float (&dw)[2][8]) {
+    constexpr int kLanes = D / 8;
+    const int lane_in_warp = lane_id(), lane = lane_in_warp % kLanes;
+    const int64_t token = have ? (a.chunks == 1 ? unit : unit / a.chunks) : 0;
+    const int32_t h0 = have && a.chunks > 1 ? (int32_t)(unit - token * a.chunks) * a.heads : 0;
+    const Turn<D, PAIRS> turn(a, token, have, lane, BACKWARD ? -1.f : 1.f);
+    for (int32_t b = 0; b < a.heads; b += kRotateHeads) {
+        Raw8<T> x[kRotateHeads], dy[kRotateHeads];
+#pragma unroll
+        for (int i = 0; i < kRotateHeads; ++i) {
+            const int32_t h = h0 + b + i;
+            const bool is_k = h >= a.Hq, mine = have && b + i < a.heads && h < a.H;
+            const int64_t at = (int64_t)(is_k ? h - a.Hq : h) * D + lane * 8;
+            zero8(x[i]);
+            if (mine && (!BACKWARD || (is_k ? a.w[1] : a.w[0]) != nullptr)) load8(x[i], static_cast<const T *>((is_k ? a.x[1] : a.x[0])) + token * (is_k ? a.x_stride[1] : a.x_stride[0]) + at);
+            if constexpr (BACKWARD) {
+                zero8(dy[i]);
+                if (mine) load8(dy[i], static_cast<const T *>((is_k ? a.dy[1] : a.dy[0])) + token * (is_k ? a.dy_stride[1] : a.dy_stride[0]) + at);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kRotateHeads; ++i) {
+            const int32_t h = h0 + b + i;
+            const bool is_k = h >= a.Hq, mine = have && b + i < a.heads && h < a.H;
+            if (!__any_sync(kFull, mine)) break;
+            const bool norm = mine && (is_k ? a.w[1] : a.w[0]) != nullptr;
+            float z[8];
+            widen8(x[i], z);
+            float sum = 0.f;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += z[e] * z[e];
+            const float r = rsqrtf(group_sum<kLanes>(sum) * (1.f / D) + a.eps);
+            if constexpr (!BACKWARD) {
+                if (norm) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = z[e] * r * (is_k ? w[1][e] : w[0][e]);
+                }
+                turn.apply(z, lane_in_warp);
+            } else {
+                float g[8], dot = 0.f;
+                widen8(dy[i], g);
+                turn.apply(g, lane_in_warp);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    z[e] *= r;
+                    const float step = z[e] * g[e];
+                    if (norm) {
+                        if (is_k) dw[1][e] += step;
+                        else dw[0][e] += step;
+                    }
+                    g[e] *= is_k ? w[1][e] : w[0][e];
+                    dot += z[e] * g[e];
+                }
+                dot = group_sum<kLanes>(dot) * (1.f / D);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) z[e] = norm ? r * (g[e] - z[e] * dot) : g[e];
+            }
+            if (mine) {
+                Raw8<T> y;
+                narrow8(z, y);
+                store8(y, static_cast<T *>((is_k ? a.y[1] : a.y[0])) + token * (is_k ? a.y_stride[1] : a.y_stride[0]) + (int64_t)(is_k ? h - a.Hq : h) * D + lane * 8);
+            }
+        }
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void load_weights(const RotateArgs &a, float (&w)[2][8]) {
+    const int lane = lane_id() % (D / 8);
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[s][e] = a.w[s] ? __ldca(a.w[s] + lane * 8 + e) : 1.f;
+}
+
+template <typename T, int D, bool PAIRS>
+__global__ void __launch_bounds__(kRotateThreads)
+qk_rotate_kernel(const RotateArgs a) {
+    pdl_enter();
+    constexpr int kGroups = kRotateThreads / (D / 8);
+    float w[2][8], dw[2][8];
+    load_weights<D>(a, w);
+    const int64_t unit = (int64_t)blockIdx.x * kGroups + threadIdx.x / (D / 8);
+    rotate_unit<T, D, PAIRS, false>(a, unit, unit < a.units, w, dw);
+}
+
+template <typename T, int D, bool PAIRS>
+__global__ void __launch_bounds__(kRotateThreads)
+qk_rotate_backward_kernel(const RotateArgs a) {
+    pdl_enter();
+    constexpr int kLanes = D / 8, kGroups = kRotateThreads / kLanes;
+    __shared__ float s_dw[kGroups][2][D + 4];
+    float w[2][8], dw[2][8] = {};
+    load_weights<D>(a, w);
+    const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+    for (int64_t first = (int64_t)blockIdx.x * kGroups; first < a.units; first += (int64_t)gridDim.x * kGroups)
+        rotate_unit<T, D, PAIRS, true>(a, first + group, first + group < a.units, w, dw);
+    if (a.parts == nullptr) return;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s_dw[group][s][lane * 8 + e] = dw[s][e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * D; i += kRotateThreads) {
+        float sum = 0.f;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) sum += s_dw[g][i / D][i % D];
+        a.parts[(int64_t)blockIdx.x * 2 * D + i] = sum;
+    }
+}
+
+// The weights' gradients from the CTAs' parts, always in the same order: 32 columns a CTA, the parts dealt to its warps.
+__global__ void __launch_bounds__(1024)
+qk_rotate_weights_kernel(const float *parts, int32_t n_parts, int32_t D, float *dq_weight, float *dk_weight) {
+    pdl_enter();
+    __shared__ double s_sum[32][33];
+    const int lane = lane_id(), warp = threadIdx.x >> 5, column = blockIdx.x * kWarp + lane;
+    double sum = 0.0;
+    for (int32_t p = warp; p < n_parts; p += 32) sum += (double)__ldcg(parts + (int64_t)p * 2 * D + column);
+    s_sum[warp][lane] = sum;
+    __syncthreads();
+    if (warp != 0) return;
+    sum = 0.0;
+#pragma unroll
+    for (int p = 0; p < 32; ++p) sum += s_sum[p][lane];
+    float *to = column < D ? dq_weight : dk_weight;
+    if (to != nullptr) to[column % D] = (float)sum;
+}
+
+template <typename T, int D, bool PAIRS>
+static cudaError_t launch_rotate(const RotateArgs &a, bool backward, int grid, cudaStream_t stream) {
+    return launch_pdl(backward ? qk_rotate_backward_kernel<T, D, PAIRS> : qk_rotate_kernel<T, D, PAIRS>, grid, kRotateThreads, 0, stream, a);
+}
+
+template <typename T>
+static cudaError_t launch_rotate_of(const RotateArgs &a, int32_t D, bool pairs, bool backward, int grid, cudaStream_t stream) {
+    if (D == 128) return pairs ? launch_rotate<T, 128, true>(a, backward, grid, stream) : launch_rotate<T, 128, false>(a, backward, grid, stream);
+    return pairs ? launch_rotate<T, 64, true>(a, backward, grid, stream) : launch_rotate<T, 64, false>(a, backward, grid, stream);
+}
+
+static bool rows_ok(const void *p, int64_t stride, int32_t heads, int32_t D, int32_t size) {
+    if (heads == 0) return true;
+    return p != nullptr && !(reinterpret_cast<uintptr_t>(p) & 15u) && stride >= (int64_t)heads * D && stride * size % 16 == 0;
+}
+
+static bool rotate_ok(int32_t dtype, int64_t n, int32_t Hq, int32_t Hk, int32_t D, int32_t rot, int32_t layout, float eps) {
+    if (dtype != HORA_DTYPE_F32 && dtype != HORA_DTYPE_BF16 && dtype != HORA_DTYPE_F16) return false;
+    if (n < 0 || n > 0x7FFFFFFF || Hq < 0 || Hk < 0 || Hq > 65536 || Hk > 65536 || Hq + Hk < 1 || (D != 64 && D != 128)) return false;
+    if (rot < 0 || rot > D || rot % 16 || (layout != HORA_ROTATE_HALVES && layout != HORA_ROTATE_PAIRS)) return false;
+    return eps >= 0.f && eps <= 1e30f;
+}
+
+// How the work is cut: whole tokens while there are enough of them, else a few heads to a unit.
+static int units_of(RotateArgs &a, int64_t n, int32_t Hq, int32_t Hk, int32_t D) {
+    a.Hq = Hq;
+    a.H = Hq + Hk;
+    const int64_t most = (a.H + kRotateHeads - 1) / kRotateHeads, want = (kRotateUnits + n - 1) / n;
+    const int32_t chunks = (int32_t)(want < most ? want : most);
+    a.heads = (a.H + chunks - 1) / chunks;
+    a.heads = (a.heads + kRotateHeads - 1) / kRotateHeads * kRotateHeads;
+    a.chunks = (a.H + a.heads - 1) / a.heads;
+    a.units = n * a.chunks;
+    const int64_t groups = kRotateThreads / (D / 8);
+    return (int)((a.units + groups - 1) / groups);
+}
+
+static hora_status_t launch_rotate_as(const RotateArgs &a, int32_t dtype, int32_t D, int32_t layout, bool backward, int grid, cudaStream_t s) {
+    const bool pairs = layout == HORA_ROTATE_PAIRS;
+    const cudaError_t e = dtype == HORA_DTYPE_F32    ? launch_rotate_of<float>(a, D, pairs, backward, grid, s)
+                          : dtype == HORA_DTYPE_BF16 ? launch_rotate_of<__nv_bfloat16>(a, D, pairs, backward, grid, s)
+                                                     : launch_rotate_of<__half>(a, D, pairs, backward, grid, s);
+    count_launches(1);
+    return cuda_ok(e);
+}
+
+}  // namespace hora
+
+extern "C" hora_status_t hora_qk_rotate(const void *q, const void *k, int32_t dtype, int64_t q_row_stride, int64_t k_row_stride, int64_t n_tokens,
+                                        int32_t Hq, int32_t Hk, int32_t D, const int32_t *positions, const double *inv_freq, int32_t rot,
+                                        int32_t layout, const float *q_weight, const float *k_weight, float eps, void *q_out, void *k_out,
+                                        int64_t q_out_row_stride, int64_t k_out_row_stride, void *stream) {
+    using namespace hora;
+    if (!rotate_ok(dtype, n_tokens, Hq, Hk, D, rot, layout, eps)) return HORA_ERR_INVALID_ARG;
+    if (n_tokens == 0) return HORA_OK;
+    const int32_t size = dtype_bytes(dtype);
+    if (!rows_ok(q, q_row_stride, Hq, D, size) || !rows_ok(k, k_row_stride, Hk, D, size) || !rows_ok(q_out, q_out_row_stride, Hq, D, size) ||
+        !rows_ok(k_out, k_out_row_stride, Hk, D, size) || (rot > 0 && (positions == nullptr || inv_freq == nullptr)))
+        return HORA_ERR_INVALID_ARG;
+    RotateArgs a = {};
+    a.x[0] = q; a.x[1] = k;
+    a.x_stride[0] = q_row_stride; a.x_stride[1] = k_row_stride;
+    a.y[0] = q_out; a.y[1] = k_out;
+    a.y_stride[0] = q_out_row_stride; a.y_stride[1] = k_out_row_stride;
+    a.w[0] = q_weight; a.w[1] = k_weight;
+    a.positions = positions;
+    a.inv_freq = inv_freq;
+    a.rot = rot;
+    a.eps = eps;
+    const int grid = units_of(a, n_tokens, Hq, Hk, D);
+    return launch_rotate_as(a, dtype, D, layout, false, grid, static_cast<cudaStream_t>(stream));
+}
+
+extern "C" size_t hora_qk_rotate_backward_workspace_bytes(int32_t D) {
+    return D != 64 && D != 128 ? 0 : (size_t)hora::sm_count() * hora::kRotatePerSm * 2 * D * sizeof(float);
+}
+
+extern "C" hora_status_t hora_qk_rotate_backward(const void *dq_out, const void *dk_out, int32_t dtype, int64_t dq_out_row_stride,
+                                                 int64_t dk_out_row_stride, const void *q, const void *k, int64_t q_row_stride,
+                                                 int64_t k_row_stride, int64_t n_tokens, int32_t Hq, int32_t Hk, int32_t D,
+                                                 const int32_t *positions, const double *inv_freq, int32_t rot, int32_t layout,
+                                                 const float *q_weight, const float *k_weight, float eps, void *dq, void *dk,
+                                                 int64_t dq_row_stride, int64_t dk_row_stride, float *dq_weight, float *dk_weight,
+                                                 void *workspace, size_t workspace_bytes, void *stream) {
+    using namespace hora;
+    if (!rotate_ok(dtype, n_tokens, Hq, Hk, D, rot, layout, eps)) return HORA_ERR_INVALID_ARG;
+    if ((dq_weight != nullptr && q_weight == nullptr) || (dk_weight != nullptr && k_weight == nullptr)) return HORA_ERR_INVALID_ARG;
+    const int32_t size = dtype_bytes(dtype);
+    if (n_tokens > 0) {
+        if (!rows_ok(dq_out, dq_out_row_stride, Hq, D, size) || !rows_ok(dk_out, dk_out_row_stride, Hk, D, size) ||
+            !rows_ok(dq, dq_row_stride, Hq, D, size) || !rows_ok(dk, dk_row_stride, Hk, D, size))
+            return HORA_ERR_INVALID_ARG;
+        if ((q_weight != nullptr && !rows_ok(q, q_row_stride, Hq, D, size)) || (k_weight != nullptr && !rows_ok(k, k_row_stride, Hk, D, size)) ||
+            (rot > 0 && (positions == nullptr || inv_freq == nullptr)))
+            return HORA_ERR_INVALID_ARG;
+    }
+    const bool weights = dq_weight != nullptr || dk_weight != nullptr;
+    if (weights && (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) || workspace_bytes < hora_qk_rotate_backward_workspace_bytes(D)))
+        return HORA_ERR_WORKSPACE;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    int grid = 0;
+    if (n_tokens > 0) {
+        RotateArgs a = {};
+        a.x[0] = q; a.x[1] = k;
+        a.x_stride[0] = q_row_stride; a.x_stride[1] = k_row_stride;
+        a.dy[0] = dq_out; a.dy[1] = dk_out;
+        a.dy_stride[0] = dq_out_row_stride; a.dy_stride[1] = dk_out_row_stride;
+        a.y[0] = dq; a.y[1] = dk;
+        a.y_stride[0] = dq_row_stride; a.y_stride[1] = dk_row_stride;
+        a.w[0] = q_weight; a.w[1] = k_weight;
+        a.positions = positions;
+        a.inv_freq = inv_freq;
+        a.rot = rot;
+        a.eps = eps;
+        a.parts = weights ? static_cast<float *>(workspace) : nullptr;
+        grid = clamp_grid(units_of(a, n_tokens, Hq, Hk, D), kRotatePerSm);
+        const hora_status_t rc = launch_rotate_as(a, dtype, D, layout, true, grid, s);
+        if (rc != HORA_OK) return rc;
+    }
+    if (!weights) return HORA_OK;
+    const cudaError_t e = launch_pdl(qk_rotate_weights_kernel, 2 * D / kWarp, 1024, 0, s, static_cast<const float *>(workspace), (int32_t)grid, D, dq_weight, dk_weight);
+    count_launches(1);
+    return cuda_ok(e);
+}

@@ -26,6 +26,7 @@ FLAG_SHARED_INT_PRIOR = 4            # the same flag under the name of its first
 ADV_GRPO, ADV_RLOO = 0, 1
 WEIGHT_PER_TOKEN, WEIGHT_CONST_LENGTH = 0, 1
 DTYPE_F32, DTYPE_BF16, DTYPE_F16, DTYPE_E4M3 = range(4)
+ROTATE_HALVES, ROTATE_PAIRS = 0, 1
 _DTYPES = {torch.float32: DTYPE_F32, torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.float8_e4m3fn: DTYPE_E4M3}
 
 EXPORTS = ("hora_gains", "hora_allocate_workspace_bytes", "hora_allocate", "hora_group_advantage",
@@ -35,7 +36,9 @@ EXPORTS = ("hora_gains", "hora_allocate_workspace_bytes", "hora_allocate", "hora
            "hora_learned_prior", "hora_beta_binomial_nll", "hora_pass_at_k", "hora_pass_at_k_workspace_bytes",
            "hora_group_advantage_tokens", "hora_allocation_share", "hora_allocate_hard_first",
            "hora_allocate_hard_first_workspace_bytes", "hora_fp64_probe", "hora_checked_violation", "hora_kv_write",
-           "hora_kv_read", "hora_group_attention", "hora_group_attention_workspace_bytes", "hora_verify_drafts")
+           "hora_kv_read", "hora_group_attention", "hora_group_attention_workspace_bytes", "hora_verify_drafts",
+           "hora_qk_rotate", "hora_qk_rotate_backward", "hora_qk_rotate_backward_workspace_bytes", "hora_packed_attention",
+           "hora_packed_attention_backward", "hora_packed_attention_workspace_bytes")
 
 
 class HoraError(RuntimeError):
@@ -125,6 +128,20 @@ def load() -> C.CDLL:
     L.hora_group_attention.restype = C.c_int
     L.hora_verify_drafts.argtypes = [p, i32, i64, p, i64, p, p, i64, i32, i32, p, p, p, p, p, p]
     L.hora_verify_drafts.restype = C.c_int
+    L.hora_qk_rotate.argtypes = [p, p, i32, i64, i64, i64, i32, i32, i32, p, p, i32, i32, p, p, C.c_float, p, p, i64, i64, p]
+    L.hora_qk_rotate.restype = C.c_int
+    L.hora_qk_rotate_backward_workspace_bytes.argtypes = [i32]
+    L.hora_qk_rotate_backward_workspace_bytes.restype = C.c_size_t
+    L.hora_qk_rotate_backward.argtypes = [p, p, i32, i64, i64, p, p, i64, i64, i64, i32, i32, i32, p, p, i32, i32, p, p, C.c_float, p, p, i64, i64,
+                                          p, p, p, C.c_size_t, p]
+    L.hora_qk_rotate_backward.restype = C.c_int
+    L.hora_packed_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
+    L.hora_packed_attention_workspace_bytes.restype = C.c_size_t
+    L.hora_packed_attention.argtypes = [p, p, p, i32, i64, i64, i64, p, i64, p, i64, i32, i32, i32, C.c_float, i32, p, i64, p, p, p, C.c_size_t, p]
+    L.hora_packed_attention.restype = C.c_int
+    L.hora_packed_attention_backward.argtypes = [p, p, p, p, p, p, i32, i64, i64, i64, i64, i64, p, i64, p, i64, i32, i32, i32, C.c_float, i32, p, p, p,
+                                                 i64, i64, p, p, C.c_size_t, p]
+    L.hora_packed_attention_backward.restype = C.c_int
     L.hora_checked_violation.restype = C.c_int32
     L.hora_fp64_probe.argtypes = [i32, p, p]
     L.hora_fp64_probe.restype = C.c_uint64
@@ -568,6 +585,210 @@ class GroupAttention:
             for t in (self.workspace, self.out, self.lse):
                 t.record_stream(torch.cuda.current_stream(t.device))
         return out, lse
+
+
+# ------------------------------------------------------------------------------------------------
+# Prompts and training steps.
+def _heads(t: Optional[torch.Tensor], like, name: str, dtype=None) -> int:
+    """Distance (elements) between the tokens of t [n, H, D]; `like`: the shape it must have."""
+    if t is None:
+        raise ValueError(f"{name} is missing")
+    if t.dim() != 3 or tuple(t.shape) != tuple(like) or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{name} must be a tensor of the shape {tuple(like)}{'' if dtype is None else f' and of {dtype}'}, got {tuple(t.shape)} of {t.dtype}")
+    H, D = t.shape[1:]
+    if t.is_cuda and t.stride()[1:] == (D, 1) and t.shape[0] != 1:
+        return t.stride(0)
+    return _row_stride(t, 1, (H, D), name)
+
+
+def _one_device(first: torch.Tensor, *others) -> None:
+    """All tensors of a call lie on the current device, where its kernels are launched."""
+    dev = first.get_device()
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on cuda:{dev}, the current device is cuda:{torch.cuda.current_device()}")
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"all tensors must be on cuda:{dev}, got one on {t.device}")
+
+
+def _rotation(positions, inv_freq, q_weight, k_weight, n, D):
+    """The arguments both directions share, from positions on: rot follows from inv_freq."""
+    if inv_freq is not None and inv_freq.dim() != 1:
+        raise ValueError("inv_freq must have one dimension")
+    if inv_freq is not None and inv_freq.numel() and (positions is None or tuple(positions.shape) != (n,)):
+        raise ValueError("positions must hold one value for each token")
+    return (_at(positions, torch.int32, "positions"), _at(inv_freq, torch.float64, "inv_freq"), 0 if inv_freq is None else 2 * inv_freq.numel(),
+            _at(q_weight, torch.float32, "q_weight", D), _at(k_weight, torch.float32, "k_weight", D))
+
+
+def _sides(q, k, name):
+    """Shapes of the two sides; one of them may be left out."""
+    x = q if q is not None else k
+    if x is None or x.dim() != 3 or (q is not None and k is not None and (k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2] or k.dtype != q.dtype)):
+        raise ValueError(f"{name}: queries [n, Hq, D] and keys [n, Hk, D] of one type, or one of them")
+    return x, x.shape[0], 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], x.shape[2]
+
+
+def _side(t, like, name):
+    """(pointer, token stride) of a side that may be missing with its model."""
+    if like is None:
+        if t is not None:
+            raise ValueError(f"{name} is given without its other tensors")
+        return None, 0
+    stride = _heads(t, like.shape, name, like.dtype)
+    return t.data_ptr(), stride
+
+
+def hora_qk_rotate(q, k, positions, inv_freq, q_out, k_out, q_weight=None, k_weight=None, eps=1e-6, layout=ROTATE_HALVES):
+    """q, q_out [n, Hq, D], k, k_out [n, Hk, D] (tokens may be strided; either side may be None); positions [n] int32, inv_freq [rot/2]
+    fp64 (None: no rotation), weights [D] fp32 or None (no norm)."""
+    x, n, Hq, Hk, D = _sides(q, k, "hora_qk_rotate")
+    (qp, qs), (kp, ks), (qo, qos), (ko, kos) = _side(q, q, "q"), _side(k, k, "k"), _side(q_out, q, "q_out"), _side(k_out, k, "k_out")
+    pos, freq, rot, wq, wk = _rotation(positions, inv_freq, q_weight, k_weight, n, D)
+    _one_device(x, q, k, q_out, k_out, positions, inv_freq, q_weight, k_weight)
+    _check(load().hora_qk_rotate(qp, kp, _dtype_code(x, "q"), qs, ks, n, Hq, Hk, D, pos, freq, rot, layout, wq, wk, eps, qo, ko, qos, kos, _raw_stream(x)),
+           "hora_qk_rotate")
+
+
+def hora_qk_rotate_backward_workspace_bytes(D) -> int:
+    return int(load().hora_qk_rotate_backward_workspace_bytes(D))
+
+
+def hora_qk_rotate_backward(dq_out, dk_out, q, k, positions, inv_freq, dq, dk, dq_weight=None, dk_weight=None, q_weight=None, k_weight=None, eps=1e-6,
+                            layout=ROTATE_HALVES, workspace=None):
+    """The gradients dq, dk (and dq_weight, dk_weight [D] fp32) from dq_out, dk_out; q, k as given to hora_qk_rotate (None without a norm)."""
+    x, n, Hq, Hk, D = _sides(dq_out, dk_out, "hora_qk_rotate_backward")
+    (gq, gqs), (gk, gks), (oq, oqs), (ok, oks) = _side(dq_out, dq_out, "dq_out"), _side(dk_out, dk_out, "dk_out"), _side(dq, dq_out, "dq"), _side(dk, dk_out, "dk")
+    (qp, qs), (kp, ks) = _side(q, dq_out if q_weight is not None else q, "q"), _side(k, dk_out if k_weight is not None else k, "k")
+    pos, freq, rot, wq, wk = _rotation(positions, inv_freq, q_weight, k_weight, n, D)
+    _one_device(x, dk_out, q, k, dq, dk, dq_weight, dk_weight, positions, inv_freq, q_weight, k_weight, workspace)
+    _check(load().hora_qk_rotate_backward(gq, gk, _dtype_code(x, "dq_out"), gqs, gks, qp, kp, qs, ks, n, Hq, Hk, D, pos, freq, rot, layout, wq, wk, eps, oq, ok, oqs,
+                                          oks, _at(dq_weight, torch.float32, "dq_weight", D), _at(dk_weight, torch.float32, "dk_weight", D),
+                                          _at(workspace, torch.uint8, "workspace"), 0 if workspace is None else workspace.numel(), _raw_stream(x)),
+           "hora_qk_rotate_backward")
+
+
+class QkRotation:
+    """hora_qk_rotate with what stays from call to call: frequencies, head weights, and the backward pass's workspace."""
+
+    def __init__(self, inv_freq, D: int, *, q_weight=None, k_weight=None, eps: float = 1e-6, layout: int = ROTATE_HALVES):
+        first = next((t for t in (inv_freq, q_weight, k_weight) if t is not None), None)
+        if first is None:
+            raise ValueError("neither frequencies nor weights: there is nothing to do")
+        self.inv_freq, self.D, self.q_weight, self.k_weight, self.eps, self.layout = inv_freq, D, q_weight, k_weight, eps, layout
+        self.workspace = torch.empty(max(hora_qk_rotate_backward_workspace_bytes(D), 256), dtype=torch.uint8, device=first.device)
+        self._streams = set()
+
+    def run(self, q, k, positions, q_out=None, k_out=None):
+        """q [n, Hq, D], k [n, Hk, D]; returns (q_out, k_out), packed unless others are given."""
+        if q is not None and q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if k is not None and k_out is None:
+            k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        hora_qk_rotate(q, k, positions, self.inv_freq, q_out, k_out, self.q_weight, self.k_weight, self.eps, self.layout)
+        return q_out, k_out
+
+    def backward(self, dq_out, dk_out, q, k, positions, dq=None, dk=None, dq_weight=None, dk_weight=None):
+        """Returns (dq, dk), packed unless others are given; the weights' gradients where they are asked for."""
+        if dq_out is not None and dq is None:
+            dq = torch.empty(dq_out.shape, dtype=dq_out.dtype, device=dq_out.device)
+        if dk_out is not None and dk is None:
+            dk = torch.empty(dk_out.shape, dtype=dk_out.dtype, device=dk_out.device)
+        hora_qk_rotate_backward(dq_out, dk_out, q, k, positions, self.inv_freq, dq, dk, dq_weight, dk_weight, self.q_weight, self.k_weight, self.eps, self.layout,
+                                self.workspace)
+        _used_on(self, dq if dq is not None else dk, self.workspace)
+        return dq, dk
+
+
+def _used_on(owner, t, *buffers) -> None:
+    """The owner's memory is not handed on before the stream that it was just used on is through with it."""
+    raw = _raw_stream(t)
+    if raw not in owner._streams:
+        owner._streams.add(raw)
+        for b in buffers:
+            if b is not None:
+                b.record_stream(torch.cuda.current_stream(b.device))
+
+
+def hora_packed_attention_workspace_bytes(T, S, Hq, Hkv, D, backward) -> int:
+    return int(load().hora_packed_attention_workspace_bytes(T, S, Hq, Hkv, D, int(bool(backward))))
+
+
+def _packed_shapes(q, k, v, seq_offsets, group_offsets):
+    """(T, Hq, Hkv, D, q stride, kv stride, the arguments from T to D)."""
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q must have the shape [T, Hq, D], k and v [T, Hkv, D]")
+    T, Hq, D = q.shape
+    Hkv = k.shape[1]
+    qs, ks = _heads(q, q.shape, "q"), _heads(k, (T, Hkv, D), "k", q.dtype)
+    if _heads(v, (T, Hkv, D), "v", q.dtype) != ks:
+        raise ValueError("k and v must have the same row stride")
+    for t, name in ((seq_offsets, "seq_offsets"), (group_offsets, "group_offsets")):
+        if t is not None and (t.dim() != 1 or t.numel() < 1):
+            raise ValueError(f"{name} must have one dimension")
+    N = 0 if group_offsets is None else group_offsets.numel() - 1
+    return T, Hq, Hkv, D, qs, ks, (T, _at(seq_offsets, torch.int64, "seq_offsets"), seq_offsets.numel() - 1, _at(group_offsets, torch.int64, "group_offsets"), N, Hq, Hkv, D)
+
+
+def hora_packed_attention(q, k, v, seq_offsets, group_offsets, sm_scale, causal, out, lse, workspace, status_dev=None):
+    """q, out [T, Hq, D], k, v [T, Hkv, D] (tokens may be strided), lse [T, Hq] fp32 or None; seq_offsets [S+1], group_offsets [N+1] int64 or None."""
+    T, Hq, Hkv, D, qs, ks, shape = _packed_shapes(q, k, v, seq_offsets, group_offsets)
+    _one_device(q, k, v, seq_offsets, group_offsets, out, lse, workspace, status_dev)
+    _check(load().hora_packed_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), _dtype_code(q, "q"), qs, ks, *shape, float(sm_scale), int(causal), out.data_ptr(),
+                                        _heads(out, q.shape, "out", q.dtype), _at(lse, torch.float32, "lse", T * Hq), _at(status_dev, torch.int32, "status_dev"),
+                                        _at(workspace, torch.uint8, "workspace"), workspace.numel(), _raw_stream(q)), "hora_packed_attention")
+
+
+def hora_packed_attention_backward(q, k, v, out, lse, dout, seq_offsets, group_offsets, sm_scale, causal, dq, dk, dv, workspace, status_dev=None):
+    """The gradients dq [T, Hq, D], dk, dv [T, Hkv, D] (tokens may be strided) from dout; out, lse as hora_packed_attention left them."""
+    T, Hq, Hkv, D, qs, ks, shape = _packed_shapes(q, k, v, seq_offsets, group_offsets)
+    _one_device(q, k, v, out, lse, dout, seq_offsets, group_offsets, dq, dk, dv, workspace, status_dev)
+    dks = _heads(dk, k.shape, "dk", q.dtype)
+    if _heads(dv, k.shape, "dv", q.dtype) != dks:
+        raise ValueError("dk and dv must have the same row stride")
+    if lse is None:
+        raise ValueError("lse is missing")
+    _check(load().hora_packed_attention_backward(
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _at(lse, torch.float32, "lse", T * Hq), dout.data_ptr(), _dtype_code(q, "q"), qs, ks,
+        _heads(out, q.shape, "out", q.dtype), _heads(dout, q.shape, "dout", q.dtype), *shape, float(sm_scale), int(causal), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+        _heads(dq, q.shape, "dq", q.dtype), dks, _at(status_dev, torch.int32, "status_dev"), _at(workspace, torch.uint8, "workspace"), workspace.numel(),
+        _raw_stream(q)), "hora_packed_attention_backward")
+
+
+class PackedAttention:
+    """hora_packed_attention over offsets that stay where they are (their contents may change): owns the workspace and, unless others are given,
+    the outputs, which the next call overwrites."""
+
+    def __init__(self, seq_offsets, T: int, Hq: int, Hkv: int, D: int, dtype, *, group_offsets=None, causal: bool = True, sm_scale: Optional[float] = None,
+                 status_dev=None, backward: bool = False):
+        dev, S = seq_offsets.device, seq_offsets.numel() - 1
+        need = hora_packed_attention_workspace_bytes(T, S, Hq, Hkv, D, backward)
+        if need == 0:
+            raise ValueError(f"no such shape: {T} tokens in {S} sequences, {Hq} and {Hkv} heads of {D}")
+        self.seq_offsets, self.group_offsets, self.causal, self.status_dev = seq_offsets, group_offsets, causal, status_dev
+        self.sm_scale = D ** -0.5 if sm_scale is None else sm_scale
+        self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        new = lambda h: torch.empty((T, h, D), dtype=dtype, device=dev)  # noqa: E731
+        self.out, self.lse = new(Hq), torch.empty((T, Hq), dtype=torch.float32, device=dev)
+        self.dq, self.dk, self.dv = (new(Hq), new(Hkv), new(Hkv)) if backward else (None, None, None)
+        self._streams = set()
+
+    def run(self, q, k, v, out=None, lse=None):
+        """Returns (out, lse)."""
+        out, lse = self.out if out is None else out, self.lse if lse is None else lse
+        hora_packed_attention(q, k, v, self.seq_offsets, self.group_offsets, self.sm_scale, self.causal, out, lse, self.workspace, self.status_dev)
+        _used_on(self, q, self.workspace, self.out, self.lse, self.dq, self.dk, self.dv)
+        return out, lse
+
+    def backward(self, q, k, v, out, lse, dout, dq=None, dk=None, dv=None):
+        """Returns (dq, dk, dv) for what run was given and returned."""
+        if self.dq is None:
+            raise ValueError("made without backward=True")
+        dq, dk, dv = self.dq if dq is None else dq, self.dk if dk is None else dk, self.dv if dv is None else dv
+        hora_packed_attention_backward(q, k, v, out, lse, dout, self.seq_offsets, self.group_offsets, self.sm_scale, self.causal, dq, dk, dv, self.workspace,
+                                       self.status_dev)
+        _used_on(self, q, self.workspace, self.out, self.lse, self.dq, self.dk, self.dv)
+        return dq, dk, dv
 
 
 # ------------------------------------------------------------------------------------------------
