@@ -57,7 +57,7 @@ __device__ __forceinline__ int32_t steps_of(int32_t n) { return (int32_t)(((int6
 // Steps of one item of a sequence; KEYS: of its keys, else of its queries.
 template <bool KEYS>
 __device__ __forceinline__ int32_t item_steps(const PackedArgs &a, const PackedSequence &q, int32_t i) {
-    if constexpr (KEYS) {
+    if constexpr (KEYS) {                                // tiles of queries, for each block of the cache head's query heads
         const int32_t q0 = a.causal ? q.lo + i * kPackedRows : q.lo;
         return (int32_t)(((int64_t)q.seen_to - q0 + a.tp - 1) / a.tp);
     } else {
@@ -70,6 +70,11 @@ __device__ __forceinline__ int32_t items_of(const PackedArgs &a, const PackedSeq
     const int32_t per = KEYS ? kPackedRows : a.tile_tokens;
     return (int32_t)(((int64_t)q.hi - q.lo + per - 1) / per);
 }
+// Parts that an item of keys is cut into: none is longer than what a CTA has to do on average, or than kPartSteps where that is more.
+// Parts of items that are cut, times heads, are then 2 n_sm at most: each item has less than n / most + 1 <= 2 n / most of them.
+constexpr int kPartSteps = 8;
+__device__ __forceinline__ int32_t parts_of(int32_t steps, int32_t most) { return steps > most ? (steps + most - 1) / most : 1; }
+
 __device__ __forceinline__ int32_t bucket_of(int32_t steps) {
     return min(kListBuckets - 1, max(0, kListBuckets - 1 - (int32_t)((__float_as_uint((float)max(1, steps)) >> 18) - (127u << 5))));
 }
@@ -109,16 +114,38 @@ __device__ __forceinline__ void for_items(const PackedArgs &a, const PackedSeque
 // Lists of items, those with most steps first.  Which of two with about the same number comes first may differ from run to run; results do not.
 template <bool KEYS>
 __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s_groups, int32_t *s_bucket, int32_t *s_warp, bool &bad) {
+    __shared__ int64_t s_sum[kListWarps];
+    __shared__ int32_t s_next[2];
     const int warp = threadIdx.x >> 5, lane = lane_id();
     const int32_t each = min((int32_t)kWarp, (a.S + kListWarps - 1) / kListWarps);               // sequences of a warp at a time
     const bool once = each * kListWarps >= a.S;
     for (int i = threadIdx.x; i < kListBuckets; i += kListThreads) s_bucket[i] = 0;
     __syncthreads();
     PackedSequence kept = {0, 0, 0, 0, 0};
+    int32_t most = 0x7FFFFFFF;
+    if constexpr (KEYS) {
+        int64_t mine = 0;
+        for (int64_t base = (int64_t)warp * each; base < a.S; base += (int64_t)kListWarps * each) {
+            kept = lane < each ? packed_sequence(a, s_groups, (int32_t)min((int64_t)a.S, base + lane), bad) : PackedSequence{0, 0, 0, 0, 0};
+            for_items<true>(a, kept, [&](const PackedSequence &s, int32_t i) { mine += item_steps<true>(a, s, i); });
+        }
+#pragma unroll
+        for (int d = kWarp / 2; d > 0; d >>= 1) mine += __shfl_xor_sync(kFull, mine, d);
+        if (lane == 0) s_sum[warp] = mine;
+        __syncthreads();
+        int64_t all = 0;
+        for (int w = 0; w < kListWarps; ++w) all += s_sum[w];
+        const int64_t per = (all * a.Hkv + a.n_sm - 1) / a.n_sm;
+        most = (int32_t)min((int64_t)0x7FFFFFFF, max((int64_t)(kPartSteps * a.hp + a.g - 1) / a.g, per));
+        for (int i = threadIdx.x; i < 8 * a.n_sm; i += kListThreads) a.tickets[i] = 0;
+        if (threadIdx.x == 0) s_next[0] = s_next[1] = 0;
+    }
     for (int64_t base = (int64_t)warp * each; base < a.S; base += (int64_t)kListWarps * each) {
-        const PackedSequence q = lane < each ? packed_sequence(a, s_groups, (int32_t)min((int64_t)a.S, base + lane), bad) : PackedSequence{0, 0, 0, 0, 0};
-        for_items<KEYS>(a, q, [&](const PackedSequence &s, int32_t i) { atomicAdd(s_bucket + bucket_of(item_steps<KEYS>(a, s, i)), 1); });
-        kept = q;
+        if (!KEYS || !once) kept = lane < each ? packed_sequence(a, s_groups, (int32_t)min((int64_t)a.S, base + lane), bad) : PackedSequence{0, 0, 0, 0, 0};
+        for_items<KEYS>(a, kept, [&](const PackedSequence &s, int32_t i) {
+            const int32_t steps = item_steps<KEYS>(a, s, i), parts = KEYS ? parts_of(steps, most) : 1;
+            atomicAdd(s_bucket + bucket_of((steps + parts - 1) / parts), parts);
+        });
     }
     __syncthreads();
     static_assert(kListBuckets == kListThreads, "a thread to each bucket");
@@ -144,11 +171,23 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
     for (int64_t base = (int64_t)warp * each; base < a.S; base += (int64_t)kListWarps * each) {
         const PackedSequence q = once ? kept : lane < each ? packed_sequence(a, s_groups, (int32_t)min((int64_t)a.S, base + lane), bad) : PackedSequence{0, 0, 0, 0, 0};
         for_items<KEYS>(a, q, [&](const PackedSequence &s, int32_t i) {
-            const int32_t to = atomicAdd(s_bucket + bucket_of(item_steps<KEYS>(a, s, i)), 1);
-            if (to >= cap) return;
+            const int32_t steps = item_steps<KEYS>(a, s, i), parts = KEYS ? parts_of(steps, most) : 1, part_steps = (steps + parts - 1) / parts;
+            const int32_t to = atomicAdd(s_bucket + bucket_of(part_steps), parts);
+            if (to + parts > cap) return;
             if constexpr (KEYS) {
-                const int32_t key0 = s.lo + i * kPackedRows;
-                reinterpret_cast<int4 *>(a.key_items)[to] = make_int4(key0, min(kPackedRows, s.hi - key0), a.causal ? key0 : s.lo, s.seen_to);
+                const int32_t key0 = s.lo + i * kPackedRows, q0 = a.causal ? key0 : s.lo;
+                int32_t slot0 = 0, ticket = 0;
+                if (parts > 1) {
+                    slot0 = atomicAdd(s_next, parts);
+                    ticket = atomicAdd(s_next + 1, 1);
+                }
+                int4 *item = reinterpret_cast<int4 *>(a.key_items + to);
+                for (int32_t p = 0; p < parts; ++p) {
+                    const int64_t from = q0 + (int64_t)p * part_steps * a.tp;
+                    item[2 * p] = make_int4(key0, min(kPackedRows, s.hi - key0), (int32_t)min((int64_t)s.seen_to, from),
+                                            (int32_t)min((int64_t)s.seen_to, from + (int64_t)part_steps * a.tp));
+                    item[2 * p + 1] = make_int4(slot0, parts, p, ticket);
+                }
             } else {
                 const int32_t token0 = s.lo + i * a.tile_tokens;
                 int4 *item = reinterpret_cast<int4 *>(a.query_items + to);
@@ -174,7 +213,7 @@ packed_plan_kernel(const PackedArgs a) {
         }
         if (threadIdx.x == 0 && (__ldcg(a.group_offsets) != 0 || __ldcg(a.group_offsets + a.N) + a.N != a.S)) bad = true;
     }
-    if (threadIdx.x < 2) a.counts[2 + threadIdx.x] = 0;
+    if (threadIdx.x < 4) a.counts[2 + threadIdx.x] = 0;
     __syncthreads();
     list_items<false>(a, s_groups, s_bucket, s_warp, bad);
     if (a.key_items != nullptr) list_items<true>(a, s_groups, s_bucket, s_warp, bad);
@@ -264,15 +303,18 @@ static size_t lay_out(PackedArgs &a, bool backward, char *base) {
     };
     tile_shape(a);
     a.tile_tokens = backward ? a.tp : 2 * a.tp;
-    const int64_t queries = (int64_t)a.T / a.tile_tokens + a.S, keys = (int64_t)a.T / kPackedRows + a.S;
+    a.n_sm = sm_count();
+    const int64_t queries = (int64_t)a.T / a.tile_tokens + a.S, keys = (int64_t)a.T / kPackedRows + a.S + 2 * a.n_sm;
     a.query_cap = (int32_t)(queries < 0x7FFFFFFF ? queries : 0x7FFFFFFF);
     a.key_cap = (int32_t)(keys < 0x7FFFFFFF ? keys : 0x7FFFFFFF);
-    a.counts = reinterpret_cast<int32_t *>(take(16));
+    a.counts = reinterpret_cast<int32_t *>(take(32));
     a.query_items = reinterpret_cast<QueryItem *>(take((size_t)a.query_cap * sizeof(QueryItem)));
     a.key_items = nullptr;
     if (backward) {
         a.key_items = reinterpret_cast<KeyItem *>(take((size_t)a.key_cap * sizeof(KeyItem)));
         a.stats = reinterpret_cast<float2 *>(take((size_t)a.T * a.Hq * sizeof(float2)));
+        a.tickets = reinterpret_cast<int32_t *>(take((size_t)a.n_sm * 8 * sizeof(int32_t)));
+        a.slots = reinterpret_cast<float *>(take((size_t)2 * a.n_sm * 2 * kPackedRows * a.D * sizeof(float)));
     }
     return used;
 }

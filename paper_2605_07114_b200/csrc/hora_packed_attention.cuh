@@ -23,9 +23,11 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 struct QueryItem {
     int32_t token0, tokens, own0, end, shared0, shared1, pad[2];
 };
-// Keys that are an item, and the run of tokens whose queries may see them.
+// Keys that are an item, and the run of tokens whose queries may see them; or a part of that run (of a prompt's keys under a large group), whose
+// sums are then left in 32 bits in the slots slot0 + part (times heads), and added up, in order, by those that come last to
+// the item's tickets.
 struct KeyItem {
-    int32_t key0, keys, q0, q1;
+    int32_t key0, keys, q0, q1, slot0, parts, part, ticket;
 };
 
 struct PackedArgs {
@@ -39,17 +41,68 @@ struct PackedArgs {
     int32_t causal, half;                                // half: fp16 (weights and gradients of scores are held relative to a scale, see below)
     float scale, scale_log2;
     int32_t tile_tokens;                                 // tokens of a query item
-    int32_t query_cap, key_cap;
+    int32_t query_cap, key_cap, n_sm;
     // workspace
-    int32_t *counts;                                     // query items, key items, bits of the largest |dout row|^2 and |v row|^2
+    int32_t *counts;                                     // query items, key items, bits of the largest |dout row|^2 and |v row|^2, items taken of either list
     QueryItem *query_items;
     KeyItem *key_items;
+    int32_t *tickets;                                    // [n_sm][8]: by warp
+    float *slots;                                        // [2 n_sm][dV, dK][128][D]
     float2 *stats;                                       // [T][Hq] (lse in units of log2, dout . out)
 };
 
-// The r-th item of a CTA: all rounds but the last are full.
-__device__ __forceinline__ int64_t dealt(int32_t r) {
-    return (int64_t)r * gridDim.x + ((r & 1) ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+// CTAs take the items of a list one after the other, the longest first: the first by their own number, the following ones from a counter.
+// One warp (`feeder`) takes them and passes them on to the CTA's other warps through a ring in shared memory, a few items ahead.
+constexpr int kFeedDepth = 3;
+struct FeedSlot {
+    int4 a, b;
+    int32_t part, valid, pad[2];                         // which head (or block of heads)
+};
+struct Feed {
+    FeedSlot slot[kFeedDepth];
+    uint64_t full[kFeedDepth], empty[kFeedDepth];
+};
+__device__ __forceinline__ void feed_init(Feed &f, int readers) {
+    for (int i = 0; i < kFeedDepth; ++i) {
+        bar_init(smem_at(f.full + i), 1);
+        bar_init(smem_at(f.empty + i), readers);
+    }
+}
+// One lane.  VECTORS: of 16 bytes an item.
+template <int VECTORS>
+__device__ __forceinline__ void feed(Feed &f, const int4 *items, int32_t n_items, int32_t parts, int32_t *taken, volatile int32_t *failed) {
+    const int64_t all = (int64_t)n_items * parts;
+    for (uint32_t r = 0;; ++r) {
+        // the counter cannot pass 2^31: every CTA takes at most one more than there are
+        const int64_t x = r == 0 ? blockIdx.x : (int64_t)gridDim.x + (uint32_t)atomicAdd(taken, 1);
+        FeedSlot s = {};
+        s.valid = x < all;
+        if (s.valid) {
+            const int64_t i = x / parts;
+            s.part = (int32_t)(x - i * parts);
+            s.a = __ldcg(items + i * VECTORS);
+            if (VECTORS > 1) s.b = __ldcg(items + i * VECTORS + 1);
+        }
+        const uint32_t at = r % kFeedDepth;
+        if (r >= kFeedDepth && !bar_wait(smem_at(f.empty + at), (r / kFeedDepth + 1) & 1, failed)) return;
+        f.slot[at] = s;
+        bar_arrive(smem_at(f.full + at));
+        if (!s.valid) return;
+    }
+}
+// The r-th item of the CTA; by whole warps (ONE: by a single lane, which is then the reader).  Not valid after the last and when the CTA has given up.
+template <bool ONE>
+__device__ __forceinline__ FeedSlot feed_next(Feed &f, uint32_t r, volatile int32_t *failed) {
+    const uint32_t at = r % kFeedDepth;
+    bool ok = bar_wait(smem_at(f.full + at), (r / kFeedDepth) & 1, failed);
+    if (!ONE) ok = __all_sync(kFull, ok);
+    FeedSlot s = {};
+    if (ok) {
+        s = f.slot[at];
+        if (!ONE) __syncwarp();
+        if (ONE || lane_id() == 0) bar_arrive(smem_at(f.empty + at));
+    }
+    return s;
 }
 
 // In fp16 the smallest weights and gradients of scores would be lost: weights are held times 2^10, gradients of scores times a power

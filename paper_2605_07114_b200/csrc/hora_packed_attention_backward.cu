@@ -25,22 +25,24 @@ namespace hora {
 namespace {
 
 constexpr int kTile = kPackedRows, kHalfTile = kTile / 2;
-constexpr int kMiddleThreads = 256, kLoadWarp = 8, kProductWarp = 9, kStatsThreads = 64;
+constexpr int kMiddleThreads = 256, kLoadWarp = 8, kProductWarp = 9, kStatsWarp = 10, kFeedWarp = 11;
+constexpr int kKeysReaders = 11, kQueriesReaders = 10;   // warps that take items from the feeder
 
 template <typename Q>
 constexpr uint32_t kType = std::is_same<Q, __nv_bfloat16>::value ? 1u : 0u;
 template <typename Q>
-constexpr uint32_t kIdescScores = (1u << 4) | (kType<Q> << 7) | (kType<Q> << 10) | ((kTile / 8) << 17) | ((kTile / 16) << 24);
+constexpr uint32_t kIdescScores = (1u << 4) | (kType<Q> << 7) | (kType<Q> << 10) | ((kTile / 16) << 24);                // and the columns / 8 at bit 17
 template <typename Q, int D>
 constexpr uint32_t kIdescSum = (1u << 4) | (kType<Q> << 7) | (kType<Q> << 10) | (1u << 16) | ((D / 8) << 17) | ((kTile / 16) << 24);
 
-// The product of two tiles of 128 rows over D: rows of `a` by rows of `b`.  One elected lane.
+// The product over D of a tile's 128 rows `a` and the first `count` rows of `b` (up to a multiple of sixteen).  One elected lane.
 template <typename Q, int D>
-__device__ __forceinline__ void product_of_rows(uint32_t d, uint32_t a, uint32_t b) {
+__device__ __forceinline__ void product_of_rows(uint32_t d, uint32_t a, uint32_t b, int32_t count) {
+    const uint32_t idesc = kIdescScores<Q> | (uint32_t)((count + 15) >> 4) << 18;
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) {
         const uint32_t off = ((x >> 2) * (kTile * 128) + (x & 3) * 32) >> 4;
-        mma_smem(d, a + off, b + off, kIdescScores<Q>, x > 0);
+        mma_smem(d, a + off, b + off, idesc, x > 0);
     }
 }
 // d += w b, w 128 x `count` in tensor memory (16 bits, its two halves of 64 columns 64 columns of 32 bits apart), b `count` rows of D.
@@ -97,6 +99,7 @@ struct KeysSmem {
 };
 
 struct KeysShared {
+    Feed feed;
     float lse[4][kTile], delta[4][kTile];                // by stage: -lse, -dout.out, as the exponents and sums need them
     uint64_t full[4], empty[4], keys, keys_free, scores, weights, products, gradients, sums, sums_free;
     int32_t failed;
@@ -104,23 +107,23 @@ struct KeysShared {
 };
 
 struct KeyWork {
-    int32_t key0, keys, q0, q1, head, steps;
+    int32_t key0, keys, q0, q1, head, steps, slot0, parts, part, ticket;
     bool valid;
 };
 
-__device__ __forceinline__ KeyWork fetch_keys(const PackedArgs &a, int32_t r, int32_t n_items) {
-    const int64_t x = dealt(r);
-    KeyWork w = {};
-    w.valid = x < (int64_t)n_items * a.Hkv;
-    if (!w.valid) return w;
-    const int64_t i = x / a.Hkv;
-    w.head = (int32_t)(x - i * a.Hkv);
-    const int4 v = __ldcg(reinterpret_cast<const int4 *>(a.key_items + i));
-    w.key0 = v.x;
-    w.keys = v.y;
-    w.q0 = v.z;
-    w.q1 = v.w;
-    w.steps = (v.w - v.z + a.tp - 1) / a.tp * (a.g / a.hp);
+__device__ __forceinline__ KeyWork make_keys(const PackedArgs &a, const FeedSlot &f) {
+    KeyWork w;
+    w.valid = f.valid;
+    w.head = f.part;
+    w.key0 = f.a.x;
+    w.keys = f.a.y;
+    w.q0 = f.a.z;
+    w.q1 = f.a.w;
+    w.slot0 = f.b.x;
+    w.parts = f.b.y;
+    w.part = f.b.z;
+    w.ticket = f.b.w;
+    w.steps = (f.a.w - f.a.z + a.tp - 1) / a.tp * (a.g / a.hp);
     return w;
 }
 
@@ -162,8 +165,9 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
                    sums_free = smem_at(&sh.sums_free);
     if (threadIdx.x == 0) {
         sh.failed = 0;
+        feed_init(sh.feed, kKeysReaders);
         for (int s = 0; s < kStages; ++s) {
-            bar_init(full + 8 * s, 1 + kStatsThreads);
+            bar_init(full + 8 * s, 1 + kWarp);
             bar_init(empty + 8 * s, 1);
         }
         bar_init(keys, 1);
@@ -193,18 +197,18 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
     fence_after();
     const uint32_t tmem = sh.tmem;                       // columns: S^T, dP^T, dV, dK
     pdl_enter();
-    const int32_t n_items = __ldcg(a.counts + 1);
     const int shift = gradient_shift(a), up = a.half ? kHalfShift : 0;
     bool ok = true;
 
-    if (warp == kLoadWarp) {
+    if (warp == kFeedWarp) {
+        if (lane == 0) feed<2>(sh.feed, reinterpret_cast<const int4 *>(a.key_items), __ldcg(a.counts + 1), a.Hkv, a.counts + 5, failed);
+    } else if (warp == kLoadWarp) {
         if (lane == 0) {
             int32_t pos = 0;
             uint32_t turn = 0;
-            KeyWork next = fetch_keys(a, 0, n_items);
-            for (int32_t r = 0; next.valid && ok; ++r, ++turn) {
-                const KeyWork it = next;
-                next = fetch_keys(a, r + 1, n_items);
+            for (int32_t r = 0; ok; ++r, ++turn) {
+                const KeyWork it = make_keys(a, feed_next<true>(sh.feed, r, failed));
+                if (!it.valid) break;
                 if (r > 0) ok = bar_wait(keys_free, (turn + 1) & 1, failed);
                 if (!ok) break;
                 bar_expect(keys, 2 * Smem::kTileBytes);
@@ -225,7 +229,7 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
                     }
                 }
             }
-            if (!ok) {
+            if (*failed) {
                 // copies on their way to the CTA: the barriers of their stages may lack the other arrivals, so it is time that is waited for
                 int32_t never = 0;
                 if (turn > 0) bar_wait(keys, (turn - 1) & 1, &never);
@@ -236,10 +240,9 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
         const uint32_t k_rows = operand(base + Smem::kK, 16), v_rows = operand(base + Smem::kV, 16);
         uint32_t weights_phase = 0, gradients_phase = 0;
         int32_t pos = 0;
-        KeyWork next = fetch_keys(a, 0, n_items);
-        for (int32_t r = 0; next.valid && ok; ++r) {
-            const KeyWork it = next;
-            next = fetch_keys(a, r + 1, n_items);
+        for (int32_t r = 0; ok; ++r) {
+            const KeyWork it = make_keys(a, feed_next<false>(sh.feed, r, failed));
+            if (!it.valid) break;
             auto arrived = [&](int32_t s) {              // the tiles of step s
                 const int32_t x = pos + s;
                 if (!bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, failed)) return false;
@@ -259,14 +262,15 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
             ok = bar_wait(keys, r & 1, failed) && arrived(0);
             if (!ok) break;
             if (elect_one()) {
-                product_of_rows<Q, D>(tmem, k_rows, tile(0, 0, 16));
+                const int32_t count = key_step(a, it, 0).count;
+                product_of_rows<Q, D>(tmem, k_rows, tile(0, 0, 16), count);
                 mma_commit(scores);
-                product_of_rows<Q, D>(tmem + kTile, v_rows, tile(0, 1, 16));
+                product_of_rows<Q, D>(tmem + kTile, v_rows, tile(0, 1, 16), count);
                 mma_commit(products);
             }
             __syncwarp();
             for (int32_t s = 0; s < it.steps; ++s) {
-                const int32_t count = key_step(a, it, s).count;
+                const int32_t count = key_step(a, it, s).count, next_count = key_step(a, it, s + 1).count;
                 const bool more = s + 1 < it.steps;
                 ok = bar_wait(weights, weights_phase, failed);
                 weights_phase ^= 1;
@@ -279,7 +283,7 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
                     ok = arrived(s + 1);
                     if (!ok) break;
                     if (elect_one()) {
-                        product_of_rows<Q, D>(tmem, k_rows, tile(s + 1, 0, 16));
+                        product_of_rows<Q, D>(tmem, k_rows, tile(s + 1, 0, 16), next_count);
                         mma_commit(scores);
                     }
                     __syncwarp();
@@ -292,7 +296,7 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
                     product_with_weights<Q, D>(tmem + 256 + D, tmem + kTile, tile(s, 0, kTile * 128), count, s == 0);
                     mma_commit(empty + 8 * ((pos + s) % kStages));
                     if (more) {
-                        product_of_rows<Q, D>(tmem + kTile, v_rows, tile(s + 1, 1, 16));
+                        product_of_rows<Q, D>(tmem + kTile, v_rows, tile(s + 1, 1, 16), next_count);
                         mma_commit(products);
                     } else {
                         mma_commit(keys_free);
@@ -303,31 +307,29 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
             }
             pos += it.steps;
         }
-    } else if (warp > kProductWarp) {
+    } else if (warp == kStatsWarp) {
         // ---- of each row of a step: -lse and -dout.out
-        const int x0 = threadIdx.x - (kProductWarp + 1) * kWarp;
         const float c = exp2f((float)(shift - up));
         int32_t pos = 0;
-        KeyWork next = fetch_keys(a, 0, n_items);
-        for (int32_t r = 0; next.valid && ok; ++r) {
-            const KeyWork it = next;
-            next = fetch_keys(a, r + 1, n_items);
+        for (int32_t r = 0; ok; ++r) {
+            const KeyWork it = make_keys(a, feed_next<false>(sh.feed, r, failed));
+            if (!it.valid) break;
             for (int32_t s = 0; s < it.steps; ++s, ++pos) {
                 const KeyStep k = key_step(a, it, s);
                 const int stage = pos % kStages;
-                float2 st[2];
+                float2 st[kTile / kWarp];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int32_t row = x0 + i * kStatsThreads, token = k.token0 + row / a.hp;
+                for (int i = 0; i < kTile / kWarp; ++i) {
+                    const int32_t row = lane + i * kWarp, token = k.token0 + row / a.hp;
                     st[i] = make_float2(INFINITY, 0.f);
                     if (row < k.count && HORA_IN(token, a.T)) st[i] = __ldcg(a.stats + (int64_t)token * a.Hq + k.block * a.hp + row % a.hp);
                 }
                 if (pos >= kStages) ok = bar_wait(empty + 8 * stage, (pos / kStages + 1) & 1, failed);
                 if (!ok) break;
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    sh.lse[stage][x0 + i * kStatsThreads] = (float)up - st[i].x;
-                    sh.delta[stage][x0 + i * kStatsThreads] = -st[i].y * c;
+                for (int i = 0; i < kTile / kWarp; ++i) {
+                    sh.lse[stage][lane + i * kWarp] = (float)up - st[i].x;
+                    sh.delta[stage][lane + i * kWarp] = -st[i].y * c;
                 }
                 bar_arrive(full + 8 * stage);
             }
@@ -341,10 +343,9 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
         const float2 scale2 = make_float2(a.scale_log2, a.scale_log2), c2 = make_float2(c, c);
         uint32_t phase = 0;
         int32_t pos = 0;
-        KeyWork next = fetch_keys(a, 0, n_items);
-        for (int32_t r = 0; next.valid && ok; ++r) {
-            const KeyWork it = next;
-            next = fetch_keys(a, r + 1, n_items);
+        for (int32_t r = 0; ok; ++r) {
+            const KeyWork it = make_keys(a, feed_next<false>(sh.feed, r, failed));
+            if (!it.valid) break;
             for (int32_t s = 0; s < it.steps; ++s, ++pos, phase ^= 1) {
                 const KeyStep k = key_step(a, it, s);
                 const int stage = pos % kStages;
@@ -417,10 +418,62 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
             ok = __all_sync(kFull, ok);
             if (!ok) break;
             fence_after();
-            const int64_t to = (int64_t)(it.key0 + row) * a.dkv_stride + (int64_t)it.head * D;
-            store_row<D>(static_cast<Q *>(half ? a.dk : a.dv) + to, lanes + 256 + half * D, half ? a.scale * exp2f((float)-shift) : exp2f((float)-up), row < it.keys);
-            fence_before();
-            bar_arrive(sums_free);
+            Q *to = static_cast<Q *>(half ? a.dk : a.dv) + (int64_t)(it.key0 + row) * a.dkv_stride + (int64_t)it.head * D;
+            const float factor = half ? a.scale * exp2f((float)-shift) : exp2f((float)-up);
+            if (it.parts == 1) {
+                store_row<D>(to, lanes + 256 + half * D, factor, row < it.keys);
+                fence_before();
+                bar_arrive(sums_free);
+            } else {
+                // [slot][dV, dK][D / 4][128] of four values: neighbouring threads next to each other
+                const int64_t slot = ((int64_t)it.slot0 * a.Hkv + it.head) * 2 + half, step = (int64_t)a.Hkv * 2;
+                float4 *mine = reinterpret_cast<float4 *>(a.slots) + (slot + it.part * step) * (D / 4 * kTile) + row;
+                if (HORA_IN(slot + it.part * step, 4 * a.n_sm)) {
+#pragma unroll 1
+                    for (int b = 0; b < D / 32; ++b) {
+                        float o[32];
+                        tmem_load(lanes + 256 + half * D + b * 32, o);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int v = 0; v < 8; ++v) mine[(b * 8 + v) * kTile] = make_float4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
+                    }
+                }
+                fence_before();
+                bar_arrive(sums_free);
+                __threadfence();
+                __syncwarp();
+                const int32_t ticket = (it.ticket * a.Hkv + it.head) * 8 + warp;             // of the warp's rows
+                int32_t before = 0;
+                if (lane == 0 && HORA_IN(ticket, 8 * a.n_sm)) before = atomicAdd(a.tickets + ticket, 1);
+                if (__shfl_sync(kFull, before, 0) == it.parts - 1) {     // the other parts are there: all of them, in their order
+                    __threadfence();
+                    const float4 *from = reinterpret_cast<const float4 *>(a.slots) + slot * (D / 4 * kTile) + row;
+#pragma unroll 1
+                    for (int b = 0; b < D / 16; ++b) {
+                        float4 sum[4] = {};
+                        for (int32_t x = 0; x < it.parts; ++x) {
+                            float4 y[4];
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) y[v] = __ldcg(from + x * step * (D / 4 * kTile) + (b * 4 + v) * kTile);
+#pragma unroll
+                            for (int v = 0; v < 4; ++v) {
+                                sum[v].x += y[v].x;
+                                sum[v].y += y[v].y;
+                                sum[v].z += y[v].z;
+                                sum[v].w += y[v].w;
+                            }
+                        }
+                        if (row < it.keys) {
+#pragma unroll
+                            for (int v = 0; v < 4; v += 2) {
+                                const float x[8] = {sum[v].x * factor, sum[v].y * factor, sum[v].z * factor, sum[v].w * factor,
+                                                    sum[v + 1].x * factor, sum[v + 1].y * factor, sum[v + 1].z * factor, sum[v + 1].w * factor};
+                                *reinterpret_cast<uint4 *>(to + b * 16 + v * 4) = pack8<Q>(x);
+                            }
+                        }
+                    }
+                }
+            }
         }
     }
     fence_before();
@@ -443,38 +496,34 @@ struct QueriesSmem {
 };
 
 struct QueriesShared {
+    Feed feed;
     uint64_t full[10], empty[10], queries, queries_free, scores, scores_free, products, gradients, sums, sums_free;
     int32_t failed;
     uint32_t tmem;
 };
 
 struct QueryWork {
-    int32_t token0, tokens, own0, end, shared0, shared1, block, n_shared, n;
+    int32_t token0, tokens, own0, end, shared0, shared1, block, n_shared, n, last;       // last: behind the last key that is seen of the own sequence
     bool valid;
 
-    __device__ __forceinline__ void keys(int32_t j, int32_t &key0, int32_t &count) const {
-        key0 = j < n_shared ? shared0 + j * kTile : own0 + (j - n_shared) * kTile;
-        count = min(kTile, (j < n_shared ? shared1 : end) - key0);
-    }
+    __device__ __forceinline__ int32_t key0(int32_t j) const { return j < n_shared ? shared0 + j * kTile : own0 + (j - n_shared) * kTile; }
+    __device__ __forceinline__ int32_t count(int32_t j) const { return min(kTile, (j < n_shared ? shared1 : end) - key0(j)); }
+    __device__ __forceinline__ int32_t seen(int32_t j) const { return min(kTile, (j < n_shared ? shared1 : last) - key0(j)); }
 };
 
-__device__ __forceinline__ QueryWork fetch_queries(const PackedArgs &a, int32_t r, int32_t n_items) {
-    const int64_t x = dealt(r);
-    QueryWork w = {};
-    w.valid = x < (int64_t)n_items * a.blocks;
-    if (!w.valid) return w;
-    const int64_t i = x / a.blocks;
-    w.block = (int32_t)(x - i * a.blocks);
-    const int4 *p = reinterpret_cast<const int4 *>(a.query_items + i);
-    const int4 u = __ldcg(p), v = __ldcg(p + 1);
-    w.token0 = u.x;
-    w.tokens = u.y;
-    w.own0 = u.z;
-    w.end = u.w;
-    w.shared0 = v.x;
-    w.shared1 = v.y;
-    w.n_shared = (v.y - v.x + kTile - 1) / kTile;
-    w.n = w.n_shared + ((a.causal ? u.x + u.y : u.w) - u.z + kTile - 1) / kTile;
+__device__ __forceinline__ QueryWork make_queries(const PackedArgs &a, const FeedSlot &f) {
+    QueryWork w;
+    w.valid = f.valid;
+    w.block = f.part;
+    w.token0 = f.a.x;
+    w.tokens = f.a.y;
+    w.own0 = f.a.z;
+    w.end = f.a.w;
+    w.shared0 = f.b.x;
+    w.shared1 = f.b.y;
+    w.n_shared = (f.b.y - f.b.x + kTile - 1) / kTile;
+    w.last = a.causal ? f.a.x + f.a.y : f.a.w;
+    w.n = w.n_shared + (w.last - f.a.z + kTile - 1) / kTile;
     return w;
 }
 
@@ -498,6 +547,7 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
                    sums = smem_at(&sh.sums), sums_free = smem_at(&sh.sums_free);
     if (threadIdx.x == 0) {
         sh.failed = 0;
+        feed_init(sh.feed, kQueriesReaders);
         for (int s = 0; s < kStages; ++s) {
             bar_init(full + 8 * s, 1);
             bar_init(empty + 8 * s, 1);
@@ -522,18 +572,18 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
     fence_after();
     const uint32_t tmem = sh.tmem;                       // columns: S, dP, dQ
     pdl_enter();
-    const int32_t n_items = __ldcg(a.counts);
     const int shift = gradient_shift(a), up = a.half ? kHalfShift : 0;
     bool ok = true;
 
-    if (warp == kLoadWarp) {
+    if (warp == kFeedWarp) {
+        if (lane == 0) feed<2>(sh.feed, reinterpret_cast<const int4 *>(a.query_items), __ldcg(a.counts), a.blocks, a.counts + 4, failed);
+    } else if (warp == kLoadWarp) {
         if (lane == 0) {
             int32_t pos = 0;
             uint32_t turn = 0;
-            QueryWork next = fetch_queries(a, 0, n_items);
-            for (int32_t r = 0; next.valid && ok; ++r, ++turn) {
-                const QueryWork it = next;
-                next = fetch_queries(a, r + 1, n_items);
+            for (int32_t r = 0; ok; ++r, ++turn) {
+                const QueryWork it = make_queries(a, feed_next<true>(sh.feed, r, failed));
+                if (!it.valid) break;
                 const int32_t head = it.block * a.hp / a.g;
                 if (r > 0) ok = bar_wait(queries_free, (turn + 1) & 1, failed);
                 if (!ok) break;
@@ -543,8 +593,7 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
                     tma_box3(base + Smem::kDo + p * (kTile * 128), &do_map, p * 64, it.block * a.hp, it.token0, queries);
                 }
                 for (int32_t j = 0; j < it.n && ok; ++j) {
-                    int32_t key0, count;
-                    it.keys(j, key0, count);
+                    const int32_t key0 = it.key0(j);
                     for (int which = 0; which < 2; ++which, ++pos) {
                         const int stage = pos % kStages;
                         if (pos >= kStages) ok = bar_wait(empty + 8 * stage, (pos / kStages + 1) & 1, failed);
@@ -555,7 +604,7 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
                     }
                 }
             }
-            if (!ok) {
+            if (*failed) {
                 int32_t never = 0;
                 if (turn > 0) bar_wait(queries, (turn - 1) & 1, &never);
                 for (int32_t x = max(0, pos - kStages); x < pos; ++x) bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, &never);
@@ -565,17 +614,15 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
         const uint32_t q_rows = operand(base + Smem::kQ, 16), do_rows = operand(base + Smem::kDo, 16);
         uint32_t free_phase = 0, gradients_phase = 0;
         int32_t pos = 0;
-        QueryWork next = fetch_queries(a, 0, n_items);
-        for (int32_t r = 0; next.valid && ok; ++r) {
-            const QueryWork it = next;
-            next = fetch_queries(a, r + 1, n_items);
+        for (int32_t r = 0; ok; ++r) {
+            const QueryWork it = make_queries(a, feed_next<false>(sh.feed, r, failed));
+            if (!it.valid) break;
             auto at = [&](int32_t j, int which) { return base + Smem::kRing + (uint32_t)((pos + 2 * j + which) % kStages) * Smem::kTileBytes; };
             auto arrived = [&](int32_t j, int which) {
                 const int32_t x = pos + 2 * j + which;
                 if (!bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, failed)) return false;
-                int32_t key0, count;
-                it.keys(j, key0, count);
-                if (which == 0 && (count & 15)) {
+                const int32_t count = it.count(j);
+                if (which == 0 && (count & 15) && it.seen(j) > (count & ~15)) {
                     clear_rows<D>(at(j, 0), count);
                     publish_clears();
                 }
@@ -584,14 +631,14 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
             };
             auto scores_of = [&](int32_t j) {
                 if (elect_one()) {
-                    product_of_rows<Q, D>(tmem, q_rows, operand(at(j, 0), 16));
+                    product_of_rows<Q, D>(tmem, q_rows, operand(at(j, 0), 16), it.seen(j));
                     mma_commit(scores);
                 }
                 __syncwarp();
             };
             auto products_of = [&](int32_t j) {
                 if (elect_one()) {
-                    product_of_rows<Q, D>(tmem + kTile, do_rows, operand(at(j, 1), 16));
+                    product_of_rows<Q, D>(tmem + kTile, do_rows, operand(at(j, 1), 16), it.seen(j));
                     mma_commit(products);
                     mma_commit(empty + 8 * ((pos + 2 * j + 1) % kStages));
                     if (j + 1 == it.n) mma_commit(queries_free);
@@ -625,9 +672,7 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
                 if (!ok) break;
                 fence_after();
                 if (elect_one()) {
-                    int32_t key0, count;
-                    it.keys(j, key0, count);
-                    product_with_weights<Q, D>(tmem + 256, tmem + kTile, operand(at(j, 0), kTile * 128), count, j == 0);
+                    product_with_weights<Q, D>(tmem + 256, tmem + kTile, operand(at(j, 0), kTile * 128), it.seen(j), j == 0);
                     mma_commit(empty + 8 * ((pos + 2 * j) % kStages));
                     if (!more) mma_commit(sums);
                 }
@@ -653,13 +698,11 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
             return st;
         };
         uint32_t phase = 0;
-        QueryWork next = fetch_queries(a, 0, n_items);
-        float2 st = stats_of(next);
-        for (int32_t r = 0; next.valid && ok; ++r) {
-            const QueryWork it = next;
+        for (int32_t r = 0; ok; ++r) {
+            const QueryWork it = make_queries(a, feed_next<false>(sh.feed, r, failed));
+            if (!it.valid) break;
+            const float2 st = stats_of(it);
             const float2 lse2 = make_float2((float)up - st.x, (float)up - st.x), delta2 = make_float2(-st.y * c, -st.y * c);
-            next = fetch_queries(a, r + 1, n_items);
-            st = stats_of(next);
             const bool have = row_token < it.tokens;
             const int32_t token = it.token0 + row_token;
             const int32_t seen_to = a.causal && have ? min(it.end, token + 1) : it.end;
@@ -742,7 +785,7 @@ hora_status_t launch_backward(const PackedArgs &a, const void *q, const void *k,
     cudaError_t e = allow_shared(reinterpret_cast<const void *>(packed_keys_kernel<Q, D>), kKeysSmem, keys_devices);
     if (e == cudaSuccess) e = allow_shared(reinterpret_cast<const void *>(packed_queries_kernel<Q, D>), kQueriesSmem, queries_devices);
     if (e == cudaSuccess)
-        e = launch_pdl(packed_keys_kernel<Q, D>, clamp_grid((int64_t)a.key_cap * a.Hkv, 1), kPackedThreads, kKeysSmem, stream, a, q_map, do_map, k_map, v_map);
+        e = launch_pdl(packed_keys_kernel<Q, D>, clamp_grid(((int64_t)a.T / kTile + a.S) * a.Hkv + 2 * a.n_sm, 1), kPackedThreads, kKeysSmem, stream, a, q_map, do_map, k_map, v_map);
     if (e == cudaSuccess)
         e = launch_pdl(packed_queries_kernel<Q, D>, clamp_grid((int64_t)a.query_cap * a.blocks, 1), kPackedThreads, kQueriesSmem, stream, a, q_map, do_map, k_map, v_map);
     count_launches(2);

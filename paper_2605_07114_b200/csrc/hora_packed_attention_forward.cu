@@ -23,79 +23,149 @@ namespace hora {
 namespace {
 
 constexpr int kTile = kPackedRows;
-constexpr int kLoadWarp = 8, kProductWarp = 9;
+constexpr int kLoadWarp = 8, kClearWarp = 10, kFeedWarp = 11;
+constexpr int kFeedReaders = 11;                         // warps that take items from the feeder
 
 template <int D>
 struct ForwardSmem {
     static constexpr int kTileBytes = kTile * D * 2;
-    static constexpr int kStages = D == 128 ? 5 : 10;
-    static constexpr int kQ = 0, kRing = 2 * kTileBytes, kSmall = kRing + kStages * kTileBytes;
+    static constexpr int kStages = D == 128 ? 4 : 8;
+    static constexpr int kQ = 0, kRing = 2 * kTileBytes, kStaging = kRing + kStages * kTileBytes;        // staging: 32 rows of 64 bytes a warp
+    static constexpr int kSmall = kStaging + 8 * kWarp * 64;
 };
 
 struct ForwardShared {
-    uint64_t full[10], empty[10], queries, queries_free, scores[2], weights[2], output[2], output_free[2];
+    Feed feed;
+    uint64_t full[8], empty[8], cleared[8], queries, queries_free, scores[2], weights[4], output[2], output_free[2];
     int32_t failed;
     uint32_t tmem;
 };
 
 // An item as the warps need it: runs of keys, steps of each tile.
 struct Item {
-    int32_t token0, end, own0, shared0, shared1, last_token;
+    int32_t token0, end, own0, shared0, shared1;
     int32_t block;
-    int32_t n_shared, n[2], tokens[2];
-    bool valid;
+    int32_t n_shared, n[2], tokens[2], last[2];          // last: behind the last key that the tile sees of its own sequence
 
     __device__ __forceinline__ int32_t steps() const { return max(n[0], n[1]); }
-    // first key of step j and how many keys of the sequence there are from it on
-    __device__ __forceinline__ void keys(int32_t j, int32_t &key0, int32_t &count) const {
-        if (j < n_shared) {
-            key0 = shared0 + j * kTile;
-            count = shared1 - key0;
-        } else {
-            key0 = own0 + (j - n_shared) * kTile;
-            count = end - key0;
-        }
-        count = min(count, kTile);
-    }
+    // first key of step j and how many keys of the sequence there are from it on; and those that tile t sees
+    __device__ __forceinline__ int32_t key0(int32_t j) const { return j < n_shared ? shared0 + j * kTile : own0 + (j - n_shared) * kTile; }
+    __device__ __forceinline__ int32_t count(int32_t j) const { return min(kTile, (j < n_shared ? shared1 : end) - key0(j)); }
+    __device__ __forceinline__ int32_t seen(int32_t j, int t) const { return min(kTile, (j < n_shared ? shared1 : t ? last[1] : last[0]) - key0(j)); }
 };
 
-struct RawItem {
-    int4 a, b;
-    int32_t block;
-    bool valid;
-};
-
-__device__ __forceinline__ RawItem fetch_item(const PackedArgs &a, int32_t r, int32_t n_items) {
-    const int64_t x = dealt(r);
-    RawItem f = {};
-    f.valid = x < (int64_t)n_items * a.blocks;
-    if (!f.valid) return f;
-    const int64_t i = x / a.blocks;
-    f.block = (int32_t)(x - i * a.blocks);
-    const int4 *p = reinterpret_cast<const int4 *>(a.query_items + i);
-    f.a = __ldcg(p);
-    f.b = __ldcg(p + 1);
-    return f;
-}
-
-__device__ __forceinline__ Item make_item(const PackedArgs &a, const RawItem &f) {
+__device__ __forceinline__ Item make_item(const PackedArgs &a, const FeedSlot &f) {
     Item q;
-    q.valid = f.valid;
     q.token0 = f.a.x;
     q.own0 = f.a.z;
     q.end = f.a.w;
     q.shared0 = f.b.x;
     q.shared1 = f.b.y;
-    q.block = f.block;
+    q.block = f.part;
     q.n_shared = (q.shared1 - q.shared0 + kTile - 1) / kTile;
     q.tokens[0] = min(a.tp, f.a.y);
     q.tokens[1] = f.a.y - q.tokens[0];
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const int32_t last = a.causal ? q.token0 + t * a.tp + q.tokens[t] : q.end;
-        q.n[t] = q.tokens[t] > 0 ? q.n_shared + (last - q.own0 + kTile - 1) / kTile : 0;
+        q.last[t] = a.causal ? q.token0 + t * a.tp + q.tokens[t] : q.end;
+        q.n[t] = q.tokens[t] > 0 ? q.n_shared + (q.last[t] - q.own0 + kTile - 1) / kTile : 0;
     }
     return q;
+}
+
+// Raises a row's reference to the maximum `top` of the step's scores where it has grown by more than 2^8; the output is scaled then.
+// `have`: the row is a token's; others may hold anything and have no say.
+template <int D>
+__device__ __forceinline__ void raise_reference(uint32_t t_o, float top, bool have, bool first, float &m, float &l) {
+    if (first) {
+        m = top;
+    } else if (__any_sync(kFull, have && top > m + 8.f)) {
+        const float up = fmaxf(m, top), f = up == -INFINITY ? 1.f : exp2_approx(m - up);
+        l *= f;
+        m = up;
+#pragma unroll 1
+        for (int b = 0; b < D / 16; ++b) {
+            float o[16];
+            tmem_load16(t_o + b * 16, o);
+            tmem_load_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] *= f;
+            tmem_store16(t_o + b * 16, o);
+        }
+    }
+}
+
+__device__ __forceinline__ void tell_weights(uint32_t bar) {
+    tmem_store_wait();
+    fence_before();
+    bar_arrive(bar);
+}
+
+// A row's part in a step: `seen` scores in tensor memory, of which the row sees `limit`, to weights there; `whole`: every row of the warp
+// sees 128.  Tells the first half of the weights when it is there, then the second half.
+// The warps of a multiprocessor share its instruction cache, and the one that issues the products waits for its instructions longest: so this
+// loops over 32 scores at a time (which are read again for it), with the next ones on their way (unrolled over 128 scores held in registers, in
+// three variants: 60 prompts 148 us in place of 130, 16381 tokens 2010 us in place of 1870).
+template <typename Q, int D>
+__device__ __forceinline__ void softmax_step(uint32_t t_s, uint32_t t_o, uint32_t bar, float scale_log2, int32_t seen, int32_t limit, bool whole, bool have, bool first,
+                                             float &m, float &l) {
+    float top[4];
+    {
+        float s[4][32];
+#pragma unroll
+        for (int b = 0; b < 4; ++b) tmem_load(t_s + b * 32, s[b]);
+        tmem_load_wait();
+        if (!whole) {
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+                const int32_t n = limit - b * 32;
+                const uint32_t sees = n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1u;
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                    if (!(sees & (1u << e))) s[b][e] = -INFINITY;
+                tmem_store32(t_s + b * 32, s[b]);
+            }
+            tmem_store_wait();
+        }
+#pragma unroll
+        for (int b = 0; b < 4; ++b) {
+            top[b] = s[b][0];
+#pragma unroll
+            for (int e = 1; e < 31; e += 2) top[b] = fmaxf(top[b], fmaxf(s[b][e], s[b][e + 1]));
+            top[b] = fmaxf(top[b], s[b][31]);
+        }
+    }
+    raise_reference<D>(t_o, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * scale_log2, have, first, m, l);
+    // where no key has been seen the reference is -infinity and every weight has to come out as 0
+    const float z = m == -INFINITY ? 0.f : m;
+    const float2 scale2 = make_float2(scale_log2, scale_log2), z2 = make_float2(-z, -z);
+    float2 sum = make_float2(0.f, 0.f);
+    float s[32], next[32];
+    tmem_load(t_s, s);
+    tmem_load_wait();
+#pragma unroll 1
+    for (int b = 0; b < 4; ++b) {
+        if (b * 32 < seen) {
+            tmem_load(t_s + (b < 3 ? b + 1 : 3) * 32, next);
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {                // in place of scores that have been read
+                uint32_t w[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float2 y = fma2(make_float2(s[x * 16 + 2 * e], s[x * 16 + 2 * e + 1]), scale2, z2);
+                    y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
+                    sum = add2(sum, y);
+                    w[e] = pack2(y.x, y.y, Q());
+                }
+                tmem_store8(t_s + b * 16 + x * 8, w);
+            }
+            tmem_load_wait();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) s[e] = next[e];
+        }
+        if (b & 1) tell_weights(bar + 8 * (b >> 1));
+    }
+    l += sum.x + sum.y;
 }
 
 extern __shared__ __align__(1024) uint8_t s_forward[];
@@ -116,18 +186,20 @@ packed_forward_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
         return;
     }
     const uint32_t full = smem_at(sh.full), empty = smem_at(sh.empty), queries = smem_at(&sh.queries), queries_free = smem_at(&sh.queries_free),
-                   scores = smem_at(sh.scores), weights = smem_at(sh.weights), output = smem_at(sh.output), output_free = smem_at(sh.output_free);
+                   cleared = smem_at(sh.cleared), scores = smem_at(sh.scores), weights = smem_at(sh.weights), output = smem_at(sh.output), output_free = smem_at(sh.output_free);
     if (threadIdx.x == 0) {
         sh.failed = 0;
+        feed_init(sh.feed, kFeedReaders);
         for (int s = 0; s < kStages; ++s) {
             bar_init(full + 8 * s, 1);
             bar_init(empty + 8 * s, 1);
+            bar_init(cleared + 8 * s, 1);
         }
         bar_init(queries, 1);
         bar_init(queries_free, 1);
         for (int t = 0; t < 2; ++t) {
             bar_init(scores + 8 * t, 1);
-            bar_init(weights + 8 * t, kTile);
+            for (int h = 0; h < 2; ++h) bar_init(weights + 16 * t + 8 * h, kTile);
             bar_init(output + 8 * t, 1);
             bar_init(output_free + 8 * t, kTile);
         }
@@ -143,92 +215,60 @@ packed_forward_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
     fence_after();
     const uint32_t tmem = sh.tmem;                       // columns: S of the two tiles, 128 each, then O, D each
     pdl_enter();
-    const int32_t n_items = __ldcg(a.counts);
     bool ok = true;
 
-    if (warp == kLoadWarp) {
-        if (lane == 0) {
-            int32_t pos = 0;                             // copies into the ring so far
-            uint32_t turn = 0;
-            RawItem next = fetch_item(a, 0, n_items);
-            for (int32_t r = 0; next.valid && ok; ++r, ++turn) {
-                const Item it = make_item(a, next);
-                next = fetch_item(a, r + 1, n_items);
-                const int32_t head = it.block * a.hp / a.g;
-                const int tiles = it.tokens[1] > 0 ? 2 : 1;
-                if (r > 0) ok = bar_wait(queries_free, (turn + 1) & 1, failed);
-                if (!ok) break;
-                bar_expect(queries, tiles * kParts * a.hp * a.tp * 128);
-                for (int t = 0; t < tiles; ++t)
-                    for (int p = 0; p < kParts; ++p)
-                        tma_box3(base + Smem::kQ + t * Smem::kTileBytes + p * (kTile * 128), &q_map, p * 64, it.block * a.hp, it.token0 + t * a.tp, queries);
+    if (warp >= 8) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        if (warp == kFeedWarp) {
+            if (lane == 0) feed<2>(sh.feed, reinterpret_cast<const int4 *>(a.query_items), __ldcg(a.counts), a.blocks, a.counts + 4, failed);
+        } else if (warp == kLoadWarp) {
+            if (lane == 0) {
+                int32_t pos = 0;                         // copies into the ring so far
+                uint32_t r = 0;
+                for (; ok; ++r) {
+                    const FeedSlot f = feed_next<true>(sh.feed, r, failed);
+                    if (!f.valid) break;
+                    const Item it = make_item(a, f);
+                    const int32_t head = it.block * a.hp / a.g;
+                    const int tiles = it.tokens[1] > 0 ? 2 : 1;
+                    if (r > 0) ok = bar_wait(queries_free, (r + 1) & 1, failed);
+                    if (!ok) break;
+                    bar_expect(queries, tiles * kParts * a.hp * a.tp * 128);
+                    for (int t = 0; t < tiles; ++t)
+                        for (int p = 0; p < kParts; ++p)
+                            tma_box3(base + Smem::kQ + t * Smem::kTileBytes + p * (kTile * 128), &q_map, p * 64, it.block * a.hp, it.token0 + t * a.tp, queries);
+                    const int32_t n = it.steps();
+                    for (int32_t j = 0; j < n && ok; ++j)
+                        for (int which = 0; which < 2; ++which, ++pos) {
+                            const int stage = pos % kStages;
+                            if (pos >= kStages) ok = bar_wait(empty + 8 * stage, (pos / kStages + 1) & 1, failed);
+                            if (!ok) break;
+                            bar_expect(full + 8 * stage, Smem::kTileBytes);
+                            for (int p = 0; p < kParts; ++p)
+                                tma_box3(base + Smem::kRing + stage * Smem::kTileBytes + p * (kTile * 128), which ? &v_map : &k_map, p * 64, head, it.key0(j), full + 8 * stage);
+                        }
+                }
+                // the CTA may not end while copies are on their way to it: each is waited for by its use, unless the CTA has given up
+                if (*failed) {
+                    int32_t never = 0;
+                    for (int32_t x = max(0, pos - kStages); x < pos; ++x) bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, &never);
+                    if (r > 0) bar_wait(queries, (r - 1) & 1, &never);
+                }
+            }
+        } else if (warp == kClearWarp) {
+            // ---- values that are not of the sequence, among the last sixteen that a product reads
+            int32_t pos = 0;
+            for (uint32_t r = 0; ok; ++r) {
+                const FeedSlot f = feed_next<false>(sh.feed, r, failed);
+                if (!f.valid) break;
+                const Item it = make_item(a, f);
                 const int32_t n = it.steps();
                 for (int32_t j = 0; j < n && ok; ++j) {
-                    int32_t key0, count;
-                    it.keys(j, key0, count);
-                    for (int which = 0; which < 2 && ok; ++which, ++pos) {
-                        const int stage = pos % kStages;
-                        if (pos >= kStages) ok = bar_wait(empty + 8 * stage, (pos / kStages + 1) & 1, failed);
-                        if (!ok) break;
-                        bar_expect(full + 8 * stage, Smem::kTileBytes);
-                        for (int p = 0; p < kParts; ++p)
-                            tma_box3(base + Smem::kRing + stage * Smem::kTileBytes + p * (kTile * 128), which ? &v_map : &k_map, p * 64, head, key0, full + 8 * stage);
-                    }
-                }
-            }
-            // the CTA may not end while copies are on their way to it: each is waited for by its use, unless the CTA has given up
-            if (!ok) {
-                int32_t never = 0;
-                for (int32_t x = max(0, pos - kStages); x < pos; ++x) bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, &never);
-                if (turn > 0) bar_wait(queries, (turn - 1) & 1, &never);
-            }
-        }
-    } else if (warp == kProductWarp) {
-        constexpr uint32_t kType = std::is_same<Q, __nv_bfloat16>::value ? 1u : 0u;
-        constexpr uint32_t kIdescS = (1u << 4) | (kType << 7) | (kType << 10) | ((kTile / 8) << 17) | ((kTile / 16) << 24);
-        constexpr uint32_t kIdescO = (1u << 4) | (kType << 7) | (kType << 10) | (1u << 16) | ((D / 8) << 17) | ((kTile / 16) << 24);
-        const uint32_t k0 = operand(base + Smem::kRing, 16), v0 = operand(base + Smem::kRing, kTile * 128), q0 = operand(base + Smem::kQ, 16);
-        uint32_t weights_phase = 0, free_phase = 0, started = 0;
-        int32_t pos = 0;
-        RawItem next = fetch_item(a, 0, n_items);
-        for (int32_t r = 0; next.valid && ok; ++r) {
-            const Item it = make_item(a, next);
-            next = fetch_item(a, r + 1, n_items);
-            const int32_t n = it.steps();
-            auto stage_of = [&](int32_t j, int which) { return (uint32_t)((pos + 2 * j + which) % kStages); };
-            auto arrived = [&](int32_t j, int which) {
-                const int32_t x = pos + 2 * j + which;
-                return bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, failed);
-            };
-            auto scores_of = [&](int t, int32_t j) {
-                if (elect_one()) {
-                    const uint32_t k = k0 + stage_of(j, 0) * (Smem::kTileBytes >> 4), q = q0 + t * (Smem::kTileBytes >> 4);
-#pragma unroll
-                    for (int x = 0; x < D / 16; ++x) {
-                        const uint32_t off = ((x >> 2) * (kTile * 128) + (x & 3) * 32) >> 4;
-                        mma_smem(tmem + t * kTile, q + off, k + off, kIdescS, x > 0);
-                    }
-                    mma_commit(scores + 8 * t);
-                }
-                __syncwarp();
-            };
-            ok = bar_wait(queries, r & 1, failed) && arrived(0, 0);
-            if (!ok) break;
-            fence_after();
-            for (int t = 0; t < 2; ++t)
-                if (it.n[t] > 0) scores_of(t, 0);
-            if (elect_one()) {
-                mma_commit(empty + 8 * stage_of(0, 0));
-                if (n == 1) mma_commit(queries_free);
-            }
-            __syncwarp();
-            for (int32_t j = 0; j < n && ok; ++j) {
-                int32_t key0, count;
-                it.keys(j, key0, count);
-                ok = arrived(j, 1);
-                if (!ok) break;
-                if (count & 15) {                        // values that are not of the sequence, among the last sixteen
-                    const uint32_t at = base + Smem::kRing + stage_of(j, 1) * Smem::kTileBytes;
+                    const int32_t count = it.count(j), x = pos + 2 * j + 1;
+                    // every copy is waited for: a barrier only tells two neighbouring ones apart
+                    ok = __all_sync(kFull, bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, failed));
+                    if (!ok || !(count & 15)) continue;
+                    const uint32_t at = base + Smem::kRing + (uint32_t)(x % kStages) * Smem::kTileBytes;
                     const int32_t clear = ((count + 15) & ~15) - count;
                     for (int32_t c = lane; c < clear * (D / 8); c += kWarp) {
                         const uint32_t to = at + (c % (D / 8) >> 3) * (kTile * 128) + (count + c / (D / 8)) * 128 + (c & 7) * 16;
@@ -236,152 +276,159 @@ packed_forward_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
+                    if (lane == 0) bar_arrive(cleared + 8 * (x % kStages));
                 }
-                for (int t = 0; t < 2 && ok; ++t) {
-                    if (j < it.n[t]) {
-                        ok = bar_wait(weights + 8 * t, (weights_phase >> t) & 1, failed);
-                        weights_phase ^= 1u << t;
-                        if (ok && j == 0 && ((started >> t) & 1)) {      // the output of the item before has been read
-                            ok = bar_wait(output_free + 8 * t, (free_phase >> t) & 1, failed);
-                            free_phase ^= 1u << t;
-                        }
-                        if (!ok) break;
-                        started |= 1u << t;
-                        fence_after();
-                        if (elect_one()) {
-                            const uint32_t v = v0 + stage_of(j, 1) * (Smem::kTileBytes >> 4), w = tmem + t * kTile;
-#pragma unroll
-                            for (int g = 0; g < kTile / 16; ++g)
-                                if (g * 16 < count) mma_tmem(tmem + 256 + t * D, w + g * 8, v + g * (2048 >> 4), kIdescO, j > 0 || g > 0);
-                            if (j == it.n[t] - 1) mma_commit(output + 8 * t);
-                        }
-                        __syncwarp();
-                    }
-                    if (j + 1 < it.n[t]) {
-                        ok = arrived(j + 1, 0);
-                        if (!ok) break;
-                        fence_after();
-                        scores_of(t, j + 1);
-                    }
-                }
-                if (!ok) break;
-                if (elect_one()) {
-                    mma_commit(empty + 8 * stage_of(j, 1));
-                    if (j + 1 < n) mma_commit(empty + 8 * stage_of(j + 1, 0));
-                    if (j + 2 == n) mma_commit(queries_free);
-                }
-                __syncwarp();
+                pos += 2 * n;
             }
-            pos += 2 * n;
+        } else {
+            // ---- products, of the two tiles in turn: while one's wait for their weights the other's are under way.  A wait that has failed is not
+            // looked at here: what follows is of no use, but in bounds, and there is no next item
+            const uint32_t lead = elect_one();
+            constexpr uint32_t kType = std::is_same<Q, __nv_bfloat16>::value ? 1u : 0u;
+            constexpr uint32_t kIdescS = (1u << 4) | (kType << 7) | (kType << 10) | ((kTile / 16) << 24);      // and the columns / 8 at bit 17
+            constexpr uint32_t kIdescO = (1u << 4) | (kType << 7) | (kType << 10) | (1u << 16) | ((D / 8) << 17) | ((kTile / 16) << 24);
+            const uint32_t k0 = operand(base + Smem::kRing, 16), v0 = operand(base + Smem::kRing, kTile * 128), q0 = operand(base + Smem::kQ, 16);
+            uint32_t weights_phase = 0, cleared_phase = 0, free_phase = 0, started = 0, pos = 0;
+            auto arrived = [&](uint32_t x) { bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, failed); };
+            for (uint32_t r = 0;; ++r) {
+                const FeedSlot f = feed_next<false>(sh.feed, r, failed);
+                if (!f.valid) break;
+                const Item it = make_item(a, f);
+                const int32_t n = it.steps();
+                auto scores_of = [&](uint32_t t, int32_t seen, uint32_t x) {                                   // x: place of the keys in the ring
+                    const uint32_t k = k0 + x % kStages * (Smem::kTileBytes >> 4), q = q0 + t * (Smem::kTileBytes >> 4);
+                    const uint32_t idesc = kIdescS | (uint32_t)((seen + 15) >> 4) << 18, to = tmem + t * kTile;
+#pragma unroll
+                    for (int x = 0; x < D / 16; ++x) {
+                        const uint32_t off = ((x >> 2) * (kTile * 128) + (x & 3) * 32) >> 4;
+                        mma_smem(lead, to, q + off, k + off, idesc, x > 0);
+                    }
+                    mma_commit(lead, scores + 8 * t);
+                };
+                bar_wait(queries, r & 1, failed);
+                arrived(pos);
+                fence_after();
+#pragma unroll 1
+                for (uint32_t t = 0; t < 2; ++t)
+                    if ((t ? it.n[1] : it.n[0]) > 0) scores_of(t, it.seen(0, t), pos);
+                mma_commit(lead, empty + 8 * (pos % kStages));
+                if (n == 1) mma_commit(lead, queries_free);
+#pragma unroll 1
+                for (int32_t j = 0; j < n; ++j, pos += 2) {
+                    const uint32_t values = pos + 1, keys = pos + 2, v = v0 + values % kStages * (Smem::kTileBytes >> 4);
+                    arrived(values);
+                    if (it.count(j) & 15) {
+                        bar_wait(cleared + 8 * (values % kStages), cleared_phase >> values % kStages & 1, failed);
+                        cleared_phase ^= 1u << values % kStages;
+                    }
+                    if (j + 1 < n) arrived(keys);
+#pragma unroll 1
+                    for (uint32_t t = 0; t < 2; ++t) {
+                        const int32_t mine = t ? it.n[1] : it.n[0];
+                        if (j >= mine) continue;
+                        const int32_t seen = it.seen(j, t);
+                        const uint32_t w = tmem + t * kTile, o = tmem + 256 + t * D, told = weights + 16 * t, phase = weights_phase >> t & 1;
+                        weights_phase ^= 1u << t;
+                        bar_wait(told, phase, failed);
+                        if (j == 0) {                    // the output of the item before has been read
+                            if (started >> t & 1) {
+                                bar_wait(output_free + 8 * t, free_phase >> t & 1, failed);
+                                free_phase ^= 1u << t;
+                            }
+                            started |= 1u << t;
+                        }
+                        fence_after();
+                        mma_tmem(lead, o, w, v, kIdescO, j > 0);
+                        if (seen == kTile) {
+#pragma unroll
+                            for (int g = 1; g < 4; ++g) mma_tmem(lead, o, w + g * 8, v + g * (2048 >> 4), kIdescO, 1);
+                            bar_wait(told + 8, phase, failed);
+                            fence_after();
+#pragma unroll
+                            for (int g = 4; g < 8; ++g) mma_tmem(lead, o, w + g * 8, v + g * (2048 >> 4), kIdescO, 1);
+                        } else {
+                            bar_wait(told + 8, phase, failed);
+                            fence_after();
+#pragma unroll 1
+                            for (int g = 1; g * 16 < seen; ++g) mma_tmem(lead, o, w + g * 8, v + g * (2048 >> 4), kIdescO, 1);
+                        }
+                        if (j + 1 < mine) scores_of(t, it.seen(j + 1, t), keys);
+                        else mma_commit(lead, output + 8 * t);
+                    }
+                    mma_commit(lead, empty + 8 * (values % kStages));
+                    if (j + 1 < n) mma_commit(lead, empty + 8 * (keys % kStages));
+                    if (j + 2 == n) mma_commit(lead, queries_free);
+                }
+            }
         }
-    } else if (warp < 8) {
+    } else {
         // ---- softmax: thread `row` of a tile has row `row` of its scores
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const int t = warp >> 2, row = threadIdx.x & (kTile - 1);
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
         const uint32_t t_s = lanes + t * kTile, t_o = lanes + 256 + t * D;
         const int32_t row_token = row / a.hp, row_head = row - row_token * a.hp;
         uint32_t scores_phase = 0, n_output = 0;
-        RawItem next = fetch_item(a, 0, n_items);
-        for (int32_t r = 0; next.valid && ok; ++r) {
-            const Item it = make_item(a, next);
-            next = fetch_item(a, r + 1, n_items);
-            const int32_t n = it.n[t];
+        for (uint32_t r = 0; ok; ++r) {
+            const FeedSlot f = feed_next<false>(sh.feed, r, failed);
+            if (!f.valid) break;
+            const Item it = make_item(a, f);
+            const int32_t n = t ? it.n[1] : it.n[0], tokens = t ? it.tokens[1] : it.tokens[0];
             if (n == 0) continue;
             const int32_t token = it.token0 + t * a.tp + row_token;
-            const bool have = row_token < it.tokens[t];
+            const bool have = row_token < tokens;
             const int32_t seen_to = a.causal && have ? min(it.end, token + 1) : it.end;
             float m = -INFINITY, l = 0.f;
             for (int32_t j = 0; j < n; ++j) {
-                int32_t limit;                           // keys of the step that the row sees
-                if (j < it.n_shared) limit = it.shared1 - it.shared0 - j * kTile;
-                else limit = seen_to - it.own0 - (j - it.n_shared) * kTile;
+                // keys of the step that the row sees
+                const int32_t limit = j < it.n_shared ? it.shared1 - it.shared0 - j * kTile : seen_to - it.own0 - (j - it.n_shared) * kTile;
                 ok = bar_wait(scores + 8 * t, scores_phase, failed);
                 scores_phase ^= 1;
                 ok = __all_sync(kFull, ok);
                 if (!ok) break;
                 fence_after();
-                float s[4][32];
-#pragma unroll
-                for (int b = 0; b < 4; ++b) tmem_load(t_s + b * 32, s[b]);
-                tmem_load_wait();
-                if (__any_sync(kFull, limit < kTile)) {
-#pragma unroll
-                    for (int b = 0; b < 4; ++b)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            if (b * 32 + e >= limit) s[b][e] = -INFINITY;
-                }
-                float t4[4];
-#pragma unroll
-                for (int b = 0; b < 4; ++b) {
-                    t4[b] = s[b][0];
-#pragma unroll
-                    for (int e = 1; e < 31; e += 2) t4[b] = fmaxf(t4[b], fmaxf(s[b][e], s[b][e + 1]));
-                    t4[b] = fmaxf(t4[b], s[b][31]);
-                }
-                const float top = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3])) * a.scale_log2;
-                if (j == 0) {
-                    m = top;
-                } else if (__any_sync(kFull, have && top > m + 8.f)) {      // rows of no token may hold anything: they have no say
-                    const float up = fmaxf(m, top), f = up == -INFINITY ? 1.f : exp2_approx(m - up);
-                    l *= f;
-                    m = up;
-#pragma unroll 1
-                    for (int b = 0; b < D / 16; ++b) {
-                        float o[16];
-                        tmem_load16(t_o + b * 16, o);
-                        tmem_load_wait();
-#pragma unroll
-                        for (int e = 0; e < 16; ++e) o[e] *= f;
-                        tmem_store16(t_o + b * 16, o);
-                    }
-                }
-                // where no key has been seen the reference is -infinity and every weight has to come out as 0
-                const float z = m == -INFINITY ? 0.f : m;
-                float2 sum = make_float2(0.f, 0.f);
-#pragma unroll
-                for (int b = 0; b < 8; ++b) {
-                    uint32_t w[8];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        float2 y = make_float2(s[b >> 1][(b & 1) * 16 + 2 * e], s[b >> 1][(b & 1) * 16 + 2 * e + 1]);
-                        y = fma2(y, make_float2(a.scale_log2, a.scale_log2), make_float2(-z, -z));
-                        y = make_float2(exp2_approx(y.x), exp2_approx(y.y));
-                        sum = add2(sum, y);
-                        w[e] = pack2(y.x, y.y, Q());
-                    }
-                    tmem_store8(t_s + b * 8, w);
-                }
-                l += sum.x + sum.y;
-                tmem_store_wait();
-                fence_before();
-                bar_arrive(weights + 8 * t);
+                softmax_step<Q, D>(t_s, t_o, weights + 16 * t, a.scale_log2, it.seen(j, t), limit, !__any_sync(kFull, limit < kTile), have, j == 0, m, l);
             }
             if (!ok) break;
             ok = bar_wait(output + 8 * t, n_output++ & 1, failed);
             ok = __all_sync(kFull, ok);
             if (!ok) break;
             fence_after();
-            const float inv = l == 0.f ? 0.f : 1.f / l;       // NaN where a score was NaN: it is in no maximum, but in the sum
+            const float inv = l == 0.f ? 0.f : 1.f / l;  // NaN where a score was NaN: it is in no maximum, but in the sum
             const int32_t head = it.block * a.hp + row_head;
-            Q *out = static_cast<Q *>(a.out) + (int64_t)token * a.out_stride + (int64_t)head * D;
+            const int64_t to = have ? (int64_t)token * a.out_stride + (int64_t)head * D : -1;
+            // 32 columns at a time through shared memory, so that four lanes store 64 bytes of a row
+            const uint32_t staging = base + Smem::kStaging + warp * (kWarp * 64);
+            int64_t at[4];
+#pragma unroll
+            for (int v = 0; v < 4; ++v) at[v] = __shfl_sync(kFull, to, v * 8 + (lane >> 2));
 #pragma unroll 1
-            for (int b = 0; b < D / 32; ++b) {
+            for (int p = 0; p < D / 32; ++p) {
                 float o[32];
-                tmem_load(t_o + b * 32, o);
+                tmem_load(t_o + p * 32, o);
                 tmem_load_wait();
-                if (have) {
+                if (p == D / 32 - 1) {
+                    fence_before();
+                    bar_arrive(output_free + 8 * t);
+                }
+                __syncwarp();
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        float x[8];
+                for (int v = 0; v < 4; ++v) {
+                    float x[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] = o[v * 8 + e] * inv;
-                        *reinterpret_cast<uint4 *>(out + b * 32 + v * 8) = pack8<Q>(x);
-                    }
+                    for (int e = 0; e < 8; ++e) x[e] = o[v * 8 + e] * inv;
+                    const uint4 y = pack8<Q>(x);
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(staging + lane * 64 + ((v ^ (lane >> 1 & 3)) << 4)), "r"(y.x), "r"(y.y), "r"(y.z), "r"(y.w) : "memory");
+                }
+                __syncwarp();
+#pragma unroll
+                for (int v = 0; v < 4; ++v) {
+                    const int x = v * 8 + (lane >> 2);   // row of the warp
+                    uint4 y;
+                    asm volatile("ld.shared.v4.b32 {%0,%1,%2,%3}, [%4];" : "=r"(y.x), "=r"(y.y), "=r"(y.z), "=r"(y.w) : "r"(staging + x * 64 + (((lane & 3) ^ (x >> 1 & 3)) << 4)) : "memory");
+                    if (at[v] >= 0) *reinterpret_cast<uint4 *>(static_cast<Q *>(a.out) + at[v] + p * 32 + (lane & 3) * 8) = y;
                 }
             }
-            fence_before();
-            bar_arrive(output_free + 8 * t);
             if (have && a.lse != nullptr) a.lse[(int64_t)token * a.Hq + head] = (m == -INFINITY ? 0.f : kLn2 * m) + logf(l);
         }
     }

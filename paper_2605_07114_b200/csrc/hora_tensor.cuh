@@ -25,6 +25,7 @@ __device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
 }
 // Waits for the phase of the given parity to complete; false when the limit is reached or another wait of the CTA has failed.
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int32_t *failed) {
+#pragma unroll 1
     for (uint32_t i = 0; i < kWaitTries; ++i) {
         uint32_t done;
         asm volatile(
@@ -83,6 +84,25 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+// The same by whole warps, one lane of which (`lead`) is to issue: without a branch, so that what an instruction takes from
+// uniform registers is worked out there.
+__device__ __forceinline__ void mma_smem(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
+    asm volatile(
+        "{\n.reg .pred p, l;\n.reg .b64 da, db;\nmov.b64 da, {%1, %5};\nmov.b64 db, {%2, %5};\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 l, %6, 0;\n"
+        "@l tcgen05.mma.cta_group::1.kind::f16 [%0], da, db, %3, p;\n}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(add), "r"(kOperandHigh), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void mma_tmem(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t add) {
+    asm volatile(
+        "{\n.reg .pred p, l;\n.reg .b64 db;\nmov.b64 db, {%2, %5};\nsetp.ne.b32 p, %4, 0;\nsetp.ne.b32 l, %6, 0;\n"
+        "@l tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"(add), "r"(kOperandHigh), "r"(lead)
+        : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t lead, uint32_t bar) {
+    asm volatile("{\n.reg .pred l;\nsetp.ne.b32 l, %1, 0;\n@l tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(bar), "r"(lead) : "memory");
+}
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
@@ -114,6 +134,15 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const float (&r)[16]) 
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"f"(r[0]), "f"(r[1]),
         "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]),
         "f"(r[14]), "f"(r[15]), "r"(at)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store32(uint32_t at, const float (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"f"(r[0]), "f"(r[1]),
+        "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]),
+        "f"(r[14]), "f"(r[15]), "f"(r[16]), "f"(r[17]), "f"(r[18]), "f"(r[19]), "f"(r[20]), "f"(r[21]), "f"(r[22]), "f"(r[23]), "f"(r[24]),
+        "f"(r[25]), "f"(r[26]), "f"(r[27]), "f"(r[28]), "f"(r[29]), "f"(r[30]), "f"(r[31]), "r"(at)
         : "memory");
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
