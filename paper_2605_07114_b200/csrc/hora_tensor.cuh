@@ -43,6 +43,22 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     return false;
 }
 
+// Two of them: asked for together, since an answer takes a hundred cycles and more even where there is nothing to wait for.
+__device__ __forceinline__ void bar_wait_both(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1, volatile int32_t *failed) {
+    uint32_t done;
+    asm volatile(
+        "{\n.reg .pred p, q;\n"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
+        "mbarrier.test_wait.parity.shared::cta.b64 q, [%3], %4;\n"
+        "and.pred p, p, q;\nselp.b32 %0, 1, 0, p;\n}"
+        : "=r"(done)
+        : "r"(bar0), "r"(parity0), "r"(bar1), "r"(parity1)
+        : "memory");
+    if (done) return;
+    bar_wait(bar0, parity0, failed);
+    bar_wait(bar1, parity1, failed);
+}
+
 __device__ __forceinline__ void tma_box(uint32_t to, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to), "l"(map),
                  "r"(x), "r"(y), "r"(bar)
