@@ -10,7 +10,7 @@
 // which the same tiles of dO and Q are read the other way round.  Nothing but the four operands ever is in shared memory.
 //   Queries: an item is one tile of queries; S = Q K^T, dP = dO V^T, dQ += dS K.
 //   Eight warps do what is between the products, two threads to a row, 64 columns each; while they work on the weights of a step the tensor
-// cores compute its dP, and while they work on its dS the tensor cores have the next step's scores to do.
+// cores compute its dP, and while they work on its dS the tensor cores have the next step's scores to do.  Two warps issue the products.
 //   Rows of a tile that are not of the run of queries (or keys) are cleared in shared memory where a product sums over them.
 //   Every wait has a limit; a wait that reaches it makes the CTA give up and report HORA_ERR_INTERNAL.
 #define HORA_FILE_ID 12
@@ -25,8 +25,8 @@ namespace hora {
 namespace {
 
 constexpr int kTile = kPackedRows, kHalfTile = kTile / 2;
-constexpr int kMiddleThreads = 256, kLoadWarp = 8, kProductWarp = 9, kStatsWarp = 10, kFeedWarp = 11;
-constexpr int kKeysReaders = 11, kQueriesReaders = 10;   // warps that take items from the feeder
+constexpr int kMiddleThreads = 256, kLoadWarp = 8, kProductWarp = 9, kFeedWarp = 11;   // two warps issue products
+constexpr int kFeedReaders = 11;                         // warps that take items from the feeder
 
 template <typename Q>
 constexpr uint32_t kType = std::is_same<Q, __nv_bfloat16>::value ? 1u : 0u;
@@ -35,22 +35,27 @@ constexpr uint32_t kIdescScores = (1u << 4) | (kType<Q> << 7) | (kType<Q> << 10)
 template <typename Q, int D>
 constexpr uint32_t kIdescSum = (1u << 4) | (kType<Q> << 7) | (kType<Q> << 10) | (1u << 16) | ((D / 8) << 17) | ((kTile / 16) << 24);
 
-// The product over D of a tile's 128 rows `a` and the first `count` rows of `b` (up to a multiple of sixteen).  One elected lane.
+// The product over D of a tile's 128 rows `a` and the first `count` rows of `b` (up to a multiple of sixteen).  Whole warps, here and below.
 template <typename Q, int D>
-__device__ __forceinline__ void product_of_rows(uint32_t d, uint32_t a, uint32_t b, int32_t count) {
+__device__ __forceinline__ void product_of_rows(uint32_t lead, uint32_t d, uint32_t a, uint32_t b, int32_t count) {
     const uint32_t idesc = kIdescScores<Q> | (uint32_t)((count + 15) >> 4) << 18;
 #pragma unroll
     for (int x = 0; x < D / 16; ++x) {
         const uint32_t off = ((x >> 2) * (kTile * 128) + (x & 3) * 32) >> 4;
-        mma_smem(d, a + off, b + off, idesc, x > 0);
+        mma_smem(lead, d, a + off, b + off, idesc, x > 0);
     }
 }
 // d += w b, w 128 x `count` in tensor memory (16 bits, its two halves of 64 columns 64 columns of 32 bits apart), b `count` rows of D.
 template <typename Q, int D>
-__device__ __forceinline__ void product_with_weights(uint32_t d, uint32_t w, uint32_t b, int32_t count, bool first) {
+__device__ __forceinline__ void product_with_weights(uint32_t lead, uint32_t d, uint32_t w, uint32_t b, int32_t count, bool first) {
+    mma_tmem(lead, d, w, b, kIdescSum<Q, D>, !first);
+    if (count > kTile - 16) {
 #pragma unroll
-    for (int g = 0; g < kTile / 16; ++g)
-        if (g * 16 < count) mma_tmem(d, w + (g < 4 ? g * 8 : kHalfTile + (g - 4) * 8), b + g * (2048 >> 4), kIdescSum<Q, D>, !first || g > 0);
+        for (int g = 1; g < kTile / 16; ++g) mma_tmem(lead, d, w + (g < 4 ? g * 8 : kHalfTile + (g - 4) * 8), b + g * (2048 >> 4), kIdescSum<Q, D>, 1);
+    } else {
+#pragma unroll 1
+        for (int g = 1; g * 16 < count; ++g) mma_tmem(lead, d, w + g * 8 + (g < 4 ? 0 : kHalfTile - 32), b + g * (2048 >> 4), kIdescSum<Q, D>, 1);
+    }
 }
 
 // Rows count .. of a tile up to the last sixteen that a product reads are set to zero.  All lanes of a warp.
@@ -150,7 +155,8 @@ __global__ void __launch_bounds__(kPackedThreads, 1)
 packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap do_map,
                    const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     using Smem = KeysSmem<D>;
-    constexpr int kStages = Smem::kStages, kParts = D / 64;
+    constexpr uint32_t kStages = Smem::kStages;
+    constexpr int kParts = D / 64;
     KeysShared &sh = *reinterpret_cast<KeysShared *>(s_backward + Smem::kSmall);
     const uint32_t base = smem_at(s_backward);
     const int warp = threadIdx.x >> 5, lane = lane_id();
@@ -165,24 +171,24 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
                    sums_free = smem_at(&sh.sums_free);
     if (threadIdx.x == 0) {
         sh.failed = 0;
-        feed_init(sh.feed, kKeysReaders);
-        for (int s = 0; s < kStages; ++s) {
+        feed_init(sh.feed, kFeedReaders);
+        for (uint32_t s = 0; s < kStages; ++s) {
             bar_init(full + 8 * s, 1 + kWarp);
-            bar_init(empty + 8 * s, 1);
+            bar_init(empty + 8 * s, 2);
         }
         bar_init(keys, 1);
-        bar_init(keys_free, 1);
+        bar_init(keys_free, 2);
         bar_init(scores, 1);
         bar_init(weights, kMiddleThreads);
         bar_init(products, 1);
         bar_init(gradients, kMiddleThreads);
-        bar_init(sums, 1);
+        bar_init(sums, 2);
         bar_init(sums_free, kMiddleThreads);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     // rows that no tile of queries fills
     const int32_t rows = a.hp * a.tp, idle = kTile - rows;
-    for (int32_t c = threadIdx.x; c < 2 * kStages * kParts * idle * 8; c += kPackedThreads) {
+    for (int32_t c = threadIdx.x; c < 2 * (int32_t)kStages * kParts * idle * 8; c += kPackedThreads) {
         const int32_t x = c >> 3, part = x / idle;
         const uint32_t to = base + Smem::kRing + part * (kTile * 128) + (rows + x - part * idle) * 128 + (c & 7) * 16;
         asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(to), "r"(0) : "memory");
@@ -203,24 +209,39 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
     if (warp == kFeedWarp) {
         if (lane == 0) feed<2>(sh.feed, reinterpret_cast<const int4 *>(a.key_items), __ldcg(a.counts + 1), a.Hkv, a.counts + 5, failed);
     } else if (warp == kLoadWarp) {
-        if (lane == 0) {
-            int32_t pos = 0;
-            uint32_t turn = 0;
-            for (int32_t r = 0; ok; ++r, ++turn) {
-                const KeyWork it = make_keys(a, feed_next<true>(sh.feed, r, failed));
-                if (!it.valid) break;
-                if (r > 0) ok = bar_wait(keys_free, (turn + 1) & 1, failed);
-                if (!ok) break;
+        // ---- keys, values, tiles of queries and of gradients of outputs; and of each row of a step -lse and -dout.out
+        const float c = exp2f((float)(shift - up));
+        uint32_t pos = 0, r = 0;
+        for (; ok; ++r) {
+            const KeyWork it = make_keys(a, feed_next<false>(sh.feed, r, failed));
+            if (!it.valid) break;
+            if (r > 0) ok = __all_sync(kFull, bar_wait(keys_free, (r + 1) & 1, failed));
+            if (!ok) break;
+            if (lane == 0) {
                 bar_expect(keys, 2 * Smem::kTileBytes);
                 for (int p = 0; p < kParts; ++p) {
                     tma_box3(base + Smem::kK + p * (kTile * 128), &k_map, p * 64, it.head, it.key0, keys);
                     tma_box3(base + Smem::kV + p * (kTile * 128), &v_map, p * 64, it.head, it.key0, keys);
                 }
-                for (int32_t s = 0; s < it.steps; ++s, ++pos) {
-                    const KeyStep k = key_step(a, it, s);
-                    const int stage = pos % kStages;
-                    if (pos >= kStages) ok = bar_wait(empty + 8 * stage, (pos / kStages + 1) & 1, failed);
-                    if (!ok) break;
+            }
+            __syncwarp();
+            auto stats_of = [&](int32_t s, float2 (&st)[kTile / kWarp]) {
+                const KeyStep k = key_step(a, it, s);
+#pragma unroll
+                for (int i = 0; i < kTile / kWarp; ++i) {
+                    const int32_t row = lane + i * kWarp, token = k.token0 + row / a.hp;
+                    st[i] = make_float2(INFINITY, 0.f);
+                    if (row < k.count && HORA_IN(token, a.T)) st[i] = __ldcg(a.stats + (int64_t)token * a.Hq + k.block * a.hp + row % a.hp);
+                }
+            };
+            float2 st[kTile / kWarp];
+            stats_of(0, st);
+            for (int32_t s = 0; s < it.steps; ++s, ++pos) {
+                const KeyStep k = key_step(a, it, s);
+                const uint32_t stage = pos % kStages;
+                if (pos >= kStages) ok = __all_sync(kFull, bar_wait(empty + 8 * stage, (pos / kStages + 1) & 1, failed));
+                if (!ok) break;
+                if (lane == 0) {
                     bar_expect(full + 8 * stage, 2 * kParts * rows * 128);
                     const uint32_t at = base + Smem::kRing + stage * 2 * Smem::kTileBytes;
                     for (int p = 0; p < kParts; ++p) {
@@ -228,111 +249,67 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
                         tma_box3(at + Smem::kTileBytes + p * (kTile * 128), &do_map, p * 64, k.block * a.hp, k.token0, full + 8 * stage);
                     }
                 }
-            }
-            if (*failed) {
-                // copies on their way to the CTA: the barriers of their stages may lack the other arrivals, so it is time that is waited for
-                int32_t never = 0;
-                if (turn > 0) bar_wait(keys, (turn - 1) & 1, &never);
-                for (int32_t x = max(0, pos - kStages); x < pos; ++x) bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, &never);
-            }
-        }
-    } else if (warp == kProductWarp) {
-        const uint32_t k_rows = operand(base + Smem::kK, 16), v_rows = operand(base + Smem::kV, 16);
-        uint32_t weights_phase = 0, gradients_phase = 0;
-        int32_t pos = 0;
-        for (int32_t r = 0; ok; ++r) {
-            const KeyWork it = make_keys(a, feed_next<false>(sh.feed, r, failed));
-            if (!it.valid) break;
-            auto arrived = [&](int32_t s) {              // the tiles of step s
-                const int32_t x = pos + s;
-                if (!bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, failed)) return false;
-                const KeyStep k = key_step(a, it, s);
-                if (!k.whole && (k.count & 15)) {
-                    const uint32_t at = base + Smem::kRing + (x % kStages) * 2 * Smem::kTileBytes;
-                    clear_rows<D>(at, k.count);
-                    clear_rows<D>(at + Smem::kTileBytes, k.count);
-                    publish_clears();
-                }
-                fence_after();
-                return true;
-            };
-            auto tile = [&](int32_t s, int which, uint32_t lead) {
-                return operand(base + Smem::kRing + ((pos + s) % kStages * 2 + which) * Smem::kTileBytes, lead);
-            };
-            ok = bar_wait(keys, r & 1, failed) && arrived(0);
-            if (!ok) break;
-            if (elect_one()) {
-                const int32_t count = key_step(a, it, 0).count;
-                product_of_rows<Q, D>(tmem, k_rows, tile(0, 0, 16), count);
-                mma_commit(scores);
-                product_of_rows<Q, D>(tmem + kTile, v_rows, tile(0, 1, 16), count);
-                mma_commit(products);
-            }
-            __syncwarp();
-            for (int32_t s = 0; s < it.steps; ++s) {
-                const int32_t count = key_step(a, it, s).count, next_count = key_step(a, it, s + 1).count;
-                const bool more = s + 1 < it.steps;
-                ok = bar_wait(weights, weights_phase, failed);
-                weights_phase ^= 1;
-                if (ok && s == 0 && r > 0) ok = bar_wait(sums_free, (r + 1) & 1, failed);
-                if (!ok) break;
-                fence_after();
-                if (elect_one()) product_with_weights<Q, D>(tmem + 256, tmem, tile(s, 1, kTile * 128), count, s == 0);
                 __syncwarp();
-                if (more) {
-                    ok = arrived(s + 1);
-                    if (!ok) break;
-                    if (elect_one()) {
-                        product_of_rows<Q, D>(tmem, k_rows, tile(s + 1, 0, 16), next_count);
-                        mma_commit(scores);
-                    }
-                    __syncwarp();
-                }
-                ok = bar_wait(gradients, gradients_phase, failed);
-                gradients_phase ^= 1;
-                if (!ok) break;
-                fence_after();
-                if (elect_one()) {
-                    product_with_weights<Q, D>(tmem + 256 + D, tmem + kTile, tile(s, 0, kTile * 128), count, s == 0);
-                    mma_commit(empty + 8 * ((pos + s) % kStages));
-                    if (more) {
-                        product_of_rows<Q, D>(tmem + kTile, v_rows, tile(s + 1, 1, 16), next_count);
-                        mma_commit(products);
-                    } else {
-                        mma_commit(keys_free);
-                        mma_commit(sums);
-                    }
-                }
-                __syncwarp();
-            }
-            pos += it.steps;
-        }
-    } else if (warp == kStatsWarp) {
-        // ---- of each row of a step: -lse and -dout.out
-        const float c = exp2f((float)(shift - up));
-        int32_t pos = 0;
-        for (int32_t r = 0; ok; ++r) {
-            const KeyWork it = make_keys(a, feed_next<false>(sh.feed, r, failed));
-            if (!it.valid) break;
-            for (int32_t s = 0; s < it.steps; ++s, ++pos) {
-                const KeyStep k = key_step(a, it, s);
-                const int stage = pos % kStages;
-                float2 st[kTile / kWarp];
-#pragma unroll
-                for (int i = 0; i < kTile / kWarp; ++i) {
-                    const int32_t row = lane + i * kWarp, token = k.token0 + row / a.hp;
-                    st[i] = make_float2(INFINITY, 0.f);
-                    if (row < k.count && HORA_IN(token, a.T)) st[i] = __ldcg(a.stats + (int64_t)token * a.Hq + k.block * a.hp + row % a.hp);
-                }
-                if (pos >= kStages) ok = bar_wait(empty + 8 * stage, (pos / kStages + 1) & 1, failed);
-                if (!ok) break;
 #pragma unroll
                 for (int i = 0; i < kTile / kWarp; ++i) {
                     sh.lse[stage][lane + i * kWarp] = (float)up - st[i].x;
                     sh.delta[stage][lane + i * kWarp] = -st[i].y * c;
                 }
                 bar_arrive(full + 8 * stage);
+                if (s + 1 < it.steps) stats_of(s + 1, st);
             }
+        }
+        if (*failed && lane == 0) {                      // copies on their way to the CTA
+            int32_t never = 0;
+            if (r > 0) bar_wait(keys, (r - 1) & 1, &never);
+            for (uint32_t x = pos < kStages ? 0 : pos - kStages; x < pos; ++x) bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, &never);
+        }
+    } else if (warp >= kProductWarp) {
+        // ---- products: one warp S^T and dV, the other dP^T and dK, each with its own part of tensor memory.  A wait that has failed is not looked
+        // at here: what follows is of no use, but in bounds, and there is no next item
+        const uint32_t which = warp - kProductWarp, lead = elect_one();
+        const uint32_t rows_a = operand(base + (which ? Smem::kV : Smem::kK), 16), between = tmem + which * kTile, sum = tmem + 256 + which * D;
+        const uint32_t there = which ? products : scores, back = which ? gradients : weights;
+        uint32_t phase = 0, pos = 0;
+        for (uint32_t r = 0;; ++r) {
+            const KeyWork it = make_keys(a, feed_next<false>(sh.feed, r, failed));
+            if (!it.valid) break;
+            // the tiles of step s, rows of others cleared by both warps: either may be the first to need it
+            auto arrived = [&](int32_t s, uint32_t stage) {
+                bar_wait(full + 8 * stage, (pos + s) / kStages & 1, failed);
+                const KeyStep k = key_step(a, it, s);
+                if (!k.whole && (k.count & 15)) {
+                    const uint32_t at = base + Smem::kRing + stage * 2 * Smem::kTileBytes;
+                    clear_rows<D>(at, k.count);
+                    clear_rows<D>(at + Smem::kTileBytes, k.count);
+                    publish_clears();
+                }
+                fence_after();
+                // S^T from the queries, dP^T from the gradients of outputs
+                product_of_rows<Q, D>(lead, between, rows_a, operand(base + Smem::kRing + (stage * 2 + which) * Smem::kTileBytes, 16), k.count);
+                mma_commit(lead, there);
+                return k.count;
+            };
+            bar_wait(keys, r & 1, failed);
+            int32_t count = arrived(0, pos % kStages);
+#pragma unroll 1
+            for (int32_t s = 0; s < it.steps; ++s) {
+                const uint32_t stage = (pos + s) % kStages;
+                bar_wait(back, phase, failed);
+                phase ^= 1;
+                if (s == 0 && r > 0) bar_wait(sums_free, (r + 1) & 1, failed);
+                fence_after();
+                // dV from the gradients of outputs, dK from the queries
+                product_with_weights<Q, D>(lead, sum, between, operand(base + Smem::kRing + (stage * 2 + 1 - which) * Smem::kTileBytes, kTile * 128), count, s == 0);
+                mma_commit(lead, empty + 8 * stage);
+                if (s + 1 < it.steps) {
+                    count = arrived(s + 1, (pos + s + 1) % kStages);
+                } else {
+                    mma_commit(lead, keys_free);
+                    mma_commit(lead, sums);
+                }
+            }
+            pos += it.steps;
         }
     } else {
         // ---- between the products: thread `row` of either half has 64 columns (queries) of a key
@@ -341,14 +318,13 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
         const uint32_t t_s = lanes + half * kHalfTile, t_dp = lanes + kTile + half * kHalfTile;
         const float c = exp2f((float)(shift - up));
         const float2 scale2 = make_float2(a.scale_log2, a.scale_log2), c2 = make_float2(c, c);
-        uint32_t phase = 0;
-        int32_t pos = 0;
+        uint32_t phase = 0, pos = 0;
         for (int32_t r = 0; ok; ++r) {
             const KeyWork it = make_keys(a, feed_next<false>(sh.feed, r, failed));
             if (!it.valid) break;
             for (int32_t s = 0; s < it.steps; ++s, ++pos, phase ^= 1) {
                 const KeyStep k = key_step(a, it, s);
-                const int stage = pos % kStages;
+                const uint32_t stage = pos % kStages;
                 ok = bar_wait(full + 8 * stage, (pos / kStages) & 1, failed) && bar_wait(scores, phase, failed);
                 ok = __all_sync(kFull, ok);
                 if (!ok) break;
@@ -491,13 +467,13 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
 template <int D>
 struct QueriesSmem {
     static constexpr int kTileBytes = kTile * D * 2;
-    static constexpr int kStages = D == 128 ? 5 : 10;    // keys or values
-    static constexpr int kQ = 0, kDo = kTileBytes, kRing = 2 * kTileBytes, kSmall = kRing + kStages * kTileBytes;
+    static constexpr int kKeyStages = D == 128 ? 3 : 4, kValueStages = D == 128 ? 2 : 4;
+    static constexpr int kQ = 0, kDo = kTileBytes, kKeys = 2 * kTileBytes, kValues = kKeys + kKeyStages * kTileBytes, kSmall = kValues + kValueStages * kTileBytes;
 };
 
 struct QueriesShared {
     Feed feed;
-    uint64_t full[10], empty[10], queries, queries_free, scores, scores_free, products, gradients, sums, sums_free;
+    uint64_t full[8], empty[8], queries, queries_free, scores, scores_free, products[2], gradients[2], sums, sums_free;       // full, empty: keys, then values
     int32_t failed;
     uint32_t tmem;
 };
@@ -532,7 +508,8 @@ __global__ void __launch_bounds__(kPackedThreads, 1)
 packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap do_map,
                       const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map) {
     using Smem = QueriesSmem<D>;
-    constexpr int kStages = Smem::kStages, kParts = D / 64;
+    constexpr uint32_t kKeyStages = Smem::kKeyStages, kValueStages = Smem::kValueStages;
+    constexpr int kParts = D / 64;
     QueriesShared &sh = *reinterpret_cast<QueriesShared *>(s_backward + Smem::kSmall);
     const uint32_t base = smem_at(s_backward);
     const int warp = threadIdx.x >> 5, lane = lane_id();
@@ -543,21 +520,23 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
         return;
     }
     const uint32_t full = smem_at(sh.full), empty = smem_at(sh.empty), queries = smem_at(&sh.queries), queries_free = smem_at(&sh.queries_free),
-                   scores = smem_at(&sh.scores), scores_free = smem_at(&sh.scores_free), products = smem_at(&sh.products), gradients = smem_at(&sh.gradients),
+                   scores = smem_at(&sh.scores), scores_free = smem_at(&sh.scores_free), products = smem_at(sh.products), gradients = smem_at(sh.gradients),
                    sums = smem_at(&sh.sums), sums_free = smem_at(&sh.sums_free);
     if (threadIdx.x == 0) {
         sh.failed = 0;
-        feed_init(sh.feed, kQueriesReaders);
-        for (int s = 0; s < kStages; ++s) {
+        feed_init(sh.feed, kFeedReaders);
+        for (uint32_t s = 0; s < kKeyStages + kValueStages; ++s) {
             bar_init(full + 8 * s, 1);
-            bar_init(empty + 8 * s, 1);
+            bar_init(empty + 8 * s, s < kKeyStages ? 2 : 1);             // both products' warps read keys
         }
         bar_init(queries, 1);
-        bar_init(queries_free, 1);
+        bar_init(queries_free, 2);
         bar_init(scores, 1);
         bar_init(scores_free, kMiddleThreads);
-        bar_init(products, 1);
-        bar_init(gradients, kMiddleThreads);
+        for (int b = 0; b < 2; ++b) {
+            bar_init(products + 8 * b, 1);
+            bar_init(gradients + 8 * b, kMiddleThreads);
+        }
         bar_init(sums, 1);
         bar_init(sums_free, kMiddleThreads);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -570,7 +549,7 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
     }
     __syncthreads();
     fence_after();
-    const uint32_t tmem = sh.tmem;                       // columns: S, dP, dQ
+    const uint32_t tmem = sh.tmem;                       // columns: S, dP in two places, dQ
     pdl_enter();
     const int shift = gradient_shift(a), up = a.half ? kHalfShift : 0;
     bool ok = true;
@@ -579,116 +558,101 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
         if (lane == 0) feed<2>(sh.feed, reinterpret_cast<const int4 *>(a.query_items), __ldcg(a.counts), a.blocks, a.counts + 4, failed);
     } else if (warp == kLoadWarp) {
         if (lane == 0) {
-            int32_t pos = 0;
-            uint32_t turn = 0;
-            for (int32_t r = 0; ok; ++r, ++turn) {
+            uint32_t pos = 0, r = 0;                     // steps so far
+            auto bring = [&](uint32_t first, uint32_t stages, uint32_t to, const CUtensorMap *map, int32_t head, int32_t key0) {
+                const uint32_t stage = pos % stages, bar = first + stage;
+                if (pos >= stages) ok = bar_wait(empty + 8 * bar, (pos / stages + 1) & 1, failed);
+                if (!ok) return;
+                bar_expect(full + 8 * bar, Smem::kTileBytes);
+                for (int p = 0; p < kParts; ++p) tma_box3(base + to + stage * Smem::kTileBytes + p * (kTile * 128), map, p * 64, head, key0, full + 8 * bar);
+            };
+            for (; ok; ++r) {
                 const QueryWork it = make_queries(a, feed_next<true>(sh.feed, r, failed));
                 if (!it.valid) break;
                 const int32_t head = it.block * a.hp / a.g;
-                if (r > 0) ok = bar_wait(queries_free, (turn + 1) & 1, failed);
+                if (r > 0) ok = bar_wait(queries_free, (r + 1) & 1, failed);
                 if (!ok) break;
                 bar_expect(queries, 2 * kParts * a.hp * a.tp * 128);
                 for (int p = 0; p < kParts; ++p) {
                     tma_box3(base + Smem::kQ + p * (kTile * 128), &q_map, p * 64, it.block * a.hp, it.token0, queries);
                     tma_box3(base + Smem::kDo + p * (kTile * 128), &do_map, p * 64, it.block * a.hp, it.token0, queries);
                 }
-                for (int32_t j = 0; j < it.n && ok; ++j) {
-                    const int32_t key0 = it.key0(j);
-                    for (int which = 0; which < 2; ++which, ++pos) {
-                        const int stage = pos % kStages;
-                        if (pos >= kStages) ok = bar_wait(empty + 8 * stage, (pos / kStages + 1) & 1, failed);
-                        if (!ok) break;
-                        bar_expect(full + 8 * stage, Smem::kTileBytes);
-                        for (int p = 0; p < kParts; ++p)
-                            tma_box3(base + Smem::kRing + stage * Smem::kTileBytes + p * (kTile * 128), which ? &v_map : &k_map, p * 64, head, key0, full + 8 * stage);
-                    }
+                for (int32_t j = 0; j < it.n && ok; ++j, ++pos) {
+                    bring(0, kKeyStages, Smem::kKeys, &k_map, head, it.key0(j));
+                    if (ok) bring(kKeyStages, kValueStages, Smem::kValues, &v_map, head, it.key0(j));
                 }
             }
             if (*failed) {
                 int32_t never = 0;
-                if (turn > 0) bar_wait(queries, (turn - 1) & 1, &never);
-                for (int32_t x = max(0, pos - kStages); x < pos; ++x) bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, &never);
+                if (r > 0) bar_wait(queries, (r - 1) & 1, &never);
+                for (uint32_t x = pos < kKeyStages ? 0 : pos - kKeyStages; x < pos; ++x) bar_wait(full + 8 * (x % kKeyStages), x / kKeyStages & 1, &never);
+                for (uint32_t x = pos < kValueStages ? 0 : pos - kValueStages; x < pos; ++x) bar_wait(full + 8 * (kKeyStages + x % kValueStages), x / kValueStages & 1, &never);
             }
         }
     } else if (warp == kProductWarp) {
-        const uint32_t q_rows = operand(base + Smem::kQ, 16), do_rows = operand(base + Smem::kDo, 16);
-        uint32_t free_phase = 0, gradients_phase = 0;
-        int32_t pos = 0;
-        for (int32_t r = 0; ok; ++r) {
+        // ---- S.  As above, failed waits are not looked at by the warps with the products
+        const uint32_t lead = elect_one(), q_rows = operand(base + Smem::kQ, 16);
+        uint32_t pos = 0;
+        for (uint32_t r = 0;; ++r) {
             const QueryWork it = make_queries(a, feed_next<false>(sh.feed, r, failed));
             if (!it.valid) break;
-            auto at = [&](int32_t j, int which) { return base + Smem::kRing + (uint32_t)((pos + 2 * j + which) % kStages) * Smem::kTileBytes; };
-            auto arrived = [&](int32_t j, int which) {
-                const int32_t x = pos + 2 * j + which;
-                if (!bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, failed)) return false;
-                const int32_t count = it.count(j);
-                if (which == 0 && (count & 15) && it.seen(j) > (count & ~15)) {
-                    clear_rows<D>(at(j, 0), count);
-                    publish_clears();
-                }
+            bar_wait(queries, r & 1, failed);
+#pragma unroll 1
+            for (int32_t j = 0; j < it.n; ++j, ++pos) {
+                const uint32_t stage = pos % kKeyStages;
+                bar_wait(full + 8 * stage, pos / kKeyStages & 1, failed);
+                if (pos > 0) bar_wait(scores_free, (pos + 1) & 1, failed);
                 fence_after();
-                return true;
-            };
-            auto scores_of = [&](int32_t j) {
-                if (elect_one()) {
-                    product_of_rows<Q, D>(tmem, q_rows, operand(at(j, 0), 16), it.seen(j));
-                    mma_commit(scores);
-                }
-                __syncwarp();
-            };
-            auto products_of = [&](int32_t j) {
-                if (elect_one()) {
-                    product_of_rows<Q, D>(tmem + kTile, do_rows, operand(at(j, 1), 16), it.seen(j));
-                    mma_commit(products);
-                    mma_commit(empty + 8 * ((pos + 2 * j + 1) % kStages));
-                    if (j + 1 == it.n) mma_commit(queries_free);
-                }
-                __syncwarp();
-            };
-            ok = bar_wait(queries, r & 1, failed) && arrived(0, 0);
-            // the scores of the item before have been read: its last gradients came after that
-            if (!ok) break;
-            if (r > 0) {
-                ok = bar_wait(scores_free, free_phase, failed);
-                free_phase ^= 1;
-                if (!ok) break;
-                fence_after();
+                product_of_rows<Q, D>(lead, tmem, q_rows, operand(base + Smem::kKeys + stage * Smem::kTileBytes, 16), it.seen(j));
+                mma_commit(lead, scores);
+                mma_commit(lead, empty + 8 * stage);
             }
-            scores_of(0);
-            ok = arrived(0, 1);
-            if (!ok) break;
-            products_of(0);
-            for (int32_t j = 0; j < it.n; ++j) {
-                const bool more = j + 1 < it.n;
-                if (more) {
-                    ok = bar_wait(scores_free, free_phase, failed);
-                    free_phase ^= 1;
-                    if (!ok || !arrived(j + 1, 0)) { ok = false; break; }
-                    scores_of(j + 1);
-                }
-                ok = bar_wait(gradients, gradients_phase, failed);
-                gradients_phase ^= 1;
-                if (ok && j == 0 && r > 0) ok = bar_wait(sums_free, (r + 1) & 1, failed);
-                if (!ok) break;
+            mma_commit(lead, queries_free);
+        }
+    } else if (warp == kProductWarp + 1) {
+        // ---- dP, a step ahead, and dQ
+        const uint32_t lead = elect_one(), do_rows = operand(base + Smem::kDo, 16);
+        uint32_t phase = 0, pos = 0;
+        for (uint32_t r = 0;; ++r) {
+            const QueryWork it = make_queries(a, feed_next<false>(sh.feed, r, failed));
+            if (!it.valid) break;
+            auto products_of = [&](int32_t j, uint32_t b) {
+                const uint32_t stage = (pos + j) % kValueStages;
+                bar_wait(full + 8 * (kKeyStages + stage), (pos + j) / kValueStages & 1, failed);
                 fence_after();
-                if (elect_one()) {
-                    product_with_weights<Q, D>(tmem + 256, tmem + kTile, operand(at(j, 0), kTile * 128), it.seen(j), j == 0);
-                    mma_commit(empty + 8 * ((pos + 2 * j) % kStages));
-                    if (!more) mma_commit(sums);
+                product_of_rows<Q, D>(lead, tmem + kTile + b * kTile, do_rows, operand(base + Smem::kValues + stage * Smem::kTileBytes, 16), it.seen(j));
+                mma_commit(lead, products + 8 * b);
+                mma_commit(lead, empty + 8 * (kKeyStages + stage));
+                if (j + 1 == it.n) mma_commit(lead, queries_free);
+            };
+            bar_wait(queries, r & 1, failed);
+#pragma unroll 1
+            for (int32_t j = -2; j < it.n; ++j) {
+                const uint32_t b = j & 1;
+                if (j >= 0) {
+                    const uint32_t stage = (pos + j) % kKeyStages, at = base + Smem::kKeys + stage * Smem::kTileBytes;
+                    const int32_t count = it.count(j), seen = it.seen(j);
+                    bar_wait(full + 8 * stage, (pos + j) / kKeyStages & 1, failed);
+                    if ((count & 15) && seen > (count & ~15)) {
+                        clear_rows<D>(at, count);
+                        publish_clears();
+                    }
+                    bar_wait(gradients + 8 * b, phase >> b & 1, failed);
+                    phase ^= 1u << b;
+                    if (j == 0 && r > 0) bar_wait(sums_free, (r + 1) & 1, failed);
+                    fence_after();
+                    product_with_weights<Q, D>(lead, tmem + 3 * kTile, tmem + kTile + b * kTile, operand(at, kTile * 128), seen, j == 0);
+                    mma_commit(lead, empty + 8 * stage);
+                    if (j + 1 == it.n) mma_commit(lead, sums);
                 }
-                __syncwarp();
-                if (more) {
-                    ok = arrived(j + 1, 1);
-                    if (!ok) break;
-                    products_of(j + 1);
-                }
+                if (j + 2 < it.n) products_of(j + 2, b);
             }
-            pos += 2 * it.n;
+            pos += it.n;
         }
     } else if (warp < 8) {
         const int half = warp >> 2, row = threadIdx.x & (kTile - 1);
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
-        const uint32_t t_s = lanes + half * kHalfTile, t_dp = lanes + kTile + half * kHalfTile;
+        const uint32_t t_s = lanes + half * kHalfTile;
         const int32_t row_token = row / a.hp, row_head = row - row_token * a.hp;
         const float c = exp2f((float)(shift - up));
         const float2 scale2 = make_float2(a.scale_log2, a.scale_log2), c2 = make_float2(c, c);
@@ -697,7 +661,7 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
             if (w.valid && row_token < w.tokens && HORA_IN(w.token0 + row_token, a.T)) st = __ldcg(a.stats + (int64_t)(w.token0 + row_token) * a.Hq + w.block * a.hp + row_head);
             return st;
         };
-        uint32_t phase = 0;
+        uint32_t phase = 0, products_phase = 0;
         for (int32_t r = 0; ok; ++r) {
             const QueryWork it = make_queries(a, feed_next<false>(sh.feed, r, failed));
             if (!it.valid) break;
@@ -727,7 +691,9 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
                         p[b][e] = exp2_approx(y.x);
                         p[b][e + 1] = exp2_approx(y.y);
                     }
-                ok = bar_wait(products, phase, failed);
+                const uint32_t b2 = j & 1, t_dp = lanes + kTile + b2 * kTile + half * kHalfTile;
+                ok = bar_wait(products + 8 * b2, products_phase >> b2 & 1, failed);
+                products_phase ^= 1u << b2;
                 ok = __all_sync(kFull, ok);
                 if (!ok) break;
                 fence_after();
@@ -752,7 +718,7 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
                 }
                 tmem_store_wait();
                 fence_before();
-                bar_arrive(gradients);
+                bar_arrive(gradients + 8 * b2);
             }
             if (!ok) break;
             ok = bar_wait(sums, r & 1, failed);
@@ -760,7 +726,7 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
             if (!ok) break;
             fence_after();
             store_row<D / 2>(static_cast<Q *>(a.dq) + (int64_t)token * a.dq_stride + (int64_t)(it.block * a.hp + row_head) * D + half * (D / 2),
-                             lanes + 256 + half * (D / 2), a.scale * exp2f((float)-shift), have);
+                             lanes + 3 * kTile + half * (D / 2), a.scale * exp2f((float)-shift), have);
             fence_before();
             bar_arrive(sums_free);
         }
