@@ -10,7 +10,7 @@
 // which the same tiles of dO and Q are read the other way round.  Nothing but the four operands ever is in shared memory.
 //   Queries: an item is one tile of queries; S = Q K^T, dP = dO V^T, dQ += dS K.
 //   Eight warps do what is between the products, two threads to a row, 64 columns each; while they work on the weights of a step the tensor
-// cores compute its dP, and while they work on its dS the tensor cores have the next step's scores to do.  Two warps issue the products.
+// cores compute its dP, and while they work on its dS the tensor cores have the next step's scores to do.
 //   Rows of a tile that are not of the run of queries (or keys) are cleared in shared memory where a product sums over them.
 //   Every wait has a limit; a wait that reaches it makes the CTA give up and report HORA_ERR_INTERNAL.
 #define HORA_FILE_ID 12
@@ -25,8 +25,8 @@ namespace hora {
 namespace {
 
 constexpr int kTile = kPackedRows, kHalfTile = kTile / 2;
-constexpr int kMiddleThreads = 256, kLoadWarp = 8, kProductWarp = 9, kFeedWarp = 11;   // two warps issue products
-constexpr int kFeedReaders = 11;                         // warps that take items from the feeder
+constexpr int kMiddleThreads = 256, kLoadWarp = 8, kProductWarp = 9, kFeedWarp = 11;
+constexpr int kFeedReaders = 11;                         // warps that take items from the feeder (one less for keys)
 
 template <typename Q>
 constexpr uint32_t kType = std::is_same<Q, __nv_bfloat16>::value ? 1u : 0u;
@@ -171,18 +171,18 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
                    sums_free = smem_at(&sh.sums_free);
     if (threadIdx.x == 0) {
         sh.failed = 0;
-        feed_init(sh.feed, kFeedReaders);
+        feed_init(sh.feed, kFeedReaders - 1);
         for (uint32_t s = 0; s < kStages; ++s) {
             bar_init(full + 8 * s, 1 + kWarp);
-            bar_init(empty + 8 * s, 2);
+            bar_init(empty + 8 * s, 1);
         }
         bar_init(keys, 1);
-        bar_init(keys_free, 2);
+        bar_init(keys_free, 1);
         bar_init(scores, 1);
         bar_init(weights, kMiddleThreads);
         bar_init(products, 1);
         bar_init(gradients, kMiddleThreads);
-        bar_init(sums, 2);
+        bar_init(sums, 1);
         bar_init(sums_free, kMiddleThreads);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -264,54 +264,61 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
             if (r > 0) bar_wait(keys, (r - 1) & 1, &never);
             for (uint32_t x = pos < kStages ? 0 : pos - kStages; x < pos; ++x) bar_wait(full + 8 * (x % kStages), (x / kStages) & 1, &never);
         }
-    } else if (warp >= kProductWarp) {
-        // ---- products: one warp S^T and dV, the other dP^T and dK, each with its own part of tensor memory.  A wait that has failed is not looked
-        // at here: what follows is of no use, but in bounds, and there is no next item
-        const uint32_t which = warp - kProductWarp, lead = elect_one();
-        const uint32_t rows_a = operand(base + (which ? Smem::kV : Smem::kK), 16), between = tmem + which * kTile, sum = tmem + 256 + which * D;
-        const uint32_t there = which ? products : scores, back = which ? gradients : weights;
+    } else if (warp == kProductWarp) {
+        // ---- products, in the order dV, the next S^T, dK, the next dP^T: the weights of a step wait for its S^T alone, while dK and dP^T are under way.
+        // A wait that has failed is not looked at here: what follows is of no use, but in bounds, and there is no next item
+        const uint32_t lead = elect_one(), k_rows = operand(base + Smem::kK, 16), v_rows = operand(base + Smem::kV, 16);
         uint32_t phase = 0, pos = 0;
         for (uint32_t r = 0;; ++r) {
             const KeyWork it = make_keys(a, feed_next<false>(sh.feed, r, failed));
             if (!it.valid) break;
-            // the tiles of step s, rows of others cleared by both warps: either may be the first to need it
-            auto arrived = [&](int32_t s, uint32_t stage) {
-                bar_wait(full + 8 * stage, (pos + s) / kStages & 1, failed);
-                const KeyStep k = key_step(a, it, s);
-                if (!k.whole && (k.count & 15)) {
-                    const uint32_t at = base + Smem::kRing + stage * 2 * Smem::kTileBytes;
-                    clear_rows<D>(at, k.count);
-                    clear_rows<D>(at + Smem::kTileBytes, k.count);
-                    publish_clears();
-                }
-                fence_after();
-                // S^T from the queries, dP^T from the gradients of outputs
-                product_of_rows<Q, D>(lead, between, rows_a, operand(base + Smem::kRing + (stage * 2 + which) * Smem::kTileBytes, 16), k.count);
-                mma_commit(lead, there);
-                return k.count;
+            int32_t count = 0;
+            auto tile = [&](uint32_t x, int which, uint32_t lead_bytes) {
+                return operand(base + Smem::kRing + (x % kStages * 2 + which) * Smem::kTileBytes, lead_bytes);
             };
             bar_wait(keys, r & 1, failed);
-            int32_t count = arrived(0, pos % kStages);
 #pragma unroll 1
-            for (int32_t s = 0; s < it.steps; ++s) {
-                const uint32_t stage = (pos + s) % kStages;
-                bar_wait(back, phase, failed);
-                phase ^= 1;
-                if (s == 0 && r > 0) bar_wait(sums_free, (r + 1) & 1, failed);
-                fence_after();
-                // dV from the gradients of outputs, dK from the queries
-                product_with_weights<Q, D>(lead, sum, between, operand(base + Smem::kRing + (stage * 2 + 1 - which) * Smem::kTileBytes, kTile * 128), count, s == 0);
-                mma_commit(lead, empty + 8 * stage);
-                if (s + 1 < it.steps) {
-                    count = arrived(s + 1, (pos + s + 1) % kStages);
-                } else {
-                    mma_commit(lead, keys_free);
-                    mma_commit(lead, sums);
+            for (int32_t s = -1; s < it.steps; ++s, ++pos) {                 // pos: the place of step s + 1
+                if (s >= 0) {
+                    bar_wait(weights, phase, failed);
+                    if (s == 0 && r > 0) bar_wait(sums_free, (r + 1) & 1, failed);
+                    fence_after();
+                    product_with_weights<Q, D>(lead, tmem + 256, tmem, tile(pos - 1, 1, kTile * 128), count, s == 0);
                 }
+                int32_t next_count = 0;
+                const bool more = s + 1 < it.steps;
+                if (more) {
+                    bar_wait(full + 8 * (pos % kStages), pos / kStages & 1, failed);
+                    const KeyStep k = key_step(a, it, s + 1);
+                    next_count = k.count;
+                    if (!k.whole && (k.count & 15)) {    // rows of others
+                        const uint32_t at = base + Smem::kRing + pos % kStages * 2 * Smem::kTileBytes;
+                        clear_rows<D>(at, k.count);
+                        clear_rows<D>(at + Smem::kTileBytes, k.count);
+                        publish_clears();
+                    }
+                    fence_after();
+                    product_of_rows<Q, D>(lead, tmem, k_rows, tile(pos, 0, 16), next_count);
+                    mma_commit(lead, scores);
+                }
+                if (s >= 0) {
+                    bar_wait(gradients, phase, failed);
+                    phase ^= 1;
+                    fence_after();
+                    product_with_weights<Q, D>(lead, tmem + 256 + D, tmem + kTile, tile(pos - 1, 0, kTile * 128), count, s == 0);
+                    mma_commit(lead, empty + 8 * ((pos - 1) % kStages));
+                }
+                if (more) {
+                    product_of_rows<Q, D>(lead, tmem + kTile, v_rows, tile(pos, 1, 16), next_count);
+                    mma_commit(lead, products);
+                }
+                count = next_count;
             }
-            pos += it.steps;
+            --pos;
+            mma_commit(lead, keys_free);
+            mma_commit(lead, sums);
         }
-    } else {
+    } else if (warp < 8) {
         // ---- between the products: thread `row` of either half has 64 columns (queries) of a key
         const int half = warp >> 2, row = threadIdx.x & (kTile - 1);
         const uint32_t lanes = tmem + ((uint32_t)(warp & 3) << 21);
