@@ -231,20 +231,29 @@ packed_stats_kernel(const PackedArgs a) {
     const int64_t rows = (int64_t)tokens * a.Hq, v_rows = a.half ? (int64_t)tokens * a.Hkv : 0;
     float most_d = 0.f, most_v = 0.f;
     const int64_t stride = (int64_t)gridDim.x * kGroups;
-    for (int64_t x0 = (int64_t)blockIdx.x * kGroups + group; __any_sync(kFull, x0 < rows); x0 += stride * kRows) {
+    // a row's token and head, taken along without divisions
+    const int64_t start = (int64_t)blockIdx.x * kGroups + group;
+    int64_t token = first + start / a.Hq;
+    int32_t head = (int32_t)(start % a.Hq);
+    const int32_t step_tokens = (int32_t)(stride / a.Hq), step_heads = (int32_t)(stride % a.Hq);
+    for (int64_t x0 = start; __any_sync(kFull, x0 < rows); x0 += stride * kRows) {
         Raw8<T> o[kRows], d[kRows];
         int64_t at[kRows];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const int64_t x = x0 + i * stride;
             zero8(o[i]);
             zero8(d[i]);
             at[i] = -1;
-            if (x < rows) {
-                const int64_t token = first + x / a.Hq, h = x % a.Hq;
-                at[i] = token * a.Hq + h;
-                load8(o[i], static_cast<const T *>(a.out_in) + token * a.out_stride + h * D + lane * 8);
-                load8(d[i], static_cast<const T *>(a.dout) + token * a.dout_stride + h * D + lane * 8);
+            if (x0 + i * stride < rows) {
+                at[i] = token * a.Hq + head;
+                load8(o[i], static_cast<const T *>(a.out_in) + token * a.out_stride + head * D + lane * 8);
+                load8(d[i], static_cast<const T *>(a.dout) + token * a.dout_stride + head * D + lane * 8);
+            }
+            token += step_tokens;
+            head += step_heads;
+            if (head >= a.Hq) {
+                head -= a.Hq;
+                ++token;
             }
         }
 #pragma unroll

@@ -84,36 +84,52 @@ struct Turn {
     }
 };
 
-// One group's part: a token and `heads` of its heads.
+// One group's part: a token and `heads` of its heads.  The next heads' loads are on their way while these are worked on, the first ones' while
+// the angles are.
 template <typename T, int D, bool PAIRS, bool BACKWARD>
 __device__ __forceinline__ void rotate_unit(const RotateArgs &a, int64_t unit, bool have, const float (&w)[2][8], float (&dw)[2][8]) {
-    constexpr int kLanes = D / 8;
+    constexpr int kLanes = D / 8, kAhead = BACKWARD ? kRotateHeads / 2 : kRotateHeads;
     const int lane_in_warp = lane_id(), lane = lane_in_warp % kLanes;
     const int64_t token = have ? (a.chunks == 1 ? unit : unit / a.chunks) : 0;
     const int32_t h0 = have && a.chunks > 1 ? (int32_t)(unit - token * a.chunks) * a.heads : 0;
-    const Turn<D, PAIRS> turn(a, token, have, lane, BACKWARD ? -1.f : 1.f);
-    for (int32_t b = 0; b < a.heads; b += kRotateHeads) {
-        Raw8<T> x[kRotateHeads], dy[kRotateHeads];
+    const T *const x_q = static_cast<const T *>(a.x[0]) + token * a.x_stride[0], *const x_k = static_cast<const T *>(a.x[1]) + token * a.x_stride[1];
+    const T *const dy_q = static_cast<const T *>(a.dy[0]) + token * a.dy_stride[0], *const dy_k = static_cast<const T *>(a.dy[1]) + token * a.dy_stride[1];
+    T *const y_q = static_cast<T *>(a.y[0]) + token * a.y_stride[0], *const y_k = static_cast<T *>(a.y[1]) + token * a.y_stride[1];
+    const bool norms[2] = {a.w[0] != nullptr, a.w[1] != nullptr};
+    Raw8<T> x[kAhead], dy[kAhead];
+    auto load = [&](int32_t b) {
 #pragma unroll
-        for (int i = 0; i < kRotateHeads; ++i) {
+        for (int i = 0; i < kAhead; ++i) {
             const int32_t h = h0 + b + i;
             const bool is_k = h >= a.Hq, mine = have && b + i < a.heads && h < a.H;
-            const int64_t at = (int64_t)(is_k ? h - a.Hq : h) * D + lane * 8;
-            zero8(x[i]);
-            if (mine && (!BACKWARD || (is_k ? a.w[1] : a.w[0]) != nullptr)) load8(x[i], static_cast<const T *>((is_k ? a.x[1] : a.x[0])) + token * (is_k ? a.x_stride[1] : a.x_stride[0]) + at);
+            const int32_t at = (is_k ? h - a.Hq : h) * D + lane * 8;
+            if (mine && (!BACKWARD || (is_k ? norms[1] : norms[0]))) load8(x[i], (is_k ? x_k : x_q) + at);
+            else zero8(x[i]);
             if constexpr (BACKWARD) {
-                zero8(dy[i]);
-                if (mine) load8(dy[i], static_cast<const T *>((is_k ? a.dy[1] : a.dy[0])) + token * (is_k ? a.dy_stride[1] : a.dy_stride[0]) + at);
+                if (mine) load8(dy[i], (is_k ? dy_k : dy_q) + at);
+                else zero8(dy[i]);
             }
         }
+    };
+    load(0);
+    const Turn<D, PAIRS> turn(a, token, have, lane, BACKWARD ? -1.f : 1.f);
+#pragma unroll 1
+    for (int32_t b = 0; b < a.heads; b += kAhead) {
+        Raw8<T> x_now[kAhead], dy_now[kAhead];
 #pragma unroll
-        for (int i = 0; i < kRotateHeads; ++i) {
+        for (int i = 0; i < kAhead; ++i) {
+            x_now[i] = x[i];
+            if (BACKWARD) dy_now[i] = dy[i];
+        }
+        load(b + kAhead);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
             const int32_t h = h0 + b + i;
             const bool is_k = h >= a.Hq, mine = have && b + i < a.heads && h < a.H;
             if (!__any_sync(kFull, mine)) break;
-            const bool norm = mine && (is_k ? a.w[1] : a.w[0]) != nullptr;
+            const bool norm = mine && (is_k ? norms[1] : norms[0]);
             float z[8];
-            widen8(x[i], z);
+            widen8(x_now[i], z);
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum += z[e] * z[e];
@@ -126,7 +142,7 @@ __device__ __forceinline__ void rotate_unit(const RotateArgs &a, int64_t unit, b
                 turn.apply(z, lane_in_warp);
             } else {
                 float g[8], dot = 0.f;
-                widen8(dy[i], g);
+                widen8(dy_now[i], g);
                 turn.apply(g, lane_in_warp);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -146,7 +162,7 @@ __device__ __forceinline__ void rotate_unit(const RotateArgs &a, int64_t unit, b
             if (mine) {
                 Raw8<T> y;
                 narrow8(z, y);
-                store8(y, static_cast<T *>((is_k ? a.y[1] : a.y[0])) + token * (is_k ? a.y_stride[1] : a.y_stride[0]) + (int64_t)(is_k ? h - a.Hq : h) * D + lane * 8);
+                store8(y, (is_k ? y_k : y_q) + (is_k ? h - a.Hq : h) * D + lane * 8);
             }
         }
     }
