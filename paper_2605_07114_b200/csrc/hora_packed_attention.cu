@@ -72,7 +72,7 @@ __device__ __forceinline__ int32_t items_of(const PackedArgs &a, const PackedSeq
 }
 // Parts that an item of keys is cut into: none is longer than what a CTA has to do on average, or than kPartSteps where that is more.
 // Parts of items that are cut, times heads, are then 2 n_sm at most: each item has less than n / most + 1 <= 2 n / most of them.
-constexpr int kPartSteps = 8;
+constexpr int kPartSteps = 4;
 __device__ __forceinline__ int32_t parts_of(int32_t steps, int32_t most) { return steps > most ? (steps + most - 1) / most : 1; }
 
 __device__ __forceinline__ int32_t bucket_of(int32_t steps) {
@@ -213,10 +213,11 @@ packed_plan_kernel(const PackedArgs a) {
         }
         if (threadIdx.x == 0 && (__ldcg(a.group_offsets) != 0 || __ldcg(a.group_offsets + a.N) + a.N != a.S)) bad = true;
     }
-    if (threadIdx.x < 4) a.counts[2 + threadIdx.x] = 0;
+    if (blockIdx.x == 0 && threadIdx.x < 4) a.counts[2 + threadIdx.x] = 0;
     __syncthreads();
-    list_items<false>(a, s_groups, s_bucket, s_warp, bad);
-    if (a.key_items != nullptr) list_items<true>(a, s_groups, s_bucket, s_warp, bad);
+    // a CTA to each list
+    if (blockIdx.x == 0) list_items<false>(a, s_groups, s_bucket, s_warp, bad);
+    else list_items<true>(a, s_groups, s_bucket, s_warp, bad);
     if (bad) raise_status(a.status, HORA_ERR_INVALID_VALUE);
 }
 
@@ -345,7 +346,7 @@ static bool packed_rows(const void *p, int64_t stride, int32_t H, int32_t D) {
 }
 
 static hora_status_t launch_packed_plan(const PackedArgs &a, cudaStream_t stream) {
-    const cudaError_t e = launch_pdl(packed_plan_kernel, 1, kListThreads, 0, stream, a);
+    const cudaError_t e = launch_pdl(packed_plan_kernel, a.key_items != nullptr ? 2 : 1, kListThreads, 0, stream, a);
     count_launches(1);
     return cuda_ok(e);
 }

@@ -678,9 +678,29 @@ class QkRotation:
         self.inv_freq, self.D, self.q_weight, self.k_weight, self.eps, self.layout = inv_freq, D, q_weight, k_weight, eps, layout
         self.workspace = torch.empty(max(hora_qk_rotate_backward_workspace_bytes(D), 256), dtype=torch.uint8, device=first.device)
         self._streams = set()
+        _, freq, rot, wq, wk = _rotation(torch.empty(0, dtype=torch.int32, device=first.device), inv_freq, q_weight, k_weight, 0, D)
+        _one_device(first, inv_freq, q_weight, k_weight)
+        self._middle, self._device = (freq, rot, layout, wq, wk, float(eps)), first.get_device()
+
+    def _usual(self, q, k, positions, q_out, k_out):
+        """The usual call, marshalled in few steps: both sides, heads next to each other, everything on the object's device, which is the
+        current one.  False: it is not that."""
+        D, dev, qs, ks, os, ps = self.D, self._device, q.stride(), k.stride(), q_out.stride(), k_out.stride()
+        n, dtype = q.shape[0], q.dtype
+        if not (n > 1 and len(qs) == len(ks) == 3 and qs[1:] == ks[1:] == os[1:] == ps[1:] == (D, 1) and q.shape == q_out.shape and k.shape == k_out.shape
+                and k.shape[0] == n and q.shape[2] == k.shape[2] == D and dtype == k.dtype == q_out.dtype == k_out.dtype and dtype in _DTYPES
+                and positions.dtype == torch.int32 and positions.shape == (n,) and positions.is_contiguous()
+                and q.get_device() == k.get_device() == q_out.get_device() == k_out.get_device() == positions.get_device() == dev == torch.cuda.current_device()):
+            return False
+        freq, rot, layout, wq, wk, eps = self._middle
+        _check(load().hora_qk_rotate(q.data_ptr(), k.data_ptr(), _DTYPES[dtype], qs[0], ks[0], n, q.shape[1], k.shape[1], D, positions.data_ptr(), freq, rot, layout,
+                                     wq, wk, eps, q_out.data_ptr(), k_out.data_ptr(), os[0], ps[0], torch._C._cuda_getCurrentRawStream(dev)), "hora_qk_rotate")
+        return True
 
     def run(self, q, k, positions, q_out=None, k_out=None):
         """q [n, Hq, D], k [n, Hk, D]; returns (q_out, k_out), packed unless others are given."""
+        if q is not None and k is not None and q_out is not None and k_out is not None and positions is not None and self._usual(q, k, positions, q_out, k_out):
+            return q_out, k_out
         if q is not None and q_out is None:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         if k is not None and k_out is None:
@@ -761,6 +781,10 @@ class PackedAttention:
 
     def __init__(self, seq_offsets, T: int, Hq: int, Hkv: int, D: int, dtype, *, group_offsets=None, causal: bool = True, sm_scale: Optional[float] = None,
                  status_dev=None, backward: bool = False):
+        if seq_offsets.dim() != 1 or seq_offsets.numel() < 1 or (group_offsets is not None and (group_offsets.dim() != 1 or group_offsets.numel() < 1)):
+            raise ValueError("seq_offsets and group_offsets must have one dimension and a first entry")
+        if dtype not in (torch.bfloat16, torch.float16):
+            raise ValueError(f"unsupported dtype {dtype}")
         dev, S = seq_offsets.device, seq_offsets.numel() - 1
         need = hora_packed_attention_workspace_bytes(T, S, Hq, Hkv, D, backward)
         if need == 0:
@@ -772,11 +796,36 @@ class PackedAttention:
         self.out, self.lse = new(Hq), torch.empty((T, Hq), dtype=torch.float32, device=dev)
         self.dq, self.dk, self.dv = (new(Hq), new(Hkv), new(Hkv)) if backward else (None, None, None)
         self._streams = set()
+        # what does not change from call to call, marshalled once
+        _one_device(seq_offsets, group_offsets, status_dev, self.workspace)
+        N = 0 if group_offsets is None else group_offsets.numel() - 1
+        self._shape, self._dtype, self._device, self._code = (T, Hq, Hkv, D), dtype, seq_offsets.get_device(), _DTYPES[dtype]
+        self._middle = (T, _at(seq_offsets, torch.int64, "seq_offsets"), S, _at(group_offsets, torch.int64, "group_offsets"), N, Hq, Hkv, D, float(self.sm_scale), int(causal))
+        self._lse = self.lse.data_ptr()
+        self._tail = (_at(status_dev, torch.int32, "status_dev"), self.workspace.data_ptr(), self.workspace.numel())
+
+    def _strides(self, dtype, of_queries, of_keys):
+        """Token strides of tensors [T, Hq, D] and [T, Hkv, D] in the usual places, in few steps; None: something is not usual."""
+        (T, Hq, Hkv, D), dev, got = self._shape, self._device, []
+        if dtype != self._dtype or dev != torch.cuda.current_device() or T < 2:
+            return None
+        for shape, ts in (((T, Hq, D), of_queries), ((T, Hkv, D), of_keys)):
+            for t in ts:
+                st = t.stride()
+                if t.shape != shape or st[1:] != (D, 1) or t.dtype != dtype or t.get_device() != dev:
+                    return None
+                got.append(st[0])
+        return got
 
     def run(self, q, k, v, out=None, lse=None):
         """Returns (out, lse)."""
         out, lse = self.out if out is None else out, self.lse if lse is None else lse
-        hora_packed_attention(q, k, v, self.seq_offsets, self.group_offsets, self.sm_scale, self.causal, out, lse, self.workspace, self.status_dev)
+        st = self._strides(q.dtype, (q, out), (k, v)) if lse is self.lse else None
+        if st is not None and st[2] == st[3]:
+            _check(load().hora_packed_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), self._code, st[0], st[2], *self._middle, out.data_ptr(), st[1], self._lse,
+                                                *self._tail, torch._C._cuda_getCurrentRawStream(self._device)), "hora_packed_attention")
+        else:
+            hora_packed_attention(q, k, v, self.seq_offsets, self.group_offsets, self.sm_scale, self.causal, out, lse, self.workspace, self.status_dev)
         _used_on(self, q, self.workspace, self.out, self.lse, self.dq, self.dk, self.dv)
         return out, lse
 
@@ -785,8 +834,14 @@ class PackedAttention:
         if self.dq is None:
             raise ValueError("made without backward=True")
         dq, dk, dv = self.dq if dq is None else dq, self.dk if dk is None else dk, self.dv if dv is None else dv
-        hora_packed_attention_backward(q, k, v, out, lse, dout, self.seq_offsets, self.group_offsets, self.sm_scale, self.causal, dq, dk, dv, self.workspace,
-                                       self.status_dev)
+        st = self._strides(q.dtype, (q, out, dout, dq), (k, v, dk, dv)) if lse is self.lse else None
+        if st is not None and st[4] == st[5] and st[6] == st[7]:
+            _check(load().hora_packed_attention_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), self._lse, dout.data_ptr(), self._code, st[0], st[4], st[1],
+                                                         st[2], *self._middle, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), st[3], st[6], *self._tail,
+                                                         torch._C._cuda_getCurrentRawStream(self._device)), "hora_packed_attention_backward")
+        else:
+            hora_packed_attention_backward(q, k, v, out, lse, dout, self.seq_offsets, self.group_offsets, self.sm_scale, self.causal, dq, dk, dv, self.workspace,
+                                           self.status_dev)
         _used_on(self, q, self.workspace, self.out, self.lse, self.dq, self.dk, self.dv)
         return dq, dk, dv
 
