@@ -564,7 +564,7 @@ hora_status_t hora_qk_rotate_backward(const void *dq_out, const void *dk_out, in
  * Scores, maxima, sums and outputs are held in fp32; the weights are rounded to the 16-bit type of the product they enter.
  *
  *   q            token t at q + t * q_row_stride (elements), heads next to each other: [Hq, D], BF16 or F16; query head h reads head h / (Hq/Hkv)
- *                of k, v, token t at k + t * kv_row_stride: [Hkv, D], of the same type.  D = 64 or 128.  All 16-byte aligned, row strides at least
+ *                of k, v, token t at k + t * k_row_stride, v + t * v_row_stride: [Hkv, D], of the same type.  D = 64 or 128.  All 16-byte aligned, row strides at least
  *                the heads' width and multiples of 8 (slices of a fused projection will do).  T tokens in all.
  *                Rows of a sequence have to be finite; a score beyond fp32's range makes its row NaN.
  *   seq_offsets  [S+1] int64, non-decreasing, in [0, T] (sequences may be empty).  Tokens before the first or behind the last sequence take no
@@ -582,21 +582,21 @@ hora_status_t hora_qk_rotate_backward(const void *dq_out, const void *dk_out, in
  * rounded to the 16-bit type of the products they enter.  In F16 both are held relative to powers of two, dS to one that follows from the largest
  * rows of dout and v: a dS less than 2^-39 of 2 max|dout row| max|v row| is lost.
  *   out, lse, dout   rows like q, out_row_stride, dout_row_stride;  lse not NULL here
- *   dq, dk, dv       out: rows like q, k, v, dq_row_stride, dkv_row_stride; must not overlap any input
+ *   dq, dk, dv       out: rows like q, k, v, dq_row_stride, dk_row_stride, dv_row_stride; must not overlap any input
  *   workspace        hora_packed_attention_workspace_bytes(T, S, Hq, Hkv, D, 1) bytes
  */
 size_t hora_packed_attention_workspace_bytes(int64_t T, int64_t S, int32_t Hq, int32_t Hkv, int32_t D, int32_t backward);
 
-hora_status_t hora_packed_attention(const void *q, const void *k, const void *v, int32_t dtype, int64_t q_row_stride, int64_t kv_row_stride,
+hora_status_t hora_packed_attention(const void *q, const void *k, const void *v, int32_t dtype, int64_t q_row_stride, int64_t k_row_stride, int64_t v_row_stride,
                                     int64_t T, const int64_t *seq_offsets, int64_t S, const int64_t *group_offsets, int64_t N, int32_t Hq,
                                     int32_t Hkv, int32_t D, float sm_scale, int32_t causal, void *out, int64_t out_row_stride, float *lse,
                                     int32_t *status_dev, void *workspace, size_t workspace_bytes, void *stream);
 
 hora_status_t hora_packed_attention_backward(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *dout,
-                                             int32_t dtype, int64_t q_row_stride, int64_t kv_row_stride, int64_t out_row_stride,
+                                             int32_t dtype, int64_t q_row_stride, int64_t k_row_stride, int64_t v_row_stride, int64_t out_row_stride,
                                              int64_t dout_row_stride, int64_t T, const int64_t *seq_offsets, int64_t S,
                                              const int64_t *group_offsets, int64_t N, int32_t Hq, int32_t Hkv, int32_t D, float sm_scale,
-                                             int32_t causal, void *dq, void *dk, void *dv, int64_t dq_row_stride, int64_t dkv_row_stride,
+                                             int32_t causal, void *dq, void *dk, void *dv, int64_t dq_row_stride, int64_t dk_row_stride, int64_t dv_row_stride,
                                              int32_t *status_dev, void *workspace, size_t workspace_bytes, void *stream);
 
 /*

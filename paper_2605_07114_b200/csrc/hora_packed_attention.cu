@@ -280,7 +280,7 @@ packed_stats_kernel(const PackedArgs a) {
     for (int64_t x = (int64_t)blockIdx.x * kGroups + group; __any_sync(kFull, x < v_rows); x += stride) {
         Raw8<T> v;
         zero8(v);
-        if (x < v_rows) load8(v, static_cast<const T *>(a.v) + (first + x / a.Hkv) * a.kv_stride + x % a.Hkv * D + lane * 8);
+        if (x < v_rows) load8(v, static_cast<const T *>(a.v) + (first + x / a.Hkv) * a.v_stride + x % a.Hkv * D + lane * 8);
         float z[8], size = 0.f;
         widen8(v, z);
 #pragma unroll
@@ -360,23 +360,23 @@ static hora_status_t launch_packed_stats(const PackedArgs &a, cudaStream_t strea
 }
 
 // What both calls check and fill in alike.
-static hora_status_t packed_begin(PackedArgs &a, const void *q, const void *k, const void *v, int32_t dtype, int64_t q_row_stride, int64_t kv_row_stride,
+static hora_status_t packed_begin(PackedArgs &a, const void *q, const void *k, const void *v, int32_t dtype, int64_t q_row_stride, int64_t k_row_stride, int64_t v_row_stride,
                                   int64_t T, const int64_t *seq_offsets, int64_t S, const int64_t *group_offsets, int64_t N, int32_t Hq, int32_t Hkv,
-                                  int32_t D, float sm_scale, int32_t causal, bool backward) {
+                                  int32_t D, float sm_scale, int32_t causal) {
     if (!packed_sizes(a, T, S, N, Hq, Hkv, D) || (dtype != HORA_DTYPE_BF16 && dtype != HORA_DTYPE_F16)) return HORA_ERR_INVALID_ARG;
     if (!(sm_scale > 0.f) || sm_scale > 1e30f || (causal != 0 && causal != 1)) return HORA_ERR_INVALID_ARG;
     if ((group_offsets == nullptr) != (N == 0)) return HORA_ERR_INVALID_ARG;
     if (T == 0 || S == 0) return HORA_OK;
-    if (seq_offsets == nullptr || !packed_rows(q, q_row_stride, Hq, D) || !packed_rows(k, kv_row_stride, Hkv, D) || !packed_rows(v, kv_row_stride, Hkv, D)) return HORA_ERR_INVALID_ARG;
+    if (seq_offsets == nullptr || !packed_rows(q, q_row_stride, Hq, D) || !packed_rows(k, k_row_stride, Hkv, D) || !packed_rows(v, v_row_stride, Hkv, D)) return HORA_ERR_INVALID_ARG;
     a.seq_offsets = seq_offsets;
     a.group_offsets = group_offsets;
     a.v = v;
-    a.kv_stride = kv_row_stride;
+    a.k_stride = k_row_stride;
+    a.v_stride = v_row_stride;
     a.causal = causal;
     a.half = dtype == HORA_DTYPE_F16;
     a.scale = sm_scale;
     a.scale_log2 = sm_scale * kLog2e;
-    (void)backward;
     return HORA_OK;
 }
 
@@ -393,13 +393,13 @@ extern "C" size_t hora_packed_attention_workspace_bytes(int64_t T, int64_t S, in
     return packed_sizes(a, T, S, 0, Hq, Hkv, D) ? lay_out(a, backward != 0, nullptr) : 0;
 }
 
-extern "C" hora_status_t hora_packed_attention(const void *q, const void *k, const void *v, int32_t dtype, int64_t q_row_stride, int64_t kv_row_stride,
+extern "C" hora_status_t hora_packed_attention(const void *q, const void *k, const void *v, int32_t dtype, int64_t q_row_stride, int64_t k_row_stride, int64_t v_row_stride,
                                                int64_t T, const int64_t *seq_offsets, int64_t S, const int64_t *group_offsets, int64_t N, int32_t Hq,
                                                int32_t Hkv, int32_t D, float sm_scale, int32_t causal, void *out, int64_t out_row_stride, float *lse,
                                                int32_t *status_dev, void *workspace, size_t workspace_bytes, void *stream) {
     using namespace hora;
     PackedArgs a = {};
-    hora_status_t rc = packed_begin(a, q, k, v, dtype, q_row_stride, kv_row_stride, T, seq_offsets, S, group_offsets, N, Hq, Hkv, D, sm_scale, causal, false);
+    hora_status_t rc = packed_begin(a, q, k, v, dtype, q_row_stride, k_row_stride, v_row_stride, T, seq_offsets, S, group_offsets, N, Hq, Hkv, D, sm_scale, causal);
     if (rc != HORA_OK || T == 0 || S == 0) return rc;
     if (!packed_rows(out, out_row_stride, Hq, D)) return HORA_ERR_INVALID_ARG;
     rc = packed_workspace(a, false, workspace, workspace_bytes);
@@ -414,17 +414,17 @@ extern "C" hora_status_t hora_packed_attention(const void *q, const void *k, con
 }
 
 extern "C" hora_status_t hora_packed_attention_backward(const void *q, const void *k, const void *v, const void *out, const float *lse, const void *dout,
-                                                        int32_t dtype, int64_t q_row_stride, int64_t kv_row_stride, int64_t out_row_stride,
+                                                        int32_t dtype, int64_t q_row_stride, int64_t k_row_stride, int64_t v_row_stride, int64_t out_row_stride,
                                                         int64_t dout_row_stride, int64_t T, const int64_t *seq_offsets, int64_t S,
                                                         const int64_t *group_offsets, int64_t N, int32_t Hq, int32_t Hkv, int32_t D, float sm_scale,
-                                                        int32_t causal, void *dq, void *dk, void *dv, int64_t dq_row_stride, int64_t dkv_row_stride,
+                                                        int32_t causal, void *dq, void *dk, void *dv, int64_t dq_row_stride, int64_t dk_row_stride, int64_t dv_row_stride,
                                                         int32_t *status_dev, void *workspace, size_t workspace_bytes, void *stream) {
     using namespace hora;
     PackedArgs a = {};
-    hora_status_t rc = packed_begin(a, q, k, v, dtype, q_row_stride, kv_row_stride, T, seq_offsets, S, group_offsets, N, Hq, Hkv, D, sm_scale, causal, true);
+    hora_status_t rc = packed_begin(a, q, k, v, dtype, q_row_stride, k_row_stride, v_row_stride, T, seq_offsets, S, group_offsets, N, Hq, Hkv, D, sm_scale, causal);
     if (rc != HORA_OK || T == 0 || S == 0) return rc;
     if (lse == nullptr || !packed_rows(out, out_row_stride, Hq, D) || !packed_rows(dout, dout_row_stride, Hq, D) || !packed_rows(dq, dq_row_stride, Hq, D) ||
-        !packed_rows(dk, dkv_row_stride, Hkv, D) || !packed_rows(dv, dkv_row_stride, Hkv, D))
+        !packed_rows(dk, dk_row_stride, Hkv, D) || !packed_rows(dv, dv_row_stride, Hkv, D))
         return HORA_ERR_INVALID_ARG;
     rc = packed_workspace(a, true, workspace, workspace_bytes);
     if (rc != HORA_OK) return rc;
@@ -437,7 +437,8 @@ extern "C" hora_status_t hora_packed_attention_backward(const void *q, const voi
     a.dk = dk;
     a.dv = dv;
     a.dq_stride = dq_row_stride;
-    a.dkv_stride = dkv_row_stride;
+    a.dk_stride = dk_row_stride;
+    a.dv_stride = dv_row_stride;
     a.status = status_dev;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     rc = launch_packed_plan(a, s);

@@ -36,7 +36,7 @@ struct PackedArgs {
     void *out, *dq, *dk, *dv;
     float *lse;
     int32_t *status;
-    int64_t out_stride, dout_stride, kv_stride, dq_stride, dkv_stride;
+    int64_t out_stride, dout_stride, k_stride, v_stride, dq_stride, dk_stride, dv_stride;
     int32_t S, N, T, Hq, Hkv, D, g, hp, tp, blocks;       // blocks: of hp heads, of all query heads
     int32_t causal, half;                                // half: fp16 (weights and gradients of scores are held relative to a scale, see below)
     float scale, scale_log2;
@@ -70,13 +70,13 @@ __device__ __forceinline__ void feed_init(Feed &f, int readers) {
 }
 // One lane.  VECTORS: of 16 bytes an item.
 template <int VECTORS>
-__device__ __forceinline__ void feed(Feed &f, const int4 *items, int32_t n_items, int32_t parts, int32_t *taken, volatile int32_t *failed) {
+__device__ __forceinline__ void feed(Feed &f, const int4 *items, int32_t n_items, int32_t cap, int32_t parts, int32_t *taken, volatile int32_t *failed) {
     const int64_t all = (int64_t)n_items * parts;
     for (uint32_t r = 0;; ++r) {
         // the counter cannot pass 2^31: every CTA takes at most one more than there are
         const int64_t x = r == 0 ? blockIdx.x : (int64_t)gridDim.x + (uint32_t)atomicAdd(taken, 1);
         FeedSlot s = {};
-        s.valid = x < all;
+        s.valid = x < all && HORA_IN(x / parts, cap);
         if (s.valid) {
             const int64_t i = x / parts;
             s.part = (int32_t)(x - i * parts);

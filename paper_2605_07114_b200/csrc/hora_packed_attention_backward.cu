@@ -207,7 +207,7 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
     bool ok = true;
 
     if (warp == kFeedWarp) {
-        if (lane == 0) feed<2>(sh.feed, reinterpret_cast<const int4 *>(a.key_items), __ldcg(a.counts + 1), a.Hkv, a.counts + 5, failed);
+        if (lane == 0) feed<2>(sh.feed, reinterpret_cast<const int4 *>(a.key_items), __ldcg(a.counts + 1), a.key_cap, a.Hkv, a.counts + 5, failed);
     } else if (warp == kLoadWarp) {
         // ---- keys, values, tiles of queries and of gradients of outputs; and of each row of a step -lse and -dout.out
         const float c = exp2f((float)(shift - up));
@@ -401,10 +401,10 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
             ok = __all_sync(kFull, ok);
             if (!ok) break;
             fence_after();
-            Q *to = static_cast<Q *>(half ? a.dk : a.dv) + (int64_t)(it.key0 + row) * a.dkv_stride + (int64_t)it.head * D;
+            Q *to = static_cast<Q *>(half ? a.dk : a.dv) + (int64_t)(it.key0 + row) * (half ? a.dk_stride : a.dv_stride) + (int64_t)it.head * D;
             const float factor = half ? a.scale * exp2f((float)-shift) : exp2f((float)-up);
             if (it.parts == 1) {
-                store_row<D>(to, lanes + 256 + half * D, factor, row < it.keys);
+                store_row<D>(to, lanes + 256 + half * D, factor, row < it.keys && HORA_IN(it.key0 + row, a.T));
                 fence_before();
                 bar_arrive(sums_free);
             } else {
@@ -446,7 +446,7 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
                                 sum[v].w += y[v].w;
                             }
                         }
-                        if (row < it.keys) {
+                        if (row < it.keys && HORA_IN(it.key0 + row, a.T)) {
 #pragma unroll
                             for (int v = 0; v < 4; v += 2) {
                                 const float x[8] = {sum[v].x * factor, sum[v].y * factor, sum[v].z * factor, sum[v].w * factor,
@@ -562,7 +562,7 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
     bool ok = true;
 
     if (warp == kFeedWarp) {
-        if (lane == 0) feed<2>(sh.feed, reinterpret_cast<const int4 *>(a.query_items), __ldcg(a.counts), a.blocks, a.counts + 4, failed);
+        if (lane == 0) feed<2>(sh.feed, reinterpret_cast<const int4 *>(a.query_items), __ldcg(a.counts), a.query_cap, a.blocks, a.counts + 4, failed);
     } else if (warp == kLoadWarp) {
         if (lane == 0) {
             uint32_t pos = 0, r = 0;                     // steps so far
@@ -674,7 +674,7 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
             if (!it.valid) break;
             const float2 st = stats_of(it);
             const float2 lse2 = make_float2((float)up - st.x, (float)up - st.x), delta2 = make_float2(-st.y * c, -st.y * c);
-            const bool have = row_token < it.tokens;
+            const bool have = row_token < it.tokens && HORA_IN(it.token0 + row_token, a.T);
             const int32_t token = it.token0 + row_token;
             const int32_t seen_to = a.causal && have ? min(it.end, token + 1) : it.end;
             for (int32_t j = 0; j < it.n; ++j, phase ^= 1) {
@@ -751,7 +751,7 @@ template <typename Q, int D>
 hora_status_t launch_backward(const PackedArgs &a, const void *q, const void *k, const void *v, int64_t q_stride, int32_t dtype, cudaStream_t stream) {
     CUtensorMap q_map, do_map, k_map, v_map;
     if (!head_map(&q_map, q, dtype, D, a.Hq, a.T, q_stride, a.hp, a.tp) || !head_map(&do_map, a.dout, dtype, D, a.Hq, a.T, a.dout_stride, a.hp, a.tp) ||
-        !head_map(&k_map, k, dtype, D, a.Hkv, a.T, a.kv_stride, 1, kTile) || !head_map(&v_map, v, dtype, D, a.Hkv, a.T, a.kv_stride, 1, kTile))
+        !head_map(&k_map, k, dtype, D, a.Hkv, a.T, a.k_stride, 1, kTile) || !head_map(&v_map, v, dtype, D, a.Hkv, a.T, a.v_stride, 1, kTile))
         return HORA_ERR_CUDA;
     constexpr int kKeysSmem = KeysSmem<D>::kSmall + (int)sizeof(KeysShared), kQueriesSmem = QueriesSmem<D>::kSmall + (int)sizeof(QueriesShared);
     static std::atomic<uint64_t> keys_devices{0}, queries_devices{0};

@@ -214,7 +214,7 @@ packed_forward_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
                 const int32_t tokens = t ? it.tokens[1] : it.tokens[0];
                 if (tokens == 0) continue;
                 const int32_t token = it.token0 + t * a.tp + row_token;
-                const bool have = row_token < tokens;
+                const bool have = row_token < tokens && HORA_IN(token, a.T);
                 ok = bar_wait(summed + 8 * t, phase >> t & 1, failed);
                 const float2 ml = sh.sums[t][row];
                 bar_arrive(sums_free + 8 * t);
@@ -263,7 +263,7 @@ packed_forward_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
         }
     } else if (warp >= 8) {
         if (warp == kFeedWarp) {
-            if (lane == 0) feed<2>(sh.feed, reinterpret_cast<const int4 *>(a.query_items), __ldcg(a.counts), a.blocks, a.counts + 4, failed);
+            if (lane == 0) feed<2>(sh.feed, reinterpret_cast<const int4 *>(a.query_items), __ldcg(a.counts), a.query_cap, a.blocks, a.counts + 4, failed);
         } else if (warp == kLoadWarp) {
             if (lane == 0) {
                 int32_t pos = 0;                         // copies into the ring so far
@@ -461,8 +461,8 @@ packed_forward_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
 template <typename Q, int D>
 hora_status_t launch_forward(const PackedArgs &a, const void *q, const void *k, const void *v, int64_t q_stride, int32_t dtype, cudaStream_t stream) {
     CUtensorMap q_map, k_map, v_map;
-    if (!head_map(&q_map, q, dtype, D, a.Hq, a.T, q_stride, a.hp, a.tp) || !head_map(&k_map, k, dtype, D, a.Hkv, a.T, a.kv_stride, 1, kTile) ||
-        !head_map(&v_map, v, dtype, D, a.Hkv, a.T, a.kv_stride, 1, kTile))
+    if (!head_map(&q_map, q, dtype, D, a.Hq, a.T, q_stride, a.hp, a.tp) || !head_map(&k_map, k, dtype, D, a.Hkv, a.T, a.k_stride, 1, kTile) ||
+        !head_map(&v_map, v, dtype, D, a.Hkv, a.T, a.v_stride, 1, kTile))
         return HORA_ERR_CUDA;
     constexpr int kSmem = ForwardSmem<D>::kSmall + (int)sizeof(ForwardShared);
     static std::atomic<uint64_t> devices{0};

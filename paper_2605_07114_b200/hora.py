@@ -137,10 +137,10 @@ def load() -> C.CDLL:
     L.hora_qk_rotate_backward.restype = C.c_int
     L.hora_packed_attention_workspace_bytes.argtypes = [i64, i64, i32, i32, i32, i32]
     L.hora_packed_attention_workspace_bytes.restype = C.c_size_t
-    L.hora_packed_attention.argtypes = [p, p, p, i32, i64, i64, i64, p, i64, p, i64, i32, i32, i32, C.c_float, i32, p, i64, p, p, p, C.c_size_t, p]
+    L.hora_packed_attention.argtypes = [p, p, p, i32, i64, i64, i64, i64, p, i64, p, i64, i32, i32, i32, C.c_float, i32, p, i64, p, p, p, C.c_size_t, p]
     L.hora_packed_attention.restype = C.c_int
-    L.hora_packed_attention_backward.argtypes = [p, p, p, p, p, p, i32, i64, i64, i64, i64, i64, p, i64, p, i64, i32, i32, i32, C.c_float, i32, p, p, p,
-                                                 i64, i64, p, p, C.c_size_t, p]
+    L.hora_packed_attention_backward.argtypes = [p, p, p, p, p, p, i32, i64, i64, i64, i64, i64, i64, p, i64, p, i64, i32, i32, i32, C.c_float, i32, p, p, p,
+                                                 i64, i64, i64, p, p, C.c_size_t, p]
     L.hora_packed_attention_backward.restype = C.c_int
     L.hora_checked_violation.restype = C.c_int32
     L.hora_fp64_probe.argtypes = [i32, p, p]
@@ -735,43 +735,38 @@ def hora_packed_attention_workspace_bytes(T, S, Hq, Hkv, D, backward) -> int:
 
 
 def _packed_shapes(q, k, v, seq_offsets, group_offsets):
-    """(T, Hq, Hkv, D, q stride, kv stride, the arguments from T to D)."""
+    """(T, Hq, the token strides of q, k, v, the arguments from T to D)."""
     if q.dim() != 3 or k.dim() != 3:
         raise ValueError("q must have the shape [T, Hq, D], k and v [T, Hkv, D]")
     T, Hq, D = q.shape
     Hkv = k.shape[1]
-    qs, ks = _heads(q, q.shape, "q"), _heads(k, (T, Hkv, D), "k", q.dtype)
-    if _heads(v, (T, Hkv, D), "v", q.dtype) != ks:
-        raise ValueError("k and v must have the same row stride")
+    strides = _heads(q, q.shape, "q"), _heads(k, (T, Hkv, D), "k", q.dtype), _heads(v, (T, Hkv, D), "v", q.dtype)
     for t, name in ((seq_offsets, "seq_offsets"), (group_offsets, "group_offsets")):
         if t is not None and (t.dim() != 1 or t.numel() < 1):
             raise ValueError(f"{name} must have one dimension")
     N = 0 if group_offsets is None else group_offsets.numel() - 1
-    return T, Hq, Hkv, D, qs, ks, (T, _at(seq_offsets, torch.int64, "seq_offsets"), seq_offsets.numel() - 1, _at(group_offsets, torch.int64, "group_offsets"), N, Hq, Hkv, D)
+    return T, Hq, strides, (T, _at(seq_offsets, torch.int64, "seq_offsets"), seq_offsets.numel() - 1, _at(group_offsets, torch.int64, "group_offsets"), N, Hq, Hkv, D)
 
 
 def hora_packed_attention(q, k, v, seq_offsets, group_offsets, sm_scale, causal, out, lse, workspace, status_dev=None):
     """q, out [T, Hq, D], k, v [T, Hkv, D] (tokens may be strided), lse [T, Hq] fp32 or None; seq_offsets [S+1], group_offsets [N+1] int64 or None."""
-    T, Hq, Hkv, D, qs, ks, shape = _packed_shapes(q, k, v, seq_offsets, group_offsets)
+    T, Hq, strides, shape = _packed_shapes(q, k, v, seq_offsets, group_offsets)
     _one_device(q, k, v, seq_offsets, group_offsets, out, lse, workspace, status_dev)
-    _check(load().hora_packed_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), _dtype_code(q, "q"), qs, ks, *shape, float(sm_scale), int(causal), out.data_ptr(),
+    _check(load().hora_packed_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), _dtype_code(q, "q"), *strides, *shape, float(sm_scale), int(causal), out.data_ptr(),
                                         _heads(out, q.shape, "out", q.dtype), _at(lse, torch.float32, "lse", T * Hq), _at(status_dev, torch.int32, "status_dev"),
                                         _at(workspace, torch.uint8, "workspace"), workspace.numel(), _raw_stream(q)), "hora_packed_attention")
 
 
 def hora_packed_attention_backward(q, k, v, out, lse, dout, seq_offsets, group_offsets, sm_scale, causal, dq, dk, dv, workspace, status_dev=None):
     """The gradients dq [T, Hq, D], dk, dv [T, Hkv, D] (tokens may be strided) from dout; out, lse as hora_packed_attention left them."""
-    T, Hq, Hkv, D, qs, ks, shape = _packed_shapes(q, k, v, seq_offsets, group_offsets)
+    T, Hq, strides, shape = _packed_shapes(q, k, v, seq_offsets, group_offsets)
     _one_device(q, k, v, out, lse, dout, seq_offsets, group_offsets, dq, dk, dv, workspace, status_dev)
-    dks = _heads(dk, k.shape, "dk", q.dtype)
-    if _heads(dv, k.shape, "dv", q.dtype) != dks:
-        raise ValueError("dk and dv must have the same row stride")
     if lse is None:
         raise ValueError("lse is missing")
     _check(load().hora_packed_attention_backward(
-        q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _at(lse, torch.float32, "lse", T * Hq), dout.data_ptr(), _dtype_code(q, "q"), qs, ks,
+        q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _at(lse, torch.float32, "lse", T * Hq), dout.data_ptr(), _dtype_code(q, "q"), *strides,
         _heads(out, q.shape, "out", q.dtype), _heads(dout, q.shape, "dout", q.dtype), *shape, float(sm_scale), int(causal), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-        _heads(dq, q.shape, "dq", q.dtype), dks, _at(status_dev, torch.int32, "status_dev"), _at(workspace, torch.uint8, "workspace"), workspace.numel(),
+        _heads(dq, q.shape, "dq", q.dtype), _heads(dk, k.shape, "dk", q.dtype), _heads(dv, k.shape, "dv", q.dtype), _at(status_dev, torch.int32, "status_dev"), _at(workspace, torch.uint8, "workspace"), workspace.numel(),
         _raw_stream(q)), "hora_packed_attention_backward")
 
 
@@ -821,8 +816,8 @@ class PackedAttention:
         """Returns (out, lse)."""
         out, lse = self.out if out is None else out, self.lse if lse is None else lse
         st = self._strides(q.dtype, (q, out), (k, v)) if lse is self.lse else None
-        if st is not None and st[2] == st[3]:
-            _check(load().hora_packed_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), self._code, st[0], st[2], *self._middle, out.data_ptr(), st[1], self._lse,
+        if st is not None:
+            _check(load().hora_packed_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), self._code, st[0], st[2], st[3], *self._middle, out.data_ptr(), st[1], self._lse,
                                                 *self._tail, torch._C._cuda_getCurrentRawStream(self._device)), "hora_packed_attention")
         else:
             hora_packed_attention(q, k, v, self.seq_offsets, self.group_offsets, self.sm_scale, self.causal, out, lse, self.workspace, self.status_dev)
@@ -835,9 +830,9 @@ class PackedAttention:
             raise ValueError("made without backward=True")
         dq, dk, dv = self.dq if dq is None else dq, self.dk if dk is None else dk, self.dv if dv is None else dv
         st = self._strides(q.dtype, (q, out, dout, dq), (k, v, dk, dv)) if lse is self.lse else None
-        if st is not None and st[4] == st[5] and st[6] == st[7]:
-            _check(load().hora_packed_attention_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), self._lse, dout.data_ptr(), self._code, st[0], st[4], st[1],
-                                                         st[2], *self._middle, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), st[3], st[6], *self._tail,
+        if st is not None:
+            _check(load().hora_packed_attention_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), self._lse, dout.data_ptr(), self._code, st[0], st[4], st[5],
+                                                         st[1], st[2], *self._middle, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), st[3], st[6], st[7], *self._tail,
                                                          torch._C._cuda_getCurrentRawStream(self._device)), "hora_packed_attention_backward")
         else:
             hora_packed_attention_backward(q, k, v, out, lse, dout, self.seq_offsets, self.group_offsets, self.sm_scale, self.causal, dq, dk, dv, self.workspace,

@@ -210,11 +210,10 @@ def test_rows_at_other_distances_and_given_outputs():
     off, T, Hq, Hkv, D = offsets([90, 170]), 260, 6, 2, 128
     x = inputs(T, Hq, Hkv, D, BF, 11)
     apart = []
-    for t in x:                                          # 8, 16, .. elements more between the tokens, 16-byte aligned only
-        room = torch.empty(T, t.shape[1] * D + 8 * (len(apart) // 3 + 1), dtype=BF, device=DEV)
-        y = room[:, 8:8 + t.shape[1] * D].unflatten(1, (t.shape[1], D)) if room.shape[1] >= t.shape[1] * D + 8 else None
-        y.copy_(t)
-        apart.append(y)
+    for i, t in enumerate(x):                            # 16, 24, .. elements more between the tokens, 16-byte aligned only
+        width = t.shape[1] * D
+        apart.append(torch.empty(T, width + 8 * (i + 2), dtype=BF, device=DEV)[:, 8:8 + width].unflatten(1, (t.shape[1], D)))
+        apart[-1].copy_(t)
     i64 = torch.tensor(off, device=DEV)
     ws = torch.empty(hora.hora_packed_attention_workspace_bytes(T, 2, Hq, Hkv, D, True), dtype=torch.uint8, device=DEV)
     fused = torch.full((T, Hq + 2 * Hkv, D), 3.0, dtype=BF, device=DEV)
