@@ -274,7 +274,7 @@ packed_stats_kernel(const PackedArgs a) {
                 for (int s = kLanes / 2; s > 0; s >>= 1) size += __shfl_xor_sync(kFull, size, s);
                 most_d = fmaxf(most_d, size);
             }
-            if (lane == 0 && at[i] >= 0) a.stats[at[i]] = make_float2(__ldcg(a.lse + at[i]) * kLog2e, dot);
+            if (lane == 0 && at[i] >= 0) *reinterpret_cast<float2 *>(a.stats + at[i]) = make_float2(__ldcg(a.lse + at[i]) * kLog2e, dot);
         }
     }
     for (int64_t x = (int64_t)blockIdx.x * kGroups + group; __any_sync(kFull, x < v_rows); x += stride) {
@@ -322,7 +322,7 @@ static size_t lay_out(PackedArgs &a, bool backward, char *base) {
     a.key_items = nullptr;
     if (backward) {
         a.key_items = reinterpret_cast<KeyItem *>(take((size_t)a.key_cap * sizeof(KeyItem)));
-        a.stats = reinterpret_cast<float2 *>(take((size_t)a.T * a.Hq * sizeof(float2)));
+        a.stats = reinterpret_cast<float4 *>(take((size_t)a.T * a.Hq * sizeof(float4)));
         a.tickets = reinterpret_cast<int32_t *>(take((size_t)a.n_sm * 8 * sizeof(int32_t)));
         a.slots = reinterpret_cast<float *>(take((size_t)2 * a.n_sm * 2 * kPackedRows * a.D * sizeof(float)));
     }

@@ -48,7 +48,7 @@ struct PackedArgs {
     KeyItem *key_items;
     int32_t *tickets;                                    // [n_sm][8]: by warp
     float *slots;                                        // [2 n_sm][dV, dK][128][D]
-    float2 *stats;                                       // [T][Hq] (lse in units of log2, dout . out)
+    float4 *stats;                                       // [T][Hq] (lse in units of log2, dout . out, what that is off by in two parts)
 };
 
 // CTAs take the items of a list one after the other, the longest first: the first by their own number, the following ones from a counter.

@@ -25,6 +25,7 @@ namespace hora {
 namespace {
 
 constexpr int kTile = kPackedRows, kHalfTile = kTile / 2;
+constexpr int kRest = kHalfTile / 2;                     // columns from gradients of scores to what rounding them left
 constexpr int kMiddleThreads = 256, kLoadWarp = 8, kProductWarp = 9, kFeedWarp = 11;
 constexpr int kFeedReaders = 11;                         // warps that take items from the feeder (one less for keys)
 
@@ -57,6 +58,9 @@ __device__ __forceinline__ void product_with_weights(uint32_t lead, uint32_t d, 
         for (int g = 1; g * 16 < count; ++g) mma_tmem(lead, d, w + g * 8 + (g < 4 ? 0 : kHalfTile - 32), b + g * (2048 >> 4), kIdescSum<Q, D>, 1);
     }
 }
+
+__device__ __forceinline__ float2 unpack2(uint32_t w, __nv_bfloat16) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+__device__ __forceinline__ float2 unpack2(uint32_t w, __half) { return half2_bits(w); }
 
 // Rows count .. of a tile up to the last sixteen that a product reads are set to zero.  All lanes of a warp.
 template <int D>
@@ -225,16 +229,16 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
                 }
             }
             __syncwarp();
-            auto stats_of = [&](int32_t s, float2 (&st)[kTile / kWarp]) {
+            auto stats_of = [&](int32_t s, float4 (&st)[kTile / kWarp]) {
                 const KeyStep k = key_step(a, it, s);
 #pragma unroll
                 for (int i = 0; i < kTile / kWarp; ++i) {
                     const int32_t row = lane + i * kWarp, token = k.token0 + row / a.hp;
-                    st[i] = make_float2(INFINITY, 0.f);
+                    st[i] = make_float4(INFINITY, 0.f, 0.f, 0.f);
                     if (row < k.count && HORA_IN(token, a.T)) st[i] = __ldcg(a.stats + (int64_t)token * a.Hq + k.block * a.hp + row % a.hp);
                 }
             };
-            float2 st[kTile / kWarp];
+            float4 st[kTile / kWarp];
             stats_of(0, st);
             for (int32_t s = 0; s < it.steps; ++s, ++pos) {
                 const KeyStep k = key_step(a, it, s);
@@ -253,7 +257,7 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
 #pragma unroll
                 for (int i = 0; i < kTile / kWarp; ++i) {
                     sh.lse[stage][lane + i * kWarp] = (float)up - st[i].x;
-                    sh.delta[stage][lane + i * kWarp] = -st[i].y * c;
+                    sh.delta[stage][lane + i * kWarp] = -(st[i].y + (st[i].z + st[i].w)) * c;
                 }
                 bar_arrive(full + 8 * stage);
                 if (s + 1 < it.steps) stats_of(s + 1, st);
@@ -648,7 +652,9 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
                     phase ^= 1u << b;
                     if (j == 0 && r > 0) bar_wait(sums_free, (r + 1) & 1, failed);
                     fence_after();
-                    product_with_weights<Q, D>(lead, tmem + 3 * kTile, tmem + kTile + b * kTile, operand(at, kTile * 128), seen, j == 0);
+                    const uint32_t ds = tmem + kTile + b * kTile, k_columns = operand(at, kTile * 128);
+                    product_with_weights<Q, D>(lead, tmem + 3 * kTile, ds, k_columns, seen, j == 0);
+                    product_with_weights<Q, D>(lead, tmem + 3 * kTile, ds + kRest, k_columns, seen, false);
                     mma_commit(lead, empty + 8 * stage);
                     if (j + 1 == it.n) mma_commit(lead, sums);
                 }
@@ -665,18 +671,20 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
         const float2 scale2 = make_float2(a.scale_log2, a.scale_log2), c2 = make_float2(c, c);
         auto stats_of = [&](const QueryWork &w) {
             float2 st = make_float2(INFINITY, 0.f);
-            if (w.valid && row_token < w.tokens && HORA_IN(w.token0 + row_token, a.T)) st = __ldcg(a.stats + (int64_t)(w.token0 + row_token) * a.Hq + w.block * a.hp + row_head);
+            if (w.valid && row_token < w.tokens && HORA_IN(w.token0 + row_token, a.T)) st = __ldcg(reinterpret_cast<const float2 *>(a.stats + (int64_t)(w.token0 + row_token) * a.Hq + w.block * a.hp + row_head));
             return st;
         };
         uint32_t phase = 0, products_phase = 0;
         for (int32_t r = 0; ok; ++r) {
             const QueryWork it = make_queries(a, feed_next<false>(sh.feed, r, failed));
             if (!it.valid) break;
+            const int64_t row_at = (int64_t)(it.token0 + row_token) * a.Hq + it.block * a.hp + row_head;
             const float2 st = stats_of(it);
             const float2 lse2 = make_float2((float)up - st.x, (float)up - st.x), delta2 = make_float2(-st.y * c, -st.y * c);
             const bool have = row_token < it.tokens && HORA_IN(it.token0 + row_token, a.T);
             const int32_t token = it.token0 + row_token;
             const int32_t seen_to = a.causal && have ? min(it.end, token + 1) : it.end;
+            float2 off = make_float2(0.f, 0.f);
             for (int32_t j = 0; j < it.n; ++j, phase ^= 1) {
                 const int32_t limit = (j < it.n_shared ? it.shared1 - it.shared0 - j * kTile : seen_to - it.own0 - (j - it.n_shared) * kTile) - half * kHalfTile;
                 ok = bar_wait(scores, phase, failed);
@@ -710,7 +718,7 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
                 tmem_load_wait();
 #pragma unroll
                 for (int b = 0; b < 4; ++b) {
-                    uint32_t w[8];
+                    uint32_t w[8], rest[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float *x = p[b >> 1] + (b & 1) * 16 + 2 * e, *d = dp[b >> 1] + (b & 1) * 16 + 2 * e;
@@ -719,15 +727,21 @@ packed_queries_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
                             if (b * 16 + 2 * e >= limit) y.x = 0.f;
                             if (b * 16 + 2 * e + 1 >= limit) y.y = 0.f;
                         }
+                        off = add2(off, y);
                         w[e] = pack2(y.x, y.y, Q());
+                        const float2 held = unpack2(w[e], Q());
+                        rest[e] = pack2(y.x - held.x, y.y - held.y, Q());
                     }
                     tmem_store8(t_dp + b * 8, w);
+                    tmem_store8(t_dp + kRest + b * 8, rest);
                 }
                 tmem_store_wait();
                 fence_before();
                 bar_arrive(gradients + 8 * b2);
             }
             if (!ok) break;
+            // a row's dS add up to nothing; what they add up to is what dout . out was off by
+            if (have && ok) (half ? a.stats[row_at].w : a.stats[row_at].z) = (off.x + off.y) * exp2f((float)-shift);
             ok = bar_wait(sums, r & 1, failed);
             ok = __all_sync(kFull, ok);
             if (!ok) break;
@@ -758,9 +772,9 @@ hora_status_t launch_backward(const PackedArgs &a, const void *q, const void *k,
     cudaError_t e = allow_shared(reinterpret_cast<const void *>(packed_keys_kernel<Q, D>), kKeysSmem, keys_devices);
     if (e == cudaSuccess) e = allow_shared(reinterpret_cast<const void *>(packed_queries_kernel<Q, D>), kQueriesSmem, queries_devices);
     if (e == cudaSuccess)
-        e = launch_pdl(packed_keys_kernel<Q, D>, clamp_grid(((int64_t)a.T / kTile + a.S) * a.Hkv + 2 * a.n_sm, 1), kPackedThreads, kKeysSmem, stream, a, q_map, do_map, k_map, v_map);
-    if (e == cudaSuccess)
         e = launch_pdl(packed_queries_kernel<Q, D>, clamp_grid((int64_t)a.query_cap * a.blocks, 1), kPackedThreads, kQueriesSmem, stream, a, q_map, do_map, k_map, v_map);
+    if (e == cudaSuccess)
+        e = launch_pdl(packed_keys_kernel<Q, D>, clamp_grid(((int64_t)a.T / kTile + a.S) * a.Hkv + 2 * a.n_sm, 1), kPackedThreads, kKeysSmem, stream, a, q_map, do_map, k_map, v_map);
     count_launches(2);
     return cuda_ok(e);
 }
