@@ -71,100 +71,159 @@ struct Turn {
             }
         }
     }
+};
 
-    // all lanes of the warp
-    __device__ __forceinline__ void apply(float (&z)[8], int lane_in_warp) const {
-        float p[8];
+// The eight values of the lane `other` away, as they lie in memory.  All lanes of the warp.
+__device__ __forceinline__ uint4 shuffled(const uint4 &v, int from) {
+    return make_uint4(__shfl_sync(kFull, v.x, from), __shfl_sync(kFull, v.y, from), __shfl_sync(kFull, v.z, from), __shfl_sync(kFull, v.w, from));
+}
+__device__ __forceinline__ float4 shuffled(const float4 &v, int from) {
+    return make_float4(__shfl_sync(kFull, v.x, from), __shfl_sync(kFull, v.y, from), __shfl_sync(kFull, v.z, from), __shfl_sync(kFull, v.w, from));
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> shuffled(const Raw8<T> &v, int from) {
+    Raw8<T> r;
+    r.a = shuffled(v.a, from);
+    if constexpr (sizeof(Raw8<T>) == 32) r.b = shuffled(v.b, from);
+    return r;
+}
+template <typename T, bool PAIRS>
+__device__ __forceinline__ void others8(const Raw8<T> &v, const float (&x)[8], int from, float (&p)[8]) {
+    if constexpr (PAIRS) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = PAIRS ? z[i ^ 1] : __shfl_sync(kFull, z[i], lane_in_warp + other);
-        if (turned) {
+        for (int i = 0; i < 8; ++i) p[i] = x[i ^ 1];
+    } else {
+        widen8(shuffled(v, from), p);
+    }
+}
+
+// One group's heads of one side, from..to - 1 of it: x (and dy) at a token's first head, the result to y.  The next heads' loads are on their
+// way while these are worked on; `first` has been called before the angles were worked out.  The weights enter the angles' cosines and sines once for
+// all heads; what a lane takes from the other lane of its pairs it takes as it lies in memory (the kernels issue in 0.7 of the cycles: their
+// instructions count).
+template <typename T, int D, bool PAIRS, bool BACKWARD>
+struct Side {
+    static constexpr int kLanes = D / 8, kAhead = BACKWARD ? kRotateHeads / 2 : kRotateHeads;
+    const T *x, *dy;
+    T *y;
+    int32_t from, to;
+    bool norm;
+    Raw8<T> next_x[kAhead], next_dy[kAhead];
+
+    __device__ __forceinline__ void load(int32_t h) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = z[i] * c[i] + p[i] * s[i];
+        for (int i = 0; i < kAhead; ++i) {
+            if (h + i < to && (!BACKWARD || norm)) load8(next_x[i], x + (h + i) * D);
+            else zero8(next_x[i]);
+            if constexpr (BACKWARD) {
+                if (h + i < to) load8(next_dy[i], dy + (h + i) * D);
+                else zero8(next_dy[i]);
+            }
+        }
+    }
+
+    // `most`: heads of the warp's group with the most
+    __device__ __forceinline__ void run(const Turn<D, PAIRS> &turn, const float (&w)[8], float (&dw)[8], float eps, int lane_in_warp, int32_t most) {
+        const int source = lane_in_warp + turn.other;
+        float c[8], s[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            // forwards the weights of both values of a pair enter: r (x w c + x' w' s)
+            const float other_w = BACKWARD ? 1.f : PAIRS ? w[i ^ 1] : __shfl_sync(kFull, w[i], source);
+            c[i] = BACKWARD ? turn.c[i] : turn.c[i] * w[i];
+            s[i] = BACKWARD ? turn.s[i] : turn.s[i] * other_w;
+        }
+#pragma unroll 1
+        for (int32_t b = 0; b < most; b += kAhead) {
+            Raw8<T> now_x[kAhead], now_dy[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                now_x[i] = next_x[i];
+                if (BACKWARD) now_dy[i] = next_dy[i];
+            }
+            const int32_t h = from + b;
+            load(h + kAhead);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                if (b + i >= most) break;
+                float z[8], p[8];
+                float r = 1.f;
+                widen8(now_x[i], z);
+                if (norm) {                              // alike for the whole warp
+                    float sum = 0.f;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum += z[e] * z[e];
+                    r = rsqrtf(group_sum<kLanes>(sum) * (1.f / D) + eps);
+                }
+                if constexpr (!BACKWARD) {
+                    others8<T, PAIRS>(now_x[i], z, source, p);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        z[e] *= c[e];
+                        if (turn.turned) z[e] += p[e] * s[e];
+                        z[e] *= r;
+                    }
+                } else {
+                    float g[8];
+                    widen8(now_dy[i], g);
+                    others8<T, PAIRS>(now_dy[i], g, source, p);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        g[e] *= c[e];
+                        if (turn.turned) g[e] += p[e] * s[e];
+                    }
+                    if (norm) {
+                        float dot = 0.f;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            dw[e] += r * z[e] * g[e];
+                            g[e] *= w[e];
+                            dot += z[e] * g[e];
+                        }
+                        dot = group_sum<kLanes>(dot) * (1.f / D) * r * r;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) g[e] = r * (g[e] - z[e] * dot);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) z[e] = g[e];
+                }
+                if (h + i < to) {
+                    Raw8<T> out;
+                    narrow8(z, out);
+                    store8(out, y + (h + i) * D);
+                }
+            }
         }
     }
 };
 
-// One group's part: a token and `heads` of its heads.  The next heads' loads are on their way while these are worked on, the first ones' while
-// the angles are.
+// One group's part: a token and `heads` of its heads.
 template <typename T, int D, bool PAIRS, bool BACKWARD>
 __device__ __forceinline__ void rotate_unit(const RotateArgs &a, int64_t unit, bool have, const float (&w)[2][8], float (&dw)[2][8]) {
-    constexpr int kLanes = D / 8, kAhead = BACKWARD ? kRotateHeads / 2 : kRotateHeads;
+    constexpr int kLanes = D / 8;
     const int lane_in_warp = lane_id(), lane = lane_in_warp % kLanes;
     const int64_t token = have ? (a.chunks == 1 ? unit : unit / a.chunks) : 0;
-    const int32_t h0 = have && a.chunks > 1 ? (int32_t)(unit - token * a.chunks) * a.heads : 0;
-    const T *const x_q = static_cast<const T *>(a.x[0]) + token * a.x_stride[0], *const x_k = static_cast<const T *>(a.x[1]) + token * a.x_stride[1];
-    const T *const dy_q = static_cast<const T *>(a.dy[0]) + token * a.dy_stride[0], *const dy_k = static_cast<const T *>(a.dy[1]) + token * a.dy_stride[1];
-    T *const y_q = static_cast<T *>(a.y[0]) + token * a.y_stride[0], *const y_k = static_cast<T *>(a.y[1]) + token * a.y_stride[1];
-    const bool norms[2] = {a.w[0] != nullptr, a.w[1] != nullptr};
-    Raw8<T> x[kAhead], dy[kAhead];
-    auto load = [&](int32_t b) {
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int32_t h = h0 + b + i;
-            const bool is_k = h >= a.Hq, mine = have && b + i < a.heads && h < a.H;
-            const int32_t at = (is_k ? h - a.Hq : h) * D + lane * 8;
-            if (mine && (!BACKWARD || (is_k ? norms[1] : norms[0]))) load8(x[i], (is_k ? x_k : x_q) + at);
-            else zero8(x[i]);
-            if constexpr (BACKWARD) {
-                if (mine) load8(dy[i], (is_k ? dy_k : dy_q) + at);
-                else zero8(dy[i]);
-            }
-        }
+    const int32_t h0 = have && a.chunks > 1 ? (int32_t)(unit - token * a.chunks) * a.heads : 0, h1 = have ? min(a.H, h0 + a.heads) : h0;
+    auto side = [&](int k) {
+        Side<T, D, PAIRS, BACKWARD> s;
+        s.x = static_cast<const T *>(k ? a.x[1] : a.x[0]) + token * (k ? a.x_stride[1] : a.x_stride[0]) + lane * 8;
+        s.dy = static_cast<const T *>(k ? a.dy[1] : a.dy[0]) + token * (k ? a.dy_stride[1] : a.dy_stride[0]) + lane * 8;
+        s.y = static_cast<T *>(k ? a.y[1] : a.y[0]) + token * (k ? a.y_stride[1] : a.y_stride[0]) + lane * 8;
+        s.from = k ? max(h0 - a.Hq, 0) : h0;
+        s.to = k ? max(h1 - a.Hq, s.from) : max(min(h1, a.Hq), h0);
+        s.norm = (k ? a.w[1] : a.w[0]) != nullptr;
+        return s;
     };
-    load(0);
+    Side<T, D, PAIRS, BACKWARD> q = side(0);
+    q.load(q.from);
     const Turn<D, PAIRS> turn(a, token, have, lane, BACKWARD ? -1.f : 1.f);
-#pragma unroll 1
-    for (int32_t b = 0; b < a.heads; b += kAhead) {
-        Raw8<T> x_now[kAhead], dy_now[kAhead];
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            x_now[i] = x[i];
-            if (BACKWARD) dy_now[i] = dy[i];
-        }
-        load(b + kAhead);
-#pragma unroll
-        for (int i = 0; i < kAhead; ++i) {
-            const int32_t h = h0 + b + i;
-            const bool is_k = h >= a.Hq, mine = have && b + i < a.heads && h < a.H;
-            if (!__any_sync(kFull, mine)) break;
-            const bool norm = mine && (is_k ? norms[1] : norms[0]);
-            float z[8];
-            widen8(x_now[i], z);
-            float sum = 0.f;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sum += z[e] * z[e];
-            const float r = rsqrtf(group_sum<kLanes>(sum) * (1.f / D) + a.eps);
-            if constexpr (!BACKWARD) {
-                if (norm) {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) z[e] = z[e] * r * (is_k ? w[1][e] : w[0][e]);
-                }
-                turn.apply(z, lane_in_warp);
-            } else {
-                float g[8], dot = 0.f;
-                widen8(dy_now[i], g);
-                turn.apply(g, lane_in_warp);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    z[e] *= r;
-                    const float step = z[e] * g[e];
-                    if (norm) {
-                        if (is_k) dw[1][e] += step;
-                        else dw[0][e] += step;
-                    }
-                    g[e] *= is_k ? w[1][e] : w[0][e];
-                    dot += z[e] * g[e];
-                }
-                dot = group_sum<kLanes>(dot) * (1.f / D);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) z[e] = norm ? r * (g[e] - z[e] * dot) : g[e];
-            }
-            if (mine) {
-                Raw8<T> y;
-                narrow8(z, y);
-                store8(y, (is_k ? y_k : y_q) + (is_k ? h - a.Hq : h) * D + lane * 8);
-            }
-        }
+    int32_t most = __reduce_max_sync(kFull, q.to - q.from);
+    if (most > 0) q.run(turn, w[0], dw[0], a.eps, lane_in_warp, most);
+    Side<T, D, PAIRS, BACKWARD> k = side(1);
+    most = __reduce_max_sync(kFull, k.to - k.from);
+    if (most > 0) {
+        k.load(k.from);
+        k.run(turn, w[1], dw[1], a.eps, lane_in_warp, most);
     }
 }
 
@@ -178,7 +237,7 @@ __device__ __forceinline__ void load_weights(const RotateArgs &a, float (&w)[2][
 }
 
 template <typename T, int D, bool PAIRS>
-__global__ void __launch_bounds__(kRotateThreads, sizeof(T) == 2 ? 3 : 2)          // three CTAs an SM: 279 -> 267 us for 131072 tokens; fp32 rows would spill
+__global__ void __launch_bounds__(kRotateThreads, sizeof(T) == 2 ? 3 : 2)
 qk_rotate_kernel(const RotateArgs a) {
     pdl_enter();
     constexpr int kGroups = kRotateThreads / (D / 8);
@@ -189,7 +248,7 @@ qk_rotate_kernel(const RotateArgs a) {
 }
 
 template <typename T, int D, bool PAIRS>
-__global__ void __launch_bounds__(kRotateThreads)
+__global__ void __launch_bounds__(kRotateThreads, 2)
 qk_rotate_backward_kernel(const RotateArgs a) {
     pdl_enter();
     constexpr int kLanes = D / 8, kGroups = kRotateThreads / kLanes;
