@@ -173,7 +173,6 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
         for_items<KEYS>(a, q, [&](const PackedSequence &s, int32_t i) {
             const int32_t steps = item_steps<KEYS>(a, s, i), parts = KEYS ? parts_of(steps, most) : 1, part_steps = (steps + parts - 1) / parts;
             const int32_t to = atomicAdd(s_bucket + bucket_of(part_steps), parts);
-            if (to + parts > cap) return;
             if constexpr (KEYS) {
                 const int32_t key0 = s.lo + i * kPackedRows, q0 = a.causal ? key0 : s.lo;
                 int32_t slot0 = 0, ticket = 0;
@@ -182,13 +181,14 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
                     ticket = atomicAdd(s_next + 1, 1);
                 }
                 int4 *item = reinterpret_cast<int4 *>(a.key_items + to);
-                for (int32_t p = 0; p < parts; ++p) {
+                for (int32_t p = 0; p < parts && to + p < cap; ++p) {
                     const int64_t from = q0 + (int64_t)p * part_steps * a.tp;
                     item[2 * p] = make_int4(key0, min(kPackedRows, s.hi - key0), (int32_t)min((int64_t)s.seen_to, from),
                                             (int32_t)min((int64_t)s.seen_to, from + (int64_t)part_steps * a.tp));
                     item[2 * p + 1] = make_int4(slot0, parts, p, ticket);
                 }
             } else {
+                if (to >= cap) return;
                 const int32_t token0 = s.lo + i * a.tile_tokens;
                 int4 *item = reinterpret_cast<int4 *>(a.query_items + to);
                 item[0] = make_int4(token0, min(a.tile_tokens, s.hi - token0), s.lo, s.hi);
@@ -341,6 +341,8 @@ static bool packed_sizes(PackedArgs &a, int64_t T, int64_t S, int64_t N, int32_t
     return true;
 }
 
+static bool aligned(const void *p, uintptr_t bytes) { return !(reinterpret_cast<uintptr_t>(p) & (bytes - 1)); }
+
 static bool packed_rows(const void *p, int64_t stride, int32_t H, int32_t D) {
     return p != nullptr && !(reinterpret_cast<uintptr_t>(p) & 15u) && stride >= (int64_t)H * D && stride % 8 == 0 && stride < (1ll << 38);
 }
@@ -367,7 +369,7 @@ static hora_status_t packed_begin(PackedArgs &a, const void *q, const void *k, c
     if (!(sm_scale > 0.f) || sm_scale > 1e30f || (causal != 0 && causal != 1)) return HORA_ERR_INVALID_ARG;
     if ((group_offsets == nullptr) != (N == 0)) return HORA_ERR_INVALID_ARG;
     if (T == 0 || S == 0) return HORA_OK;
-    if (seq_offsets == nullptr || !packed_rows(q, q_row_stride, Hq, D) || !packed_rows(k, k_row_stride, Hkv, D) || !packed_rows(v, v_row_stride, Hkv, D)) return HORA_ERR_INVALID_ARG;
+    if (seq_offsets == nullptr || !aligned(seq_offsets, 8) || !aligned(group_offsets, 8) || !packed_rows(q, q_row_stride, Hq, D) || !packed_rows(k, k_row_stride, Hkv, D) || !packed_rows(v, v_row_stride, Hkv, D)) return HORA_ERR_INVALID_ARG;
     a.seq_offsets = seq_offsets;
     a.group_offsets = group_offsets;
     a.v = v;
@@ -401,7 +403,7 @@ extern "C" hora_status_t hora_packed_attention(const void *q, const void *k, con
     PackedArgs a = {};
     hora_status_t rc = packed_begin(a, q, k, v, dtype, q_row_stride, k_row_stride, v_row_stride, T, seq_offsets, S, group_offsets, N, Hq, Hkv, D, sm_scale, causal);
     if (rc != HORA_OK || T == 0 || S == 0) return rc;
-    if (!packed_rows(out, out_row_stride, Hq, D)) return HORA_ERR_INVALID_ARG;
+    if (!packed_rows(out, out_row_stride, Hq, D) || !aligned(lse, 4) || !aligned(status_dev, 4)) return HORA_ERR_INVALID_ARG;
     rc = packed_workspace(a, false, workspace, workspace_bytes);
     if (rc != HORA_OK) return rc;
     a.out = out;
@@ -423,7 +425,7 @@ extern "C" hora_status_t hora_packed_attention_backward(const void *q, const voi
     PackedArgs a = {};
     hora_status_t rc = packed_begin(a, q, k, v, dtype, q_row_stride, k_row_stride, v_row_stride, T, seq_offsets, S, group_offsets, N, Hq, Hkv, D, sm_scale, causal);
     if (rc != HORA_OK || T == 0 || S == 0) return rc;
-    if (lse == nullptr || !packed_rows(out, out_row_stride, Hq, D) || !packed_rows(dout, dout_row_stride, Hq, D) || !packed_rows(dq, dq_row_stride, Hq, D) ||
+    if (lse == nullptr || !aligned(lse, 4) || !aligned(status_dev, 4) || !packed_rows(out, out_row_stride, Hq, D) || !packed_rows(dout, dout_row_stride, Hq, D) || !packed_rows(dq, dq_row_stride, Hq, D) ||
         !packed_rows(dk, dk_row_stride, Hkv, D) || !packed_rows(dv, dv_row_stride, Hkv, D))
         return HORA_ERR_INVALID_ARG;
     rc = packed_workspace(a, true, workspace, workspace_bytes);

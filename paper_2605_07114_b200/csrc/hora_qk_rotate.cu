@@ -313,6 +313,12 @@ static bool rotate_ok(int32_t dtype, int64_t n, int32_t Hq, int32_t Hk, int32_t 
     return eps >= 0.f && eps <= 1e30f;
 }
 
+static bool tables_ok(const int32_t *positions, const double *inv_freq, int32_t rot, const float *q_weight, const float *k_weight) {
+    if (rot > 0 && (positions == nullptr || inv_freq == nullptr)) return false;
+    return !(reinterpret_cast<uintptr_t>(inv_freq) & 7u) &&
+           !((reinterpret_cast<uintptr_t>(positions) | reinterpret_cast<uintptr_t>(q_weight) | reinterpret_cast<uintptr_t>(k_weight)) & 3u);
+}
+
 // How the work is cut: whole tokens while there are enough of them, else a few heads to a unit.
 static int units_of(RotateArgs &a, int64_t n, int32_t Hq, int32_t Hk, int32_t D) {
     a.Hq = Hq;
@@ -347,7 +353,7 @@ extern "C" hora_status_t hora_qk_rotate(const void *q, const void *k, int32_t dt
     if (n_tokens == 0) return HORA_OK;
     const int32_t size = dtype_bytes(dtype);
     if (!rows_ok(q, q_row_stride, Hq, D, size) || !rows_ok(k, k_row_stride, Hk, D, size) || !rows_ok(q_out, q_out_row_stride, Hq, D, size) ||
-        !rows_ok(k_out, k_out_row_stride, Hk, D, size) || (rot > 0 && (positions == nullptr || inv_freq == nullptr)))
+        !rows_ok(k_out, k_out_row_stride, Hk, D, size) || !tables_ok(positions, inv_freq, rot, q_weight, k_weight))
         return HORA_ERR_INVALID_ARG;
     RotateArgs a = {};
     a.x[0] = q; a.x[1] = k;
@@ -383,7 +389,8 @@ extern "C" hora_status_t hora_qk_rotate_backward(const void *dq_out, const void 
             !rows_ok(dq, dq_row_stride, Hq, D, size) || !rows_ok(dk, dk_row_stride, Hk, D, size))
             return HORA_ERR_INVALID_ARG;
         if ((q_weight != nullptr && !rows_ok(q, q_row_stride, Hq, D, size)) || (k_weight != nullptr && !rows_ok(k, k_row_stride, Hk, D, size)) ||
-            (rot > 0 && (positions == nullptr || inv_freq == nullptr)))
+            !tables_ok(positions, inv_freq, rot, q_weight, k_weight) ||
+            ((reinterpret_cast<uintptr_t>(dq_weight) | reinterpret_cast<uintptr_t>(dk_weight)) & 3u))
             return HORA_ERR_INVALID_ARG;
     }
     const bool weights = dq_weight != nullptr || dk_weight != nullptr;

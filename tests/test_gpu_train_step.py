@@ -216,6 +216,23 @@ def test_rows_far_apart(n):
     assert torch.equal(dq, near[0]) and torch.equal(dk, near[1])
 
 
+def test_nothing_to_do():
+    from paper_2605_07114_b200 import hora
+    for T, off in ((0, [0]), (0, [0, 0, 0]), (40, [0]), (40, [17, 17, 17])):
+        x = tpa.inputs(T, 4, 2, 64, BF, 26)
+        got, status = tpa.run(*x, off)
+        assert status == 0 and all(bool((t == -7).all()) for t in got.values())
+
+
+def test_overlapping_sequences_write_nothing_else():
+    """Offsets that are not in order, with keys under so many queries that they are cut into parts: reported, and what is behind the tokens stays."""
+    T = 2000
+    x = tpa.inputs(T, 8, 2, 64, BF, 27)
+    for off in ([0, T] * 40, [0, T, 0, 700, 0, T, 0, T, 100, T]):
+        got, status = tpa.run(*x, off)
+        assert status == 2
+
+
 def test_thousands_of_short_sequences_and_groups():
     off = tpa.offsets([1 + i % 3 for i in range(5000)])
     x = tpa.inputs(off[-1], 2, 1, 64, BF, 22)

@@ -29,7 +29,7 @@ ROTATE_BAD = [dict(n=-1), dict(n=1 << 31), dict(Hq=-1), dict(Hk=-1), dict(Hq=0, 
 
 @pytest.mark.parametrize("over", ROTATE_BAD + [
     dict(q=None), dict(k=None), dict(qo=None), dict(ko=None), dict(q=P + 8), dict(k=P + 2), dict(qo=P + 4), dict(ko=P + 8), dict(qs=1023), dict(qs=1028), dict(ks=248),
-    dict(qos=1020), dict(kos=260), dict(pos=None), dict(f=None),
+    dict(qos=1020), dict(kos=260), dict(pos=None), dict(f=None), dict(f=P + 4), dict(pos=P + 2), dict(wq=P + 1), dict(wk=P + 2),
 ])
 def test_rotate(lib, over):
     assert rotate(lib, **over) == INVALID
@@ -49,7 +49,7 @@ def rotate_backward(lib, **over):
 
 @pytest.mark.parametrize("over", ROTATE_BAD + [
     dict(gq=None), dict(gk=None), dict(dq=None), dict(dk=None), dict(q=None), dict(k=None), dict(gq=P + 8), dict(dk=P + 2), dict(q=P + 4), dict(gqs=1016), dict(dks=252),
-    dict(qs=1030), dict(pos=None), dict(f=None), dict(wq=None), dict(wk=None),
+    dict(qs=1030), dict(pos=None), dict(f=None), dict(wq=None), dict(wk=None), dict(f=P + 4), dict(dwq=P + 2), dict(dwk=P + 1),
 ])
 def test_rotate_backward(lib, over):
     assert rotate_backward(lib, **over) == INVALID
@@ -82,7 +82,7 @@ ATTENTION_BAD = [
     dict(T=-1), dict(T=1 << 31), dict(S=-1), dict(S=1 << 30), dict(N=-1), dict(N=5), dict(N=0), dict(go=None), dict(Hq=0), dict(Hkv=0), dict(Hq=7), dict(Hq=1 << 17), dict(D=96),
     dict(D=256), dict(dt=F32), dict(dt=E4M3), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")), dict(scale=float("inf")), dict(causal=2), dict(causal=-1),
     dict(q=None), dict(k=None), dict(v=None), dict(so=None), dict(out=None), dict(q=P + 8), dict(k=P + 2), dict(v=P + 4), dict(out=P + 8), dict(qs=1023), dict(qs=1028), dict(ks=248), dict(vs=252),
-    dict(os=1020), dict(os=1000),
+    dict(os=1020), dict(os=1000), dict(so=P + 4), dict(go=P + 2), dict(lse=P + 2),
 ]
 
 
