@@ -7,7 +7,8 @@
 // other value of a pair (i, i + rot/2) one more.  Such a group of lanes takes one token and several of its heads, one after the other: the
 // angles are worked out once for all of them, in 64 bits up to the fraction of a turn (a position of 10^5 times a frequency of 1
 // has lost 2^-8 of a radian in 32 bits), the weights are held in registers, and four heads' loads are in flight.
-//   What bounds it: HBM.  Nothing is read twice and nothing but the results is written.
+//   What bounds it: HBM and issue slots, about equally.  Nothing is read twice and nothing but the results is written: 131072 tokens of 20 heads of 128 in
+// bf16 254 us, 5.3 TB/s (0.81 of the copy rate), 50021 tokens of 32 heads and back 396 us, 5.2 TB/s, seven of ten cycles issuing.
 #define HORA_FILE_ID 8
 #include "hora_rows16.cuh"
 
