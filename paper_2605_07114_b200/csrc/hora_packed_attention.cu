@@ -199,9 +199,8 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
     __syncthreads();
 }
 
-__global__ void __launch_bounds__(kListThreads)
-packed_plan_kernel(const PackedArgs a) {
-    pdl_enter();
+// Block 0 lists the queries' items, block 1 the keys'.
+__device__ __forceinline__ void packed_plan(const PackedArgs &a) {
     __shared__ int64_t s_groups[kListOffsets];
     __shared__ int32_t s_bucket[kListBuckets], s_warp[kListWarps];
     bool bad = false;
@@ -213,7 +212,7 @@ packed_plan_kernel(const PackedArgs a) {
         }
         if (threadIdx.x == 0 && (__ldcg(a.group_offsets) != 0 || __ldcg(a.group_offsets + a.N) + a.N != a.S)) bad = true;
     }
-    if (blockIdx.x == 0 && threadIdx.x < 4) a.counts[2 + threadIdx.x] = 0;
+    if (blockIdx.x == 0 && threadIdx.x < 2) a.counts[4 + threadIdx.x] = 0;
     __syncthreads();
     // a CTA to each list
     if (blockIdx.x == 0) list_items<false>(a, s_groups, s_bucket, s_warp, bad);
@@ -221,19 +220,23 @@ packed_plan_kernel(const PackedArgs a) {
     if (bad) raise_status(a.status, HORA_ERR_INVALID_VALUE);
 }
 
+__global__ void __launch_bounds__(kListThreads)
+packed_plan_kernel(const PackedArgs a) {
+    pdl_enter();
+    packed_plan(a);
+}
+
 // Of every row (token, head) lse in units of log2 and dout . out, and for fp16 the largest |dout row|^2 and |v row|^2.
 template <typename T, int D>
-__global__ void __launch_bounds__(256)
-packed_stats_kernel(const PackedArgs a) {
-    pdl_enter();
-    constexpr int kLanes = D / 8, kGroups = 256 / kLanes, kRows = 4;
+__device__ __forceinline__ void packed_row_stats(const PackedArgs &a, int32_t cta, int32_t ctas) {
+    constexpr int kLanes = D / 8, kGroups = kListThreads / kLanes, kRows = 4;
     const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
     const int32_t first = packed_offset(a, 0), tokens = max(0, packed_offset(a, a.S) - first);
     const int64_t rows = (int64_t)tokens * a.Hq, v_rows = a.half ? (int64_t)tokens * a.Hkv : 0;
     float most_d = 0.f, most_v = 0.f;
-    const int64_t stride = (int64_t)gridDim.x * kGroups;
+    const int64_t stride = (int64_t)ctas * kGroups;
     // a row's token and head, taken along without divisions
-    const int64_t start = (int64_t)blockIdx.x * kGroups + group;
+    const int64_t start = (int64_t)cta * kGroups + group;
     int64_t token = first + start / a.Hq;
     int32_t head = (int32_t)(start % a.Hq);
     const int32_t step_tokens = (int32_t)(stride / a.Hq), step_heads = (int32_t)(stride % a.Hq);
@@ -277,7 +280,7 @@ packed_stats_kernel(const PackedArgs a) {
             if (lane == 0 && at[i] >= 0) *reinterpret_cast<float2 *>(a.stats + at[i]) = make_float2(__ldcg(a.lse + at[i]) * kLog2e, dot);
         }
     }
-    for (int64_t x = (int64_t)blockIdx.x * kGroups + group; __any_sync(kFull, x < v_rows); x += stride) {
+    for (int64_t x = (int64_t)cta * kGroups + group; __any_sync(kFull, x < v_rows); x += stride) {
         Raw8<T> v;
         zero8(v);
         if (x < v_rows) load8(v, static_cast<const T *>(a.v) + (first + x / a.Hkv) * a.v_stride + x % a.Hkv * D + lane * 8);
@@ -293,6 +296,15 @@ packed_stats_kernel(const PackedArgs a) {
         atomicMax(a.counts + 2, __float_as_int(most_d));
         atomicMax(a.counts + 3, __float_as_int(most_v));
     }
+}
+
+// The backward pass's first kernel: two CTAs for the plan, beside them the rows' statistics.
+template <typename T, int D>
+__global__ void __launch_bounds__(kListThreads)
+packed_begin_kernel(const PackedArgs a) {
+    pdl_enter();
+    if (blockIdx.x < 2) packed_plan(a);
+    else packed_row_stats<T, D>(a, blockIdx.x - 2, gridDim.x - 2);
 }
 
 // Heads of a tile: the most that divide g and leave no more than eight of the 128 rows idle (one head always does).
@@ -348,15 +360,17 @@ static bool packed_rows(const void *p, int64_t stride, int32_t H, int32_t D) {
 }
 
 static hora_status_t launch_packed_plan(const PackedArgs &a, cudaStream_t stream) {
-    const cudaError_t e = launch_pdl(packed_plan_kernel, a.key_items != nullptr ? 2 : 1, kListThreads, 0, stream, a);
+    const cudaError_t e = launch_pdl(packed_plan_kernel, 1, kListThreads, 0, stream, a);
     count_launches(1);
     return cuda_ok(e);
 }
 
 template <typename T>
-static hora_status_t launch_packed_stats(const PackedArgs &a, cudaStream_t stream) {
-    const int grid = clamp_grid((int64_t)a.T * a.Hq * a.D / (256 * 8 * 4) + 1, 8);
-    const cudaError_t e = a.D == 128 ? launch_pdl(packed_stats_kernel<T, 128>, grid, 256, 0, stream, a) : launch_pdl(packed_stats_kernel<T, 64>, grid, 256, 0, stream, a);
+static hora_status_t launch_packed_begin(const PackedArgs &a, cudaStream_t stream) {
+    cudaError_t e = cudaSuccess;
+    if (a.half) e = cudaMemsetAsync(a.counts + 2, 0, 8, stream);         // the largest rows so far
+    const int grid = 2 + clamp_grid((int64_t)a.T * a.Hq * a.D / (kListThreads * 8 * 4) + 1, 1);
+    if (e == cudaSuccess) e = a.D == 128 ? launch_pdl(packed_begin_kernel<T, 128>, grid, kListThreads, 0, stream, a) : launch_pdl(packed_begin_kernel<T, 64>, grid, kListThreads, 0, stream, a);
     count_launches(1);
     return cuda_ok(e);
 }
@@ -443,7 +457,6 @@ extern "C" hora_status_t hora_packed_attention_backward(const void *q, const voi
     a.dv_stride = dv_row_stride;
     a.status = status_dev;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    rc = launch_packed_plan(a, s);
-    if (rc == HORA_OK) rc = dtype == HORA_DTYPE_BF16 ? launch_packed_stats<__nv_bfloat16>(a, s) : launch_packed_stats<__half>(a, s);
+    rc = dtype == HORA_DTYPE_BF16 ? launch_packed_begin<__nv_bfloat16>(a, s) : launch_packed_begin<__half>(a, s);
     return rc == HORA_OK ? launch_packed_backward(a, q, k, v, q_row_stride, dtype, s) : rc;
 }

@@ -443,17 +443,22 @@ packed_keys_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_map
 #pragma unroll 1
                     for (int b = 0; b < D / 16; ++b) {
                         float4 sum[4] = {};
-                        for (int32_t x = 0; x < it.parts; ++x) {
-                            float4 y[4];
+                        for (int32_t x = 0; x < it.parts; x += 4) {          // sixteen loads in flight
+                            float4 y[4][4];
 #pragma unroll
-                            for (int v = 0; v < 4; ++v) y[v] = __ldcg(from + x * step * (D / 4 * kTile) + (b * 4 + v) * kTile);
+                            for (int u = 0; u < 4; ++u)
 #pragma unroll
-                            for (int v = 0; v < 4; ++v) {
-                                sum[v].x += y[v].x;
-                                sum[v].y += y[v].y;
-                                sum[v].z += y[v].z;
-                                sum[v].w += y[v].w;
-                            }
+                                for (int v = 0; v < 4; ++v)
+                                    y[u][v] = x + u < it.parts ? __ldcg(from + (x + u) * step * (D / 4 * kTile) + (b * 4 + v) * kTile) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                                for (int v = 0; v < 4; ++v) {
+                                    sum[v].x += y[u][v].x;
+                                    sum[v].y += y[u][v].y;
+                                    sum[v].z += y[u][v].z;
+                                    sum[v].w += y[u][v].w;
+                                }
                         }
                         if (row < it.keys && HORA_IN(it.key0 + row, a.T)) {
 #pragma unroll
