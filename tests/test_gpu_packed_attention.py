@@ -74,6 +74,9 @@ SHAPES = [
     ([130, 259], 28, 1, 128, HF, True),
     ([1500], 8, 1, 128, BF, True),
     ([1333, 700], 3, 3, 64, BF, False),
+    ([70, 2], 128, 1, 64, BF, True),
+    ([130, 40], 200, 1, 128, HF, True),
+    ([95, 300], 48, 1, 128, BF, False),
 ]
 
 
