@@ -680,21 +680,23 @@ class QkRotation:
         self._streams = set()
         _, freq, rot, wq, wk = _rotation(torch.empty(0, dtype=torch.int32, device=first.device), inv_freq, q_weight, k_weight, 0, D)
         _one_device(first, inv_freq, q_weight, k_weight)
-        self._middle, self._device = (freq, rot, layout, wq, wk, float(eps)), first.get_device()
+        # as ctypes values, which cost the call half of what Python's do
+        self._middle = (C.c_void_p(freq), C.c_int32(rot), C.c_int32(layout), C.c_void_p(wq), C.c_void_p(wk), C.c_float(eps))
+        self._D, self._device = C.c_int32(D), first.get_device()
 
     def _usual(self, q, k, positions, q_out, k_out):
         """The usual call, marshalled in few steps: both sides, heads next to each other, everything on the object's device, which is the
         current one.  False: it is not that."""
         D, dev, qs, ks, os, ps = self.D, self._device, q.stride(), k.stride(), q_out.stride(), k_out.stride()
-        n, dtype = q.shape[0], q.dtype
-        if not (n > 1 and len(qs) == len(ks) == 3 and qs[1:] == ks[1:] == os[1:] == ps[1:] == (D, 1) and q.shape == q_out.shape and k.shape == k_out.shape
-                and k.shape[0] == n and q.shape[2] == k.shape[2] == D and dtype == k.dtype == q_out.dtype == k_out.dtype and dtype in _DTYPES
+        q_shape, k_shape, dtype = q.shape, k.shape, q.dtype
+        n = q_shape[0] if len(qs) == len(ks) == 3 else 0
+        if not (n > 1 and qs[1:] == ks[1:] == os[1:] == ps[1:] == (D, 1) and q_shape == q_out.shape and k_shape == k_out.shape
+                and k_shape[0] == n and q_shape[2] == k_shape[2] == D and dtype == k.dtype == q_out.dtype == k_out.dtype and dtype in _DTYPES
                 and positions.dtype == torch.int32 and positions.shape == (n,) and positions.is_contiguous()
                 and q.get_device() == k.get_device() == q_out.get_device() == k_out.get_device() == positions.get_device() == dev == torch.cuda.current_device()):
             return False
-        freq, rot, layout, wq, wk, eps = self._middle
-        _check(load().hora_qk_rotate(q.data_ptr(), k.data_ptr(), _DTYPES[dtype], qs[0], ks[0], n, q.shape[1], k.shape[1], D, positions.data_ptr(), freq, rot, layout,
-                                     wq, wk, eps, q_out.data_ptr(), k_out.data_ptr(), os[0], ps[0], torch._C._cuda_getCurrentRawStream(dev)), "hora_qk_rotate")
+        _check(load().hora_qk_rotate(q.data_ptr(), k.data_ptr(), _DTYPES[dtype], qs[0], ks[0], n, q_shape[1], k_shape[1], self._D, positions.data_ptr(), *self._middle,
+                                     q_out.data_ptr(), k_out.data_ptr(), os[0], ps[0], torch._C._cuda_getCurrentRawStream(dev)), "hora_qk_rotate")
         return True
 
     def run(self, q, k, positions, q_out=None, k_out=None):
@@ -795,9 +797,11 @@ class PackedAttention:
         _one_device(seq_offsets, group_offsets, status_dev, self.workspace)
         N = 0 if group_offsets is None else group_offsets.numel() - 1
         self._shape, self._dtype, self._device, self._code = (T, Hq, Hkv, D), dtype, seq_offsets.get_device(), _DTYPES[dtype]
-        self._middle = (T, _at(seq_offsets, torch.int64, "seq_offsets"), S, _at(group_offsets, torch.int64, "group_offsets"), N, Hq, Hkv, D, float(self.sm_scale), int(causal))
-        self._lse = self.lse.data_ptr()
-        self._tail = (_at(status_dev, torch.int32, "status_dev"), self.workspace.data_ptr(), self.workspace.numel())
+        i32, i64, p = C.c_int32, C.c_int64, C.c_void_p                      # as ctypes values, which cost the call half of what Python's do
+        self._middle = (i64(T), p(_at(seq_offsets, torch.int64, "seq_offsets")), i64(S), p(_at(group_offsets, torch.int64, "group_offsets")), i64(N), i32(Hq), i32(Hkv),
+                        i32(D), C.c_float(self.sm_scale), i32(int(causal)))
+        self._lse = p(self.lse.data_ptr())
+        self._tail = (p(_at(status_dev, torch.int32, "status_dev")), p(self.workspace.data_ptr()), C.c_size_t(self.workspace.numel()))
 
     def _strides(self, dtype, of_queries, of_keys):
         """Token strides of tensors [T, Hq, D] and [T, Hkv, D] in the usual places, in few steps; None: something is not usual."""
