@@ -133,8 +133,10 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
         for (int d = kWarp / 2; d > 0; d >>= 1) mine += __shfl_xor_sync(kFull, mine, d);
         if (lane == 0) s_sum[warp] = mine;
         __syncthreads();
-        int64_t all = 0;
-        for (int w = 0; w < kListWarps; ++w) all += s_sum[w];
+        static_assert(kListWarps == kWarp, "a lane to each warp's sum");
+        int64_t all = s_sum[lane];
+#pragma unroll
+        for (int d = kWarp / 2; d > 0; d >>= 1) all += __shfl_xor_sync(kFull, all, d);
         const int64_t per = (all * a.Hkv + a.n_sm - 1) / a.n_sm;
         most = (int32_t)min((int64_t)0x7FFFFFFF, max((int64_t)(kPartSteps * a.hp + a.g - 1) / a.g, per));
         for (int i = threadIdx.x; i < 8 * a.n_sm; i += kListThreads) a.tickets[i] = 0;
@@ -158,10 +160,11 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
     }
     if (lane == kWarp - 1) s_warp[warp] = upto;
     __syncthreads();
-    int32_t before = 0, all = 0;
-    for (int w = 0; w < kListWarps; ++w) {
-        if (w < warp) before += s_warp[w];
-        all += s_warp[w];
+    int32_t all = s_warp[lane], before = lane < warp ? all : 0;              // a lane to each warp's sum
+#pragma unroll
+    for (int d = kWarp / 2; d > 0; d >>= 1) {
+        before += __shfl_xor_sync(kFull, before, d);
+        all += __shfl_xor_sync(kFull, all, d);
     }
     s_bucket[threadIdx.x] = before + upto - mine;
     const int32_t cap = KEYS ? a.key_cap : a.query_cap;
