@@ -573,7 +573,8 @@ hora_status_t hora_qk_rotate_backward(const void *dq_out, const void *dk_out, in
  *   out          like q, out_row_stride;  lse [T, Hq] fp32 or NULL
  *   workspace    hora_packed_attention_workspace_bytes(T, S, Hq, Hkv, D, 0) bytes, 256-byte aligned, contents undefined on entry and exit
  *   status_dev   optional: INVALID_VALUE for offsets that decrease or leave [0, T] and group_offsets that do not fit.  Such values are
- *                clamped: outputs they touch are wrong, nothing else is read or written.
+ *                clamped: outputs they touch are wrong (and left as they were where sequences overlap so much that the workspace does not hold
+ *                their tiles), nothing else is read or written.
  * out must not overlap q, k or v.  T == 0 or S == 0 is a no-op.  Limits: T < 2^31 - 256, S < 2^30, Hq <= 65536.
  *
  * hora_packed_attention_backward — the gradients, for what hora_packed_attention was given and left:

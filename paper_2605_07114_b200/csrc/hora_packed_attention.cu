@@ -80,8 +80,9 @@ __device__ __forceinline__ int32_t bucket_of(int32_t steps) {
 }
 
 // f(sequence, item) for all items of 32 * each sequences of a warp's lanes: the items are dealt to the lanes whatever sequence they are of.
+// `left`: how many more the warp may take; false, and none taken, where there are more.
 template <bool KEYS, typename F>
-__device__ __forceinline__ void for_items(const PackedArgs &a, const PackedSequence &mine, F f) {
+__device__ __forceinline__ bool for_items(const PackedArgs &a, const PackedSequence &mine, int64_t &left, F f) {
     const int lane = lane_id();
     const int32_t n = items_of<KEYS>(a, mine);
     int64_t upto = n;
@@ -91,6 +92,8 @@ __device__ __forceinline__ void for_items(const PackedArgs &a, const PackedSeque
         if (lane >= d) upto += o;
     }
     const int64_t all = __shfl_sync(kFull, upto, kWarp - 1);
+    if (all > left) return false;
+    left -= all;
     for (int64_t base = 0; base < all; base += kWarp) {
         const int64_t x = base + lane;
         int at = 0;                                      // the first lane whose items reach beyond x
@@ -109,12 +112,16 @@ __device__ __forceinline__ void for_items(const PackedArgs &a, const PackedSeque
         q.seen_to = __shfl_sync(kFull, mine.seen_to, at);
         if (x < all) f(q, (int32_t)(x - first));
     }
+    return true;
 }
 
 // Lists of items, those with most steps first.  Which of two with about the same number comes first may differ from run to run; results do not.
+// Sequences that follow one another have no more items than there are places.  Offsets that are not in order make sequences that overlap, and any
+// number of items up to S T: each warp counts its own in 64 bits and stops once they are more than the places, so that neither the counts nor the time
+// depend on how many more; the list is then left empty.
 template <bool KEYS>
 __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s_groups, int32_t *s_bucket, int32_t *s_warp, bool &bad) {
-    __shared__ int64_t s_sum[kListWarps];
+    __shared__ int64_t s_sum[kListWarps], s_items[kListWarps];
     __shared__ int32_t s_next[2];
     const int warp = threadIdx.x >> 5, lane = lane_id();
     const int32_t each = min((int32_t)kWarp, (a.S + kListWarps - 1) / kListWarps);               // sequences of a warp at a time
@@ -122,18 +129,32 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
     for (int i = threadIdx.x; i < kListBuckets; i += kListThreads) s_bucket[i] = 0;
     __syncthreads();
     PackedSequence kept = {0, 0, 0, 0, 0};
+    const int32_t cap = KEYS ? a.key_cap : a.query_cap;
+    int64_t left = cap;
+    bool fits = true;
+    auto too_many = [&]() {                              // of all warps together, after a barrier; empties the list
+        int64_t all = s_items[lane];
+#pragma unroll
+        for (int d = kWarp / 2; d > 0; d >>= 1) all += __shfl_xor_sync(kFull, all, d);
+        if (all <= cap) return false;
+        if (threadIdx.x == 0) a.counts[KEYS ? 1 : 0] = 0;
+        bad = true;
+        return true;
+    };
     int32_t most = 0x7FFFFFFF;
     if constexpr (KEYS) {
         int64_t mine = 0;
-        for (int64_t base = (int64_t)warp * each; base < a.S; base += (int64_t)kListWarps * each) {
+        for (int64_t base = (int64_t)warp * each; base < a.S && fits; base += (int64_t)kListWarps * each) {
             kept = lane < each ? packed_sequence(a, s_groups, (int32_t)min((int64_t)a.S, base + lane), bad) : PackedSequence{0, 0, 0, 0, 0};
-            for_items<true>(a, kept, [&](const PackedSequence &s, int32_t i) { mine += item_steps<true>(a, s, i); });
+            fits = for_items<true>(a, kept, left, [&](const PackedSequence &s, int32_t i) { mine += item_steps<true>(a, s, i); });
         }
+        if (lane == 0) s_items[warp] = fits ? cap - left : (int64_t)cap + 1;
 #pragma unroll
         for (int d = kWarp / 2; d > 0; d >>= 1) mine += __shfl_xor_sync(kFull, mine, d);
         if (lane == 0) s_sum[warp] = mine;
         __syncthreads();
         static_assert(kListWarps == kWarp, "a lane to each warp's sum");
+        if (too_many()) return;
         int64_t all = s_sum[lane];
 #pragma unroll
         for (int d = kWarp / 2; d > 0; d >>= 1) all += __shfl_xor_sync(kFull, all, d);
@@ -141,15 +162,18 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
         most = (int32_t)min((int64_t)0x7FFFFFFF, max((int64_t)(kPartSteps * a.hp + a.g - 1) / a.g, per));
         for (int i = threadIdx.x; i < 8 * a.n_sm; i += kListThreads) a.tickets[i] = 0;
         if (threadIdx.x == 0) s_next[0] = s_next[1] = 0;
+        left = cap;
     }
-    for (int64_t base = (int64_t)warp * each; base < a.S; base += (int64_t)kListWarps * each) {
+    for (int64_t base = (int64_t)warp * each; base < a.S && fits; base += (int64_t)kListWarps * each) {
         if (!KEYS || !once) kept = lane < each ? packed_sequence(a, s_groups, (int32_t)min((int64_t)a.S, base + lane), bad) : PackedSequence{0, 0, 0, 0, 0};
-        for_items<KEYS>(a, kept, [&](const PackedSequence &s, int32_t i) {
+        fits = for_items<KEYS>(a, kept, left, [&](const PackedSequence &s, int32_t i) {
             const int32_t steps = item_steps<KEYS>(a, s, i), parts = KEYS ? parts_of(steps, most) : 1;
             atomicAdd(s_bucket + bucket_of((steps + parts - 1) / parts), parts);
         });
     }
+    if (!KEYS && lane == 0) s_items[warp] = fits ? cap - left : (int64_t)cap + 1;
     __syncthreads();
+    if (!KEYS && too_many()) return;
     static_assert(kListBuckets == kListThreads, "a thread to each bucket");
     const int32_t mine = s_bucket[threadIdx.x];
     int32_t upto = mine;
@@ -167,13 +191,16 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
         all += __shfl_xor_sync(kFull, all, d);
     }
     s_bucket[threadIdx.x] = before + upto - mine;
-    const int32_t cap = KEYS ? a.key_cap : a.query_cap;
-    if (threadIdx.x == 0) a.counts[KEYS ? 1 : 0] = min(all, cap);
-    if (all > cap) bad = true;                           // offsets that are not in order: sequences that overlap
+    // keys: parts are at most 2 n_sm more than items, so 32 bits hold them, but they too can be more than the places where sequences overlap
+    const bool full = all > cap;
+    if (full) bad = true;
+    if (threadIdx.x == 0) a.counts[KEYS ? 1 : 0] = full ? 0 : all;
+    if (full) return;
     __syncthreads();
+    left = cap;
     for (int64_t base = (int64_t)warp * each; base < a.S; base += (int64_t)kListWarps * each) {
         const PackedSequence q = once ? kept : lane < each ? packed_sequence(a, s_groups, (int32_t)min((int64_t)a.S, base + lane), bad) : PackedSequence{0, 0, 0, 0, 0};
-        for_items<KEYS>(a, q, [&](const PackedSequence &s, int32_t i) {
+        for_items<KEYS>(a, q, left, [&](const PackedSequence &s, int32_t i) {
             const int32_t steps = item_steps<KEYS>(a, s, i), parts = KEYS ? parts_of(steps, most) : 1, part_steps = (steps + parts - 1) / parts;
             const int32_t to = atomicAdd(s_bucket + bucket_of(part_steps), parts);
             if constexpr (KEYS) {
@@ -184,14 +211,14 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
                     ticket = atomicAdd(s_next + 1, 1);
                 }
                 int4 *item = reinterpret_cast<int4 *>(a.key_items + to);
-                for (int32_t p = 0; p < parts && to + p < cap; ++p) {
+                for (int32_t p = 0; p < parts && HORA_IN(to + p, cap); ++p) {
                     const int64_t from = q0 + (int64_t)p * part_steps * a.tp;
                     item[2 * p] = make_int4(key0, min(kPackedRows, s.hi - key0), (int32_t)min((int64_t)s.seen_to, from),
                                             (int32_t)min((int64_t)s.seen_to, from + (int64_t)part_steps * a.tp));
                     item[2 * p + 1] = make_int4(slot0, parts, p, ticket);
                 }
             } else {
-                if (to >= cap) return;
+                if (!HORA_IN(to, cap)) return;
                 const int32_t token0 = s.lo + i * a.tile_tokens;
                 int4 *item = reinterpret_cast<int4 *>(a.query_items + to);
                 item[0] = make_int4(token0, min(a.tile_tokens, s.hi - token0), s.lo, s.hi);
