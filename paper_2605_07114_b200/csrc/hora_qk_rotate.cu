@@ -155,6 +155,8 @@ struct Side {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) sum += z[e] * z[e];
                     r = rsqrtf(group_sum<kLanes>(sum) * (1.f / D) + eps);
+                    // lanes with no head left hold zeros, whose r is infinite where eps is 0: infinity times zero would be in dw
+                    if (BACKWARD && h + i >= to) r = 0.f;
                 }
                 if constexpr (!BACKWARD) {
                     others8<T, PAIRS>(now_x[i], z, source, p);
