@@ -561,7 +561,9 @@ hora_status_t hora_qk_rotate_backward(const void *dq_out, const void *dk_out, in
  * keys' and values' gradients are summed over the group.  causal = 1: of its own sequence a query sees itself and what is before it; 0: all of it.
  * For each head
  *   s_j = sm_scale * q . k_j,   out = sum_j e^(s_j) v_j / sum_j e^(s_j),   lse = log sum_j e^(s_j)
- * Scores, maxima, sums and outputs are held in fp32; the weights are rounded to the 16-bit type of the product they enter.
+ * Scores, maxima, sums and outputs are held in fp32; the weights are rounded to the 16-bit type of the product they enter, in F16 held times 2^7
+ * relative to the largest (a weight below 2^-32 of it is lost).  An fp32 score of the magnitude 2^n is off by 2^(n-24) and its weight by e to
+ * that: scores are meant to stay below 2^20.
  *
  *   q            token t at q + t * q_row_stride (elements), heads next to each other: [Hq, D], BF16 or F16; query head h reads head h / (Hq/Hkv)
  *                of k, v, token t at k + t * k_row_stride, v + t * v_row_stride: [Hkv, D], of the same type.  D = 64 or 128.  All 16-byte aligned, row strides at least

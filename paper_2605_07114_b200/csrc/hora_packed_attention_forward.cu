@@ -1,6 +1,6 @@
 // hora_packed_attention: the forward kernel.
 //
-// Per row: m the running maximum of s = scale q.k (in units of log2), l = sum 2^(s - m), o = sum 2^(s - m) v;  out = o / l,
+// Per row: m a reference near the running maximum of s = scale q.k (in units of log2), l = sum 2^(s - m), o = sum 2^(s - m) v;  out = o / l,
 // lse = m ln 2 + log l.  A CTA holds an SM and works on two tiles of 128 query rows at a time, which share the keys and values.
 // Each tile has four warps for its softmax, one thread to a row, and one that issues its products; one more warp brings in queries, keys and
 // values by TMA, and four read, norm and store outputs while the next item is under way.  S = Q K^T is accumulated in tensor memory, 64 keys
@@ -8,6 +8,10 @@
 // bits (rounded once, as the product needs them; sums are of the unrounded ones) and are the left operand of O += P V.
 //   O is scaled only when a row's maximum has grown by more than 2^8 (weights up to 256 are as exact as weights up to 1), after the product
 // before has been waited for.
+//   fp16 has only 2^-14 below 1 at full precision and nothing below 2^-25, where rows with one dominant key of little value live on their small
+// weights (a key 16 above the others' mean score among 16381: 6 % off).  There weights are held times 2^7, the most with which none passes 2^15: m is
+// that much below the maximum when it is set.  (2^10, as in the backward pass, leaves a maximum only 2^4 to grow by before O has to be scaled: 5 % more
+// time for scores of a deviation of 2.)  bf16 has fp32's exponents.
 //   Keys that are not of the sequence are in no row's sum; the product stops at the last sixteen that hold one of it, and values
 // of others among those are cleared in shared memory first, since 0 * NaN is not 0.
 //   The warps of a multiprocessor share its instruction cache, and those that issue the products wait for their instructions longest: the code is
@@ -82,6 +86,10 @@ __device__ __forceinline__ Item make_item(const PackedArgs &a, const FeedSlot &f
     return q;
 }
 
+// How far below a row's maximum its reference lies when it is set.
+template <typename Q>
+constexpr float kBelow = std::is_same<Q, __half>::value ? 7.f : 0.f;
+
 // A row's part in 64 keys: scores in tensor memory, of which the row sees `limit`, to weights there; `whole`: every row of the warp sees all.
 // `have`: the row is a token's; others may hold anything and have no say.  `first`: there is no output yet; else `before` tells that the product
 // before is in.
@@ -110,12 +118,14 @@ __device__ __forceinline__ bool softmax_step(uint32_t t_s, uint32_t t_o, float s
         top[b] = fmaxf(top[b], s[b][31]);
     }
     top[0] = fmaxf(top[0], top[1]) * scale_log2;
+    // beyond 2^22 differences of scores are rounded by so much that weights need the room themselves
+    const float below = kBelow<Q> > 0.f && fabsf(top[0]) < 4194304.f ? kBelow<Q> : 0.f;
     if (first) {
-        m = top[0];
-    } else if (__any_sync(kFull, have && top[0] > m + 8.f)) {
+        m = top[0] - below;
+    } else if (__any_sync(kFull, have && top[0] > m + (below + 8.f))) {
         if (!__all_sync(kFull, bar_wait(before, before_phase, failed))) return false;
         fence_after();
-        const float up = fmaxf(m, top[0]), f = up == -INFINITY ? 1.f : exp2_approx(m - up);
+        const float up = fmaxf(m, top[0] - below), f = up == -INFINITY ? 1.f : exp2_approx(m - up);
         l *= f;
         m = up;
 #pragma unroll 1
@@ -224,7 +234,8 @@ packed_forward_kernel(const PackedArgs a, const __grid_constant__ CUtensorMap q_
                 const float2 ml = sh.sums[t][row];
                 bar_arrive(sums_free + 8 * t);
                 const float inv = ml.y == 0.f ? 0.f : 1.f / ml.y;        // NaN where a score was NaN: it is in no maximum, but in the sum
-                if (have && ok && a.lse != nullptr) a.lse[(int64_t)token * a.Hq + head] = (ml.x == -INFINITY ? 0.f : kLn2 * ml.x) + logf(ml.y);
+                constexpr float kSum = std::is_same<Q, __half>::value ? 1.f / 128.f : 1.f;      // 2^-kBelow
+                if (have && ok && a.lse != nullptr) a.lse[(int64_t)token * a.Hq + head] = (ml.x == -INFINITY ? 0.f : kLn2 * (ml.x + kBelow<Q>)) + logf(ml.y * kSum);
                 ok = ok && bar_wait(output + 8 * t, phase >> t & 1, failed);
                 phase ^= 1u << t;
                 ok = __all_sync(kFull, ok);
