@@ -7,6 +7,7 @@ fallback: if the shared library is missing or a call fails, an exception is rais
 from __future__ import annotations
 
 import ctypes as C
+import operator
 import os
 from dataclasses import dataclass
 from typing import Optional
@@ -668,26 +669,34 @@ def hora_qk_rotate_backward(dq_out, dk_out, q, k, positions, inv_freq, dq, dk, d
            "hora_qk_rotate_backward")
 
 
+def _kept(name: str) -> property:
+    """What an object was made with, and holds the marshalled form of: to be read and written into, not exchanged."""
+    return property(operator.attrgetter("_" + name))
+
+
 class QkRotation:
-    """hora_qk_rotate with what stays from call to call: frequencies, head weights, and the backward pass's workspace."""
+    """hora_qk_rotate with what stays from call to call: frequencies, head weights, and the backward pass's workspace.  The tensors' contents may
+    change, the attributes may not."""
+
+    inv_freq, D, q_weight, k_weight, eps, layout, workspace = map(_kept, ("inv_freq", "D", "q_weight", "k_weight", "eps", "layout", "workspace"))
 
     def __init__(self, inv_freq, D: int, *, q_weight=None, k_weight=None, eps: float = 1e-6, layout: int = ROTATE_HALVES):
         first = next((t for t in (inv_freq, q_weight, k_weight) if t is not None), None)
         if first is None:
             raise ValueError("neither frequencies nor weights: there is nothing to do")
-        self.inv_freq, self.D, self.q_weight, self.k_weight, self.eps, self.layout = inv_freq, D, q_weight, k_weight, eps, layout
-        self.workspace = torch.empty(max(hora_qk_rotate_backward_workspace_bytes(D), 256), dtype=torch.uint8, device=first.device)
+        self._inv_freq, self._D, self._q_weight, self._k_weight, self._eps, self._layout = inv_freq, D, q_weight, k_weight, eps, layout
+        self._workspace = torch.empty(max(hora_qk_rotate_backward_workspace_bytes(D), 256), dtype=torch.uint8, device=first.device)
         self._streams = set()
         _, freq, rot, wq, wk = _rotation(torch.empty(0, dtype=torch.int32, device=first.device), inv_freq, q_weight, k_weight, 0, D)
         _one_device(first, inv_freq, q_weight, k_weight)
         # as ctypes values, which cost the call half of what Python's do
         self._middle = (C.c_void_p(freq), C.c_int32(rot), C.c_int32(layout), C.c_void_p(wq), C.c_void_p(wk), C.c_float(eps))
-        self._D, self._device = C.c_int32(D), first.get_device()
+        self._D_arg, self._device = C.c_int32(D), first.get_device()
 
     def _usual(self, q, k, positions, q_out, k_out):
         """The usual call, marshalled in few steps: both sides, heads next to each other, everything on the object's device, which is the
         current one.  False: it is not that."""
-        D, dev, qs, ks, os, ps = self.D, self._device, q.stride(), k.stride(), q_out.stride(), k_out.stride()
+        D, dev, qs, ks, os, ps = self._D, self._device, q.stride(), k.stride(), q_out.stride(), k_out.stride()
         q_shape, k_shape, dtype = q.shape, k.shape, q.dtype
         n = q_shape[0] if len(qs) == len(ks) == 3 else 0
         if not (n > 1 and qs[1:] == ks[1:] == os[1:] == ps[1:] == (D, 1) and q_shape == q_out.shape and k_shape == k_out.shape
@@ -695,7 +704,7 @@ class QkRotation:
                 and positions.dtype == torch.int32 and positions.shape == (n,) and positions.is_contiguous()
                 and q.get_device() == k.get_device() == q_out.get_device() == k_out.get_device() == positions.get_device() == dev == torch.cuda.current_device()):
             return False
-        _check(load().hora_qk_rotate(q.data_ptr(), k.data_ptr(), _DTYPES[dtype], qs[0], ks[0], n, q_shape[1], k_shape[1], self._D, positions.data_ptr(), *self._middle,
+        _check(load().hora_qk_rotate(q.data_ptr(), k.data_ptr(), _DTYPES[dtype], qs[0], ks[0], n, q_shape[1], k_shape[1], self._D_arg, positions.data_ptr(), *self._middle,
                                      q_out.data_ptr(), k_out.data_ptr(), os[0], ps[0], torch._C._cuda_getCurrentRawStream(dev)), "hora_qk_rotate")
         return True
 
@@ -707,7 +716,7 @@ class QkRotation:
             q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         if k is not None and k_out is None:
             k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-        hora_qk_rotate(q, k, positions, self.inv_freq, q_out, k_out, self.q_weight, self.k_weight, self.eps, self.layout)
+        hora_qk_rotate(q, k, positions, self._inv_freq, q_out, k_out, self._q_weight, self._k_weight, self._eps, self._layout)
         return q_out, k_out
 
     def backward(self, dq_out, dk_out, q, k, positions, dq=None, dk=None, dq_weight=None, dk_weight=None):
@@ -716,9 +725,9 @@ class QkRotation:
             dq = torch.empty(dq_out.shape, dtype=dq_out.dtype, device=dq_out.device)
         if dk_out is not None and dk is None:
             dk = torch.empty(dk_out.shape, dtype=dk_out.dtype, device=dk_out.device)
-        hora_qk_rotate_backward(dq_out, dk_out, q, k, positions, self.inv_freq, dq, dk, dq_weight, dk_weight, self.q_weight, self.k_weight, self.eps, self.layout,
-                                self.workspace)
-        _used_on(self, dq if dq is not None else dk, self.workspace)
+        hora_qk_rotate_backward(dq_out, dk_out, q, k, positions, self._inv_freq, dq, dk, dq_weight, dk_weight, self._q_weight, self._k_weight, self._eps, self._layout,
+                                self._workspace)
+        _used_on(self, dq if dq is not None else dk, self._workspace)
         return dq, dk
 
 
@@ -773,8 +782,11 @@ def hora_packed_attention_backward(q, k, v, out, lse, dout, seq_offsets, group_o
 
 
 class PackedAttention:
-    """hora_packed_attention over offsets that stay where they are (their contents may change): owns the workspace and, unless others are given,
-    the outputs, which the next call overwrites."""
+    """hora_packed_attention over offsets that stay where they are (their contents may change, the attributes may not): owns the workspace and,
+    unless others are given, the outputs, which the next call overwrites."""
+
+    seq_offsets, group_offsets, causal, status_dev, sm_scale, workspace, out, lse, dq, dk, dv = map(
+        _kept, ("seq_offsets", "group_offsets", "causal", "status_dev", "sm_scale", "workspace", "out", "lse", "dq", "dk", "dv"))
 
     def __init__(self, seq_offsets, T: int, Hq: int, Hkv: int, D: int, dtype, *, group_offsets=None, causal: bool = True, sm_scale: Optional[float] = None,
                  status_dev=None, backward: bool = False):
@@ -786,22 +798,22 @@ class PackedAttention:
         need = hora_packed_attention_workspace_bytes(T, S, Hq, Hkv, D, backward)
         if need == 0:
             raise ValueError(f"no such shape: {T} tokens in {S} sequences, {Hq} and {Hkv} heads of {D}")
-        self.seq_offsets, self.group_offsets, self.causal, self.status_dev = seq_offsets, group_offsets, causal, status_dev
-        self.sm_scale = D ** -0.5 if sm_scale is None else sm_scale
-        self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
+        self._seq_offsets, self._group_offsets, self._causal, self._status_dev = seq_offsets, group_offsets, causal, status_dev
+        self._sm_scale = D ** -0.5 if sm_scale is None else sm_scale
+        self._workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=dev)
         new = lambda h: torch.empty((T, h, D), dtype=dtype, device=dev)  # noqa: E731
-        self.out, self.lse = new(Hq), torch.empty((T, Hq), dtype=torch.float32, device=dev)
-        self.dq, self.dk, self.dv = (new(Hq), new(Hkv), new(Hkv)) if backward else (None, None, None)
+        self._out, self._lse = new(Hq), torch.empty((T, Hq), dtype=torch.float32, device=dev)
+        self._dq, self._dk, self._dv = (new(Hq), new(Hkv), new(Hkv)) if backward else (None, None, None)
         self._streams = set()
         # what does not change from call to call, marshalled once
-        _one_device(seq_offsets, group_offsets, status_dev, self.workspace)
+        _one_device(seq_offsets, group_offsets, status_dev, self._workspace)
         N = 0 if group_offsets is None else group_offsets.numel() - 1
         self._shape, self._dtype, self._device, self._code = (T, Hq, Hkv, D), dtype, seq_offsets.get_device(), _DTYPES[dtype]
         i32, i64, p = C.c_int32, C.c_int64, C.c_void_p                      # as ctypes values, which cost the call half of what Python's do
         self._middle = (i64(T), p(_at(seq_offsets, torch.int64, "seq_offsets")), i64(S), p(_at(group_offsets, torch.int64, "group_offsets")), i64(N), i32(Hq), i32(Hkv),
-                        i32(D), C.c_float(self.sm_scale), i32(int(causal)))
-        self._lse = p(self.lse.data_ptr())
-        self._tail = (p(_at(status_dev, torch.int32, "status_dev")), p(self.workspace.data_ptr()), C.c_size_t(self.workspace.numel()))
+                        i32(D), C.c_float(self._sm_scale), i32(int(causal)))
+        self._lse_arg = p(self._lse.data_ptr())
+        self._tail = (p(_at(status_dev, torch.int32, "status_dev")), p(self._workspace.data_ptr()), C.c_size_t(self._workspace.numel()))
 
     def _strides(self, dtype, of_queries, of_keys):
         """Token strides of tensors [T, Hq, D] and [T, Hkv, D] in the usual places, in few steps; None: something is not usual."""
@@ -818,30 +830,30 @@ class PackedAttention:
 
     def run(self, q, k, v, out=None, lse=None):
         """Returns (out, lse)."""
-        out, lse = self.out if out is None else out, self.lse if lse is None else lse
-        st = self._strides(q.dtype, (q, out), (k, v)) if lse is self.lse else None
+        out, lse = self._out if out is None else out, self._lse if lse is None else lse
+        st = self._strides(q.dtype, (q, out), (k, v)) if lse is self._lse else None
         if st is not None:
-            _check(load().hora_packed_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), self._code, st[0], st[2], st[3], *self._middle, out.data_ptr(), st[1], self._lse,
+            _check(load().hora_packed_attention(q.data_ptr(), k.data_ptr(), v.data_ptr(), self._code, st[0], st[2], st[3], *self._middle, out.data_ptr(), st[1], self._lse_arg,
                                                 *self._tail, torch._C._cuda_getCurrentRawStream(self._device)), "hora_packed_attention")
         else:
-            hora_packed_attention(q, k, v, self.seq_offsets, self.group_offsets, self.sm_scale, self.causal, out, lse, self.workspace, self.status_dev)
-        _used_on(self, q, self.workspace, self.out, self.lse, self.dq, self.dk, self.dv)
+            hora_packed_attention(q, k, v, self._seq_offsets, self._group_offsets, self._sm_scale, self._causal, out, lse, self._workspace, self._status_dev)
+        _used_on(self, q, self._workspace, self._out, self._lse, self._dq, self._dk, self._dv)
         return out, lse
 
     def backward(self, q, k, v, out, lse, dout, dq=None, dk=None, dv=None):
         """Returns (dq, dk, dv) for what run was given and returned."""
-        if self.dq is None:
+        if self._dq is None:
             raise ValueError("made without backward=True")
-        dq, dk, dv = self.dq if dq is None else dq, self.dk if dk is None else dk, self.dv if dv is None else dv
-        st = self._strides(q.dtype, (q, out, dout, dq), (k, v, dk, dv)) if lse is self.lse else None
+        dq, dk, dv = self._dq if dq is None else dq, self._dk if dk is None else dk, self._dv if dv is None else dv
+        st = self._strides(q.dtype, (q, out, dout, dq), (k, v, dk, dv)) if lse is self._lse else None
         if st is not None:
-            _check(load().hora_packed_attention_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), self._lse, dout.data_ptr(), self._code, st[0], st[4], st[5],
+            _check(load().hora_packed_attention_backward(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), self._lse_arg, dout.data_ptr(), self._code, st[0], st[4], st[5],
                                                          st[1], st[2], *self._middle, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), st[3], st[6], st[7], *self._tail,
                                                          torch._C._cuda_getCurrentRawStream(self._device)), "hora_packed_attention_backward")
         else:
-            hora_packed_attention_backward(q, k, v, out, lse, dout, self.seq_offsets, self.group_offsets, self.sm_scale, self.causal, dq, dk, dv, self.workspace,
-                                           self.status_dev)
-        _used_on(self, q, self.workspace, self.out, self.lse, self.dq, self.dk, self.dv)
+            hora_packed_attention_backward(q, k, v, out, lse, dout, self._seq_offsets, self._group_offsets, self._sm_scale, self._causal, dq, dk, dv, self._workspace,
+                                           self._status_dev)
+        _used_on(self, q, self._workspace, self._out, self._lse, self._dq, self._dk, self._dv)
         return dq, dk, dv
 
 
