@@ -41,21 +41,30 @@ class rotate(torch.autograd.Function):
 
 
 class attend(torch.autograd.Function):
-    """Attention of the packed tokens, a group's prompt shared by its rollouts."""
+    """Attention of the packed tokens, a group's prompt shared by its rollouts.  Workspaces live for a call; an object that owns the output must not be kept
+    for the backward pass: output, graph and object would hold each other, and their memory."""
 
     @staticmethod
     def forward(ctx, q, k, v, seq_offsets, group_offsets, status):
-        T, Hq, D = q.shape
-        op = hora.PackedAttention(seq_offsets, T, Hq, k.shape[1], D, q.dtype, group_offsets=group_offsets, status_dev=status, backward=True)
-        out, lse = op.run(q, k, v)
-        ctx.op = op
+        out, lse = torch.empty(q.shape, dtype=q.dtype, device=q.device), torch.empty(q.shape[:2], device=q.device)
+        ctx.at = seq_offsets, group_offsets, q.shape[2] ** -0.5, True
+        ctx.status = status
+        hora.hora_packed_attention(q, k, v, *ctx.at, out, lse, attend.workspace(q, k, seq_offsets, False), status)
         ctx.save_for_backward(q, k, v, out, lse)
         return out
 
     @staticmethod
     def backward(ctx, dout):
         q, k, v, out, lse = ctx.saved_tensors
-        return (*ctx.op.backward(q, k, v, out, lse, dout.contiguous()), None, None, None)
+        grads = [torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in (q, k, v)]
+        hora.hora_packed_attention_backward(q, k, v, out, lse, dout.contiguous(), *ctx.at, *grads, attend.workspace(q, k, ctx.at[0], True), ctx.status)
+        return (*grads, None, None, None)
+
+    @staticmethod
+    def workspace(q, k, seq_offsets, backward):
+        T, Hq, D = q.shape
+        need = hora.hora_packed_attention_workspace_bytes(T, seq_offsets.numel() - 1, Hq, k.shape[1], D, backward)
+        return torch.empty(need, dtype=torch.uint8, device=q.device)
 
 
 class Model(torch.nn.Module):
