@@ -6,7 +6,7 @@
 // sequence, or of its group if it is of a prompt.
 //   A tile of queries is tp tokens times hp heads of one cache head's g (hp divides g, hp * tp <= 128): all of them read the same keys.
 // Few tokens to a tile mean that the causal border cuts off little of it, and short sequences fill it.  A plan lists the tiles by
-// falling number of steps; CTAs, one to an SM, deal them out in turn (forwards and backwards, like cards), so none has much more to do.
+// falling number of steps; CTAs, one to an SM, take them from a counter, the longest first, so that none ends much later than the others.
 #pragma once
 
 #include "hora_checked.cuh"

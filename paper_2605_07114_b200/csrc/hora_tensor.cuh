@@ -43,22 +43,6 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
     return false;
 }
 
-// Two of them: asked for together, since an answer takes a hundred cycles and more even where there is nothing to wait for.
-__device__ __forceinline__ void bar_wait_both(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1, volatile int32_t *failed) {
-    uint32_t done;
-    asm volatile(
-        "{\n.reg .pred p, q;\n"
-        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-        "mbarrier.test_wait.parity.shared::cta.b64 q, [%3], %4;\n"
-        "and.pred p, p, q;\nselp.b32 %0, 1, 0, p;\n}"
-        : "=r"(done)
-        : "r"(bar0), "r"(parity0), "r"(bar1), "r"(parity1)
-        : "memory");
-    if (done) return;
-    bar_wait(bar0, parity0, failed);
-    bar_wait(bar1, parity1, failed);
-}
-
 __device__ __forceinline__ void tma_box(uint32_t to, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar) {
     asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to), "l"(map),
                  "r"(x), "r"(y), "r"(bar)
@@ -150,15 +134,6 @@ __device__ __forceinline__ void tmem_store16(uint32_t at, const float (&r)[16]) 
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15};" ::"f"(r[0]), "f"(r[1]),
         "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]),
         "f"(r[14]), "f"(r[15]), "r"(at)
-        : "memory");
-}
-__device__ __forceinline__ void tmem_store32(uint32_t at, const float (&r)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31};" ::"f"(r[0]), "f"(r[1]),
-        "f"(r[2]), "f"(r[3]), "f"(r[4]), "f"(r[5]), "f"(r[6]), "f"(r[7]), "f"(r[8]), "f"(r[9]), "f"(r[10]), "f"(r[11]), "f"(r[12]), "f"(r[13]),
-        "f"(r[14]), "f"(r[15]), "f"(r[16]), "f"(r[17]), "f"(r[18]), "f"(r[19]), "f"(r[20]), "f"(r[21]), "f"(r[22]), "f"(r[23]), "f"(r[24]),
-        "f"(r[25]), "f"(r[26]), "f"(r[27]), "f"(r[28]), "f"(r[29]), "f"(r[30]), "f"(r[31]), "r"(at)
         : "memory");
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
