@@ -121,7 +121,8 @@ __device__ __forceinline__ bool for_items(const PackedArgs &a, const PackedSeque
 // depend on how many more; the list is then left empty.
 template <bool KEYS>
 __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s_groups, int32_t *s_bucket, int32_t *s_warp, bool &bad) {
-    __shared__ int64_t s_sum[kListWarps], s_items[kListWarps];
+    __shared__ int64_t s_sum[kListWarps];
+    __shared__ uint32_t s_items[kListWarps];
     __shared__ int32_t s_next[2];
     const int warp = threadIdx.x >> 5, lane = lane_id();
     const int32_t each = min((int32_t)kWarp, (a.S + kListWarps - 1) / kListWarps);               // sequences of a warp at a time
@@ -133,9 +134,8 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
     int64_t left = cap;
     bool fits = true;
     auto too_many = [&]() {                              // of all warps together, after a barrier; empties the list
-        int64_t all = s_items[lane];
-#pragma unroll
-        for (int d = kWarp / 2; d > 0; d >>= 1) all += __shfl_xor_sync(kFull, all, d);
+        const uint32_t n = s_items[lane];                // 2^31 at most, in two halves whose sums 32 bits hold
+        const int64_t all = ((int64_t)__reduce_add_sync(kFull, n >> 16) << 16) + __reduce_add_sync(kFull, n & 0xFFFFu);
         if (all <= cap) return false;
         if (threadIdx.x == 0) a.counts[KEYS ? 1 : 0] = 0;
         bad = true;
@@ -148,7 +148,7 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
             kept = lane < each ? packed_sequence(a, s_groups, (int32_t)min((int64_t)a.S, base + lane), bad) : PackedSequence{0, 0, 0, 0, 0};
             fits = for_items<true>(a, kept, left, [&](const PackedSequence &s, int32_t i) { mine += item_steps<true>(a, s, i); });
         }
-        if (lane == 0) s_items[warp] = fits ? cap - left : (int64_t)cap + 1;
+        if (lane == 0) s_items[warp] = fits ? (uint32_t)(cap - left) : (uint32_t)cap + 1u;
 #pragma unroll
         for (int d = kWarp / 2; d > 0; d >>= 1) mine += __shfl_xor_sync(kFull, mine, d);
         if (lane == 0) s_sum[warp] = mine;
@@ -171,7 +171,7 @@ __device__ __forceinline__ void list_items(const PackedArgs &a, const int64_t *s
             atomicAdd(s_bucket + bucket_of((steps + parts - 1) / parts), parts);
         });
     }
-    if (!KEYS && lane == 0) s_items[warp] = fits ? cap - left : (int64_t)cap + 1;
+    if (!KEYS && lane == 0) s_items[warp] = fits ? (uint32_t)(cap - left) : (uint32_t)cap + 1u;
     __syncthreads();
     if (!KEYS && too_many()) return;
     static_assert(kListBuckets == kListThreads, "a thread to each bucket");
