@@ -11,6 +11,12 @@ torch = pytest.importorskip("torch")
 DEV, PATTERN, MARGIN = "cuda", 0xA5, 1 << 20
 
 
+@pytest.fixture(autouse=True, scope="module")
+def gigabytes_are_given_back():
+    yield
+    torch.cuda.empty_cache()
+
+
 def guarded(nbytes):
     """A buffer of bytes, and the larger one around it, all of the pattern."""
     around = torch.full((nbytes + 2 * MARGIN,), PATTERN, dtype=torch.uint8, device=DEV)

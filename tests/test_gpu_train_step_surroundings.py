@@ -9,7 +9,7 @@ pytestmark = pytest.mark.gpu
 torch = pytest.importorskip("torch")
 
 import test_gpu_packed_attention as tpa  # noqa: E402
-from test_gpu_packed_overlap import PATTERN, guarded, surroundings_intact  # noqa: E402
+from test_gpu_train_step_overlap import PATTERN, gigabytes_are_given_back, guarded, surroundings_intact  # noqa: E402, F401
 
 DEV, BF, HF = "cuda", torch.bfloat16, torch.float16
 T2 = 2000
