@@ -16,10 +16,10 @@
 // of others among those are cleared in shared memory first, since 0 * NaN is not 0.
 //   The warps of a multiprocessor share its instruction cache, and those that issue the products wait for their instructions longest: the code is
 // kept small (waits that were unrolled, 165 KB in all, cost a quarter of the time).
-//   What bounds it: power for one long document (16381 tokens of 32 heads of 128: 1.75 to 2.15 ms, 1020 to 1250 TFLOP/s); else the chain scores -
+//   What bounds it: power for one long document (16381 tokens of 32 heads of 128: 1.9 to 2.2 ms, 1000 to 1160 TFLOP/s); else the chain scores -
 // maximum - weights - product of its eight softmax warps, 1.3 thousand cycles for 64 keys of both tiles (exponentials alone take 1.0), and
-// the way of the next queries into shared memory (60 prompts up to 509 tokens: 114 us, 0.57 PFLOP/s; 15 groups of 32 rollouts: 1.1 ms,
-// 0.78 PFLOP/s).  64 keys at a time because the next scores are then there when a softmax is through (128 at a time: 137 us for the 60
+// the way of the next queries into shared memory (60 prompts up to 509 tokens: 114 us and 0.57 PFLOP/s where inputs stay from pass to pass, 136 where
+// they change; 15 groups of 32 rollouts: 1.1 ms and 0.78 PFLOP/s, 1.25 to 1.3 ms).  64 keys at a time because the next scores are then there when a softmax is through (128 at a time: 137 us for the 60
 // prompts), although a product of 64 keys takes the tensor cores as long as one of 128.
 //   Every wait has a limit; a wait that reaches it makes the CTA give up and report HORA_ERR_INTERNAL.
 #define HORA_FILE_ID 11

@@ -8,7 +8,9 @@
 // angles are worked out once for all of them, in 64 bits up to the fraction of a turn (a position of 10^5 times a frequency of 1
 // has lost 2^-8 of a radian in 32 bits), the weights are held in registers, and four heads' loads are in flight.
 //   What bounds it: HBM and issue slots, about equally.  Nothing is read twice and nothing but the results is written: 131072 tokens of 20 heads of 128 in
-// bf16 254 us, 5.3 TB/s (0.81 of the copy rate), 50021 tokens of 32 heads and back 396 us, 5.2 TB/s, seven of ten cycles issuing.
+// bf16 254 us, 5.3 TB/s (0.81 of the copy rate) where inputs stay from pass to pass, 272 to 283 where they change; 50021 tokens of 32 heads and back 396
+// and 403 to 420 us, 5.2 TB/s; seven of ten cycles issuing.  The forward kernels of 16-bit types are held to 80 registers, so that three CTAs fit an SM,
+// for which they spill 12 (neighbouring pairs) to 68 bytes a thread; of the backward ones, held to 128, those of fp32 do, 8 to 56.
 #define HORA_FILE_ID 8
 #include "hora_rows16.cuh"
 
